@@ -124,8 +124,9 @@ def _codes(x):
     v[:, :H] = x
     v = v.view(rows, n, GROUP)
     top = v.abs().amax(2, keepdim=True)
-    codes = torch.round(v * torch.where(top > 0, 127.0 / top, 0.0)).clamp(-127, 127)
-    return codes.view(rows, n * GROUP)[:, :H].to(torch.int8).contiguous(), (top / 127.0).view(rows, n)
+    most = torch.full_like(top, 127.0)         # quotients of tensors: those with a plain number go by its reciprocal
+    codes = torch.round(v * torch.where(top > 0, most / top, 0.0)).clamp(-127, 127)
+    return codes.view(rows, n * GROUP)[:, :H].to(torch.int8).contiguous(), (top / most).view(rows, n)
 
 
 def _values(codes, scales):
