@@ -458,6 +458,133 @@ int psgd_orthogonalize(int count, const psgd_matrix *mats, acsc_dtype dt, int r,
 int psgd_decompress(int count, const psgd_matrix *mats, acsc_dtype dt, int r, hipStream_t stream);
 int psgd_step(int count, const psgd_matrix *mats, acsc_dtype dt, int r, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * The feed-forward block between two boundaries: layer norm, fused linear
+ * layers and 8-bit activation checkpoints (Sec. 3.1 and Alg. 1: a stage runs
+ * its layers on the unpacked activation and hands their weight gradients to
+ * the corrector; with many microbatches in flight it is the kept activations
+ * that fill a stage's memory).
+ * ---------------------------------------------------------------------- */
+
+/* Activation functions; gelu is x Phi(x) with the exact normal distribution. */
+typedef enum acsc_act { ACSC_ACT_NONE = 0, ACSC_ACT_RELU = 1, ACSC_ACT_GELU = 2, ACSC_ACT_SILU = 3 } acsc_act;
+
+/* An 8-bit checkpoint of a [rows, H] tensor.  Columns 128 g .. 128 g + 127 of
+ * a row form group g; with a the group's largest magnitude,
+ *   scale = a / 127,   code = rint(x * (127 / a)),   value = code * scale
+ * (each operation rounded once in fp32, ties to even).  A group with
+ * a < 2^-120 is stored as zeros with scale 0; a group that holds an infinity
+ * or a NaN gets scale = NaN, so that every value of it reads as NaN. */
+#define ACSC_Q8_GROUP 128
+typedef struct q8_tensor {
+    int8_t *codes;       /* device [rows, ld_codes], ld_codes >= H                 */
+    float *scales;       /* device [rows, ld_scales], ld_scales >= ceil(H / 128)   */
+    int64_t ld_codes, ld_scales;
+} q8_tensor;
+
+/* q <- checkpoint of x [rows, ld_x] of dt (rows >= 0, 1 <= H <= 2^22). */
+int q8_encode(const void *x, acsc_dtype dt, int64_t rows, int H, int64_t ld_x, const q8_tensor *q,
+              hipStream_t stream);
+
+/* y <- act(value of q), rounded once to dt: a kept tensor (ACSC_ACT_NONE), or
+ * the activation recomputed from its kept argument. */
+int q8_decode(const q8_tensor *q, int64_t rows, int H, acsc_act act, void *y, acsc_dtype dt, int64_t ld_y,
+              hipStream_t stream);
+
+/* Layer norm of the rows of x [rows, ld_x] of dt, 1 <= H <= 32768:
+ *   mu = mean(x), rho = 1 / sqrt(mean((x - mu)^2) + eps),
+ *   y = (x - mu) rho gamma + beta
+ * gamma, beta  device [H] of dt; NULL: ones, zeros.
+ * mean, rstd   device fp32 [rows] or NULL: receive mu and rho (the backward
+ *              pass needs both).
+ * q            NULL, or a checkpoint of x written in the same pass.
+ * y may equal x (with ld_y == ld_x).  eps > 0.  Statistics are fp32, the
+ * variance from centred values. */
+int ln_forward(const void *x, acsc_dtype dt, int64_t rows, int H, int64_t ld_x, const void *gamma,
+               const void *beta, float eps, void *y, int64_t ld_y, float *mean, float *rstd,
+               const q8_tensor *q, hipStream_t stream);
+
+/* y of ln_forward again, from kept statistics and either x or its checkpoint
+ * (exactly one of x and q is not NULL; dt is y's, gamma's and beta's type,
+ * and x's). */
+int ln_recompute(const void *x, int64_t ld_x, const q8_tensor *q, acsc_dtype dt, int64_t rows, int H,
+                 const float *mean, const float *rstd, const void *gamma, const void *beta, void *y,
+                 int64_t ld_y, hipStream_t stream);
+
+/* Bytes of workspace that ln_backward needs. */
+int ln_workspace_size(int64_t rows, int H, size_t *bytes);
+
+/* Gradients of ln_forward, from x or its checkpoint (exactly one of x and q):
+ *   h = (x - mean) rstd,  g = dy gamma,
+ *   dx = rstd (g - mean(g) - h mean(g h)) + add
+ *   dgamma (+)= sum over rows of dy h,   dbeta (+)= sum over rows of dy
+ * add          device [rows, ld_add] of dt or NULL: the gradient that reaches x
+ *              past the norm (the residual branch).  dx may equal dy or add.
+ * dgamma, dbeta  device fp32 [H], each or both NULL; accumulate != 0 adds to
+ *              what they hold (gradients of several microbatches).  Sums are
+ *              taken in a fixed order: the same call gives the same bits.
+ * rows == 0 leaves dx alone and gives zero sums.
+ * ws           256-byte aligned; needed only with dgamma or dbeta. */
+int ln_backward(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, const q8_tensor *q, acsc_dtype dt,
+                int64_t rows, int H, const float *mean, const float *rstd, const void *gamma, const void *add,
+                int64_t ld_add, void *dx, int64_t ld_dx, float *dgamma, float *dbeta, int accumulate, void *ws,
+                size_t ws_bytes, hipStream_t stream);
+
+/* Which product of a linear layer a workspace is for. */
+typedef enum lin_op { LIN_FORWARD = 0, LIN_BACKWARD_INPUT = 1, LIN_BACKWARD_WEIGHT = 2 } lin_op;
+
+/* Bytes of workspace for one product of a linear layer with n_in inputs and
+ * n_out outputs on `rows` tokens, whatever its strides, alignment and
+ * epilogue. */
+int lin_workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, size_t *bytes);
+
+/* One linear layer and what follows it, in one pass over the output:
+ *   z = x W^T + bias;   y = act(z) + residual
+ * x        device [rows, ld_x] of dt (n_in columns);  W device [n_out, ld_w].
+ * bias     device [n_out] of dt or NULL;  residual device [rows, ld_res] of dt
+ *          or NULL (may equal y, with ld_res == ld_y).
+ * y        device [rows, ld_y] of dt; must not overlap x or W.
+ * z        device [rows, ld_z] of dt or NULL: receives the pre-activation.
+ * q        NULL, or a checkpoint of the pre-activation [rows, n_out], coded
+ *          from its fp32 values.
+ * Products accumulate in fp32 and the epilogue works on the fp32 sum; y is
+ * rounded once.  bf16 products run on bf16 matrix cores, fp32 ones on fp32
+ * matrix cores.  Rows are independent: a non-finite value in a row of x
+ * reaches that row of y only.  A product cut along n_in (few tiles) adds its
+ * pieces in a fixed order: the same call gives the same bits.
+ * 1 <= n_in, n_out <= 2^22, 0 <= rows < 2^31. */
+int lin_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t rows, int n_in, int n_out, const void *W,
+                int64_t ld_w, const void *bias, acsc_act act, const void *residual, int64_t ld_res, void *y,
+                int64_t ld_y, void *z, int64_t ld_z, const q8_tensor *q, void *ws, size_t ws_bytes,
+                hipStream_t stream);
+
+/* dz = dy act'(z), from the kept pre-activation (exactly one of z and q is
+ * not NULL).  dz may equal dy.  relu'(0) = 0. */
+int lin_backward_act(const void *dy, int64_t ld_dy, const void *z, int64_t ld_z, const q8_tensor *q, acsc_dtype dt,
+                     int64_t rows, int n_out, acsc_act act, void *dz, int64_t ld_dz, hipStream_t stream);
+
+/* Gradient of the layer's input: dx = dz W.  With act != ACSC_ACT_NONE the
+ * input was act(z) of the layer before, and the gradient of its z is wanted:
+ *   dx = (dz W) act'(z)
+ * from that layer's kept pre-activation (one of z and q; [rows, n_in]). */
+int lin_backward_input(const void *dz, int64_t ld_dz, acsc_dtype dt, int64_t rows, int n_in, int n_out,
+                       const void *W, int64_t ld_w, acsc_act act, const void *z, int64_t ld_z, const q8_tensor *q,
+                       void *dx, int64_t ld_dx, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Gradients of the layer's weights and bias:
+ *   dW (+)= dz^T act(x),   db (+)= sum over rows of dz
+ * x        device [rows, ld_x] of dt, or its checkpoint q (exactly one).  With
+ *          act != ACSC_ACT_NONE it holds the kept pre-activation of the layer
+ *          before; its activation is recomputed inside the call and rounded to
+ *          dt, as that layer's output was.
+ * dW       device [n_out, ld_dw] of dw_dt (the gradient's type: bf16 goes to
+ *          sc_correct as it is, fp32 serves accumulation).
+ * db       device fp32 [n_out] or NULL.
+ * accumulate != 0 adds to what dW and db hold.  rows == 0 gives zero sums. */
+int lin_backward_weight(const void *dz, int64_t ld_dz, const void *x, int64_t ld_x, const q8_tensor *q,
+                        acsc_act act, acsc_dtype dt, int64_t rows, int n_in, int n_out, void *dW, acsc_dtype dw_dt,
+                        int64_t ld_dw, float *db, int accumulate, void *ws, size_t ws_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional
+from typing import NamedTuple, Optional, Union
 
 import torch
 
@@ -61,6 +61,18 @@ class PsgdMatrix(C.Structure):
     _fields_ = [("G", C.c_void_p), ("E", C.c_void_p), ("P", C.c_void_p), ("Q", C.c_void_p),
                 ("out", C.c_void_p), ("m", C.c_int), ("n", C.c_int), ("ws", C.c_void_p),
                 ("ws_bytes", C.c_size_t)]
+
+
+class _Q8Tensor(C.Structure):
+    """q8_tensor: the device arrays of an 8-bit checkpoint."""
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("ld_codes", C.c_int64), ("ld_scales", C.c_int64)]
+
+
+class Q8(NamedTuple):
+    """An 8-bit checkpoint of a [rows, H] tensor: codes int8 [rows, H] and one
+    fp32 scale for each 128 columns of a row, scales [rows, ceil(H / 128)]."""
+    codes: torch.Tensor
+    scales: torch.Tensor
 
 
 def _load():
@@ -118,6 +130,22 @@ def _load():
         fn = getattr(lib, name)
         fn.restype = i32
         fn.argtypes = [i32, C.POINTER(PsgdMatrix), i32, i32, vp]
+    qp = C.POINTER(_Q8Tensor)
+    for name, types in (
+            ("q8_encode", [vp, i32, i64, i32, i64, qp, vp]),
+            ("q8_decode", [qp, i64, i32, i32, vp, i32, i64, vp]),
+            ("ln_forward", [vp, i32, i64, i32, i64, vp, vp, f32, vp, i64, vp, vp, qp, vp]),
+            ("ln_recompute", [vp, i64, qp, i32, i64, i32, vp, vp, vp, vp, vp, i64, vp]),
+            ("ln_workspace_size", [i64, i32, C.POINTER(sz)]),
+            ("ln_backward", [vp, i64, vp, i64, qp, i32, i64, i32, vp, vp, vp, vp, i64, vp, i64, vp, vp, i32, vp, sz, vp]),
+            ("lin_workspace_size", [i32, i64, i32, i32, i32, C.POINTER(sz)]),
+            ("lin_forward", [vp, i64, i32, i64, i32, i32, vp, i64, vp, i32, vp, i64, vp, i64, vp, i64, qp, vp, sz, vp]),
+            ("lin_backward_act", [vp, i64, vp, i64, qp, i32, i64, i32, i32, vp, i64, vp]),
+            ("lin_backward_input", [vp, i64, i32, i64, i32, i32, vp, i64, i32, vp, i64, qp, vp, i64, vp, sz, vp]),
+            ("lin_backward_weight", [vp, i64, vp, i64, qp, i32, i32, i64, i32, i32, vp, i32, i64, vp, i32, vp, sz, vp])):
+        fn = getattr(lib, name)
+        fn.restype = i32
+        fn.argtypes = types
     lib.acsc_stats_enable.restype = i32
     lib.acsc_stats_enable.argtypes = [i32]
     lib.acsc_stats_only.restype = i32
@@ -136,7 +164,9 @@ EXPORTED = ("acsc_last_error", "acsc_version", "acsc_stats_enable", "acsc_stats_
             "sc_build_subspace_batched", "sc_build_ritz_batched", "sc_build_status",
             "sc_adamw_workspace_size", "sc_correct_adamw_batched",
             "ac_bern_mask", "ac_bern_pack", "ac_bern_unpack",
-            "psgd_workspace_size", "psgd_project", "psgd_orthogonalize", "psgd_decompress", "psgd_step")
+            "psgd_workspace_size", "psgd_project", "psgd_orthogonalize", "psgd_decompress", "psgd_step",
+            "q8_encode", "q8_decode", "ln_forward", "ln_recompute", "ln_workspace_size", "ln_backward",
+            "lin_workspace_size", "lin_forward", "lin_backward_act", "lin_backward_input", "lin_backward_weight")
 
 
 def _check(rc: int):
@@ -592,3 +622,256 @@ def psgd_decompress(items, r: int, dtype: torch.dtype = torch.bfloat16, stream=N
 def psgd_step(items, r: int, dtype: torch.dtype = torch.bfloat16, stream=None):
     """The three phases on one worker (items: dicts with G, E, P, Q, out, ws)."""
     _psgd("psgd_step", items, r, dtype, stream)
+
+
+Q8_GROUP = 128
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+LIN_FORWARD, LIN_BACKWARD_INPUT, LIN_BACKWARD_WEIGHT = 0, 1, 2
+
+
+def _act(act: str) -> int:
+    if act not in ACTS:
+        raise AcscError(ACSC_EINVAL, f"unknown activation {act!r}: one of {', '.join(ACTS)}")
+    return ACTS[act]
+
+
+def _rows(t: torch.Tensor, shape, dtype: torch.dtype, name: str) -> int:
+    """The row stride of a [rows, cols] tensor with unit column stride."""
+    _need_cuda(t)
+    if t.dim() != 2 or tuple(t.shape) != tuple(shape) or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise AcscError(ACSC_EINVAL, f"{name} must be {list(shape)} with unit column stride")
+    if t.dtype != dtype:
+        raise AcscError(ACSC_EDTYPE, f"{name} must be {dtype}, not {t.dtype}")
+    # the stride of a single row, or of none, means nothing
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _vec(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, name: str) -> None:
+    if t is None:
+        return
+    _need_cuda(t)
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise AcscError(ACSC_EINVAL, f"{name} must be [{n}] and contiguous")
+    if t.dtype != dtype:
+        raise AcscError(ACSC_EDTYPE, f"{name} must be {dtype}, not {t.dtype}")
+
+
+def _two_d(t: torch.Tensor, name: str):
+    if t.dim() != 2:
+        raise AcscError(ACSC_EINVAL, f"{name} must be 2-D")
+    return t.shape
+
+
+def _q8_new(rows: int, H: int, device) -> Q8:
+    return Q8(torch.empty(rows, H, dtype=torch.int8, device=device),
+              torch.empty(rows, -(-H // Q8_GROUP), dtype=torch.float32, device=device))
+
+
+def _q8_ref(q: Optional[Q8], rows: int, H: int):
+    if q is None:
+        return None
+    ldc = _rows(q.codes, (rows, H), torch.int8, "codes")
+    lds = _rows(q.scales, (rows, -(-H // Q8_GROUP)), torch.float32, "scales")
+    return C.byref(_Q8Tensor(_p(q.codes), _p(q.scales), ldc, lds))
+
+
+def _kept(src: Union[torch.Tensor, Q8, None], shape, dtype: torch.dtype, name: str):
+    """(pointer, row stride, checkpoint) of a tensor or its checkpoint."""
+    if src is None:
+        return None, 0, None
+    if isinstance(src, Q8):
+        return None, 0, _q8_ref(src, *shape)
+    ld = _rows(src, shape, dtype, name)
+    return _ptr(src), ld, None
+
+
+def _ws(nbytes: int, ws: Optional[torch.Tensor], device, stream):
+    if ws is None and nbytes:
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        if stream is not None:
+            ws.record_stream(stream)   # freed here, perhaps before that stream has used it
+    return _ptr(ws), (ws.numel() * ws.element_size() if ws is not None else 0), ws
+
+
+def q8_encode(x: torch.Tensor, q: Optional[Q8] = None, stream=None) -> Q8:
+    """The 8-bit checkpoint of x [rows, H] (row stride x.stride(0))."""
+    rows, H = _two_d(x, "x")
+    dt, ld = _dt(x), _rows(x, x.shape, x.dtype, "x")
+    if q is None:
+        q = _q8_new(rows, H, x.device)
+    _check(lib.q8_encode(_ptr(x), dt, rows, H, ld, _q8_ref(q, rows, H), _stream(stream)))
+    return q
+
+
+def q8_decode(q: Q8, dtype: torch.dtype, act: str = "none", y: Optional[torch.Tensor] = None,
+              stream=None) -> torch.Tensor:
+    """act(values of q) [rows, H], rounded once to dtype."""
+    rows, H = _two_d(q.codes, "codes")
+    if y is None:
+        y = torch.empty(rows, H, dtype=dtype, device=q.codes.device)
+    ld = _rows(y, (rows, H), dtype, "y")
+    _check(lib.q8_decode(_q8_ref(q, rows, H), rows, H, _act(act), _ptr(y), _dt(y), ld, _stream(stream)))
+    return y
+
+
+def ln_forward(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+               eps: float = 1e-5, checkpoint: bool = False, y: Optional[torch.Tensor] = None, stream=None):
+    """Layer norm of the rows of x [rows, H]: (y, mean [rows], rstd [rows], q),
+    q the 8-bit checkpoint of x if asked for, else None."""
+    rows, H = _two_d(x, "x")
+    dt, ld = _dt(x), _rows(x, x.shape, x.dtype, "x")
+    _vec(gamma, H, x.dtype, "gamma")
+    _vec(beta, H, x.dtype, "beta")
+    if y is None:
+        y = torch.empty(rows, H, dtype=x.dtype, device=x.device)
+    ldy = _rows(y, x.shape, x.dtype, "y")
+    mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+    rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+    q = _q8_new(rows, H, x.device) if checkpoint else None
+    _check(lib.ln_forward(_ptr(x), dt, rows, H, ld, _ptr(gamma), _ptr(beta), float(eps), _ptr(y), ldy, _ptr(mean),
+                          _ptr(rstd), _q8_ref(q, rows, H), _stream(stream)))
+    return y, mean, rstd, q
+
+
+def ln_recompute(src: Union[torch.Tensor, Q8], mean: torch.Tensor, rstd: torch.Tensor,
+                 gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+                 dtype: torch.dtype = torch.bfloat16, y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """ln_forward's y again from x or its checkpoint and the kept statistics."""
+    rows, H = _two_d(src.codes if isinstance(src, Q8) else src, "src")
+    p, ld, q = _kept(src, (rows, H), dtype, "src")
+    for t, n, d, name in ((mean, rows, torch.float32, "mean"), (rstd, rows, torch.float32, "rstd"),
+                          (gamma, H, dtype, "gamma"), (beta, H, dtype, "beta")):
+        _vec(t, n, d, name)
+    if y is None:
+        y = torch.empty(rows, H, dtype=dtype, device=mean.device)
+    ldy = _rows(y, (rows, H), dtype, "y")
+    _check(lib.ln_recompute(p, ld, q, _dt(y), rows, H, _ptr(mean), _ptr(rstd), _ptr(gamma), _ptr(beta), _ptr(y), ldy,
+                            _stream(stream)))
+    return y
+
+
+def ln_workspace_size(rows: int, H: int) -> int:
+    b = C.c_size_t(0)
+    _check(lib.ln_workspace_size(rows, H, C.byref(b)))
+    return b.value
+
+
+def ln_backward(dy: torch.Tensor, src: Union[torch.Tensor, Q8], mean: torch.Tensor, rstd: torch.Tensor,
+                gamma: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None,
+                dx: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None,
+                dbeta: Optional[torch.Tensor] = None, accumulate: bool = False, ws: Optional[torch.Tensor] = None,
+                stream=None):
+    """(dx, dgamma, dbeta) of ln_forward from x or its checkpoint; add: the
+    gradient that reaches x past the norm.  dgamma, dbeta: fp32 [H]; with
+    accumulate they are given and added to."""
+    rows, H = _two_d(dy, "dy")
+    dt, lddy = _dt(dy), _rows(dy, dy.shape, dy.dtype, "dy")
+    p, ld, q = _kept(src, (rows, H), dy.dtype, "src")
+    ldadd = _rows(add, dy.shape, dy.dtype, "add") if add is not None else 0
+    if accumulate and (dgamma is None or dbeta is None):
+        raise AcscError(ACSC_EINVAL, "accumulate needs dgamma and dbeta")
+    if dx is None:
+        dx = torch.empty(rows, H, dtype=dy.dtype, device=dy.device)
+    if dgamma is None:
+        dgamma = torch.empty(H, dtype=torch.float32, device=dy.device)
+    if dbeta is None:
+        dbeta = torch.empty(H, dtype=torch.float32, device=dy.device)
+    for t, n, d, name in ((mean, rows, torch.float32, "mean"), (rstd, rows, torch.float32, "rstd"),
+                          (gamma, H, dy.dtype, "gamma"), (dgamma, H, torch.float32, "dgamma"),
+                          (dbeta, H, torch.float32, "dbeta")):
+        _vec(t, n, d, name)
+    lddx = _rows(dx, dy.shape, dy.dtype, "dx")
+    wp, wn, keep = _ws(ln_workspace_size(rows, H), ws, dy.device, stream)
+    _check(lib.ln_backward(_ptr(dy), lddy, p, ld, q, dt, rows, H, _ptr(mean), _ptr(rstd), _ptr(gamma), _ptr(add), ldadd,
+                           _ptr(dx), lddx, _ptr(dgamma), _ptr(dbeta), int(accumulate), wp, wn, _stream(stream)))
+    return dx, dgamma, dbeta
+
+
+def lin_workspace_size(op: int, rows: int, n_in: int, n_out: int, dtype: torch.dtype) -> int:
+    """Bytes for one product (LIN_FORWARD, LIN_BACKWARD_INPUT, LIN_BACKWARD_WEIGHT) of a linear layer."""
+    b = C.c_size_t(0)
+    code = BF16 if dtype == torch.bfloat16 else F32
+    _check(lib.lin_workspace_size(op, rows, n_in, n_out, code, C.byref(b)))
+    return b.value
+
+
+def lin_forward(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
+                residual: Optional[torch.Tensor] = None, keep: Optional[str] = None, y: Optional[torch.Tensor] = None,
+                ws: Optional[torch.Tensor] = None, stream=None):
+    """y = act(x W^T + bias) + residual for x [rows, n_in], W [n_out, n_in]:
+    (y, kept), kept the pre-activation if keep is "z", its 8-bit checkpoint if
+    keep is "q8", else None."""
+    rows, n_in = _two_d(x, "x")
+    n_out = _two_d(W, "W")[0]
+    dt, ldx, ldw = _dt(x), _rows(x, x.shape, x.dtype, "x"), _rows(W, (n_out, n_in), x.dtype, "W")
+    _vec(bias, n_out, x.dtype, "bias")
+    shape = (rows, n_out)
+    ldr = _rows(residual, shape, x.dtype, "residual") if residual is not None else 0
+    if y is None:
+        y = torch.empty(shape, dtype=x.dtype, device=x.device)
+    ldy = _rows(y, shape, x.dtype, "y")
+    if keep not in (None, "z", "q8"):
+        raise AcscError(ACSC_EINVAL, f"keep must be None, 'z' or 'q8', not {keep!r}")
+    z = torch.empty(shape, dtype=x.dtype, device=x.device) if keep == "z" else None
+    q = _q8_new(rows, n_out, x.device) if keep == "q8" else None
+    wp, wn, hold = _ws(lin_workspace_size(LIN_FORWARD, rows, n_in, n_out, x.dtype), ws, x.device, stream)
+    _check(lib.lin_forward(_ptr(x), ldx, dt, rows, n_in, n_out, _ptr(W), ldw, _ptr(bias), _act(act), _ptr(residual), ldr,
+                           _ptr(y), ldy, _ptr(z), n_out, _q8_ref(q, rows, n_out), wp, wn, _stream(stream)))
+    return y, (z if q is None else q)
+
+
+def lin_backward_act(dy: torch.Tensor, z: Union[torch.Tensor, Q8], act: str, dz: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
+    """dz = dy act'(z) from the kept pre-activation or its checkpoint."""
+    rows, n = _two_d(dy, "dy")
+    ld = _rows(dy, dy.shape, dy.dtype, "dy")
+    p, ldz, q = _kept(z, (rows, n), dy.dtype, "z")
+    if dz is None:
+        dz = torch.empty(rows, n, dtype=dy.dtype, device=dy.device)
+    lddz = _rows(dz, dy.shape, dy.dtype, "dz")
+    _check(lib.lin_backward_act(_ptr(dy), ld, p, ldz, q, _dt(dy), rows, n, _act(act), _ptr(dz), lddz, _stream(stream)))
+    return dz
+
+
+def lin_backward_input(dz: torch.Tensor, W: torch.Tensor, act: str = "none",
+                       z: Union[torch.Tensor, Q8, None] = None, dx: Optional[torch.Tensor] = None,
+                       ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """dx = dz W; with act, (dz W) act'(z) from the pre-activation z [rows,
+    n_in] that the layer before kept, or its checkpoint."""
+    rows, n_out = _two_d(dz, "dz")
+    n_in = _two_d(W, "W")[1]
+    lddz, ldw = _rows(dz, dz.shape, dz.dtype, "dz"), _rows(W, (n_out, n_in), dz.dtype, "W")
+    p, ldz, q = _kept(z, (rows, n_in), dz.dtype, "z")
+    if dx is None:
+        dx = torch.empty(rows, n_in, dtype=dz.dtype, device=dz.device)
+    lddx = _rows(dx, (rows, n_in), dz.dtype, "dx")
+    wp, wn, hold = _ws(lin_workspace_size(LIN_BACKWARD_INPUT, rows, n_in, n_out, dz.dtype), ws, dz.device, stream)
+    _check(lib.lin_backward_input(_ptr(dz), lddz, _dt(dz), rows, n_in, n_out, _ptr(W), ldw, _act(act), p, ldz, q, _ptr(dx),
+                                  lddx, wp, wn, _stream(stream)))
+    return dx
+
+
+def lin_backward_weight(dz: torch.Tensor, x: Union[torch.Tensor, Q8], act: str = "none",
+                        dw_dtype: Optional[torch.dtype] = None, bias: bool = True, dW: Optional[torch.Tensor] = None,
+                        db: Optional[torch.Tensor] = None, accumulate: bool = False, ws: Optional[torch.Tensor] = None,
+                        stream=None):
+    """(dW [n_out, n_in] of dw_dtype (dz's by default), db fp32 [n_out] or None)
+    from dz [rows, n_out] and the layer's input act(x), x [rows, n_in] or its
+    checkpoint.  With accumulate, dW (and db, unless bias is False) are given
+    and added to."""
+    rows, n_out = _two_d(dz, "dz")
+    n_in = _two_d(x.codes if isinstance(x, Q8) else x, "x")[1]
+    lddz = _rows(dz, dz.shape, dz.dtype, "dz")
+    p, ldx, q = _kept(x, (rows, n_in), dz.dtype, "x")
+    if accumulate and (dW is None or (bias and db is None)):
+        raise AcscError(ACSC_EINVAL, "accumulate needs dW and db")
+    if dW is None:
+        dW = torch.empty(n_out, n_in, dtype=dw_dtype or dz.dtype, device=dz.device)
+    if db is None and bias:
+        db = torch.empty(n_out, dtype=torch.float32, device=dz.device)
+    _vec(db, n_out, torch.float32, "db")
+    lddw = _rows(dW, (n_out, n_in), dw_dtype or dW.dtype, "dW")
+    wp, wn, hold = _ws(lin_workspace_size(LIN_BACKWARD_WEIGHT, rows, n_in, n_out, dz.dtype), ws, dz.device, stream)
+    _check(lib.lin_backward_weight(_ptr(dz), lddz, p, ldx, q, _act(act), _dt(dz), rows, n_in, n_out, _ptr(dW), _dt(dW), lddw,
+                                   _ptr(db), int(accumulate), wp, wn, _stream(stream)))
+    return dW, db

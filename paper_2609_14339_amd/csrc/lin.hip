@@ -1,0 +1,550 @@
+// Linear layers: the entry points, the fp32 product, and the kernels that add
+// the pieces of a product cut along its sum.
+#include "lin.h"
+
+namespace acsc {
+
+int q8_decode_run(const Q8 &q, int64_t rows, int H, int act, void *y, acsc_dtype dt, int64_t ldy, hipStream_t st);
+
+namespace {
+
+constexpr int kTile = 128, kBK = 32;
+
+// The fp32 product on v_mfma_f32_16x16x4_f32: 128 x 128 tiles, four waves of
+// 32 rows by 128 columns, so that a wave holds whole checkpoint groups.  The
+// matrix instruction's first operand is B's side, which puts four consecutive
+// columns of one row in a lane.  Tiles go through registers into LDS as they
+// are stored (rows padded to 36, or k-lines to 132 floats: fragment reads are
+// free of bank conflicts in both), the next step's loads in flight while one
+// is multiplied; any alignment, edges read as zeros.
+template <typename T, bool COL>
+struct Stage {
+    static constexpr int kPitch = COL ? kTile + 4 : kBK + 4;
+    static constexpr int kFloats = COL ? kBK * kPitch : kTile * kPitch;
+    float r[4][4];
+    __device__ __forceinline__ void load(const Operand &o, int64_t i0, int64_t ni, int k0, int kend)
+    {
+        const T *p = static_cast<const T *>(o.p);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            if (COL) {
+                const int k = k0 + (threadIdx.x >> 5) + 8 * s;
+                const int64_t i = i0 + (threadIdx.x & 31) * 4;
+                load4(p + static_cast<int64_t>(k) * o.ld + i, k < kend ? static_cast<int>(min<int64_t>(ni - i, 4)) : 0, r[s]);
+            } else {
+                const int k = k0 + (threadIdx.x & 7) * 4;
+                const int64_t i = i0 + (threadIdx.x >> 3) + 32 * s;
+                load4(p + i * o.ld + k, i < ni ? kend - k : 0, r[s]);
+            }
+        }
+    }
+    __device__ __forceinline__ void put(float *lds) const
+    {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int a = COL ? ((threadIdx.x >> 5) + 8 * s) * kPitch + (threadIdx.x & 31) * 4
+                              : ((threadIdx.x >> 3) + 32 * s) * kPitch + (threadIdx.x & 7) * 4;
+            *reinterpret_cast<f32x4 *>(lds + a) = f32x4{r[s][0], r[s][1], r[s][2], r[s][3]};
+        }
+    }
+    // element e: k = kk * 16 + 4 (lane / 16) + e of line i (+ lane % 16)
+    static __device__ __forceinline__ f32x4 frag(const float *lds, int i, int kk)
+    {
+        const int lane = threadIdx.x & 63, line = i + (lane & 15), k = kk * 16 + (lane >> 4) * 4;
+        if (COL)
+            return f32x4{lds[k * kPitch + line], lds[(k + 1) * kPitch + line], lds[(k + 2) * kPitch + line],
+                         lds[(k + 3) * kPitch + line]};
+        return *reinterpret_cast<const f32x4 *>(lds + line * kPitch + k);
+    }
+};
+
+template <typename T, bool ACOL, bool BCOL, int KIND, typename TO>
+__global__ __launch_bounds__(256) void lin_f32_kernel(Gemm g)
+{
+    __shared__ __align__(16) float As[Stage<T, ACOL>::kFloats];
+    __shared__ __align__(16) float Bs[Stage<T, BCOL>::kFloats];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int tile = blockIdx.x, split = blockIdx.y;
+    const int64_t m0 = static_cast<int64_t>(tile / g.tn) * kTile;
+    const int n0 = tile % g.tn * kTile;
+    const int kbeg = split * g.kchunk, kend = min(g.K, kbeg + g.kchunk);
+    const bool sums = KIND == kWeight && g.dbpart && n0 == 0;
+    f32x4 acc[2][8], dacc[2];
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+        dacc[a] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            acc[a][j] = f32x4{0, 0, 0, 0};
+    }
+    Stage<T, ACOL> sa;
+    Stage<T, BCOL> sb;
+    sa.load(g.A, m0, g.M, kbeg, kend);
+    sb.load(g.B, n0, g.N, kbeg, kend);
+    for (int k0 = kbeg; k0 < kend; k0 += kBK) {
+        sa.put(As);
+        sb.put(Bs);
+        __syncthreads();
+        if (k0 + kBK < kend) {
+            sa.load(g.A, m0, g.M, k0 + kBK, kend);
+            sb.load(g.B, n0, g.N, k0 + kBK, kend);
+        }
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            f32x4 fa[2], fb[8];
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+                fa[a] = Stage<T, ACOL>::frag(As, wave * 32 + a * 16, kk);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                fb[j] = Stage<T, BCOL>::frag(Bs, j * 16, kk);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        acc[a][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j][e], fa[a][e], acc[a][j], 0, 0, 0);
+            if (sums)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int a = 0; a < 2; ++a)
+                        dacc[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(1.f, fa[a][e], dacc[a], 0, 0, 0);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+        const int64_t m = m0 + wave * 32 + a * 16 + (lane & 15);
+        const int n = n0 + (lane >> 4) * 4;
+        if (sums && lane < 16 && m < g.M)
+            g.dbpart[split * g.M + m] = dacc[a][0];
+        float v[8][4];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[j][i] = acc[a][j][i];
+        if (g.splits > 1) {
+            if (m < g.M)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    store4(g.part + (split * g.M + m) * g.ldp + n + 16 * j, g.N - n - 16 * j, v[j]);
+        } else {
+            epilogue<TO, KIND, 8>(g.e, v, m < g.M, m, n, g.N);
+        }
+    }
+}
+
+// Adds the pieces of a cut product in order and takes the sum through the
+// epilogue: four columns a thread, 1024 columns of a row a workgroup.
+template <int KIND, typename TO>
+__global__ __launch_bounds__(256) void lin_join_kernel(Gemm g)
+{
+    const int64_t m = blockIdx.y;
+    const int n = (blockIdx.x * 256 + threadIdx.x) * 4;
+    float v[1][4] = {{0.f, 0.f, 0.f, 0.f}};
+    if (n < g.N) {
+        const f32x4 *p = reinterpret_cast<const f32x4 *>(g.part + m * g.ldp + n);
+        const int64_t step = g.M * g.ldp / 4;
+        f32x4 s = p[0];
+        for (int i = 1; i < g.splits; ++i)
+            s += p[i * step];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[0][i] = s[i];
+    }
+    epilogue<TO, KIND, 1>(g.e, v, n < g.N, m, n, g.N);
+}
+
+__global__ __launch_bounds__(256) void lin_join_db_kernel(const float *part, int64_t M, int splits, float *db, int accumulate)
+{
+    const int64_t m = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (m >= M)
+        return;
+    float s = 0.f;
+    for (int i = 0; i < splits; ++i)
+        s += part[i * M + m];
+    db[m] = accumulate ? db[m] + s : s;
+}
+
+// rows == 0: the weight gradients are sums over nothing.
+template <typename TO>
+__global__ __launch_bounds__(256) void lin_zero_kernel(TO *y, int64_t ldy, int64_t M, int N)
+{
+    const int n = blockIdx.x * 256 + threadIdx.x;
+    if (n < N)
+        for (int64_t m = blockIdx.y; m < M; m += gridDim.y)
+            y[m * ldy + n] = 0;
+}
+
+// dz = dy act'(z), eight columns a lane.
+template <typename T>
+__global__ __launch_bounds__(256) void lin_act_kernel(const T *dy, int64_t lddy, const T *z, int64_t ldz, Q8 q, int64_t rows,
+                                                      int N, int act, T *dz, int64_t lddz)
+{
+    const int chunks = (N + 7) / 8;
+    const int64_t total = rows * chunks;
+    for (int64_t w = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; w < total; w += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t row = w / chunks;
+        const int col = static_cast<int>(w - row * chunks) * 8;
+        float g[8], v[8];
+        load8(dy + row * lddy + col, N - col, g);
+        if (q.codes)
+            load_codes(q.codes + row * q.ldc + col, N - col, q.scales[row * q.lds + col / kGroup], v);
+        else
+            load8(z + row * ldz + col, N - col, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            g[i] *= act_slope(v[i], act);
+        store8(dz + row * lddz + col, N - col, g);
+    }
+}
+
+// act(x) of a whole operand, eight columns a lane.
+template <typename T>
+__global__ __launch_bounds__(256) void lin_apply_kernel(const T *x, int64_t ldx, int64_t rows, int N, int act, T *y, int64_t ldy)
+{
+    const int chunks = (N + 7) / 8;
+    const int64_t total = rows * chunks;
+    for (int64_t w = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; w < total; w += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t row = w / chunks;
+        const int col = static_cast<int>(w - row * chunks) * 8;
+        float v[8];
+        load8(x + row * ldx + col, N - col, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = act_value(v[i], act);
+        store8(y + row * ldy + col, N - col, v);
+    }
+}
+
+inline size_t up256(size_t b) { return (b + 255) / 256 * 256; }
+
+// How a product is cut, and what of the workspace it takes.
+struct Plan {
+    int tm, tn, splits, kchunk;
+    int64_t ldp;
+    size_t part, db;     // bytes of the pieces, and of db's
+    size_t bytes() const { return part + db; }
+};
+
+inline Plan plan_of(int64_t M, int N, int K, bool weight)
+{
+    Plan p{};
+    p.tm = static_cast<int>((M + kTile - 1) / kTile);
+    p.tn = (N + kTile - 1) / kTile;
+    const int64_t tiles = static_cast<int64_t>(p.tm) * p.tn;
+    const int steps = (K + kBK - 1) / kBK;
+    int s = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(tiles, 1), steps / 4)));
+    const int per = (steps + s - 1) / s;
+    p.splits = (steps + per - 1) / per;
+    p.kchunk = per * kBK;
+    p.ldp = (N + 3) / 4 * 4;
+    p.part = p.splits > 1 ? up256(static_cast<size_t>(p.splits) * M * p.ldp * 4) : 0;
+    p.db = weight ? up256(static_cast<size_t>(p.splits) * M * 4) : 0;
+    return p;
+}
+
+template <bool ACOL, bool BCOL, int KIND, typename T, typename TO>
+int run_product(Gemm &g, const Plan &p, char *ws, float *db, hipStream_t st, const char *tag)
+{
+    g.tm = p.tm;
+    g.tn = p.tn;
+    g.splits = p.splits;
+    g.kchunk = p.kchunk;
+    g.ldp = p.ldp;
+    g.part = reinterpret_cast<float *>(ws);
+    g.dbpart = db ? reinterpret_cast<float *>(ws + p.part) : nullptr;
+    ACSC_LAUNCH(tag, (lin_f32_kernel<T, ACOL, BCOL, KIND, TO>), dim3(p.tm * p.tn, p.splits), dim3(256), 0, st, g);
+    if (int rc = check_launch(tag))
+        return rc;
+    if (p.splits > 1) {
+        ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO>), dim3((g.N + 1023) / 1024, static_cast<unsigned>(g.M)), dim3(256),
+                    0, st, g);
+        if (int rc = check_launch("lin_join"))
+            return rc;
+    }
+    if (db) {
+        ACSC_LAUNCH("lin_join_db", lin_join_db_kernel, dim3(static_cast<unsigned>((g.M + 255) / 256)), dim3(256), 0, st,
+                    g.dbpart, g.M, p.splits, db, g.e.accumulate);
+        return check_launch("lin_join_db");
+    }
+    return ACSC_OK;
+}
+
+inline int check_layer(int64_t rows, int n_in, int n_out, int dt)
+{
+    ACSC_CHECK_ARG(dt == ACSC_F32 || dt == ACSC_BF16, ACSC_EDTYPE, "unknown dtype %d", dt);
+    ACSC_CHECK_ARG(rows >= 0 && rows < (1ll << 31), ACSC_EINVAL, "rows=%lld outside [0, 2^31)", (long long)rows);
+    ACSC_CHECK_ARG(n_in >= 1 && n_in <= (1 << 22), ACSC_EINVAL, "n_in=%d outside [1, 2^22]", n_in);
+    ACSC_CHECK_ARG(n_out >= 1 && n_out <= (1 << 22), ACSC_EINVAL, "n_out=%d outside [1, 2^22]", n_out);
+    return ACSC_OK;
+}
+
+inline int check_mat(const void *p, bool need, int64_t ld, int cols, int dt, const char *name)
+{
+    ACSC_CHECK_ARG(!need || p, ACSC_EINVAL, "null pointer %s", name);
+    ACSC_CHECK_ARG(ld >= cols && ld < (1ll << 40), ACSC_EINVAL, "ld of %s is %lld for %d columns", name, (long long)ld, cols);
+    ACSC_CHECK_ARG(aligned(p, dtype_size(static_cast<acsc_dtype>(dt))), ACSC_EALIGN, "%s not aligned to its elements",
+                   name);
+    return ACSC_OK;
+}
+
+// A kept pre-activation: one of z and q.
+inline int check_kept(const void *z, int64_t ldz, const q8_tensor *q, int64_t rows, int cols, int dt)
+{
+    ACSC_CHECK_ARG(rows == 0 || (z != nullptr) != (q != nullptr), ACSC_EINVAL, "exactly one of the tensor and its checkpoint is needed");
+    if (z)
+        return check_mat(z, true, ldz, cols, dt, "z");
+    return q ? check_q8(q, rows, cols) : ACSC_OK;
+}
+
+inline int check_ws(const void *ws, size_t have, size_t need)
+{
+    if (need == 0)
+        return ACSC_OK;
+    ACSC_CHECK_ARG(ws, ACSC_EINVAL, "null workspace");
+    ACSC_CHECK_ARG(aligned(ws, 256), ACSC_EALIGN, "workspace not 256-byte aligned");
+    ACSC_CHECK_ARG(have >= need, ACSC_ENOSPC, "workspace of %zu bytes, %zu needed", have, need);
+    return ACSC_OK;
+}
+
+// The largest tile grid: blockIdx.x is 32 bits.
+inline int check_tiles(const Plan &p)
+{
+    ACSC_CHECK_ARG(static_cast<int64_t>(p.tm) * p.tn < (1ll << 31), ACSC_EINVAL, "product too large");
+    return ACSC_OK;
+}
+
+// Bytes of an activation recomputed for the weight gradient.
+inline size_t recomputed_bytes(int64_t rows, int n_in, acsc_dtype dt)
+{
+    return up256(static_cast<size_t>(rows) * ((n_in + 7) / 8 * 8) * dtype_size(dt));
+}
+
+}  // namespace
+}  // namespace acsc
+
+using namespace acsc;
+
+extern "C" int lin_workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, size_t *bytes)
+{
+    clear_error();
+    if (int rc = check_layer(rows, n_in, n_out, dt))
+        return rc;
+    ACSC_CHECK_ARG(bytes, ACSC_EINVAL, "null pointer bytes");
+    ACSC_CHECK_ARG(op == LIN_FORWARD || op == LIN_BACKWARD_INPUT || op == LIN_BACKWARD_WEIGHT, ACSC_EINVAL,
+                   "unknown product %d", (int)op);
+    if (rows == 0)
+        *bytes = 0;
+    else if (op == LIN_FORWARD)
+        *bytes = plan_of(rows, n_out, n_in, false).bytes();
+    else if (op == LIN_BACKWARD_INPUT)
+        *bytes = plan_of(rows, n_in, n_out, false).bytes();
+    else
+        *bytes = plan_of(n_out, n_in, static_cast<int>(rows), true).bytes() + recomputed_bytes(rows, n_in, dt);
+    return ACSC_OK;
+}
+
+extern "C" int lin_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t rows, int n_in, int n_out, const void *W,
+                           int64_t ld_w, const void *bias, acsc_act act, const void *residual, int64_t ld_res, void *y,
+                           int64_t ld_y, void *z, int64_t ld_z, const q8_tensor *q, void *ws, size_t ws_bytes,
+                           hipStream_t stream)
+{
+    clear_error();
+    if (int rc = check_layer(rows, n_in, n_out, dt))
+        return rc;
+    if (int rc = check_act(act))
+        return rc;
+    const bool some = rows > 0;
+    if (int rc = check_mat(x, some, ld_x, n_in, dt, "x"))
+        return rc;
+    if (int rc = check_mat(W, some, ld_w, n_in, dt, "W"))
+        return rc;
+    if (int rc = check_mat(y, some, ld_y, n_out, dt, "y"))
+        return rc;
+    ACSC_CHECK_ARG(aligned(bias, dtype_size(dt)), ACSC_EALIGN, "bias not aligned to its elements");
+    if (residual)
+        if (int rc = check_mat(residual, some, ld_res, n_out, dt, "residual"))
+            return rc;
+    ACSC_CHECK_ARG(residual != y || !some || ld_res == ld_y, ACSC_EINVAL, "y in place of the residual needs ld_y == ld_res");
+    ACSC_CHECK_ARG(!some || (y != x && y != W && y != z), ACSC_EINVAL, "y must not overlap x, W or z");
+    if (z)
+        if (int rc = check_mat(z, some, ld_z, n_out, dt, "z"))
+            return rc;
+    if (q)
+        if (int rc = check_q8(q, rows, n_out))
+            return rc;
+    const Plan p = plan_of(rows, n_out, n_in, false);
+    if (int rc = check_tiles(p))
+        return rc;
+    if (some)
+        if (int rc = check_ws(ws, ws_bytes, p.bytes()))
+            return rc;
+    if (!some)
+        return ACSC_OK;
+    Gemm g{};
+    g.A = {x, ld_x};
+    g.B = {W, ld_w};
+    g.M = rows;
+    g.N = n_out;
+    g.K = n_in;
+    g.e = Epi{y, ld_y, bias, residual, ld_res, z, ld_z, q8_of(q), act, 0};
+    char *w = static_cast<char *>(ws);
+    if (dt == ACSC_BF16)
+        return run_product<false, false, kForward, uint16_t, uint16_t>(g, p, w, nullptr, stream, "lin_forward");
+    return run_product<false, false, kForward, float, float>(g, p, w, nullptr, stream, "lin_forward");
+}
+
+extern "C" int lin_backward_act(const void *dy, int64_t ld_dy, const void *z, int64_t ld_z, const q8_tensor *q,
+                                acsc_dtype dt, int64_t rows, int n_out, acsc_act act, void *dz, int64_t ld_dz,
+                                hipStream_t stream)
+{
+    clear_error();
+    if (int rc = check_layer(rows, 1, n_out, dt))
+        return rc;
+    if (int rc = check_act(act))
+        return rc;
+    if (int rc = check_mat(dy, rows > 0, ld_dy, n_out, dt, "dy"))
+        return rc;
+    if (int rc = check_kept(z, ld_z, q, rows, n_out, dt))
+        return rc;
+    if (int rc = check_mat(dz, rows > 0, ld_dz, n_out, dt, "dz"))
+        return rc;
+    ACSC_CHECK_ARG(dz != dy || rows == 0 || ld_dz == ld_dy, ACSC_EINVAL, "dz in place of dy needs ld_dz == ld_dy");
+    if (rows == 0)
+        return ACSC_OK;
+    const int64_t blocks = std::min<int64_t>((rows * ((n_out + 7) / 8) + 255) / 256, 1 << 20);
+    if (dt == ACSC_BF16)
+        ACSC_LAUNCH("lin_backward_act", lin_act_kernel<uint16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
+                    static_cast<const uint16_t *>(dy), ld_dy, static_cast<const uint16_t *>(z), ld_z, q8_of(q), rows, n_out,
+                    act, static_cast<uint16_t *>(dz), ld_dz);
+    else
+        ACSC_LAUNCH("lin_backward_act", lin_act_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
+                    static_cast<const float *>(dy), ld_dy, static_cast<const float *>(z), ld_z, q8_of(q), rows, n_out, act,
+                    static_cast<float *>(dz), ld_dz);
+    return check_launch("lin_backward_act");
+}
+
+extern "C" int lin_backward_input(const void *dz, int64_t ld_dz, acsc_dtype dt, int64_t rows, int n_in, int n_out,
+                                  const void *W, int64_t ld_w, acsc_act act, const void *z, int64_t ld_z,
+                                  const q8_tensor *q, void *dx, int64_t ld_dx, void *ws, size_t ws_bytes,
+                                  hipStream_t stream)
+{
+    clear_error();
+    if (int rc = check_layer(rows, n_in, n_out, dt))
+        return rc;
+    if (int rc = check_act(act))
+        return rc;
+    const bool some = rows > 0;
+    if (int rc = check_mat(dz, some, ld_dz, n_out, dt, "dz"))
+        return rc;
+    if (int rc = check_mat(W, some, ld_w, n_in, dt, "W"))
+        return rc;
+    if (act != ACSC_ACT_NONE)
+        if (int rc = check_kept(z, ld_z, q, rows, n_in, dt))
+            return rc;
+    if (int rc = check_mat(dx, some, ld_dx, n_in, dt, "dx"))
+        return rc;
+    ACSC_CHECK_ARG(!some || (dx != dz && dx != W), ACSC_EINVAL, "dx must not overlap dz or W");
+    const Plan p = plan_of(rows, n_in, n_out, false);
+    if (int rc = check_tiles(p))
+        return rc;
+    if (some)
+        if (int rc = check_ws(ws, ws_bytes, p.bytes()))
+            return rc;
+    if (!some)
+        return ACSC_OK;
+    Gemm g{};
+    g.A = {dz, ld_dz};
+    g.B = {W, ld_w};
+    g.M = rows;
+    g.N = n_in;
+    g.K = n_out;
+    g.e = Epi{dx, ld_dx, nullptr, nullptr, 0, const_cast<void *>(z), ld_z, q8_of(q), act, 0};
+    char *w = static_cast<char *>(ws);
+    if (dt == ACSC_BF16)
+        return run_product<false, true, kGate, uint16_t, uint16_t>(g, p, w, nullptr, stream, "lin_backward_input");
+    return run_product<false, true, kGate, float, float>(g, p, w, nullptr, stream, "lin_backward_input");
+}
+
+extern "C" int lin_backward_weight(const void *dz, int64_t ld_dz, const void *x, int64_t ld_x, const q8_tensor *q,
+                                   acsc_act act, acsc_dtype dt, int64_t rows, int n_in, int n_out, void *dW,
+                                   acsc_dtype dw_dt, int64_t ld_dw, float *db, int accumulate, void *ws,
+                                   size_t ws_bytes, hipStream_t stream)
+{
+    clear_error();
+    if (int rc = check_layer(rows, n_in, n_out, dt))
+        return rc;
+    ACSC_CHECK_ARG(dw_dt == ACSC_F32 || dw_dt == ACSC_BF16, ACSC_EDTYPE, "unknown dtype %d of dW", (int)dw_dt);
+    if (int rc = check_act(act))
+        return rc;
+    const bool some = rows > 0;
+    if (int rc = check_mat(dz, some, ld_dz, n_out, dt, "dz"))
+        return rc;
+    if (int rc = check_kept(x, ld_x, q, rows, n_in, dt))
+        return rc;
+    if (int rc = check_mat(dW, true, ld_dw, n_in, dw_dt, "dW"))
+        return rc;
+    ACSC_CHECK_ARG(aligned(db, 4), ACSC_EALIGN, "db not 4-byte aligned");
+    if (!some) {
+        if (accumulate)
+            return ACSC_OK;
+        const dim3 grid((n_in + 255) / 256, std::min(n_out, 65535));
+        if (dw_dt == ACSC_BF16)
+            ACSC_LAUNCH("lin_zero", lin_zero_kernel<uint16_t>, grid, dim3(256), 0, stream, static_cast<uint16_t *>(dW), ld_dw,
+                        static_cast<int64_t>(n_out), n_in);
+        else
+            ACSC_LAUNCH("lin_zero", lin_zero_kernel<float>, grid, dim3(256), 0, stream, static_cast<float *>(dW), ld_dw,
+                        static_cast<int64_t>(n_out), n_in);
+        if (db)
+            ACSC_LAUNCH("lin_zero", lin_zero_kernel<float>, dim3((n_out + 255) / 256, 1), dim3(256), 0, stream, db, 0,
+                        static_cast<int64_t>(1), n_out);
+        return check_launch("lin_zero");
+    }
+    const Plan p = plan_of(n_out, n_in, static_cast<int>(rows), true);
+    if (int rc = check_tiles(p))
+        return rc;
+    const size_t again = recomputed_bytes(rows, n_in, dt);
+    if (int rc = check_ws(ws, ws_bytes, p.bytes() + again))
+        return rc;
+    char *w = static_cast<char *>(ws);
+    // the activation, or the checkpoint's values, whole: read once here, and
+    // by the product many times
+    if (q || act != ACSC_ACT_NONE) {
+        void *whole = w + p.bytes();
+        const int64_t ld = (n_in + 7) / 8 * 8;
+        int rc = ACSC_OK;
+        if (q) {
+            rc = q8_decode_run(q8_of(q), rows, n_in, act, whole, dt, ld, stream);
+        } else {
+            const int64_t blocks = std::min<int64_t>((rows * ((n_in + 7) / 8) + 255) / 256, 1 << 20);
+            if (dt == ACSC_BF16)
+                ACSC_LAUNCH("lin_apply", lin_apply_kernel<uint16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
+                            static_cast<const uint16_t *>(x), ld_x, rows, n_in, act, static_cast<uint16_t *>(whole), ld);
+            else
+                ACSC_LAUNCH("lin_apply", lin_apply_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
+                            static_cast<const float *>(x), ld_x, rows, n_in, act, static_cast<float *>(whole), ld);
+            rc = check_launch("lin_apply");
+        }
+        if (rc)
+            return rc;
+        x = whole;
+        ld_x = ld;
+    }
+    Gemm g{};
+    g.A = {dz, ld_dz};
+    g.B = {x, ld_x};
+    g.M = n_out;
+    g.N = n_in;
+    g.K = static_cast<int>(rows);
+    g.e = Epi{dW, ld_dw, nullptr, nullptr, 0, nullptr, 0, q8_of(nullptr), ACSC_ACT_NONE, accumulate};
+    const char *tag = "lin_backward_weight";
+    if (dt == ACSC_BF16)
+        return dw_dt == ACSC_BF16 ? run_product<true, true, kWeight, uint16_t, uint16_t>(g, p, w, db, stream, tag)
+                                  : run_product<true, true, kWeight, uint16_t, float>(g, p, w, db, stream, tag);
+    return dw_dt == ACSC_BF16 ? run_product<true, true, kWeight, float, uint16_t>(g, p, w, db, stream, tag)
+                              : run_product<true, true, kWeight, float, float>(g, p, w, db, stream, tag);
+}

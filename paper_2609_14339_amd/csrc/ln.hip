@@ -1,0 +1,527 @@
+// Layer norm of token rows: forward (optionally writing the 8-bit checkpoint
+// of its input), the output again from kept statistics, and backward with the
+// reduction of the weight gradients over the rows.
+//
+// All of it is HBM bound: a row is read once into registers (eight columns a
+// lane and chunk), its statistics are taken there (the variance from centred
+// values), and the result is written.  NT threads share a row, in chunks of
+// 8 NT columns; rows of up to 2048 columns belong to one wave, which needs no
+// barrier, wider ones to a workgroup.
+#include "q8.h"
+
+namespace acsc {
+namespace {
+
+constexpr int kMaxH = 32768;
+
+// Sum over the wave, in every lane: rows of 16 by row_ror, then across rows.
+__device__ __forceinline__ float wave_sum(float x)
+{
+#define ACSC_ROR(n) x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + n, 0xF, 0xF, false))
+    ACSC_ROR(8);
+    ACSC_ROR(4);
+    ACSC_ROR(2);
+    ACSC_ROR(1);
+#undef ACSC_ROR
+    x += __shfl_xor(x, 16);
+    x += __shfl_xor(x, 32);
+    return x;
+}
+
+// Sums over the NT threads of a row.  `slot` holds NT / 64 values per sum and
+// is written once between two barriers of the caller's row loop.
+template <int NT, int N>
+__device__ __forceinline__ void row_sum(float (&s)[N], float *slot)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        s[i] = wave_sum(s[i]);
+    if (NT > 64) {
+        constexpr int W = NT / 64;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                slot[i * W + (threadIdx.x >> 6)] = s[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            s[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w)
+                s[i] += slot[i * W + w];
+        }
+    }
+}
+
+template <typename T>
+struct Fwd {
+    const T *x;
+    int64_t ldx;
+    Q8 src;                     // recompute from a checkpoint
+    const T *gamma, *beta;
+    T *y;
+    int64_t ldy;
+    float *mean, *rstd;         // out (forward) or in (recompute)
+    Q8 q;                       // checkpoint out
+    int64_t rows;
+    int H;
+    float eps;
+};
+
+// NT threads a row; workgroups of max(NT, 256) threads.
+template <typename T, int NT, int CH, bool AGAIN>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void ln_forward_kernel(Fwd<T> p)
+{
+    constexpr int RPB = NT < 256 ? 256 / NT : 1;
+    __shared__ float slots[2][NT / 64];
+    const int t = threadIdx.x % NT;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * RPB + (RPB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0);
+    if (RPB > 1 && row >= p.rows)
+        return;
+    float v[CH][8];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = (c * NT + t) * 8;
+        if (AGAIN && p.src.codes)
+            load_codes(p.src.codes + row * p.src.ldc + col, p.H - col,
+                       col < p.H ? p.src.scales[row * p.src.lds + col / kGroup] : 0.f, v[c]);
+        else
+            load8(p.x + row * p.ldx + col, p.H - col, v[c]);
+    }
+    float mu, rs;
+    if (AGAIN) {
+        mu = p.mean[row];
+        rs = p.rstd[row];
+    } else {
+        float s[1] = {0.f};
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                s[0] += v[c][i];
+        row_sum<NT>(s, slots[0]);
+        mu = s[0] / p.H;
+        s[0] = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int left = p.H - (c * NT + t) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = i < left ? v[c][i] - mu : 0.f;
+                s[0] += d * d;
+            }
+        }
+        row_sum<NT>(s, slots[1]);
+        rs = 1.f / sqrtf(s[0] / p.H + p.eps);
+        if (t == 0) {
+            if (p.mean)
+                p.mean[row] = mu;
+            if (p.rstd)
+                p.rstd[row] = rs;
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = (c * NT + t) * 8, left = p.H - col;
+        if (!AGAIN && p.q.codes) {
+            uint32_t a = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                a = max(a, mag(v[c][i]));
+            a = max16(a);
+            float scale, inv;
+            group_scale(a, scale, inv);
+            if (left > 0) {
+                store_codes(p.q.codes + row * p.q.ldc + col, left, inv, v[c]);
+                if ((t & 15) == 0)
+                    p.q.scales[row * p.q.lds + col / kGroup] = scale;
+            }
+        }
+        if (left > 0) {
+            float g[8], b[8], o[8];
+            if (p.gamma)
+                load8(p.gamma + col, left, g);
+            if (p.beta)
+                load8(p.beta + col, left, b);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                // one rounding each, so that both forms of the kernel give the same bits
+                o[i] = (v[c][i] - mu) * rs;
+                o[i] = __builtin_fmaf(o[i], p.gamma ? g[i] : 1.f, p.beta ? b[i] : 0.f);
+            }
+            store8(p.y + row * p.ldy + col, left, o);
+        }
+    }
+}
+
+template <typename T>
+struct Bwd {
+    const T *dy;
+    int64_t lddy;
+    const T *x;
+    int64_t ldx;
+    Q8 q;
+    const float *mean, *rstd;
+    const T *gamma;
+    const T *add;
+    int64_t ldadd;
+    T *dx;
+    int64_t lddx;
+    float *part;                // [workgroups][2][H] or nullptr
+    int64_t rows;
+    int H;
+};
+
+// A workgroup walks rows blockIdx.x, + gridDim.x, ... (four at a time where a
+// wave holds a row) and keeps the column sums of dy h and dy in registers;
+// its waves' sums meet in LDS in wave order, and every workgroup leaves one
+// partial.
+template <typename T, int NT, int CH>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void ln_backward_kernel(Bwd<T> p)
+{
+    constexpr int RPB = NT < 256 ? 256 / NT : 1;
+    __shared__ float slots[2][2 * (NT / 64)];
+    __shared__ float meet[RPB > 1 ? 2 * NT * CH * 8 : 1];
+    const int t = threadIdx.x % NT;
+    const int sub = RPB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
+    float dg[CH][8], db[CH][8];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            dg[c][i] = db[c][i] = 0.f;
+    int flip = 0;
+    for (int64_t row = static_cast<int64_t>(blockIdx.x) * RPB + sub; row < p.rows;
+         row += static_cast<int64_t>(gridDim.x) * RPB, flip ^= 1) {
+        float h[CH][8], g[CH][8];
+        const float mu = p.mean[row], rs = p.rstd[row];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * NT + t) * 8, left = p.H - col;
+            if (p.q.codes)
+                load_codes(p.q.codes + row * p.q.ldc + col, left, left > 0 ? p.q.scales[row * p.q.lds + col / kGroup] : 0.f,
+                           h[c]);
+            else
+                load8(p.x + row * p.ldx + col, left, h[c]);
+            load8(p.dy + row * p.lddy + col, left, g[c]);
+        }
+        float s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * NT + t) * 8, left = p.H - col;
+            float w[8];
+            if (p.gamma)
+                load8(p.gamma + col, left, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                h[c][i] = i < left ? (h[c][i] - mu) * rs : 0.f;
+                dg[c][i] += g[c][i] * h[c][i];
+                db[c][i] += g[c][i];
+                if (p.gamma)
+                    g[c][i] *= w[i];
+                s[0] += g[c][i];
+                s[1] += g[c][i] * h[c][i];
+            }
+        }
+        row_sum<NT>(s, slots[flip]);
+        const float m1 = s[0] / p.H, m2 = s[1] / p.H;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * NT + t) * 8, left = p.H - col;
+            if (left > 0) {
+                float o[8], a[8];
+                if (p.add)
+                    load8(p.add + row * p.ldadd + col, left, a);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    o[i] = rs * (g[c][i] - m1 - h[c][i] * m2);
+                    if (p.add)
+                        o[i] += a[i];
+                }
+                store8(p.dx + row * p.lddx + col, left, o);
+            }
+        }
+    }
+    if (!p.part)
+        return;
+    if (RPB > 1) {
+        for (int w = 0; w < RPB; ++w) {
+            if (sub == w) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        // [sum][chunk][i][lane]: consecutive lanes in consecutive banks
+                        float *m = meet + ((c * 8 + i) * NT + t);
+                        m[0] = w ? m[0] + dg[c][i] : dg[c][i];
+                        m[NT * CH * 8] = w ? m[NT * CH * 8] + db[c][i] : db[c][i];
+                    }
+            }
+            __syncthreads();
+        }
+        if (sub != 0)
+            return;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dg[c][i] = meet[(c * 8 + i) * NT + t];
+                db[c][i] = meet[(c * 8 + i) * NT + t + NT * CH * 8];
+            }
+    }
+    float *out = p.part + static_cast<int64_t>(blockIdx.x) * 2 * p.H;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = (c * NT + t) * 8, left = p.H - col;
+        if (left > 0) {
+            store8(out + col, left, dg[c]);
+            store8(out + p.H + col, left, db[c]);
+        }
+    }
+}
+
+// Column sums over the partials, in their order: 64 columns and 4 slices of
+// the partials a workgroup, the slices joined in order.
+__global__ __launch_bounds__(256) void ln_join_kernel(const float *part, int n, int H, float *dgamma, float *dbeta,
+                                                      int accumulate)
+{
+    __shared__ float meet[4][64];
+    const int lane = threadIdx.x & 63, sl = threadIdx.x >> 6;
+    const int col = blockIdx.x * 64 + lane;       // over 2 H: the dgamma columns, then dbeta's
+    const int per = (n + 3) / 4, end = min(n, (sl + 1) * per);
+    float s = 0.f;
+    if (col < 2 * H)
+        for (int i = sl * per; i < end; ++i)
+            s += part[static_cast<int64_t>(i) * 2 * H + col];
+    meet[sl][lane] = s;
+    __syncthreads();
+    if (sl == 0 && col < 2 * H) {
+        s = ((meet[0][lane] + meet[1][lane]) + meet[2][lane]) + meet[3][lane];
+        float *out = col < H ? dgamma : dbeta;
+        if (out) {
+            out += col < H ? col : col - H;
+            *out = accumulate ? *out + s : s;
+        }
+    }
+}
+
+// Threads and chunks for a row of H columns.
+struct Shape {
+    int nt, ch;
+};
+inline Shape shape_of(int H)
+{
+    if (H <= 512)
+        return {64, 1};
+    if (H <= 1024)
+        return {64, 2};
+    if (H <= 2048)
+        return {64, 4};
+    if (H <= 4096)
+        return {256, 2};
+    if (H <= 8192)
+        return {256, 4};
+    if (H <= 16384)
+        return {1024, 2};
+    return {1024, 4};
+}
+
+// Workgroups of the backward pass, which is also its number of partials.
+inline int bwd_groups(int64_t rows, int H)
+{
+    const int rpb = shape_of(H).nt == 64 ? 4 : 1;
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((rows + rpb - 1) / rpb, 512)));
+}
+
+inline int check_common(int64_t rows, int H, int dt)
+{
+    ACSC_CHECK_ARG(dt == ACSC_F32 || dt == ACSC_BF16, ACSC_EDTYPE, "unknown dtype %d", dt);
+    ACSC_CHECK_ARG(rows >= 0 && rows < (1ll << 31), ACSC_EINVAL, "rows=%lld outside [0, 2^31)", (long long)rows);
+    ACSC_CHECK_ARG(H >= 1 && H <= kMaxH, ACSC_EINVAL, "H=%d outside [1, %d]", H, kMaxH);
+    return ACSC_OK;
+}
+
+inline int check_mat(const void *p, int64_t rows, int64_t ld, int H, int dt, const char *name)
+{
+    ACSC_CHECK_ARG(rows == 0 || p, ACSC_EINVAL, "null pointer %s", name);
+    ACSC_CHECK_ARG(ld >= H, ACSC_EINVAL, "ld of %s is %lld < H=%d", name, (long long)ld, H);
+    ACSC_CHECK_ARG(aligned(p, dtype_size(static_cast<acsc_dtype>(dt))), ACSC_EALIGN, "%s not aligned to its elements",
+                   name);
+    return ACSC_OK;
+}
+
+template <typename T, bool AGAIN>
+int run_forward(const Fwd<T> &p, hipStream_t st)
+{
+    const Shape s = shape_of(p.H);
+    const int64_t blocks = s.nt == 64 ? (p.rows + 3) / 4 : p.rows;
+    const dim3 grid(static_cast<unsigned>(blocks));
+    const char *tag = AGAIN ? "ln_recompute" : "ln_forward";
+#define ACSC_CASE(NT, CH)                                                                                       \
+    if (s.nt == NT && s.ch == CH)                                                                             \
+        ACSC_LAUNCH(tag, (ln_forward_kernel<T, NT, CH, AGAIN>), grid, dim3(NT < 256 ? 256 : NT), 0, st, p);
+    ACSC_CASE(64, 1)
+    ACSC_CASE(64, 2)
+    ACSC_CASE(64, 4)
+    ACSC_CASE(256, 2)
+    ACSC_CASE(256, 4)
+    ACSC_CASE(1024, 2)
+    ACSC_CASE(1024, 4)
+#undef ACSC_CASE
+    return check_launch(tag);
+}
+
+template <typename T>
+int run_backward(const Bwd<T> &p, int groups, hipStream_t st)
+{
+    const Shape s = shape_of(p.H);
+    const dim3 grid(groups);
+#define ACSC_CASE(NT, CH)                                                                                       \
+    if (s.nt == NT && s.ch == CH)                                                                             \
+        ACSC_LAUNCH("ln_backward", (ln_backward_kernel<T, NT, CH>), grid, dim3(NT < 256 ? 256 : NT), 0, st, p);
+    ACSC_CASE(64, 1)
+    ACSC_CASE(64, 2)
+    ACSC_CASE(64, 4)
+    ACSC_CASE(256, 2)
+    ACSC_CASE(256, 4)
+    ACSC_CASE(1024, 2)
+    ACSC_CASE(1024, 4)
+#undef ACSC_CASE
+    return check_launch("ln_backward");
+}
+
+template <typename T>
+const T *as(const void *p)
+{
+    return static_cast<const T *>(p);
+}
+
+}  // namespace
+}  // namespace acsc
+
+using namespace acsc;
+
+extern "C" int ln_forward(const void *x, acsc_dtype dt, int64_t rows, int H, int64_t ld_x, const void *gamma,
+                          const void *beta, float eps, void *y, int64_t ld_y, float *mean, float *rstd,
+                          const q8_tensor *q, hipStream_t stream)
+{
+    clear_error();
+    if (int rc = check_common(rows, H, dt))
+        return rc;
+    ACSC_CHECK_ARG(std::isfinite(eps) && eps > 0.f, ACSC_EINVAL, "eps=%g must be positive", eps);
+    if (int rc = check_mat(x, rows, ld_x, H, dt, "x"))
+        return rc;
+    if (int rc = check_mat(y, rows, ld_y, H, dt, "y"))
+        return rc;
+    ACSC_CHECK_ARG(y != x || rows == 0 || ld_y == ld_x, ACSC_EINVAL, "y in place of x needs ld_y == ld_x");
+    ACSC_CHECK_ARG(aligned(gamma, dtype_size(dt)) && aligned(beta, dtype_size(dt)), ACSC_EALIGN,
+                   "gamma or beta not aligned to its elements");
+    ACSC_CHECK_ARG(aligned(mean, 4) && aligned(rstd, 4), ACSC_EALIGN, "mean or rstd not 4-byte aligned");
+    if (q)
+        if (int rc = check_q8(q, rows, H))
+            return rc;
+    if (rows == 0)
+        return ACSC_OK;
+    const Q8 none{nullptr, nullptr, 0, 0};
+    if (dt == ACSC_BF16)
+        return run_forward<uint16_t, false>({as<uint16_t>(x), ld_x, none, as<uint16_t>(gamma), as<uint16_t>(beta),
+                                             static_cast<uint16_t *>(y), ld_y, mean, rstd, q8_of(q), rows, H, eps}, stream);
+    return run_forward<float, false>({as<float>(x), ld_x, none, as<float>(gamma), as<float>(beta),
+                                      static_cast<float *>(y), ld_y, mean, rstd, q8_of(q), rows, H, eps}, stream);
+}
+
+extern "C" int ln_recompute(const void *x, int64_t ld_x, const q8_tensor *q, acsc_dtype dt, int64_t rows, int H,
+                            const float *mean, const float *rstd, const void *gamma, const void *beta, void *y,
+                            int64_t ld_y, hipStream_t stream)
+{
+    clear_error();
+    if (int rc = check_common(rows, H, dt))
+        return rc;
+    ACSC_CHECK_ARG(rows == 0 || (x != nullptr) != (q != nullptr), ACSC_EINVAL, "exactly one of x and its checkpoint is needed");
+    if (x)
+        if (int rc = check_mat(x, rows, ld_x, H, dt, "x"))
+            return rc;
+    if (q)
+        if (int rc = check_q8(q, rows, H))
+            return rc;
+    if (int rc = check_mat(y, rows, ld_y, H, dt, "y"))
+        return rc;
+    ACSC_CHECK_ARG(y != x || rows == 0 || ld_y == ld_x, ACSC_EINVAL, "y in place of x needs ld_y == ld_x");
+    ACSC_CHECK_ARG(rows == 0 || (mean && rstd), ACSC_EINVAL, "null statistics");
+    ACSC_CHECK_ARG(aligned(mean, 4) && aligned(rstd, 4), ACSC_EALIGN, "mean or rstd not 4-byte aligned");
+    ACSC_CHECK_ARG(aligned(gamma, dtype_size(dt)) && aligned(beta, dtype_size(dt)), ACSC_EALIGN,
+                   "gamma or beta not aligned to its elements");
+    if (rows == 0)
+        return ACSC_OK;
+    const Q8 none{nullptr, nullptr, 0, 0};
+    float *mu = const_cast<float *>(mean), *rs = const_cast<float *>(rstd);   // read only there
+    if (dt == ACSC_BF16)
+        return run_forward<uint16_t, true>({as<uint16_t>(x), ld_x, q8_of(q), as<uint16_t>(gamma), as<uint16_t>(beta),
+                                            static_cast<uint16_t *>(y), ld_y, mu, rs, none, rows, H, 0.f}, stream);
+    return run_forward<float, true>({as<float>(x), ld_x, q8_of(q), as<float>(gamma), as<float>(beta),
+                                     static_cast<float *>(y), ld_y, mu, rs, none, rows, H, 0.f}, stream);
+}
+
+extern "C" int ln_workspace_size(int64_t rows, int H, size_t *bytes)
+{
+    clear_error();
+    if (int rc = check_common(rows, H, ACSC_F32))
+        return rc;
+    ACSC_CHECK_ARG(bytes, ACSC_EINVAL, "null pointer bytes");
+    *bytes = static_cast<size_t>(bwd_groups(rows, H)) * 2 * H * sizeof(float);
+    return ACSC_OK;
+}
+
+extern "C" int ln_backward(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, const q8_tensor *q,
+                           acsc_dtype dt, int64_t rows, int H, const float *mean, const float *rstd,
+                           const void *gamma, const void *add, int64_t ld_add, void *dx, int64_t ld_dx, float *dgamma,
+                           float *dbeta, int accumulate, void *ws, size_t ws_bytes, hipStream_t stream)
+{
+    clear_error();
+    if (int rc = check_common(rows, H, dt))
+        return rc;
+    ACSC_CHECK_ARG(rows == 0 || (x != nullptr) != (q != nullptr), ACSC_EINVAL, "exactly one of x and its checkpoint is needed");
+    if (int rc = check_mat(dy, rows, ld_dy, H, dt, "dy"))
+        return rc;
+    if (x)
+        if (int rc = check_mat(x, rows, ld_x, H, dt, "x"))
+            return rc;
+    if (q)
+        if (int rc = check_q8(q, rows, H))
+            return rc;
+    if (add)
+        if (int rc = check_mat(add, rows, ld_add, H, dt, "add"))
+            return rc;
+    if (int rc = check_mat(dx, rows, ld_dx, H, dt, "dx"))
+        return rc;
+    ACSC_CHECK_ARG(dx != dy || rows == 0 || ld_dx == ld_dy, ACSC_EINVAL, "dx in place of dy needs ld_dx == ld_dy");
+    ACSC_CHECK_ARG(dx != add || rows == 0 || ld_dx == ld_add, ACSC_EINVAL, "dx in place of add needs ld_dx == ld_add");
+    ACSC_CHECK_ARG(rows == 0 || (mean && rstd), ACSC_EINVAL, "null statistics");
+    ACSC_CHECK_ARG(aligned(mean, 4) && aligned(rstd, 4) && aligned(dgamma, 4) && aligned(dbeta, 4), ACSC_EALIGN,
+                   "an fp32 array is not 4-byte aligned");
+    ACSC_CHECK_ARG(aligned(gamma, dtype_size(dt)), ACSC_EALIGN, "gamma not aligned to its elements");
+    const bool sums = dgamma || dbeta;
+    const int groups = bwd_groups(rows, H);
+    if (sums) {
+        ACSC_CHECK_ARG(ws, ACSC_EINVAL, "null workspace");
+        ACSC_CHECK_ARG(aligned(ws, 256), ACSC_EALIGN, "workspace not 256-byte aligned");
+        const size_t need = static_cast<size_t>(groups) * 2 * H * sizeof(float);
+        ACSC_CHECK_ARG(ws_bytes >= need, ACSC_ENOSPC, "workspace of %zu bytes, %zu needed", ws_bytes, need);
+    }
+    if (rows == 0 && !sums)
+        return ACSC_OK;
+    float *part = sums ? static_cast<float *>(ws) : nullptr;
+    int rc;
+    if (dt == ACSC_BF16)
+        rc = run_backward<uint16_t>({as<uint16_t>(dy), ld_dy, as<uint16_t>(x), ld_x, q8_of(q), mean, rstd,
+                                     as<uint16_t>(gamma), as<uint16_t>(add), ld_add, static_cast<uint16_t *>(dx), ld_dx,
+                                     part, rows, H}, groups, stream);
+    else
+        rc = run_backward<float>({as<float>(dy), ld_dy, as<float>(x), ld_x, q8_of(q), mean, rstd, as<float>(gamma),
+                                  as<float>(add), ld_add, static_cast<float *>(dx), ld_dx, part, rows, H}, groups, stream);
+    if (rc || !sums)
+        return rc;
+    ACSC_LAUNCH("ln_join", ln_join_kernel, dim3((2 * H + 63) / 64), dim3(256), 0, stream, part, groups, H, dgamma, dbeta,
+                accumulate);
+    return check_launch("ln_join");
+}

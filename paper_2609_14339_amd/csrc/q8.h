@@ -1,0 +1,283 @@
+// Device code that the norm, the linear layers and the checkpoints share:
+// eight-column accesses, activation functions, and the 8-bit checkpoint's
+// coding of one group.
+#pragma once
+
+#include "common.h"
+
+namespace acsc {
+
+constexpr int kGroup = ACSC_Q8_GROUP;
+
+// The checkpoint descriptor as kernels take it (codes == nullptr: none).
+struct Q8 {
+    int8_t *codes;
+    float *scales;
+    int64_t ldc, lds;
+};
+
+inline Q8 q8_of(const q8_tensor *q)
+{
+    return q ? Q8{q->codes, q->scales, q->ld_codes, q->ld_scales} : Q8{nullptr, nullptr, 0, 0};
+}
+
+// Host checks of a checkpoint of a [rows, H] tensor.
+inline int check_q8(const q8_tensor *q, int64_t rows, int H)
+{
+    ACSC_CHECK_ARG(rows == 0 || (q->codes && q->scales), ACSC_EINVAL, "null pointer in the checkpoint");
+    ACSC_CHECK_ARG(q->ld_codes >= H, ACSC_EINVAL, "ld_codes=%lld < H=%d", (long long)q->ld_codes, H);
+    ACSC_CHECK_ARG(q->ld_scales >= (H + kGroup - 1) / kGroup, ACSC_EINVAL, "ld_scales=%lld < %d groups",
+                   (long long)q->ld_scales, (H + kGroup - 1) / kGroup);
+    ACSC_CHECK_ARG(aligned(q->scales, 4), ACSC_EALIGN, "scales not 4-byte aligned");
+    return ACSC_OK;
+}
+
+inline int check_act(int act)
+{
+    ACSC_CHECK_ARG(act >= ACSC_ACT_NONE && act <= ACSC_ACT_SILU, ACSC_EINVAL, "unknown activation %d", act);
+    return ACSC_OK;
+}
+
+struct __attribute__((packed, aligned(1))) C8Any {
+    uint32_t w[2];
+};
+
+// Eight consecutive elements as floats; only the first nv are read (the rest
+// become 0).  Whole chunks are 16-byte accesses at any element's alignment.
+__device__ __forceinline__ void load8(const uint16_t *p, int nv, float (&v)[8])
+{
+    if (nv >= 8) {
+        const Bf8Any c = *reinterpret_cast<const Bf8Any *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(c.w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(c.w[i] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = i < nv ? bf16_to_f32(p[i]) : 0.f;
+    }
+}
+__device__ __forceinline__ void load8(const float *p, int nv, float (&v)[8])
+{
+    if (nv >= 8) {
+        const F4Any a = *reinterpret_cast<const F4Any *>(p), b = *reinterpret_cast<const F4Any *>(p + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = a.v[i];
+            v[4 + i] = b.v[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = i < nv ? p[i] : 0.f;
+    }
+}
+__device__ __forceinline__ void store8(uint16_t *p, int nv, const float (&v)[8])
+{
+    if (nv >= 8) {
+        Bf8Any c;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            c.w[i] = f32x2_to_bf16x2(v[2 * i], v[2 * i + 1]);
+        *reinterpret_cast<Bf8Any *>(p) = c;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < nv)
+                p[i] = f32_to_bf16(v[i]);
+    }
+}
+__device__ __forceinline__ void store8(float *p, int nv, const float (&v)[8])
+{
+    if (nv >= 8) {
+        F4Any a, b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            a.v[i] = v[i];
+            b.v[i] = v[4 + i];
+        }
+        *reinterpret_cast<F4Any *>(p) = a;
+        *reinterpret_cast<F4Any *>(p + 4) = b;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < nv)
+                p[i] = v[i];
+    }
+}
+// Four consecutive elements, as above.
+struct __attribute__((packed, aligned(2))) Bf4Any {
+    uint32_t w[2];
+};
+__device__ __forceinline__ void load4(const uint16_t *p, int nv, float (&v)[4])
+{
+    if (nv >= 4) {
+        const Bf4Any c = *reinterpret_cast<const Bf4Any *>(p);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            v[2 * i] = __uint_as_float(c.w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(c.w[i] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = i < nv ? bf16_to_f32(p[i]) : 0.f;
+    }
+}
+__device__ __forceinline__ void load4(const float *p, int nv, float (&v)[4])
+{
+    if (nv >= 4) {
+        const F4Any a = *reinterpret_cast<const F4Any *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = a.v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = i < nv ? p[i] : 0.f;
+    }
+}
+__device__ __forceinline__ void store4(uint16_t *p, int nv, const float (&v)[4])
+{
+    if (nv >= 4) {
+        Bf4Any c;
+        c.w[0] = f32x2_to_bf16x2(v[0], v[1]);
+        c.w[1] = f32x2_to_bf16x2(v[2], v[3]);
+        *reinterpret_cast<Bf4Any *>(p) = c;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < nv)
+                p[i] = f32_to_bf16(v[i]);
+    }
+}
+__device__ __forceinline__ void store4(float *p, int nv, const float (&v)[4])
+{
+    if (nv >= 4) {
+        F4Any a;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            a.v[i] = v[i];
+        *reinterpret_cast<F4Any *>(p) = a;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < nv)
+                p[i] = v[i];
+    }
+}
+
+// Values of N = 4 or 8 consecutive codes under one scale.
+template <int N>
+__device__ __forceinline__ void load_codes(const int8_t *p, int nv, float scale, float (&v)[N])
+{
+    if (nv >= N) {
+        struct __attribute__((packed, aligned(1))) Any {
+            uint32_t w[N / 4];
+        };
+        const Any c = *reinterpret_cast<const Any *>(p);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = static_cast<float>(static_cast<int8_t>(c.w[i / 4] >> (8 * (i % 4)))) * scale;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = i < nv ? static_cast<float>(p[i]) * scale : 0.f;
+    }
+}
+
+// A group's largest magnitude is found as the maximum of its values' bits
+// without the sign: that order puts NaN above infinity above every number.
+__device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// scale = a / 127 and inv = 127 / a of a group whose largest magnitude has the
+// bits a.  A group below 2^-120 (127 / a would leave fp32's range not far
+// below) is kept as zeros; one with an infinity or NaN reads as NaN.
+__device__ __forceinline__ void group_scale(uint32_t a, float &scale, float &inv)
+{
+    if (a >= 0x7f800000u) {
+        scale = __uint_as_float(0x7fc00000u);
+        inv = 0.f;
+    } else if (a < 0x03800000u) {   // 2^-120
+        scale = inv = 0.f;
+    } else {
+        const float f = __uint_as_float(a);
+        scale = f / 127.f;
+        inv = 127.f / f;
+    }
+}
+
+// Codes of N values: rint(x * inv), in -127 .. 127 because |x| <= a makes
+// |x * inv| round to at most 127 (1 + 2^-23).  inv = 0 gives zeros, for the
+// non-finite values of a NaN group too.
+template <int N>
+__device__ __forceinline__ void store_codes(int8_t *p, int nv, float inv, const float (&v)[N])
+{
+    uint32_t w[N / 4];
+#pragma unroll
+    for (int q = 0; q < N / 4; ++q) {
+        w[q] = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float t = inv == 0.f ? 0.f : v[4 * q + i] * inv;
+            w[q] |= (static_cast<uint32_t>(static_cast<int>(rintf(t))) & 0xffu) << (8 * i);
+        }
+    }
+    if (nv >= N) {
+        struct __attribute__((packed, aligned(1))) Any {
+            uint32_t w[N / 4];
+        };
+        Any c;
+#pragma unroll
+        for (int q = 0; q < N / 4; ++q)
+            c.w[q] = w[q];
+        *reinterpret_cast<Any *>(p) = c;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < nv)
+                p[i] = static_cast<int8_t>(w[i / 4] >> (8 * (i % 4)));
+    }
+}
+
+// Maximum over the 16 lanes of a row of the wave, in every lane (row_ror).
+__device__ __forceinline__ uint32_t max16(uint32_t x)
+{
+#define ACSC_ROR(n) x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), 0x120 + n, 0xF, 0xF, false)))
+    ACSC_ROR(8);
+    ACSC_ROR(4);
+    ACSC_ROR(2);
+    ACSC_ROR(1);
+#undef ACSC_ROR
+    return x;
+}
+
+// act(z) and act'(z).  gelu(z) = z Phi(z), Phi(z) = erfc(-z / sqrt 2) / 2;
+// gelu'(z) = Phi(z) + z phi(z).  silu(z) = z s, s = 1 / (1 + exp(-z)).
+// Limits at infinities follow the definitions' plain arithmetic.
+__device__ __forceinline__ float act_value(float z, int act)
+{
+    if (act == ACSC_ACT_RELU)
+        return z > 0.f ? z : (z != z ? z : 0.f);
+    if (act == ACSC_ACT_GELU)
+        return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    if (act == ACSC_ACT_SILU)
+        return z / (1.f + expf(-z));
+    return z;
+}
+__device__ __forceinline__ float act_slope(float z, int act)
+{
+    if (act == ACSC_ACT_RELU)
+        return z > 0.f ? 1.f : (z != z ? z : 0.f);
+    if (act == ACSC_ACT_GELU)
+        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+    if (act == ACSC_ACT_SILU) {
+        const float s = 1.f / (1.f + expf(-z));
+        return s * (1.f + z * (1.f - s));
+    }
+    return 1.f;
+}
+
+}  // namespace acsc
