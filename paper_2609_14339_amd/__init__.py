@@ -139,6 +139,7 @@ def _load():
             ("ln_workspace_size", [i64, i32, C.POINTER(sz)]),
             ("ln_backward", [vp, i64, vp, i64, qp, i32, i64, i32, vp, vp, vp, vp, i64, vp, i64, vp, vp, i32, vp, sz, vp]),
             ("lin_workspace_size", [i32, i64, i32, i32, i32, C.POINTER(sz)]),
+            ("lin_workspace_size_unaligned", [i32, i64, i32, i32, i32, C.POINTER(sz)]),
             ("lin_forward", [vp, i64, i32, i64, i32, i32, vp, i64, vp, i32, vp, i64, vp, i64, vp, i64, qp, vp, sz, vp]),
             ("lin_backward_act", [vp, i64, vp, i64, qp, i32, i64, i32, i32, vp, i64, vp]),
             ("lin_backward_input", [vp, i64, i32, i64, i32, i32, vp, i64, i32, vp, i64, qp, vp, i64, vp, sz, vp]),
@@ -166,7 +167,7 @@ EXPORTED = ("acsc_last_error", "acsc_version", "acsc_stats_enable", "acsc_stats_
             "ac_bern_mask", "ac_bern_pack", "ac_bern_unpack",
             "psgd_workspace_size", "psgd_project", "psgd_orthogonalize", "psgd_decompress", "psgd_step",
             "q8_encode", "q8_decode", "ln_forward", "ln_recompute", "ln_workspace_size", "ln_backward",
-            "lin_workspace_size", "lin_forward", "lin_backward_act", "lin_backward_input", "lin_backward_weight")
+            "lin_workspace_size", "lin_workspace_size_unaligned", "lin_forward", "lin_backward_act", "lin_backward_input", "lin_backward_weight")
 
 
 def _check(rc: int):
@@ -788,11 +789,30 @@ def ln_backward(dy: torch.Tensor, src: Union[torch.Tensor, Q8], mean: torch.Tens
 
 
 def lin_workspace_size(op: int, rows: int, n_in: int, n_out: int, dtype: torch.dtype) -> int:
-    """Bytes for one product (LIN_FORWARD, LIN_BACKWARD_INPUT, LIN_BACKWARD_WEIGHT) of a linear layer."""
+    """Bytes for one product (LIN_FORWARD, LIN_BACKWARD_INPUT, LIN_BACKWARD_WEIGHT) of a linear layer whose
+    operands are 16-byte aligned with row strides of multiples of eight elements."""
     b = C.c_size_t(0)
     code = BF16 if dtype == torch.bfloat16 else F32
     _check(lib.lin_workspace_size(op, rows, n_in, n_out, code, C.byref(b)))
     return b.value
+
+
+def lin_workspace_size_unaligned(op: int, rows: int, n_in: int, n_out: int, dtype: torch.dtype) -> int:
+    """The same for operands of any alignment and stride."""
+    b = C.c_size_t(0)
+    code = BF16 if dtype == torch.bfloat16 else F32
+    _check(lib.lin_workspace_size_unaligned(op, rows, n_in, n_out, code, C.byref(b)))
+    return b.value
+
+
+def _lin_ws(op: int, rows: int, n_in: int, n_out: int, ops, ws: Optional[torch.Tensor], stream):
+    """A workspace for a product of these (tensor, row stride) operands, unless one is given."""
+    t = ops[0][0]
+    if ws is not None:
+        return _ws(0, ws, t.device, stream)
+    plain = all(ld % 8 == 0 and o.data_ptr() % 16 == 0 and ld < 1 << 22 for o, ld in ops)
+    size = lin_workspace_size if plain else lin_workspace_size_unaligned
+    return _ws(size(op, rows, n_in, n_out, t.dtype), ws, t.device, stream)
 
 
 def lin_forward(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
@@ -814,7 +834,7 @@ def lin_forward(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
         raise AcscError(ACSC_EINVAL, f"keep must be None, 'z' or 'q8', not {keep!r}")
     z = torch.empty(shape, dtype=x.dtype, device=x.device) if keep == "z" else None
     q = _q8_new(rows, n_out, x.device) if keep == "q8" else None
-    wp, wn, hold = _ws(lin_workspace_size(LIN_FORWARD, rows, n_in, n_out, x.dtype), ws, x.device, stream)
+    wp, wn, hold = _lin_ws(LIN_FORWARD, rows, n_in, n_out, ((x, ldx), (W, ldw)), ws, stream)
     _check(lib.lin_forward(_ptr(x), ldx, dt, rows, n_in, n_out, _ptr(W), ldw, _ptr(bias), _act(act), _ptr(residual), ldr,
                            _ptr(y), ldy, _ptr(z), n_out, _q8_ref(q, rows, n_out), wp, wn, _stream(stream)))
     return y, (z if q is None else q)
@@ -845,7 +865,7 @@ def lin_backward_input(dz: torch.Tensor, W: torch.Tensor, act: str = "none",
     if dx is None:
         dx = torch.empty(rows, n_in, dtype=dz.dtype, device=dz.device)
     lddx = _rows(dx, (rows, n_in), dz.dtype, "dx")
-    wp, wn, hold = _ws(lin_workspace_size(LIN_BACKWARD_INPUT, rows, n_in, n_out, dz.dtype), ws, dz.device, stream)
+    wp, wn, hold = _lin_ws(LIN_BACKWARD_INPUT, rows, n_in, n_out, ((dz, lddz), (W, ldw)), ws, stream)
     _check(lib.lin_backward_input(_ptr(dz), lddz, _dt(dz), rows, n_in, n_out, _ptr(W), ldw, _act(act), p, ldz, q, _ptr(dx),
                                   lddx, wp, wn, _stream(stream)))
     return dx
@@ -871,7 +891,7 @@ def lin_backward_weight(dz: torch.Tensor, x: Union[torch.Tensor, Q8], act: str =
         db = torch.empty(n_out, dtype=torch.float32, device=dz.device)
     _vec(db, n_out, torch.float32, "db")
     lddw = _rows(dW, (n_out, n_in), dw_dtype or dW.dtype, "dW")
-    wp, wn, hold = _ws(lin_workspace_size(LIN_BACKWARD_WEIGHT, rows, n_in, n_out, dz.dtype), ws, dz.device, stream)
+    wp, wn, hold = _lin_ws(LIN_BACKWARD_WEIGHT, rows, n_in, n_out, ((dz, lddz),) if q is not None else ((dz, lddz), (x, ldx)), ws, stream)
     _check(lib.lin_backward_weight(_ptr(dz), lddz, p, ldx, q, _act(act), _dt(dz), rows, n_in, n_out, _ptr(dW), _dt(dW), lddw,
                                    _ptr(db), int(accumulate), wp, wn, _stream(stream)))
     return dW, db

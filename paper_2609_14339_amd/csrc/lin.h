@@ -44,108 +44,110 @@ struct Gemm {
     int kchunk;
     float *part;      // splits > 1: piece s at part + s * M * ldp
     int64_t ldp;
-    float *dbpart;    // weight gradient with db: piece s at dbpart + s * M, else nullptr
     Epi e;
 };
 
-// One row's values at columns n0 + 16 j .. n0 + 16 j + 3 (j < NJ), through the
-// epilogue.  With NJ = 8 the four lanes 16 apart hold one group of 128
-// columns of the row; with NJ = 1 a run of 32 lanes does.  Every lane of the
-// wave calls it (`on`: its row exists); T is the type of y, z, bias and
-// residual.
-template <typename T, int KIND, int NJ>
-__device__ __forceinline__ void epilogue(const Epi &e, float (&v)[NJ][4], bool on, int64_t m, int n0, int N)
+// Eight values of row m at columns n .. n + 7 (n a multiple of 8) through the
+// epilogue.  Sixteen lanes of the wave, aligned, hold one group of 128
+// columns of a row, and every lane of the wave calls it (`on`: the row
+// exists); T is the type of y, z, bias and residual.
+template <typename T, int KIND>
+__device__ __forceinline__ void epilogue(const Epi &e, float (&v)[8], bool on, int64_t m, int n, int N)
 {
+    const int left = on ? N - n : 0;
     if (KIND == kForward) {
         if (e.bias) {
+            float b[8];
+            load8(static_cast<const T *>(e.bias) + n, left, b);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                float b[4];
-                load4(static_cast<const T *>(e.bias) + n0 + 16 * j, N - n0 - 16 * j, b);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    v[j][i] += b[i];
-            }
+            for (int i = 0; i < 8; ++i)
+                v[i] += b[i];
         }
-        if (e.z && on) {
-            T *z = static_cast<T *>(e.z) + m * e.ldz;
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-                store4(z + n0 + 16 * j, N - n0 - 16 * j, v[j]);
-        }
+        if (e.z)
+            store8(static_cast<T *>(e.z) + m * e.ldz + n, left, v);
         if (e.q.codes) {
             uint32_t a = 0;
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (n0 + 16 * j + i < N)
-                        a = max(a, mag(v[j][i]));
-            if (NJ == 1)
-                a = max16(a);
-            a = max(a, static_cast<uint32_t>(__shfl_xor(static_cast<int>(a), 16)));
-            if (NJ > 1)
-                a = max(a, static_cast<uint32_t>(__shfl_xor(static_cast<int>(a), 32)));
+            for (int i = 0; i < 8; ++i)
+                if (i < left)
+                    a = max(a, mag(v[i]));
+            a = max16(a);
             float scale, inv;
             group_scale(a, scale, inv);
-            if (on) {
-                int8_t *c = e.q.codes + m * e.q.ldc;
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-                    store_codes(c + n0 + 16 * j, N - n0 - 16 * j, inv, v[j]);
-                if (n0 < N && n0 % kGroup == 0)
-                    e.q.scales[m * e.q.lds + n0 / kGroup] = scale;
-            }
+            store_codes(e.q.codes + m * e.q.ldc + n, left, inv, v);
+            if (left > 0 && n % kGroup == 0)
+                e.q.scales[m * e.q.lds + n / kGroup] = scale;
         }
         if (e.act != ACSC_ACT_NONE) {
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    v[j][i] = act_value(v[j][i], e.act);
+            for (int i = 0; i < 8; ++i)
+                v[i] = act_value(v[i], e.act);
         }
-        if (e.res && on) {
-            const T *r = static_cast<const T *>(e.res) + m * e.ldr;
+        if (e.res) {
+            float b[8];
+            load8(static_cast<const T *>(e.res) + m * e.ldr + n, left, b);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                float b[4];
-                load4(r + n0 + 16 * j, N - n0 - 16 * j, b);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    v[j][i] += b[i];
-            }
+            for (int i = 0; i < 8; ++i)
+                v[i] += b[i];
         }
     }
-    if (!on)
+    if (left <= 0)
         return;
     if (KIND == kGate && e.act != ACSC_ACT_NONE) {
+        float z[8];
+        if (e.q.codes)
+            load_codes(e.q.codes + m * e.q.ldc + n, left, e.q.scales[m * e.q.lds + n / kGroup], z);
+        else
+            load8(static_cast<const T *>(e.z) + m * e.ldz + n, left, z);
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const int n = n0 + 16 * j;
-            if (n < N) {
-                float z[4];
-                if (e.q.codes)
-                    load_codes(e.q.codes + m * e.q.ldc + n, N - n, e.q.scales[m * e.q.lds + n / kGroup], z);
-                else
-                    load4(static_cast<const T *>(e.z) + m * e.ldz + n, N - n, z);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    v[j][i] *= act_slope(z[i], e.act);
-            }
-        }
+        for (int i = 0; i < 8; ++i)
+            v[i] *= act_slope(z[i], e.act);
     }
-    T *y = static_cast<T *>(e.y) + m * e.ldy;
+    T *y = static_cast<T *>(e.y) + m * e.ldy + n;
+    if (KIND == kWeight && e.accumulate) {
+        float o[8];
+        load8(y, left, o);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-        const int n = n0 + 16 * j;
-        if (KIND == kWeight && e.accumulate) {
-            float o[4];
-            load4(y + n, N - n, o);
+        for (int i = 0; i < 8; ++i)
+            v[i] += o[i];
+    }
+    store8(y, left, v);
+}
+
+// A wave's accumulators of 16 NA rows by 128 columns through the epilogue, or
+// into a piece of a cut product.  acc[a][j] holds in lane L the columns
+// 16 j + 4 (L / 16) + i of row 16 a + L % 16; they turn into runs of eight
+// columns in `lds` (8 KiB NA, the wave's own), whose 16-byte chunks are
+// XOR-swizzled by the row so that neither side conflicts: rows then go out as
+// 256 (bf16) contiguous bytes.
+template <typename T, int KIND, int NA>
+__device__ __forceinline__ void put_rows(const Gemm &g, const f32x4 (&acc)[NA][8], char *lds, int64_t m0, int n0,
+                                         int split)
+{
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                v[j][i] += o[i];
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int row = a * 16 + (lane & 15), chunk = (j * 4 + (lane >> 4)) ^ (row & 31);
+            *reinterpret_cast<f32x4 *>(lds + row * 512 + chunk * 16) = acc[a][j];
         }
-        store4(y + n, N - n, v[j]);
+    // the wave reads what its own lanes wrote: LDS keeps a wave's order
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll 1
+    for (int r = 0; r < NA * 4; ++r) {
+        const int row = r * 4 + (lane >> 4), c = (lane & 15) * 2;
+        const f32x4 lo = *reinterpret_cast<const f32x4 *>(lds + row * 512 + (c ^ (row & 31)) * 16);
+        const f32x4 hi = *reinterpret_cast<const f32x4 *>(lds + row * 512 + ((c + 1) ^ (row & 31)) * 16);
+        float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        const int64_t m = m0 + row;
+        const int n = n0 + (lane & 15) * 8;
+        if (g.splits > 1)
+            store8(g.part + (split * g.M + m) * g.ldp + n, m < g.M ? g.N - n : 0, v);
+        else
+            epilogue<T, KIND>(g.e, v, m < g.M, m, n, g.N);
     }
 }
 

@@ -5,6 +5,8 @@
 namespace acsc {
 
 int q8_decode_run(const Q8 &q, int64_t rows, int H, int act, void *y, acsc_dtype dt, int64_t ldy, hipStream_t st);
+int lin_bf16_pack(const void *x, int64_t ldx, int64_t rows, int cols, void *y, int64_t ldy, hipStream_t st);
+int lin_bf16_run(const Gemm &g, int tile, EpiKind kind, acsc_dtype out, hipStream_t st, const char *tag);
 
 namespace {
 
@@ -17,14 +19,14 @@ constexpr int kTile = 128, kBK = 32;
 // are stored (rows padded to 36, or k-lines to 132 floats: fragment reads are
 // free of bank conflicts in both), the next step's loads in flight while one
 // is multiplied; any alignment, edges read as zeros.
-template <typename T, bool COL>
+template <bool COL>
 struct Stage {
     static constexpr int kPitch = COL ? kTile + 4 : kBK + 4;
     static constexpr int kFloats = COL ? kBK * kPitch : kTile * kPitch;
     float r[4][4];
     __device__ __forceinline__ void load(const Operand &o, int64_t i0, int64_t ni, int k0, int kend)
     {
-        const T *p = static_cast<const T *>(o.p);
+        const float *p = static_cast<const float *>(o.p);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             if (COL) {
@@ -58,27 +60,27 @@ struct Stage {
     }
 };
 
-template <typename T, bool ACOL, bool BCOL, int KIND, typename TO>
+template <bool ACOL, bool BCOL, int KIND, typename TO>
 __global__ __launch_bounds__(256) void lin_f32_kernel(Gemm g)
 {
-    __shared__ __align__(16) float As[Stage<T, ACOL>::kFloats];
-    __shared__ __align__(16) float Bs[Stage<T, BCOL>::kFloats];
+    // the tiles; after the last step 8 KiB a wave for the epilogue
+    constexpr int kFloats = Stage<ACOL>::kFloats + Stage<BCOL>::kFloats;
+    __shared__ __align__(16) float lds[kFloats > 8192 ? kFloats : 8192];
+    float *As = lds, *Bs = lds + Stage<ACOL>::kFloats;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int tile = blockIdx.x, split = blockIdx.y;
     const int64_t m0 = static_cast<int64_t>(tile / g.tn) * kTile;
     const int n0 = tile % g.tn * kTile;
     const int kbeg = split * g.kchunk, kend = min(g.K, kbeg + g.kchunk);
-    const bool sums = KIND == kWeight && g.dbpart && n0 == 0;
-    f32x4 acc[2][8], dacc[2];
+    f32x4 acc[2][8];
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
-        dacc[a] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             acc[a][j] = f32x4{0, 0, 0, 0};
     }
-    Stage<T, ACOL> sa;
-    Stage<T, BCOL> sb;
+    Stage<ACOL> sa;
+    Stage<BCOL> sb;
     sa.load(g.A, m0, g.M, kbeg, kend);
     sb.load(g.B, n0, g.N, kbeg, kend);
     for (int k0 = kbeg; k0 < kend; k0 += kBK) {
@@ -94,10 +96,10 @@ __global__ __launch_bounds__(256) void lin_f32_kernel(Gemm g)
             f32x4 fa[2], fb[8];
 #pragma unroll
             for (int a = 0; a < 2; ++a)
-                fa[a] = Stage<T, ACOL>::frag(As, wave * 32 + a * 16, kk);
+                fa[a] = Stage<ACOL>::frag(As, wave * 32 + a * 16, kk);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                fb[j] = Stage<T, BCOL>::frag(Bs, j * 16, kk);
+                fb[j] = Stage<BCOL>::frag(Bs, j * 16, kk);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -105,68 +107,86 @@ __global__ __launch_bounds__(256) void lin_f32_kernel(Gemm g)
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
                         acc[a][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j][e], fa[a][e], acc[a][j], 0, 0, 0);
-            if (sums)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int a = 0; a < 2; ++a)
-                        dacc[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(1.f, fa[a][e], dacc[a], 0, 0, 0);
         }
         __syncthreads();
     }
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
-        const int64_t m = m0 + wave * 32 + a * 16 + (lane & 15);
-        const int n = n0 + (lane >> 4) * 4;
-        if (sums && lane < 16 && m < g.M)
-            g.dbpart[split * g.M + m] = dacc[a][0];
-        float v[8][4];
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                v[j][i] = acc[a][j][i];
-        if (g.splits > 1) {
-            if (m < g.M)
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    store4(g.part + (split * g.M + m) * g.ldp + n + 16 * j, g.N - n - 16 * j, v[j]);
-        } else {
-            epilogue<TO, KIND, 8>(g.e, v, m < g.M, m, n, g.N);
-        }
+        const f32x4(&one)[1][8] = reinterpret_cast<const f32x4(&)[1][8]>(acc[a]);
+        put_rows<TO, KIND, 1>(g, one, reinterpret_cast<char *>(lds) + wave * 8192, m0 + wave * 32 + a * 16, n0, split);
     }
 }
 
 // Adds the pieces of a cut product in order and takes the sum through the
-// epilogue: four columns a thread, 1024 columns of a row a workgroup.
+// epilogue: eight columns a thread, 2048 columns of a row a workgroup.
 template <int KIND, typename TO>
 __global__ __launch_bounds__(256) void lin_join_kernel(Gemm g)
 {
     const int64_t m = blockIdx.y;
-    const int n = (blockIdx.x * 256 + threadIdx.x) * 4;
-    float v[1][4] = {{0.f, 0.f, 0.f, 0.f}};
+    const int n = (blockIdx.x * 256 + threadIdx.x) * 8;
+    float v[8] = {};
     if (n < g.N) {
+        // rows of pieces are whole 32-byte runs
         const f32x4 *p = reinterpret_cast<const f32x4 *>(g.part + m * g.ldp + n);
         const int64_t step = g.M * g.ldp / 4;
-        f32x4 s = p[0];
-        for (int i = 1; i < g.splits; ++i)
-            s += p[i * step];
+        f32x4 lo = p[0], hi = p[1];
+        for (int i = 1; i < g.splits; ++i) {
+            lo += p[i * step];
+            hi += p[i * step + 1];
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            v[0][i] = s[i];
+        for (int i = 0; i < 4; ++i) {
+            v[i] = lo[i];
+            v[4 + i] = hi[i];
+        }
     }
-    epilogue<TO, KIND, 1>(g.e, v, n < g.N, m, n, g.N);
+    epilogue<TO, KIND>(g.e, v, n < g.N, m, n, g.N);
 }
 
-__global__ __launch_bounds__(256) void lin_join_db_kernel(const float *part, int64_t M, int splits, float *db, int accumulate)
+// Column sums of dz for db: eight columns a lane, 512 a workgroup, whose four
+// waves take every fourth row of its `per` rows and meet in LDS in order.
+// One slice of rows writes db, several leave partials.
+template <typename T>
+__global__ __launch_bounds__(256) void lin_db_kernel(const T *dz, int64_t ld, int64_t rows, int N, int per, float *part,
+                                                     float *db, int accumulate)
 {
-    const int64_t m = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (m >= M)
+    __shared__ float meet[4][512];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n = blockIdx.x * 512 + lane * 8;
+    const int64_t end = min<int64_t>(rows, (blockIdx.y + static_cast<int64_t>(1)) * per);
+    float s[8] = {};
+#pragma unroll 4
+    for (int64_t r = blockIdx.y * static_cast<int64_t>(per) + wave; r < end; r += 4) {
+        float v[8];
+        load8(dz + r * ld + n, N - n, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            s[i] += v[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        meet[wave][i * 64 + lane] = s[i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < 512; c += 256) {
+        const int at = (c & 7) * 64 + (c >> 3), col = blockIdx.x * 512 + c;
+        if (col < N) {
+            const float v = ((meet[0][at] + meet[1][at]) + meet[2][at]) + meet[3][at];
+            if (part)
+                part[static_cast<int64_t>(blockIdx.y) * N + col] = v;
+            else
+                db[col] = accumulate ? db[col] + v : v;
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void lin_join_db_kernel(const float *part, int N, int slices, float *db, int accumulate)
+{
+    const int n = blockIdx.x * 256 + threadIdx.x;
+    if (n >= N)
         return;
     float s = 0.f;
-    for (int i = 0; i < splits; ++i)
-        s += part[i * M + m];
-    db[m] = accumulate ? db[m] + s : s;
+    for (int i = 0; i < slices; ++i)
+        s += part[static_cast<int64_t>(i) * N + n];
+    db[n] = accumulate ? db[n] + s : s;
 }
 
 // rows == 0: the weight gradients are sums over nothing.
@@ -222,54 +242,162 @@ __global__ __launch_bounds__(256) void lin_apply_kernel(const T *x, int64_t ldx,
 
 inline size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 
-// How a product is cut, and what of the workspace it takes.
+// How a product is cut, and what of the workspace it takes: the pieces, db's
+// pieces, and copies of the operands that the bf16 kernel cannot read where
+// they are.
 struct Plan {
-    int tm, tn, splits, kchunk;
+    int tile, tm, tn, splits, kchunk;
+    int slices, slice;                      // of the rows, for db
     int64_t ldp;
-    size_t part, db;     // bytes of the pieces, and of db's
-    size_t bytes() const { return part + db; }
+    bool pack_a, pack_b;
+    int64_t lda, ldb;                       // row strides of the copies
+    size_t part, db, a, b;                  // bytes
+    size_t bytes() const { return part + db + a + b; }
 };
 
-inline Plan plan_of(int64_t M, int N, int K, bool weight)
+inline int up8(int n) { return (n + 7) / 8 * 8; }
+
+// A row operand keeps the sum's index in its rows, a col operand its own.
+struct Shape {
+    int64_t M;
+    int N, K;
+    bool acol, bcol;
+};
+inline Shape shape_of(EpiKind kind, int64_t rows, int n_in, int n_out)
+{
+    if (kind == kForward)
+        return {rows, n_out, n_in, false, false};
+    if (kind == kGate)
+        return {rows, n_in, n_out, false, true};
+    return {n_out, n_in, static_cast<int>(rows), true, true};
+}
+
+// Whether the bf16 kernel reads an operand where it is: 16-byte lines, whole
+// chunks of eight, offsets within a tile of under 2^32 bytes.
+inline bool readable(const Operand &o, bool col, int64_t inner)
+{
+    return aligned(o.p, 16) && o.ld % 8 == 0 && inner % 8 == 0 && o.ld * 2 * (col ? 64 : 256) < (1ll << 31);
+}
+
+inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bool fits_b)
 {
     Plan p{};
-    p.tm = static_cast<int>((M + kTile - 1) / kTile);
-    p.tn = (N + kTile - 1) / kTile;
+    const bool bf16 = dt == ACSC_BF16;
+    const int bk = bf16 ? 64 : kBK;
+    const int steps = (s.K + bk - 1) / bk;
+    p.tile = kTile;
+    if (bf16) {
+        const int64_t big = ((s.M + 255) / 256) * ((s.N + 255) / 256);
+        if (big >= 192)
+            p.tile = 256;
+    }
+    p.tm = static_cast<int>((s.M + p.tile - 1) / p.tile);
+    p.tn = (s.N + p.tile - 1) / p.tile;
     const int64_t tiles = static_cast<int64_t>(p.tm) * p.tn;
-    const int steps = (K + kBK - 1) / kBK;
-    int s = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(tiles, 1), steps / 4)));
-    const int per = (steps + s - 1) / s;
+    const int cut = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(512 / tiles, steps / 4)));
+    const int per = (steps + cut - 1) / cut;
     p.splits = (steps + per - 1) / per;
-    p.kchunk = per * kBK;
-    p.ldp = (N + 3) / 4 * 4;
-    p.part = p.splits > 1 ? up256(static_cast<size_t>(p.splits) * M * p.ldp * 4) : 0;
-    p.db = weight ? up256(static_cast<size_t>(p.splits) * M * 4) : 0;
+    p.kchunk = per * bk;
+    p.ldp = up8(s.N);
+    p.part = p.splits > 1 ? up256(static_cast<size_t>(p.splits) * s.M * p.ldp * 4) : 0;
+    if (kind == kWeight) {
+        // db's slices of at least 32 rows, up to about two workgroups a CU
+        const int64_t blocks = (s.M + 511) / 512;
+        p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(512 / blocks, s.K / 32)));
+        p.slice = (s.K + p.slices - 1) / p.slices;
+        p.slices = (s.K + p.slice - 1) / p.slice;
+        p.db = p.slices > 1 ? up256(static_cast<size_t>(p.slices) * s.M * 4) : 0;
+    }
+    if (bf16) {
+        p.pack_a = !fits_a;
+        p.pack_b = !fits_b;
+        p.lda = up8(s.acol ? static_cast<int>(s.M) : s.K);
+        p.ldb = up8(s.bcol ? s.N : s.K);
+        p.a = p.pack_a ? up256(static_cast<size_t>(s.acol ? s.K : s.M) * p.lda * 2) : 0;
+        p.b = p.pack_b ? up256(static_cast<size_t>(s.bcol ? s.K : s.N) * p.ldb * 2) : 0;
+    }
     return p;
 }
 
-template <bool ACOL, bool BCOL, int KIND, typename T, typename TO>
-int run_product(Gemm &g, const Plan &p, char *ws, float *db, hipStream_t st, const char *tag)
+template <bool ACOL, bool BCOL, int KIND, typename TO>
+void launch_f32(const Gemm &g, hipStream_t st, const char *tag)
 {
+    ACSC_LAUNCH(tag, (lin_f32_kernel<ACOL, BCOL, KIND, TO>), dim3(g.tm * g.tn, g.splits), dim3(256), 0, st, g);
+}
+
+template <int KIND, typename TO>
+void launch_join(const Gemm &g, hipStream_t st)
+{
+    ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO>), dim3((g.N + 2047) / 2048, static_cast<unsigned>(g.M)), dim3(256), 0,
+                st, g);
+}
+
+// The product, its pieces' sum and db; `out` is the type of the output.
+int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype dt, acsc_dtype out, char *ws, float *db,
+                hipStream_t st, const char *tag)
+{
+    g.M = s.M;
+    g.N = s.N;
+    g.K = s.K;
     g.tm = p.tm;
     g.tn = p.tn;
     g.splits = p.splits;
     g.kchunk = p.kchunk;
     g.ldp = p.ldp;
     g.part = reinterpret_cast<float *>(ws);
-    g.dbpart = db ? reinterpret_cast<float *>(ws + p.part) : nullptr;
-    ACSC_LAUNCH(tag, (lin_f32_kernel<T, ACOL, BCOL, KIND, TO>), dim3(p.tm * p.tn, p.splits), dim3(256), 0, st, g);
-    if (int rc = check_launch(tag))
-        return rc;
-    if (p.splits > 1) {
-        ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO>), dim3((g.N + 1023) / 1024, static_cast<unsigned>(g.M)), dim3(256),
-                    0, st, g);
-        if (int rc = check_launch("lin_join"))
+    if (db) {
+        float *part = p.slices > 1 ? reinterpret_cast<float *>(ws + p.part) : nullptr;
+        const dim3 grid(static_cast<unsigned>((g.M + 511) / 512), p.slices);
+        const int n = static_cast<int>(g.M);
+        if (dt == ACSC_BF16)
+            ACSC_LAUNCH("lin_db", lin_db_kernel<uint16_t>, grid, dim3(256), 0, st, static_cast<const uint16_t *>(g.A.p), g.A.ld,
+                        static_cast<int64_t>(s.K), n, p.slice, part, db, g.e.accumulate);
+        else
+            ACSC_LAUNCH("lin_db", lin_db_kernel<float>, grid, dim3(256), 0, st, static_cast<const float *>(g.A.p), g.A.ld,
+                        static_cast<int64_t>(s.K), n, p.slice, part, db, g.e.accumulate);
+        if (part)
+            ACSC_LAUNCH("lin_join_db", lin_join_db_kernel, dim3((n + 255) / 256), dim3(256), 0, st, part, n, p.slices, db,
+                        g.e.accumulate);
+        if (int rc = check_launch("lin_db"))
             return rc;
     }
-    if (db) {
-        ACSC_LAUNCH("lin_join_db", lin_join_db_kernel, dim3(static_cast<unsigned>((g.M + 255) / 256)), dim3(256), 0, st,
-                    g.dbpart, g.M, p.splits, db, g.e.accumulate);
-        return check_launch("lin_join_db");
+    if (dt == ACSC_BF16) {
+        char *copy = ws + p.part + p.db;
+        if (p.pack_a) {
+            if (int rc = lin_bf16_pack(g.A.p, g.A.ld, s.acol ? s.K : s.M, s.acol ? static_cast<int>(s.M) : s.K, copy, p.lda, st))
+                return rc;
+            g.A = {copy, p.lda};
+            copy += p.a;
+        }
+        if (p.pack_b) {
+            if (int rc = lin_bf16_pack(g.B.p, g.B.ld, s.bcol ? s.K : s.N, s.bcol ? s.N : s.K, copy, p.ldb, st))
+                return rc;
+            g.B = {copy, p.ldb};
+        }
+        if (int rc = lin_bf16_run(g, p.tile, kind, out, st, tag))
+            return rc;
+    } else {
+        if (kind == kForward)
+            launch_f32<false, false, kForward, float>(g, st, tag);
+        else if (kind == kGate)
+            launch_f32<false, true, kGate, float>(g, st, tag);
+        else if (out == ACSC_BF16)
+            launch_f32<true, true, kWeight, uint16_t>(g, st, tag);
+        else
+            launch_f32<true, true, kWeight, float>(g, st, tag);
+        if (int rc = check_launch(tag))
+            return rc;
+    }
+    if (p.splits > 1) {
+        const bool b = out == ACSC_BF16;
+        if (kind == kForward)
+            b ? launch_join<kForward, uint16_t>(g, st) : launch_join<kForward, float>(g, st);
+        else if (kind == kGate)
+            b ? launch_join<kGate, uint16_t>(g, st) : launch_join<kGate, float>(g, st);
+        else
+            b ? launch_join<kWeight, uint16_t>(g, st) : launch_join<kWeight, float>(g, st);
+        if (int rc = check_launch("lin_join"))
+            return rc;
     }
     return ACSC_OK;
 }
@@ -329,7 +457,7 @@ inline size_t recomputed_bytes(int64_t rows, int n_in, acsc_dtype dt)
 
 using namespace acsc;
 
-extern "C" int lin_workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, size_t *bytes)
+static int workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, bool any, size_t *bytes)
 {
     clear_error();
     if (int rc = check_layer(rows, n_in, n_out, dt))
@@ -337,15 +465,26 @@ extern "C" int lin_workspace_size(lin_op op, int64_t rows, int n_in, int n_out, 
     ACSC_CHECK_ARG(bytes, ACSC_EINVAL, "null pointer bytes");
     ACSC_CHECK_ARG(op == LIN_FORWARD || op == LIN_BACKWARD_INPUT || op == LIN_BACKWARD_WEIGHT, ACSC_EINVAL,
                    "unknown product %d", (int)op);
+    *bytes = 0;
     if (rows == 0)
-        *bytes = 0;
-    else if (op == LIN_FORWARD)
-        *bytes = plan_of(rows, n_out, n_in, false).bytes();
-    else if (op == LIN_BACKWARD_INPUT)
-        *bytes = plan_of(rows, n_in, n_out, false).bytes();
-    else
-        *bytes = plan_of(n_out, n_in, static_cast<int>(rows), true).bytes() + recomputed_bytes(rows, n_in, dt);
+        return ACSC_OK;
+    const EpiKind kind = op == LIN_FORWARD ? kForward : op == LIN_BACKWARD_INPUT ? kGate : kWeight;
+    const Shape s = shape_of(kind, rows, n_in, n_out);
+    const Operand best{nullptr, 8};
+    const bool a = !any && readable(best, s.acol, s.acol ? s.M : s.K);
+    const bool b = !any && readable(best, s.bcol, s.bcol ? s.N : s.K);
+    *bytes = plan_of(kind, s, dt, a, b).bytes() + (kind == kWeight ? recomputed_bytes(rows, n_in, dt) : 0);
     return ACSC_OK;
+}
+
+extern "C" int lin_workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, size_t *bytes)
+{
+    return workspace_size(op, rows, n_in, n_out, dt, false, bytes);
+}
+
+extern "C" int lin_workspace_size_unaligned(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, size_t *bytes)
+{
+    return workspace_size(op, rows, n_in, n_out, dt, true, bytes);
 }
 
 extern "C" int lin_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t rows, int n_in, int n_out, const void *W,
@@ -377,25 +516,19 @@ extern "C" int lin_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t r
     if (q)
         if (int rc = check_q8(q, rows, n_out))
             return rc;
-    const Plan p = plan_of(rows, n_out, n_in, false);
-    if (int rc = check_tiles(p))
-        return rc;
-    if (some)
-        if (int rc = check_ws(ws, ws_bytes, p.bytes()))
-            return rc;
     if (!some)
         return ACSC_OK;
     Gemm g{};
     g.A = {x, ld_x};
     g.B = {W, ld_w};
-    g.M = rows;
-    g.N = n_out;
-    g.K = n_in;
+    const Shape s = shape_of(kForward, rows, n_in, n_out);
+    const Plan p = plan_of(kForward, s, dt, readable(g.A, false, n_in), readable(g.B, false, n_in));
+    if (int rc = check_tiles(p))
+        return rc;
+    if (int rc = check_ws(ws, ws_bytes, p.bytes()))
+        return rc;
     g.e = Epi{y, ld_y, bias, residual, ld_res, z, ld_z, q8_of(q), act, 0};
-    char *w = static_cast<char *>(ws);
-    if (dt == ACSC_BF16)
-        return run_product<false, false, kForward, uint16_t, uint16_t>(g, p, w, nullptr, stream, "lin_forward");
-    return run_product<false, false, kForward, float, float>(g, p, w, nullptr, stream, "lin_forward");
+    return run_product(g, kForward, p, s, dt, dt, static_cast<char *>(ws), nullptr, stream, "lin_forward");
 }
 
 extern "C" int lin_backward_act(const void *dy, int64_t ld_dy, const void *z, int64_t ld_z, const q8_tensor *q,
@@ -449,25 +582,19 @@ extern "C" int lin_backward_input(const void *dz, int64_t ld_dz, acsc_dtype dt, 
     if (int rc = check_mat(dx, some, ld_dx, n_in, dt, "dx"))
         return rc;
     ACSC_CHECK_ARG(!some || (dx != dz && dx != W), ACSC_EINVAL, "dx must not overlap dz or W");
-    const Plan p = plan_of(rows, n_in, n_out, false);
-    if (int rc = check_tiles(p))
-        return rc;
-    if (some)
-        if (int rc = check_ws(ws, ws_bytes, p.bytes()))
-            return rc;
     if (!some)
         return ACSC_OK;
     Gemm g{};
     g.A = {dz, ld_dz};
     g.B = {W, ld_w};
-    g.M = rows;
-    g.N = n_in;
-    g.K = n_out;
+    const Shape s = shape_of(kGate, rows, n_in, n_out);
+    const Plan p = plan_of(kGate, s, dt, readable(g.A, false, n_out), readable(g.B, true, n_in));
+    if (int rc = check_tiles(p))
+        return rc;
+    if (int rc = check_ws(ws, ws_bytes, p.bytes()))
+        return rc;
     g.e = Epi{dx, ld_dx, nullptr, nullptr, 0, const_cast<void *>(z), ld_z, q8_of(q), act, 0};
-    char *w = static_cast<char *>(ws);
-    if (dt == ACSC_BF16)
-        return run_product<false, true, kGate, uint16_t, uint16_t>(g, p, w, nullptr, stream, "lin_backward_input");
-    return run_product<false, true, kGate, float, float>(g, p, w, nullptr, stream, "lin_backward_input");
+    return run_product(g, kGate, p, s, dt, dt, static_cast<char *>(ws), nullptr, stream, "lin_backward_input");
 }
 
 extern "C" int lin_backward_weight(const void *dz, int64_t ld_dz, const void *x, int64_t ld_x, const q8_tensor *q,
@@ -504,47 +631,37 @@ extern "C" int lin_backward_weight(const void *dz, int64_t ld_dz, const void *x,
                         static_cast<int64_t>(1), n_out);
         return check_launch("lin_zero");
     }
-    const Plan p = plan_of(n_out, n_in, static_cast<int>(rows), true);
+    // the activation, or the checkpoint's values, whole: read once here, and
+    // by the product many times.  Its rows end at a multiple of eight, so the
+    // product reads it where it is.
+    const bool again = q || act != ACSC_ACT_NONE;
+    const size_t whole = again ? recomputed_bytes(rows, n_in, dt) : 0;
+    const Shape s = shape_of(kWeight, rows, n_in, n_out);
+    Gemm g{};
+    g.A = {dz, ld_dz};
+    g.B = again ? Operand{ws, up8(n_in)} : Operand{x, ld_x};
+    const Plan p = plan_of(kWeight, s, dt, readable(g.A, true, n_out), again || readable(g.B, true, n_in));
     if (int rc = check_tiles(p))
         return rc;
-    const size_t again = recomputed_bytes(rows, n_in, dt);
-    if (int rc = check_ws(ws, ws_bytes, p.bytes() + again))
+    if (int rc = check_ws(ws, ws_bytes, p.bytes() + whole))
         return rc;
-    char *w = static_cast<char *>(ws);
-    // the activation, or the checkpoint's values, whole: read once here, and
-    // by the product many times
-    if (q || act != ACSC_ACT_NONE) {
-        void *whole = w + p.bytes();
-        const int64_t ld = (n_in + 7) / 8 * 8;
+    if (again) {
         int rc = ACSC_OK;
         if (q) {
-            rc = q8_decode_run(q8_of(q), rows, n_in, act, whole, dt, ld, stream);
+            rc = q8_decode_run(q8_of(q), rows, n_in, act, ws, dt, g.B.ld, stream);
         } else {
             const int64_t blocks = std::min<int64_t>((rows * ((n_in + 7) / 8) + 255) / 256, 1 << 20);
             if (dt == ACSC_BF16)
                 ACSC_LAUNCH("lin_apply", lin_apply_kernel<uint16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
-                            static_cast<const uint16_t *>(x), ld_x, rows, n_in, act, static_cast<uint16_t *>(whole), ld);
+                            static_cast<const uint16_t *>(x), ld_x, rows, n_in, act, static_cast<uint16_t *>(ws), g.B.ld);
             else
                 ACSC_LAUNCH("lin_apply", lin_apply_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
-                            static_cast<const float *>(x), ld_x, rows, n_in, act, static_cast<float *>(whole), ld);
+                            static_cast<const float *>(x), ld_x, rows, n_in, act, static_cast<float *>(ws), g.B.ld);
             rc = check_launch("lin_apply");
         }
         if (rc)
             return rc;
-        x = whole;
-        ld_x = ld;
     }
-    Gemm g{};
-    g.A = {dz, ld_dz};
-    g.B = {x, ld_x};
-    g.M = n_out;
-    g.N = n_in;
-    g.K = static_cast<int>(rows);
     g.e = Epi{dW, ld_dw, nullptr, nullptr, 0, nullptr, 0, q8_of(nullptr), ACSC_ACT_NONE, accumulate};
-    const char *tag = "lin_backward_weight";
-    if (dt == ACSC_BF16)
-        return dw_dt == ACSC_BF16 ? run_product<true, true, kWeight, uint16_t, uint16_t>(g, p, w, db, stream, tag)
-                                  : run_product<true, true, kWeight, uint16_t, float>(g, p, w, db, stream, tag);
-    return dw_dt == ACSC_BF16 ? run_product<true, true, kWeight, float, uint16_t>(g, p, w, db, stream, tag)
-                              : run_product<true, true, kWeight, float, float>(g, p, w, db, stream, tag);
+    return run_product(g, kWeight, p, s, dt, dw_dt, static_cast<char *>(ws) + whole, db, stream, "lin_backward_weight");
 }

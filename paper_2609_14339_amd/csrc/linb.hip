@@ -1,0 +1,350 @@
+// The bf16 product of the linear layers on v_mfma_f32_16x16x32_bf16.
+//
+// A workgroup takes a T x T tile of C (T = 256: eight waves of 64 rows by 128
+// columns; T = 128: four of 32 by 128) in steps of 64 along the sum.  Each
+// step's tiles of A and B come straight from memory into LDS
+// (global_load_lds_dwordx4), into two stages in turn; no register holds them
+// on the way.  An operand stays in LDS as it is stored: lines of 64 k (row) or
+// k-lines of 64 own indices (col), 128 bytes a line, its eight 16-byte chunks
+// XOR-swizzled by the line.  Fragments are 16-byte reads of row operands and
+// pairs of transposing 8-byte reads of col ones, so all three products of a
+// layer run at the stored layouts.  The matrix instruction's first operand is
+// B's side: a lane then holds four consecutive columns of a row.
+//
+// Half a step of fragments is read ahead: while the first half of a step is
+// multiplied the second is read; then the wave waits for its part of the next
+// step's DMA, meets the others, sends the DMA after that into the stage just
+// read, and multiplies the second half while the next step's first is read.
+#include "lin.h"
+
+#include <type_traits>
+
+namespace acsc {
+namespace {
+
+typedef __attribute__((__vector_size__(8 * sizeof(short)))) short bf16x8;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+
+constexpr int kBK = 64;
+
+// What lanes past the end of the sum read in its last step.
+__device__ const uint4 g_zeros = {0, 0, 0, 0};
+
+// As for the streaming passes: neither the 16-byte reads of 16 lines nor the
+// transposed 8-byte reads of four lines conflict.
+__device__ __forceinline__ int swz(int line) { return ((line >> 1) ^ line) & 7; }
+
+// The LDS DMA of one line group of A and one of B: 16 bytes a lane from base +
+// off (bytes) to lds + 16 lane.  lds is wave-uniform and goes through M0,
+// which needs a wait state after it is written; M0 is left as it was.
+__device__ __forceinline__ void dma16(const char *a, uint32_t aoff, uint32_t alds, const char *b, uint32_t boff,
+                                      uint32_t blds)
+{
+    uint32_t saved;
+    asm volatile("s_mov_b32 %0, m0\n\t"
+                 "s_mov_b32 m0, %3\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dwordx4 %1, %2\n\t"
+                 "s_mov_b32 m0, %6\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dwordx4 %4, %5\n\t"
+                 "s_mov_b32 m0, %0"
+                 : "=&s"(saved)
+                 : "v"(aoff), "s"(a), "s"(alds), "v"(boff), "s"(b), "s"(blds)
+                 : "memory");
+}
+__device__ __forceinline__ void dma16(const void *a, uint32_t alds, const void *b, uint32_t blds)
+{
+    uint32_t saved;
+    asm volatile("s_mov_b32 %0, m0\n\t"
+                 "s_mov_b32 m0, %2\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dwordx4 %1, off\n\t"
+                 "s_mov_b32 m0, %4\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dwordx4 %3, off\n\t"
+                 "s_mov_b32 m0, %0"
+                 : "=&s"(saved)
+                 : "v"(a), "s"(alds), "v"(b), "s"(blds)
+                 : "memory");
+}
+
+// One operand's side of the DMA: N = T / 32 instructions a wave and step.
+// Instruction d of the T / 8 moves lines 8 d .. 8 d + 7: line l of a row
+// operand is its index l, chunk c its k = 8 c ..; line l of a col operand is
+// k = l % 64 of the indices 64 (l / 64) .., chunk c eight of them.  Indices
+// past the end are read as the last ones (their results are not stored).
+template <bool COL, int T>
+struct Side {
+    static constexpr int N = 4;
+    uint32_t off[N];       // bytes from the step's base
+    const char *base;      // the tile's first index at the step's first k
+    int64_t step;          // bytes from one step's base to the next
+
+    __device__ __forceinline__ void init(const Operand &o, int64_t i0, int64_t ni, int k0, int wave)
+    {
+        const int lane = threadIdx.x & 63;
+        const int64_t ld = o.ld * 2;
+        base = static_cast<const char *>(o.p) + (COL ? k0 * ld + i0 * 2 : i0 * ld + static_cast<int64_t>(k0) * 2);
+        step = COL ? kBK * ld : kBK * 2;
+        const int last = static_cast<int>(min<int64_t>(ni - i0, T)) - 1;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int d = wave * N + i, line = d * 8 + (lane >> 3);
+            const int c = (lane & 7) ^ swz(COL ? line & 63 : line);
+            if (COL) {
+                const int x = (line >> 6) * 64 + c * 8;
+                off[i] = static_cast<uint32_t>((line & 63) * ld + min(x, last & ~7) * 2);
+            } else {
+                off[i] = static_cast<uint32_t>(min(line, last) * ld + c * 16);
+            }
+        }
+    }
+    // What instruction i reads in the last, partial step of `left` k: zeros
+    // past the end of the sum.  A row operand is readable, and zero, up to the
+    // next multiple of eight.
+    __device__ __forceinline__ const void *tail(int i, int64_t s, int left, int wave) const
+    {
+        const int lane = threadIdx.x & 63, line = (wave * N + i) * 8 + (lane >> 3);
+        const int k = COL ? line & 63 : ((lane & 7) ^ swz(line)) * 8;
+        return k < left ? static_cast<const void *>(base + s * step + off[i]) : static_cast<const void *>(&g_zeros);
+    }
+};
+
+// Fragment t of 16 indices, k half kh of a stage: lane L holds index L % 16,
+// k = 32 kh + 8 (L / 16) .. + 7.
+template <bool COL>
+struct Frag {
+    uint32_t row[2];        // row: byte offset per k half
+    uint32_t col[4][2];     // col: per 16 indices of a 64-wide block, k lines + 0 and + 4
+    __device__ __forceinline__ void init(int t0)   // the wave's first fragment of its 64-wide block
+    {
+        const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+        if (!COL) {
+#pragma unroll
+            for (int kh = 0; kh < 2; ++kh)
+                row[kh] = l16 * 128 + 16 * ((kh * 4 + g) ^ swz(l16));
+        } else {
+            // ds_read_b64_tr_b16: result lane L, element e of each group of 16
+            // lanes = element L % 4 of what lane 4 e + L / 4 read; lane 4 e + q
+            // reads indices 4 q .. 4 q + 3 of k-line e.
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int line = g * 8 + (l16 >> 2) + 4 * h, x = ((t0 + t) & 3) * 16 + (l16 & 3) * 4;
+                    col[t][h] = line * 128 + 16 * ((x >> 3) ^ swz(line)) + (x & 7) * 2;
+                }
+        }
+    }
+    __device__ __forceinline__ bf16x8 read(const unsigned char *op, int t, int kh) const
+    {
+        if (!COL)
+            return *reinterpret_cast<const bf16x8 *>(op + row[kh] + t * 2048);
+        const unsigned char *p = op + (t >> 2) * 8192 + kh * 4096;
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>((lds_byte *)(p + col[t & 3][0])));
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>((lds_byte *)(p + col[t & 3][1])));
+        return bf16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    }
+};
+
+template <int T, bool ACOL, bool BCOL, int KIND, typename TO>
+__global__ __launch_bounds__(2 * T, 2) void lin_bf16_kernel(Gemm g)
+{
+    extern __shared__ __align__(1024) unsigned char smem[];
+    constexpr int WN = T / 128;                 // waves along the columns
+    constexpr int FA = T / 64;                  // 16-row fragments of a wave, four waves along the rows
+    constexpr int OP = T * 128;                 // bytes of one operand's stage
+    constexpr int STAGE = 2 * OP;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+
+    // Workgroups go to the eight XCDs in turn; each XCD takes a run of tiles
+    // of its own, in columns of eight tiles, so that what its CUs read
+    // together stays in its L2.
+    int64_t id = blockIdx.x;
+    const int64_t tiles = static_cast<int64_t>(g.tm) * g.tn;
+    {
+        const int64_t q = tiles / 8, r = tiles % 8, x = id % 8;
+        id = x * q + min(x, r) + id / 8;
+    }
+    const int64_t band = id / (8 * g.tn), in = id - band * 8 * g.tn;
+    const int height = static_cast<int>(min<int64_t>(g.tm - band * 8, 8));
+    const int tile_m = static_cast<int>(band * 8 + in % height), tile_n = static_cast<int>(in / height);
+    const int split = blockIdx.y;
+    const int64_t m0 = static_cast<int64_t>(tile_m) * T;
+    const int n0 = tile_n * T;
+    const int kbeg = split * g.kchunk, kend = min(g.K, kbeg + g.kchunk);
+    const int nsteps = (kend - kbeg + kBK - 1) / kBK;
+
+    Side<ACOL, T> sa;
+    Side<BCOL, T> sb;
+    sa.init(g.A, m0, g.M, kbeg, wave);
+    sb.init(g.B, n0, g.N, kbeg, wave);
+    Frag<ACOL> fra;
+    Frag<BCOL> frb;
+    fra.init(FA == 4 ? 0 : 2 * (wm & 1));
+    frb.init(0);
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte *)smem));
+
+    constexpr int N = 4;                        // DMA instructions of an operand's step and wave
+    constexpr int NI = N / FA, NR = (8 + FA) / FA;   // of them, and fragments, beside eight products
+    // instruction i of step s, which is whole
+    const auto issue = [&](int s, int i) {
+        const uint32_t to = lds0 + (s & 1) * STAGE + (wave * N + i) * 1024;
+        dma16(sa.base + s * sa.step, sa.off[i], to, sb.base + s * sb.step, sb.off[i], to + OP);
+    };
+    // the same of any step
+    const auto issue_any = [&](int s, int i) {
+        const int left = kend - kbeg - s * kBK;
+        if (left >= kBK) {
+            issue(s, i);
+        } else if (left > 0) {
+            const uint32_t to = lds0 + (s & 1) * STAGE + (wave * N + i) * 1024;
+            dma16(sa.tail(i, s, left, wave), to, sb.tail(i, s, left, wave), to + OP);
+        }
+    };
+    f32x4 acc[FA][8];
+#pragma unroll
+    for (int a = 0; a < FA; ++a)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            acc[a][j] = f32x4{0, 0, 0, 0};
+    // fragments of k half kh of a stage: eight of B's side, then FA of A's
+    struct Frags {
+        bf16x8 f[8 + FA];
+    };
+    const auto read = [&](Frags &f, int stage, int kh, int r) {
+        const unsigned char *base = smem + stage * STAGE;
+        if (r < 8)
+            f.f[r] = frb.read(base + OP + wn * 16384, r, kh);
+        else
+            f.f[r] = fra.read(base + (ACOL ? (wm * FA / 4) * 8192 : wm * FA * 2048), r - 8, kh);
+    };
+    // eight products at a time, with what goes out beside them
+    const auto multiply = [&](const Frags &f, int a) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            acc[a][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.f[j], f.f[8 + a], acc[a][j], 0, 0, 0);
+    };
+    const auto meet = [&]() {
+        // this wave's DMA has landed and its LDS reads are done; then everyone's
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    Frags f0, f1;
+    const auto step = [&](int s, auto whole) {
+#pragma unroll
+        for (int a = 0; a < FA; ++a) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+                read(f1, s & 1, 1, a * NR + r);
+            multiply(f0, a);
+        }
+        meet();
+#pragma unroll
+        for (int a = 0; a < FA; ++a) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+                if (whole)
+                    issue(s + 2, a * NI + i);
+                else
+                    issue_any(s + 2, a * NI + i);
+            // past the last step this reads the other stage, unused
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+                read(f0, (s + 1) & 1, 0, a * NR + r);
+            multiply(f1, a);
+        }
+    };
+
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        issue_any(0, i);
+    meet();
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        issue_any(1, i);
+#pragma unroll
+    for (int r = 0; r < 8 + FA; ++r)
+        read(f0, 0, 0, r);
+    const int whole = (kend - kbeg) / kBK;
+    int s = 0;
+    for (; s + 2 < whole; ++s)
+        step(s, std::true_type{});
+    for (; s < nsteps; ++s)
+        step(s, std::false_type{});
+    meet();
+    constexpr int NA = 2;
+    char *own = reinterpret_cast<char *>(smem) + wave * NA * 8192;
+#pragma unroll
+    for (int a = 0; a < FA; a += NA)
+        put_rows<TO, KIND, NA>(g, reinterpret_cast<const f32x4(&)[NA][8]>(acc[a]), own, m0 + (wm * FA + a) * 16,
+                               n0 + wn * 128, split);
+}
+
+// A copy of an operand whose rows are 16-byte aligned and filled with zeros
+// up to a multiple of eight.
+__global__ __launch_bounds__(256) void lin_pack_kernel(const uint16_t *x, int64_t ldx, int64_t rows, int cols, uint16_t *y,
+                                                       int64_t ldy)
+{
+    const int chunks = static_cast<int>(ldy / 8);
+    const int64_t total = rows * chunks;
+    for (int64_t w = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; w < total; w += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t row = w / chunks;
+        const int col = static_cast<int>(w - row * chunks) * 8;
+        const uint16_t *p = x + row * ldx + col;
+        Bf8Any c = {{0, 0, 0, 0}};
+        if (cols - col >= 8) {
+            c = *reinterpret_cast<const Bf8Any *>(p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (col + i < cols)
+                    c.w[i / 2] |= static_cast<uint32_t>(p[i]) << (16 * (i & 1));
+        }
+        *reinterpret_cast<Bf8Any *>(y + row * ldy + col) = c;
+    }
+}
+
+template <int T, bool ACOL, bool BCOL, int KIND, typename TO>
+int launch(const Gemm &g, hipStream_t st, const char *tag)
+{
+    constexpr size_t bytes = 2 * 2 * T * 128;
+    if (int rc = allow_lds(lin_bf16_kernel<T, ACOL, BCOL, KIND, TO>, bytes))
+        return rc;
+    ACSC_LAUNCH(tag, (lin_bf16_kernel<T, ACOL, BCOL, KIND, TO>), dim3(g.tm * g.tn, g.splits), dim3(2 * T), bytes, st, g);
+    return check_launch(tag);
+}
+
+template <int T>
+int launch_kind(const Gemm &g, EpiKind kind, acsc_dtype out, hipStream_t st, const char *tag)
+{
+    if (kind == kForward)
+        return launch<T, false, false, kForward, uint16_t>(g, st, tag);
+    if (kind == kGate)
+        return launch<T, false, true, kGate, uint16_t>(g, st, tag);
+    return out == ACSC_BF16 ? launch<T, true, true, kWeight, uint16_t>(g, st, tag)
+                            : launch<T, true, true, kWeight, float>(g, st, tag);
+}
+
+}  // namespace
+
+int lin_bf16_pack(const void *x, int64_t ldx, int64_t rows, int cols, void *y, int64_t ldy, hipStream_t st)
+{
+    const int64_t blocks = std::min<int64_t>((rows * (ldy / 8) + 255) / 256, 1 << 20);
+    ACSC_LAUNCH("lin_pack", lin_pack_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st,
+                static_cast<const uint16_t *>(x), ldx, rows, cols, static_cast<uint16_t *>(y), ldy);
+    return check_launch("lin_pack");
+}
+
+int lin_bf16_run(const Gemm &g, int tile, EpiKind kind, acsc_dtype out, hipStream_t st, const char *tag)
+{
+    return tile == 256 ? launch_kind<256>(g, kind, out, st, tag) : launch_kind<128>(g, kind, out, st, tag);
+}
+
+}  // namespace acsc
