@@ -42,7 +42,7 @@ struct Gemm {
     int tm, tn;       // tiles along M and N
     int splits;       // pieces along K, kchunk each
     int kchunk;
-    float *part;      // splits > 1: piece s at part + s * M * ldp
+    float *part;      // piece s at part + s * M * ldp; nullptr: one piece, through the epilogue
     int64_t ldp;
     Epi e;
 };
@@ -50,19 +50,17 @@ struct Gemm {
 // Eight values of row m at columns n .. n + 7 (n a multiple of 8) through the
 // epilogue.  Sixteen lanes of the wave, aligned, hold one group of 128
 // columns of a row, and every lane of the wave calls it (`on`: the row
-// exists); T is the type of y, z, bias and residual.
+// exists); T is the type of y, z, bias and residual, `bias` the eight columns'
+// (zeros without one).
 template <typename T, int KIND>
-__device__ __forceinline__ void epilogue(const Epi &e, float (&v)[8], bool on, int64_t m, int n, int N)
+__device__ __forceinline__ void epilogue(const Epi &e, float (&v)[8], const float (&bias)[8], bool on, int64_t m, int n,
+                                         int N)
 {
     const int left = on ? N - n : 0;
     if (KIND == kForward) {
-        if (e.bias) {
-            float b[8];
-            load8(static_cast<const T *>(e.bias) + n, left, b);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                v[i] += b[i];
-        }
+        for (int i = 0; i < 8; ++i)
+            v[i] += bias[i];
         if (e.z)
             store8(static_cast<T *>(e.z) + m * e.ldz + n, left, v);
         if (e.q.codes) {
@@ -78,11 +76,7 @@ __device__ __forceinline__ void epilogue(const Epi &e, float (&v)[8], bool on, i
             if (left > 0 && n % kGroup == 0)
                 e.q.scales[m * e.q.lds + n / kGroup] = scale;
         }
-        if (e.act != ACSC_ACT_NONE) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                v[i] = act_value(v[i], e.act);
-        }
+        apply_act<T>(v, e.act);
         if (e.res) {
             float b[8];
             load8(static_cast<const T *>(e.res) + m * e.ldr + n, left, b);
@@ -99,9 +93,7 @@ __device__ __forceinline__ void epilogue(const Epi &e, float (&v)[8], bool on, i
             load_codes(e.q.codes + m * e.q.ldc + n, left, e.q.scales[m * e.q.lds + n / kGroup], z);
         else
             load8(static_cast<const T *>(e.z) + m * e.ldz + n, left, z);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v[i] *= act_slope(z[i], e.act);
+        apply_slope<T>(v, z, e.act);
     }
     T *y = static_cast<T *>(e.y) + m * e.ldy + n;
     if (KIND == kWeight && e.accumulate) {
@@ -112,6 +104,13 @@ __device__ __forceinline__ void epilogue(const Epi &e, float (&v)[8], bool on, i
             v[i] += o[i];
     }
     store8(y, left, v);
+}
+
+template <typename T, int KIND>
+__device__ __forceinline__ void load_bias(const Epi &e, int n, int N, float (&b)[8])
+{
+    if (KIND == kForward)
+        load8(static_cast<const T *>(e.bias) + n, e.bias ? N - n : 0, b);
 }
 
 // A wave's accumulators of 16 NA rows by 128 columns through the epilogue, or
@@ -136,6 +135,10 @@ __device__ __forceinline__ void put_rows(const Gemm &g, const f32x4 (&acc)[NA][8
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    const int n = n0 + (lane & 15) * 8;
+    float bias[8];
+    if (!g.part)
+        load_bias<T, KIND>(g.e, n, g.N, bias);
 #pragma unroll 1
     for (int r = 0; r < NA * 4; ++r) {
         const int row = r * 4 + (lane >> 4), c = (lane & 15) * 2;
@@ -143,11 +146,10 @@ __device__ __forceinline__ void put_rows(const Gemm &g, const f32x4 (&acc)[NA][8
         const f32x4 hi = *reinterpret_cast<const f32x4 *>(lds + row * 512 + ((c + 1) ^ (row & 31)) * 16);
         float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
         const int64_t m = m0 + row;
-        const int n = n0 + (lane & 15) * 8;
-        if (g.splits > 1)
+        if (g.part)
             store8(g.part + (split * g.M + m) * g.ldp + n, m < g.M ? g.N - n : 0, v);
         else
-            epilogue<T, KIND>(g.e, v, m < g.M, m, n, g.N);
+            epilogue<T, KIND>(g.e, v, bias, m < g.M, m, n, g.N);
     }
 }
 

@@ -6,11 +6,17 @@ namespace acsc {
 
 int q8_decode_run(const Q8 &q, int64_t rows, int H, int act, void *y, acsc_dtype dt, int64_t ldy, hipStream_t st);
 int lin_bf16_pack(const void *x, int64_t ldx, int64_t rows, int cols, void *y, int64_t ldy, hipStream_t st);
+int lin_few_run(const Gemm &g, acsc_dtype dt, hipStream_t st, const char *tag);
 int lin_bf16_run(const Gemm &g, int tile, EpiKind kind, acsc_dtype out, hipStream_t st, const char *tag);
 
 namespace {
 
 constexpr int kTile = 128, kBK = 32;
+
+// Tokens up to which a forward product reads W once and unstaged.  4096 ->
+// 14336, 1 / 8 / 16 / 32 tokens, us: bf16 24.1, 28.3, 34.9, 48.5 against 31 by
+// tiles for each; fp32 53, 60, 68, 103 against 170.
+inline int few_tokens(bool bf16) { return bf16 ? 8 : 32; }
 
 // The fp32 product on v_mfma_f32_16x16x4_f32: 128 x 128 tiles, four waves of
 // 32 rows by 128 columns, so that a wave holds whole checkpoint groups.  The
@@ -122,25 +128,29 @@ __global__ __launch_bounds__(256) void lin_f32_kernel(Gemm g)
 template <int KIND, typename TO>
 __global__ __launch_bounds__(256) void lin_join_kernel(Gemm g)
 {
-    const int64_t m = blockIdx.y;
     const int n = (blockIdx.x * 256 + threadIdx.x) * 8;
-    float v[8] = {};
-    if (n < g.N) {
-        // rows of pieces are whole 32-byte runs
-        const f32x4 *p = reinterpret_cast<const f32x4 *>(g.part + m * g.ldp + n);
-        const int64_t step = g.M * g.ldp / 4;
-        f32x4 lo = p[0], hi = p[1];
-        for (int i = 1; i < g.splits; ++i) {
-            lo += p[i * step];
-            hi += p[i * step + 1];
-        }
+    float bias[8];
+    load_bias<TO, KIND>(g.e, n, g.N, bias);
+    for (int64_t m = blockIdx.y; m < g.M; m += gridDim.y) {
+        float v[8] = {};
+        if (n < g.N) {
+            // rows of pieces are whole 32-byte runs
+            const f32x4 *p = reinterpret_cast<const f32x4 *>(g.part + m * g.ldp + n);
+            const int64_t step = g.M * g.ldp / 4;
+            f32x4 lo = p[0], hi = p[1];
+#pragma unroll 4
+            for (int i = 1; i < g.splits; ++i) {
+                lo += p[i * step];
+                hi += p[i * step + 1];
+            }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[i] = lo[i];
-            v[4 + i] = hi[i];
+            for (int i = 0; i < 4; ++i) {
+                v[i] = lo[i];
+                v[4 + i] = hi[i];
+            }
         }
+        epilogue<TO, KIND>(g.e, v, bias, n < g.N, m, n, g.N);
     }
-    epilogue<TO, KIND>(g.e, v, n < g.N, m, n, g.N);
 }
 
 // Column sums of dz for db: eight columns a lane, 512 a workgroup, whose four
@@ -215,9 +225,7 @@ __global__ __launch_bounds__(256) void lin_act_kernel(const T *dy, int64_t lddy,
             load_codes(q.codes + row * q.ldc + col, N - col, q.scales[row * q.lds + col / kGroup], v);
         else
             load8(z + row * ldz + col, N - col, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            g[i] *= act_slope(v[i], act);
+        apply_slope<T>(g, v, act);
         store8(dz + row * lddz + col, N - col, g);
     }
 }
@@ -233,9 +241,7 @@ __global__ __launch_bounds__(256) void lin_apply_kernel(const T *x, int64_t ldx,
         const int col = static_cast<int>(w - row * chunks) * 8;
         float v[8];
         load8(x + row * ldx + col, N - col, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v[i] = act_value(v[i], act);
+        apply_act<T>(v, act);
         store8(y + row * ldy + col, N - col, v);
     }
 }
@@ -246,6 +252,7 @@ inline size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 // pieces, and copies of the operands that the bf16 kernel cannot read where
 // they are.
 struct Plan {
+    bool few;                               // the product for few tokens
     int tile, tm, tn, splits, kchunk;
     int slices, slice;                      // of the rows, for db
     int64_t ldp;
@@ -279,25 +286,68 @@ inline bool readable(const Operand &o, bool col, int64_t inner)
     return aligned(o.p, 16) && o.ld % 8 == 0 && inner % 8 == 0 && o.ld * 2 * (col ? 64 : 256) < (1ll << 31);
 }
 
+// Tile and pieces of the sum, by the least estimated time.  A round is what
+// the card runs at once: a workgroup of a 256 tile per CU, two of a 128 tile
+// (or of an fp32 tile).  Measured on bf16 products, us: a 256 tile takes 1.5 a
+// step of 64 and 5 beside them (4096 x 2048 -> 8192: 56 a round of 32 steps);
+// a 128 tile 1.0 and 3 with a second one on its CU (2048 x 2048 -> 8192: 34.5
+// a round), 0.65 alone; the pieces' sum 4 for the launch and their bytes,
+// written and read, at 4.5 TB/s.  (256-tiles only where they fill a round,
+// without this: 2048 x 2048 -> 8192 in 99 us, with it 69.)
+struct Cut {
+    int tile, splits, per;
+};
+inline Cut cut_of(const Shape &s, int steps, bool bf16)
+{
+    Cut best{};
+    double least = 0;
+    for (int tile = bf16 ? 256 : 128; tile >= 128; tile -= 128) {
+        const int64_t tiles = ((s.M + tile - 1) / tile) * ((s.N + tile - 1) / tile);
+        const double step = !bf16 ? 6.0 : tile == 256 ? 1.5 : 1.0, alone = !bf16 ? 3.5 : tile == 256 ? 1.5 : 0.65;
+        const double edge = tile == 256 ? 5 : 3;
+        const int slots = tile == 256 ? 256 : 512;
+        for (int want = 1; want == 1 || (want <= 64 && steps / want >= 4 && tiles * want <= 2048); want += want < 8 ? 1 : 8) {
+            const int per = (steps + want - 1) / want, n = (steps + per - 1) / per;
+            const int64_t groups = tiles * n, rest = groups % slots;
+            double t = static_cast<double>(groups / slots) * (per * step + edge);
+            if (rest)
+                t += per * (rest <= 256 ? alone : step) + edge;
+            if (n > 1)
+                t += 4 + n * static_cast<double>(s.M) * s.N * 8 / 4.5e6;
+            if (least == 0 || t < least) {
+                least = t;
+                best = Cut{tile, n, per};
+            }
+        }
+    }
+    return best;
+}
+
 inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bool fits_b)
 {
     Plan p{};
     const bool bf16 = dt == ACSC_BF16;
     const int bk = bf16 ? 64 : kBK;
     const int steps = (s.K + bk - 1) / bk;
-    p.tile = kTile;
-    if (bf16) {
-        const int64_t big = ((s.M + 255) / 256) * ((s.N + 255) / 256);
-        if (big >= 192)
-            p.tile = 256;
+    if (kind == kForward && s.M <= few_tokens(bf16)) {
+        // 16 outputs a workgroup: a cut only where they fill half the CUs at
+        // most, at two rounds of eight lines a piece
+        const int groups = (s.N + 15) / 16, round = 8 * 128 / static_cast<int>(dtype_size(dt)), rounds = (s.K + round - 1) / round;
+        const int want = groups >= 128 ? 1 : std::max(1, std::min((255 + groups) / groups, rounds / 2));
+        const int per = (rounds + want - 1) / want;
+        p.few = true;
+        p.splits = (rounds + per - 1) / per;
+        p.kchunk = per * round;
+        p.ldp = up8(s.N);
+        p.part = up256(static_cast<size_t>(p.splits) * s.M * p.ldp * 4);
+        return p;
     }
+    const Cut c = cut_of(s, steps, bf16);
+    p.tile = c.tile;
     p.tm = static_cast<int>((s.M + p.tile - 1) / p.tile);
     p.tn = (s.N + p.tile - 1) / p.tile;
-    const int64_t tiles = static_cast<int64_t>(p.tm) * p.tn;
-    const int cut = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(512 / tiles, steps / 4)));
-    const int per = (steps + cut - 1) / cut;
-    p.splits = (steps + per - 1) / per;
-    p.kchunk = per * bk;
+    p.splits = c.splits;
+    p.kchunk = c.per * bk;
     p.ldp = up8(s.N);
     p.part = p.splits > 1 ? up256(static_cast<size_t>(p.splits) * s.M * p.ldp * 4) : 0;
     if (kind == kWeight) {
@@ -328,8 +378,8 @@ void launch_f32(const Gemm &g, hipStream_t st, const char *tag)
 template <int KIND, typename TO>
 void launch_join(const Gemm &g, hipStream_t st)
 {
-    ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO>), dim3((g.N + 2047) / 2048, static_cast<unsigned>(g.M)), dim3(256), 0,
-                st, g);
+    ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO>), dim3((g.N + 2047) / 2048, static_cast<unsigned>(std::min<int64_t>(g.M, 65535))),
+                dim3(256), 0, st, g);
 }
 
 // The product, its pieces' sum and db; `out` is the type of the output.
@@ -344,7 +394,9 @@ int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype
     g.splits = p.splits;
     g.kchunk = p.kchunk;
     g.ldp = p.ldp;
-    g.part = reinterpret_cast<float *>(ws);
+    // a piece goes through memory if there are more, or if its workgroups hold
+    // no whole checkpoint groups
+    g.part = p.splits > 1 || (p.few && g.e.q.codes) ? reinterpret_cast<float *>(ws) : nullptr;
     if (db) {
         float *part = p.slices > 1 ? reinterpret_cast<float *>(ws + p.part) : nullptr;
         const dim3 grid(static_cast<unsigned>((g.M + 511) / 512), p.slices);
@@ -361,7 +413,10 @@ int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype
         if (int rc = check_launch("lin_db"))
             return rc;
     }
-    if (dt == ACSC_BF16) {
+    if (p.few) {
+        if (int rc = lin_few_run(g, dt, st, tag))
+            return rc;
+    } else if (dt == ACSC_BF16) {
         char *copy = ws + p.part + p.db;
         if (p.pack_a) {
             if (int rc = lin_bf16_pack(g.A.p, g.A.ld, s.acol ? s.K : s.M, s.acol ? static_cast<int>(s.M) : s.K, copy, p.lda, st))
@@ -388,7 +443,7 @@ int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype
         if (int rc = check_launch(tag))
             return rc;
     }
-    if (p.splits > 1) {
+    if (g.part) {
         const bool b = out == ACSC_BF16;
         if (kind == kForward)
             b ? launch_join<kForward, uint16_t>(g, st) : launch_join<kForward, float>(g, st);

@@ -1,0 +1,149 @@
+// A linear layer's forward product for few tokens (bf16 up to 8, fp32 up to
+// 32): the weights are read once, straight into the matrix cores' lanes, at
+// whatever stride and alignment they have.
+//
+// What bounds it is the weights' bytes: no LDS, no barrier on the way.  A
+// workgroup of eight waves takes 16 outputs; in each of its 16 rows of W the
+// waves take the 128-byte lines in turn, four lines (eight 16-byte loads a
+// lane) in flight, and multiply them with the same k of the tokens, which
+// stay in the caches.  Their sums meet in LDS in wave order.  One token, bf16
+// 4096 -> 14336: 24 us, 4.9 TB/s of weights, what a copy reaches.
+#include "lin.h"
+
+namespace acsc {
+namespace {
+
+typedef __attribute__((__vector_size__(8 * sizeof(short)))) short bf16x8;
+
+constexpr int kWaves = 8;
+
+// 16 bytes of a row, the first nv elements of them, zeros after.
+struct __attribute__((packed, aligned(2))) Any16 {
+    uint32_t w[4];
+};
+template <typename T>
+__device__ __forceinline__ Any16 load16(const T *p, int nv)
+{
+    constexpr int E = 16 / sizeof(T);
+    if (nv >= E)
+        return *reinterpret_cast<const Any16 *>(p);
+    Any16 r = {{0, 0, 0, 0}};
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+        if (i < nv) {
+            if (sizeof(T) == 2)
+                r.w[i / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t *>(p)[i]) << (16 * (i & 1));
+            else
+                r.w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+        }
+    return r;
+}
+
+// Lane L of a 16-byte chunk holds row L % 16 and E values of k from E (L / 16):
+// one bf16 instruction of 32 k, or four fp32 ones of every fourth k.
+template <typename T>
+__device__ __forceinline__ f32x4 multiply(const Any16 &w, const Any16 &x, f32x4 acc)
+{
+    if (sizeof(T) == 2) {
+        bf16x8 a, b;
+        __builtin_memcpy(&a, &w, 16);
+        __builtin_memcpy(&b, &x, 16);
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.w[e]), __uint_as_float(x.w[e]), acc, 0, 0, 0);
+    return acc;
+}
+
+template <typename T, int MT>
+__global__ __launch_bounds__(kWaves * 64) void lin_few_kernel(Gemm g)
+{
+    constexpr int E = 16 / sizeof(T), LINE = 8 * E, U = 4;   // k of a chunk and of a line; lines in flight
+    __shared__ __align__(16) float meet[kWaves][MT * 16][16];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int n0 = blockIdx.x * 16, split = blockIdx.y;
+    const int kbeg = split * g.kchunk, kend = min(g.K, kbeg + g.kchunk);
+    const int k = (lane >> 4) * E;
+    const T *w = static_cast<const T *>(g.B.p) + min(n0 + (lane & 15), g.N - 1) * g.B.ld;
+    const T *x[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+        x[t] = static_cast<const T *>(g.A.p) + min<int64_t>(t * 16 + (lane & 15), g.M - 1) * g.A.ld;
+    f32x4 acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+        acc[t] = f32x4{0, 0, 0, 0};
+
+    int k0 = kbeg + wave * LINE;
+    for (; k0 + ((U - 1) * kWaves + 1) * LINE <= kend; k0 += U * kWaves * LINE) {
+        Any16 a[U][2], b[U][2][MT];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int at = k0 + u * kWaves * LINE + h * 4 * E + k;
+                a[u][h] = *reinterpret_cast<const Any16 *>(w + at);
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+                    b[u][h][t] = *reinterpret_cast<const Any16 *>(x[t] + k0 + u * kWaves * LINE + h * 4 * E + k);
+        __builtin_amdgcn_sched_barrier(0);   // all loads leave before the first product
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+                    acc[t] = multiply<T>(a[u][h], b[u][h][t], acc[t]);
+    }
+    for (; k0 < kend; k0 += kWaves * LINE)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int at = k0 + h * 4 * E + k;
+            const Any16 a = load16(w + at, kend - at);
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+                acc[t] = multiply<T>(a, load16(x[t] + at, kend - at), acc[t]);
+        }
+
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+        *reinterpret_cast<f32x4 *>(&meet[wave][t * 16 + (lane & 15)][(lane >> 4) * 4]) = acc[t];
+    __syncthreads();
+    const int m = threadIdx.x >> 1, c = (threadIdx.x & 1) * 8, n = n0 + c;
+    if (m >= MT * 16 || m >= g.M)
+        return;
+    float v[8] = {};
+    for (int i = 0; i < kWaves; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[j] += meet[i][m][c + j];
+    if (g.part) {
+        store8(g.part + (split * g.M + m) * g.ldp + n, g.N - n, v);
+    } else {
+        float bias[8];
+        load_bias<T, kForward>(g.e, n, g.N, bias);
+        epilogue<T, kForward>(g.e, v, bias, true, m, n, g.N);   // without a checkpoint: lanes of their own
+    }
+}
+
+}  // namespace
+
+int lin_few_run(const Gemm &g, acsc_dtype dt, hipStream_t st, const char *tag)
+{
+    const dim3 grid(static_cast<unsigned>((g.N + 15) / 16), g.splits);
+    if (dt == ACSC_BF16)
+        ACSC_LAUNCH(tag, (lin_few_kernel<uint16_t, 1>), grid, dim3(kWaves * 64), 0, st, g);
+    else if (g.M <= 16)
+        ACSC_LAUNCH(tag, (lin_few_kernel<float, 1>), grid, dim3(kWaves * 64), 0, st, g);
+    else
+        ACSC_LAUNCH(tag, (lin_few_kernel<float, 2>), grid, dim3(kWaves * 64), 0, st, g);
+    return check_launch(tag);
+}
+
+}  // namespace acsc

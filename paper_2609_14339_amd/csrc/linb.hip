@@ -162,7 +162,7 @@ __global__ __launch_bounds__(2 * T, 2) void lin_bf16_kernel(Gemm g)
     const int wm = wave / WN, wn = wave % WN;
 
     // Workgroups go to the eight XCDs in turn; each XCD takes a run of tiles
-    // of its own, in columns of eight tiles, so that what its CUs read
+    // of its own, in columns of four tiles, so that what its CUs read
     // together stays in its L2.
     int64_t id = blockIdx.x;
     const int64_t tiles = static_cast<int64_t>(g.tm) * g.tn;
@@ -170,9 +170,9 @@ __global__ __launch_bounds__(2 * T, 2) void lin_bf16_kernel(Gemm g)
         const int64_t q = tiles / 8, r = tiles % 8, x = id % 8;
         id = x * q + min(x, r) + id / 8;
     }
-    const int64_t band = id / (8 * g.tn), in = id - band * 8 * g.tn;
-    const int height = static_cast<int>(min<int64_t>(g.tm - band * 8, 8));
-    const int tile_m = static_cast<int>(band * 8 + in % height), tile_n = static_cast<int>(in / height);
+    const int64_t band = id / (4 * g.tn), in = id - band * 4 * g.tn;
+    const int height = static_cast<int>(min<int64_t>(g.tm - band * 4, 4));
+    const int tile_m = static_cast<int>(band * 4 + in % height), tile_n = static_cast<int>(in / height);
     const int split = blockIdx.y;
     const int64_t m0 = static_cast<int64_t>(tile_m) * T;
     const int n0 = tile_n * T;

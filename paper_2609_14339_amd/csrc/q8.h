@@ -204,26 +204,45 @@ __device__ __forceinline__ void group_scale(uint32_t a, float &scale, float &inv
         scale = inv = 0.f;
     } else {
         const float f = __uint_as_float(a);
-        scale = f / 127.f;
-        inv = 127.f / f;
+        if (a - 0x0d800000u < 0x64000000u) {   // 2^-100 <= a < 2^100: nothing under- or overflows
+            // Quotients by one residual step from a reciprocal: rounded as the
+            // divisions below are, for every 24-bit significand of a (checked
+            // over all 2^23 of them, with the hardware's reciprocal one unit
+            // off either way).
+            constexpr float r127 = 1.f / 127.f;
+            scale = f * r127;
+            scale = __builtin_fmaf(__builtin_fmaf(-127.f, scale, f), r127, scale);
+            float y = __builtin_amdgcn_rcpf(f);
+            y = __builtin_fmaf(__builtin_fmaf(-f, y, 1.f), y, y);
+            inv = 127.f * y;
+            inv = __builtin_fmaf(__builtin_fmaf(-f, inv, 127.f), y, inv);
+        } else {
+            scale = f / 127.f;
+            inv = 127.f / f;
+        }
     }
 }
 
 // Codes of N values: rint(x * inv), in -127 .. 127 because |x| <= a makes
-// |x * inv| round to at most 127 (1 + 2^-23).  inv = 0 gives zeros, for the
-// non-finite values of a NaN group too.
+// |x * inv| round to at most 127 (1 + 2^-23).  Adding 1.5 * 2^23 rounds to a
+// whole number, ties to even, whose low byte is the code; the product is
+// rounded before that, as the format asks (no contraction).  inv = 0 gives
+// zeros, for the non-finite values of a NaN group too.
 template <int N>
 __device__ __forceinline__ void store_codes(int8_t *p, int nv, float inv, const float (&v)[N])
 {
+#pragma clang fp contract(off)
     uint32_t w[N / 4];
 #pragma unroll
     for (int q = 0; q < N / 4; ++q) {
-        w[q] = 0;
+        uint32_t b[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float t = inv == 0.f ? 0.f : v[4 * q + i] * inv;
-            w[q] |= (static_cast<uint32_t>(static_cast<int>(rintf(t))) & 0xffu) << (8 * i);
+            const float t = v[4 * q + i] * inv;
+            b[i] = __float_as_uint(t + 12582912.f);
         }
+        const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400), hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0c);
+        w[q] = inv == 0.f ? 0u : lo | hi;
     }
     if (nv >= N) {
         struct __attribute__((packed, aligned(1))) Any {
@@ -254,30 +273,106 @@ __device__ __forceinline__ uint32_t max16(uint32_t x)
     return x;
 }
 
-// act(z) and act'(z).  gelu(z) = z Phi(z), Phi(z) = erfc(-z / sqrt 2) / 2;
-// gelu'(z) = Phi(z) + z phi(z).  silu(z) = z s, s = 1 / (1 + exp(-z)).
-// Limits at infinities follow the definitions' plain arithmetic.
+// act(z) and act'(z).  gelu(z) = z Phi(z), gelu'(z) = Phi(z) + z phi(z);
+// silu(z) = z s, silu'(z) = s (1 + z (1 - s)), s = 1 / (1 + exp(-z)), with
+// s and 1 - s both from exp(-|z|), so that neither is a difference.
+//
+// T is the type that the result is rounded to.  For fp32, Phi comes from the
+// library's erf.  For bf16 (half a unit: 2^-8) Phi(-|z|) is
+//   (a1 t + .. + a5 t^5) exp(-z^2 / 2) / 2,  t = 1 / (1 + p |z| / sqrt 2)
+// (Abramowitz & Stegun, Handbook of Mathematical Functions, 7.1.26: within
+// 0.75e-7), and exponentials and reciprocals are the hardware's (one unit of
+// 2^-23): a dozen instructions where erf takes some 40, in epilogues that
+// nothing hides (see the forward product's figures).
+__device__ __forceinline__ float normal_tail(float z, float &e)
+{
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
+    e = __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z);
+    float q = 0.5f * 1.061405429f;
+    q = __builtin_fmaf(q, t, 0.5f * -1.453152027f);
+    q = __builtin_fmaf(q, t, 0.5f * 1.421413741f);
+    q = __builtin_fmaf(q, t, 0.5f * -0.284496736f);
+    q = __builtin_fmaf(q, t, 0.5f * 0.254829592f);
+    return q * (t * e);
+}
+// s and 1 - s
+template <typename T>
+__device__ __forceinline__ void sigmoid(float z, float &s, float &c)
+{
+    const float e = sizeof(T) == 4 ? expf(-fabsf(z)) : __builtin_amdgcn_exp2f(-1.4426950408889634f * fabsf(z));
+    const float r = sizeof(T) == 4 ? 1.f / (1.f + e) : __builtin_amdgcn_rcpf(1.f + e);
+    s = z < 0.f ? e * r : r;
+    c = z < 0.f ? r : e * r;
+}
+template <typename T>
 __device__ __forceinline__ float act_value(float z, int act)
 {
     if (act == ACSC_ACT_RELU)
         return z > 0.f ? z : (z != z ? z : 0.f);
-    if (act == ACSC_ACT_GELU)
-        return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    if (act == ACSC_ACT_SILU)
-        return z / (1.f + expf(-z));
+    if (act == ACSC_ACT_GELU) {
+        if (sizeof(T) == 4)
+            return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+        float e;
+        const float q = normal_tail(z, e);
+        return __builtin_fmaf(-fabsf(z), q, z > 0.f || z != z ? z : 0.f);
+    }
+    if (act == ACSC_ACT_SILU) {
+        float s, c;
+        sigmoid<T>(z, s, c);
+        return z * s;
+    }
     return z;
 }
+template <typename T>
 __device__ __forceinline__ float act_slope(float z, int act)
 {
     if (act == ACSC_ACT_RELU)
         return z > 0.f ? 1.f : (z != z ? z : 0.f);
-    if (act == ACSC_ACT_GELU)
-        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+    if (act == ACSC_ACT_GELU) {
+        if (sizeof(T) == 4)
+            return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+        float e;
+        const float q = normal_tail(z, e);
+        return __builtin_fmaf(z * 0.39894228040143268f, e, z < 0.f ? q : 1.f - q);
+    }
     if (act == ACSC_ACT_SILU) {
-        const float s = 1.f / (1.f + expf(-z));
-        return s * (1.f + z * (1.f - s));
+        float s, c;
+        sigmoid<T>(z, s, c);
+        return s * __builtin_fmaf(z, c, 1.f);
     }
     return 1.f;
+}
+
+// Eight values at a time: one branch on the function, not one a value.
+template <typename T>
+__device__ __forceinline__ void apply_act(float (&v)[8], int act)
+{
+    const auto each = [&](int a) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = act_value<T>(v[i], a);
+    };
+    if (act == ACSC_ACT_GELU)
+        each(ACSC_ACT_GELU);
+    else if (act == ACSC_ACT_SILU)
+        each(ACSC_ACT_SILU);
+    else if (act == ACSC_ACT_RELU)
+        each(ACSC_ACT_RELU);
+}
+template <typename T>
+__device__ __forceinline__ void apply_slope(float (&v)[8], const float (&z)[8], int act)
+{
+    const auto each = [&](int a) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] *= act_slope<T>(z[i], a);
+    };
+    if (act == ACSC_ACT_GELU)
+        each(ACSC_ACT_GELU);
+    else if (act == ACSC_ACT_SILU)
+        each(ACSC_ACT_SILU);
+    else if (act == ACSC_ACT_RELU)
+        each(ACSC_ACT_RELU);
 }
 
 }  // namespace acsc

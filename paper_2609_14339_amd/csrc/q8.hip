@@ -61,9 +61,7 @@ __global__ __launch_bounds__(kQThreads) void q8_decode_kernel(Q8 q, int64_t rows
             continue;
         float v[8];
         load_codes(q.codes + row * q.ldc + col, H - col, q.scales[row * q.lds + col / kGroup], v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v[i] = act_value(v[i], act);
+        apply_act<T>(v, act);
         store8(y + row * ldy + col, H - col, v);
     }
 }
