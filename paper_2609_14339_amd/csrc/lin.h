@@ -47,16 +47,54 @@ struct Gemm {
     Epi e;
 };
 
-// Eight values of row m at columns n .. n + 7 (n a multiple of 8) through the
-// epilogue.  Sixteen lanes of the wave, aligned, hold one group of 128
-// columns of a row, and every lane of the wave calls it (`on`: the row
-// exists); T is the type of y, z, bias and residual, `bias` the eight columns'
-// (zeros without one).
+// What the epilogue reads beside the sums for eight columns of a row: the
+// residual (forward), the kept pre-activation or its codes and scale (gate),
+// or the output to add to (weight).
+template <typename T>
+struct Beside {
+    T v[8];
+    uint32_t codes[2];
+    float scale;
+};
 template <typename T, int KIND>
-__device__ __forceinline__ void epilogue(const Epi &e, float (&v)[8], const float (&bias)[8], bool on, int64_t m, int n,
-                                         int N)
+__device__ __forceinline__ bool has_beside(const Epi &e)
 {
-    const int left = on ? N - n : 0;
+    return KIND == kForward ? e.res != nullptr : KIND == kGate ? e.act != ACSC_ACT_NONE : e.accumulate != 0;
+}
+template <typename T, int KIND>
+__device__ __forceinline__ void load_beside(const Epi &e, Beside<T> &b, int64_t m, int n, int left)
+{
+    if (KIND == kGate && e.q.codes) {
+        load_raw(e.q.codes + m * e.q.ldc + n, left, b.codes);
+        b.scale = left > 0 ? e.q.scales[m * e.q.lds + n / kGroup] : 0.f;
+        return;
+    }
+    const T *p = static_cast<const T *>(KIND == kForward ? e.res : KIND == kGate ? e.z : e.y);
+    load_raw(p + m * (KIND == kForward ? e.ldr : KIND == kGate ? e.ldz : e.ldy) + n, left, b.v);
+}
+template <typename T, int KIND>
+__device__ __forceinline__ void beside_values(const Epi &e, const Beside<T> &b, float (&v)[8])
+{
+    if (KIND == kGate && e.q.codes) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = static_cast<float>(static_cast<int8_t>(b.codes[i / 4] >> (8 * (i % 4)))) * b.scale;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = to_f32(b.v[i]);
+    }
+}
+
+// Eight values of row m at columns n .. n + 7 (n a multiple of 8; the first
+// `left` of them exist, none of a row past the end) through the epilogue.
+// Sixteen lanes of the wave, aligned, hold one group of 128 columns of a row,
+// and every lane of the wave calls it.  T is the type of y, z, bias and
+// residual; `bias` holds the eight columns', zeros without one.
+template <typename T, int KIND>
+__device__ __forceinline__ void epilogue(const Epi &e, float (&v)[8], const float (&bias)[8], const Beside<T> &beside,
+                                         int64_t m, int n, int left)
+{
     if (KIND == kForward) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -67,8 +105,7 @@ __device__ __forceinline__ void epilogue(const Epi &e, float (&v)[8], const floa
             uint32_t a = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (i < left)
-                    a = max(a, mag(v[i]));
+                a = max(a, i < left ? mag(v[i]) : 0u);
             a = max16(a);
             float scale, inv;
             group_scale(a, scale, inv);
@@ -77,33 +114,19 @@ __device__ __forceinline__ void epilogue(const Epi &e, float (&v)[8], const floa
                 e.q.scales[m * e.q.lds + n / kGroup] = scale;
         }
         apply_act<T>(v, e.act);
-        if (e.res) {
-            float b[8];
-            load8(static_cast<const T *>(e.res) + m * e.ldr + n, left, b);
+    }
+    if (has_beside<T, KIND>(e)) {
+        float b[8];
+        beside_values<T, KIND>(e, beside, b);
+        if (KIND == kGate) {
+            apply_slope<T>(v, b, e.act);
+        } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 v[i] += b[i];
         }
     }
-    if (left <= 0)
-        return;
-    if (KIND == kGate && e.act != ACSC_ACT_NONE) {
-        float z[8];
-        if (e.q.codes)
-            load_codes(e.q.codes + m * e.q.ldc + n, left, e.q.scales[m * e.q.lds + n / kGroup], z);
-        else
-            load8(static_cast<const T *>(e.z) + m * e.ldz + n, left, z);
-        apply_slope<T>(v, z, e.act);
-    }
-    T *y = static_cast<T *>(e.y) + m * e.ldy + n;
-    if (KIND == kWeight && e.accumulate) {
-        float o[8];
-        load8(y, left, o);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v[i] += o[i];
-    }
-    store8(y, left, v);
+    store8(static_cast<T *>(e.y) + m * e.ldy + n, left, v);
 }
 
 template <typename T, int KIND>
@@ -118,9 +141,43 @@ __device__ __forceinline__ void load_bias(const Epi &e, int n, int N, float (&b)
 // 16 j + 4 (L / 16) + i of row 16 a + L % 16; they turn into runs of eight
 // columns in `lds` (8 KiB NA, the wave's own), whose 16-byte chunks are
 // XOR-swizzled by the row so that neither side conflicts: rows then go out as
-// 256 (bf16) contiguous bytes.
+// 256 (bf16) contiguous bytes, four a step.  What the epilogue reads leaves
+// for four steps at once (one at a time each waits a memory latency: a
+// residual on 16384 x 2048 -> 8192 cost 100 us that way, see the forward
+// kernel's figures); WHOLE: the wave's 128 columns all exist.
+template <typename T, int KIND, int NA, bool WHOLE>
+__device__ __forceinline__ void put_rows(const Gemm &g, const char *lds, int64_t m0, int n0, int split)
+{
+    const int lane = threadIdx.x & 63, n = n0 + (lane & 15) * 8;
+    const int cols = WHOLE ? 8 : g.N - n;
+    float bias[8];
+    if (!g.part)
+        load_bias<T, KIND>(g.e, n, g.N, bias);
+#pragma unroll 1
+    for (int r0 = 0; r0 < NA * 4; r0 += 4) {
+        Beside<T> beside[4];
+        if (!g.part && has_beside<T, KIND>(g.e)) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                load_beside<T, KIND>(g.e, beside[u], min<int64_t>(m0 + (r0 + u) * 4 + (lane >> 4), g.M - 1), n, cols);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int row = (r0 + u) * 4 + (lane >> 4), c = (lane & 15) * 2;
+            const f32x4 lo = *reinterpret_cast<const f32x4 *>(lds + row * 512 + (c ^ (row & 31)) * 16);
+            const f32x4 hi = *reinterpret_cast<const f32x4 *>(lds + row * 512 + ((c + 1) ^ (row & 31)) * 16);
+            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            const int64_t m = m0 + row;
+            const int left = m < g.M ? cols : 0;
+            if (g.part)
+                store8(g.part + (split * g.M + m) * g.ldp + n, left, v);
+            else
+                epilogue<T, KIND>(g.e, v, bias, beside[u], m, n, left);
+        }
+    }
+}
 template <typename T, int KIND, int NA>
-__device__ __forceinline__ void put_rows(const Gemm &g, const f32x4 (&acc)[NA][8], char *lds, int64_t m0, int n0,
+__device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8], char *lds, int64_t m0, int n0,
                                          int split)
 {
     const int lane = threadIdx.x & 63;
@@ -135,22 +192,10 @@ __device__ __forceinline__ void put_rows(const Gemm &g, const f32x4 (&acc)[NA][8
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    const int n = n0 + (lane & 15) * 8;
-    float bias[8];
-    if (!g.part)
-        load_bias<T, KIND>(g.e, n, g.N, bias);
-#pragma unroll 1
-    for (int r = 0; r < NA * 4; ++r) {
-        const int row = r * 4 + (lane >> 4), c = (lane & 15) * 2;
-        const f32x4 lo = *reinterpret_cast<const f32x4 *>(lds + row * 512 + (c ^ (row & 31)) * 16);
-        const f32x4 hi = *reinterpret_cast<const f32x4 *>(lds + row * 512 + ((c + 1) ^ (row & 31)) * 16);
-        float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        const int64_t m = m0 + row;
-        if (g.part)
-            store8(g.part + (split * g.M + m) * g.ldp + n, m < g.M ? g.N - n : 0, v);
-        else
-            epilogue<T, KIND>(g.e, v, bias, m < g.M, m, n, g.N);
-    }
+    if (n0 + 128 <= g.N)
+        put_rows<T, KIND, NA, true>(g, lds, m0, n0, split);
+    else
+        put_rows<T, KIND, NA, false>(g, lds, m0, n0, split);
 }
 
 }  // namespace acsc

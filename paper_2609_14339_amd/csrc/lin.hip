@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256) void lin_f32_kernel(Gemm g)
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
         const f32x4(&one)[1][8] = reinterpret_cast<const f32x4(&)[1][8]>(acc[a]);
-        put_rows<TO, KIND, 1>(g, one, reinterpret_cast<char *>(lds) + wave * 8192, m0 + wave * 32 + a * 16, n0, split);
+        put_tile<TO, KIND, 1>(g, one, reinterpret_cast<char *>(lds) + wave * 8192, m0 + wave * 32 + a * 16, n0, split);
     }
 }
 
@@ -149,7 +149,10 @@ __global__ __launch_bounds__(256) void lin_join_kernel(Gemm g)
                 v[4 + i] = hi[i];
             }
         }
-        epilogue<TO, KIND>(g.e, v, bias, n < g.N, m, n, g.N);
+        Beside<TO> beside;
+        if (has_beside<TO, KIND>(g.e))
+            load_beside<TO, KIND>(g.e, beside, m, n, g.N - n);
+        epilogue<TO, KIND>(g.e, v, bias, beside, m, n, g.N - n);
     }
 }
 

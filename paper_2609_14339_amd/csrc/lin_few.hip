@@ -128,7 +128,10 @@ __global__ __launch_bounds__(kWaves * 64) void lin_few_kernel(Gemm g)
     } else {
         float bias[8];
         load_bias<T, kForward>(g.e, n, g.N, bias);
-        epilogue<T, kForward>(g.e, v, bias, true, m, n, g.N);   // without a checkpoint: lanes of their own
+        Beside<T> beside;
+        if (has_beside<T, kForward>(g.e))
+            load_beside<T, kForward>(g.e, beside, m, n, g.N - n);
+        epilogue<T, kForward>(g.e, v, bias, beside, m, n, g.N - n);   // without a checkpoint: lanes of their own
     }
 }
 

@@ -283,7 +283,7 @@ __global__ __launch_bounds__(2 * T, 2) void lin_bf16_kernel(Gemm g)
     char *own = reinterpret_cast<char *>(smem) + wave * NA * 8192;
 #pragma unroll
     for (int a = 0; a < FA; a += NA)
-        put_rows<TO, KIND, NA>(g, reinterpret_cast<const f32x4(&)[NA][8]>(acc[a]), own, m0 + (wm * FA + a) * 16,
+        put_tile<TO, KIND, NA>(g, reinterpret_cast<const f32x4(&)[NA][8]>(acc[a]), own, m0 + (wm * FA + a) * 16,
                                n0 + wn * 128, split);
 }
 

@@ -107,25 +107,7 @@ __device__ __forceinline__ void store8(float *p, int nv, const float (&v)[8])
                 p[i] = v[i];
     }
 }
-// Four consecutive elements, as above.
-struct __attribute__((packed, aligned(2))) Bf4Any {
-    uint32_t w[2];
-};
-__device__ __forceinline__ void load4(const uint16_t *p, int nv, float (&v)[4])
-{
-    if (nv >= 4) {
-        const Bf4Any c = *reinterpret_cast<const Bf4Any *>(p);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            v[2 * i] = __uint_as_float(c.w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(c.w[i] & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            v[i] = i < nv ? bf16_to_f32(p[i]) : 0.f;
-    }
-}
+// Four consecutive floats, as above.
 __device__ __forceinline__ void load4(const float *p, int nv, float (&v)[4])
 {
     if (nv >= 4) {
@@ -139,35 +121,37 @@ __device__ __forceinline__ void load4(const float *p, int nv, float (&v)[4])
             v[i] = i < nv ? p[i] : 0.f;
     }
 }
-__device__ __forceinline__ void store4(uint16_t *p, int nv, const float (&v)[4])
+
+// Eight consecutive elements or codes as they are; those past the first nv
+// become 0.
+__device__ __forceinline__ void load_raw(const uint16_t *p, int nv, uint16_t (&v)[8])
 {
-    if (nv >= 4) {
-        Bf4Any c;
-        c.w[0] = f32x2_to_bf16x2(v[0], v[1]);
-        c.w[1] = f32x2_to_bf16x2(v[2], v[3]);
-        *reinterpret_cast<Bf4Any *>(p) = c;
+    if (nv >= 8) {
+        const Bf8Any c = *reinterpret_cast<const Bf8Any *>(p);
+        __builtin_memcpy(v, &c, 16);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < nv)
-                p[i] = f32_to_bf16(v[i]);
+        for (int i = 0; i < 8; ++i)
+            v[i] = i < nv ? p[i] : 0;
     }
 }
-__device__ __forceinline__ void store4(float *p, int nv, const float (&v)[4])
+__device__ __forceinline__ void load_raw(const float *p, int nv, float (&v)[8]) { load8(p, nv, v); }
+__device__ __forceinline__ void load_raw(const int8_t *p, int nv, uint32_t (&w)[2])
 {
-    if (nv >= 4) {
-        F4Any a;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            a.v[i] = v[i];
-        *reinterpret_cast<F4Any *>(p) = a;
+    if (nv >= 8) {
+        const C8Any c = *reinterpret_cast<const C8Any *>(p);
+        w[0] = c.w[0];
+        w[1] = c.w[1];
     } else {
+        w[0] = w[1] = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 8; ++i)
             if (i < nv)
-                p[i] = v[i];
+                w[i / 4] |= (static_cast<uint32_t>(p[i]) & 0xffu) << (8 * (i % 4));
     }
 }
+__device__ __forceinline__ float to_f32(uint16_t h) { return bf16_to_f32(h); }
+__device__ __forceinline__ float to_f32(float f) { return f; }
 
 // Values of N = 4 or 8 consecutive codes under one scale.
 template <int N>
