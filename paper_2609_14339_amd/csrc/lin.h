@@ -52,8 +52,8 @@ struct Gemm {
 // or the output to add to (weight).
 template <typename T>
 struct Beside {
-    T v[8];
-    uint32_t codes[2];
+    Raw8<T> v;
+    Codes8 codes;
     float scale;
 };
 template <typename T, int KIND>
@@ -78,11 +78,11 @@ __device__ __forceinline__ void beside_values(const Epi &e, const Beside<T> &b, 
     if (KIND == kGate && e.q.codes) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            v[i] = static_cast<float>(static_cast<int8_t>(b.codes[i / 4] >> (8 * (i % 4)))) * b.scale;
+            v[i] = code_value(b.codes.at(i), b.scale);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            v[i] = to_f32(b.v[i]);
+            v[i] = b.v.at(i);
     }
 }
 

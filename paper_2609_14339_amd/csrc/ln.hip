@@ -9,6 +9,8 @@
 // barrier, wider ones to a workgroup.
 #include "q8.h"
 
+#include <type_traits>
+
 namespace acsc {
 namespace {
 
@@ -172,12 +174,30 @@ struct Bwd {
     int H;
 };
 
+// Makes the compiler take what it knows of stored words as new: values are
+// then formed from them again instead of being kept in registers.
+template <int N>
+__device__ __forceinline__ void again(uint32_t (&w)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        asm volatile("" : "+v"(w[i]));
+}
+template <int N>
+__device__ __forceinline__ void again(float (&)[N])
+{
+}
+
 // A workgroup walks rows blockIdx.x, + gridDim.x, ... (four at a time where a
 // wave holds a row) and keeps the column sums of dy h and dy in registers;
 // its waves' sums meet in LDS in wave order, and every workgroup leaves one
-// partial.
-template <typename T, int NT, int CH>
-__global__ __launch_bounds__(NT < 256 ? 256 : NT) void ln_backward_kernel(Bwd<T> p)
+// partial.  The next row's loads leave before a row is worked on: 16384 x
+// 2048 in 54 us, its 268 MB at 5.0 TB/s (131 without).  KEPT: the row comes
+// from its checkpoint.  SUMS: rows past 16384 columns leave no registers for
+// the sums (4096 x 28672 with them: 940 us, most of it spilled registers);
+// ln_sums_kernel takes those in a pass of its own.
+template <typename T, int NT, int CH, bool KEPT, bool SUMS>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void ln_backward_kernel(Bwd<T> p)
 {
     constexpr int RPB = NT < 256 ? 256 / NT : 1;
     __shared__ float slots[2][2 * (NT / 64)];
@@ -185,42 +205,78 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void ln_backward_kernel(Bwd<T>
     const int t = threadIdx.x % NT;
     const int sub = RPB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
     float dg[CH][8], db[CH][8];
+    Raw8<T> w[CH];
+    const auto load_gamma = [&]() {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (p.gamma)
+                load_raw(p.gamma + (c * NT + t) * 8, p.H - (c * NT + t) * 8, w[c]);
+    };
+    if (SUMS)
+        load_gamma();
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             dg[c][i] = db[c][i] = 0.f;
-    int flip = 0;
-    for (int64_t row = static_cast<int64_t>(blockIdx.x) * RPB + sub; row < p.rows;
-         row += static_cast<int64_t>(gridDim.x) * RPB, flip ^= 1) {
-        float h[CH][8], g[CH][8];
-        const float mu = p.mean[row], rs = p.rstd[row];
+    // a row as it is stored
+    struct Row {
+        typename std::conditional<KEPT, Codes8, Raw8<T>>::type x[CH];
+        Raw8<T> dy[CH];
+        float scale[CH], mu, rs;
+    };
+    const auto load = [&](Row &r, int64_t row) {
+        r.mu = p.mean[row];
+        r.rs = p.rstd[row];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * NT + t) * 8, left = p.H - col;
-            if (p.q.codes)
-                load_codes(p.q.codes + row * p.q.ldc + col, left, left > 0 ? p.q.scales[row * p.q.lds + col / kGroup] : 0.f,
-                           h[c]);
-            else
-                load8(p.x + row * p.ldx + col, left, h[c]);
-            load8(p.dy + row * p.lddy + col, left, g[c]);
+            if constexpr (KEPT) {
+                load_raw(p.q.codes + row * p.q.ldc + col, left, r.x[c]);
+                r.scale[c] = left > 0 ? p.q.scales[row * p.q.lds + col / kGroup] : 0.f;
+            } else {
+                load_raw(p.x + row * p.ldx + col, left, r.x[c]);
+            }
+            load_raw(p.dy + row * p.lddy + col, left, r.dy[c]);
         }
+    };
+    int flip = 0;
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * RPB, first = static_cast<int64_t>(blockIdx.x) * RPB + sub;
+    Row cur, next;
+    if (SUMS && first < p.rows)
+        load(next, first);
+    for (int64_t row = first; row < p.rows; row += stride, flip ^= 1) {
+        Raw8<T> add[CH];
+        if (SUMS)
+            cur = next;
+        else
+            load(cur, row);
+        if (p.add)
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+                load_raw(p.add + row * p.ldadd + (c * NT + t) * 8, p.H - (c * NT + t) * 8, add[c]);
+        if (SUMS && row + stride < p.rows)
+            load(next, row + stride);
+        if (!SUMS)
+            load_gamma();
+        const auto h = [&](int c, int i) {
+            return ((KEPT ? code_value(cur.x[c].at(i), cur.scale[c]) : cur.x[c].at(i)) - cur.mu) * cur.rs;
+        };
+        const auto g = [&](int c, int i) { return p.gamma ? cur.dy[c].at(i) * w[c].at(i) : cur.dy[c].at(i); };
         float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int col = (c * NT + t) * 8, left = p.H - col;
-            float w[8];
-            if (p.gamma)
-                load8(p.gamma + col, left, w);
+            again(w[c].w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                h[c][i] = i < left ? (h[c][i] - mu) * rs : 0.f;
-                dg[c][i] += g[c][i] * h[c][i];
-                db[c][i] += g[c][i];
-                if (p.gamma)
-                    g[c][i] *= w[i];
-                s[0] += g[c][i];
-                s[1] += g[c][i] * h[c][i];
+                // past the end of the row dy = 0, which leaves every sum alone
+                const float hi = h(c, i), dy = cur.dy[c].at(i), gi = g(c, i);
+                if (SUMS) {
+                    dg[c][i] += dy * hi;
+                    db[c][i] += dy;
+                }
+                s[0] += gi;
+                s[1] += gi * hi;
             }
         }
         row_sum<NT>(s, slots[flip]);
@@ -228,33 +284,34 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void ln_backward_kernel(Bwd<T>
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * NT + t) * 8, left = p.H - col;
+            again(cur.x[c].w);
+            again(cur.dy[c].w);
+            again(w[c].w);
             if (left > 0) {
-                float o[8], a[8];
-                if (p.add)
-                    load8(p.add + row * p.ldadd + col, left, a);
+                float o[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    o[i] = rs * (g[c][i] - m1 - h[c][i] * m2);
+                    o[i] = cur.rs * (g(c, i) - m1 - h(c, i) * m2);
                     if (p.add)
-                        o[i] += a[i];
+                        o[i] += add[c].at(i);
                 }
                 store8(p.dx + row * p.lddx + col, left, o);
             }
         }
     }
-    if (!p.part)
+    if (!SUMS || !p.part)
         return;
     if (RPB > 1) {
-        for (int w = 0; w < RPB; ++w) {
-            if (sub == w) {
+        for (int v = 0; v < RPB; ++v) {
+            if (sub == v) {
 #pragma unroll
                 for (int c = 0; c < CH; ++c)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         // [sum][chunk][i][lane]: consecutive lanes in consecutive banks
                         float *m = meet + ((c * 8 + i) * NT + t);
-                        m[0] = w ? m[0] + dg[c][i] : dg[c][i];
-                        m[NT * CH * 8] = w ? m[NT * CH * 8] + db[c][i] : db[c][i];
+                        m[0] = v ? m[0] + dg[c][i] : dg[c][i];
+                        m[NT * CH * 8] = v ? m[NT * CH * 8] + db[c][i] : db[c][i];
                     }
             }
             __syncthreads();
@@ -280,23 +337,67 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void ln_backward_kernel(Bwd<T>
     }
 }
 
-// Column sums over the partials, in their order: 64 columns and 4 slices of
-// the partials a workgroup, the slices joined in order.
-__global__ __launch_bounds__(256) void ln_join_kernel(const float *part, int n, int H, float *dgamma, float *dbeta,
-                                                      int accumulate)
+// The column sums of wide rows: 512 columns and one slice of the rows a
+// workgroup, whose four waves take every fourth row and meet in LDS in order.
+template <typename T, bool KEPT>
+__global__ __launch_bounds__(256) void ln_sums_kernel(Bwd<T> p, int per)
 {
-    __shared__ float meet[4][64];
+    __shared__ float meet[4][2][512];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = blockIdx.x * 512 + lane * 8, left = p.H - col;
+    const int64_t end = min<int64_t>(p.rows, (blockIdx.y + static_cast<int64_t>(1)) * per);
+    float dg[8] = {}, db[8] = {};
+#pragma unroll 4
+    for (int64_t row = blockIdx.y * static_cast<int64_t>(per) + wave; row < end; row += 4) {
+        float x[8], dy[8];
+        if (KEPT)
+            load_codes(p.q.codes + row * p.q.ldc + col, left, left > 0 ? p.q.scales[row * p.q.lds + col / kGroup] : 0.f, x);
+        else
+            load8(p.x + row * p.ldx + col, left, x);
+        load8(p.dy + row * p.lddy + col, left, dy);
+        const float mu = p.mean[row], rs = p.rstd[row];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            dg[i] += dy[i] * ((x[i] - mu) * rs);
+            db[i] += dy[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        meet[wave][0][i * 64 + lane] = dg[i];
+        meet[wave][1][i * 64 + lane] = db[i];
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 1024; c += 256) {
+        const int which = c >> 9, k = c & 511, at = (k & 7) * 64 + (k >> 3), n = blockIdx.x * 512 + k;
+        if (n < p.H)
+            p.part[(static_cast<int64_t>(blockIdx.y) * 2 + which) * p.H + n] =
+                ((meet[0][which][at] + meet[1][which][at]) + meet[2][which][at]) + meet[3][which][at];
+    }
+}
+
+// Column sums over the partials: 64 columns and 16 slices of the partials a
+// workgroup, each slice in order, the slices joined in order.  (Four slices
+// left a lane 128 dependent loads: 40 us for 512 partials of 2048 columns.)
+constexpr int kSlices = 16;
+__global__ __launch_bounds__(64 * kSlices) void ln_join_kernel(const float *part, int n, int H, float *dgamma, float *dbeta,
+                                                               int accumulate)
+{
+    __shared__ float meet[kSlices][64];
     const int lane = threadIdx.x & 63, sl = threadIdx.x >> 6;
     const int col = blockIdx.x * 64 + lane;       // over 2 H: the dgamma columns, then dbeta's
-    const int per = (n + 3) / 4, end = min(n, (sl + 1) * per);
+    const int per = (n + kSlices - 1) / kSlices, end = min(n, (sl + 1) * per);
     float s = 0.f;
     if (col < 2 * H)
+#pragma unroll 8
         for (int i = sl * per; i < end; ++i)
             s += part[static_cast<int64_t>(i) * 2 * H + col];
     meet[sl][lane] = s;
     __syncthreads();
     if (sl == 0 && col < 2 * H) {
-        s = ((meet[0][lane] + meet[1][lane]) + meet[2][lane]) + meet[3][lane];
+        s = meet[0][lane];
+#pragma unroll
+        for (int i = 1; i < kSlices; ++i)
+            s += meet[i][lane];
         float *out = col < H ? dgamma : dbeta;
         if (out) {
             out += col < H ? col : col - H;
@@ -305,11 +406,31 @@ __global__ __launch_bounds__(256) void ln_join_kernel(const float *part, int n, 
     }
 }
 
-// Threads and chunks for a row of H columns.
+// Threads and chunks for a row of H columns.  Forward: two chunks a thread
+// where a workgroup can hold them (16384 x 8192, us: four chunks of 256
+// threads 140, two of 512 112, one of 1024 120; 16384 x 2048 with its
+// checkpoint: four of a wave 44, one of 256 threads 38).  Backward: four,
+// which need fewer workgroups' partials.
 struct Shape {
     int nt, ch;
 };
-inline Shape shape_of(int H)
+inline Shape forward_shape(int H)
+{
+    if (H <= 512)
+        return {64, 1};
+    if (H <= 1024)
+        return {64, 2};
+    if (H <= 2048)
+        return {256, 1};
+    if (H <= 4096)
+        return {256, 2};
+    if (H <= 8192)
+        return {512, 2};
+    if (H <= 16384)
+        return {1024, 2};
+    return {1024, 4};
+}
+inline Shape backward_shape(int H)
 {
     if (H <= 512)
         return {64, 1};
@@ -321,15 +442,19 @@ inline Shape shape_of(int H)
         return {256, 2};
     if (H <= 8192)
         return {256, 4};
-    if (H <= 16384)
-        return {1024, 2};
-    return {1024, 4};
+    return {512, 4};
 }
 
-// Workgroups of the backward pass, which is also its number of partials.
+// Rows past this go without sums in the pass for dx.
+constexpr int kSumsH = 16384;
+
+// Workgroups of the backward pass, which is also its number of partials; for
+// wide rows the slices of the sums' own pass, of at least 32 rows.
 inline int bwd_groups(int64_t rows, int H)
 {
-    const int rpb = shape_of(H).nt == 64 ? 4 : 1;
+    if (H > kSumsH)
+        return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(rows / 32, 1024 / ((H + 511) / 512))));
+    const int rpb = backward_shape(H).nt == 64 ? 4 : 1;
     return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((rows + rpb - 1) / rpb, 512)));
 }
 
@@ -353,7 +478,7 @@ inline int check_mat(const void *p, int64_t rows, int64_t ld, int H, int dt, con
 template <typename T, bool AGAIN>
 int run_forward(const Fwd<T> &p, hipStream_t st)
 {
-    const Shape s = shape_of(p.H);
+    const Shape s = forward_shape(p.H);
     const int64_t blocks = s.nt == 64 ? (p.rows + 3) / 4 : p.rows;
     const dim3 grid(static_cast<unsigned>(blocks));
     const char *tag = AGAIN ? "ln_recompute" : "ln_forward";
@@ -362,32 +487,47 @@ int run_forward(const Fwd<T> &p, hipStream_t st)
         ACSC_LAUNCH(tag, (ln_forward_kernel<T, NT, CH, AGAIN>), grid, dim3(NT < 256 ? 256 : NT), 0, st, p);
     ACSC_CASE(64, 1)
     ACSC_CASE(64, 2)
-    ACSC_CASE(64, 4)
+    ACSC_CASE(256, 1)
     ACSC_CASE(256, 2)
-    ACSC_CASE(256, 4)
+    ACSC_CASE(512, 2)
     ACSC_CASE(1024, 2)
     ACSC_CASE(1024, 4)
 #undef ACSC_CASE
     return check_launch(tag);
 }
 
-template <typename T>
+template <typename T, bool KEPT>
 int run_backward(const Bwd<T> &p, int groups, hipStream_t st)
 {
-    const Shape s = shape_of(p.H);
+    if (p.H > kSumsH) {
+        if (p.part) {
+            const int per = static_cast<int>((p.rows + groups - 1) / groups);
+            ACSC_LAUNCH("ln_sums", (ln_sums_kernel<T, KEPT>), dim3((p.H + 511) / 512, groups), dim3(256), 0, st, p, per);
+        }
+        // after the sums, which read dy: dx may take its place
+        if (p.rows)
+            ACSC_LAUNCH("ln_backward", (ln_backward_kernel<T, 1024, 4, KEPT, false>),
+                        dim3(static_cast<unsigned>(std::min<int64_t>(p.rows, 1 << 20))), dim3(1024), 0, st, p);
+        return check_launch("ln_backward");
+    }
+    const Shape s = backward_shape(p.H);
     const dim3 grid(groups);
 #define ACSC_CASE(NT, CH)                                                                                       \
     if (s.nt == NT && s.ch == CH)                                                                             \
-        ACSC_LAUNCH("ln_backward", (ln_backward_kernel<T, NT, CH>), grid, dim3(NT < 256 ? 256 : NT), 0, st, p);
+        ACSC_LAUNCH("ln_backward", (ln_backward_kernel<T, NT, CH, KEPT, true>), grid, dim3(NT < 256 ? 256 : NT), 0, st, p);
     ACSC_CASE(64, 1)
     ACSC_CASE(64, 2)
     ACSC_CASE(64, 4)
     ACSC_CASE(256, 2)
     ACSC_CASE(256, 4)
-    ACSC_CASE(1024, 2)
-    ACSC_CASE(1024, 4)
+    ACSC_CASE(512, 4)
 #undef ACSC_CASE
     return check_launch("ln_backward");
+}
+template <typename T>
+int run_backward(const Bwd<T> &p, int groups, hipStream_t st)
+{
+    return p.q.codes ? run_backward<T, true>(p, groups, st) : run_backward<T, false>(p, groups, st);
 }
 
 template <typename T>
@@ -521,7 +661,7 @@ extern "C" int ln_backward(const void *dy, int64_t ld_dy, const void *x, int64_t
                                   as<float>(add), ld_add, static_cast<float *>(dx), ld_dx, part, rows, H}, groups, stream);
     if (rc || !sums)
         return rc;
-    ACSC_LAUNCH("ln_join", ln_join_kernel, dim3((2 * H + 63) / 64), dim3(256), 0, stream, part, groups, H, dgamma, dbeta,
+    ACSC_LAUNCH("ln_join", ln_join_kernel, dim3((2 * H + 63) / 64), dim3(64 * kSlices), 0, stream, part, groups, H, dgamma, dbeta,
                 accumulate);
     return check_launch("ln_join");
 }

@@ -122,36 +122,70 @@ __device__ __forceinline__ void load4(const float *p, int nv, float (&v)[4])
     }
 }
 
-// Eight consecutive elements or codes as they are; those past the first nv
-// become 0.
-__device__ __forceinline__ void load_raw(const uint16_t *p, int nv, uint16_t (&v)[8])
+// A code's value, rounded once as the format asks: not contracted into what
+// it is added to.
+__device__ __forceinline__ float code_value(float code, float scale)
+{
+#pragma clang fp contract(off)
+    return code * scale;
+}
+
+// Eight consecutive elements or codes as they are stored; those past the
+// first nv are 0.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<uint16_t> {
+    uint32_t w[4];
+    __device__ __forceinline__ float at(int i) const
+    {
+        return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    }
+};
+template <>
+struct Raw8<float> {
+    float w[8];
+    __device__ __forceinline__ float at(int i) const { return w[i]; }
+};
+struct Codes8 {
+    uint32_t w[2];
+    __device__ __forceinline__ float at(int i) const
+    {
+        return static_cast<float>(static_cast<int8_t>(w[i / 4] >> (8 * (i % 4))));
+    }
+};
+__device__ __forceinline__ void load_raw(const uint16_t *p, int nv, Raw8<uint16_t> &r)
 {
     if (nv >= 8) {
         const Bf8Any c = *reinterpret_cast<const Bf8Any *>(p);
-        __builtin_memcpy(v, &c, 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            r.w[i] = c.w[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v[i] = i < nv ? p[i] : 0;
-    }
-}
-__device__ __forceinline__ void load_raw(const float *p, int nv, float (&v)[8]) { load8(p, nv, v); }
-__device__ __forceinline__ void load_raw(const int8_t *p, int nv, uint32_t (&w)[2])
-{
-    if (nv >= 8) {
-        const C8Any c = *reinterpret_cast<const C8Any *>(p);
-        w[0] = c.w[0];
-        w[1] = c.w[1];
-    } else {
-        w[0] = w[1] = 0;
+        for (int i = 0; i < 4; ++i)
+            r.w[i] = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < nv)
-                w[i / 4] |= (static_cast<uint32_t>(p[i]) & 0xffu) << (8 * (i % 4));
+                r.w[i / 2] |= static_cast<uint32_t>(p[i]) << (16 * (i & 1));
     }
 }
-__device__ __forceinline__ float to_f32(uint16_t h) { return bf16_to_f32(h); }
-__device__ __forceinline__ float to_f32(float f) { return f; }
+__device__ __forceinline__ void load_raw(const float *p, int nv, Raw8<float> &r) { load8(p, nv, r.w); }
+__device__ __forceinline__ void load_raw(const int8_t *p, int nv, Codes8 &r)
+{
+    if (nv >= 8) {
+        const C8Any c = *reinterpret_cast<const C8Any *>(p);
+        r.w[0] = c.w[0];
+        r.w[1] = c.w[1];
+    } else {
+        r.w[0] = r.w[1] = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < nv)
+                r.w[i / 4] |= (static_cast<uint32_t>(p[i]) & 0xffu) << (8 * (i % 4));
+    }
+}
 
 // Values of N = 4 or 8 consecutive codes under one scale.
 template <int N>
@@ -164,11 +198,11 @@ __device__ __forceinline__ void load_codes(const int8_t *p, int nv, float scale,
         const Any c = *reinterpret_cast<const Any *>(p);
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            v[i] = static_cast<float>(static_cast<int8_t>(c.w[i / 4] >> (8 * (i % 4)))) * scale;
+            v[i] = code_value(static_cast<float>(static_cast<int8_t>(c.w[i / 4] >> (8 * (i % 4)))), scale);
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            v[i] = i < nv ? static_cast<float>(p[i]) * scale : 0.f;
+            v[i] = i < nv ? code_value(static_cast<float>(p[i]), scale) : 0.f;
     }
 }
 

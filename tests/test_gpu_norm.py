@@ -172,3 +172,21 @@ def test_gradients_against_differences(pk, H):
         diff = (f(*args(1)) - f(*args(-1))) / (2 * h)
         scale = float((grad.double() * d.double()).norm())
         assert abs(float(diff - (grad.double() * d.double()).sum())) <= 2e-3 * scale
+
+
+@pytest.mark.parametrize("kept", ["whole", "q8"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_wide_rows_whose_sums_take_a_pass_of_their_own(pk, dtype, kept):
+    """More than 16384 columns, enough rows for several slices of the column sums; dx in place of dy."""
+    rows, H = 131, 16385 if dtype == torch.float32 else 20000
+    x, gamma, beta, dy, add = tensors(rows, H, dtype, 0)
+    _, mu, rs, q = pk.ln_forward(x, gamma, beta, EPS, checkpoint=True)
+    src, value = (q, pk.q8_decode(q, torch.float32)) if kept == "q8" else (x, x)
+    rdx, rdg, rdb = ref_backward(dy, value, mu, rs, gamma, add)
+    h = (value.double() - mu.double()[:, None]) * rs.double()[:, None]
+    terms = ((dy.double() * h).abs().sum(0), dy.double().abs().sum(0))
+    into = dy.clone()
+    dx, dg, db = pk.ln_backward(into, src, mu, rs, gamma, add=add, dx=into)
+    near(dx, rdx, TOL[dtype])
+    for got, want, t in ((dg, rdg, terms[0]), (db, rdb, terms[1])):
+        assert ((got.double() - want).abs() <= 2.0 ** -24 * (rows + 8) * t).all()
