@@ -9,6 +9,7 @@ raises ``ImportError``.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import NamedTuple, Optional, Union
 
@@ -630,31 +631,47 @@ ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 LIN_FORWARD, LIN_BACKWARD_INPUT, LIN_BACKWARD_WEIGHT = 0, 1, 2
 
 
+# Small calls are bound by what these few lines cost on the host (a launch
+# takes 5 us): attributes are read once, pointers go as plain integers, sizes
+# that depend on shapes alone are kept.
+
 def _act(act: str) -> int:
-    if act not in ACTS:
+    code = ACTS.get(act)
+    if code is None:
         raise AcscError(ACSC_EINVAL, f"unknown activation {act!r}: one of {', '.join(ACTS)}")
-    return ACTS[act]
+    return code
+
+
+def _raw_stream(stream) -> int:
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def _rows(t: torch.Tensor, shape, dtype: torch.dtype, name: str) -> int:
     """The row stride of a [rows, cols] tensor with unit column stride."""
-    _need_cuda(t)
-    if t.dim() != 2 or tuple(t.shape) != tuple(shape) or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise AcscError(ACSC_EINVAL, f"{name} must be {list(shape)} with unit column stride")
-    if t.dtype != dtype:
+    if not t.is_cuda:
+        raise AcscError(ACSC_EINVAL, "tensors must live on the GPU")
+    if t.shape != shape:
+        raise AcscError(ACSC_EINVAL, f"{name} must be {list(shape)}, not {list(t.shape)}")
+    if t.dtype is not dtype:
         raise AcscError(ACSC_EDTYPE, f"{name} must be {dtype}, not {t.dtype}")
+    ld, unit = t.stride()
+    if unit != 1 and shape[1] > 1:
+        raise AcscError(ACSC_EINVAL, f"{name} must have unit column stride")
     # the stride of a single row, or of none, means nothing
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+    return ld if shape[0] > 1 else max(shape[1], 1)
 
 
-def _vec(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, name: str) -> None:
-    if t is None:
-        return
-    _need_cuda(t)
-    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+def _vec(t: torch.Tensor, n: int, dtype: torch.dtype, name: str) -> int:
+    """The address of a contiguous [n] tensor."""
+    if not t.is_cuda:
+        raise AcscError(ACSC_EINVAL, "tensors must live on the GPU")
+    if t.shape != (n,) or not t.is_contiguous():
         raise AcscError(ACSC_EINVAL, f"{name} must be [{n}] and contiguous")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise AcscError(ACSC_EDTYPE, f"{name} must be {dtype}, not {t.dtype}")
+    return t.data_ptr()
 
 
 def _two_d(t: torch.Tensor, name: str):
@@ -664,16 +681,15 @@ def _two_d(t: torch.Tensor, name: str):
 
 
 def _q8_new(rows: int, H: int, device) -> Q8:
-    return Q8(torch.empty(rows, H, dtype=torch.int8, device=device),
-              torch.empty(rows, -(-H // Q8_GROUP), dtype=torch.float32, device=device))
+    return Q8(torch.empty((rows, H), dtype=torch.int8, device=device),
+              torch.empty((rows, -(-H // Q8_GROUP)), dtype=torch.float32, device=device))
 
 
-def _q8_ref(q: Optional[Q8], rows: int, H: int):
-    if q is None:
-        return None
-    ldc = _rows(q.codes, (rows, H), torch.int8, "codes")
-    lds = _rows(q.scales, (rows, -(-H // Q8_GROUP)), torch.float32, "scales")
-    return C.byref(_Q8Tensor(_p(q.codes), _p(q.scales), ldc, lds))
+def _q8_ref(q: Q8, rows: int, H: int):
+    codes, scales = q
+    ldc = _rows(codes, (rows, H), torch.int8, "codes")
+    lds = _rows(scales, (rows, -(-H // Q8_GROUP)), torch.float32, "scales")
+    return C.byref(_Q8Tensor(codes.data_ptr(), scales.data_ptr(), ldc, lds))
 
 
 def _kept(src: Union[torch.Tensor, Q8, None], shape, dtype: torch.dtype, name: str):
@@ -681,17 +697,32 @@ def _kept(src: Union[torch.Tensor, Q8, None], shape, dtype: torch.dtype, name: s
     if src is None:
         return None, 0, None
     if isinstance(src, Q8):
-        return None, 0, _q8_ref(src, *shape)
+        return None, 0, _q8_ref(src, shape[0], shape[1])
     ld = _rows(src, shape, dtype, name)
-    return _ptr(src), ld, None
+    return src.data_ptr(), ld, None
 
 
 def _ws(nbytes: int, ws: Optional[torch.Tensor], device, stream):
-    if ws is None and nbytes:
+    """(address, bytes, what keeps it alive) of a workspace: the given one, or a new one."""
+    if ws is None:
+        if not nbytes:
+            return None, 0, None
         ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
         if stream is not None:
             ws.record_stream(stream)   # freed here, perhaps before that stream has used it
-    return _ptr(ws), (ws.numel() * ws.element_size() if ws is not None else 0), ws
+        return ws.data_ptr(), nbytes, ws
+    _need_cuda(ws)
+    return ws.data_ptr(), ws.numel() * ws.element_size(), ws
+
+
+@functools.lru_cache(maxsize=1024)
+def _lin_bytes(aligned: bool, op: int, rows: int, n_in: int, n_out: int, dtype: torch.dtype) -> int:
+    return (lin_workspace_size if aligned else lin_workspace_size_unaligned)(op, rows, n_in, n_out, dtype)
+
+
+@functools.lru_cache(maxsize=1024)
+def _ln_bytes(rows: int, H: int) -> int:
+    return ln_workspace_size(rows, H)
 
 
 def q8_encode(x: torch.Tensor, q: Optional[Q8] = None, stream=None) -> Q8:
@@ -700,7 +731,9 @@ def q8_encode(x: torch.Tensor, q: Optional[Q8] = None, stream=None) -> Q8:
     dt, ld = _dt(x), _rows(x, x.shape, x.dtype, "x")
     if q is None:
         q = _q8_new(rows, H, x.device)
-    _check(lib.q8_encode(_ptr(x), dt, rows, H, ld, _q8_ref(q, rows, H), _stream(stream)))
+    rc = lib.q8_encode(x.data_ptr(), dt, rows, H, ld, _q8_ref(q, rows, H), _raw_stream(stream))
+    if rc:
+        _check(rc)
     return q
 
 
@@ -709,9 +742,11 @@ def q8_decode(q: Q8, dtype: torch.dtype, act: str = "none", y: Optional[torch.Te
     """act(values of q) [rows, H], rounded once to dtype."""
     rows, H = _two_d(q.codes, "codes")
     if y is None:
-        y = torch.empty(rows, H, dtype=dtype, device=q.codes.device)
+        y = torch.empty((rows, H), dtype=dtype, device=q.codes.device)
     ld = _rows(y, (rows, H), dtype, "y")
-    _check(lib.q8_decode(_q8_ref(q, rows, H), rows, H, _act(act), _ptr(y), _dt(y), ld, _stream(stream)))
+    rc = lib.q8_decode(_q8_ref(q, rows, H), rows, H, _act(act), y.data_ptr(), _dt(y), ld, _raw_stream(stream))
+    if rc:
+        _check(rc)
     return y
 
 
@@ -719,18 +754,22 @@ def ln_forward(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Opti
                eps: float = 1e-5, checkpoint: bool = False, y: Optional[torch.Tensor] = None, stream=None):
     """Layer norm of the rows of x [rows, H]: (y, mean [rows], rstd [rows], q),
     q the 8-bit checkpoint of x if asked for, else None."""
-    rows, H = _two_d(x, "x")
-    dt, ld = _dt(x), _rows(x, x.shape, x.dtype, "x")
-    _vec(gamma, H, x.dtype, "gamma")
-    _vec(beta, H, x.dtype, "beta")
+    shape = rows, H = _two_d(x, "x")
+    dtype, dev = x.dtype, x.device
+    ld = _rows(x, shape, dtype, "x")
+    pg = None if gamma is None else _vec(gamma, H, dtype, "gamma")
+    pb = None if beta is None else _vec(beta, H, dtype, "beta")
     if y is None:
-        y = torch.empty(rows, H, dtype=x.dtype, device=x.device)
-    ldy = _rows(y, x.shape, x.dtype, "y")
-    mean = torch.empty(rows, dtype=torch.float32, device=x.device)
-    rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-    q = _q8_new(rows, H, x.device) if checkpoint else None
-    _check(lib.ln_forward(_ptr(x), dt, rows, H, ld, _ptr(gamma), _ptr(beta), float(eps), _ptr(y), ldy, _ptr(mean),
-                          _ptr(rstd), _q8_ref(q, rows, H), _stream(stream)))
+        y, ldy = torch.empty((rows, H), dtype=dtype, device=dev), max(H, 1)
+    else:
+        ldy = _rows(y, shape, dtype, "y")
+    mean = torch.empty(rows, dtype=torch.float32, device=dev)
+    rstd = torch.empty(rows, dtype=torch.float32, device=dev)
+    q = _q8_new(rows, H, dev) if checkpoint else None
+    rc = lib.ln_forward(x.data_ptr(), _dt(x), rows, H, ld, pg, pb, eps, y.data_ptr(), ldy, mean.data_ptr(),
+                        rstd.data_ptr(), None if q is None else _q8_ref(q, rows, H), _raw_stream(stream))
+    if rc:
+        _check(rc)
     return y, mean, rstd, q
 
 
@@ -740,14 +779,13 @@ def ln_recompute(src: Union[torch.Tensor, Q8], mean: torch.Tensor, rstd: torch.T
     """ln_forward's y again from x or its checkpoint and the kept statistics."""
     rows, H = _two_d(src.codes if isinstance(src, Q8) else src, "src")
     p, ld, q = _kept(src, (rows, H), dtype, "src")
-    for t, n, d, name in ((mean, rows, torch.float32, "mean"), (rstd, rows, torch.float32, "rstd"),
-                          (gamma, H, dtype, "gamma"), (beta, H, dtype, "beta")):
-        _vec(t, n, d, name)
+    pm, pr = _vec(mean, rows, torch.float32, "mean"), _vec(rstd, rows, torch.float32, "rstd")
+    pg = None if gamma is None else _vec(gamma, H, dtype, "gamma")
+    pb = None if beta is None else _vec(beta, H, dtype, "beta")
     if y is None:
-        y = torch.empty(rows, H, dtype=dtype, device=mean.device)
+        y = torch.empty((rows, H), dtype=dtype, device=mean.device)
     ldy = _rows(y, (rows, H), dtype, "y")
-    _check(lib.ln_recompute(p, ld, q, _dt(y), rows, H, _ptr(mean), _ptr(rstd), _ptr(gamma), _ptr(beta), _ptr(y), ldy,
-                            _stream(stream)))
+    _check(lib.ln_recompute(p, ld, q, _dt(y), rows, H, pm, pr, pg, pb, y.data_ptr(), ldy, _raw_stream(stream)))
     return y
 
 
@@ -765,26 +803,29 @@ def ln_backward(dy: torch.Tensor, src: Union[torch.Tensor, Q8], mean: torch.Tens
     """(dx, dgamma, dbeta) of ln_forward from x or its checkpoint; add: the
     gradient that reaches x past the norm.  dgamma, dbeta: fp32 [H]; with
     accumulate they are given and added to."""
-    rows, H = _two_d(dy, "dy")
-    dt, lddy = _dt(dy), _rows(dy, dy.shape, dy.dtype, "dy")
-    p, ld, q = _kept(src, (rows, H), dy.dtype, "src")
-    ldadd = _rows(add, dy.shape, dy.dtype, "add") if add is not None else 0
+    shape = rows, H = _two_d(dy, "dy")
+    dtype, dev = dy.dtype, dy.device
+    lddy = _rows(dy, shape, dtype, "dy")
+    p, ld, q = _kept(src, shape, dtype, "src")
+    pa, ldadd = (None, 0) if add is None else (add.data_ptr(), _rows(add, shape, dtype, "add"))
     if accumulate and (dgamma is None or dbeta is None):
         raise AcscError(ACSC_EINVAL, "accumulate needs dgamma and dbeta")
     if dx is None:
-        dx = torch.empty(rows, H, dtype=dy.dtype, device=dy.device)
+        dx, lddx = torch.empty((rows, H), dtype=dtype, device=dev), max(H, 1)
+    else:
+        lddx = _rows(dx, shape, dtype, "dx")
     if dgamma is None:
-        dgamma = torch.empty(H, dtype=torch.float32, device=dy.device)
+        dgamma = torch.empty(H, dtype=torch.float32, device=dev)
     if dbeta is None:
-        dbeta = torch.empty(H, dtype=torch.float32, device=dy.device)
-    for t, n, d, name in ((mean, rows, torch.float32, "mean"), (rstd, rows, torch.float32, "rstd"),
-                          (gamma, H, dy.dtype, "gamma"), (dgamma, H, torch.float32, "dgamma"),
-                          (dbeta, H, torch.float32, "dbeta")):
-        _vec(t, n, d, name)
-    lddx = _rows(dx, dy.shape, dy.dtype, "dx")
-    wp, wn, keep = _ws(ln_workspace_size(rows, H), ws, dy.device, stream)
-    _check(lib.ln_backward(_ptr(dy), lddy, p, ld, q, dt, rows, H, _ptr(mean), _ptr(rstd), _ptr(gamma), _ptr(add), ldadd,
-                           _ptr(dx), lddx, _ptr(dgamma), _ptr(dbeta), int(accumulate), wp, wn, _stream(stream)))
+        dbeta = torch.empty(H, dtype=torch.float32, device=dev)
+    pm, pr = _vec(mean, rows, torch.float32, "mean"), _vec(rstd, rows, torch.float32, "rstd")
+    pg = None if gamma is None else _vec(gamma, H, dtype, "gamma")
+    wp, wn, keep = _ws(_ln_bytes(rows, H), ws, dev, stream)
+    rc = lib.ln_backward(dy.data_ptr(), lddy, p, ld, q, _dt(dy), rows, H, pm, pr, pg, pa, ldadd, dx.data_ptr(), lddx,
+                         _vec(dgamma, H, torch.float32, "dgamma"), _vec(dbeta, H, torch.float32, "dbeta"),
+                         int(accumulate), wp, wn, _raw_stream(stream))
+    if rc:
+        _check(rc)
     return dx, dgamma, dbeta
 
 
@@ -805,14 +846,15 @@ def lin_workspace_size_unaligned(op: int, rows: int, n_in: int, n_out: int, dtyp
     return b.value
 
 
-def _lin_ws(op: int, rows: int, n_in: int, n_out: int, ops, ws: Optional[torch.Tensor], stream):
-    """A workspace for a product of these (tensor, row stride) operands, unless one is given."""
-    t = ops[0][0]
+def _lin_ws(op: int, rows: int, n_in: int, n_out: int, a, lda: int, b, ldb: int, ws: Optional[torch.Tensor], stream):
+    """A workspace for a product of operands a and b (their row strides; b may
+    be None), unless one is given."""
     if ws is not None:
-        return _ws(0, ws, t.device, stream)
-    plain = all(ld % 8 == 0 and o.data_ptr() % 16 == 0 and ld < 1 << 22 for o, ld in ops)
-    size = lin_workspace_size if plain else lin_workspace_size_unaligned
-    return _ws(size(op, rows, n_in, n_out, t.dtype), ws, t.device, stream)
+        return _ws(0, ws, a.device, stream)
+    aligned = not ((lda | a.data_ptr() >> 1) & 7) and lda < 1 << 22
+    if b is not None:
+        aligned = aligned and not ((ldb | b.data_ptr() >> 1) & 7) and ldb < 1 << 22
+    return _ws(_lin_bytes(aligned, op, rows, n_in, n_out, a.dtype), None, a.device, stream)
 
 
 def lin_forward(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
@@ -823,33 +865,46 @@ def lin_forward(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
     keep is "q8", else None."""
     rows, n_in = _two_d(x, "x")
     n_out = _two_d(W, "W")[0]
-    dt, ldx, ldw = _dt(x), _rows(x, x.shape, x.dtype, "x"), _rows(W, (n_out, n_in), x.dtype, "W")
-    _vec(bias, n_out, x.dtype, "bias")
+    dtype, dev = x.dtype, x.device
+    ldx, ldw = _rows(x, (rows, n_in), dtype, "x"), _rows(W, (n_out, n_in), dtype, "W")
+    pb = None if bias is None else _vec(bias, n_out, dtype, "bias")
     shape = (rows, n_out)
-    ldr = _rows(residual, shape, x.dtype, "residual") if residual is not None else 0
+    pr, ldr = (None, 0) if residual is None else (residual.data_ptr(), _rows(residual, shape, dtype, "residual"))
     if y is None:
-        y = torch.empty(shape, dtype=x.dtype, device=x.device)
-    ldy = _rows(y, shape, x.dtype, "y")
-    if keep not in (None, "z", "q8"):
+        y, ldy = torch.empty(shape, dtype=dtype, device=dev), n_out
+    else:
+        ldy = _rows(y, shape, dtype, "y")
+    z = q = pz = pq = None
+    if keep == "z":
+        z = torch.empty(shape, dtype=dtype, device=dev)
+        pz = z.data_ptr()
+    elif keep == "q8":
+        q = _q8_new(rows, n_out, dev)
+        pq = _q8_ref(q, rows, n_out)
+    elif keep is not None:
         raise AcscError(ACSC_EINVAL, f"keep must be None, 'z' or 'q8', not {keep!r}")
-    z = torch.empty(shape, dtype=x.dtype, device=x.device) if keep == "z" else None
-    q = _q8_new(rows, n_out, x.device) if keep == "q8" else None
-    wp, wn, hold = _lin_ws(LIN_FORWARD, rows, n_in, n_out, ((x, ldx), (W, ldw)), ws, stream)
-    _check(lib.lin_forward(_ptr(x), ldx, dt, rows, n_in, n_out, _ptr(W), ldw, _ptr(bias), _act(act), _ptr(residual), ldr,
-                           _ptr(y), ldy, _ptr(z), n_out, _q8_ref(q, rows, n_out), wp, wn, _stream(stream)))
+    wp, wn, hold = _lin_ws(LIN_FORWARD, rows, n_in, n_out, x, ldx, W, ldw, ws, stream)
+    rc = lib.lin_forward(x.data_ptr(), ldx, _dt(x), rows, n_in, n_out, W.data_ptr(), ldw, pb, _act(act), pr, ldr,
+                         y.data_ptr(), ldy, pz, n_out, pq, wp, wn, _raw_stream(stream))
+    if rc:
+        _check(rc)
     return y, (z if q is None else q)
 
 
 def lin_backward_act(dy: torch.Tensor, z: Union[torch.Tensor, Q8], act: str, dz: Optional[torch.Tensor] = None,
                      stream=None) -> torch.Tensor:
     """dz = dy act'(z) from the kept pre-activation or its checkpoint."""
-    rows, n = _two_d(dy, "dy")
-    ld = _rows(dy, dy.shape, dy.dtype, "dy")
-    p, ldz, q = _kept(z, (rows, n), dy.dtype, "z")
+    shape = rows, n = _two_d(dy, "dy")
+    ld = _rows(dy, shape, dy.dtype, "dy")
+    p, ldz, q = _kept(z, shape, dy.dtype, "z")
     if dz is None:
-        dz = torch.empty(rows, n, dtype=dy.dtype, device=dy.device)
-    lddz = _rows(dz, dy.shape, dy.dtype, "dz")
-    _check(lib.lin_backward_act(_ptr(dy), ld, p, ldz, q, _dt(dy), rows, n, _act(act), _ptr(dz), lddz, _stream(stream)))
+        dz, lddz = torch.empty((rows, n), dtype=dy.dtype, device=dy.device), max(n, 1)
+    else:
+        lddz = _rows(dz, shape, dy.dtype, "dz")
+    rc = lib.lin_backward_act(dy.data_ptr(), ld, p, ldz, q, _dt(dy), rows, n, _act(act), dz.data_ptr(), lddz,
+                              _raw_stream(stream))
+    if rc:
+        _check(rc)
     return dz
 
 
@@ -860,14 +915,18 @@ def lin_backward_input(dz: torch.Tensor, W: torch.Tensor, act: str = "none",
     n_in] that the layer before kept, or its checkpoint."""
     rows, n_out = _two_d(dz, "dz")
     n_in = _two_d(W, "W")[1]
-    lddz, ldw = _rows(dz, dz.shape, dz.dtype, "dz"), _rows(W, (n_out, n_in), dz.dtype, "W")
-    p, ldz, q = _kept(z, (rows, n_in), dz.dtype, "z")
+    dtype, dev = dz.dtype, dz.device
+    lddz, ldw = _rows(dz, (rows, n_out), dtype, "dz"), _rows(W, (n_out, n_in), dtype, "W")
+    p, ldz, q = _kept(z, (rows, n_in), dtype, "z")
     if dx is None:
-        dx = torch.empty(rows, n_in, dtype=dz.dtype, device=dz.device)
-    lddx = _rows(dx, (rows, n_in), dz.dtype, "dx")
-    wp, wn, hold = _lin_ws(LIN_BACKWARD_INPUT, rows, n_in, n_out, ((dz, lddz), (W, ldw)), ws, stream)
-    _check(lib.lin_backward_input(_ptr(dz), lddz, _dt(dz), rows, n_in, n_out, _ptr(W), ldw, _act(act), p, ldz, q, _ptr(dx),
-                                  lddx, wp, wn, _stream(stream)))
+        dx, lddx = torch.empty((rows, n_in), dtype=dtype, device=dev), n_in
+    else:
+        lddx = _rows(dx, (rows, n_in), dtype, "dx")
+    wp, wn, hold = _lin_ws(LIN_BACKWARD_INPUT, rows, n_in, n_out, dz, lddz, W, ldw, ws, stream)
+    rc = lib.lin_backward_input(dz.data_ptr(), lddz, _dt(dz), rows, n_in, n_out, W.data_ptr(), ldw, _act(act), p, ldz, q,
+                                dx.data_ptr(), lddx, wp, wn, _raw_stream(stream))
+    if rc:
+        _check(rc)
     return dx
 
 
@@ -881,17 +940,24 @@ def lin_backward_weight(dz: torch.Tensor, x: Union[torch.Tensor, Q8], act: str =
     and added to."""
     rows, n_out = _two_d(dz, "dz")
     n_in = _two_d(x.codes if isinstance(x, Q8) else x, "x")[1]
-    lddz = _rows(dz, dz.shape, dz.dtype, "dz")
-    p, ldx, q = _kept(x, (rows, n_in), dz.dtype, "x")
+    dtype, dev = dz.dtype, dz.device
+    lddz = _rows(dz, (rows, n_out), dtype, "dz")
+    p, ldx, q = _kept(x, (rows, n_in), dtype, "x")
     if accumulate and (dW is None or (bias and db is None)):
         raise AcscError(ACSC_EINVAL, "accumulate needs dW and db")
     if dW is None:
-        dW = torch.empty(n_out, n_in, dtype=dw_dtype or dz.dtype, device=dz.device)
+        dW, lddw = torch.empty((n_out, n_in), dtype=dw_dtype or dtype, device=dev), n_in
+    else:
+        lddw = _rows(dW, (n_out, n_in), dw_dtype or dW.dtype, "dW")
     if db is None and bias:
-        db = torch.empty(n_out, dtype=torch.float32, device=dz.device)
-    _vec(db, n_out, torch.float32, "db")
-    lddw = _rows(dW, (n_out, n_in), dw_dtype or dW.dtype, "dW")
-    wp, wn, hold = _lin_ws(LIN_BACKWARD_WEIGHT, rows, n_in, n_out, ((dz, lddz),) if q is not None else ((dz, lddz), (x, ldx)), ws, stream)
-    _check(lib.lin_backward_weight(_ptr(dz), lddz, p, ldx, q, _act(act), _dt(dz), rows, n_in, n_out, _ptr(dW), _dt(dW), lddw,
-                                   _ptr(db), int(accumulate), wp, wn, _stream(stream)))
+        db = torch.empty(n_out, dtype=torch.float32, device=dev)
+    pdb = None if db is None else _vec(db, n_out, torch.float32, "db")
+    code = _act(act)
+    # the activation is recomputed into the workspace: no operand of the caller's
+    wp, wn, hold = _lin_ws(LIN_BACKWARD_WEIGHT, rows, n_in, n_out, dz, lddz, None if q is not None or code else x, ldx, ws,
+                           stream)
+    rc = lib.lin_backward_weight(dz.data_ptr(), lddz, p, ldx, q, code, _dt(dz), rows, n_in, n_out, dW.data_ptr(), _dt(dW),
+                                 lddw, pdb, int(accumulate), wp, wn, _raw_stream(stream))
+    if rc:
+        _check(rc)
     return dW, db
