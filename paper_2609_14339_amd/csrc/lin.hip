@@ -156,38 +156,40 @@ __global__ __launch_bounds__(256) void lin_join_kernel(Gemm g)
     }
 }
 
-// Column sums of dz for db: eight columns a lane, 512 a workgroup, whose four
-// waves take every fourth row of its `per` rows and meet in LDS in order.
-// One slice of rows writes db, several leave partials.
+// Column sums of dz for db: eight columns a lane, 512 a workgroup, whose
+// sixteen waves take every sixteenth row of its `per` rows and meet in LDS in
+// order.  One slice of rows writes db, several leave partials.
+constexpr int kDbWaves = 16;
 template <typename T>
-__global__ __launch_bounds__(256) void lin_db_kernel(const T *dz, int64_t ld, int64_t rows, int N, int per, float *part,
-                                                     float *db, int accumulate)
+__global__ __launch_bounds__(64 * kDbWaves) void lin_db_kernel(const T *dz, int64_t ld, int64_t rows, int N, int per,
+                                                               float *part, float *db, int accumulate)
 {
-    __shared__ float meet[4][512];
+    __shared__ float meet[kDbWaves][512];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n = blockIdx.x * 512 + lane * 8;
     const int64_t end = min<int64_t>(rows, (blockIdx.y + static_cast<int64_t>(1)) * per);
     float s[8] = {};
 #pragma unroll 4
-    for (int64_t r = blockIdx.y * static_cast<int64_t>(per) + wave; r < end; r += 4) {
-        float v[8];
-        load8(dz + r * ld + n, N - n, v);
+    for (int64_t r = blockIdx.y * static_cast<int64_t>(per) + wave; r < end; r += kDbWaves) {
+        Raw8<T> v;
+        load_raw(dz + r * ld + n, N - n, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            s[i] += v[i];
+            s[i] += v.at(i);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         meet[wave][i * 64 + lane] = s[i];
     __syncthreads();
-    for (int c = threadIdx.x; c < 512; c += 256) {
-        const int at = (c & 7) * 64 + (c >> 3), col = blockIdx.x * 512 + c;
-        if (col < N) {
-            const float v = ((meet[0][at] + meet[1][at]) + meet[2][at]) + meet[3][at];
-            if (part)
-                part[static_cast<int64_t>(blockIdx.y) * N + col] = v;
-            else
-                db[col] = accumulate ? db[col] + v : v;
-        }
+    const int c = threadIdx.x, at = (c & 7) * 64 + (c >> 3), col = blockIdx.x * 512 + c;
+    if (c < 512 && col < N) {
+        float v = meet[0][at];
+#pragma unroll
+        for (int w = 1; w < kDbWaves; ++w)
+            v += meet[w][at];
+        if (part)
+            part[static_cast<int64_t>(blockIdx.y) * N + col] = v;
+        else
+            db[col] = accumulate ? db[col] + v : v;
     }
 }
 
@@ -294,7 +296,8 @@ inline bool readable(const Operand &o, bool col, int64_t inner)
 // (or of an fp32 tile).  Measured on bf16 products, us: a 256 tile takes 1.5 a
 // step of 64 and 5 beside them (4096 x 2048 -> 8192: 56 a round of 32 steps);
 // a 128 tile 1.0 and 3 with a second one on its CU (2048 x 2048 -> 8192: 34.5
-// a round), 0.65 alone; the pieces' sum 4 for the launch and their bytes,
+// a round), 0.65 alone; an fp32 tile 4.8 a step of 32 (112 TFLOP/s at 4096^3),
+// 2.6 alone; the pieces' sum 4 for the launch and their bytes,
 // written and read, at 4.5 TB/s.  (256-tiles only where they fill a round,
 // without this: 2048 x 2048 -> 8192 in 99 us, with it 69.)
 struct Cut {
@@ -306,7 +309,7 @@ inline Cut cut_of(const Shape &s, int steps, bool bf16)
     double least = 0;
     for (int tile = bf16 ? 256 : 128; tile >= 128; tile -= 128) {
         const int64_t tiles = ((s.M + tile - 1) / tile) * ((s.N + tile - 1) / tile);
-        const double step = !bf16 ? 6.0 : tile == 256 ? 1.5 : 1.0, alone = !bf16 ? 3.5 : tile == 256 ? 1.5 : 0.65;
+        const double step = !bf16 ? 4.8 : tile == 256 ? 1.5 : 1.0, alone = !bf16 ? 2.6 : tile == 256 ? 1.5 : 0.65;
         const double edge = tile == 256 ? 5 : 3;
         const int slots = tile == 256 ? 256 : 512;
         for (int want = 1; want == 1 || (want <= 64 && steps / want >= 4 && tiles * want <= 2048); want += want < 8 ? 1 : 8) {
@@ -354,9 +357,10 @@ inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bo
     p.ldp = up8(s.N);
     p.part = p.splits > 1 ? up256(static_cast<size_t>(p.splits) * s.M * p.ldp * 4) : 0;
     if (kind == kWeight) {
-        // db's slices of at least 32 rows, up to about two workgroups a CU
+        // db's slices of at least 64 rows, four a wave, up to about one
+        // workgroup a CU; up to 128 rows in one, without a launch to join them
         const int64_t blocks = (s.M + 511) / 512;
-        p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(512 / blocks, s.K / 32)));
+        p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(256 / blocks, s.K <= 128 ? 1 : s.K / 64)));
         p.slice = (s.K + p.slices - 1) / p.slices;
         p.slices = (s.K + p.slice - 1) / p.slice;
         p.db = p.slices > 1 ? up256(static_cast<size_t>(p.slices) * s.M * 4) : 0;
@@ -405,10 +409,10 @@ int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype
         const dim3 grid(static_cast<unsigned>((g.M + 511) / 512), p.slices);
         const int n = static_cast<int>(g.M);
         if (dt == ACSC_BF16)
-            ACSC_LAUNCH("lin_db", lin_db_kernel<uint16_t>, grid, dim3(256), 0, st, static_cast<const uint16_t *>(g.A.p), g.A.ld,
+            ACSC_LAUNCH("lin_db", lin_db_kernel<uint16_t>, grid, dim3(64 * kDbWaves), 0, st, static_cast<const uint16_t *>(g.A.p), g.A.ld,
                         static_cast<int64_t>(s.K), n, p.slice, part, db, g.e.accumulate);
         else
-            ACSC_LAUNCH("lin_db", lin_db_kernel<float>, grid, dim3(256), 0, st, static_cast<const float *>(g.A.p), g.A.ld,
+            ACSC_LAUNCH("lin_db", lin_db_kernel<float>, grid, dim3(64 * kDbWaves), 0, st, static_cast<const float *>(g.A.p), g.A.ld,
                         static_cast<int64_t>(s.K), n, p.slice, part, db, g.e.accumulate);
         if (part)
             ACSC_LAUNCH("lin_join_db", lin_join_db_kernel, dim3((n + 255) / 256), dim3(256), 0, st, part, n, p.slices, db,
