@@ -47,6 +47,13 @@ struct Gemm {
     Epi e;
 };
 
+// A kept input of the weight gradient: its checkpoint (or none: the tensor),
+// and the activation that it still has to go through.
+struct Kept {
+    Q8 q;
+    int act;
+};
+
 // What the epilogue reads beside the sums for eight columns of a row: the
 // residual (forward), the kept pre-activation or its codes and scale (gate),
 // or the output to add to (weight).

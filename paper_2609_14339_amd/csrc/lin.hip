@@ -7,16 +7,24 @@ namespace acsc {
 int q8_decode_run(const Q8 &q, int64_t rows, int H, int act, void *y, acsc_dtype dt, int64_t ldy, hipStream_t st);
 int lin_bf16_pack(const void *x, int64_t ldx, int64_t rows, int cols, void *y, int64_t ldy, hipStream_t st);
 int lin_few_run(const Gemm &g, acsc_dtype dt, hipStream_t st, const char *tag);
+int lin_few_weight_run(const Gemm &g, const Kept &kept, acsc_dtype dt, acsc_dtype out, float *db, hipStream_t st,
+                       const char *tag);
 int lin_bf16_run(const Gemm &g, int tile, EpiKind kind, acsc_dtype out, hipStream_t st, const char *tag);
 
 namespace {
 
 constexpr int kTile = 128, kBK = 32;
 
-// Tokens up to which a forward product reads W once and unstaged.  4096 ->
-// 14336, 1 / 8 / 16 / 32 tokens, us: bf16 24.1, 28.3, 34.9, 48.5 against 31 by
-// tiles for each; fp32 53, 60, 68, 103 against 170.
-inline int few_tokens(bool bf16) { return bf16 ? 8 : 32; }
+// Tokens up to which a product does without tiles.  Forward: W is read once
+// and unstaged; 4096 -> 14336, 1 / 8 / 16 / 32 tokens, us: bf16 24.1, 28.3, 34.9,
+// 48.5 against 31 by tiles for each; fp32 53, 60, 68, 103 against 170.  Weight
+// gradient: outer products of unrounded activations; bf16 8192 -> 8192, 1 / 4 /
+// 8 tokens: 25.6, 30.0, 38.8 against 43 by tiles.  (The input gradient by
+// vector FMAs on rows of W read once took 39 against 36 by tiles.)
+inline int few_tokens(EpiKind kind, bool bf16)
+{
+    return kind == kForward ? (bf16 ? 8 : 32) : kind == kWeight ? 8 : 0;
+}
 
 // The fp32 product on v_mfma_f32_16x16x4_f32: 128 x 128 tiles, four waves of
 // 32 rows by 128 columns, so that a wave holds whole checkpoint groups.  The
@@ -335,7 +343,12 @@ inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bo
     const bool bf16 = dt == ACSC_BF16;
     const int bk = bf16 ? 64 : kBK;
     const int steps = (s.K + bk - 1) / bk;
-    if (kind == kForward && s.M <= few_tokens(bf16)) {
+    if (kind == kWeight && s.K <= few_tokens(kind, bf16)) {
+        p.few = true;
+        p.splits = 1;
+        return p;
+    }
+    if (kind == kForward && s.M <= few_tokens(kind, bf16)) {
         // 16 outputs a workgroup: a cut only where they fill half the CUs at
         // most, at two rounds of eight lines a piece
         const int groups = (s.N + 15) / 16, round = 8 * 128 / static_cast<int>(dtype_size(dt)), rounds = (s.K + round - 1) / round;
@@ -535,7 +548,8 @@ static int workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dty
     const Operand best{nullptr, 8};
     const bool a = !any && readable(best, s.acol, s.acol ? s.M : s.K);
     const bool b = !any && readable(best, s.bcol, s.bcol ? s.N : s.K);
-    *bytes = plan_of(kind, s, dt, a, b).bytes() + (kind == kWeight ? recomputed_bytes(rows, n_in, dt) : 0);
+    *bytes = plan_of(kind, s, dt, a, b).bytes() +
+             (kind == kWeight && rows > few_tokens(kind, dt == ACSC_BF16) ? recomputed_bytes(rows, n_in, dt) : 0);
     return ACSC_OK;
 }
 
@@ -693,13 +707,23 @@ extern "C" int lin_backward_weight(const void *dz, int64_t ld_dz, const void *x,
                         static_cast<int64_t>(1), n_out);
         return check_launch("lin_zero");
     }
+    // Few tokens: from what was kept, in one kernel.  Otherwise
     // the activation, or the checkpoint's values, whole: read once here, and
     // by the product many times.  Its rows end at a multiple of eight, so the
     // product reads it where it is.
-    const bool again = q || act != ACSC_ACT_NONE;
-    const size_t whole = again ? recomputed_bytes(rows, n_in, dt) : 0;
     const Shape s = shape_of(kWeight, rows, n_in, n_out);
     Gemm g{};
+    g.e = Epi{dW, ld_dw, nullptr, nullptr, 0, nullptr, 0, q8_of(nullptr), ACSC_ACT_NONE, accumulate};
+    if (rows <= few_tokens(kWeight, dt == ACSC_BF16)) {
+        g.A = {dz, ld_dz};
+        g.B = {x, ld_x};
+        g.M = s.M;
+        g.N = s.N;
+        g.K = s.K;
+        return lin_few_weight_run(g, Kept{q8_of(q), act}, dt, dw_dt, db, stream, "lin_backward_weight");
+    }
+    const bool again = q || act != ACSC_ACT_NONE;
+    const size_t whole = again ? recomputed_bytes(rows, n_in, dt) : 0;
     g.A = {dz, ld_dz};
     g.B = again ? Operand{ws, up8(n_in)} : Operand{x, ld_x};
     const Plan p = plan_of(kWeight, s, dt, readable(g.A, true, n_out), again || readable(g.B, true, n_in));
@@ -724,6 +748,5 @@ extern "C" int lin_backward_weight(const void *dz, int64_t ld_dz, const void *x,
         if (rc)
             return rc;
     }
-    g.e = Epi{dW, ld_dw, nullptr, nullptr, 0, nullptr, 0, q8_of(nullptr), ACSC_ACT_NONE, accumulate};
     return run_product(g, kWeight, p, s, dt, dw_dt, static_cast<char *>(ws) + whole, db, stream, "lin_backward_weight");
 }

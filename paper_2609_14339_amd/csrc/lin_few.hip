@@ -135,6 +135,84 @@ __global__ __launch_bounds__(kWaves * 64) void lin_few_kernel(Gemm g)
     }
 }
 
+// The weight gradient of few tokens: outer products, bound by writing dW.  A
+// lane holds eight columns of the T inputs in fp32 (formed here from what was
+// kept, so nothing is rounded on the way), a wave `per` rows of dW one after
+// the other; dz waits in LDS.  The workgroups of the first columns add up db.
+constexpr int kRowsMost = 64;
+template <typename T, typename TO, int TT>
+__global__ __launch_bounds__(256) void lin_few_weight_kernel(Gemm g, Kept kept, int per, float *db)
+{
+    __shared__ __align__(16) float dz[4 * kRowsMost][TT];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int n = blockIdx.x * 512 + lane * 8, left = g.N - n;
+    const int64_t m0 = static_cast<int64_t>(blockIdx.y) * 4 * per;
+    const int rows = static_cast<int>(min<int64_t>(g.M - m0, 4 * per));
+    for (int i = threadIdx.x; i < rows * TT; i += 256) {
+        const int t = i / rows, r = i - t * rows;
+        float v = 0.f;
+        if (t < g.K) {
+            const T x = static_cast<const T *>(g.A.p)[t * g.A.ld + m0 + r];
+            if constexpr (sizeof(T) == 2)
+                v = bf16_to_f32(x);
+            else
+                v = x;
+        }
+        dz[r][t] = v;
+    }
+    float a[TT][8];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            a[t][i] = 0.f;
+        if (t < g.K) {
+            if (kept.q.codes)
+                load_codes(kept.q.codes + t * kept.q.ldc + n, left, left > 0 ? kept.q.scales[t * kept.q.lds + n / kGroup] : 0.f,
+                           a[t]);
+            else
+                load8(static_cast<const T *>(g.B.p) + t * g.B.ld + n, left, a[t]);
+            apply_act<float>(a[t], kept.act);
+        }
+    }
+    __syncthreads();
+    if (db && blockIdx.x == 0 && threadIdx.x < rows) {
+        float s = 0.f;
+        for (int t = 0; t < g.K; ++t)
+            s += dz[threadIdx.x][t];
+        db[m0 + threadIdx.x] = g.e.accumulate ? db[m0 + threadIdx.x] + s : s;
+    }
+    const int end = min(rows, (wave + 1) * per);
+    for (int r = wave * per; r < end; ++r) {
+        float v[8] = {};
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            const float d = dz[r][t];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                v[i] = __builtin_fmaf(d, a[t][i], v[i]);
+        }
+        const float bias[8] = {};
+        Beside<TO> beside;
+        if (has_beside<TO, kWeight>(g.e))
+            load_beside<TO, kWeight>(g.e, beside, m0 + r, n, left);
+        epilogue<TO, kWeight>(g.e, v, bias, beside, m0 + r, n, left);
+    }
+}
+
+template <typename T, typename TO>
+void launch_weight(const Gemm &g, const Kept &kept, float *db, hipStream_t st, const char *tag)
+{
+    const int64_t cols = (g.N + 511) / 512;
+    // rows of a wave: two workgroups a CU, at most 64 to an activation
+    const int per = static_cast<int>(std::max<int64_t>(2, std::min<int64_t>(kRowsMost, g.M * cols / (4 * 512))));
+    const dim3 grid(static_cast<unsigned>(cols), static_cast<unsigned>((g.M + 4 * per - 1) / (4 * per)));
+    if (g.K <= 4)
+        ACSC_LAUNCH(tag, (lin_few_weight_kernel<T, TO, 4>), grid, dim3(256), 0, st, g, kept, per, db);
+    else
+        ACSC_LAUNCH(tag, (lin_few_weight_kernel<T, TO, 8>), grid, dim3(256), 0, st, g, kept, per, db);
+}
+
 }  // namespace
 
 int lin_few_run(const Gemm &g, acsc_dtype dt, hipStream_t st, const char *tag)
@@ -146,6 +224,18 @@ int lin_few_run(const Gemm &g, acsc_dtype dt, hipStream_t st, const char *tag)
         ACSC_LAUNCH(tag, (lin_few_kernel<float, 1>), grid, dim3(kWaves * 64), 0, st, g);
     else
         ACSC_LAUNCH(tag, (lin_few_kernel<float, 2>), grid, dim3(kWaves * 64), 0, st, g);
+    return check_launch(tag);
+}
+
+int lin_few_weight_run(const Gemm &g, const Kept &kept, acsc_dtype dt, acsc_dtype out, float *db, hipStream_t st,
+                       const char *tag)
+{
+    if (dt == ACSC_BF16)
+        out == ACSC_BF16 ? launch_weight<uint16_t, uint16_t>(g, kept, db, st, tag)
+                         : launch_weight<uint16_t, float>(g, kept, db, st, tag);
+    else
+        out == ACSC_BF16 ? launch_weight<float, uint16_t>(g, kept, db, st, tag)
+                         : launch_weight<float, float>(g, kept, db, st, tag);
     return check_launch(tag);
 }
 

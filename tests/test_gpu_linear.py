@@ -60,7 +60,9 @@ def product(a, b, n):
 # (rows, n_in, n_out): one token, one input, one output, tiles filled and not, k tails of every kind, many pieces
 SHAPES = [(1, 1, 1), (1, 64, 300), (1, 4096, 512), (3, 7, 5), (17, 100, 129), (16, 256, 256), (64, 96, 1000),
           (128, 256, 128), (33, 1000, 77), (257, 264, 392), (300, 513, 260), (512, 2048, 256), (5, 5000, 31),
-          (700, 72, 1024)]
+          (700, 72, 1024),
+          # few tokens: the products that do not tile them, at their limits and past
+          (8, 700, 1030), (9, 520, 130), (12, 4100, 600), (2, 130, 5000), (15, 33, 1025)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])

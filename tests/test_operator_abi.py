@@ -94,9 +94,9 @@ def test_linear(pk):
     assert wgt(dw_dt=4) == EDTYPE and wgt(dt=4) == EDTYPE and wgt(act=7) == EINVAL
     assert wgt(x=None) == EINVAL and wgt(q=q8(pk)) == EINVAL and wgt(dW=None) == EINVAL and wgt(lddw=63) == EINVAL
     assert wgt(dW=3 * F + 2, dw_dt=0) == EALIGN and wgt(db=F + 1) == EALIGN
-    assert wgt(n=10, act=2) == ENOSPC and wgt(n=1 << 30, act=2, ws=F + 16) == EALIGN
-    assert pk.lib.lin_workspace_size_unaligned(2, 4, 64, 32, 1, C.byref(need)) == 0 and need.value > 0
-    assert wgt(dz=F + 2, n=64) == ENOSPC                 # an unaligned operand is copied first
+    assert wgt(n=10, act=2, rows=100) == ENOSPC and wgt(n=1 << 30, act=2, ws=F + 16, rows=100) == EALIGN
+    assert pk.lib.lin_workspace_size_unaligned(2, 100, 64, 32, 1, C.byref(need)) == 0 and need.value > 0
+    assert wgt(dz=F + 2, n=64, rows=100) == ENOSPC       # an unaligned operand is copied first
     assert wgt(dz=None, x=None, rows=0, acc=1) == 0
     assert pk.lib.lin_backward_act(F, 32, None, 32, None, 1, 4, 32, 2, F, 32, None) == EINVAL
     assert pk.lib.lin_backward_act(F, 32, F, 32, None, 1, 4, 32, 2, F, 40, None) == EINVAL
