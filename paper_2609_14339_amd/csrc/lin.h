@@ -44,6 +44,9 @@ struct Gemm {
     int kchunk;
     float *part;      // piece s at part + s * M * ldp; nullptr: one piece, through the epilogue
     int64_t ldp;
+    const float *dbpart;   // weight gradient: slices of column sums of dz, [slices][M], that the product's first
+    int slices;            // tiles add into db; nullptr: none
+    float *db;
     Epi e;
 };
 
@@ -183,6 +186,21 @@ __device__ __forceinline__ void put_rows(const Gemm &g, const char *lds, int64_t
         }
     }
 }
+// The first column of tiles adds the slices of db, in order.
+template <int KIND>
+__device__ __forceinline__ void put_db(const Gemm &g, int64_t m0, int rows, int tile_n, int split)
+{
+    if (KIND != kWeight || !g.dbpart || tile_n != 0 || split != 0)
+        return;
+    for (int64_t m = m0 + threadIdx.x; m < min<int64_t>(g.M, m0 + rows); m += blockDim.x) {
+        float s = 0.f;
+#pragma unroll 8
+        for (int i = 0; i < g.slices; ++i)
+            s += g.dbpart[i * g.M + m];
+        g.db[m] = g.e.accumulate ? g.db[m] + s : s;
+    }
+}
+
 template <typename T, int KIND, int NA>
 __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8], char *lds, int64_t m0, int n0,
                                          int split)

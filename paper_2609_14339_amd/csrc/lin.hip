@@ -4,8 +4,6 @@
 
 namespace acsc {
 
-int q8_decode_run(const Q8 &q, int64_t rows, int H, int act, void *y, acsc_dtype dt, int64_t ldy, hipStream_t st);
-int lin_bf16_pack(const void *x, int64_t ldx, int64_t rows, int cols, void *y, int64_t ldy, hipStream_t st);
 int lin_few_run(const Gemm &g, acsc_dtype dt, hipStream_t st, const char *tag);
 int lin_few_weight_run(const Gemm &g, const Kept &kept, acsc_dtype dt, acsc_dtype out, float *db, hipStream_t st,
                        const char *tag);
@@ -124,6 +122,7 @@ __global__ __launch_bounds__(256) void lin_f32_kernel(Gemm g)
         }
         __syncthreads();
     }
+    put_db<KIND>(g, m0, kTile, tile % g.tn, split);
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
         const f32x4(&one)[1][8] = reinterpret_cast<const f32x4(&)[1][8]>(acc[a]);
@@ -164,22 +163,65 @@ __global__ __launch_bounds__(256) void lin_join_kernel(Gemm g)
     }
 }
 
-// Column sums of dz for db: eight columns a lane, 512 a workgroup, whose
-// sixteen waves take every sixteenth row of its `per` rows and meet in LDS in
-// order.  One slice of rows writes db, several leave partials.
-constexpr int kDbWaves = 16;
+// What a product needs done first, up to three jobs in one launch (a launch
+// costs a small call 4 us): operands as the product reads them, and db.
+struct Job {
+    int db;              // 0: y <- act(x), or of a checkpoint's values, its rows filled with zeros up to a multiple
+    const void *x;       // of eight; 1: column sums of x
+    int64_t ldx, rows;
+    int cols;
+    void *y;             // job 1: db itself, or slices of it
+    int64_t ldy;         // job 1: rows of a slice
+    Q8 q;
+    int act, accumulate;
+    int blocks;          // workgroups of the job
+    int across;          // job 1: workgroups along the columns
+};
+struct Jobs {
+    int n;
+    Job j[3];
+};
+
+// An operand: a wave takes 512 columns of a row, eight a lane.  Sums: 512
+// columns and one slice of rows a workgroup, whose four waves take every
+// fourth row and meet in LDS in order.
 template <typename T>
-__global__ __launch_bounds__(64 * kDbWaves) void lin_db_kernel(const T *dz, int64_t ld, int64_t rows, int N, int per,
-                                                               float *part, float *db, int accumulate)
+__global__ __launch_bounds__(256) void lin_prepare_kernel(Jobs jobs)
 {
-    __shared__ float meet[kDbWaves][512];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n = blockIdx.x * 512 + lane * 8;
-    const int64_t end = min<int64_t>(rows, (blockIdx.y + static_cast<int64_t>(1)) * per);
+    __shared__ float meet[4][512];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    int block = blockIdx.x, which = 0;
+    while (which + 1 < jobs.n && block >= jobs.j[which].blocks) {
+        block -= jobs.j[which].blocks;
+        ++which;
+    }
+    const Job &j = jobs.j[which];
+    const T *x = static_cast<const T *>(j.x);
+    if (!j.db) {
+        const int segs = (j.cols + 511) / 512;
+        T *y = static_cast<T *>(j.y);
+        for (int64_t w = static_cast<int64_t>(block) * 4 + wave; w < j.rows * segs; w += static_cast<int64_t>(j.blocks) * 4) {
+            const int64_t row = w / segs;
+            const int col = static_cast<int>(w - row * segs) * 512 + lane * 8;
+            if (col >= j.cols)
+                continue;
+            float v[8];
+            if (j.q.codes)
+                load_codes(j.q.codes + row * j.q.ldc + col, j.cols - col, j.q.scales[row * j.q.lds + col / kGroup], v);
+            else
+                load8(x + row * j.ldx + col, j.cols - col, v);
+            apply_act<T>(v, j.act);
+            store8(y + row * j.ldy + col, 8, v);
+        }
+        return;
+    }
+    const int cb = block % j.across, sl = block / j.across, n = cb * 512 + lane * 8;
+    const int64_t end = min<int64_t>(j.rows, (sl + static_cast<int64_t>(1)) * j.ldy);
     float s[8] = {};
-#pragma unroll 4
-    for (int64_t r = blockIdx.y * static_cast<int64_t>(per) + wave; r < end; r += kDbWaves) {
+#pragma unroll 8
+    for (int64_t r = sl * j.ldy + wave; r < end; r += 4) {
         Raw8<T> v;
-        load_raw(dz + r * ld + n, N - n, v);
+        load_raw(x + r * j.ldx + n, j.cols - n, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             s[i] += v.at(i);
@@ -188,28 +230,15 @@ __global__ __launch_bounds__(64 * kDbWaves) void lin_db_kernel(const T *dz, int6
     for (int i = 0; i < 8; ++i)
         meet[wave][i * 64 + lane] = s[i];
     __syncthreads();
-    const int c = threadIdx.x, at = (c & 7) * 64 + (c >> 3), col = blockIdx.x * 512 + c;
-    if (c < 512 && col < N) {
-        float v = meet[0][at];
-#pragma unroll
-        for (int w = 1; w < kDbWaves; ++w)
-            v += meet[w][at];
-        if (part)
-            part[static_cast<int64_t>(blockIdx.y) * N + col] = v;
-        else
-            db[col] = accumulate ? db[col] + v : v;
+    const bool one = j.blocks == j.across;
+    float *out = static_cast<float *>(j.y) + static_cast<int64_t>(sl) * j.cols;
+    for (int c = threadIdx.x; c < 512; c += 256) {
+        const int at = (c & 7) * 64 + (c >> 3), col = cb * 512 + c;
+        if (col < j.cols) {
+            const float v = ((meet[0][at] + meet[1][at]) + meet[2][at]) + meet[3][at];
+            out[col] = one && j.accumulate ? out[col] + v : v;
+        }
     }
-}
-
-__global__ __launch_bounds__(256) void lin_join_db_kernel(const float *part, int N, int slices, float *db, int accumulate)
-{
-    const int n = blockIdx.x * 256 + threadIdx.x;
-    if (n >= N)
-        return;
-    float s = 0.f;
-    for (int i = 0; i < slices; ++i)
-        s += part[static_cast<int64_t>(i) * N + n];
-    db[n] = accumulate ? db[n] + s : s;
 }
 
 // rows == 0: the weight gradients are sums over nothing.
@@ -222,16 +251,18 @@ __global__ __launch_bounds__(256) void lin_zero_kernel(TO *y, int64_t ldy, int64
             y[m * ldy + n] = 0;
 }
 
-// dz = dy act'(z), eight columns a lane.
+// dz = dy act'(z): a wave takes 512 columns of a row, eight a lane.
 template <typename T>
 __global__ __launch_bounds__(256) void lin_act_kernel(const T *dy, int64_t lddy, const T *z, int64_t ldz, Q8 q, int64_t rows,
                                                       int N, int act, T *dz, int64_t lddz)
 {
-    const int chunks = (N + 7) / 8;
-    const int64_t total = rows * chunks;
-    for (int64_t w = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; w < total; w += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t row = w / chunks;
-        const int col = static_cast<int>(w - row * chunks) * 8;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int segs = (N + 511) / 512;
+    for (int64_t w = static_cast<int64_t>(blockIdx.x) * 4 + wave; w < rows * segs; w += static_cast<int64_t>(gridDim.x) * 4) {
+        const int64_t row = w / segs;
+        const int col = static_cast<int>(w - row * segs) * 512 + lane * 8;
+        if (col >= N)
+            continue;
         float g[8], v[8];
         load8(dy + row * lddy + col, N - col, g);
         if (q.codes)
@@ -240,22 +271,6 @@ __global__ __launch_bounds__(256) void lin_act_kernel(const T *dy, int64_t lddy,
             load8(z + row * ldz + col, N - col, v);
         apply_slope<T>(g, v, act);
         store8(dz + row * lddz + col, N - col, g);
-    }
-}
-
-// act(x) of a whole operand, eight columns a lane.
-template <typename T>
-__global__ __launch_bounds__(256) void lin_apply_kernel(const T *x, int64_t ldx, int64_t rows, int N, int act, T *y, int64_t ldy)
-{
-    const int chunks = (N + 7) / 8;
-    const int64_t total = rows * chunks;
-    for (int64_t w = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; w < total; w += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t row = w / chunks;
-        const int col = static_cast<int>(w - row * chunks) * 8;
-        float v[8];
-        load8(x + row * ldx + col, N - col, v);
-        apply_act<T>(v, act);
-        store8(y + row * ldy + col, N - col, v);
     }
 }
 
@@ -370,10 +385,9 @@ inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bo
     p.ldp = up8(s.N);
     p.part = p.splits > 1 ? up256(static_cast<size_t>(p.splits) * s.M * p.ldp * 4) : 0;
     if (kind == kWeight) {
-        // db's slices of at least 64 rows, four a wave, up to about one
-        // workgroup a CU; up to 128 rows in one, without a launch to join them
+        // db's slices of at least 32 rows, up to about two workgroups a CU
         const int64_t blocks = (s.M + 511) / 512;
-        p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(256 / blocks, s.K <= 128 ? 1 : s.K / 64)));
+        p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(512 / blocks, s.K / 32)));
         p.slice = (s.K + p.slices - 1) / p.slices;
         p.slices = (s.K + p.slice - 1) / p.slice;
         p.db = p.slices > 1 ? up256(static_cast<size_t>(p.slices) * s.M * 4) : 0;
@@ -402,9 +416,31 @@ void launch_join(const Gemm &g, hipStream_t st)
                 dim3(256), 0, st, g);
 }
 
-// The product, its pieces' sum and db; `out` is the type of the output.
+// An input of the weight gradient that is formed again from what was kept.
+struct Again {
+    Operand from;
+    void *to;
+    Kept kept;
+};
+
+inline void add_operand(Jobs &jobs, const Operand &from, int64_t rows, int cols, void *to, int64_t ld, const Kept &kept)
+{
+    Job &j = jobs.j[jobs.n++];
+    j.x = from.p;
+    j.ldx = from.ld;
+    j.rows = rows;
+    j.cols = cols;
+    j.y = to;
+    j.ldy = ld;
+    j.q = kept.q;
+    j.act = kept.act;
+    j.blocks = static_cast<int>(std::min<int64_t>((rows * ((cols + 511) / 512) + 3) / 4, 1 << 18));
+}
+
+// What comes first, the product and its pieces' sum; `out` is the type of the
+// output.
 int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype dt, acsc_dtype out, char *ws, float *db,
-                hipStream_t st, const char *tag)
+                const Again *again, hipStream_t st, const char *tag)
 {
     g.M = s.M;
     g.N = s.N;
@@ -417,38 +453,53 @@ int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype
     // a piece goes through memory if there are more, or if its workgroups hold
     // no whole checkpoint groups
     g.part = p.splits > 1 || (p.few && g.e.q.codes) ? reinterpret_cast<float *>(ws) : nullptr;
+    Jobs jobs{};
+    if (again)
+        add_operand(jobs, again->from, s.K, s.N, again->to, up8(s.N), again->kept);
     if (db) {
-        float *part = p.slices > 1 ? reinterpret_cast<float *>(ws + p.part) : nullptr;
-        const dim3 grid(static_cast<unsigned>((g.M + 511) / 512), p.slices);
-        const int n = static_cast<int>(g.M);
+        Job &j = jobs.j[jobs.n++];
+        j.db = 1;
+        j.x = g.A.p;
+        j.ldx = g.A.ld;
+        j.rows = s.K;
+        j.cols = static_cast<int>(s.M);
+        j.accumulate = g.e.accumulate;
+        j.across = static_cast<int>((s.M + 511) / 512);
+        j.blocks = j.across * p.slices;
+        j.ldy = p.slice;
+        j.y = p.slices > 1 ? static_cast<void *>(ws + p.part) : db;
+        if (p.slices > 1) {
+            g.dbpart = reinterpret_cast<float *>(ws + p.part);
+            g.slices = p.slices;
+            g.db = db;
+        }
+    }
+    char *copy = ws + p.part + p.db;
+    const Kept plain{q8_of(nullptr), ACSC_ACT_NONE};
+    if (p.pack_a) {
+        add_operand(jobs, g.A, s.acol ? s.K : s.M, s.acol ? static_cast<int>(s.M) : s.K, copy, p.lda, plain);
+        g.A = {copy, p.lda};
+        copy += p.a;
+    }
+    if (p.pack_b) {
+        add_operand(jobs, g.B, s.bcol ? s.K : s.N, s.bcol ? s.N : s.K, copy, p.ldb, plain);
+        g.B = {copy, p.ldb};
+    }
+    if (jobs.n) {
+        int blocks = 0;
+        for (int i = 0; i < jobs.n; ++i)
+            blocks += jobs.j[i].blocks;
         if (dt == ACSC_BF16)
-            ACSC_LAUNCH("lin_db", lin_db_kernel<uint16_t>, grid, dim3(64 * kDbWaves), 0, st, static_cast<const uint16_t *>(g.A.p), g.A.ld,
-                        static_cast<int64_t>(s.K), n, p.slice, part, db, g.e.accumulate);
+            ACSC_LAUNCH("lin_prepare", lin_prepare_kernel<uint16_t>, dim3(blocks), dim3(256), 0, st, jobs);
         else
-            ACSC_LAUNCH("lin_db", lin_db_kernel<float>, grid, dim3(64 * kDbWaves), 0, st, static_cast<const float *>(g.A.p), g.A.ld,
-                        static_cast<int64_t>(s.K), n, p.slice, part, db, g.e.accumulate);
-        if (part)
-            ACSC_LAUNCH("lin_join_db", lin_join_db_kernel, dim3((n + 255) / 256), dim3(256), 0, st, part, n, p.slices, db,
-                        g.e.accumulate);
-        if (int rc = check_launch("lin_db"))
+            ACSC_LAUNCH("lin_prepare", lin_prepare_kernel<float>, dim3(blocks), dim3(256), 0, st, jobs);
+        if (int rc = check_launch("lin_prepare"))
             return rc;
     }
     if (p.few) {
         if (int rc = lin_few_run(g, dt, st, tag))
             return rc;
     } else if (dt == ACSC_BF16) {
-        char *copy = ws + p.part + p.db;
-        if (p.pack_a) {
-            if (int rc = lin_bf16_pack(g.A.p, g.A.ld, s.acol ? s.K : s.M, s.acol ? static_cast<int>(s.M) : s.K, copy, p.lda, st))
-                return rc;
-            g.A = {copy, p.lda};
-            copy += p.a;
-        }
-        if (p.pack_b) {
-            if (int rc = lin_bf16_pack(g.B.p, g.B.ld, s.bcol ? s.K : s.N, s.bcol ? s.N : s.K, copy, p.ldb, st))
-                return rc;
-            g.B = {copy, p.ldb};
-        }
         if (int rc = lin_bf16_run(g, p.tile, kind, out, st, tag))
             return rc;
     } else {
@@ -604,7 +655,7 @@ extern "C" int lin_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t r
     if (int rc = check_ws(ws, ws_bytes, p.bytes()))
         return rc;
     g.e = Epi{y, ld_y, bias, residual, ld_res, z, ld_z, q8_of(q), act, 0};
-    return run_product(g, kForward, p, s, dt, dt, static_cast<char *>(ws), nullptr, stream, "lin_forward");
+    return run_product(g, kForward, p, s, dt, dt, static_cast<char *>(ws), nullptr, nullptr, stream, "lin_forward");
 }
 
 extern "C" int lin_backward_act(const void *dy, int64_t ld_dy, const void *z, int64_t ld_z, const q8_tensor *q,
@@ -625,7 +676,7 @@ extern "C" int lin_backward_act(const void *dy, int64_t ld_dy, const void *z, in
     ACSC_CHECK_ARG(dz != dy || rows == 0 || ld_dz == ld_dy, ACSC_EINVAL, "dz in place of dy needs ld_dz == ld_dy");
     if (rows == 0)
         return ACSC_OK;
-    const int64_t blocks = std::min<int64_t>((rows * ((n_out + 7) / 8) + 255) / 256, 1 << 20);
+    const int64_t blocks = std::min<int64_t>((rows * ((n_out + 511) / 512) + 3) / 4, 1 << 20);
     if (dt == ACSC_BF16)
         ACSC_LAUNCH("lin_backward_act", lin_act_kernel<uint16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
                     static_cast<const uint16_t *>(dy), ld_dy, static_cast<const uint16_t *>(z), ld_z, q8_of(q), rows, n_out,
@@ -670,7 +721,7 @@ extern "C" int lin_backward_input(const void *dz, int64_t ld_dz, acsc_dtype dt, 
     if (int rc = check_ws(ws, ws_bytes, p.bytes()))
         return rc;
     g.e = Epi{dx, ld_dx, nullptr, nullptr, 0, const_cast<void *>(z), ld_z, q8_of(q), act, 0};
-    return run_product(g, kGate, p, s, dt, dt, static_cast<char *>(ws), nullptr, stream, "lin_backward_input");
+    return run_product(g, kGate, p, s, dt, dt, static_cast<char *>(ws), nullptr, nullptr, stream, "lin_backward_input");
 }
 
 extern "C" int lin_backward_weight(const void *dz, int64_t ld_dz, const void *x, int64_t ld_x, const q8_tensor *q,
@@ -731,22 +782,7 @@ extern "C" int lin_backward_weight(const void *dz, int64_t ld_dz, const void *x,
         return rc;
     if (int rc = check_ws(ws, ws_bytes, p.bytes() + whole))
         return rc;
-    if (again) {
-        int rc = ACSC_OK;
-        if (q) {
-            rc = q8_decode_run(q8_of(q), rows, n_in, act, ws, dt, g.B.ld, stream);
-        } else {
-            const int64_t blocks = std::min<int64_t>((rows * ((n_in + 7) / 8) + 255) / 256, 1 << 20);
-            if (dt == ACSC_BF16)
-                ACSC_LAUNCH("lin_apply", lin_apply_kernel<uint16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
-                            static_cast<const uint16_t *>(x), ld_x, rows, n_in, act, static_cast<uint16_t *>(ws), g.B.ld);
-            else
-                ACSC_LAUNCH("lin_apply", lin_apply_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
-                            static_cast<const float *>(x), ld_x, rows, n_in, act, static_cast<float *>(ws), g.B.ld);
-            rc = check_launch("lin_apply");
-        }
-        if (rc)
-            return rc;
-    }
-    return run_product(g, kWeight, p, s, dt, dw_dt, static_cast<char *>(ws) + whole, db, stream, "lin_backward_weight");
+    const Again a{{x, ld_x}, ws, Kept{q8_of(q), act}};
+    return run_product(g, kWeight, p, s, dt, dw_dt, static_cast<char *>(ws) + whole, db, again ? &a : nullptr, stream,
+                       "lin_backward_weight");
 }

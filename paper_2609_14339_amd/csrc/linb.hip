@@ -279,36 +279,13 @@ __global__ __launch_bounds__(2 * T, 2) void lin_bf16_kernel(Gemm g)
     for (; s < nsteps; ++s)
         step(s, std::false_type{});
     meet();
+    put_db<KIND>(g, m0, T, tile_n, split);
     constexpr int NA = 2;
     char *own = reinterpret_cast<char *>(smem) + wave * NA * 8192;
 #pragma unroll
     for (int a = 0; a < FA; a += NA)
         put_tile<TO, KIND, NA>(g, reinterpret_cast<const f32x4(&)[NA][8]>(acc[a]), own, m0 + (wm * FA + a) * 16,
                                n0 + wn * 128, split);
-}
-
-// A copy of an operand whose rows are 16-byte aligned and filled with zeros
-// up to a multiple of eight.
-__global__ __launch_bounds__(256) void lin_pack_kernel(const uint16_t *x, int64_t ldx, int64_t rows, int cols, uint16_t *y,
-                                                       int64_t ldy)
-{
-    const int chunks = static_cast<int>(ldy / 8);
-    const int64_t total = rows * chunks;
-    for (int64_t w = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; w < total; w += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t row = w / chunks;
-        const int col = static_cast<int>(w - row * chunks) * 8;
-        const uint16_t *p = x + row * ldx + col;
-        Bf8Any c = {{0, 0, 0, 0}};
-        if (cols - col >= 8) {
-            c = *reinterpret_cast<const Bf8Any *>(p);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (col + i < cols)
-                    c.w[i / 2] |= static_cast<uint32_t>(p[i]) << (16 * (i & 1));
-        }
-        *reinterpret_cast<Bf8Any *>(y + row * ldy + col) = c;
-    }
 }
 
 template <int T, bool ACOL, bool BCOL, int KIND, typename TO>
@@ -333,14 +310,6 @@ int launch_kind(const Gemm &g, EpiKind kind, acsc_dtype out, hipStream_t st, con
 }
 
 }  // namespace
-
-int lin_bf16_pack(const void *x, int64_t ldx, int64_t rows, int cols, void *y, int64_t ldy, hipStream_t st)
-{
-    const int64_t blocks = std::min<int64_t>((rows * (ldy / 8) + 255) / 256, 1 << 20);
-    ACSC_LAUNCH("lin_pack", lin_pack_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st,
-                static_cast<const uint16_t *>(x), ldx, rows, cols, static_cast<uint16_t *>(y), ldy);
-    return check_launch("lin_pack");
-}
 
 int lin_bf16_run(const Gemm &g, int tile, EpiKind kind, acsc_dtype out, hipStream_t st, const char *tag)
 {

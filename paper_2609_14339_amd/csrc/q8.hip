@@ -73,21 +73,6 @@ inline dim3 grid_of(int64_t rows, int H)
 }
 
 }  // namespace
-
-// act(values of q) as dt, for calls that need a kept operand whole.
-int q8_decode_run(const Q8 &q, int64_t rows, int H, int act, void *y, acsc_dtype dt, int64_t ldy, hipStream_t st)
-{
-    if (rows == 0)
-        return ACSC_OK;
-    if (dt == ACSC_BF16)
-        ACSC_LAUNCH("q8_decode", q8_decode_kernel<uint16_t>, grid_of(rows, H), dim3(kQThreads), 0, st, q, rows, H, act,
-                    static_cast<uint16_t *>(y), ldy);
-    else
-        ACSC_LAUNCH("q8_decode", q8_decode_kernel<float>, grid_of(rows, H), dim3(kQThreads), 0, st, q, rows, H, act,
-                    static_cast<float *>(y), ldy);
-    return check_launch("q8_decode");
-}
-
 }  // namespace acsc
 
 using namespace acsc;
@@ -127,5 +112,13 @@ extern "C" int q8_decode(const q8_tensor *q, int64_t rows, int H, acsc_act act, 
         return rc;
     if (int rc = check_tensor(y, rows, ld_y, H, dt, "y"))
         return rc;
-    return q8_decode_run(q8_of(q), rows, H, act, y, dt, ld_y, stream);
+    if (rows == 0)
+        return ACSC_OK;
+    if (dt == ACSC_BF16)
+        ACSC_LAUNCH("q8_decode", q8_decode_kernel<uint16_t>, grid_of(rows, H), dim3(kQThreads), 0, stream, q8_of(q), rows, H,
+                    act, static_cast<uint16_t *>(y), ld_y);
+    else
+        ACSC_LAUNCH("q8_decode", q8_decode_kernel<float>, grid_of(rows, H), dim3(kQThreads), 0, stream, q8_of(q), rows, H, act,
+                    static_cast<float *>(y), ld_y);
+    return check_launch("q8_decode");
 }
