@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libacsc.so")
 OBJDIR = os.path.join(HERE, "_build")
 SOURCES = ["common.hip", "ac.hip", "sc.hip", "pass.hip", "blend.hip", "chol.hip", "orth.hip", "f32.hip",
-           "static_scratch.hip", "q8.hip", "ln.hip", "lin.hip", "linb.hip", "lin_few.hip"]
+           "static_scratch.hip", "q8.hip", "ln.hip", "lin.hip", "lin_tile.hip", "lin_few.hip"]
 ARCH = "gfx950"
 
 

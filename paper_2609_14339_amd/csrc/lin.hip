@@ -1,5 +1,5 @@
-// Linear layers: the entry points, the fp32 product, and the kernels that add
-// the pieces of a product cut along its sum.
+// Linear layers: the entry points, how a product is cut, and the kernels
+// before and after it.
 #include "lin.h"
 
 namespace acsc {
@@ -7,11 +7,9 @@ namespace acsc {
 int lin_few_run(const Gemm &g, acsc_dtype dt, hipStream_t st, const char *tag);
 int lin_few_weight_run(const Gemm &g, const Kept &kept, acsc_dtype dt, acsc_dtype out, float *db, hipStream_t st,
                        const char *tag);
-int lin_bf16_run(const Gemm &g, int tile, EpiKind kind, acsc_dtype out, hipStream_t st, const char *tag);
+int lin_tile_run(const Gemm &g, int tile, EpiKind kind, acsc_dtype dt, acsc_dtype out, hipStream_t st, const char *tag);
 
 namespace {
-
-constexpr int kTile = 128, kBK = 32;
 
 // Tokens up to which a product does without tiles.  Forward: W is read once
 // and unstaged; 4096 -> 14336, 1 / 8 / 16 / 32 tokens, us: bf16 24.1, 28.3, 34.9,
@@ -22,112 +20,6 @@ constexpr int kTile = 128, kBK = 32;
 inline int few_tokens(EpiKind kind, bool bf16)
 {
     return kind == kForward ? (bf16 ? 8 : 32) : kind == kWeight ? 8 : 0;
-}
-
-// The fp32 product on v_mfma_f32_16x16x4_f32: 128 x 128 tiles, four waves of
-// 32 rows by 128 columns, so that a wave holds whole checkpoint groups.  The
-// matrix instruction's first operand is B's side, which puts four consecutive
-// columns of one row in a lane.  Tiles go through registers into LDS as they
-// are stored (rows padded to 36, or k-lines to 132 floats: fragment reads are
-// free of bank conflicts in both), the next step's loads in flight while one
-// is multiplied; any alignment, edges read as zeros.
-template <bool COL>
-struct Stage {
-    static constexpr int kPitch = COL ? kTile + 4 : kBK + 4;
-    static constexpr int kFloats = COL ? kBK * kPitch : kTile * kPitch;
-    float r[4][4];
-    __device__ __forceinline__ void load(const Operand &o, int64_t i0, int64_t ni, int k0, int kend)
-    {
-        const float *p = static_cast<const float *>(o.p);
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            if (COL) {
-                const int k = k0 + (threadIdx.x >> 5) + 8 * s;
-                const int64_t i = i0 + (threadIdx.x & 31) * 4;
-                load4(p + static_cast<int64_t>(k) * o.ld + i, k < kend ? static_cast<int>(min<int64_t>(ni - i, 4)) : 0, r[s]);
-            } else {
-                const int k = k0 + (threadIdx.x & 7) * 4;
-                const int64_t i = i0 + (threadIdx.x >> 3) + 32 * s;
-                load4(p + i * o.ld + k, i < ni ? kend - k : 0, r[s]);
-            }
-        }
-    }
-    __device__ __forceinline__ void put(float *lds) const
-    {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int a = COL ? ((threadIdx.x >> 5) + 8 * s) * kPitch + (threadIdx.x & 31) * 4
-                              : ((threadIdx.x >> 3) + 32 * s) * kPitch + (threadIdx.x & 7) * 4;
-            *reinterpret_cast<f32x4 *>(lds + a) = f32x4{r[s][0], r[s][1], r[s][2], r[s][3]};
-        }
-    }
-    // element e: k = kk * 16 + 4 (lane / 16) + e of line i (+ lane % 16)
-    static __device__ __forceinline__ f32x4 frag(const float *lds, int i, int kk)
-    {
-        const int lane = threadIdx.x & 63, line = i + (lane & 15), k = kk * 16 + (lane >> 4) * 4;
-        if (COL)
-            return f32x4{lds[k * kPitch + line], lds[(k + 1) * kPitch + line], lds[(k + 2) * kPitch + line],
-                         lds[(k + 3) * kPitch + line]};
-        return *reinterpret_cast<const f32x4 *>(lds + line * kPitch + k);
-    }
-};
-
-template <bool ACOL, bool BCOL, int KIND, typename TO>
-__global__ __launch_bounds__(256) void lin_f32_kernel(Gemm g)
-{
-    // the tiles; after the last step 8 KiB a wave for the epilogue
-    constexpr int kFloats = Stage<ACOL>::kFloats + Stage<BCOL>::kFloats;
-    __shared__ __align__(16) float lds[kFloats > 8192 ? kFloats : 8192];
-    float *As = lds, *Bs = lds + Stage<ACOL>::kFloats;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int tile = blockIdx.x, split = blockIdx.y;
-    const int64_t m0 = static_cast<int64_t>(tile / g.tn) * kTile;
-    const int n0 = tile % g.tn * kTile;
-    const int kbeg = split * g.kchunk, kend = min(g.K, kbeg + g.kchunk);
-    f32x4 acc[2][8];
-#pragma unroll
-    for (int a = 0; a < 2; ++a) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            acc[a][j] = f32x4{0, 0, 0, 0};
-    }
-    Stage<ACOL> sa;
-    Stage<BCOL> sb;
-    sa.load(g.A, m0, g.M, kbeg, kend);
-    sb.load(g.B, n0, g.N, kbeg, kend);
-    for (int k0 = kbeg; k0 < kend; k0 += kBK) {
-        sa.put(As);
-        sb.put(Bs);
-        __syncthreads();
-        if (k0 + kBK < kend) {
-            sa.load(g.A, m0, g.M, k0 + kBK, kend);
-            sb.load(g.B, n0, g.N, k0 + kBK, kend);
-        }
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            f32x4 fa[2], fb[8];
-#pragma unroll
-            for (int a = 0; a < 2; ++a)
-                fa[a] = Stage<ACOL>::frag(As, wave * 32 + a * 16, kk);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                fb[j] = Stage<BCOL>::frag(Bs, j * 16, kk);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int a = 0; a < 2; ++a)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        acc[a][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j][e], fa[a][e], acc[a][j], 0, 0, 0);
-        }
-        __syncthreads();
-    }
-    put_db<KIND>(g, m0, kTile, tile % g.tn, split);
-#pragma unroll
-    for (int a = 0; a < 2; ++a) {
-        const f32x4(&one)[1][8] = reinterpret_cast<const f32x4(&)[1][8]>(acc[a]);
-        put_tile<TO, KIND, 1>(g, one, reinterpret_cast<char *>(lds) + wave * 8192, m0 + wave * 32 + a * 16, n0, split);
-    }
 }
 
 // Adds the pieces of a cut product in order and takes the sum through the
@@ -277,7 +169,7 @@ __global__ __launch_bounds__(256) void lin_act_kernel(const T *dy, int64_t lddy,
 inline size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 
 // How a product is cut, and what of the workspace it takes: the pieces, db's
-// pieces, and copies of the operands that the bf16 kernel cannot read where
+// pieces, and copies of the operands that the tile kernel cannot read where
 // they are.
 struct Plan {
     bool few;                               // the product for few tokens
@@ -307,11 +199,12 @@ inline Shape shape_of(EpiKind kind, int64_t rows, int n_in, int n_out)
     return {n_out, n_in, static_cast<int>(rows), true, true};
 }
 
-// Whether the bf16 kernel reads an operand where it is: 16-byte lines, whole
-// chunks of eight, offsets within a tile of under 2^32 bytes.
-inline bool readable(const Operand &o, bool col, int64_t inner)
+// Whether the tile kernel reads an operand where it is: rows of whole 16-byte
+// chunks, offsets within a tile and step of under 2^31 bytes.
+inline bool readable(const Operand &o, bool col, int64_t inner, acsc_dtype dt)
 {
-    return aligned(o.p, 16) && o.ld % 8 == 0 && inner % 8 == 0 && o.ld * 2 * (col ? 64 : 256) < (1ll << 31);
+    const int es = static_cast<int>(dtype_size(dt)), chunk = 16 / es;
+    return aligned(o.p, 16) && o.ld % chunk == 0 && inner % chunk == 0 && o.ld * es * (col ? 64 : 256) < (1ll << 31);
 }
 
 // Tile and pieces of the sum, by the least estimated time.  A round is what
@@ -356,7 +249,7 @@ inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bo
 {
     Plan p{};
     const bool bf16 = dt == ACSC_BF16;
-    const int bk = bf16 ? 64 : kBK;
+    const int bk = 128 / static_cast<int>(dtype_size(dt));
     const int steps = (s.K + bk - 1) / bk;
     if (kind == kWeight && s.K <= few_tokens(kind, bf16)) {
         p.few = true;
@@ -392,21 +285,14 @@ inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bo
         p.slices = (s.K + p.slice - 1) / p.slice;
         p.db = p.slices > 1 ? up256(static_cast<size_t>(p.slices) * s.M * 4) : 0;
     }
-    if (bf16) {
-        p.pack_a = !fits_a;
-        p.pack_b = !fits_b;
-        p.lda = up8(s.acol ? static_cast<int>(s.M) : s.K);
-        p.ldb = up8(s.bcol ? s.N : s.K);
-        p.a = p.pack_a ? up256(static_cast<size_t>(s.acol ? s.K : s.M) * p.lda * 2) : 0;
-        p.b = p.pack_b ? up256(static_cast<size_t>(s.bcol ? s.K : s.N) * p.ldb * 2) : 0;
-    }
+    const int64_t es = static_cast<int64_t>(dtype_size(dt));
+    p.pack_a = !fits_a;
+    p.pack_b = !fits_b;
+    p.lda = up8(s.acol ? static_cast<int>(s.M) : s.K);
+    p.ldb = up8(s.bcol ? s.N : s.K);
+    p.a = p.pack_a ? up256(static_cast<size_t>(s.acol ? s.K : s.M) * p.lda * es) : 0;
+    p.b = p.pack_b ? up256(static_cast<size_t>(s.bcol ? s.K : s.N) * p.ldb * es) : 0;
     return p;
-}
-
-template <bool ACOL, bool BCOL, int KIND, typename TO>
-void launch_f32(const Gemm &g, hipStream_t st, const char *tag)
-{
-    ACSC_LAUNCH(tag, (lin_f32_kernel<ACOL, BCOL, KIND, TO>), dim3(g.tm * g.tn, g.splits), dim3(256), 0, st, g);
 }
 
 template <int KIND, typename TO>
@@ -499,20 +385,8 @@ int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype
     if (p.few) {
         if (int rc = lin_few_run(g, dt, st, tag))
             return rc;
-    } else if (dt == ACSC_BF16) {
-        if (int rc = lin_bf16_run(g, p.tile, kind, out, st, tag))
-            return rc;
-    } else {
-        if (kind == kForward)
-            launch_f32<false, false, kForward, float>(g, st, tag);
-        else if (kind == kGate)
-            launch_f32<false, true, kGate, float>(g, st, tag);
-        else if (out == ACSC_BF16)
-            launch_f32<true, true, kWeight, uint16_t>(g, st, tag);
-        else
-            launch_f32<true, true, kWeight, float>(g, st, tag);
-        if (int rc = check_launch(tag))
-            return rc;
+    } else if (int rc = lin_tile_run(g, p.tile, kind, dt, out, st, tag)) {
+        return rc;
     }
     if (g.part) {
         const bool b = out == ACSC_BF16;
@@ -597,8 +471,8 @@ static int workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dty
     const EpiKind kind = op == LIN_FORWARD ? kForward : op == LIN_BACKWARD_INPUT ? kGate : kWeight;
     const Shape s = shape_of(kind, rows, n_in, n_out);
     const Operand best{nullptr, 8};
-    const bool a = !any && readable(best, s.acol, s.acol ? s.M : s.K);
-    const bool b = !any && readable(best, s.bcol, s.bcol ? s.N : s.K);
+    const bool a = !any && readable(best, s.acol, s.acol ? s.M : s.K, dt);
+    const bool b = !any && readable(best, s.bcol, s.bcol ? s.N : s.K, dt);
     *bytes = plan_of(kind, s, dt, a, b).bytes() +
              (kind == kWeight && rows > few_tokens(kind, dt == ACSC_BF16) ? recomputed_bytes(rows, n_in, dt) : 0);
     return ACSC_OK;
@@ -649,7 +523,7 @@ extern "C" int lin_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t r
     g.A = {x, ld_x};
     g.B = {W, ld_w};
     const Shape s = shape_of(kForward, rows, n_in, n_out);
-    const Plan p = plan_of(kForward, s, dt, readable(g.A, false, n_in), readable(g.B, false, n_in));
+    const Plan p = plan_of(kForward, s, dt, readable(g.A, false, n_in, dt), readable(g.B, false, n_in, dt));
     if (int rc = check_tiles(p))
         return rc;
     if (int rc = check_ws(ws, ws_bytes, p.bytes()))
@@ -715,7 +589,7 @@ extern "C" int lin_backward_input(const void *dz, int64_t ld_dz, acsc_dtype dt, 
     g.A = {dz, ld_dz};
     g.B = {W, ld_w};
     const Shape s = shape_of(kGate, rows, n_in, n_out);
-    const Plan p = plan_of(kGate, s, dt, readable(g.A, false, n_out), readable(g.B, true, n_in));
+    const Plan p = plan_of(kGate, s, dt, readable(g.A, false, n_out, dt), readable(g.B, true, n_in, dt));
     if (int rc = check_tiles(p))
         return rc;
     if (int rc = check_ws(ws, ws_bytes, p.bytes()))
@@ -777,7 +651,7 @@ extern "C" int lin_backward_weight(const void *dz, int64_t ld_dz, const void *x,
     const size_t whole = again ? recomputed_bytes(rows, n_in, dt) : 0;
     g.A = {dz, ld_dz};
     g.B = again ? Operand{ws, up8(n_in)} : Operand{x, ld_x};
-    const Plan p = plan_of(kWeight, s, dt, readable(g.A, true, n_out), again || readable(g.B, true, n_in));
+    const Plan p = plan_of(kWeight, s, dt, readable(g.A, true, n_out, dt), again || readable(g.B, true, n_in, dt));
     if (int rc = check_tiles(p))
         return rc;
     if (int rc = check_ws(ws, ws_bytes, p.bytes() + whole))

@@ -1,15 +1,17 @@
-// The bf16 product of the linear layers on v_mfma_f32_16x16x32_bf16.
+// The tiled products of the linear layers, on v_mfma_f32_16x16x32_bf16 and
+// v_mfma_f32_16x16x4_f32.
 //
-// A workgroup takes a T x T tile of C (T = 256: eight waves of 64 rows by 128
-// columns; T = 128: four of 32 by 128) in steps of 64 along the sum.  Each
-// step's tiles of A and B come straight from memory into LDS
-// (global_load_lds_dwordx4), into two stages in turn; no register holds them
-// on the way.  An operand stays in LDS as it is stored: lines of 64 k (row) or
-// k-lines of 64 own indices (col), 128 bytes a line, its eight 16-byte chunks
-// XOR-swizzled by the line.  Fragments are 16-byte reads of row operands and
-// pairs of transposing 8-byte reads of col ones, so all three products of a
-// layer run at the stored layouts.  The matrix instruction's first operand is
-// B's side: a lane then holds four consecutive columns of a row.
+// A workgroup takes a T x T tile of C (T = 256, bf16 only: eight waves of 64
+// rows by 128 columns; T = 128: four of 32 by 128) in steps of 128 bytes along
+// the sum (64 bf16, 32 fp32).  Each step's tiles of A and B come straight from
+// memory into LDS (global_load_lds_dwordx4), into two stages in turn; no
+// register holds them on the way.  An operand stays in LDS as it is stored:
+// lines of one index's step (row) or k-lines of 128 bytes of its own indices
+// (col), their eight 16-byte chunks XOR-swizzled by the line.  Fragments are
+// 16-byte reads of row operands; of col ones pairs of transposing 8-byte reads
+// (bf16) or four 4-byte reads (fp32); so all three products of a layer run at
+// the stored layouts.  The matrix instruction's first operand is B's side: a
+// lane then holds four consecutive columns of a row.
 //
 // Half a step of fragments is read ahead: while the first half of a step is
 // multiplied the second is read; then the wave waits for its part of the next
@@ -27,7 +29,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
 
-constexpr int kBK = 64;
 
 // What lanes past the end of the sum read in its last step.
 __device__ const uint4 g_zeros = {0, 0, 0, 0};
@@ -71,14 +72,14 @@ __device__ __forceinline__ void dma16(const void *a, uint32_t alds, const void *
                  : "memory");
 }
 
-// One operand's side of the DMA: N = T / 32 instructions a wave and step.
-// Instruction d of the T / 8 moves lines 8 d .. 8 d + 7: line l of a row
-// operand is its index l, chunk c its k = 8 c ..; line l of a col operand is
-// k = l % 64 of the indices 64 (l / 64) .., chunk c eight of them.  Indices
+// One operand's side of the DMA: N instructions a wave and step.  Instruction
+// d of the T / 8 moves lines 8 d .. 8 d + 7: line l of a row operand is its
+// index l, chunk c its c-th 16 bytes of k; line l of a col operand is k = l %
+// BK of the l / BK-th 128 bytes of indices, chunk c 16 bytes of them.  Indices
 // past the end are read as the last ones (their results are not stored).
-template <bool COL, int T>
+template <typename E, bool COL, int T>
 struct Side {
-    static constexpr int N = 4;
+    static constexpr int N = 4, ES = sizeof(E), BK = 128 / ES, EC = 16 / ES;
     uint32_t off[N];       // bytes from the step's base
     const char *base;      // the tile's first index at the step's first k
     int64_t step;          // bytes from one step's base to the next
@@ -86,40 +87,42 @@ struct Side {
     __device__ __forceinline__ void init(const Operand &o, int64_t i0, int64_t ni, int k0, int wave)
     {
         const int lane = threadIdx.x & 63;
-        const int64_t ld = o.ld * 2;
-        base = static_cast<const char *>(o.p) + (COL ? k0 * ld + i0 * 2 : i0 * ld + static_cast<int64_t>(k0) * 2);
-        step = COL ? kBK * ld : kBK * 2;
+        const int64_t ld = o.ld * ES;
+        base = static_cast<const char *>(o.p) + (COL ? k0 * ld + i0 * ES : i0 * ld + static_cast<int64_t>(k0) * ES);
+        step = COL ? BK * ld : BK * ES;
         const int last = static_cast<int>(min<int64_t>(ni - i0, T)) - 1;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int d = wave * N + i, line = d * 8 + (lane >> 3);
-            const int c = (lane & 7) ^ swz(COL ? line & 63 : line);
-            if (COL) {
-                const int x = (line >> 6) * 64 + c * 8;
-                off[i] = static_cast<uint32_t>((line & 63) * ld + min(x, last & ~7) * 2);
-            } else {
+            const int d = wave * N + i, line = d * 8 + (lane >> 3), k = line % BK;
+            const int c = (lane & 7) ^ swz(COL ? k : line);
+            if (COL)
+                off[i] = static_cast<uint32_t>(k * ld + min(line / BK * BK + c * EC, last & ~(EC - 1)) * ES);
+            else
                 off[i] = static_cast<uint32_t>(min(line, last) * ld + c * 16);
-            }
         }
     }
     // What instruction i reads in the last, partial step of `left` k: zeros
     // past the end of the sum.  A row operand is readable, and zero, up to the
-    // next multiple of eight.
+    // next multiple of a chunk.
     __device__ __forceinline__ const void *tail(int i, int64_t s, int left, int wave) const
     {
         const int lane = threadIdx.x & 63, line = (wave * N + i) * 8 + (lane >> 3);
-        const int k = COL ? line & 63 : ((lane & 7) ^ swz(line)) * 8;
+        const int k = COL ? line % BK : ((lane & 7) ^ swz(line)) * EC;
         return k < left ? static_cast<const void *>(base + s * step + off[i]) : static_cast<const void *>(&g_zeros);
     }
 };
 
-// Fragment t of 16 indices, k half kh of a stage: lane L holds index L % 16,
-// k = 32 kh + 8 (L / 16) .. + 7.
+// Fragment t of 16 indices, k half kh of a stage.  bf16: lane L holds index
+// L % 16, k = 32 kh + 8 (L / 16) .. + 7.  fp32: index L % 16, k = 16 kh +
+// 4 (L / 16) .. + 3, one for each of four instructions.
+template <typename E, bool COL>
+struct Frag;
 template <bool COL>
-struct Frag {
+struct Frag<uint16_t, COL> {
+    typedef bf16x8 Value;
     uint32_t row[2];        // row: byte offset per k half
     uint32_t col[4][2];     // col: per 16 indices of a 64-wide block, k lines + 0 and + 4
-    __device__ __forceinline__ void init(int t0)   // the wave's first fragment of its 64-wide block
+    __device__ __forceinline__ void init(int t0)   // the wave's first fragment of its block
     {
         const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
         if (!COL) {
@@ -139,7 +142,7 @@ struct Frag {
                 }
         }
     }
-    __device__ __forceinline__ bf16x8 read(const unsigned char *op, int t, int kh) const
+    __device__ __forceinline__ Value read(const unsigned char *op, int t, int kh) const
     {
         if (!COL)
             return *reinterpret_cast<const bf16x8 *>(op + row[kh] + t * 2048);
@@ -148,12 +151,60 @@ struct Frag {
         const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>((lds_byte *)(p + col[t & 3][1])));
         return bf16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     }
+    static __device__ __forceinline__ f32x4 multiply(const Value &b, const Value &a, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, c, 0, 0, 0);
+    }
+    static constexpr int kBlock = 64;   // indices of a col operand's 128 bytes
+};
+template <bool COL>
+struct Frag<float, COL> {
+    typedef f32x4 Value;
+    uint32_t row[2];
+    uint32_t col[2][4];     // per 16 indices of a 32-wide block, k
+    __device__ __forceinline__ void init(int t0)
+    {
+        const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+        if (!COL) {
+#pragma unroll
+            for (int kh = 0; kh < 2; ++kh)
+                row[kh] = l16 * 128 + 16 * ((kh * 4 + g) ^ swz(l16));
+        } else {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int line = g * 4 + e, x = ((t0 + t) & 1) * 16 + l16;
+                    col[t][e] = line * 128 + 16 * ((x >> 2) ^ swz(line)) + (x & 3) * 4;
+                }
+        }
+    }
+    __device__ __forceinline__ Value read(const unsigned char *op, int t, int kh) const
+    {
+        if (!COL)
+            return *reinterpret_cast<const f32x4 *>(op + row[kh] + t * 2048);
+        const unsigned char *p = op + (t >> 1) * 4096 + kh * 2048;
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] = *reinterpret_cast<const float *>(p + col[t & 1][e]);
+        return v;
+    }
+    static __device__ __forceinline__ f32x4 multiply(const Value &b, const Value &a, f32x4 c)
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(b[e], a[e], c, 0, 0, 0);
+        return c;
+    }
+    static constexpr int kBlock = 32;
 };
 
-template <int T, bool ACOL, bool BCOL, int KIND, typename TO>
-__global__ __launch_bounds__(2 * T, 2) void lin_bf16_kernel(Gemm g)
+template <typename E, int T, bool ACOL, bool BCOL, int KIND, typename TO>
+__global__ __launch_bounds__(2 * T, 2) void lin_tile_kernel(Gemm g)
 {
     extern __shared__ __align__(1024) unsigned char smem[];
+    constexpr int kBK = 128 / sizeof(E);
     constexpr int WN = T / 128;                 // waves along the columns
     constexpr int FA = T / 64;                  // 16-row fragments of a wave, four waves along the rows
     constexpr int OP = T * 128;                 // bytes of one operand's stage
@@ -179,13 +230,16 @@ __global__ __launch_bounds__(2 * T, 2) void lin_bf16_kernel(Gemm g)
     const int kbeg = split * g.kchunk, kend = min(g.K, kbeg + g.kchunk);
     const int nsteps = (kend - kbeg + kBK - 1) / kBK;
 
-    Side<ACOL, T> sa;
-    Side<BCOL, T> sb;
+    Side<E, ACOL, T> sa;
+    Side<E, BCOL, T> sb;
     sa.init(g.A, m0, g.M, kbeg, wave);
     sb.init(g.B, n0, g.N, kbeg, wave);
-    Frag<ACOL> fra;
-    Frag<BCOL> frb;
-    fra.init(FA == 4 ? 0 : 2 * (wm & 1));
+    typedef Frag<E, ACOL> FragA;
+    typedef Frag<E, BCOL> FragB;
+    FragA fra;
+    FragB frb;
+    constexpr int BA = FragA::kBlock / 16;      // fragments of a col operand's block
+    fra.init(wm * FA % BA);
     frb.init(0);
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte *)smem));
 
@@ -214,20 +268,20 @@ __global__ __launch_bounds__(2 * T, 2) void lin_bf16_kernel(Gemm g)
             acc[a][j] = f32x4{0, 0, 0, 0};
     // fragments of k half kh of a stage: eight of B's side, then FA of A's
     struct Frags {
-        bf16x8 f[8 + FA];
+        typename FragA::Value f[8 + FA];
     };
     const auto read = [&](Frags &f, int stage, int kh, int r) {
         const unsigned char *base = smem + stage * STAGE;
         if (r < 8)
             f.f[r] = frb.read(base + OP + wn * 16384, r, kh);
         else
-            f.f[r] = fra.read(base + (ACOL ? (wm * FA / 4) * 8192 : wm * FA * 2048), r - 8, kh);
+            f.f[r] = fra.read(base + (ACOL ? wm * FA / BA * (BA * 2048) : wm * FA * 2048), r - 8, kh);
     };
     // eight products at a time, with what goes out beside them
     const auto multiply = [&](const Frags &f, int a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            acc[a][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.f[j], f.f[8 + a], acc[a][j], 0, 0, 0);
+            acc[a][j] = FragA::multiply(f.f[j], f.f[8 + a], acc[a][j]);
     };
     const auto meet = [&]() {
         // this wave's DMA has landed and its LDS reads are done; then everyone's
@@ -288,32 +342,34 @@ __global__ __launch_bounds__(2 * T, 2) void lin_bf16_kernel(Gemm g)
                                n0 + wn * 128, split);
 }
 
-template <int T, bool ACOL, bool BCOL, int KIND, typename TO>
+template <typename E, int T, bool ACOL, bool BCOL, int KIND, typename TO>
 int launch(const Gemm &g, hipStream_t st, const char *tag)
 {
     constexpr size_t bytes = 2 * 2 * T * 128;
-    if (int rc = allow_lds(lin_bf16_kernel<T, ACOL, BCOL, KIND, TO>, bytes))
+    if (int rc = allow_lds(lin_tile_kernel<E, T, ACOL, BCOL, KIND, TO>, bytes))
         return rc;
-    ACSC_LAUNCH(tag, (lin_bf16_kernel<T, ACOL, BCOL, KIND, TO>), dim3(g.tm * g.tn, g.splits), dim3(2 * T), bytes, st, g);
+    ACSC_LAUNCH(tag, (lin_tile_kernel<E, T, ACOL, BCOL, KIND, TO>), dim3(g.tm * g.tn, g.splits), dim3(2 * T), bytes, st, g);
     return check_launch(tag);
 }
 
-template <int T>
+template <typename E, int T>
 int launch_kind(const Gemm &g, EpiKind kind, acsc_dtype out, hipStream_t st, const char *tag)
 {
     if (kind == kForward)
-        return launch<T, false, false, kForward, uint16_t>(g, st, tag);
+        return launch<E, T, false, false, kForward, E>(g, st, tag);
     if (kind == kGate)
-        return launch<T, false, true, kGate, uint16_t>(g, st, tag);
-    return out == ACSC_BF16 ? launch<T, true, true, kWeight, uint16_t>(g, st, tag)
-                            : launch<T, true, true, kWeight, float>(g, st, tag);
+        return launch<E, T, false, true, kGate, E>(g, st, tag);
+    return out == ACSC_BF16 ? launch<E, T, true, true, kWeight, uint16_t>(g, st, tag)
+                            : launch<E, T, true, true, kWeight, float>(g, st, tag);
 }
 
 }  // namespace
 
-int lin_bf16_run(const Gemm &g, int tile, EpiKind kind, acsc_dtype out, hipStream_t st, const char *tag)
+int lin_tile_run(const Gemm &g, int tile, EpiKind kind, acsc_dtype dt, acsc_dtype out, hipStream_t st, const char *tag)
 {
-    return tile == 256 ? launch_kind<256>(g, kind, out, st, tag) : launch_kind<128>(g, kind, out, st, tag);
+    if (dt == ACSC_F32)
+        return launch_kind<float, 128>(g, kind, out, st, tag);
+    return tile == 256 ? launch_kind<uint16_t, 256>(g, kind, out, st, tag) : launch_kind<uint16_t, 128>(g, kind, out, st, tag);
 }
 
 }  // namespace acsc
