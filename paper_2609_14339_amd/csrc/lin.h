@@ -40,10 +40,11 @@ struct Gemm {
     int64_t M;
     int N, K;
     int tm, tn;       // tiles along M and N
-    int splits;       // pieces along K, kchunk each
+    int whole;        // tiles that are not cut along K; the rest is cut into
+    int splits;       // pieces of kchunk each
     int kchunk;
-    float *part;      // piece s at part + s * M * ldp; nullptr: one piece, through the epilogue
-    int64_t ldp;
+    float *part;      // the pieces: of tiles [splits][tiles - whole][T][T]; of few tokens [splits][M][ldp], nullptr:
+    int64_t ldp;      // one piece, through the epilogue
     const float *dbpart;   // weight gradient: slices of column sums of dz, [slices][M], that the product's first
     int slices;            // tiles add into db; nullptr: none
     float *db;
@@ -156,17 +157,16 @@ __device__ __forceinline__ void load_bias(const Epi &e, int n, int N, float (&b)
 // residual on 16384 x 2048 -> 8192 cost 100 us that way, see the forward
 // kernel's figures); WHOLE: the wave's 128 columns all exist.
 template <typename T, int KIND, int NA, bool WHOLE>
-__device__ __forceinline__ void put_rows(const Gemm &g, const char *lds, int64_t m0, int n0, int split)
+__device__ __forceinline__ void put_rows(const Gemm &g, const char *lds, int64_t m0, int n0)
 {
     const int lane = threadIdx.x & 63, n = n0 + (lane & 15) * 8;
     const int cols = WHOLE ? 8 : g.N - n;
     float bias[8];
-    if (!g.part)
-        load_bias<T, KIND>(g.e, n, g.N, bias);
+    load_bias<T, KIND>(g.e, n, g.N, bias);
 #pragma unroll 1
     for (int r0 = 0; r0 < NA * 4; r0 += 4) {
         Beside<T> beside[4];
-        if (!g.part && has_beside<T, KIND>(g.e)) {
+        if (has_beside<T, KIND>(g.e)) {
 #pragma unroll
             for (int u = 0; u < 4; ++u)
                 load_beside<T, KIND>(g.e, beside[u], min<int64_t>(m0 + (r0 + u) * 4 + (lane >> 4), g.M - 1), n, cols);
@@ -179,18 +179,15 @@ __device__ __forceinline__ void put_rows(const Gemm &g, const char *lds, int64_t
             float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
             const int64_t m = m0 + row;
             const int left = m < g.M ? cols : 0;
-            if (g.part)
-                store8(g.part + (split * g.M + m) * g.ldp + n, left, v);
-            else
-                epilogue<T, KIND>(g.e, v, bias, beside[u], m, n, left);
+            epilogue<T, KIND>(g.e, v, bias, beside[u], m, n, left);
         }
     }
 }
 // The first column of tiles adds the slices of db, in order.
 template <int KIND>
-__device__ __forceinline__ void put_db(const Gemm &g, int64_t m0, int rows, int tile_n, int split)
+__device__ __forceinline__ void put_db(const Gemm &g, int64_t m0, int rows)
 {
-    if (KIND != kWeight || !g.dbpart || tile_n != 0 || split != 0)
+    if (KIND != kWeight || !g.dbpart)
         return;
     for (int64_t m = m0 + threadIdx.x; m < min<int64_t>(g.M, m0 + rows); m += blockDim.x) {
         float s = 0.f;
@@ -201,11 +198,21 @@ __device__ __forceinline__ void put_db(const Gemm &g, int64_t m0, int rows, int 
     }
 }
 
+// `part`: the piece's rows and columns of this wave, T a row, or nullptr.
 template <typename T, int KIND, int NA>
 __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8], char *lds, int64_t m0, int n0,
-                                         int split)
+                                         float *part, int ld)
 {
     const int lane = threadIdx.x & 63;
+    if (part) {
+        // four consecutive columns a lane, 64 bytes of a row at a time
+#pragma unroll
+        for (int a = 0; a < NA; ++a)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                *reinterpret_cast<f32x4 *>(part + (a * 16 + (lane & 15)) * ld + j * 16 + (lane >> 4) * 4) = acc[a][j];
+        return;
+    }
 #pragma unroll
     for (int a = 0; a < NA; ++a)
 #pragma unroll
@@ -218,9 +225,19 @@ __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     if (n0 + 128 <= g.N)
-        put_rows<T, KIND, NA, true>(g, lds, m0, n0, split);
+        put_rows<T, KIND, NA, true>(g, lds, m0, n0);
     else
-        put_rows<T, KIND, NA, false>(g, lds, m0, n0, split);
+        put_rows<T, KIND, NA, false>(g, lds, m0, n0);
+}
+
+// Tile `id` of the product's order: bands of four rows of tiles, column by
+// column, so that what an XCD's CUs read together stays in its L2.
+__device__ __forceinline__ void tile_at(const Gemm &g, int64_t id, int &tile_m, int &tile_n)
+{
+    const int64_t band = id / (4 * g.tn), in = id - band * 4 * g.tn;
+    const int height = static_cast<int>(min<int64_t>(g.tm - band * 4, 4));
+    tile_m = static_cast<int>(band * 4 + in % height);
+    tile_n = static_cast<int>(in / height);
 }
 
 }  // namespace acsc

@@ -23,36 +23,53 @@ inline int few_tokens(EpiKind kind, bool bf16)
 }
 
 // Adds the pieces of a cut product in order and takes the sum through the
-// epilogue: eight columns a thread, 2048 columns of a row a workgroup.
+// epilogue, eight columns a thread: of few tokens, 2048 columns of a row a
+// workgroup; of tiles, 2048 elements of a tile.
+__device__ __forceinline__ void add_pieces(const float *p, int64_t step, int splits, float (&v)[8])
+{
+    const f32x4 *q = reinterpret_cast<const f32x4 *>(p);
+    f32x4 lo = q[0], hi = q[1];
+#pragma unroll 4
+    for (int i = 1; i < splits; ++i) {
+        lo += q[i * step / 4];
+        hi += q[i * step / 4 + 1];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[i] = lo[i];
+        v[4 + i] = hi[i];
+    }
+}
 template <int KIND, typename TO>
+__device__ __forceinline__ void join(const Gemm &g, const float *p, int64_t step, bool on, int64_t m, int n)
+{
+    const int left = on ? g.N - n : 0;
+    float v[8] = {}, bias[8];
+    if (left > 0)
+        add_pieces(p, step, g.splits, v);
+    load_bias<TO, KIND>(g.e, n, g.N, bias);
+    Beside<TO> beside;
+    if (has_beside<TO, KIND>(g.e))
+        load_beside<TO, KIND>(g.e, beside, on ? m : 0, n, left);
+    epilogue<TO, KIND>(g.e, v, bias, beside, m, n, left);
+}
+template <typename TO>
+__global__ __launch_bounds__(256) void lin_join_few_kernel(Gemm g)
+{
+    const int64_t m = blockIdx.y;
+    const int n = (blockIdx.x * 256 + threadIdx.x) * 8;
+    join<kForward, TO>(g, g.part + m * g.ldp + n, g.M * g.ldp, true, m, n);
+}
+template <int KIND, typename TO, int T>
 __global__ __launch_bounds__(256) void lin_join_kernel(Gemm g)
 {
-    const int n = (blockIdx.x * 256 + threadIdx.x) * 8;
-    float bias[8];
-    load_bias<TO, KIND>(g.e, n, g.N, bias);
-    for (int64_t m = blockIdx.y; m < g.M; m += gridDim.y) {
-        float v[8] = {};
-        if (n < g.N) {
-            // rows of pieces are whole 32-byte runs
-            const f32x4 *p = reinterpret_cast<const f32x4 *>(g.part + m * g.ldp + n);
-            const int64_t step = g.M * g.ldp / 4;
-            f32x4 lo = p[0], hi = p[1];
-#pragma unroll 4
-            for (int i = 1; i < g.splits; ++i) {
-                lo += p[i * step];
-                hi += p[i * step + 1];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[i] = lo[i];
-                v[4 + i] = hi[i];
-            }
-        }
-        Beside<TO> beside;
-        if (has_beside<TO, KIND>(g.e))
-            load_beside<TO, KIND>(g.e, beside, m, n, g.N - n);
-        epilogue<TO, KIND>(g.e, v, bias, beside, m, n, g.N - n);
-    }
+    constexpr int PER = T * T / 2048;
+    const int64_t id = blockIdx.x / PER, count = static_cast<int64_t>(g.tm) * g.tn - g.whole;
+    const int c = (blockIdx.x % PER) * 256 + threadIdx.x, row = c / (T / 8), col = c % (T / 8) * 8;
+    int tile_m, tile_n;
+    tile_at(g, g.whole + id, tile_m, tile_n);
+    const int64_t m = static_cast<int64_t>(tile_m) * T + row;
+    join<KIND, TO>(g, g.part + (id * T + row) * T + col, count * T * T, m < g.M, m, tile_n * T + col);
 }
 
 // What a product needs done first, up to three jobs in one launch (a launch
@@ -173,7 +190,7 @@ inline size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 // they are.
 struct Plan {
     bool few;                               // the product for few tokens
-    int tile, tm, tn, splits, kchunk;
+    int tile, tm, tn, whole, splits, kchunk;
     int slices, slice;                      // of the rows, for db
     int64_t ldp;
     bool pack_a, pack_b;
@@ -208,16 +225,17 @@ inline bool readable(const Operand &o, bool col, int64_t inner, acsc_dtype dt)
 }
 
 // Tile and pieces of the sum, by the least estimated time.  A round is what
-// the card runs at once: a workgroup of a 256 tile per CU, two of a 128 tile
-// (or of an fp32 tile).  Measured on bf16 products, us: a 256 tile takes 1.5 a
-// step of 64 and 5 beside them (4096 x 2048 -> 8192: 56 a round of 32 steps);
-// a 128 tile 1.0 and 3 with a second one on its CU (2048 x 2048 -> 8192: 34.5
-// a round), 0.65 alone; an fp32 tile 4.8 a step of 32 (112 TFLOP/s at 4096^3),
-// 2.6 alone; the pieces' sum 4 for the launch and their bytes,
-// written and read, at 4.5 TB/s.  (256-tiles only where they fill a round,
-// without this: 2048 x 2048 -> 8192 in 99 us, with it 69.)
+// the card runs at once: a workgroup of a 256 tile per CU, two of a 128 tile.
+// Whole rounds of tiles are not cut; the tiles of a last, partial one may be,
+// so that their pieces fill the card.  Measured, us: a 256 tile takes 1.5 a
+// step of 64 and 5 beside them (bf16 4096 x 2048 -> 8192: 56 a round of 32
+// steps); a bf16 128 tile 1.0 and 3 with a second one on its CU (2048 x 2048 ->
+// 8192: 34.5 a round), 0.65 alone; an fp32 tile 4.1 a step of 32 (130 TFLOP/s
+// at 4096^3), 2.2 alone; the pieces' sum 4 for the launch and their bytes,
+// written and read, at 4.5 TB/s.  (256 tiles in two pieces each for 2048 x
+// 2048 -> 8192: 99 us, 128 tiles whole 58; PENDING)
 struct Cut {
-    int tile, splits, per;
+    int tile, whole, splits, per;
 };
 inline Cut cut_of(const Shape &s, int steps, bool bf16)
 {
@@ -225,20 +243,24 @@ inline Cut cut_of(const Shape &s, int steps, bool bf16)
     double least = 0;
     for (int tile = bf16 ? 256 : 128; tile >= 128; tile -= 128) {
         const int64_t tiles = ((s.M + tile - 1) / tile) * ((s.N + tile - 1) / tile);
-        const double step = !bf16 ? 4.8 : tile == 256 ? 1.5 : 1.0, alone = !bf16 ? 2.6 : tile == 256 ? 1.5 : 0.65;
+        const double step = !bf16 ? 4.1 : tile == 256 ? 1.5 : 1.0, alone = !bf16 ? 2.2 : tile == 256 ? 1.5 : 0.65;
         const double edge = tile == 256 ? 5 : 3;
         const int slots = tile == 256 ? 256 : 512;
-        for (int want = 1; want == 1 || (want <= 64 && steps / want >= 4 && tiles * want <= 2048); want += want < 8 ? 1 : 8) {
+        const auto rounds = [&](int64_t groups, int per) {
+            const int64_t rest = groups % slots;
+            return static_cast<double>(groups / slots) * (per * step + edge) +
+                   (rest ? per * (rest <= 256 ? alone : step) + edge : 0);
+        };
+        const int64_t rest = tiles % slots;
+        for (int want = 1; want == 1 || (rest && want <= 64 && steps / want >= 4 && rest * want <= 2048);
+             want += want < 8 ? 1 : 8) {
             const int per = (steps + want - 1) / want, n = (steps + per - 1) / per;
-            const int64_t groups = tiles * n, rest = groups % slots;
-            double t = static_cast<double>(groups / slots) * (per * step + edge);
-            if (rest)
-                t += per * (rest <= 256 ? alone : step) + edge;
-            if (n > 1)
-                t += 4 + n * static_cast<double>(s.M) * s.N * 8 / 4.5e6;
+            const double t = n == 1 ? rounds(tiles, steps)
+                                    : rounds(tiles - rest, steps) + rounds(rest * n, per) + 4 +
+                                          n * static_cast<double>(rest) * tile * tile * 8 / 4.5e6;
             if (least == 0 || t < least) {
                 least = t;
-                best = Cut{tile, n, per};
+                best = Cut{tile, static_cast<int>(n == 1 ? tiles : tiles - rest), n, per};
             }
         }
     }
@@ -273,10 +295,10 @@ inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bo
     p.tile = c.tile;
     p.tm = static_cast<int>((s.M + p.tile - 1) / p.tile);
     p.tn = (s.N + p.tile - 1) / p.tile;
+    p.whole = c.whole;
     p.splits = c.splits;
     p.kchunk = c.per * bk;
-    p.ldp = up8(s.N);
-    p.part = p.splits > 1 ? up256(static_cast<size_t>(p.splits) * s.M * p.ldp * 4) : 0;
+    p.part = up256(static_cast<size_t>(static_cast<int64_t>(p.tm) * p.tn - p.whole) * p.splits * p.tile * p.tile * 4);
     if (kind == kWeight) {
         // db's slices of at least 32 rows, up to about two workgroups a CU
         const int64_t blocks = (s.M + 511) / 512;
@@ -296,10 +318,13 @@ inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bo
 }
 
 template <int KIND, typename TO>
-void launch_join(const Gemm &g, hipStream_t st)
+void launch_join(const Gemm &g, const Plan &p, hipStream_t st)
 {
-    ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO>), dim3((g.N + 2047) / 2048, static_cast<unsigned>(std::min<int64_t>(g.M, 65535))),
-                dim3(256), 0, st, g);
+    const int tail = p.tm * p.tn - p.whole;
+    if (p.tile == 256)
+        ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 256>), dim3(tail * 32), dim3(256), 0, st, g);
+    else
+        ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 128>), dim3(tail * 8), dim3(256), 0, st, g);
 }
 
 // An input of the weight gradient that is formed again from what was kept.
@@ -336,9 +361,11 @@ int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype
     g.splits = p.splits;
     g.kchunk = p.kchunk;
     g.ldp = p.ldp;
-    // a piece goes through memory if there are more, or if its workgroups hold
-    // no whole checkpoint groups
-    g.part = p.splits > 1 || (p.few && g.e.q.codes) ? reinterpret_cast<float *>(ws) : nullptr;
+    g.whole = p.whole;
+    // the product for few tokens: a piece goes through memory if there are
+    // more, or if its workgroups hold no whole checkpoint groups
+    const bool pieces = p.splits > 1 || (p.few && g.e.q.codes);
+    g.part = pieces ? reinterpret_cast<float *>(ws) : nullptr;
     Jobs jobs{};
     if (again)
         add_operand(jobs, again->from, s.K, s.N, again->to, up8(s.N), again->kept);
@@ -388,14 +415,21 @@ int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype
     } else if (int rc = lin_tile_run(g, p.tile, kind, dt, out, st, tag)) {
         return rc;
     }
-    if (g.part) {
+    if (pieces) {
         const bool b = out == ACSC_BF16;
-        if (kind == kForward)
-            b ? launch_join<kForward, uint16_t>(g, st) : launch_join<kForward, float>(g, st);
-        else if (kind == kGate)
-            b ? launch_join<kGate, uint16_t>(g, st) : launch_join<kGate, float>(g, st);
-        else
-            b ? launch_join<kWeight, uint16_t>(g, st) : launch_join<kWeight, float>(g, st);
+        if (p.few) {
+            const dim3 grid((g.N + 2047) / 2048, static_cast<unsigned>(g.M));
+            if (b)
+                ACSC_LAUNCH("lin_join", lin_join_few_kernel<uint16_t>, grid, dim3(256), 0, st, g);
+            else
+                ACSC_LAUNCH("lin_join", lin_join_few_kernel<float>, grid, dim3(256), 0, st, g);
+        } else if (kind == kForward) {
+            b ? launch_join<kForward, uint16_t>(g, p, st) : launch_join<kForward, float>(g, p, st);
+        } else if (kind == kGate) {
+            b ? launch_join<kGate, uint16_t>(g, p, st) : launch_join<kGate, float>(g, p, st);
+        } else {
+            b ? launch_join<kWeight, uint16_t>(g, p, st) : launch_join<kWeight, float>(g, p, st);
+        }
         if (int rc = check_launch("lin_join"))
             return rc;
     }
@@ -442,7 +476,7 @@ inline int check_ws(const void *ws, size_t have, size_t need)
 // The largest tile grid: blockIdx.x is 32 bits.
 inline int check_tiles(const Plan &p)
 {
-    ACSC_CHECK_ARG(static_cast<int64_t>(p.tm) * p.tn < (1ll << 31), ACSC_EINVAL, "product too large");
+    ACSC_CHECK_ARG(p.few || static_cast<int64_t>(p.tm) * p.tn < (1ll << 31), ACSC_EINVAL, "product too large");
     return ACSC_OK;
 }
 

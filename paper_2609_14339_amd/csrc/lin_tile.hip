@@ -213,21 +213,26 @@ __global__ __launch_bounds__(2 * T, 2) void lin_tile_kernel(Gemm g)
     const int wm = wave / WN, wn = wave % WN;
 
     // Workgroups go to the eight XCDs in turn; each XCD takes a run of tiles
-    // of its own, in columns of four tiles, so that what its CUs read
-    // together stays in its L2.
-    int64_t id = blockIdx.x;
-    const int64_t tiles = static_cast<int64_t>(g.tm) * g.tn;
+    // of its own.  First the whole tiles, then the pieces of the others, a
+    // piece of each in turn.
+    int64_t id = blockIdx.x, count = g.whole, first = 0;
+    int split = -1;
+    if (id >= g.whole) {
+        first = g.whole;
+        count = static_cast<int64_t>(g.tm) * g.tn - g.whole;
+        split = static_cast<int>((id - first) / count);
+        id = (id - first) % count;
+    }
     {
-        const int64_t q = tiles / 8, r = tiles % 8, x = id % 8;
+        const int64_t q = count / 8, r = count % 8, x = id % 8;
         id = x * q + min(x, r) + id / 8;
     }
-    const int64_t band = id / (4 * g.tn), in = id - band * 4 * g.tn;
-    const int height = static_cast<int>(min<int64_t>(g.tm - band * 4, 4));
-    const int tile_m = static_cast<int>(band * 4 + in % height), tile_n = static_cast<int>(in / height);
-    const int split = blockIdx.y;
+    float *part = split < 0 ? nullptr : g.part + (split * count + id) * T * T;
+    int tile_m, tile_n;
+    tile_at(g, first + id, tile_m, tile_n);
     const int64_t m0 = static_cast<int64_t>(tile_m) * T;
     const int n0 = tile_n * T;
-    const int kbeg = split * g.kchunk, kend = min(g.K, kbeg + g.kchunk);
+    const int kbeg = split < 0 ? 0 : split * g.kchunk, kend = split < 0 ? g.K : min(g.K, kbeg + g.kchunk);
     const int nsteps = (kend - kbeg + kBK - 1) / kBK;
 
     Side<E, ACOL, T> sa;
@@ -333,13 +338,16 @@ __global__ __launch_bounds__(2 * T, 2) void lin_tile_kernel(Gemm g)
     for (; s < nsteps; ++s)
         step(s, std::false_type{});
     meet();
-    put_db<KIND>(g, m0, T, tile_n, split);
+    if (tile_n == 0 && split <= 0)
+        put_db<KIND>(g, m0, T);
+    if (part)
+        part += wm * FA * 16 * T + wn * 128;
     constexpr int NA = 2;
     char *own = reinterpret_cast<char *>(smem) + wave * NA * 8192;
 #pragma unroll
     for (int a = 0; a < FA; a += NA)
         put_tile<TO, KIND, NA>(g, reinterpret_cast<const f32x4(&)[NA][8]>(acc[a]), own, m0 + (wm * FA + a) * 16,
-                               n0 + wn * 128, split);
+                               n0 + wn * 128, part ? part + a * 16 * T : nullptr, T);
 }
 
 template <typename E, int T, bool ACOL, bool BCOL, int KIND, typename TO>
@@ -348,7 +356,7 @@ int launch(const Gemm &g, hipStream_t st, const char *tag)
     constexpr size_t bytes = 2 * 2 * T * 128;
     if (int rc = allow_lds(lin_tile_kernel<E, T, ACOL, BCOL, KIND, TO>, bytes))
         return rc;
-    ACSC_LAUNCH(tag, (lin_tile_kernel<E, T, ACOL, BCOL, KIND, TO>), dim3(g.tm * g.tn, g.splits), dim3(2 * T), bytes, st, g);
+    ACSC_LAUNCH(tag, (lin_tile_kernel<E, T, ACOL, BCOL, KIND, TO>), dim3(g.whole + (g.tm * g.tn - g.whole) * g.splits), dim3(2 * T), bytes, st, g);
     return check_launch(tag);
 }
 
