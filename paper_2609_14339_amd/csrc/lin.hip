@@ -231,9 +231,11 @@ inline bool readable(const Operand &o, bool col, int64_t inner, acsc_dtype dt)
 // step of 64 and 5 beside them (bf16 4096 x 2048 -> 8192: 56 a round of 32
 // steps); a bf16 128 tile 1.0 and 3 with a second one on its CU (2048 x 2048 ->
 // 8192: 34.5 a round), 0.65 alone; an fp32 tile 4.1 a step of 32 (130 TFLOP/s
-// at 4096^3), 2.2 alone; the pieces' sum 4 for the launch and their bytes,
-// written and read, at 4.5 TB/s.  (256 tiles in two pieces each for 2048 x
-// 2048 -> 8192: 99 us, 128 tiles whole 58; PENDING)
+// at 4096^3), 2.2 alone; the pieces' sum 10 for waiting and the launch, and
+// their bytes, written and read, at 4.5 TB/s.  Both sides: 2048 x 2048 -> 8192
+// in 256 tiles of two pieces each 99 us, in whole 128 tiles 58; the tiles of
+// the last round cut or not, 15057 x 3904 -> 1216 144 or 170, input gradient of
+// 1198 x 13312 -> 2176 79 or 91, 3000 x 3000 -> 3000 (not chosen) 88 or 76.
 struct Cut {
     int tile, whole, splits, per;
 };
@@ -256,7 +258,7 @@ inline Cut cut_of(const Shape &s, int steps, bool bf16)
              want += want < 8 ? 1 : 8) {
             const int per = (steps + want - 1) / want, n = (steps + per - 1) / per;
             const double t = n == 1 ? rounds(tiles, steps)
-                                    : rounds(tiles - rest, steps) + rounds(rest * n, per) + 4 +
+                                    : rounds(tiles - rest, steps) + rounds(rest * n, per) + 10 +
                                           n * static_cast<double>(rest) * tile * tile * 8 / 4.5e6;
             if (least == 0 || t < least) {
                 least = t;
