@@ -7,19 +7,21 @@ namespace acsc {
 int lin_few_run(const Gemm &g, acsc_dtype dt, hipStream_t st, const char *tag);
 int lin_few_weight_run(const Gemm &g, const Kept &kept, acsc_dtype dt, acsc_dtype out, float *db, hipStream_t st,
                        const char *tag);
-int lin_tile_run(const Gemm &g, int tile, EpiKind kind, acsc_dtype dt, acsc_dtype out, hipStream_t st, const char *tag);
+int lin_tile_run(const Gemm &g, int tile_rows, EpiKind kind, acsc_dtype dt, acsc_dtype out, hipStream_t st, const char *tag);
 
 namespace {
 
 // Tokens up to which a product does without tiles.  Forward: W is read once
-// and unstaged; 4096 -> 14336, 1 / 8 / 16 / 32 tokens, us: bf16 24.1, 28.3, 34.9,
-// 48.5 against 31 by tiles for each; fp32 53, 60, 68, 103 against 170.  Weight
-// gradient: outer products of unrounded activations; bf16 8192 -> 8192, 1 / 4 /
-// 8 tokens: 25.6, 30.0, 38.8 against 43 by tiles.  (The input gradient by
-// vector FMAs on rows of W read once took 39 against 36 by tiles.)
-inline int few_tokens(EpiKind kind, bool bf16)
+// and unstaged; 4096 -> 14336, 1 / 8 / 16 / 32 tokens, us: bf16 24, 28, 35, 48
+// against 31 by tiles for 4 to 64; fp32 53, 60, 68, 103 against 56.  Where the
+// tile kernel cannot read W it has to be copied first, three times its bytes:
+// there the kernel is used as far as it goes.  Weight gradient: outer products
+// of unrounded activations; bf16 8192 -> 8192, 1 / 4 / 8 tokens: 25.6, 30.0,
+// 38.8 against 43 by tiles.  (The input gradient by vector FMAs on rows of W
+// read once took 39 against 31 by tiles.)
+inline int few_tokens(EpiKind kind, bool bf16, bool fits_b)
 {
-    return kind == kForward ? (bf16 ? 8 : 32) : kind == kWeight ? 8 : 0;
+    return kind == kForward ? (fits_b ? 8 : bf16 ? 16 : 32) : kind == kWeight ? 8 : 0;
 }
 
 // Adds the pieces of a cut product in order and takes the sum through the
@@ -60,16 +62,16 @@ __global__ __launch_bounds__(256) void lin_join_few_kernel(Gemm g)
     const int n = (blockIdx.x * 256 + threadIdx.x) * 8;
     join<kForward, TO>(g, g.part + m * g.ldp + n, g.M * g.ldp, true, m, n);
 }
-template <int KIND, typename TO, int T>
+template <int KIND, typename TO, int TM, int T>
 __global__ __launch_bounds__(256) void lin_join_kernel(Gemm g)
 {
-    constexpr int PER = T * T / 2048;
+    constexpr int PER = TM * T / 2048;
     const int64_t id = blockIdx.x / PER, count = static_cast<int64_t>(g.tm) * g.tn - g.whole;
     const int c = (blockIdx.x % PER) * 256 + threadIdx.x, row = c / (T / 8), col = c % (T / 8) * 8;
     int tile_m, tile_n;
     tile_at(g, g.whole + id, tile_m, tile_n);
-    const int64_t m = static_cast<int64_t>(tile_m) * T + row;
-    join<KIND, TO>(g, g.part + (id * T + row) * T + col, count * T * T, m < g.M, m, tile_n * T + col);
+    const int64_t m = static_cast<int64_t>(tile_m) * TM + row;
+    join<KIND, TO>(g, g.part + (id * TM + row) * T + col, count * TM * T, m < g.M, m, tile_n * T + col);
 }
 
 // What a product needs done first, up to three jobs in one launch (a launch
@@ -190,7 +192,8 @@ inline size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 // they are.
 struct Plan {
     bool few;                               // the product for few tokens
-    int tile, tm, tn, whole, splits, kchunk;
+    int rows, tile;                         // of a tile: its rows and columns
+    int tm, tn, whole, splits, kchunk;
     int slices, slice;                      // of the rows, for db
     int64_t ldp;
     bool pack_a, pack_b;
@@ -225,44 +228,59 @@ inline bool readable(const Operand &o, bool col, int64_t inner, acsc_dtype dt)
 }
 
 // Tile and pieces of the sum, by the least estimated time.  A round is what
-// the card runs at once: a workgroup of a 256 tile per CU, two of a 128 tile.
-// Whole rounds of tiles are not cut; the tiles of a last, partial one may be,
-// so that their pieces fill the card.  Measured, us: a 256 tile takes 1.5 a
-// step of 64 and 5 beside them (bf16 4096 x 2048 -> 8192: 56 a round of 32
-// steps); a bf16 128 tile 1.0 and 3 with a second one on its CU (2048 x 2048 ->
-// 8192: 34.5 a round), 0.65 alone; an fp32 tile 4.1 a step of 32 (130 TFLOP/s
-// at 4096^3), 2.2 alone; the pieces' sum 10 for waiting and the launch, and
-// their bytes, written and read, at 4.5 TB/s.  Both sides: 2048 x 2048 -> 8192
-// in 256 tiles of two pieces each 99 us, in whole 128 tiles 58; the tiles of
-// the last round cut or not, 15057 x 3904 -> 1216 144 or 170, input gradient of
-// 1198 x 13312 -> 2176 79 or 91, 3000 x 3000 -> 3000 (not chosen) 88 or 76.
+// the card runs at once, `at_once` workgroups a CU.  Whole rounds of tiles are
+// not cut; the tiles of a last, partial one may be, so that their pieces fill
+// the card.  The times are measured: a 256 tile takes 1.5 us a step of 64 and
+// 5 beside them (bf16 4096 x 2048 -> 8192: 56 a round of 32 steps); a bf16 128
+// tile 1.0 and 3 with a second one on its CU (2048 x 2048 -> 8192: 34.5 a
+// round), 0.65 alone; an fp32 tile 4.1 a step of 32 (130 TFLOP/s at 4096^3),
+// 2.2 alone; the narrow tiles wait for W's bytes from memory, and 4096 ->
+// 14336 alone took 0.9 (bf16) and 1.2 (fp32); the pieces' sum 10 for waiting
+// and the launch, and their bytes, written and read, at 4.5 TB/s.
+// Both sides: 2048 x 2048 -> 8192 in 256 tiles of two pieces each 99 us, in
+// whole 128 tiles 58; the tiles of the last round cut or not, 15057 x 3904 ->
+// 1216 144 or 163, input gradient of 1198 x 13312 -> 2176 81 or 93, 3000 x 3000
+// -> 3000 (not chosen) 88 or 80; 4096 -> 14336, forward / input gradient of 12,
+// 52, 128 tokens: tiles of 32 rows bf16 29/31, 57/39, 63/57, fp32 -/56, 86/87,
+// 207/139; of 64 31/37, 31/38, 60/44, -/78, 84/83, 151/137; of 128 44/40, 46/41,
+// 46/46, -/136, 147/131, 143/137.
 struct Cut {
-    int tile, whole, splits, per;
+    int rows, tile, whole, splits, per;
 };
-inline Cut cut_of(const Shape &s, int steps, bool bf16)
+struct Tile {
+    int rows, cols;
+    int at_once;          // workgroups of a CU
+    double step, alone;   // us of a step with as many, and with one
+    double edge;
+};
+inline Cut cut_of(EpiKind kind, const Shape &s, int steps, bool bf16)
 {
+    static const Tile kBf16[] = {
+        {256, 256, 1, 1.5, 1.5, 5}, {128, 128, 2, 1.0, 0.65, 3}, {64, 128, 3, 1.05, 0.85, 3}, {32, 128, 4, 1.0, 0.8, 3}};
+    static const Tile kF32[] = {{128, 128, 2, 4.1, 2.2, 3}, {64, 128, 3, 3.2, 1.2, 3}, {32, 128, 4, 2.3, 1.2, 3}};
+    const Tile *first = bf16 ? kBf16 : kF32, *end = bf16 ? std::end(kBf16) : std::end(kF32);
     Cut best{};
     double least = 0;
-    for (int tile = bf16 ? 256 : 128; tile >= 128; tile -= 128) {
-        const int64_t tiles = ((s.M + tile - 1) / tile) * ((s.N + tile - 1) / tile);
-        const double step = !bf16 ? 4.1 : tile == 256 ? 1.5 : 1.0, alone = !bf16 ? 2.2 : tile == 256 ? 1.5 : 0.65;
-        const double edge = tile == 256 ? 5 : 3;
-        const int slots = tile == 256 ? 256 : 512;
+    for (const Tile *t = first; t != end; ++t) {
+        if (t->rows != t->cols && kind == kWeight)
+            continue;
+        const int64_t tiles = ((s.M + t->rows - 1) / t->rows) * ((s.N + t->cols - 1) / t->cols);
+        const int slots = 256 * t->at_once;
         const auto rounds = [&](int64_t groups, int per) {
-            const int64_t rest = groups % slots;
-            return static_cast<double>(groups / slots) * (per * step + edge) +
-                   (rest ? per * (rest <= 256 ? alone : step) + edge : 0);
+            const int64_t rest = groups % slots, beside = (rest + 255) / 256 - 1;
+            const double step = t->at_once > 1 ? t->alone + (t->step - t->alone) * static_cast<double>(beside) / (t->at_once - 1) : t->alone;
+            return static_cast<double>(groups / slots) * (per * t->step + t->edge) + (rest ? per * step + t->edge : 0);
         };
         const int64_t rest = tiles % slots;
         for (int want = 1; want == 1 || (rest && want <= 64 && steps / want >= 4 && rest * want <= 2048);
              want += want < 8 ? 1 : 8) {
             const int per = (steps + want - 1) / want, n = (steps + per - 1) / per;
-            const double t = n == 1 ? rounds(tiles, steps)
-                                    : rounds(tiles - rest, steps) + rounds(rest * n, per) + 10 +
-                                          n * static_cast<double>(rest) * tile * tile * 8 / 4.5e6;
-            if (least == 0 || t < least) {
-                least = t;
-                best = Cut{tile, static_cast<int>(n == 1 ? tiles : tiles - rest), n, per};
+            const double us = n == 1 ? rounds(tiles, steps)
+                                     : rounds(tiles - rest, steps) + rounds(rest * n, per) + 10 +
+                                           n * static_cast<double>(rest) * t->rows * t->cols * 8 / 4.5e6;
+            if (least == 0 || us < least) {
+                least = us;
+                best = Cut{t->rows, t->cols, static_cast<int>(n == 1 ? tiles : tiles - rest), n, per};
             }
         }
     }
@@ -275,12 +293,12 @@ inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bo
     const bool bf16 = dt == ACSC_BF16;
     const int bk = 128 / static_cast<int>(dtype_size(dt));
     const int steps = (s.K + bk - 1) / bk;
-    if (kind == kWeight && s.K <= few_tokens(kind, bf16)) {
+    if (kind == kWeight && s.K <= few_tokens(kind, bf16, fits_b)) {
         p.few = true;
         p.splits = 1;
         return p;
     }
-    if (kind == kForward && s.M <= few_tokens(kind, bf16)) {
+    if (kind == kForward && s.M <= few_tokens(kind, bf16, fits_b)) {
         // 16 outputs a workgroup: a cut only where they fill half the CUs at
         // most, at two rounds of eight lines a piece
         const int groups = (s.N + 15) / 16, round = 8 * 128 / static_cast<int>(dtype_size(dt)), rounds = (s.K + round - 1) / round;
@@ -293,14 +311,15 @@ inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bo
         p.part = up256(static_cast<size_t>(p.splits) * s.M * p.ldp * 4);
         return p;
     }
-    const Cut c = cut_of(s, steps, bf16);
+    const Cut c = cut_of(kind, s, steps, bf16);
+    p.rows = c.rows;
     p.tile = c.tile;
-    p.tm = static_cast<int>((s.M + p.tile - 1) / p.tile);
+    p.tm = static_cast<int>((s.M + p.rows - 1) / p.rows);
     p.tn = (s.N + p.tile - 1) / p.tile;
     p.whole = c.whole;
     p.splits = c.splits;
     p.kchunk = c.per * bk;
-    p.part = up256(static_cast<size_t>(static_cast<int64_t>(p.tm) * p.tn - p.whole) * p.splits * p.tile * p.tile * 4);
+    p.part = up256(static_cast<size_t>(static_cast<int64_t>(p.tm) * p.tn - p.whole) * p.splits * p.rows * p.tile * 4);
     if (kind == kWeight) {
         // db's slices of at least 32 rows, up to about two workgroups a CU
         const int64_t blocks = (s.M + 511) / 512;
@@ -323,10 +342,21 @@ template <int KIND, typename TO>
 void launch_join(const Gemm &g, const Plan &p, hipStream_t st)
 {
     const int tail = p.tm * p.tn - p.whole;
-    if (p.tile == 256)
-        ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 256>), dim3(tail * 32), dim3(256), 0, st, g);
-    else
-        ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 128>), dim3(tail * 8), dim3(256), 0, st, g);
+    const dim3 grid(tail * (p.rows * p.tile / 2048));
+    if (p.rows == 256) {
+        ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 256, 256>), grid, dim3(256), 0, st, g);
+        return;
+    }
+    if constexpr (KIND != kWeight) {
+        if (p.rows < 128) {
+            if (p.rows == 64)
+                ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 64, 128>), grid, dim3(256), 0, st, g);
+            else
+                ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 32, 128>), grid, dim3(256), 0, st, g);
+            return;
+        }
+    }
+    ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 128, 128>), grid, dim3(256), 0, st, g);
 }
 
 // An input of the weight gradient that is formed again from what was kept.
@@ -414,7 +444,7 @@ int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype
     if (p.few) {
         if (int rc = lin_few_run(g, dt, st, tag))
             return rc;
-    } else if (int rc = lin_tile_run(g, p.tile, kind, dt, out, st, tag)) {
+    } else if (int rc = lin_tile_run(g, p.rows, kind, dt, out, st, tag)) {
         return rc;
     }
     if (pieces) {
@@ -507,10 +537,14 @@ static int workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dty
     const EpiKind kind = op == LIN_FORWARD ? kForward : op == LIN_BACKWARD_INPUT ? kGate : kWeight;
     const Shape s = shape_of(kind, rows, n_in, n_out);
     const Operand best{nullptr, 8};
-    const bool a = !any && readable(best, s.acol, s.acol ? s.M : s.K, dt);
-    const bool b = !any && readable(best, s.bcol, s.bcol ? s.N : s.K, dt);
-    *bytes = plan_of(kind, s, dt, a, b).bytes() +
-             (kind == kWeight && rows > few_tokens(kind, dt == ACSC_BF16) ? recomputed_bytes(rows, n_in, dt) : 0);
+    const bool a = readable(best, s.acol, s.acol ? s.M : s.K, dt);
+    const bool b = readable(best, s.bcol, s.bcol ? s.N : s.K, dt);
+    // with any alignment: the most that either operand's copy, or its absence, takes
+    *bytes = plan_of(kind, s, dt, a, b).bytes();
+    for (int copies = 1; any && copies < 4; ++copies)
+        *bytes = std::max(*bytes, plan_of(kind, s, dt, a && !(copies & 1), b && !(copies & 2)).bytes());
+    if (kind == kWeight && rows > few_tokens(kind, dt == ACSC_BF16, true))
+        *bytes += recomputed_bytes(rows, n_in, dt);
     return ACSC_OK;
 }
 
@@ -675,7 +709,7 @@ extern "C" int lin_backward_weight(const void *dz, int64_t ld_dz, const void *x,
     const Shape s = shape_of(kWeight, rows, n_in, n_out);
     Gemm g{};
     g.e = Epi{dW, ld_dw, nullptr, nullptr, 0, nullptr, 0, q8_of(nullptr), ACSC_ACT_NONE, accumulate};
-    if (rows <= few_tokens(kWeight, dt == ACSC_BF16)) {
+    if (rows <= few_tokens(kWeight, dt == ACSC_BF16, true)) {
         g.A = {dz, ld_dz};
         g.B = {x, ld_x};
         g.M = s.M;

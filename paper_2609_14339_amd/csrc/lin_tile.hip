@@ -1,9 +1,10 @@
 // The tiled products of the linear layers, on v_mfma_f32_16x16x32_bf16 and
 // v_mfma_f32_16x16x4_f32.
 //
-// A workgroup takes a T x T tile of C (T = 256, bf16 only: eight waves of 64
-// rows by 128 columns; T = 128: four of 32 by 128) in steps of 128 bytes along
-// the sum (64 bf16, 32 fp32).  Each step's tiles of A and B come straight from
+// A workgroup takes a TM x T tile of C in steps of 128 bytes along the sum (64
+// bf16, 32 fp32): 256 x 256 (bf16 only) by eight waves of 64 rows and 128
+// columns, 128 x 128 by four of 32 rows, and, for the few rows of a forward
+// product or an input gradient, 64 x 128 by four of 16 and 32 x 128 by two.  Each step's tiles of A and B come straight from
 // memory into LDS (global_load_lds_dwordx4), into two stages in turn; no
 // register holds them on the way.  An operand stays in LDS as it is stored:
 // lines of one index's step (row) or k-lines of 128 bytes of its own indices
@@ -56,6 +57,30 @@ __device__ __forceinline__ void dma16(const char *a, uint32_t aoff, uint32_t ald
                  : "v"(aoff), "s"(a), "s"(alds), "v"(boff), "s"(b), "s"(blds)
                  : "memory");
 }
+__device__ __forceinline__ void dma16(const char *b, uint32_t boff, uint32_t blds)
+{
+    uint32_t saved;
+    asm volatile("s_mov_b32 %0, m0\n\t"
+                 "s_mov_b32 m0, %3\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dwordx4 %1, %2\n\t"
+                 "s_mov_b32 m0, %0"
+                 : "=&s"(saved)
+                 : "v"(boff), "s"(b), "s"(blds)
+                 : "memory");
+}
+__device__ __forceinline__ void dma16(const void *b, uint32_t blds)
+{
+    uint32_t saved;
+    asm volatile("s_mov_b32 %0, m0\n\t"
+                 "s_mov_b32 m0, %2\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dwordx4 %1, off\n\t"
+                 "s_mov_b32 m0, %0"
+                 : "=&s"(saved)
+                 : "v"(b), "s"(blds)
+                 : "memory");
+}
 __device__ __forceinline__ void dma16(const void *a, uint32_t alds, const void *b, uint32_t blds)
 {
     uint32_t saved;
@@ -72,14 +97,14 @@ __device__ __forceinline__ void dma16(const void *a, uint32_t alds, const void *
                  : "memory");
 }
 
-// One operand's side of the DMA: N instructions a wave and step.  Instruction
-// d of the T / 8 moves lines 8 d .. 8 d + 7: line l of a row operand is its
+// One operand's side of the DMA: N instructions a wave and step for the tile's
+// T indices.  Instruction d of the T / 8 moves lines 8 d .. 8 d + 7: line l of a row operand is its
 // index l, chunk c its c-th 16 bytes of k; line l of a col operand is k = l %
 // BK of the l / BK-th 128 bytes of indices, chunk c 16 bytes of them.  Indices
 // past the end are read as the last ones (their results are not stored).
-template <typename E, bool COL, int T>
+template <typename E, bool COL, int T, int N>
 struct Side {
-    static constexpr int N = 4, ES = sizeof(E), BK = 128 / ES, EC = 16 / ES;
+    static constexpr int ES = sizeof(E), BK = 128 / ES, EC = 16 / ES;
     uint32_t off[N];       // bytes from the step's base
     const char *base;      // the tile's first index at the step's first k
     int64_t step;          // bytes from one step's base to the next
@@ -200,15 +225,20 @@ struct Frag<float, COL> {
     static constexpr int kBlock = 32;
 };
 
-template <typename E, int T, bool ACOL, bool BCOL, int KIND, typename TO>
-__global__ __launch_bounds__(2 * T, 2) void lin_tile_kernel(Gemm g)
+// Fragments of 16 rows of a wave, and waves, for a tile of TM rows.
+constexpr int fragments(int TM) { return TM < 64 ? 1 : TM / 64; }
+constexpr int waves(int TM, int T) { return TM / (16 * fragments(TM)) * (T / 128); }
+
+template <typename E, int TM, int T, bool ACOL, bool BCOL, int KIND, typename TO>
+__global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_kernel(Gemm g)
 {
     extern __shared__ __align__(1024) unsigned char smem[];
+    static_assert(!ACOL || TM == T, "a col operand A fills whole blocks");
     constexpr int kBK = 128 / sizeof(E);
     constexpr int WN = T / 128;                 // waves along the columns
-    constexpr int FA = T / 64;                  // 16-row fragments of a wave, four waves along the rows
-    constexpr int OP = T * 128;                 // bytes of one operand's stage
-    constexpr int STAGE = 2 * OP;
+    constexpr int FA = fragments(TM);
+    constexpr int OP = TM * 128;                // bytes of A's part of a stage
+    constexpr int STAGE = OP + T * 128;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
@@ -227,16 +257,19 @@ __global__ __launch_bounds__(2 * T, 2) void lin_tile_kernel(Gemm g)
         const int64_t q = count / 8, r = count % 8, x = id % 8;
         id = x * q + min(x, r) + id / 8;
     }
-    float *part = split < 0 ? nullptr : g.part + (split * count + id) * T * T;
+    float *part = split < 0 ? nullptr : g.part + (split * count + id) * TM * T;
     int tile_m, tile_n;
     tile_at(g, first + id, tile_m, tile_n);
-    const int64_t m0 = static_cast<int64_t>(tile_m) * T;
+    const int64_t m0 = static_cast<int64_t>(tile_m) * TM;
     const int n0 = tile_n * T;
-    const int kbeg = split < 0 ? 0 : split * g.kchunk, kend = split < 0 ? g.K : min(g.K, kbeg + g.kchunk);
+    const int kbeg = split < 0 ? 0 : split * g.kchunk;
+    const int kend = split < 0 ? g.K : kbeg + min(g.K - kbeg, g.kchunk);
     const int nsteps = (kend - kbeg + kBK - 1) / kBK;
 
-    Side<E, ACOL, T> sa;
-    Side<E, BCOL, T> sb;
+    // DMA instructions of a wave and step
+    constexpr int NA = TM / 8 / waves(TM, T), NB = T / 8 / waves(TM, T);
+    Side<E, ACOL, TM, NA> sa;
+    Side<E, BCOL, T, NB> sb;
     sa.init(g.A, m0, g.M, kbeg, wave);
     sb.init(g.B, n0, g.N, kbeg, wave);
     typedef Frag<E, ACOL> FragA;
@@ -248,12 +281,15 @@ __global__ __launch_bounds__(2 * T, 2) void lin_tile_kernel(Gemm g)
     frb.init(0);
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte *)smem));
 
-    constexpr int N = 4;                        // DMA instructions of an operand's step and wave
-    constexpr int NI = N / FA, NR = (8 + FA) / FA;   // of them, and fragments, beside eight products
+    constexpr int NI = NB / FA, NR = (8 + FA) / FA;   // DMA of a side, and fragments, beside eight products
+    const auto to_a = [&](int s, int i) { return lds0 + (s & 1) * STAGE + (wave * NA + i) * 1024; };
+    const auto to_b = [&](int s, int i) { return lds0 + (s & 1) * STAGE + OP + (wave * NB + i) * 1024; };
     // instruction i of step s, which is whole
     const auto issue = [&](int s, int i) {
-        const uint32_t to = lds0 + (s & 1) * STAGE + (wave * N + i) * 1024;
-        dma16(sa.base + s * sa.step, sa.off[i], to, sb.base + s * sb.step, sb.off[i], to + OP);
+        if (i < NA)
+            dma16(sa.base + s * sa.step, sa.off[i < NA ? i : 0], to_a(s, i), sb.base + s * sb.step, sb.off[i], to_b(s, i));
+        else
+            dma16(sb.base + s * sb.step, sb.off[i], to_b(s, i));
     };
     // the same of any step
     const auto issue_any = [&](int s, int i) {
@@ -261,8 +297,10 @@ __global__ __launch_bounds__(2 * T, 2) void lin_tile_kernel(Gemm g)
         if (left >= kBK) {
             issue(s, i);
         } else if (left > 0) {
-            const uint32_t to = lds0 + (s & 1) * STAGE + (wave * N + i) * 1024;
-            dma16(sa.tail(i, s, left, wave), to, sb.tail(i, s, left, wave), to + OP);
+            if (i < NA)
+                dma16(sa.tail(i < NA ? i : 0, s, left, wave), to_a(s, i), sb.tail(i, s, left, wave), to_b(s, i));
+            else
+                dma16(sb.tail(i, s, left, wave), to_b(s, i));
         }
     };
     f32x4 acc[FA][8];
@@ -322,11 +360,11 @@ __global__ __launch_bounds__(2 * T, 2) void lin_tile_kernel(Gemm g)
     };
 
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < NB; ++i)
         issue_any(0, i);
     meet();
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < NB; ++i)
         issue_any(1, i);
 #pragma unroll
     for (int r = 0; r < 8 + FA; ++r)
@@ -339,45 +377,58 @@ __global__ __launch_bounds__(2 * T, 2) void lin_tile_kernel(Gemm g)
         step(s, std::false_type{});
     meet();
     if (tile_n == 0 && split <= 0)
-        put_db<KIND>(g, m0, T);
+        put_db<KIND>(g, m0, TM);
     if (part)
         part += wm * FA * 16 * T + wn * 128;
-    constexpr int NA = 2;
-    char *own = reinterpret_cast<char *>(smem) + wave * NA * 8192;
+    constexpr int PUT = FA < 2 ? FA : 2;        // fragments' rows at a time
+    char *own = reinterpret_cast<char *>(smem) + wave * PUT * 8192;
 #pragma unroll
-    for (int a = 0; a < FA; a += NA)
-        put_tile<TO, KIND, NA>(g, reinterpret_cast<const f32x4(&)[NA][8]>(acc[a]), own, m0 + (wm * FA + a) * 16,
+    for (int a = 0; a < FA; a += PUT)
+        put_tile<TO, KIND, PUT>(g, reinterpret_cast<const f32x4(&)[PUT][8]>(acc[a]), own, m0 + (wm * FA + a) * 16,
                                n0 + wn * 128, part ? part + a * 16 * T : nullptr, T);
 }
 
-template <typename E, int T, bool ACOL, bool BCOL, int KIND, typename TO>
+template <typename E, int TM, int T, bool ACOL, bool BCOL, int KIND, typename TO>
 int launch(const Gemm &g, hipStream_t st, const char *tag)
 {
-    constexpr size_t bytes = 2 * 2 * T * 128;
-    if (int rc = allow_lds(lin_tile_kernel<E, T, ACOL, BCOL, KIND, TO>, bytes))
+    constexpr size_t bytes = 2 * (TM + T) * 128;
+    if (int rc = allow_lds(lin_tile_kernel<E, TM, T, ACOL, BCOL, KIND, TO>, bytes))
         return rc;
-    ACSC_LAUNCH(tag, (lin_tile_kernel<E, T, ACOL, BCOL, KIND, TO>), dim3(g.whole + (g.tm * g.tn - g.whole) * g.splits), dim3(2 * T), bytes, st, g);
+    ACSC_LAUNCH(tag, (lin_tile_kernel<E, TM, T, ACOL, BCOL, KIND, TO>),
+                dim3(g.whole + (g.tm * g.tn - g.whole) * g.splits), dim3(64 * waves(TM, T)), bytes, st, g);
     return check_launch(tag);
 }
 
-template <typename E, int T>
+template <typename E, int TM, int T>
 int launch_kind(const Gemm &g, EpiKind kind, acsc_dtype out, hipStream_t st, const char *tag)
 {
     if (kind == kForward)
-        return launch<E, T, false, false, kForward, E>(g, st, tag);
+        return launch<E, TM, T, false, false, kForward, E>(g, st, tag);
     if (kind == kGate)
-        return launch<E, T, false, true, kGate, E>(g, st, tag);
-    return out == ACSC_BF16 ? launch<E, T, true, true, kWeight, uint16_t>(g, st, tag)
-                            : launch<E, T, true, true, kWeight, float>(g, st, tag);
+        return launch<E, TM, T, false, true, kGate, E>(g, st, tag);
+    if constexpr (TM == T)
+        return out == ACSC_BF16 ? launch<E, TM, T, true, true, kWeight, uint16_t>(g, st, tag)
+                                : launch<E, TM, T, true, true, kWeight, float>(g, st, tag);
+    return ACSC_EINVAL;   // narrow tiles are of the other two kinds
+}
+
+template <typename E>
+int launch_narrow(const Gemm &g, int tile_rows, EpiKind kind, acsc_dtype out, hipStream_t st, const char *tag)
+{
+    if (tile_rows == 128)
+        return launch_kind<E, 128, 128>(g, kind, out, st, tag);
+    return tile_rows == 64 ? launch_kind<E, 64, 128>(g, kind, out, st, tag)
+                           : launch_kind<E, 32, 128>(g, kind, out, st, tag);
 }
 
 }  // namespace
 
-int lin_tile_run(const Gemm &g, int tile, EpiKind kind, acsc_dtype dt, acsc_dtype out, hipStream_t st, const char *tag)
+int lin_tile_run(const Gemm &g, int tile_rows, EpiKind kind, acsc_dtype dt, acsc_dtype out, hipStream_t st, const char *tag)
 {
     if (dt == ACSC_F32)
-        return launch_kind<float, 128>(g, kind, out, st, tag);
-    return tile == 256 ? launch_kind<uint16_t, 256>(g, kind, out, st, tag) : launch_kind<uint16_t, 128>(g, kind, out, st, tag);
+        return launch_narrow<float>(g, tile_rows, kind, out, st, tag);
+    return tile_rows == 256 ? launch_kind<uint16_t, 256, 256>(g, kind, out, st, tag)
+                            : launch_narrow<uint16_t>(g, tile_rows, kind, out, st, tag);
 }
 
 }  // namespace acsc
