@@ -75,13 +75,21 @@ __device__ __forceinline__ bool has_beside(const Epi &e)
 template <typename T, int KIND>
 __device__ __forceinline__ void load_beside(const Epi &e, Beside<T> &b, int64_t m, int n, int left)
 {
-    if (KIND == kGate && e.q.codes) {
-        load_raw(e.q.codes + m * e.q.ldc + n, left, b.codes);
-        b.scale = left > 0 ? e.q.scales[m * e.q.lds + n / kGroup] : 0.f;
+    const T *p = static_cast<const T *>(KIND == kForward ? e.res : KIND == kGate ? e.z : e.y);
+    p += m * (KIND == kForward ? e.ldr : KIND == kGate ? e.ldz : e.ldy) + n;
+    if (KIND != kGate) {
+        load_raw(p, left, b.v);
         return;
     }
-    const T *p = static_cast<const T *>(KIND == kForward ? e.res : KIND == kGate ? e.z : e.y);
-    load_raw(p + m * (KIND == kForward ? e.ldr : KIND == kGate ? e.ldz : e.ldy) + n, left, b.v);
+    // written once, after both ways: in each of them, b stays in memory
+    Beside<T> r = {};
+    if (e.q.codes) {
+        load_raw(e.q.codes + m * e.q.ldc + n, left, r.codes);
+        r.scale = left > 0 ? e.q.scales[m * e.q.lds + n / kGroup] : 0.f;
+    } else {
+        load_raw(p, left, r.v);
+    }
+    b = r;
 }
 template <typename T, int KIND>
 __device__ __forceinline__ void beside_values(const Epi &e, const Beside<T> &b, float (&v)[8])

@@ -337,6 +337,63 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void ln_bac
     }
 }
 
+// dx of fp32 rows past 8192 columns, which with their sums leave no registers
+// either: a workgroup reads a row for its two sums and again, from the caches,
+// for dx, with the column sums taken by ln_sums_kernel (PENDINGW).
+template <bool KEPT>
+__global__ __launch_bounds__(1024, 8) void ln_backward_wide_kernel(Bwd<float> p)
+{
+    __shared__ float slots[2][32];
+    int flip = 0;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, flip ^= 1) {
+        const float mu = p.mean[row], rs = p.rstd[row];
+        // eight columns: dy gamma and the normalised input
+        const auto load = [&](int col, float (&g)[8], float (&h)[8]) {
+            const int left = p.H - col;
+            float w[8];
+            if (KEPT)
+                load_codes(p.q.codes + row * p.q.ldc + col, left, p.q.scales[row * p.q.lds + col / kGroup], h);
+            else
+                load8(p.x + row * p.ldx + col, left, h);
+            load8(p.dy + row * p.lddy + col, left, g);
+            if (p.gamma)
+                load8(p.gamma + col, left, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                h[i] = (h[i] - mu) * rs;
+                g[i] = p.gamma ? g[i] * w[i] : g[i];
+            }
+        };
+        float s[2] = {0.f, 0.f};
+#pragma unroll 1
+        for (int col = threadIdx.x * 8; col < p.H; col += 8192) {
+            float g[8], h[8];
+            load(col, g, h);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s[0] += g[i];
+                s[1] += g[i] * h[i];   // past the end of the row g = 0
+            }
+        }
+        row_sum<1024>(s, slots[flip]);
+        const float m1 = s[0] / p.H, m2 = s[1] / p.H;
+#pragma unroll 1
+        for (int col = threadIdx.x * 8; col < p.H; col += 8192) {
+            const int left = p.H - col;
+            float g[8], h[8], o[8];
+            load(col, g, h);
+            if (p.add)
+                load8(p.add + row * p.ldadd + col, left, o);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = rs * (g[i] - m1 - h[i] * m2);
+                o[i] = p.add ? d + o[i] : d;
+            }
+            store8(p.dx + row * p.lddx + col, left, o);
+        }
+    }
+}
+
 // The column sums of wide rows: 512 columns and one slice of the rows a
 // workgroup, whose four waves take every fourth row and meet in LDS in order.
 template <typename T, bool KEPT>
@@ -430,31 +487,31 @@ inline Shape forward_shape(int H)
         return {1024, 2};
     return {1024, 4};
 }
-inline Shape backward_shape(int H)
+inline Shape backward_shape(int H, bool f32)
 {
     if (H <= 512)
         return {64, 1};
     if (H <= 1024)
         return {64, 2};
     if (H <= 2048)
-        return {64, 4};
+        return f32 ? Shape{256, 1} : Shape{64, 4};
     if (H <= 4096)
         return {256, 2};
     if (H <= 8192)
-        return {256, 4};
+        return f32 ? Shape{512, 2} : Shape{256, 4};
     return {512, 4};
 }
 
 // Rows past this go without sums in the pass for dx.
-constexpr int kSumsH = 16384;
+inline int sums_most(bool f32) { return f32 ? 8192 : 16384; }
 
 // Workgroups of the backward pass, which is also its number of partials; for
 // wide rows the slices of the sums' own pass, of at least 32 rows.
-inline int bwd_groups(int64_t rows, int H)
+inline int bwd_groups(int64_t rows, int H, bool f32)
 {
-    if (H > kSumsH)
+    if (H > sums_most(f32))
         return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(rows / 32, 1024 / ((H + 511) / 512))));
-    const int rpb = backward_shape(H).nt == 64 ? 4 : 1;
+    const int rpb = backward_shape(H, f32).nt == 64 ? 4 : 1;
     return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((rows + rpb - 1) / rpb, 512)));
 }
 
@@ -499,28 +556,38 @@ int run_forward(const Fwd<T> &p, hipStream_t st)
 template <typename T, bool KEPT>
 int run_backward(const Bwd<T> &p, int groups, hipStream_t st)
 {
-    if (p.H > kSumsH) {
+    constexpr bool f32 = sizeof(T) == 4;
+    if (p.H > sums_most(f32)) {
         if (p.part) {
             const int per = static_cast<int>((p.rows + groups - 1) / groups);
             ACSC_LAUNCH("ln_sums", (ln_sums_kernel<T, KEPT>), dim3((p.H + 511) / 512, groups), dim3(256), 0, st, p, per);
         }
         // after the sums, which read dy: dx may take its place
-        if (p.rows)
-            ACSC_LAUNCH("ln_backward", (ln_backward_kernel<T, 1024, 4, KEPT, false>),
-                        dim3(static_cast<unsigned>(std::min<int64_t>(p.rows, 1 << 20))), dim3(1024), 0, st, p);
+        const dim3 grid(static_cast<unsigned>(std::min<int64_t>(p.rows, 1 << 20)));
+        if (p.rows) {
+            if constexpr (f32)
+                ACSC_LAUNCH("ln_backward", (ln_backward_wide_kernel<KEPT>), grid, dim3(1024), 0, st, p);
+            else
+                ACSC_LAUNCH("ln_backward", (ln_backward_kernel<T, 1024, 4, KEPT, false>), grid, dim3(1024), 0, st, p);
+        }
         return check_launch("ln_backward");
     }
-    const Shape s = backward_shape(p.H);
+    const Shape s = backward_shape(p.H, f32);
     const dim3 grid(groups);
 #define ACSC_CASE(NT, CH)                                                                                       \
     if (s.nt == NT && s.ch == CH)                                                                             \
         ACSC_LAUNCH("ln_backward", (ln_backward_kernel<T, NT, CH, KEPT, true>), grid, dim3(NT < 256 ? 256 : NT), 0, st, p);
     ACSC_CASE(64, 1)
     ACSC_CASE(64, 2)
-    ACSC_CASE(64, 4)
     ACSC_CASE(256, 2)
-    ACSC_CASE(256, 4)
-    ACSC_CASE(512, 4)
+    if constexpr (f32) {
+        ACSC_CASE(256, 1)
+        ACSC_CASE(512, 2)
+    } else {
+        ACSC_CASE(64, 4)
+        ACSC_CASE(256, 4)
+        ACSC_CASE(512, 4)
+    }
 #undef ACSC_CASE
     return check_launch("ln_backward");
 }
@@ -608,7 +675,7 @@ extern "C" int ln_workspace_size(int64_t rows, int H, size_t *bytes)
     if (int rc = check_common(rows, H, ACSC_F32))
         return rc;
     ACSC_CHECK_ARG(bytes, ACSC_EINVAL, "null pointer bytes");
-    *bytes = static_cast<size_t>(bwd_groups(rows, H)) * 2 * H * sizeof(float);
+    *bytes = static_cast<size_t>(std::max(bwd_groups(rows, H, false), bwd_groups(rows, H, true))) * 2 * H * sizeof(float);
     return ACSC_OK;
 }
 
@@ -641,7 +708,7 @@ extern "C" int ln_backward(const void *dy, int64_t ld_dy, const void *x, int64_t
                    "an fp32 array is not 4-byte aligned");
     ACSC_CHECK_ARG(aligned(gamma, dtype_size(dt)), ACSC_EALIGN, "gamma not aligned to its elements");
     const bool sums = dgamma || dbeta;
-    const int groups = bwd_groups(rows, H);
+    const int groups = bwd_groups(rows, H, dt == ACSC_F32);
     if (sums) {
         ACSC_CHECK_ARG(ws, ACSC_EINVAL, "null workspace");
         ACSC_CHECK_ARG(aligned(ws, 256), ACSC_EALIGN, "workspace not 256-byte aligned");
