@@ -339,7 +339,8 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void ln_bac
 
 // dx of fp32 rows past 8192 columns, which with their sums leave no registers
 // either: a workgroup reads a row for its two sums and again, from the caches,
-// for dx, with the column sums taken by ln_sums_kernel (PENDINGW).
+// for dx, with the column sums taken by ln_sums_kernel (8192 x 28672: 1185 us;
+// held in registers, 1024 threads, with 300 bytes a lane of them spilled: 2540).
 template <bool KEPT>
 __global__ __launch_bounds__(1024, 8) void ln_backward_wide_kernel(Bwd<float> p)
 {
@@ -464,14 +465,16 @@ __global__ __launch_bounds__(64 * kSlices) void ln_join_kernel(const float *part
 }
 
 // Threads and chunks for a row of H columns.  Forward: two chunks a thread
-// where a workgroup can hold them (16384 x 8192, us: four chunks of 256
+// where a workgroup can hold them (16384 x 8192 bf16, us: four chunks of 256
 // threads 140, two of 512 112, one of 1024 120; 16384 x 2048 with its
-// checkpoint: four of a wave 44, one of 256 threads 38).  Backward: four,
-// which need fewer workgroups' partials.
+// checkpoint: four of a wave 44, one of 256 threads 38), and of fp32, twice the
+// bytes, one (16384 x 8192: two of 512 331, one of 1024 267).  Backward: four,
+// which need fewer workgroups' partials, and of fp32 two, which is what its
+// registers hold (16384 x 2048: four of a wave 235, one of 256 threads 79).
 struct Shape {
     int nt, ch;
 };
-inline Shape forward_shape(int H)
+inline Shape forward_shape(int H, bool f32)
 {
     if (H <= 512)
         return {64, 1};
@@ -480,9 +483,9 @@ inline Shape forward_shape(int H)
     if (H <= 2048)
         return {256, 1};
     if (H <= 4096)
-        return {256, 2};
+        return f32 ? Shape{512, 1} : Shape{256, 2};
     if (H <= 8192)
-        return {512, 2};
+        return f32 ? Shape{1024, 1} : Shape{512, 2};
     if (H <= 16384)
         return {1024, 2};
     return {1024, 4};
@@ -535,7 +538,7 @@ inline int check_mat(const void *p, int64_t rows, int64_t ld, int H, int dt, con
 template <typename T, bool AGAIN>
 int run_forward(const Fwd<T> &p, hipStream_t st)
 {
-    const Shape s = forward_shape(p.H);
+    const Shape s = forward_shape(p.H, sizeof(T) == 4);
     const int64_t blocks = s.nt == 64 ? (p.rows + 3) / 4 : p.rows;
     const dim3 grid(static_cast<unsigned>(blocks));
     const char *tag = AGAIN ? "ln_recompute" : "ln_forward";
@@ -547,6 +550,8 @@ int run_forward(const Fwd<T> &p, hipStream_t st)
     ACSC_CASE(256, 1)
     ACSC_CASE(256, 2)
     ACSC_CASE(512, 2)
+    ACSC_CASE(512, 1)
+    ACSC_CASE(1024, 1)
     ACSC_CASE(1024, 2)
     ACSC_CASE(1024, 4)
 #undef ACSC_CASE
