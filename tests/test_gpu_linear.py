@@ -101,6 +101,37 @@ def test_forward(pk, dtype, rows, n_in, n_out, act, full, pad):
     within(q.codes.double() * step, z, step * (0.5 + 127 * 8 * U) + ez)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [7, 10, 16, 17, 32, 33, 50, 64, 65, 97, 130])
+@pytest.mark.parametrize("n_in,n_out,pad", [(4104, 1160, 0), (1160, 4104, 8), (2053, 771, 3)])
+def test_few_rows(pk, dtype, rows, n_in, n_out, pad):
+    """The forward product and the input gradient of few tokens on wide layers: narrow tiles, whole and cut, one and
+    several of them, their last rows and columns part full; operands of odd strides copied or read where they are."""
+    s = rows + n_in
+    x = randn(rows, n_in, dtype=dtype, seed=s, pad=pad)
+    W = randn(n_out, n_in, dtype=dtype, seed=s + 1, scale=1 / math.sqrt(n_in), pad=pad)
+    b, r = randn(n_out, dtype=dtype, seed=s + 2), randn(rows, n_out, dtype=dtype, seed=s + 3, pad=pad)
+    z, ez = product(x, W.t(), n_in)
+    z, ez = z + b.double(), ez + 2 * U * b.double().abs()
+    a, _ = act_pair(z, "silu")
+    y = a + r.double()
+    got, q = pk.lin_forward(x, W, b, "silu", r, keep="q8")
+    within(got, y, (1.13 * ez + 4 * U * z.abs() + 2 * U * (a.abs() + y.abs())) * (1 + 2.0 ** -8) + store(dtype, y))
+    step = q.scales.double().repeat_interleave(GROUP, 1)[:, :n_out]
+    within(q.codes.double() * step, z, step * (0.5 + 127 * 8 * U) + ez)
+    for again in (pk.lin_forward(x, W, b, "silu", r), pk.lin_forward(x, W, b, "silu", r, keep="z")):
+        assert torch.equal(again[0], got)
+    within(again[1], z, ez * (1 + 2.0 ** -8) + store(dtype, z))
+    dz, kept = randn(rows, n_out, dtype=dtype, seed=s + 4, pad=pad), randn(rows, n_in, dtype=dtype, seed=s + 5, pad=pad)
+    p, ep = product(dz, W, n_out)
+    within(pk.lin_backward_input(dz, W), p, ep * (1 + 2.0 ** -8) + store(dtype, p))
+    code = pk.q8_encode(kept)
+    for src, v in ((kept, kept.double()), (code, pk.q8_decode(code, F32).double())):
+        want = p * act_pair(v, "silu")[1]
+        tol = ep * 1.13 + 8 * U * p.abs() + 2 * U * want.abs()
+        within(pk.lin_backward_input(dz, W, "silu", src), want, tol * (1 + 2.0 ** -8) + store(dtype, want))
+
+
 @pytest.mark.parametrize("kept", ["z", "q8"])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows,n_in,n_out", SHAPES)
