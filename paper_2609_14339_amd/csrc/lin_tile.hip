@@ -4,20 +4,34 @@
 // A workgroup takes a TM x T tile of C in steps of 128 bytes along the sum (64
 // bf16, 32 fp32): 256 x 256 (bf16 only) by eight waves of 64 rows and 128
 // columns, 128 x 128 by four of 32 rows, and, for the few rows of a forward
-// product or an input gradient, 64 x 128 by four of 16 and 32 x 128 by two.  Each step's tiles of A and B come straight from
-// memory into LDS (global_load_lds_dwordx4), into two stages in turn; no
-// register holds them on the way.  An operand stays in LDS as it is stored:
-// lines of one index's step (row) or k-lines of 128 bytes of its own indices
-// (col), their eight 16-byte chunks XOR-swizzled by the line.  Fragments are
-// 16-byte reads of row operands; of col ones pairs of transposing 8-byte reads
-// (bf16) or four 4-byte reads (fp32); so all three products of a layer run at
-// the stored layouts.  The matrix instruction's first operand is B's side: a
-// lane then holds four consecutive columns of a row.
+// product or an input gradient, 64 x 128 by four of 16 and 32 x 128 by two.
+// Each step's tiles of A and B come straight from memory into LDS
+// (global_load_lds_dwordx4); no register holds them on the way.  An operand
+// stays in LDS as it is stored: lines of one index's step (row) or k-lines of
+// 128 bytes of its own indices (col), their eight 16-byte chunks XOR-swizzled
+// by the line.  Fragments are 16-byte reads of row operands; of col ones pairs
+// of transposing 8-byte reads (bf16) or four 4-byte reads (fp32); so all three
+// products of a layer run at the stored layouts.  The matrix instruction's
+// first operand is B's side: a lane then holds four consecutive columns of a
+// row.
 //
-// Half a step of fragments is read ahead: while the first half of a step is
-// multiplied the second is read; then the wave waits for its part of the next
-// step's DMA, meets the others, sends the DMA after that into the stage just
-// read, and multiplies the second half while the next step's first is read.
+// Half a step of fragments is read ahead.  While the first half of a step is
+// multiplied the second is read, and A of two steps on leaves for the third of
+// its stages; then the wave waits for what it sent of the next step, meets the
+// others, sends B of two steps on into the stage just read, and multiplies the
+// second half while the next step's first is read.  So the DMA, which bounds
+// the kernel, is under way all the time: with two stages of both operands,
+// all of it behind the meeting, 8192 x 28672 -> 8192 forward took 2850 us and
+// 2720 so.  (Four waves of 128 x 128 keep 256 accumulators a lane, which the
+// compiler moves between register files all the time; steps of half the length
+// in rings of three to five stages read lines of 64 bytes and lose 8%.)
+//
+// Measured, bf16 TFLOP/s, forward / input gradient / weight gradient: 8192 x
+// 28672 -> 8192 1415 / 1406 / 1390, 8192 x 8192 -> 8192 1456 / 1400 / 1400,
+// 16384 x 2048 -> 8192 1308 / 1342 / 1376; fp32 4096^3 127 / 134 / 134 of 157
+// that the matrix cores have at 2.4 GHz.  What bounds it: at 8192 x 28672 ->
+// 8192 the products alone, from registers, run at 2260 (the clock is near 1.7
+// GHz by then), with their LDS reads at 1750, the DMA alone at 1450.
 #include "lin.h"
 
 #include <type_traits>
@@ -229,6 +243,10 @@ struct Frag<float, COL> {
 constexpr int fragments(int TM) { return TM < 64 ? 1 : TM / 64; }
 constexpr int waves(int TM, int T) { return TM / (16 * fragments(TM)) * (T / 128); }
 
+// Stages of A: a third one where it fits beside the other workgroup (see the
+// step below); B has two.
+constexpr int a_stages(int TM) { return TM < 128 ? 2 : 3; }
+
 template <typename E, int TM, int T, bool ACOL, bool BCOL, int KIND, typename TO>
 __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_kernel(Gemm g)
 {
@@ -237,8 +255,9 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
     constexpr int kBK = 128 / sizeof(E);
     constexpr int WN = T / 128;                 // waves along the columns
     constexpr int FA = fragments(TM);
-    constexpr int OP = TM * 128;                // bytes of A's part of a stage
-    constexpr int STAGE = OP + T * 128;
+    constexpr int OPA = TM * 128, OPB = T * 128;   // bytes of a step's A and B
+    constexpr int AS = a_stages(TM);
+    constexpr int B0 = AS * OPA;                // B's stages follow A's
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
@@ -281,27 +300,28 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
     frb.init(0);
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte *)smem));
 
-    constexpr int NI = NB / FA, NR = (8 + FA) / FA;   // DMA of a side, and fragments, beside eight products
-    const auto to_a = [&](int s, int i) { return lds0 + (s & 1) * STAGE + (wave * NA + i) * 1024; };
-    const auto to_b = [&](int s, int i) { return lds0 + (s & 1) * STAGE + OP + (wave * NB + i) * 1024; };
-    // instruction i of step s, which is whole
-    const auto issue = [&](int s, int i) {
-        if (i < NA)
-            dma16(sa.base + s * sa.step, sa.off[i < NA ? i : 0], to_a(s, i), sb.base + s * sb.step, sb.off[i], to_b(s, i));
-        else
-            dma16(sb.base + s * sb.step, sb.off[i], to_b(s, i));
+    constexpr int NR = (8 + FA) / FA;           // fragments read beside eight products
+    // instruction i of step s, which is whole, into stage `at`
+    const auto issue_a = [&](int s, int at, int i) {
+        dma16(sa.base + s * sa.step, sa.off[i], lds0 + at * OPA + (wave * NA + i) * 1024);
+    };
+    const auto issue_b = [&](int s, int i) {
+        dma16(sb.base + s * sb.step, sb.off[i], lds0 + B0 + (s & 1) * OPB + (wave * NB + i) * 1024);
     };
     // the same of any step
-    const auto issue_any = [&](int s, int i) {
+    const auto any_a = [&](int s, int at, int i) {
         const int left = kend - kbeg - s * kBK;
-        if (left >= kBK) {
-            issue(s, i);
-        } else if (left > 0) {
-            if (i < NA)
-                dma16(sa.tail(i < NA ? i : 0, s, left, wave), to_a(s, i), sb.tail(i, s, left, wave), to_b(s, i));
-            else
-                dma16(sb.tail(i, s, left, wave), to_b(s, i));
-        }
+        if (left >= kBK)
+            issue_a(s, at, i);
+        else if (left > 0)
+            dma16(sa.tail(i, s, left, wave), lds0 + at * OPA + (wave * NA + i) * 1024);
+    };
+    const auto any_b = [&](int s, int i) {
+        const int left = kend - kbeg - s * kBK;
+        if (left >= kBK)
+            issue_b(s, i);
+        else if (left > 0)
+            dma16(sb.tail(i, s, left, wave), lds0 + B0 + (s & 1) * OPB + (wave * NB + i) * 1024);
     };
     f32x4 acc[FA][8];
 #pragma unroll
@@ -313,12 +333,11 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
     struct Frags {
         typename FragA::Value f[8 + FA];
     };
-    const auto read = [&](Frags &f, int stage, int kh, int r) {
-        const unsigned char *base = smem + stage * STAGE;
+    const auto read = [&](Frags &f, int s, int at, int kh, int r) {
         if (r < 8)
-            f.f[r] = frb.read(base + OP + wn * 16384, r, kh);
+            f.f[r] = frb.read(smem + B0 + (s & 1) * OPB + wn * 16384, r, kh);
         else
-            f.f[r] = fra.read(base + (ACOL ? wm * FA / BA * (BA * 2048) : wm * FA * 2048), r - 8, kh);
+            f.f[r] = fra.read(smem + at * OPA + (ACOL ? wm * FA / BA * (BA * 2048) : wm * FA * 2048), r - 8, kh);
     };
     // eight products at a time, with what goes out beside them
     const auto multiply = [&](const Frags &f, int a) {
@@ -326,56 +345,84 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
         for (int j = 0; j < 8; ++j)
             acc[a][j] = FragA::multiply(f.f[j], f.f[8 + a], acc[a][j]);
     };
-    const auto meet = [&]() {
-        // this wave's DMA has landed and its LDS reads are done; then everyone's
+    // this wave's DMA has landed, but for the newest `ahead`, and its LDS reads
+    // are done; then everyone's
+    const auto meet = [&](auto ahead) {
         __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(ahead.value) : "memory");
     };
+    typedef std::integral_constant<int, 0> All;
+    typedef std::integral_constant<int, AS == 3 ? NA : 0> ButA;
     Frags f0, f1;
+    int at = 0;                                 // A's stage of the step at hand
     const auto step = [&](int s, auto whole) {
+        const int at1 = at + 1 == AS ? 0 : at + 1, at2 = at1 + 1 == AS ? 0 : at1 + 1;
 #pragma unroll
         for (int a = 0; a < FA; ++a) {
             __builtin_amdgcn_sched_barrier(0);
+            if (AS == 3)
+#pragma unroll
+                for (int i = 0; i < NA / FA; ++i)
+                    if (whole)
+                        issue_a(s + 2, at2, a * (NA / FA) + i);
+                    else
+                        any_a(s + 2, at2, a * (NA / FA) + i);
 #pragma unroll
             for (int r = 0; r < NR; ++r)
-                read(f1, s & 1, 1, a * NR + r);
+                read(f1, s, at, 1, a * NR + r);
             multiply(f0, a);
         }
-        meet();
+        if (whole)
+            meet(ButA{});
+        else
+            meet(All{});
 #pragma unroll
         for (int a = 0; a < FA; ++a) {
             __builtin_amdgcn_sched_barrier(0);
+            if (AS == 2)
 #pragma unroll
-            for (int i = 0; i < NI; ++i)
+                for (int i = 0; i < NA / FA; ++i)
+                    if (whole)
+                        issue_a(s + 2, at2, a * (NA / FA) + i);
+                    else
+                        any_a(s + 2, at2, a * (NA / FA) + i);
+#pragma unroll
+            for (int i = 0; i < NB / FA; ++i)
                 if (whole)
-                    issue(s + 2, a * NI + i);
+                    issue_b(s + 2, a * (NB / FA) + i);
                 else
-                    issue_any(s + 2, a * NI + i);
-            // past the last step this reads the other stage, unused
+                    any_b(s + 2, a * (NB / FA) + i);
+            // past the last step this reads another stage, unused
 #pragma unroll
             for (int r = 0; r < NR; ++r)
-                read(f0, (s + 1) & 1, 0, a * NR + r);
+                read(f0, s + 1, at1, 0, a * NR + r);
             multiply(f1, a);
         }
+        at = at1;
     };
 
+    for (int s = 0; s < 2; ++s) {
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
-        issue_any(0, i);
-    meet();
+        for (int i = 0; i < NA; ++i)
+            any_a(s, s, i);
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
-        issue_any(1, i);
+        for (int i = 0; i < NB; ++i)
+            any_b(s, i);
+    }
+    const int whole = (kend - kbeg) / kBK;
+    if (whole >= 2)
+        meet(std::integral_constant<int, NA + NB>{});
+    else
+        meet(All{});
 #pragma unroll
     for (int r = 0; r < 8 + FA; ++r)
-        read(f0, 0, 0, r);
-    const int whole = (kend - kbeg) / kBK;
+        read(f0, 0, 0, 0, r);
     int s = 0;
     for (; s + 2 < whole; ++s)
         step(s, std::true_type{});
     for (; s < nsteps; ++s)
         step(s, std::false_type{});
-    meet();
+    meet(All{});
     if (tile_n == 0 && split <= 0)
         put_db<KIND>(g, m0, TM);
     if (part)
@@ -391,7 +438,7 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
 template <typename E, int TM, int T, bool ACOL, bool BCOL, int KIND, typename TO>
 int launch(const Gemm &g, hipStream_t st, const char *tag)
 {
-    constexpr size_t bytes = 2 * (TM + T) * 128;
+    constexpr size_t bytes = (a_stages(TM) * TM + 2 * T) * 128;
     if (int rc = allow_lds(lin_tile_kernel<E, TM, T, ACOL, BCOL, KIND, TO>, bytes))
         return rc;
     ACSC_LAUNCH(tag, (lin_tile_kernel<E, TM, T, ACOL, BCOL, KIND, TO>),
