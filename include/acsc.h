@@ -578,8 +578,8 @@ int lin_backward_input(const void *dz, int64_t ld_dz, acsc_dtype dt, int64_t row
  *   dW (+)= dz^T act(x),   db (+)= sum over rows of dz
  * x        device [rows, ld_x] of dt, or its checkpoint q (exactly one).  With
  *          act != ACSC_ACT_NONE it holds the kept pre-activation of the layer
- *          before; its activation is recomputed inside the call and rounded to
- *          dt, as that layer's output was.
+ *          before; its activation is recomputed inside the call and, for more
+ *          than eight rows, rounded to dt, as that layer's output was.
  * dW       device [n_out, ld_dw] of dw_dt (the gradient's type: bf16 goes to
  *          sc_correct as it is, fp32 serves accumulation).
  * db       device fp32 [n_out] or NULL.

@@ -31,7 +31,8 @@
 // 16384 x 2048 -> 8192 1308 / 1342 / 1376; fp32 4096^3 127 / 134 / 134 of 157
 // that the matrix cores have at 2.4 GHz.  What bounds it: at 8192 x 28672 ->
 // 8192 the products alone, from registers, run at 2260 (the clock is near 1.7
-// GHz by then), with their LDS reads at 1750, the DMA alone at 1450.
+// GHz by then), with their LDS reads at 1750, the DMA alone, two
+// stages deep, at 1450.
 #include "lin.h"
 
 #include <type_traits>
