@@ -35,6 +35,7 @@
 // stages deep, at 1450.
 #include "lin.h"
 
+#include <atomic>
 #include <type_traits>
 
 namespace acsc {
@@ -440,8 +441,17 @@ template <typename E, int TM, int T, bool ACOL, bool BCOL, int KIND, typename TO
 int launch(const Gemm &g, hipStream_t st, const char *tag)
 {
     constexpr size_t bytes = (a_stages(TM) * TM + 2 * T) * 128;
-    if (int rc = allow_lds(lin_tile_kernel<E, TM, T, ACOL, BCOL, KIND, TO>, bytes))
-        return rc;
+    // once a device: asked for on every call it costs the host more than the launch
+    static std::atomic<uint64_t> allowed{0};
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess)
+        return set_error(ACSC_EHIP, "cannot query the device");
+    if (dev > 63 || !(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
+        if (int rc = allow_lds(lin_tile_kernel<E, TM, T, ACOL, BCOL, KIND, TO>, bytes))
+            return rc;
+        if (dev < 64)
+            allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
     ACSC_LAUNCH(tag, (lin_tile_kernel<E, TM, T, ACOL, BCOL, KIND, TO>),
                 dim3(g.whole + (g.tm * g.tn - g.whole) * g.splits), dim3(64 * waves(TM, T)), bytes, st, g);
     return check_launch(tag);
