@@ -535,9 +535,9 @@ typedef enum lin_op { LIN_FORWARD = 0, LIN_BACKWARD_INPUT = 1, LIN_BACKWARD_WEIG
 
 /* Bytes of workspace for one product of a linear layer with n_in inputs and
  * n_out outputs on `rows` tokens, whatever its epilogue.  For operands (x, W,
- * dz) that are 16-byte aligned with row strides of multiples of eight
- * elements; lin_workspace_size_unaligned covers every alignment and stride
- * (such operands are copied into the workspace first). */
+ * dz) that are 4-byte aligned with row strides under 2^21 elements, in bf16
+ * even ones; lin_workspace_size_unaligned covers every alignment and stride
+ * (other operands are copied into the workspace first). */
 int lin_workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, size_t *bytes);
 int lin_workspace_size_unaligned(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, size_t *bytes);
 

@@ -831,7 +831,7 @@ def ln_backward(dy: torch.Tensor, src: Union[torch.Tensor, Q8], mean: torch.Tens
 
 def lin_workspace_size(op: int, rows: int, n_in: int, n_out: int, dtype: torch.dtype) -> int:
     """Bytes for one product (LIN_FORWARD, LIN_BACKWARD_INPUT, LIN_BACKWARD_WEIGHT) of a linear layer whose
-    operands are 16-byte aligned with row strides of multiples of eight elements."""
+    operands have row strides under 2^21 and, in bf16, are 4-byte aligned with even strides."""
     b = C.c_size_t(0)
     code = BF16 if dtype == torch.bfloat16 else F32
     _check(lib.lin_workspace_size(op, rows, n_in, n_out, code, C.byref(b)))
@@ -851,9 +851,9 @@ def _lin_ws(op: int, rows: int, n_in: int, n_out: int, a, lda: int, b, ldb: int,
     be None), unless one is given."""
     if ws is not None:
         return _ws(0, ws, a.device, stream)
-    aligned = not ((lda | a.data_ptr() >> 1) & 7) and lda < 1 << 22
-    if b is not None:
-        aligned = aligned and not ((ldb | b.data_ptr() >> 1) & 7) and ldb < 1 << 22
+    aligned = lda < 1 << 21 and (b is None or ldb < 1 << 21)
+    if aligned and a.dtype is torch.bfloat16:
+        aligned = not ((lda | a.data_ptr() >> 1) & 1) and (b is None or not ((ldb | b.data_ptr() >> 1) & 1))
     return _ws(_lin_bytes(aligned, op, rows, n_in, n_out, a.dtype), None, a.device, stream)
 
 

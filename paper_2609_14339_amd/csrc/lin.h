@@ -43,6 +43,7 @@ struct Gemm {
     int whole;        // tiles that are not cut along K; the rest is cut into
     int splits;       // pieces of kchunk each
     int kchunk;
+    bool words_a, words_b;   // operands whose k (row) or indices (col) end inside a 16-byte chunk, not copied
     float *part;      // the pieces: of tiles [splits][tiles - whole][T][T]; of few tokens [splits][M][ldp], nullptr:
     int64_t ldp;      // one piece, through the epilogue
     const float *dbpart;   // weight gradient: slices of column sums of dz, [slices][M], that the product's first

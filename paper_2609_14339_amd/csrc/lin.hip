@@ -12,16 +12,16 @@ int lin_tile_run(const Gemm &g, int tile_rows, EpiKind kind, acsc_dtype dt, acsc
 namespace {
 
 // Tokens up to which a product does without tiles.  Forward: W is read once
-// and unstaged; 4096 -> 14336, 1 / 8 / 16 / 32 tokens, us: bf16 24, 28, 35, 48
-// against 31 by tiles for 4 to 64; fp32 53, 60, 68, 103 against 56.  Where the
-// tile kernel cannot read W it has to be copied first, three times its bytes:
-// there the kernel is used as far as it goes.  Weight gradient: outer products
-// of unrounded activations; bf16 8192 -> 8192, 1 / 4 / 8 tokens: 25.6, 30.0,
-// 38.8 against 43 by tiles.  (The input gradient by vector FMAs on rows of W
-// read once took 39 against 31 by tiles.)
-inline int few_tokens(EpiKind kind, bool bf16, bool fits_b)
+// and unstaged; 4096 -> 14336, 1 / 8 / 16 tokens, us: bf16 24, 28, 35 against 31
+// by tiles for 4 to 64; fp32 53, 60, 68 against 56.  Where the tile kernel
+// cannot read W it has to be copied first, three times its bytes: there the
+// kernel is used as far as it goes.  Weight gradient: outer products of
+// unrounded activations; bf16 8192 -> 8192, 1 / 4 / 8 tokens: 25.6, 30.0, 38.8
+// against 43 by tiles.  (The input gradient by vector FMAs on rows of W read
+// once took 39 against 31 by tiles.)
+inline int few_tokens(EpiKind kind, bool fits_b)
 {
-    return kind == kForward ? (fits_b ? 8 : bf16 ? 16 : 32) : kind == kWeight ? 8 : 0;
+    return kind == kForward ? (fits_b ? 8 : 16) : kind == kWeight ? 8 : 0;
 }
 
 // Adds the pieces of a cut product in order and takes the sum through the
@@ -219,12 +219,17 @@ inline Shape shape_of(EpiKind kind, int64_t rows, int n_in, int n_out)
     return {n_out, n_in, static_cast<int>(rows), true, true};
 }
 
-// Whether the tile kernel reads an operand where it is: rows of whole 16-byte
-// chunks, offsets within a tile and step of under 2^31 bytes.
+// Whether the tile kernel reads an operand where it is: rows at multiples of
+// the word that the DMA reads, rows of whole words, of a chunk at least if a
+// col operand's last chunk runs on into the next row, and offsets within a
+// tile and step of under 2^31 bytes.  Both sides, bf16 rows at odd words
+// copied first or read there, us: 20 x 4098 -> 14338 67 and 29, 8190 x 8190 ->
+// 8190 907 and 890, its input gradient 899 and 813.
 inline bool readable(const Operand &o, bool col, int64_t inner, acsc_dtype dt)
 {
-    const int es = static_cast<int>(dtype_size(dt)), chunk = 16 / es;
-    return aligned(o.p, 16) && o.ld % chunk == 0 && inner % chunk == 0 && o.ld * es * (col ? 64 : 256) < (1ll << 31);
+    const int es = static_cast<int>(dtype_size(dt)), chunk = 16 / es, unit = 4 / es;
+    return aligned(o.p, unit * es) && o.ld % unit == 0 && inner * es % 4 == 0 && (!col || inner % chunk == 0 || o.ld >= chunk) &&
+           o.ld * es * (col ? 64 : 256) < (1ll << 31);
 }
 
 // Tile and pieces of the sum, by the least estimated time.  A round is what
@@ -293,12 +298,12 @@ inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bo
     const bool bf16 = dt == ACSC_BF16;
     const int bk = 128 / static_cast<int>(dtype_size(dt));
     const int steps = (s.K + bk - 1) / bk;
-    if (kind == kWeight && s.K <= few_tokens(kind, bf16, fits_b)) {
+    if (kind == kWeight && s.K <= few_tokens(kind, fits_b)) {
         p.few = true;
         p.splits = 1;
         return p;
     }
-    if (kind == kForward && s.M <= few_tokens(kind, bf16, fits_b)) {
+    if (kind == kForward && s.M <= few_tokens(kind, fits_b)) {
         // 16 outputs a workgroup: a cut only where they fill half the CUs at
         // most, at two rounds of eight lines a piece
         const int groups = (s.N + 15) / 16, round = 8 * 128 / static_cast<int>(dtype_size(dt)), rounds = (s.K + round - 1) / round;
@@ -394,6 +399,9 @@ int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype
     g.kchunk = p.kchunk;
     g.ldp = p.ldp;
     g.whole = p.whole;
+    const int chunk = 16 / static_cast<int>(dtype_size(dt));
+    g.words_a = !p.pack_a && (s.acol ? s.M : s.K) % chunk;
+    g.words_b = !p.pack_b && !again && (s.bcol ? s.N : s.K) % chunk;
     // the product for few tokens: a piece goes through memory if there are
     // more, or if its workgroups hold no whole checkpoint groups
     const bool pieces = p.splits > 1 || (p.few && g.e.q.codes);
@@ -536,14 +544,16 @@ static int workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dty
         return ACSC_OK;
     const EpiKind kind = op == LIN_FORWARD ? kForward : op == LIN_BACKWARD_INPUT ? kGate : kWeight;
     const Shape s = shape_of(kind, rows, n_in, n_out);
-    const Operand best{nullptr, 8};
-    const bool a = readable(best, s.acol, s.acol ? s.M : s.K, dt);
-    const bool b = readable(best, s.bcol, s.bcol ? s.N : s.K, dt);
+    // the strides that the size is good for: all from the rows' own length on, of whole words
+    const auto best = [&](bool col, int64_t inner) {
+        return readable(Operand{nullptr, dt == ACSC_F32 ? inner : (inner + 1) / 2 * 2}, col, inner, dt);
+    };
+    const bool a = best(s.acol, s.acol ? s.M : s.K), b = best(s.bcol, s.bcol ? s.N : s.K);
     // with any alignment: the most that either operand's copy, or its absence, takes
     *bytes = plan_of(kind, s, dt, a, b).bytes();
     for (int copies = 1; any && copies < 4; ++copies)
         *bytes = std::max(*bytes, plan_of(kind, s, dt, a && !(copies & 1), b && !(copies & 2)).bytes());
-    if (kind == kWeight && rows > few_tokens(kind, dt == ACSC_BF16, true))
+    if (kind == kWeight && rows > few_tokens(kind, true))
         *bytes += recomputed_bytes(rows, n_in, dt);
     return ACSC_OK;
 }
@@ -709,7 +719,7 @@ extern "C" int lin_backward_weight(const void *dz, int64_t ld_dz, const void *x,
     const Shape s = shape_of(kWeight, rows, n_in, n_out);
     Gemm g{};
     g.e = Epi{dW, ld_dw, nullptr, nullptr, 0, nullptr, 0, q8_of(nullptr), ACSC_ACT_NONE, accumulate};
-    if (rows <= few_tokens(kWeight, dt == ACSC_BF16, true)) {
+    if (rows <= few_tokens(kWeight, true)) {
         g.A = {dz, ld_dz};
         g.B = {x, ld_x};
         g.M = s.M;

@@ -1,5 +1,4 @@
-// A linear layer's forward product for few tokens (bf16 up to 8, fp32 up to
-// 32): the weights are read once, straight into the matrix cores' lanes, at
+// A linear layer's forward product for few tokens (up to 16): the weights are read once, straight into the matrix cores' lanes, at
 // whatever stride and alignment they have.
 //
 // What bounds it is the weights' bytes: no LDS, no barrier on the way.  A
@@ -56,28 +55,22 @@ __device__ __forceinline__ f32x4 multiply(const Any16 &w, const Any16 &x, f32x4 
     return acc;
 }
 
-template <typename T, int MT>
+template <typename T>
 __global__ __launch_bounds__(kWaves * 64) void lin_few_kernel(Gemm g)
 {
     constexpr int E = 16 / sizeof(T), LINE = 8 * E, U = 4;   // k of a chunk and of a line; lines in flight
-    __shared__ __align__(16) float meet[kWaves][MT * 16][16];
+    __shared__ __align__(16) float meet[kWaves][16][16];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int n0 = blockIdx.x * 16, split = blockIdx.y;
     const int kbeg = split * g.kchunk, kend = min(g.K, kbeg + g.kchunk);
     const int k = (lane >> 4) * E;
     const T *w = static_cast<const T *>(g.B.p) + min(n0 + (lane & 15), g.N - 1) * g.B.ld;
-    const T *x[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-        x[t] = static_cast<const T *>(g.A.p) + min<int64_t>(t * 16 + (lane & 15), g.M - 1) * g.A.ld;
-    f32x4 acc[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-        acc[t] = f32x4{0, 0, 0, 0};
+    const T *x = static_cast<const T *>(g.A.p) + min<int64_t>(lane & 15, g.M - 1) * g.A.ld;
+    f32x4 acc = {0, 0, 0, 0};
 
     int k0 = kbeg + wave * LINE;
     for (; k0 + ((U - 1) * kWaves + 1) * LINE <= kend; k0 += U * kWaves * LINE) {
-        Any16 a[U][2], b[U][2][MT];
+        Any16 a[U][2], b[U][2];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -89,34 +82,25 @@ __global__ __launch_bounds__(kWaves * 64) void lin_few_kernel(Gemm g)
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int t = 0; t < MT; ++t)
-                    b[u][h][t] = *reinterpret_cast<const Any16 *>(x[t] + k0 + u * kWaves * LINE + h * 4 * E + k);
+                b[u][h] = *reinterpret_cast<const Any16 *>(x + k0 + u * kWaves * LINE + h * 4 * E + k);
         __builtin_amdgcn_sched_barrier(0);   // all loads leave before the first product
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int t = 0; t < MT; ++t)
-                    acc[t] = multiply<T>(a[u][h], b[u][h][t], acc[t]);
+                acc = multiply<T>(a[u][h], b[u][h], acc);
     }
     for (; k0 < kend; k0 += kWaves * LINE)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int at = k0 + h * 4 * E + k;
-            const Any16 a = load16(w + at, kend - at);
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-                acc[t] = multiply<T>(a, load16(x[t] + at, kend - at), acc[t]);
+            acc = multiply<T>(load16(w + at, kend - at), load16(x + at, kend - at), acc);
         }
 
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-        *reinterpret_cast<f32x4 *>(&meet[wave][t * 16 + (lane & 15)][(lane >> 4) * 4]) = acc[t];
+    *reinterpret_cast<f32x4 *>(&meet[wave][lane & 15][(lane >> 4) * 4]) = acc;
     __syncthreads();
     const int m = threadIdx.x >> 1, c = (threadIdx.x & 1) * 8, n = n0 + c;
-    if (m >= MT * 16 || m >= g.M)
+    if (m >= 16 || m >= g.M)
         return;
     float v[8] = {};
     for (int i = 0; i < kWaves; ++i)
@@ -219,11 +203,9 @@ int lin_few_run(const Gemm &g, acsc_dtype dt, hipStream_t st, const char *tag)
 {
     const dim3 grid(static_cast<unsigned>((g.N + 15) / 16), g.splits);
     if (dt == ACSC_BF16)
-        ACSC_LAUNCH(tag, (lin_few_kernel<uint16_t, 1>), grid, dim3(kWaves * 64), 0, st, g);
-    else if (g.M <= 16)
-        ACSC_LAUNCH(tag, (lin_few_kernel<float, 1>), grid, dim3(kWaves * 64), 0, st, g);
+        ACSC_LAUNCH(tag, lin_few_kernel<uint16_t>, grid, dim3(kWaves * 64), 0, st, g);
     else
-        ACSC_LAUNCH(tag, (lin_few_kernel<float, 2>), grid, dim3(kWaves * 64), 0, st, g);
+        ACSC_LAUNCH(tag, lin_few_kernel<float>, grid, dim3(kWaves * 64), 0, st, g);
     return check_launch(tag);
 }
 

@@ -54,26 +54,10 @@ __device__ const uint4 g_zeros = {0, 0, 0, 0};
 // transposed 8-byte reads of four lines conflict.
 __device__ __forceinline__ int swz(int line) { return ((line >> 1) ^ line) & 7; }
 
-// The LDS DMA of one line group of A and one of B: 16 bytes a lane from base +
-// off (bytes) to lds + 16 lane.  lds is wave-uniform and goes through M0,
-// which needs a wait state after it is written; M0 is left as it was.
-__device__ __forceinline__ void dma16(const char *a, uint32_t aoff, uint32_t alds, const char *b, uint32_t boff,
-                                      uint32_t blds)
-{
-    uint32_t saved;
-    asm volatile("s_mov_b32 %0, m0\n\t"
-                 "s_mov_b32 m0, %3\n\t"
-                 "s_nop 0\n\t"
-                 "global_load_lds_dwordx4 %1, %2\n\t"
-                 "s_mov_b32 m0, %6\n\t"
-                 "s_nop 0\n\t"
-                 "global_load_lds_dwordx4 %4, %5\n\t"
-                 "s_mov_b32 m0, %0"
-                 : "=&s"(saved)
-                 : "v"(aoff), "s"(a), "s"(alds), "v"(boff), "s"(b), "s"(blds)
-                 : "memory");
-}
-__device__ __forceinline__ void dma16(const char *b, uint32_t boff, uint32_t blds)
+// LDS DMA of 16 bytes a lane from base + off (bytes) to lds + 16 lane, or of 4
+// bytes a lane from p to lds + 4 lane.  lds is wave-uniform and goes through
+// M0, which needs a wait state after it is written; M0 is left as it was.
+__device__ __forceinline__ void dma16(const char *base, uint32_t off, uint32_t lds)
 {
     uint32_t saved;
     asm volatile("s_mov_b32 %0, m0\n\t"
@@ -82,10 +66,10 @@ __device__ __forceinline__ void dma16(const char *b, uint32_t boff, uint32_t bld
                  "global_load_lds_dwordx4 %1, %2\n\t"
                  "s_mov_b32 m0, %0"
                  : "=&s"(saved)
-                 : "v"(boff), "s"(b), "s"(blds)
+                 : "v"(off), "s"(base), "s"(lds)
                  : "memory");
 }
-__device__ __forceinline__ void dma16(const void *b, uint32_t blds)
+__device__ __forceinline__ void dma16(const void *p, uint32_t lds)
 {
     uint32_t saved;
     asm volatile("s_mov_b32 %0, m0\n\t"
@@ -94,22 +78,19 @@ __device__ __forceinline__ void dma16(const void *b, uint32_t blds)
                  "global_load_lds_dwordx4 %1, off\n\t"
                  "s_mov_b32 m0, %0"
                  : "=&s"(saved)
-                 : "v"(b), "s"(blds)
+                 : "v"(p), "s"(lds)
                  : "memory");
 }
-__device__ __forceinline__ void dma16(const void *a, uint32_t alds, const void *b, uint32_t blds)
+__device__ __forceinline__ void dma4(const void *p, uint32_t lds)
 {
     uint32_t saved;
     asm volatile("s_mov_b32 %0, m0\n\t"
                  "s_mov_b32 m0, %2\n\t"
                  "s_nop 0\n\t"
-                 "global_load_lds_dwordx4 %1, off\n\t"
-                 "s_mov_b32 m0, %4\n\t"
-                 "s_nop 0\n\t"
-                 "global_load_lds_dwordx4 %3, off\n\t"
+                 "global_load_lds_dword %1, off\n\t"
                  "s_mov_b32 m0, %0"
                  : "=&s"(saved)
-                 : "v"(a), "s"(alds), "v"(b), "s"(blds)
+                 : "v"(p), "s"(lds)
                  : "memory");
 }
 
@@ -117,7 +98,8 @@ __device__ __forceinline__ void dma16(const void *a, uint32_t alds, const void *
 // T indices.  Instruction d of the T / 8 moves lines 8 d .. 8 d + 7: line l of a row operand is its
 // index l, chunk c its c-th 16 bytes of k; line l of a col operand is k = l %
 // BK of the l / BK-th 128 bytes of indices, chunk c 16 bytes of them.  Indices
-// past the end are read as the last ones (their results are not stored).
+// past the end are read as the last ones (their results are not stored); a col
+// operand's last 16 bytes of a row may run on into the next row.
 template <typename E, bool COL, int T, int N>
 struct Side {
     static constexpr int ES = sizeof(E), BK = 128 / ES, EC = 16 / ES;
@@ -142,14 +124,36 @@ struct Side {
                 off[i] = static_cast<uint32_t>(min(line, last) * ld + c * 16);
         }
     }
-    // What instruction i reads in the last, partial step of `left` k: zeros
-    // past the end of the sum.  A row operand is readable, and zero, up to the
-    // next multiple of a chunk.
-    __device__ __forceinline__ const void *tail(int i, int64_t s, int left, int wave) const
+    // The sum's last step of `left` k, zeros past the end.  In chunks where a row
+    // operand is readable, and zero, up to the next multiple of one, or a col
+    // operand's indices are whole chunks (or readable up to there).
+    __device__ __forceinline__ void chunks(int64_t s, int left, int wave, uint32_t lds) const
     {
-        const int lane = threadIdx.x & 63, line = (wave * N + i) * 8 + (lane >> 3);
-        const int k = COL ? line % BK : ((lane & 7) ^ swz(line)) * EC;
-        return k < left ? static_cast<const void *>(base + s * step + off[i]) : static_cast<const void *>(&g_zeros);
+        const int lane = threadIdx.x & 63;
+        const char *from = base + s * step;
+        asm volatile("" : "+v"(from));   // in vector registers here, so that the whole steps' stays in scalar ones
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int line = (wave * N + i) * 8 + (lane >> 3), k = COL ? line % BK : ((lane & 7) ^ swz(line)) * EC;
+            dma16(k < left ? static_cast<const void *>(from + off[i]) : static_cast<const void *>(&g_zeros), lds + i * 1024);
+        }
+    }
+    // Word by word otherwise: nothing is read past a row operand's k or the end
+    // of a col operand.
+    __device__ __forceinline__ void words(int64_t s, int left, int last, int64_t ld, int wave, uint32_t lds) const
+    {
+        constexpr int EW = 4 / ES;       // elements of a word
+        const int lane = threadIdx.x & 63;
+        const char *from = base + s * step;
+        asm volatile("" : "+v"(from));
+#pragma unroll 4
+        for (int q = 0; q < 4 * N; ++q) {
+            const int line = wave * N * 8 + q * 2 + (lane >> 5), at = lane & 31;
+            const int kl = line % BK, e = ((at >> 2) ^ swz(COL ? kl : line)) * EC + (at & 3) * EW;
+            const int k = COL ? kl : e;
+            const int64_t by = COL ? kl * ld + min(line / BK * BK + e, last & ~(EW - 1)) * ES : min(line, last) * ld + e * ES;
+            dma4(k < left ? static_cast<const void *>(from + by) : static_cast<const void *>(&g_zeros), lds + q * 256);
+        }
     }
 };
 
@@ -286,6 +290,11 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
     const int kbeg = split < 0 ? 0 : split * g.kchunk;
     const int kend = split < 0 ? g.K : kbeg + min(g.K - kbeg, g.kchunk);
     const int nsteps = (kend - kbeg + kBK - 1) / kBK;
+    // steps of whole chunks: not a partial one, nor the sum's last where a col
+    // operand's last chunk would run on past its end
+    const bool ragged = (ACOL && g.words_a) || (BCOL && g.words_b);
+    const int whole = (kend - kbeg) / kBK - (ragged && kend == g.K && g.K % kBK == 0);
+    const int lasta = static_cast<int>(min<int64_t>(g.M - m0, TM)) - 1, lastb = min(g.N - n0, T) - 1;
 
     // DMA instructions of a wave and step
     constexpr int NA = TM / 8 / waves(TM, T), NB = T / 8 / waves(TM, T);
@@ -310,20 +319,34 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
     const auto issue_b = [&](int s, int i) {
         dma16(sb.base + s * sb.step, sb.off[i], lds0 + B0 + (s & 1) * OPB + (wave * NB + i) * 1024);
     };
-    // the same of any step
-    const auto any_a = [&](int s, int at, int i) {
-        const int left = kend - kbeg - s * kBK;
-        if (left >= kBK)
-            issue_a(s, at, i);
-        else if (left > 0)
-            dma16(sa.tail(i, s, left, wave), lds0 + at * OPA + (wave * NA + i) * 1024);
+    // all of any step, into A's stage `at` (A and B leave in turn)
+    const auto any_a = [&](int s, int at) {
+        if (s < whole) {
+#pragma unroll
+            for (int i = 0; i < NA; ++i)
+                issue_a(s, at, i);
+        } else if (s < nsteps) {
+            const int left = kend - kbeg - s * kBK;
+            const uint32_t to = lds0 + at * OPA + wave * NA * 1024;
+            if (g.words_a)
+                sa.words(s, left, lasta, g.A.ld * sizeof(E), wave, to);
+            else
+                sa.chunks(s, left, wave, to);
+        }
     };
-    const auto any_b = [&](int s, int i) {
-        const int left = kend - kbeg - s * kBK;
-        if (left >= kBK)
-            issue_b(s, i);
-        else if (left > 0)
-            dma16(sb.tail(i, s, left, wave), lds0 + B0 + (s & 1) * OPB + (wave * NB + i) * 1024);
+    const auto any_b = [&](int s) {
+        if (s < whole) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+                issue_b(s, i);
+        } else if (s < nsteps) {
+            const int left = kend - kbeg - s * kBK;
+            const uint32_t to = lds0 + B0 + (s & 1) * OPB + wave * NB * 1024;
+            if (g.words_b)
+                sb.words(s, left, lastb, g.B.ld * sizeof(E), wave, to);
+            else
+                sb.chunks(s, left, wave, to);
+        }
     };
     f32x4 acc[FA][8];
 #pragma unroll
@@ -357,7 +380,7 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
     typedef std::integral_constant<int, AS == 3 ? NA : 0> ButA;
     Frags f0, f1;
     int at = 0;                                 // A's stage of the step at hand
-    const auto step = [&](int s, auto whole) {
+    const auto step = [&](int s, auto inner) {   // inner: step s + 2 goes in chunks
         const int at1 = at + 1 == AS ? 0 : at + 1, at2 = at1 + 1 == AS ? 0 : at1 + 1;
 #pragma unroll
         for (int a = 0; a < FA; ++a) {
@@ -365,35 +388,32 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
             if (AS == 3)
 #pragma unroll
                 for (int i = 0; i < NA / FA; ++i)
-                    if (whole)
+                    if (inner)
                         issue_a(s + 2, at2, a * (NA / FA) + i);
-                    else
-                        any_a(s + 2, at2, a * (NA / FA) + i);
 #pragma unroll
             for (int r = 0; r < NR; ++r)
                 read(f1, s, at, 1, a * NR + r);
             multiply(f0, a);
         }
-        if (whole)
+        if (inner) {
             meet(ButA{});
-        else
+        } else {
             meet(All{});
+            any_a(s + 2, at2);
+            any_b(s + 2);
+        }
 #pragma unroll
         for (int a = 0; a < FA; ++a) {
             __builtin_amdgcn_sched_barrier(0);
             if (AS == 2)
 #pragma unroll
                 for (int i = 0; i < NA / FA; ++i)
-                    if (whole)
+                    if (inner)
                         issue_a(s + 2, at2, a * (NA / FA) + i);
-                    else
-                        any_a(s + 2, at2, a * (NA / FA) + i);
 #pragma unroll
             for (int i = 0; i < NB / FA; ++i)
-                if (whole)
+                if (inner)
                     issue_b(s + 2, a * (NB / FA) + i);
-                else
-                    any_b(s + 2, a * (NB / FA) + i);
             // past the last step this reads another stage, unused
 #pragma unroll
             for (int r = 0; r < NR; ++r)
@@ -404,14 +424,9 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
     };
 
     for (int s = 0; s < 2; ++s) {
-#pragma unroll
-        for (int i = 0; i < NA; ++i)
-            any_a(s, s, i);
-#pragma unroll
-        for (int i = 0; i < NB; ++i)
-            any_b(s, i);
+        any_a(s, s);
+        any_b(s);
     }
-    const int whole = (kend - kbeg) / kBK;
     if (whole >= 2)
         meet(std::integral_constant<int, NA + NB>{});
     else
