@@ -166,10 +166,10 @@ __device__ __forceinline__ void load_bias(const Epi &e, int n, int N, float (&b)
 // residual on 16384 x 2048 -> 8192 cost 100 us that way, see the forward
 // kernel's figures); WHOLE: the wave's 128 columns all exist.
 template <typename T, int KIND, int NA, bool WHOLE>
-__device__ __forceinline__ void put_rows(const Gemm &g, const char *lds, int64_t m0, int n0)
+__device__ __forceinline__ void put_rows(const Gemm &g, const char *lds, int64_t m0, int n0, int end)
 {
     const int lane = threadIdx.x & 63, n = n0 + (lane & 15) * 8;
-    const int cols = WHOLE ? 8 : g.N - n;
+    const int cols = WHOLE ? 8 : end - n;
     float bias[8];
     load_bias<T, KIND>(g.e, n, g.N, bias);
 #pragma unroll 1
@@ -207,10 +207,11 @@ __device__ __forceinline__ void put_db(const Gemm &g, int64_t m0, int rows)
     }
 }
 
-// `part`: the piece's rows and columns of this wave, T a row, or nullptr.
+// The tile's columns stop at `end`.  `part`: the piece's rows and columns of
+// this wave, ld a row, or nullptr.
 template <typename T, int KIND, int NA>
 __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8], char *lds, int64_t m0, int n0,
-                                         float *part, int ld)
+                                         int end, float *part, int ld)
 {
     const int lane = threadIdx.x & 63;
     if (part) {
@@ -219,7 +220,8 @@ __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8
         for (int a = 0; a < NA; ++a)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                *reinterpret_cast<f32x4 *>(part + (a * 16 + (lane & 15)) * ld + j * 16 + (lane >> 4) * 4) = acc[a][j];
+                if (j * 16 < ld)
+                    *reinterpret_cast<f32x4 *>(part + (a * 16 + (lane & 15)) * ld + j * 16 + (lane >> 4) * 4) = acc[a][j];
         return;
     }
 #pragma unroll
@@ -233,10 +235,10 @@ __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    if (n0 + 128 <= g.N)
-        put_rows<T, KIND, NA, true>(g, lds, m0, n0);
+    if (n0 + 128 <= end)
+        put_rows<T, KIND, NA, true>(g, lds, m0, n0, end);
     else
-        put_rows<T, KIND, NA, false>(g, lds, m0, n0);
+        put_rows<T, KIND, NA, false>(g, lds, m0, n0, end);
 }
 
 // Tile `id` of the product's order: bands of four rows of tiles, column by

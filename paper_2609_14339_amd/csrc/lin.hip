@@ -7,7 +7,8 @@ namespace acsc {
 int lin_few_run(const Gemm &g, acsc_dtype dt, hipStream_t st, const char *tag);
 int lin_few_weight_run(const Gemm &g, const Kept &kept, acsc_dtype dt, acsc_dtype out, float *db, hipStream_t st,
                        const char *tag);
-int lin_tile_run(const Gemm &g, int tile_rows, EpiKind kind, acsc_dtype dt, acsc_dtype out, hipStream_t st, const char *tag);
+int lin_tile_run(const Gemm &g, int rows, int cols, EpiKind kind, acsc_dtype dt, acsc_dtype out, hipStream_t st,
+                 const char *tag);
 
 namespace {
 
@@ -65,13 +66,14 @@ __global__ __launch_bounds__(256) void lin_join_few_kernel(Gemm g)
 template <int KIND, typename TO, int TM, int T>
 __global__ __launch_bounds__(256) void lin_join_kernel(Gemm g)
 {
-    constexpr int PER = TM * T / 2048;
+    // sixteen lanes at least to a row, a checkpoint's group of it
+    constexpr int W = T < 128 ? 128 : T, PER = TM * W / 2048;
     const int64_t id = blockIdx.x / PER, count = static_cast<int64_t>(g.tm) * g.tn - g.whole;
-    const int c = (blockIdx.x % PER) * 256 + threadIdx.x, row = c / (T / 8), col = c % (T / 8) * 8;
+    const int c = (blockIdx.x % PER) * 256 + threadIdx.x, row = c / (W / 8), col = c % (W / 8) * 8;
     int tile_m, tile_n;
     tile_at(g, g.whole + id, tile_m, tile_n);
     const int64_t m = static_cast<int64_t>(tile_m) * TM + row;
-    join<KIND, TO>(g, g.part + (id * TM + row) * T + col, count * TM * T, m < g.M, m, tile_n * T + col);
+    join<KIND, TO>(g, g.part + (id * TM + row) * T + col, count * TM * T, m < g.M && col < T, m, tile_n * T + col);
 }
 
 // What a product needs done first, up to three jobs in one launch (a launch
@@ -261,13 +263,15 @@ struct Tile {
 inline Cut cut_of(EpiKind kind, const Shape &s, int steps, bool bf16)
 {
     static const Tile kBf16[] = {
-        {256, 256, 1, 1.5, 1.5, 5}, {128, 128, 2, 1.0, 0.65, 3}, {64, 128, 3, 1.05, 0.85, 3}, {32, 128, 4, 1.0, 0.8, 3}};
-    static const Tile kF32[] = {{128, 128, 2, 4.1, 2.2, 3}, {64, 128, 3, 3.2, 1.2, 3}, {32, 128, 4, 2.3, 1.2, 3}};
+        {256, 256, 1, 1.5, 1.5, 5}, {128, 128, 2, 1.0, 0.65, 3}, {64, 128, 3, 1.05, 0.85, 3}, {32, 128, 4, 1.0, 0.8, 3}, {128, 64, 2, 0.8, 0.55, 3}};
+    static const Tile kF32[] = {{128, 128, 2, 4.1, 2.2, 3}, {64, 128, 3, 3.2, 1.2, 3}, {32, 128, 4, 2.3, 1.2, 3}, {128, 64, 2, 2.2, 1.2, 3}};
     const Tile *first = bf16 ? kBf16 : kF32, *end = bf16 ? std::end(kBf16) : std::end(kF32);
     Cut best{};
     double least = 0;
     for (const Tile *t = first; t != end; ++t) {
-        if (t->rows != t->cols && kind == kWeight)
+        // 32 rows of a col operand are not a whole block of it in LDS; 64
+        // columns would split the group of a checkpoint that is written
+        if ((t->rows == 32 && kind == kWeight) || (t->cols == 64 && kind == kForward && s.N > 64))
             continue;
         const int64_t tiles = ((s.M + t->rows - 1) / t->rows) * ((s.N + t->cols - 1) / t->cols);
         const int slots = 256 * t->at_once;
@@ -347,20 +351,24 @@ template <int KIND, typename TO>
 void launch_join(const Gemm &g, const Plan &p, hipStream_t st)
 {
     const int tail = p.tm * p.tn - p.whole;
-    const dim3 grid(tail * (p.rows * p.tile / 2048));
+    const dim3 grid(tail * (p.rows * std::max(p.tile, 128) / 2048));
     if (p.rows == 256) {
         ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 256, 256>), grid, dim3(256), 0, st, g);
         return;
     }
-    if constexpr (KIND != kWeight) {
-        if (p.rows < 128) {
-            if (p.rows == 64)
-                ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 64, 128>), grid, dim3(256), 0, st, g);
-            else
-                ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 32, 128>), grid, dim3(256), 0, st, g);
+    if (p.rows == 64) {
+        ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 64, 128>), grid, dim3(256), 0, st, g);
+        return;
+    }
+    if (p.tile == 64) {
+        ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 128, 64>), grid, dim3(256), 0, st, g);
+        return;
+    }
+    if constexpr (KIND != kWeight)
+        if (p.rows == 32) {
+            ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 32, 128>), grid, dim3(256), 0, st, g);
             return;
         }
-    }
     ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 128, 128>), grid, dim3(256), 0, st, g);
 }
 
@@ -452,7 +460,7 @@ int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype
     if (p.few) {
         if (int rc = lin_few_run(g, dt, st, tag))
             return rc;
-    } else if (int rc = lin_tile_run(g, p.rows, kind, dt, out, st, tag)) {
+    } else if (int rc = lin_tile_run(g, p.rows, p.tile, kind, dt, out, st, tag)) {
         return rc;
     }
     if (pieces) {

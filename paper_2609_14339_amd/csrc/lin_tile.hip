@@ -3,8 +3,8 @@
 //
 // A workgroup takes a TM x T tile of C in steps of 128 bytes along the sum (64
 // bf16, 32 fp32): 256 x 256 (bf16 only) by eight waves of 64 rows and 128
-// columns, 128 x 128 by four of 32 rows, and, for the few rows of a forward
-// product or an input gradient, 64 x 128 by four of 16 and 32 x 128 by two.
+// columns, 128 x 128 by four of 32 rows, and, for few rows, 64 x 128 by four of
+// 16 and 32 x 128 by two, for few columns 128 x 64 by four of 32.
 // Each step's tiles of A and B come straight from memory into LDS
 // (global_load_lds_dwordx4); no register holds them on the way.  An operand
 // stays in LDS as it is stored: lines of one index's step (row) or k-lines of
@@ -247,7 +247,7 @@ struct Frag<float, COL> {
 
 // Fragments of 16 rows of a wave, and waves, for a tile of TM rows.
 constexpr int fragments(int TM) { return TM < 64 ? 1 : TM / 64; }
-constexpr int waves(int TM, int T) { return TM / (16 * fragments(TM)) * (T / 128); }
+constexpr int waves(int TM, int T) { return TM / (16 * fragments(TM)) * (T < 128 ? 1 : T / 128); }
 
 // Stages of A: a third one where it fits beside the other workgroup (see the
 // step below); B has two.
@@ -257,9 +257,10 @@ template <typename E, int TM, int T, bool ACOL, bool BCOL, int KIND, typename TO
 __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_kernel(Gemm g)
 {
     extern __shared__ __align__(1024) unsigned char smem[];
-    static_assert(!ACOL || TM == T, "a col operand A fills whole blocks");
+    static_assert(!ACOL || TM >= 64, "a col operand A fills whole blocks");
     constexpr int kBK = 128 / sizeof(E);
-    constexpr int WN = T / 128;                 // waves along the columns
+    constexpr int WN = T < 128 ? 1 : T / 128;   // waves along the columns
+    constexpr int FB = T < 128 ? T / 16 : 8;    // 16-column fragments of a wave
     constexpr int FA = fragments(TM);
     constexpr int OPA = TM * 128, OPB = T * 128;   // bytes of a step's A and B
     constexpr int AS = a_stages(TM);
@@ -311,7 +312,7 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
     frb.init(0);
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte *)smem));
 
-    constexpr int NR = (8 + FA) / FA;           // fragments read beside eight products
+    constexpr int NR = (FB + FA - 1) / FA + 1;  // fragments read beside a row of products
     // instruction i of step s, which is whole, into stage `at`
     const auto issue_a = [&](int s, int at, int i) {
         dma16(sa.base + s * sa.step, sa.off[i], lds0 + at * OPA + (wave * NA + i) * 1024);
@@ -354,21 +355,23 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             acc[a][j] = f32x4{0, 0, 0, 0};
-    // fragments of k half kh of a stage: eight of B's side, then FA of A's
+    // fragments of k half kh of a stage: FB of B's side, then FA of A's
     struct Frags {
-        typename FragA::Value f[8 + FA];
+        typename FragA::Value f[FB + FA];
     };
     const auto read = [&](Frags &f, int s, int at, int kh, int r) {
-        if (r < 8)
+        if (r >= FB + FA)
+            return;
+        if (r < FB)
             f.f[r] = frb.read(smem + B0 + (s & 1) * OPB + wn * 16384, r, kh);
         else
-            f.f[r] = fra.read(smem + at * OPA + (ACOL ? wm * FA / BA * (BA * 2048) : wm * FA * 2048), r - 8, kh);
+            f.f[r] = fra.read(smem + at * OPA + (ACOL ? wm * FA / BA * (BA * 2048) : wm * FA * 2048), r - FB, kh);
     };
-    // eight products at a time, with what goes out beside them
+    // a row of products at a time, with what goes out beside them
     const auto multiply = [&](const Frags &f, int a) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            acc[a][j] = FragA::multiply(f.f[j], f.f[8 + a], acc[a][j]);
+        for (int j = 0; j < FB; ++j)
+            acc[a][j] = FragA::multiply(f.f[j], f.f[FB + a], acc[a][j]);
     };
     // this wave's DMA has landed, but for the newest `ahead`, and its LDS reads
     // are done; then everyone's
@@ -432,7 +435,7 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
     else
         meet(All{});
 #pragma unroll
-    for (int r = 0; r < 8 + FA; ++r)
+    for (int r = 0; r < FB + FA; ++r)
         read(f0, 0, 0, 0, r);
     int s = 0;
     for (; s + 2 < whole; ++s)
@@ -449,7 +452,7 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
 #pragma unroll
     for (int a = 0; a < FA; a += PUT)
         put_tile<TO, KIND, PUT>(g, reinterpret_cast<const f32x4(&)[PUT][8]>(acc[a]), own, m0 + (wm * FA + a) * 16,
-                               n0 + wn * 128, part ? part + a * 16 * T : nullptr, T);
+                               n0 + wn * 128, min(g.N, n0 + T), part ? part + a * 16 * T : nullptr, T);
 }
 
 template <typename E, int TM, int T, bool ACOL, bool BCOL, int KIND, typename TO>
@@ -479,29 +482,31 @@ int launch_kind(const Gemm &g, EpiKind kind, acsc_dtype out, hipStream_t st, con
         return launch<E, TM, T, false, false, kForward, E>(g, st, tag);
     if (kind == kGate)
         return launch<E, TM, T, false, true, kGate, E>(g, st, tag);
-    if constexpr (TM == T)
+    if constexpr (TM >= 64)
         return out == ACSC_BF16 ? launch<E, TM, T, true, true, kWeight, uint16_t>(g, st, tag)
                                 : launch<E, TM, T, true, true, kWeight, float>(g, st, tag);
-    return ACSC_EINVAL;   // narrow tiles are of the other two kinds
+    return ACSC_EINVAL;   // tiles of 32 rows are of the other two kinds
 }
 
 template <typename E>
-int launch_narrow(const Gemm &g, int tile_rows, EpiKind kind, acsc_dtype out, hipStream_t st, const char *tag)
+int launch_tile(const Gemm &g, int rows, int cols, EpiKind kind, acsc_dtype out, hipStream_t st, const char *tag)
 {
-    if (tile_rows == 128)
+    if (cols == 64)
+        return launch_kind<E, 128, 64>(g, kind, out, st, tag);
+    if (rows == 128)
         return launch_kind<E, 128, 128>(g, kind, out, st, tag);
-    return tile_rows == 64 ? launch_kind<E, 64, 128>(g, kind, out, st, tag)
-                           : launch_kind<E, 32, 128>(g, kind, out, st, tag);
+    return rows == 64 ? launch_kind<E, 64, 128>(g, kind, out, st, tag) : launch_kind<E, 32, 128>(g, kind, out, st, tag);
 }
 
 }  // namespace
 
-int lin_tile_run(const Gemm &g, int tile_rows, EpiKind kind, acsc_dtype dt, acsc_dtype out, hipStream_t st, const char *tag)
+int lin_tile_run(const Gemm &g, int rows, int cols, EpiKind kind, acsc_dtype dt, acsc_dtype out, hipStream_t st,
+                 const char *tag)
 {
     if (dt == ACSC_F32)
-        return launch_narrow<float>(g, tile_rows, kind, out, st, tag);
-    return tile_rows == 256 ? launch_kind<uint16_t, 256, 256>(g, kind, out, st, tag)
-                            : launch_narrow<uint16_t>(g, tile_rows, kind, out, st, tag);
+        return launch_tile<float>(g, rows, cols, kind, out, st, tag);
+    return rows == 256 ? launch_kind<uint16_t, 256, 256>(g, kind, out, st, tag)
+                       : launch_tile<uint16_t>(g, rows, cols, kind, out, st, tag);
 }
 
 }  // namespace acsc

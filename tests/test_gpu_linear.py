@@ -132,6 +132,39 @@ def test_few_rows(pk, dtype, rows, n_in, n_out, pad):
         within(pk.lin_backward_input(dz, W, "silu", src), want, tol * (1 + 2.0 ** -8) + store(dtype, want))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [33, 65, 130, 1100])
+@pytest.mark.parametrize("n_in,n_out,pad", [(1, 64, 0), (2, 3, 0), (3, 2, 0), (5, 33, 1), (64, 1000, 0), (2051, 64, 0), (4100, 50, 2),
+                                            (50, 4100, 2), (66, 130, 4)])
+def test_narrow_layers(pk, dtype, rows, n_in, n_out, pad):
+    """Few inputs or outputs: tiles of 64 columns, whole and cut; rows that are shorter than a 16-byte chunk or end inside
+    one, and sums that do."""
+    s = rows + n_in
+    x = randn(rows, n_in, dtype=dtype, seed=s, pad=pad)
+    W = randn(n_out, n_in, dtype=dtype, seed=s + 1, scale=1 / math.sqrt(n_in), pad=pad)
+    dz = randn(rows, n_out, dtype=dtype, seed=s + 2, pad=pad)
+    z, ez = product(x, W.t(), n_in)
+    got, q = pk.lin_forward(x, W, keep="q8")
+    within(got, z, ez * (1 + 2.0 ** -8) + store(dtype, z))
+    n = -(-n_out // GROUP)
+    pz, pe = torch.zeros(2, rows, n * GROUP, dtype=torch.float64, device="cuda").unbind(0)
+    pz[:, :n_out], pe[:, :n_out] = z, ez
+    top = pz.view(rows, n, GROUP).abs().amax(2)
+    within(q.scales, top / 127, (pe.view(rows, n, GROUP).amax(2) + 2 * U * top) / 127)
+    step = q.scales.double().repeat_interleave(GROUP, 1)[:, :n_out]
+    within(q.codes.double() * step, z, step * (0.5 + 127 * 8 * U) + ez)
+    p, ep = product(dz, W, n_out)
+    within(pk.lin_backward_input(dz, W), p, ep * (1 + 2.0 ** -8) + store(dtype, p))
+    p, ep = product(dz.t(), x, rows)
+    for dw_dtype in (BF16, F32):
+        dW, db = pk.lin_backward_weight(dz, x, dw_dtype=dw_dtype)
+        within(dW, p, ep * (1 + 2.0 ** -8) + store(dw_dtype, p))
+        within(db, dz.double().sum(0), 2 * U * (rows + 8) * dz.double().abs().sum(0))
+    # operands that end with the memory they were given: the last rows of a larger tensor
+    base = randn(rows + 9, n_in, dtype=dtype, seed=s + 3)
+    assert torch.equal(pk.lin_forward(base[9:], W)[0], pk.lin_forward(base[9:].clone(), W)[0])
+
+
 @pytest.mark.parametrize("kept", ["z", "q8"])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows,n_in,n_out", SHAPES)
