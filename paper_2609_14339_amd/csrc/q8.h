@@ -340,7 +340,8 @@ __device__ __forceinline__ float act_value(float z, int act)
             return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
         float e;
         const float q = normal_tail(z, e);
-        return __builtin_fmaf(-fabsf(z), q, z > 0.f || z != z ? z : 0.f);
+        // past 64 q is 0, and infinity times it would be NaN
+        return __builtin_fmaf(-fabsf(z > 64.f ? 64.f : z), q, z < 0.f ? 0.f : z);
     }
     if (act == ACSC_ACT_SILU) {
         float s, c;

@@ -257,6 +257,24 @@ def test_non_finite_values_stay_in_their_rows(pk, dtype, rows, n_in, n_out):
     assert torch.equal(w[outs], w0[outs]) and not torch.isfinite(w[3]).any() and torch.isinf(db[3])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [2, 200])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+def test_activations_at_the_ends_of_the_range(pk, dtype, rows, act):
+    """The formulas' values at infinities and NaN, and where exponentials leave the range."""
+    nan, inf = float("nan"), float("inf")
+    z = torch.tensor([inf, -inf, nan, 0.0, 1e30, -1e30, 65.0, -65.0, 64.0, -64.0, 200.0, -200.0])
+    want = dict(none=[inf, -inf, nan, 0, 1e30, -1e30, 65, -65, 64, -64, 200, -200],
+                relu=[inf, 0, nan, 0, 1e30, 0, 65, 0, 64, 0, 200, 0],
+                gelu=[inf, nan, nan, 0, 1e30, 0, 65, 0, 64, 0, 200, 0],
+                silu=[inf, nan, nan, 0, 1e30, 0, 65, 0, 64, 0, 200, 0])[act]
+    want = torch.tensor(want).to(dtype).expand(rows, -1)
+    x, W = torch.zeros(rows, 40, dtype=dtype, device="cuda"), torch.zeros(12, 40, dtype=dtype, device="cuda")
+    got = pk.lin_forward(x, W, z.to(dtype).cuda(), act)[0].cpu()
+    # silu(-64) = -64 e^-64 and silu(-65) are numbers of fp32 below 2^-86
+    assert torch.allclose(got.float(), want.float(), rtol=0, atol=2.0 ** -86, equal_nan=True)
+
+
 def test_outputs_in_place_and_margins(pk):
     rows, n_in, n_out = 70, 136, 200
     x = randn(rows, n_in, dtype=BF16, seed=1)
