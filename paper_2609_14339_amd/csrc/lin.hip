@@ -301,7 +301,8 @@ inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bo
     Plan p{};
     const bool bf16 = dt == ACSC_BF16;
     const int bk = 128 / static_cast<int>(dtype_size(dt));
-    const int steps = (s.K + bk - 1) / bk;
+    const int64_t K = s.K;   // up to 2^31 - 1 rows: what rounds it up takes 64 bits
+    const int steps = static_cast<int>((K + bk - 1) / bk);
     if (kind == kWeight && s.K <= few_tokens(kind, fits_b)) {
         p.few = true;
         p.splits = 1;
@@ -327,14 +328,14 @@ inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bo
     p.tn = (s.N + p.tile - 1) / p.tile;
     p.whole = c.whole;
     p.splits = c.splits;
-    p.kchunk = c.per * bk;
+    p.kchunk = static_cast<int>(std::min(K, static_cast<int64_t>(c.per) * bk));
     p.part = up256(static_cast<size_t>(static_cast<int64_t>(p.tm) * p.tn - p.whole) * p.splits * p.rows * p.tile * 4);
     if (kind == kWeight) {
         // db's slices of at least 32 rows, up to about two workgroups a CU
         const int64_t blocks = (s.M + 511) / 512;
-        p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(512 / blocks, s.K / 32)));
-        p.slice = (s.K + p.slices - 1) / p.slices;
-        p.slices = (s.K + p.slice - 1) / p.slice;
+        p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(512 / blocks, K / 32)));
+        p.slice = static_cast<int>((K + p.slices - 1) / p.slices);
+        p.slices = static_cast<int>((K + p.slice - 1) / p.slice);
         p.db = p.slices > 1 ? up256(static_cast<size_t>(p.slices) * s.M * 4) : 0;
     }
     const int64_t es = static_cast<int64_t>(dtype_size(dt));

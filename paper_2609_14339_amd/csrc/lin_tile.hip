@@ -290,7 +290,7 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
     const int n0 = tile_n * T;
     const int kbeg = split < 0 ? 0 : split * g.kchunk;
     const int kend = split < 0 ? g.K : kbeg + min(g.K - kbeg, g.kchunk);
-    const int nsteps = (kend - kbeg + kBK - 1) / kBK;
+    const int nsteps = (kend - kbeg - 1) / kBK + 1;   // kend - kbeg up to 2^31 - 1
     // steps of whole chunks: not a partial one, nor the sum's last where a col
     // operand's last chunk would run on past its end
     const bool ragged = (ACOL && g.words_a) || (BCOL && g.words_b);

@@ -1,0 +1,35 @@
+"""Linear layers at the largest row counts that they take, from the host side: sizes of workspaces (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+F32, BF16 = 0, 1
+
+
+@pytest.fixture(scope="module")
+def pk():
+    import paper_2609_14339_amd as pk
+    return pk
+
+
+def up(n, k):
+    return -(-n // k) * k
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("n_in,n_out", [(1, 1), (8, 300), (64, 512), (72, 1300)])
+@pytest.mark.parametrize("short", [1, 2, 31, 32, 33, 63, 64, 65, 4096, (1 << 22) - 3, 1 << 22, (1 << 22) + 5, 1 << 23])
+def test_weight_gradient_of_nearly_2_31_rows(pk, dt, n_in, n_out, short):
+    """db's sums are cut into slices of the rows whatever their number, and the product as it is at half as many rows:
+    what is left of the size beside db, the recomputed activation and copies."""
+    def pieces(rows):
+        b = C.c_size_t(0)
+        assert pk.lib.lin_workspace_size(pk.LIN_BACKWARD_WEIGHT, rows, n_in, n_out, dt, C.byref(b)) == 0
+        slices = max(1, min(512 // -(-n_out // 512), rows // 32))
+        slices = -(-rows // -(-rows // slices))
+        es = 2 if dt == BF16 else 4
+        recomputed = up(rows * up(n_in, 8) * es, 256)
+        copies = sum(up(rows * up(n, 8) * es, 256) for n in (n_in, n_out) if n < 16 // es or n * es % 4)
+        return b.value - recomputed - copies - up(slices * n_out * 4, 256)
+
+    assert pieces((1 << 31) - short) == pieces(1 << 30) >= 0
