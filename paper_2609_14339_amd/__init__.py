@@ -5,6 +5,11 @@ tensors into device pointers and the current HIP stream, calls the C entry
 point of the same name, and raises ``AcscError`` on a non-zero return code.
 There is no fallback: if the library is not built, importing this package
 raises ``ImportError``.
+
+``stream=`` runs a call on a stream other than the current one.  The caller
+orders that stream after what produced the inputs, and whoever reads the
+outputs after that stream; the memory on both sides of the call is taken care
+of here.
 """
 from __future__ import annotations
 
@@ -642,10 +647,33 @@ def _act(act: str) -> int:
     return code
 
 
-def _raw_stream(stream) -> int:
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
-    return stream.cuda_stream
+def _raw_stream() -> int:
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _on(stream, fn, *args):
+    """fn(*args) on `stream`, if that is not the current one: everything it
+    allocates comes from that stream's memory, so it waits for nothing that the
+    current stream still does with a block it freed.  What it is given is kept
+    from reuse until `stream` has got past the call, what it returns until the
+    current stream has got past its use of it."""
+    here = torch.cuda.current_stream()
+    if stream == here:
+        return fn(*args)
+    with torch.cuda.stream(stream):
+        out = fn(*args)
+    _record(args, stream)
+    _record(out, here)
+    return out
+
+
+def _record(obj, stream):
+    if isinstance(obj, torch.Tensor):
+        if obj.is_cuda:
+            obj.record_stream(stream)
+    elif isinstance(obj, (tuple, list)):
+        for o in obj:
+            _record(o, stream)
 
 
 def _rows(t: torch.Tensor, shape, dtype: torch.dtype, name: str) -> int:
@@ -702,14 +730,12 @@ def _kept(src: Union[torch.Tensor, Q8, None], shape, dtype: torch.dtype, name: s
     return src.data_ptr(), ld, None
 
 
-def _ws(nbytes: int, ws: Optional[torch.Tensor], device, stream):
+def _ws(nbytes: int, ws: Optional[torch.Tensor], device):
     """(address, bytes, what keeps it alive) of a workspace: the given one, or a new one."""
     if ws is None:
         if not nbytes:
             return None, 0, None
         ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        if stream is not None:
-            ws.record_stream(stream)   # freed here, perhaps before that stream has used it
         return ws.data_ptr(), nbytes, ws
     _need_cuda(ws)
     return ws.data_ptr(), ws.numel() * ws.element_size(), ws
@@ -727,11 +753,13 @@ def _ln_bytes(rows: int, H: int) -> int:
 
 def q8_encode(x: torch.Tensor, q: Optional[Q8] = None, stream=None) -> Q8:
     """The 8-bit checkpoint of x [rows, H] (row stride x.stride(0))."""
+    if stream is not None:
+        return _on(stream, q8_encode, x, q)
     rows, H = _two_d(x, "x")
     dt, ld = _dt(x), _rows(x, x.shape, x.dtype, "x")
     if q is None:
         q = _q8_new(rows, H, x.device)
-    rc = lib.q8_encode(x.data_ptr(), dt, rows, H, ld, _q8_ref(q, rows, H), _raw_stream(stream))
+    rc = lib.q8_encode(x.data_ptr(), dt, rows, H, ld, _q8_ref(q, rows, H), _raw_stream())
     if rc:
         _check(rc)
     return q
@@ -740,11 +768,13 @@ def q8_encode(x: torch.Tensor, q: Optional[Q8] = None, stream=None) -> Q8:
 def q8_decode(q: Q8, dtype: torch.dtype, act: str = "none", y: Optional[torch.Tensor] = None,
               stream=None) -> torch.Tensor:
     """act(values of q) [rows, H], rounded once to dtype."""
+    if stream is not None:
+        return _on(stream, q8_decode, q, dtype, act, y)
     rows, H = _two_d(q.codes, "codes")
     if y is None:
         y = torch.empty((rows, H), dtype=dtype, device=q.codes.device)
     ld = _rows(y, (rows, H), dtype, "y")
-    rc = lib.q8_decode(_q8_ref(q, rows, H), rows, H, _act(act), y.data_ptr(), _dt(y), ld, _raw_stream(stream))
+    rc = lib.q8_decode(_q8_ref(q, rows, H), rows, H, _act(act), y.data_ptr(), _dt(y), ld, _raw_stream())
     if rc:
         _check(rc)
     return y
@@ -754,6 +784,8 @@ def ln_forward(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Opti
                eps: float = 1e-5, checkpoint: bool = False, y: Optional[torch.Tensor] = None, stream=None):
     """Layer norm of the rows of x [rows, H]: (y, mean [rows], rstd [rows], q),
     q the 8-bit checkpoint of x if asked for, else None."""
+    if stream is not None:
+        return _on(stream, ln_forward, x, gamma, beta, eps, checkpoint, y)
     shape = rows, H = _two_d(x, "x")
     dtype, dev = x.dtype, x.device
     ld = _rows(x, shape, dtype, "x")
@@ -767,7 +799,7 @@ def ln_forward(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Opti
     rstd = torch.empty(rows, dtype=torch.float32, device=dev)
     q = _q8_new(rows, H, dev) if checkpoint else None
     rc = lib.ln_forward(x.data_ptr(), _dt(x), rows, H, ld, pg, pb, eps, y.data_ptr(), ldy, mean.data_ptr(),
-                        rstd.data_ptr(), None if q is None else _q8_ref(q, rows, H), _raw_stream(stream))
+                        rstd.data_ptr(), None if q is None else _q8_ref(q, rows, H), _raw_stream())
     if rc:
         _check(rc)
     return y, mean, rstd, q
@@ -777,6 +809,8 @@ def ln_recompute(src: Union[torch.Tensor, Q8], mean: torch.Tensor, rstd: torch.T
                  gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
                  dtype: torch.dtype = torch.bfloat16, y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """ln_forward's y again from x or its checkpoint and the kept statistics."""
+    if stream is not None:
+        return _on(stream, ln_recompute, src, mean, rstd, gamma, beta, dtype, y)
     rows, H = _two_d(src.codes if isinstance(src, Q8) else src, "src")
     p, ld, q = _kept(src, (rows, H), dtype, "src")
     pm, pr = _vec(mean, rows, torch.float32, "mean"), _vec(rstd, rows, torch.float32, "rstd")
@@ -785,7 +819,7 @@ def ln_recompute(src: Union[torch.Tensor, Q8], mean: torch.Tensor, rstd: torch.T
     if y is None:
         y = torch.empty((rows, H), dtype=dtype, device=mean.device)
     ldy = _rows(y, (rows, H), dtype, "y")
-    _check(lib.ln_recompute(p, ld, q, _dt(y), rows, H, pm, pr, pg, pb, y.data_ptr(), ldy, _raw_stream(stream)))
+    _check(lib.ln_recompute(p, ld, q, _dt(y), rows, H, pm, pr, pg, pb, y.data_ptr(), ldy, _raw_stream()))
     return y
 
 
@@ -803,6 +837,8 @@ def ln_backward(dy: torch.Tensor, src: Union[torch.Tensor, Q8], mean: torch.Tens
     """(dx, dgamma, dbeta) of ln_forward from x or its checkpoint; add: the
     gradient that reaches x past the norm.  dgamma, dbeta: fp32 [H]; with
     accumulate they are given and added to."""
+    if stream is not None:
+        return _on(stream, ln_backward, dy, src, mean, rstd, gamma, add, dx, dgamma, dbeta, accumulate, ws)
     shape = rows, H = _two_d(dy, "dy")
     dtype, dev = dy.dtype, dy.device
     lddy = _rows(dy, shape, dtype, "dy")
@@ -820,10 +856,10 @@ def ln_backward(dy: torch.Tensor, src: Union[torch.Tensor, Q8], mean: torch.Tens
         dbeta = torch.empty(H, dtype=torch.float32, device=dev)
     pm, pr = _vec(mean, rows, torch.float32, "mean"), _vec(rstd, rows, torch.float32, "rstd")
     pg = None if gamma is None else _vec(gamma, H, dtype, "gamma")
-    wp, wn, keep = _ws(_ln_bytes(rows, H), ws, dev, stream)
+    wp, wn, keep = _ws(_ln_bytes(rows, H), ws, dev)
     rc = lib.ln_backward(dy.data_ptr(), lddy, p, ld, q, _dt(dy), rows, H, pm, pr, pg, pa, ldadd, dx.data_ptr(), lddx,
                          _vec(dgamma, H, torch.float32, "dgamma"), _vec(dbeta, H, torch.float32, "dbeta"),
-                         int(accumulate), wp, wn, _raw_stream(stream))
+                         int(accumulate), wp, wn, _raw_stream())
     if rc:
         _check(rc)
     return dx, dgamma, dbeta
@@ -846,15 +882,15 @@ def lin_workspace_size_unaligned(op: int, rows: int, n_in: int, n_out: int, dtyp
     return b.value
 
 
-def _lin_ws(op: int, rows: int, n_in: int, n_out: int, a, lda: int, b, ldb: int, ws: Optional[torch.Tensor], stream):
+def _lin_ws(op: int, rows: int, n_in: int, n_out: int, a, lda: int, b, ldb: int, ws: Optional[torch.Tensor]):
     """A workspace for a product of operands a and b (their row strides; b may
     be None), unless one is given."""
     if ws is not None:
-        return _ws(0, ws, a.device, stream)
+        return _ws(0, ws, a.device)
     aligned = lda < 1 << 21 and (b is None or ldb < 1 << 21)
     if aligned and a.dtype is torch.bfloat16:
         aligned = not ((lda | a.data_ptr() >> 1) & 1) and (b is None or not ((ldb | b.data_ptr() >> 1) & 1))
-    return _ws(_lin_bytes(aligned, op, rows, n_in, n_out, a.dtype), None, a.device, stream)
+    return _ws(_lin_bytes(aligned, op, rows, n_in, n_out, a.dtype), None, a.device)
 
 
 def lin_forward(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
@@ -863,6 +899,8 @@ def lin_forward(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
     """y = act(x W^T + bias) + residual for x [rows, n_in], W [n_out, n_in]:
     (y, kept), kept the pre-activation if keep is "z", its 8-bit checkpoint if
     keep is "q8", else None."""
+    if stream is not None:
+        return _on(stream, lin_forward, x, W, bias, act, residual, keep, y, ws)
     rows, n_in = _two_d(x, "x")
     n_out = _two_d(W, "W")[0]
     dtype, dev = x.dtype, x.device
@@ -883,9 +921,9 @@ def lin_forward(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
         pq = _q8_ref(q, rows, n_out)
     elif keep is not None:
         raise AcscError(ACSC_EINVAL, f"keep must be None, 'z' or 'q8', not {keep!r}")
-    wp, wn, hold = _lin_ws(LIN_FORWARD, rows, n_in, n_out, x, ldx, W, ldw, ws, stream)
+    wp, wn, hold = _lin_ws(LIN_FORWARD, rows, n_in, n_out, x, ldx, W, ldw, ws)
     rc = lib.lin_forward(x.data_ptr(), ldx, _dt(x), rows, n_in, n_out, W.data_ptr(), ldw, pb, _act(act), pr, ldr,
-                         y.data_ptr(), ldy, pz, n_out, pq, wp, wn, _raw_stream(stream))
+                         y.data_ptr(), ldy, pz, n_out, pq, wp, wn, _raw_stream())
     if rc:
         _check(rc)
     return y, (z if q is None else q)
@@ -894,6 +932,8 @@ def lin_forward(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
 def lin_backward_act(dy: torch.Tensor, z: Union[torch.Tensor, Q8], act: str, dz: Optional[torch.Tensor] = None,
                      stream=None) -> torch.Tensor:
     """dz = dy act'(z) from the kept pre-activation or its checkpoint."""
+    if stream is not None:
+        return _on(stream, lin_backward_act, dy, z, act, dz)
     shape = rows, n = _two_d(dy, "dy")
     ld = _rows(dy, shape, dy.dtype, "dy")
     p, ldz, q = _kept(z, shape, dy.dtype, "z")
@@ -902,7 +942,7 @@ def lin_backward_act(dy: torch.Tensor, z: Union[torch.Tensor, Q8], act: str, dz:
     else:
         lddz = _rows(dz, shape, dy.dtype, "dz")
     rc = lib.lin_backward_act(dy.data_ptr(), ld, p, ldz, q, _dt(dy), rows, n, _act(act), dz.data_ptr(), lddz,
-                              _raw_stream(stream))
+                              _raw_stream())
     if rc:
         _check(rc)
     return dz
@@ -913,6 +953,8 @@ def lin_backward_input(dz: torch.Tensor, W: torch.Tensor, act: str = "none",
                        ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """dx = dz W; with act, (dz W) act'(z) from the pre-activation z [rows,
     n_in] that the layer before kept, or its checkpoint."""
+    if stream is not None:
+        return _on(stream, lin_backward_input, dz, W, act, z, dx, ws)
     rows, n_out = _two_d(dz, "dz")
     n_in = _two_d(W, "W")[1]
     dtype, dev = dz.dtype, dz.device
@@ -922,9 +964,9 @@ def lin_backward_input(dz: torch.Tensor, W: torch.Tensor, act: str = "none",
         dx, lddx = torch.empty((rows, n_in), dtype=dtype, device=dev), n_in
     else:
         lddx = _rows(dx, (rows, n_in), dtype, "dx")
-    wp, wn, hold = _lin_ws(LIN_BACKWARD_INPUT, rows, n_in, n_out, dz, lddz, W, ldw, ws, stream)
+    wp, wn, hold = _lin_ws(LIN_BACKWARD_INPUT, rows, n_in, n_out, dz, lddz, W, ldw, ws)
     rc = lib.lin_backward_input(dz.data_ptr(), lddz, _dt(dz), rows, n_in, n_out, W.data_ptr(), ldw, _act(act), p, ldz, q,
-                                dx.data_ptr(), lddx, wp, wn, _raw_stream(stream))
+                                dx.data_ptr(), lddx, wp, wn, _raw_stream())
     if rc:
         _check(rc)
     return dx
@@ -938,6 +980,8 @@ def lin_backward_weight(dz: torch.Tensor, x: Union[torch.Tensor, Q8], act: str =
     from dz [rows, n_out] and the layer's input act(x), x [rows, n_in] or its
     checkpoint.  With accumulate, dW (and db, unless bias is False) are given
     and added to."""
+    if stream is not None:
+        return _on(stream, lin_backward_weight, dz, x, act, dw_dtype, bias, dW, db, accumulate, ws)
     rows, n_out = _two_d(dz, "dz")
     n_in = _two_d(x.codes if isinstance(x, Q8) else x, "x")[1]
     dtype, dev = dz.dtype, dz.device
@@ -954,10 +998,9 @@ def lin_backward_weight(dz: torch.Tensor, x: Union[torch.Tensor, Q8], act: str =
     pdb = None if db is None else _vec(db, n_out, torch.float32, "db")
     code = _act(act)
     # the activation is recomputed into the workspace: no operand of the caller's
-    wp, wn, hold = _lin_ws(LIN_BACKWARD_WEIGHT, rows, n_in, n_out, dz, lddz, None if q is not None or code else x, ldx, ws,
-                           stream)
+    wp, wn, hold = _lin_ws(LIN_BACKWARD_WEIGHT, rows, n_in, n_out, dz, lddz, None if q is not None or code else x, ldx, ws)
     rc = lib.lin_backward_weight(dz.data_ptr(), lddz, p, ldx, q, code, _dt(dz), rows, n_in, n_out, dW.data_ptr(), _dt(dW),
-                                 lddw, pdb, int(accumulate), wp, wn, _raw_stream(stream))
+                                 lddw, pdb, int(accumulate), wp, wn, _raw_stream())
     if rc:
         _check(rc)
     return dW, db
