@@ -8,8 +8,9 @@ raises ``ImportError``.
 
 ``stream=`` runs a call on a stream other than the current one.  The caller
 orders that stream after what produced the inputs, and whoever reads the
-outputs after that stream; the memory on both sides of the call is taken care
-of here.
+outputs after that stream; the memory that a call allocates, and that of the
+tensors in its arguments, is taken care of here.  (A batched call's items, with
+their outputs and workspaces, stay the caller's to keep.)
 """
 from __future__ import annotations
 
@@ -200,15 +201,43 @@ def _stream(stream=None):
     return C.c_void_p(stream.cuda_stream)
 
 
+def _on(stream, fn, *args):
+    """fn(*args) on `stream`, if that is not the current one: everything it
+    allocates comes from that stream's memory, so it waits for nothing that the
+    current stream still does with a block it freed.  What it is given is kept
+    from reuse until `stream` has got past the call, what it returns until the
+    current stream has got past its use of it."""
+    here = torch.cuda.current_stream()
+    if stream == here:
+        return fn(*args)
+    with torch.cuda.stream(stream):
+        out = fn(*args)
+    _record(args, stream)
+    _record(out, here)
+    return out
+
+
+def _record(obj, stream):
+    if isinstance(obj, torch.Tensor):
+        if obj.is_cuda:
+            obj.record_stream(stream)
+    elif isinstance(obj, (tuple, list)):
+        for o in obj:
+            _record(o, stream)
+
+
 def _need_cuda(*ts):
     for t in ts:
         if t is not None and not t.is_cuda:
             raise AcscError(ACSC_EINVAL, "tensors must live on the GPU")
 
 
-def _in(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
-    """Row-major copy of an input if it is not already contiguous."""
-    return None if t is None else t.contiguous()
+def _in(t: Optional[torch.Tensor], stream=None) -> Optional[torch.Tensor]:
+    """Row-major copy of an input, made on the call's stream, if it is not
+    already contiguous."""
+    if t is None or t.is_contiguous():
+        return t
+    return t.contiguous() if stream is None else _on(stream, torch.Tensor.contiguous, t)
 
 
 def _out(*ts):
@@ -254,6 +283,8 @@ def ac_mask_pack(x: torch.Tensor, K: int, key: MaskKey, vals: Optional[torch.Ten
                  idx: Optional[torch.Tensor] = None, with_idx: bool = True, stream=None):
     """x: [rows, H] (row stride x.stride(0)).  Returns (vals [rows, K], idx
     [rows, K] int16 holding uint16 patterns, or None)."""
+    if stream is not None:
+        return _on(stream, ac_mask_pack, x, K, key, vals, idx, with_idx)
     _need_cuda(x)
     if x.dim() != 2 or x.stride(1) != 1:
         raise AcscError(ACSC_EINVAL, "x must be 2-D with unit column stride")
@@ -264,7 +295,7 @@ def ac_mask_pack(x: torch.Tensor, K: int, key: MaskKey, vals: Optional[torch.Ten
         idx = torch.empty(rows, K, dtype=torch.int16, device=x.device)
     _need_cuda(vals, idx)
     _check(lib.ac_mask_pack(_ptr(x), _dt(x), rows, H, x.stride(0), K, C.byref(key), _ptr(vals),
-                            _ptr(idx), _stream(stream)))
+                            _ptr(idx), _stream()))
     return vals, idx
 
 
@@ -272,6 +303,8 @@ def ac_unpack_scatter(vals: torch.Tensor, H: int, key: MaskKey, scale: float = 1
                       idx: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
                       stream=None) -> torch.Tensor:
     """Dense [rows, H] output (or into ``y``, row stride y.stride(0))."""
+    if stream is not None:
+        return _on(stream, ac_unpack_scatter, vals, H, key, scale, idx, y)
     _need_cuda(vals, idx)
     rows, K = vals.shape
     if y is None:
@@ -280,7 +313,7 @@ def ac_unpack_scatter(vals: torch.Tensor, H: int, key: MaskKey, scale: float = 1
     if y.dim() != 2 or y.stride(1) != 1 or not vals.is_contiguous():
         raise AcscError(ACSC_EINVAL, "vals must be contiguous and y 2-D with unit column stride")
     _check(lib.ac_unpack_scatter(_ptr(vals), _ptr(idx), _dt(vals), rows, H, K, C.byref(key),
-                                 float(scale), _ptr(y), y.stride(0), _stream(stream)))
+                                 float(scale), _ptr(y), y.stride(0), _stream()))
     return y
 
 
@@ -296,6 +329,8 @@ def ac_mask_pack_batched(x: torch.Tensor, K: int, key: MaskKey, vals: Optional[t
     [nlayers, rows, K].  idx_in: [nlayers, rows, K] index lists to pack at
     (no mask evaluated); idx_out: receives the kept positions (int16 holding
     uint16 patterns)."""
+    if stream is not None:
+        return _on(stream, ac_mask_pack_batched, x, K, key, vals, idx_in, idx_out)
     _need_cuda(x, vals, idx_in, idx_out)
     if x.dim() != 3 or x.stride(2) != 1:
         raise AcscError(ACSC_EINVAL, "x must be [nlayers, rows, H] with unit column stride")
@@ -313,7 +348,7 @@ def ac_mask_pack_batched(x: torch.Tensor, K: int, key: MaskKey, vals: Optional[t
         raise AcscError(ACSC_EINVAL, "vals must be [nlayers, rows, K] with contiguous rows")
     _check(lib.ac_mask_pack_batched(_ptr(x), _dt(x), nl, rows, H, x.stride(1), _layer_stride(x), K, C.byref(key),
                                     _ptr(vals), _layer_stride(vals), _ptr(idx_in), _ptr(idx_out), idx_stride,
-                                    _stream(stream)))
+                                    _stream()))
     return vals
 
 
@@ -323,6 +358,8 @@ def ac_unpack_scatter_batched(vals: torch.Tensor, H: int, key: MaskKey, scale: f
     """vals: [nlayers, rows, K].  Returns (or fills) y [nlayers, rows, H].
     idx_in: transmitted or kept index lists; idx_out: receives the positions
     rebuilt from the key."""
+    if stream is not None:
+        return _on(stream, ac_unpack_scatter_batched, vals, H, key, scale, idx_in, idx_out, y)
     _need_cuda(vals, idx_in, idx_out)
     if vals.dim() != 3 or vals.stride(2) != 1 or vals.stride(1) != vals.shape[2]:
         raise AcscError(ACSC_EINVAL, "vals must be [nlayers, rows, K] with contiguous rows")
@@ -340,16 +377,18 @@ def ac_unpack_scatter_batched(vals: torch.Tensor, H: int, key: MaskKey, scale: f
             idx_stride = _layer_stride(t)
     _check(lib.ac_unpack_scatter_batched(_ptr(vals), _layer_stride(vals), _dt(vals), nl, rows, H, K, C.byref(key),
                                          _ptr(idx_in), _ptr(idx_out), idx_stride, float(scale), _ptr(y), y.stride(1),
-                                         _layer_stride(y), _stream(stream)))
+                                         _layer_stride(y), _stream()))
     return y
 
 
 def ac_bern_mask(rows: int, H: int, keep: float, key: MaskKey, device="cuda", stream=None):
     """The Bernoulli mask of a [rows, H] tensor: (row_ptr int64 [rows + 1],
     bits int32 [rows, ceil(H / 32)] holding uint32 patterns)."""
+    if stream is not None:
+        return _on(stream, ac_bern_mask, rows, H, keep, key, device)
     row_ptr = torch.empty(rows + 1, dtype=torch.int64, device=device)
     bits = torch.empty(max(rows, 1), (H + 31) // 32, dtype=torch.int32, device=device)[:rows]
-    _check(lib.ac_bern_mask(rows, H, float(keep), C.byref(key), _ptr(row_ptr), _ptr(bits), _stream(stream)))
+    _check(lib.ac_bern_mask(rows, H, float(keep), C.byref(key), _ptr(row_ptr), _ptr(bits), _stream()))
     return row_ptr, bits
 
 
@@ -358,6 +397,8 @@ def ac_bern_pack(x: torch.Tensor, row_ptr: torch.Tensor, bits: torch.Tensor, nnz
     """Packed values [nnz] (and uint16 indices as int16, or None) of x [rows, H]
     under the mask (row_ptr, bits).  nnz defaults to row_ptr[-1] (a host
     read, which synchronises)."""
+    if stream is not None:
+        return _on(stream, ac_bern_pack, x, row_ptr, bits, nnz, with_idx)
     _need_cuda(x, row_ptr, bits)
     if x.dim() != 2 or x.stride(1) != 1:
         raise AcscError(ACSC_EINVAL, "x must be 2-D with unit column stride")
@@ -367,13 +408,15 @@ def ac_bern_pack(x: torch.Tensor, row_ptr: torch.Tensor, bits: torch.Tensor, nnz
     vals = torch.empty(max(nnz, 1), dtype=x.dtype, device=x.device)[:nnz]
     idx = torch.empty(max(nnz, 1), dtype=torch.int16, device=x.device)[:nnz] if with_idx else None
     _check(lib.ac_bern_pack(_ptr(x), _dt(x), rows, H, x.stride(0), _ptr(row_ptr), _ptr(bits), _ptr(vals),
-                            _ptr(idx), nnz, _stream(stream)))
+                            _ptr(idx), nnz, _stream()))
     return vals, idx
 
 
 def ac_bern_unpack(vals: torch.Tensor, H: int, row_ptr: torch.Tensor, bits: torch.Tensor, scale: float = 1.0,
                    y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Dense [rows, H]: scale * value at the kept entries, +0 elsewhere."""
+    if stream is not None:
+        return _on(stream, ac_bern_unpack, vals, H, row_ptr, bits, scale, y)
     _need_cuda(vals, row_ptr, bits)
     rows = row_ptr.numel() - 1
     if y is None:
@@ -382,7 +425,7 @@ def ac_bern_unpack(vals: torch.Tensor, H: int, row_ptr: torch.Tensor, bits: torc
     if y.dim() != 2 or y.stride(1) != 1 or not vals.is_contiguous():
         raise AcscError(ACSC_EINVAL, "vals must be contiguous and y 2-D with unit column stride")
     _check(lib.ac_bern_unpack(_ptr(vals), _dt(vals), rows, H, _ptr(row_ptr), _ptr(bits), vals.numel(),
-                              float(scale), _ptr(y), y.stride(0), _stream(stream)))
+                              float(scale), _ptr(y), y.stride(0), _stream()))
     return y
 
 
@@ -403,6 +446,8 @@ def sc_build_prior(G_anc: Optional[torch.Tensor], M: torch.Tensor, r: int, beta:
                    V_warm: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
                    out=None, dtype: Optional[torch.dtype] = None, stream=None):
     """EMA of G_anc into M (fp32, in place), then (U, s, V, d).  Returns them."""
+    if stream is not None:
+        return _on(stream, sc_build_prior, G_anc, M, r, beta, tau, oversample, power_iters, seed, V_warm, ws, out, dtype)
     _need_cuda(G_anc, M, V_warm)
     G_anc, V_warm = _in(G_anc), _in(V_warm)
     _out(M)
@@ -418,7 +463,7 @@ def sc_build_prior(G_anc: Optional[torch.Tensor], M: torch.Tensor, r: int, beta:
     code = BF16 if dt == torch.bfloat16 else F32
     _check(lib.sc_build_prior(_ptr(G_anc), code, _ptr(M), m, n, float(beta), r, oversample,
                               power_iters, float(tau), _ptr(V_warm), seed, _ptr(U), _ptr(s),
-                              _ptr(V), _ptr(d), _ptr(ws), ws.numel(), _stream(stream)))
+                              _ptr(V), _ptr(d), _ptr(ws), ws.numel(), _stream()))
     return U, s, V, d
 
 
@@ -426,6 +471,8 @@ def sc_correct(G: torch.Tensor, U: torch.Tensor, d: torch.Tensor, V: torch.Tenso
                out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
                stream=None) -> torch.Tensor:
     """G_proj = alpha G + (1 - alpha) U diag(d) U^T G V diag(d) V^T."""
+    if stream is not None:
+        return _on(stream, sc_correct, G, U, d, V, alpha, out, ws)
     _need_cuda(G, U, d, V, out)
     G, U, d, V = _in(G), _in(U), _in(d), _in(V)
     _out(out)
@@ -436,7 +483,7 @@ def sc_correct(G: torch.Tensor, U: torch.Tensor, d: torch.Tensor, V: torch.Tenso
     if ws is None:
         ws = workspace(m, n, r, 0, G.dtype, G.device)
     _check(lib.sc_correct(_ptr(G), _dt(G), m, n, _ptr(U), _ptr(d), _ptr(V), r, float(alpha),
-                          _ptr(out), _ptr(ws), ws.numel(), _stream(stream)))
+                          _ptr(out), _ptr(ws), ws.numel(), _stream()))
     return out
 
 
@@ -448,6 +495,8 @@ def sc_correct_static(G: torch.Tensor, U: torch.Tensor, d: torch.Tensor, V: torc
     """sc_correct on the library's own device scratch (no workspace; for
     callers that cannot allocate).  ``out`` must be given by a caller that
     cannot allocate; calls that overlap on one GPU race."""
+    if stream is not None:
+        return _on(stream, sc_correct_static, G, U, d, V, alpha, out)
     _need_cuda(G, U, d, V, out)
     for t in (G, U, d, V):
         if not t.is_contiguous():
@@ -458,7 +507,7 @@ def sc_correct_static(G: torch.Tensor, U: torch.Tensor, d: torch.Tensor, V: torc
     if out is None:
         out = torch.empty_like(G)
     _check(lib.sc_correct_static(_ptr(G), _dt(G), m, n, _ptr(U), _ptr(d), _ptr(V), r, float(alpha), _ptr(out),
-                                 _stream(stream)))
+                                 _stream()))
     return out
 
 
@@ -496,8 +545,8 @@ def _build_batched(fn, items, r, beta, tau, oversample, power_iters, seed, dtype
     arr = (ScMatrix * max(len(items), 1))()
     keep = []
     for i, it in enumerate(items):
-        G, M, (U, s, V, d), ws = _in(it.get("G_anc")), it["M"], it["out"], it["ws"]
-        Vw = _in(it.get("V_warm"))
+        G, M, (U, s, V, d), ws = _in(it.get("G_anc"), stream), it["M"], it["out"], it["ws"]
+        Vw = _in(it.get("V_warm"), stream)
         _need_cuda(G, M, U, s, V, d, ws, Vw)
         _out(M, U, s, V, d)
         keep += [G, Vw]
@@ -535,8 +584,8 @@ def sc_correct_batched(items, r: int, alpha: float, dtype: torch.dtype = torch.b
     arr = (ScMatrix * max(len(items), 1))()
     keep = []
     for i, it in enumerate(items):
-        G, (U, d, V), out, ws = _in(it["G"]), it["prior"], it["out"], it["ws"]
-        U, d, V = _in(U), _in(d), _in(V)
+        G, (U, d, V), out, ws = _in(it["G"], stream), it["prior"], it["out"], it["ws"]
+        U, d, V = _in(U, stream), _in(d, stream), _in(V, stream)
         _need_cuda(G, U, d, V, out, ws)
         _out(out)
         keep += [G, U, d, V]
@@ -565,8 +614,8 @@ def sc_correct_adamw_batched(items, r: int, alpha: float, lr: float, beta1: floa
     st = (AdamwState * max(len(items), 1))()
     keep = []
     for i, it in enumerate(items):
-        G, (U, d, V), ws, (W, m1, m2) = _in(it["G"]), it["prior"], it["ws"], it["state"]
-        U, d, V = _in(U), _in(d), _in(V)
+        G, (U, d, V), ws, (W, m1, m2) = _in(it["G"], stream), it["prior"], it["ws"], it["state"]
+        U, d, V = _in(U, stream), _in(d, stream), _in(V, stream)
         _need_cuda(G, U, d, V, ws, W, m1, m2, norm_out)
         _out(W, m1, m2)
         for t in (W, m1, m2):
@@ -598,7 +647,7 @@ def _psgd(name: str, items, r: int, dtype: torch.dtype, stream):
     arr = (PsgdMatrix * max(len(items), 1))()
     keep = []
     for i, it in enumerate(items):
-        G, E, P, Q, out, ws = _in(it.get("G")), it["E"], it["P"], it["Q"], it.get("out"), it["ws"]
+        G, E, P, Q, out, ws = _in(it.get("G"), stream), it["E"], it["P"], it["Q"], it.get("out"), it["ws"]
         _need_cuda(G, E, P, Q, out, ws)
         _out(E, P, Q, out)
         for t, shape in ((E, None), (P, (E.shape[0], r)), (Q, (E.shape[1], r))):
@@ -649,31 +698,6 @@ def _act(act: str) -> int:
 
 def _raw_stream() -> int:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
-
-
-def _on(stream, fn, *args):
-    """fn(*args) on `stream`, if that is not the current one: everything it
-    allocates comes from that stream's memory, so it waits for nothing that the
-    current stream still does with a block it freed.  What it is given is kept
-    from reuse until `stream` has got past the call, what it returns until the
-    current stream has got past its use of it."""
-    here = torch.cuda.current_stream()
-    if stream == here:
-        return fn(*args)
-    with torch.cuda.stream(stream):
-        out = fn(*args)
-    _record(args, stream)
-    _record(out, here)
-    return out
-
-
-def _record(obj, stream):
-    if isinstance(obj, torch.Tensor):
-        if obj.is_cuda:
-            obj.record_stream(stream)
-    elif isinstance(obj, (tuple, list)):
-        for o in obj:
-            _record(o, stream)
 
 
 def _rows(t: torch.Tensor, shape, dtype: torch.dtype, name: str) -> int:

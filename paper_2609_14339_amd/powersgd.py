@@ -13,7 +13,7 @@ from typing import List, Optional, Sequence, Tuple
 
 import torch
 
-from . import SC_KMAX, psgd_step, psgd_workspace
+from . import SC_KMAX, _on, psgd_step, psgd_workspace
 
 
 def rank_for_ratio(m: int, n: int, ratio: float = 64.0) -> int:
@@ -41,11 +41,13 @@ class PowerSGDState:
              stream=None) -> List[torch.Tensor]:
         """One compressor step on every matrix: returns the decompressed
         gradients (outs, or new tensors; an out may be its grad)."""
+        if stream is not None:
+            return _on(stream, self.step, grads, outs)
         if outs is None:
             outs = [torch.empty_like(g) for g in grads]
         for r, idx in self.groups.items():
             items = [dict(self.items[i], G=grads[i], out=outs[i]) for i in idx]
-            psgd_step(items, r, self.dtype, stream)
+            psgd_step(items, r, self.dtype)
         return list(outs)
 
     def sent_elements(self) -> int:
