@@ -77,8 +77,9 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void ln_forward_kernel(Fwd<T> 
     constexpr int RPB = NT < 256 ? 256 / NT : 1;
     __shared__ float slots[2][NT / 64];
     const int t = threadIdx.x % NT;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * RPB + (RPB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0);
-    if (RPB > 1 && row >= p.rows)
+    const int64_t row = (blockIdx.y * static_cast<int64_t>(gridDim.x) + blockIdx.x) * RPB +
+                        (RPB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0);
+    if (row >= p.rows)
         return;
     float v[CH][8];
 #pragma unroll
@@ -540,7 +541,9 @@ int run_forward(const Fwd<T> &p, hipStream_t st)
 {
     const Shape s = forward_shape(p.H, sizeof(T) == 4);
     const int64_t blocks = s.nt == 64 ? (p.rows + 3) / 4 : p.rows;
-    const dim3 grid(static_cast<unsigned>(blocks));
+    // a grid has under 2^32 threads along x: past 2^20 workgroups it goes on along y
+    const int64_t across = std::min<int64_t>(blocks, 1 << 20);
+    const dim3 grid(static_cast<unsigned>(across), static_cast<unsigned>((blocks + across - 1) / across));
     const char *tag = AGAIN ? "ln_recompute" : "ln_forward";
 #define ACSC_CASE(NT, CH)                                                                                       \
     if (s.nt == NT && s.ch == CH)                                                                             \
