@@ -537,7 +537,9 @@ typedef enum lin_op { LIN_FORWARD = 0, LIN_BACKWARD_INPUT = 1, LIN_BACKWARD_WEIG
  * n_out outputs on `rows` tokens, whatever its epilogue.  For operands (x, W,
  * dz) that are 4-byte aligned with row strides under 2^21 elements, in bf16
  * even ones; lin_workspace_size_unaligned covers every alignment and stride
- * (other operands are copied into the workspace first). */
+ * (other operands are copied into the workspace first).  A product that takes
+ * a launch of 2^32 threads or more is refused here and by its call with
+ * ACSC_EINVAL: outputs of 2^38 elements or so, or of over 2^31 - 128 rows. */
 int lin_workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, size_t *bytes);
 int lin_workspace_size_unaligned(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, size_t *bytes);
 

@@ -59,6 +59,10 @@ struct Kept {
     int act;
 };
 
+// Fragments of 16 rows of a wave, and waves, for a tile of TM rows and T columns.
+constexpr int fragments(int TM) { return TM < 64 ? 1 : TM / 64; }
+constexpr int waves(int TM, int T) { return TM / (16 * fragments(TM)) * (T < 128 ? 1 : T / 128); }
+
 // What the epilogue reads beside the sums for eight columns of a row: the
 // residual (forward), the kept pre-activation or its codes and scale (gate),
 // or the output to add to (weight).

@@ -522,10 +522,14 @@ inline int check_ws(const void *ws, size_t have, size_t need)
     return ACSC_OK;
 }
 
-// The largest tile grid: blockIdx.x is 32 bits.
+// The largest launch of tiles: a grid has under 2^32 threads along x.
 inline int check_tiles(const Plan &p)
 {
-    ACSC_CHECK_ARG(p.few || static_cast<int64_t>(p.tm) * p.tn < (1ll << 31), ACSC_EINVAL, "product too large");
+    if (p.few)
+        return ACSC_OK;
+    const int64_t tiles = static_cast<int64_t>(p.tm) * p.tn, threads = 64 * waves(p.rows, p.tile);
+    ACSC_CHECK_ARG(tiles * threads < (1ll << 32) && (p.whole + (tiles - p.whole) * p.splits) * threads < (1ll << 32),
+                   ACSC_EINVAL, "product too large: %lld tiles of %d x %d", (long long)tiles, p.rows, p.tile);
     return ACSC_OK;
 }
 
@@ -559,9 +563,14 @@ static int workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dty
     };
     const bool a = best(s.acol, s.acol ? s.M : s.K), b = best(s.bcol, s.bcol ? s.N : s.K);
     // with any alignment: the most that either operand's copy, or its absence, takes
-    *bytes = plan_of(kind, s, dt, a, b).bytes();
-    for (int copies = 1; any && copies < 4; ++copies)
-        *bytes = std::max(*bytes, plan_of(kind, s, dt, a && !(copies & 1), b && !(copies & 2)).bytes());
+    size_t most = 0;
+    for (int copies = 0; copies < (any ? 4 : 1); ++copies) {
+        const Plan p = plan_of(kind, s, dt, a && !(copies & 1), b && !(copies & 2));
+        if (int rc = check_tiles(p))
+            return rc;
+        most = std::max(most, p.bytes());
+    }
+    *bytes = most;
     if (kind == kWeight && rows > few_tokens(kind, true))
         *bytes += recomputed_bytes(rows, n_in, dt);
     return ACSC_OK;

@@ -245,10 +245,6 @@ struct Frag<float, COL> {
     static constexpr int kBlock = 32;
 };
 
-// Fragments of 16 rows of a wave, and waves, for a tile of TM rows.
-constexpr int fragments(int TM) { return TM < 64 ? 1 : TM / 64; }
-constexpr int waves(int TM, int T) { return TM / (16 * fragments(TM)) * (T < 128 ? 1 : T / 128); }
-
 // Stages of A: a third one where it fits beside the other workgroup (see the
 // step below); B has two.
 constexpr int a_stages(int TM) { return TM < 128 ? 2 : 3; }

@@ -33,3 +33,23 @@ def test_weight_gradient_of_nearly_2_31_rows(pk, dt, n_in, n_out, short):
         return b.value - recomputed - copies - up(slices * n_out * 4, 256)
 
     assert pieces((1 << 31) - short) == pieces(1 << 30) >= 0
+
+
+EINVAL = -1
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("op", [0, 1])
+def test_products_of_more_threads_than_a_launch_has(pk, op, dt):
+    """256 threads to 128 rows: 2^24 tiles are one too many, and said so before anything is launched."""
+    b = C.c_size_t(7)
+    for size in (pk.lib.lin_workspace_size, pk.lib.lin_workspace_size_unaligned):
+        assert size(op, (1 << 31) - 128, 8, 8, dt, C.byref(b)) == 0
+        assert size(op, (1 << 31) - 127, 8, 8, dt, C.byref(b)) == EINVAL and b"too large" in pk.lib.acsc_last_error()
+        assert size(op, 1 << 30, 1 << 22, 1 << 22, dt, C.byref(b)) == EINVAL and b.value == 0
+    assert pk.lib.lin_workspace_size(2, 100, 1 << 22, 1 << 22, dt, C.byref(b)) == EINVAL
+    W = 0x10000
+    call = (lambda rows: pk.lib.lin_forward(W, 8, dt, rows, 8, 8, 2 * W, 8, None, 0, None, 0, 3 * W, 8, None, 8, None, W,
+                                            1 << 62, None)) if op == 0 else \
+        (lambda rows: pk.lib.lin_backward_input(W, 8, dt, rows, 8, 8, 2 * W, 8, 0, None, 8, None, 3 * W, 8, W, 1 << 62, None))
+    assert call((1 << 31) - 1) == EINVAL and b"too large" in pk.lib.acsc_last_error()
