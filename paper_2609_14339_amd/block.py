@@ -11,6 +11,7 @@ whole (checkpoint=False).  The norm's output and the hidden activation are
 computed again from them.  layer_norm and linear are its parts as nodes of
 their own, for blocks of another form.
 
+The ops are differentiable once: the gradient of a gradient raises an error.
 Gradients of W1 and W2 come out in the weights' dtype, as sc_correct takes
 them.  Every operation is a library call; this module only wires them into
 autograd.
@@ -18,6 +19,7 @@ autograd.
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import (Q8, lin_backward_act, lin_backward_input, lin_backward_weight, lin_forward, ln_backward, ln_forward,
                ln_recompute)
@@ -50,6 +52,7 @@ class _LayerNorm(torch.autograd.Function):
         return y.view(x.shape)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g):
         mean, rstd, gamma, beta, a, b = ctx.saved_tensors
         dx, dgamma, dbeta = ln_backward(_flat(g), _load(a, b), mean, rstd, gamma)
@@ -69,6 +72,7 @@ class _Linear(torch.autograd.Function):
         return y.view(*x.shape[:-1], W.shape[0])
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g):
         x2, W, bias, a, b = ctx.saved_tensors
         dz = g2 = _flat(g)
@@ -94,6 +98,7 @@ class _MlpBlock(torch.autograd.Function):
         return out.view(x.shape)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g):
         mean, rstd, gamma, beta, W1, b1, W2, b2, *kept = ctx.saved_tensors
         x, z = _load(*kept[:2]), _load(*kept[2:])
