@@ -857,12 +857,13 @@ def ln_backward(dy: torch.Tensor, src: Union[torch.Tensor, Q8], mean: torch.Tens
                 gamma: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None,
                 dx: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None,
                 dbeta: Optional[torch.Tensor] = None, accumulate: bool = False, ws: Optional[torch.Tensor] = None,
-                stream=None):
+                stream=None, weights: bool = True):
     """(dx, dgamma, dbeta) of ln_forward from x or its checkpoint; add: the
     gradient that reaches x past the norm.  dgamma, dbeta: fp32 [H]; with
-    accumulate they are given and added to."""
+    accumulate they are given and added to; without weights they are not
+    formed, and None."""
     if stream is not None:
-        return _on(stream, ln_backward, dy, src, mean, rstd, gamma, add, dx, dgamma, dbeta, accumulate, ws)
+        return _on(stream, ln_backward, dy, src, mean, rstd, gamma, add, dx, dgamma, dbeta, accumulate, ws, None, weights)
     shape = rows, H = _two_d(dy, "dy")
     dtype, dev = dy.dtype, dy.device
     lddy = _rows(dy, shape, dtype, "dy")
@@ -874,16 +875,21 @@ def ln_backward(dy: torch.Tensor, src: Union[torch.Tensor, Q8], mean: torch.Tens
         dx, lddx = torch.empty((rows, H), dtype=dtype, device=dev), max(H, 1)
     else:
         lddx = _rows(dx, shape, dtype, "dx")
-    if dgamma is None:
-        dgamma = torch.empty(H, dtype=torch.float32, device=dev)
-    if dbeta is None:
-        dbeta = torch.empty(H, dtype=torch.float32, device=dev)
+    pdg = pdb = wp = keep = None
+    wn = 0
+    if weights:
+        if dgamma is None:
+            dgamma = torch.empty(H, dtype=torch.float32, device=dev)
+        if dbeta is None:
+            dbeta = torch.empty(H, dtype=torch.float32, device=dev)
+        pdg, pdb = _vec(dgamma, H, torch.float32, "dgamma"), _vec(dbeta, H, torch.float32, "dbeta")
+        wp, wn, keep = _ws(_ln_bytes(rows, H), ws, dev)
+    elif dgamma is not None or dbeta is not None:
+        raise AcscError(ACSC_EINVAL, "dgamma and dbeta are given, but not wanted")
     pm, pr = _vec(mean, rows, torch.float32, "mean"), _vec(rstd, rows, torch.float32, "rstd")
     pg = None if gamma is None else _vec(gamma, H, dtype, "gamma")
-    wp, wn, keep = _ws(_ln_bytes(rows, H), ws, dev)
     rc = lib.ln_backward(dy.data_ptr(), lddy, p, ld, q, _dt(dy), rows, H, pm, pr, pg, pa, ldadd, dx.data_ptr(), lddx,
-                         _vec(dgamma, H, torch.float32, "dgamma"), _vec(dbeta, H, torch.float32, "dbeta"),
-                         int(accumulate), wp, wn, _raw_stream())
+                         pdg, pdb, int(accumulate), wp, wn, _raw_stream())
     if rc:
         _check(rc)
     return dx, dgamma, dbeta

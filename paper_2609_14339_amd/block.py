@@ -55,7 +55,8 @@ class _LayerNorm(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, g):
         mean, rstd, gamma, beta, a, b = ctx.saved_tensors
-        dx, dgamma, dbeta = ln_backward(_flat(g), _load(a, b), mean, rstd, gamma)
+        need = ctx.needs_input_grad
+        dx, dgamma, dbeta = ln_backward(_flat(g), _load(a, b), mean, rstd, gamma, weights=need[1] or need[2])
         return dx.view(g.shape), _as(dgamma, gamma), _as(dbeta, beta), None, None
 
 
@@ -75,14 +76,15 @@ class _Linear(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, g):
         x2, W, bias, a, b = ctx.saved_tensors
+        need = ctx.needs_input_grad
         dz = g2 = _flat(g)
-        if ctx.act != "none":
+        if ctx.act != "none" and any(need[:3]):
             dz = lin_backward_act(g2, _load(a, b), ctx.act)
         dx = dW = db = None
-        if ctx.needs_input_grad[0]:
+        if need[0]:
             dx = lin_backward_input(dz, W).view(*g.shape[:-1], W.shape[1])
-        if ctx.needs_input_grad[1] or ctx.needs_input_grad[2]:
-            dW, db = lin_backward_weight(dz, x2, bias=bias is not None)
+        if need[1] or need[2]:
+            dW, db = lin_backward_weight(dz, x2, bias=need[2])
         return dx, dW, _as(db, bias), g if ctx.has_residual else None, None, None
 
 
@@ -103,15 +105,21 @@ class _MlpBlock(torch.autograd.Function):
         mean, rstd, gamma, beta, W1, b1, W2, b2, *kept = ctx.saved_tensors
         x, z = _load(*kept[:2]), _load(*kept[2:])
         g2 = _flat(g)
-        dW2, db2 = lin_backward_weight(g2, z, act=ctx.act, bias=b2 is not None)
-        dz = lin_backward_input(g2, W2, act=ctx.act, z=z)
-        y = ln_recompute(x, mean, rstd, gamma, beta, dtype=g2.dtype)
-        dW1, db1 = lin_backward_weight(dz, y, bias=b1 is not None)
-        del y
-        dy = lin_backward_input(dz, W1)
-        dx, dgamma, dbeta = ln_backward(dy, x, mean, rstd, gamma, add=g2)
-        return (dx.view(g.shape), _as(dgamma, gamma), _as(dbeta, beta), dW1, _as(db1, b1), dW2, _as(db2, b2), None, None,
-                None)
+        need = ctx.needs_input_grad
+        dx = dgamma = dbeta = dW1 = db1 = dW2 = db2 = None
+        if need[5] or need[6]:
+            dW2, db2 = lin_backward_weight(g2, z, act=ctx.act, bias=need[6])
+        if any(need[:5]):
+            dz = lin_backward_input(g2, W2, act=ctx.act, z=z)
+            if need[3] or need[4]:
+                y = ln_recompute(x, mean, rstd, gamma, beta, dtype=g2.dtype)
+                dW1, db1 = lin_backward_weight(dz, y, bias=need[4])
+                del y
+            if any(need[:3]):
+                dy = lin_backward_input(dz, W1)
+                dx, dgamma, dbeta = ln_backward(dy, x, mean, rstd, gamma, add=g2, weights=need[1] or need[2])
+                dx = dx.view(g.shape)
+        return (dx, _as(dgamma, gamma), _as(dbeta, beta), dW1, _as(db1, b1), dW2, _as(db2, b2), None, None, None)
 
 
 def layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, checkpoint: bool = False):

@@ -36,3 +36,58 @@ def test_second_derivatives_raise(ops, name):
     (g,) = torch.autograd.grad(out.square().sum(), p["x"], create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable|differentiate twice"):
         (p["x"].sum() + g.square().sum()).backward()
+
+
+def launches(fn):
+    """What fn returns, and the names of the kernels that it launches."""
+    import paper_2609_14339_amd as pk
+    torch.cuda.synchronize()
+    pk.acsc_stats_enable(True)
+    out = fn()
+    torch.cuda.synchronize()
+    st = {k: n for k, (n, _) in pk.acsc_stats_read().items()}
+    pk.acsc_stats_enable(False)
+    return out, st
+
+
+WEIGHT, INPUT, NORM = "lin_backward_weight", "lin_backward_input", "ln_backward"
+
+
+@pytest.mark.parametrize("name,wanted,run", [
+    ("mlp_block", ["x", "gamma", "beta", "W1", "b1", "W2", "b2"], {WEIGHT: 2, INPUT: 2, NORM: 1, "ln_recompute": 1,
+                                                                    "ln_join": 1}),
+    ("mlp_block", ["x"], {INPUT: 2, NORM: 1}),                                  # everything else is frozen
+    ("mlp_block", ["x", "gamma", "beta"], {INPUT: 2, NORM: 1, "ln_join": 1}),
+    ("mlp_block", ["W1"], {INPUT: 1, WEIGHT: 1, "ln_recompute": 1}),            # the first block, its norm frozen
+    ("mlp_block", ["W2", "b2"], {WEIGHT: 1}),
+    ("mlp_block", ["x", "b1"], {INPUT: 2, WEIGHT: 1, NORM: 1, "ln_recompute": 1}),
+    ("layer_norm", ["x"], {NORM: 1}),
+    ("layer_norm", ["beta"], {NORM: 1, "ln_join": 1}),
+    ("linear", ["x"], {"lin_backward_act": 1, INPUT: 1}),
+    ("linear", ["W1", "b1"], {"lin_backward_act": 1, WEIGHT: 1}),
+    ("linear", ["W1"], {"lin_backward_act": 1, WEIGHT: 1}),
+])
+def test_only_wanted_gradients_are_computed(ops, name, wanted, run):
+    p = make()
+    full = outputs(ops, p)[name]()
+    dy = torch.randn_like(full)
+    used = [k for k in wanted]
+    want = torch.autograd.grad(full, [p[k] for k in used], dy)
+    for k, t in p.items():
+        t.requires_grad_(k in wanted)
+    out = outputs(ops, p)[name]()
+    got, st = launches(lambda: torch.autograd.grad(out, [p[k] for k in used], dy))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert {k: n for k, n in st.items() if k not in ("lin_prepare", "lin_join")} == run
+
+
+def test_norm_gradient_without_its_weights(ops):
+    import paper_2609_14339_amd as pk
+    p = {k: t.detach() for k, t in make().items()}
+    _, mean, rstd, _ = pk.ln_forward(p["x"], p["gamma"], p["beta"])
+    dy = torch.randn_like(p["x"])
+    dx, dgamma, dbeta = pk.ln_backward(dy, p["x"], mean, rstd, p["gamma"], weights=False)
+    assert dgamma is None and dbeta is None
+    assert torch.equal(dx, pk.ln_backward(dy, p["x"], mean, rstd, p["gamma"])[0])
+    with pytest.raises(pk.AcscError, match="not wanted"):
+        pk.ln_backward(dy, p["x"], mean, rstd, p["gamma"], dgamma=torch.empty(64, device="cuda"), weights=False)
