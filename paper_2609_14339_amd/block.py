@@ -69,7 +69,7 @@ class _Linear(torch.autograd.Function):
         y, z = lin_forward(x2, W, bias, act, r2, keep)
         ctx.act = act
         ctx.save_for_backward(x2, W, bias, *_save(z))
-        ctx.has_residual = residual is not None
+        ctx.residual = None if residual is None else residual.shape
         return y.view(*x.shape[:-1], W.shape[0])
 
     @staticmethod
@@ -85,7 +85,7 @@ class _Linear(torch.autograd.Function):
             dx = lin_backward_input(dz, W).view(*g.shape[:-1], W.shape[1])
         if need[1] or need[2]:
             dW, db = lin_backward_weight(dz, x2, bias=need[2])
-        return dx, dW, _as(db, bias), g if ctx.has_residual else None, None, None
+        return dx, dW, _as(db, bias), g.reshape(ctx.residual) if need[3] else None, None, None
 
 
 class _MlpBlock(torch.autograd.Function):

@@ -91,3 +91,16 @@ def test_norm_gradient_without_its_weights(ops):
     assert torch.equal(dx, pk.ln_backward(dy, p["x"], mean, rstd, p["gamma"])[0])
     with pytest.raises(pk.AcscError, match="not wanted"):
         pk.ln_backward(dy, p["x"], mean, rstd, p["gamma"], dgamma=torch.empty(64, device="cuda"), weights=False)
+
+
+@pytest.mark.parametrize("shape", [(2, 3, 5), (6, 5, 1), (30,), (1, 30, 1)])
+def test_residual_of_another_leading_shape(ops, shape):
+    """The rows of the residual are those of the output; its gradient comes back in its own shape."""
+    p = make(rows=30)
+    x, W = p["x"].detach().view(5, 6, 64), p["W1"]
+    r = torch.randn(*shape, 96, device="cuda", requires_grad=True)
+    out = ops.linear(x, W, residual=r)
+    dy = torch.randn_like(out)
+    dr, dW = torch.autograd.grad(out, [r, W], dy)
+    assert dr.shape == r.shape and torch.equal(dr.reshape(-1), dy.reshape(-1))
+    assert torch.equal(dW, torch.autograd.grad(ops.linear(x, W), [W], dy)[0])
