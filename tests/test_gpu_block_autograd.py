@@ -104,3 +104,47 @@ def test_residual_of_another_leading_shape(ops, shape):
     dr, dW = torch.autograd.grad(out, [r, W], dy)
     assert dr.shape == r.shape and torch.equal(dr.reshape(-1), dy.reshape(-1))
     assert torch.equal(dW, torch.autograd.grad(ops.linear(x, W), [W], dy)[0])
+
+
+def rel(a, b):
+    return float((a.double() - b.double()).norm().detach() / b.double().norm().detach())
+
+
+# A value of a checkpoint is off by at most a / 254 of its group's largest: for normal values 3.5 / 254 / sqrt 3 = 0.8%
+# of their scale.  It enters these gradients once, through act' (second derivative at most 0.8 against slopes of 0.5 in
+# the mean) or through the normalised input: under 2%.
+@pytest.mark.parametrize("act", ["gelu", "silu", "none"])
+def test_linear_from_its_checkpoint(ops, act):
+    import paper_2609_14339_amd as pk
+    p = make(rows=150)
+    x, W, b = p["x"], p["W1"], p["b1"]
+    out = ops.linear(x, W, b, act=act, checkpoint=True)
+    dy = torch.randn_like(out)
+    got = torch.autograd.grad(out, [x, W, b], dy)
+    x64, W64, b64 = (t.detach().double().requires_grad_() for t in (x, W, b))
+    z = x64 @ W64.t() + b64
+    a = {"gelu": lambda: 0.5 * z * torch.erfc(-z / math.sqrt(2)), "silu": lambda: z * torch.sigmoid(z), "none": lambda: z}
+    want = torch.autograd.grad(a[act](), [x64, W64, b64], dy.double())
+    for g, w in zip(got, want):
+        assert rel(g, w) <= (2e-2 if act != "none" else 1e-5)
+    # the library's calls in turn
+    with torch.no_grad():
+        y, q = pk.lin_forward(x, W, b, act, keep="q8")
+        dz = pk.lin_backward_act(dy, q, act)
+        dW, db = pk.lin_backward_weight(dz, x)
+        assert torch.equal(y, out)
+        assert all(torch.equal(g, w) for g, w in zip(got, (pk.lin_backward_input(dz, W), dW, db)))
+
+
+def test_norm_from_its_checkpoint(ops):
+    p = make(H=300, rows=130)
+    out = ops.layer_norm(p["x"], p["gamma"], p["beta"], checkpoint=True)
+    dy = torch.randn_like(out)
+    names = ["x", "gamma", "beta"]
+    got = torch.autograd.grad(out, [p[k] for k in names], dy)
+    p64 = {k: p[k].detach().double().requires_grad_() for k in names}
+    ref = torch.nn.functional.layer_norm(p64["x"], (300,), p64["gamma"], p64["beta"], 1e-5)
+    want = torch.autograd.grad(ref, [p64[k] for k in names], dy.double())
+    assert rel(out, ref) <= 1e-6
+    for k, g, w in zip(names, got, want):
+        assert rel(g, w) <= (1e-5 if k == "beta" else 2e-2), k
