@@ -303,15 +303,44 @@ __device__ __forceinline__ uint32_t max16(uint32_t x)
 // silu(z) = z s, silu'(z) = s (1 + z (1 - s)), s = 1 / (1 + exp(-z)), with
 // s and 1 - s both from exp(-|z|), so that neither is a difference.
 //
-// T is the type that the result is rounded to.  For fp32, Phi comes from the
-// library's erf.  For bf16 (half a unit: 2^-8) Phi(-|z|) is
-//   (a1 t + .. + a5 t^5) exp(-z^2 / 2) / 2,  t = 1 / (1 + p |z| / sqrt 2)
-// (Abramowitz & Stegun, Handbook of Mathematical Functions, 7.1.26: within
-// 0.75e-7), and exponentials and reciprocals are the hardware's (one unit of
-// 2^-23): a dozen instructions where erf takes some 40, in epilogues that
+// T is the type that the result is rounded to.  Phi is formed from its tail
+// q = Phi(-|z|), as q or 1 - q, so that it keeps its relative accuracy where it
+// is small.
+//
+// bf16 (half a unit: 2^-8): q = (a1 t + .. + a5 t^5) exp(-z^2 / 2) / 2,
+// t = 1 / (1 + p |z| / sqrt 2) (Abramowitz & Stegun, Handbook of Mathematical
+// Functions, 7.1.26: within 0.75e-7), and exponentials and reciprocals are the
+// hardware's (one unit of 2^-23): a dozen instructions in epilogues that
 // nothing hides (see the forward product's figures).
+//
+// fp32: q = p(t) exp(-z^2 / 2) / (|z| + 4), t = (|z| - 4) / (|z| + 4), p the
+// polynomial of degree 9 that interpolates (x + 4) Phi(-x) exp(x^2 / 2) at the
+// Chebyshev points of t in -1 .. 1 (within 4e-8 of it, relative): q within 7 +
+// 1.2 z^2 units of 2^-24 of itself, 3 of 1 near 0; 0 from about -13.2 on, where
+// it leaves the normal range.  Decoding 8192 x 28672 through gelu takes 356 us;
+// by the library's erfc, as accurate, 435; by 1 + erf, which has lost 4% of Phi
+// at -5 and all of it at -6, 352.
+template <typename T>
 __device__ __forceinline__ float normal_tail(float z, float &e)
 {
+    if (sizeof(T) == 4) {
+        const float x = fminf(fabsf(z), 64.f), d = x + 4.f;
+        float r = __builtin_amdgcn_rcpf(d);
+        r = __builtin_fmaf(__builtin_fmaf(-d, r, 1.f), r, r);
+        const float t = __builtin_fmaf(-8.f, r, 1.f);
+        e = __builtin_amdgcn_exp2f(-0.72134752044448170f * x * x);
+        float q = -0.000162616314f;
+        q = __builtin_fmaf(q, t, 0.000129340129f);
+        q = __builtin_fmaf(q, t, 0.00157575205f);
+        q = __builtin_fmaf(q, t, -0.00347619643f);
+        q = __builtin_fmaf(q, t, -0.00752125541f);
+        q = __builtin_fmaf(q, t, 0.0603953153f);
+        q = __builtin_fmaf(q, t, -0.186524183f);
+        q = __builtin_fmaf(q, t, 0.387137562f);
+        q = __builtin_fmaf(q, t, -0.607896566f);
+        q = __builtin_fmaf(q, t, 0.755285144f);
+        return q * r * e;
+    }
     const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
     e = __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z);
     float q = 0.5f * 1.061405429f;
@@ -336,10 +365,8 @@ __device__ __forceinline__ float act_value(float z, int act)
     if (act == ACSC_ACT_RELU)
         return z > 0.f ? z : (z != z ? z : 0.f);
     if (act == ACSC_ACT_GELU) {
-        if (sizeof(T) == 4)
-            return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
         float e;
-        const float q = normal_tail(z, e);
+        const float q = normal_tail<T>(z, e);
         // past 64 q is 0, and infinity times it would be NaN
         return __builtin_fmaf(-fabsf(z > 64.f ? 64.f : z), q, z < 0.f ? 0.f : z);
     }
@@ -356,10 +383,8 @@ __device__ __forceinline__ float act_slope(float z, int act)
     if (act == ACSC_ACT_RELU)
         return z > 0.f ? 1.f : (z != z ? z : 0.f);
     if (act == ACSC_ACT_GELU) {
-        if (sizeof(T) == 4)
-            return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
         float e;
-        const float q = normal_tail(z, e);
+        const float q = normal_tail<T>(z, e);
         return __builtin_fmaf(z * 0.39894228040143268f, e, z < 0.f ? q : 1.f - q);
     }
     if (act == ACSC_ACT_SILU) {
