@@ -543,6 +543,17 @@ typedef enum lin_op { LIN_FORWARD = 0, LIN_BACKWARD_INPUT = 1, LIN_BACKWARD_WEIG
 int lin_workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, size_t *bytes);
 int lin_workspace_size_unaligned(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, size_t *bytes);
 
+/* How such a product runs (host only): in tiles of tile_rows x tile_cols of its
+ * output (the weight gradient's is [n_out, n_in]), `whole` of them along the
+ * whole sum and `cut` of them in `pieces` that are added up after it; 0 x 0: a
+ * product for few rows, in `pieces`.  For operands as in lin_workspace_size. */
+typedef struct lin_plan {
+    int tile_rows, tile_cols;
+    int64_t whole, cut;
+    int pieces;
+} lin_plan;
+int lin_product_plan(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, lin_plan *plan);
+
 /* One linear layer and what follows it, in one pass over the output:
  *   z = x W^T + bias;   y = act(z) + residual
  * x        device [rows, ld_x] of dt (n_in columns);  W device [n_out, ld_w].

@@ -75,6 +75,21 @@ class _Q8Tensor(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("ld_codes", C.c_int64), ("ld_scales", C.c_int64)]
 
 
+class _LinPlan(C.Structure):
+    """lin_plan: how a product of a linear layer is cut."""
+    _fields_ = [("tile_rows", C.c_int), ("tile_cols", C.c_int), ("whole", C.c_int64), ("cut", C.c_int64), ("pieces", C.c_int)]
+
+
+class LinPlan(NamedTuple):
+    """A product in tiles of tile_rows x tile_cols, `whole` of them in one
+    piece and `cut` of them in `pieces`; 0 x 0: a product for few rows."""
+    tile_rows: int
+    tile_cols: int
+    whole: int
+    cut: int
+    pieces: int
+
+
 class Q8(NamedTuple):
     """An 8-bit checkpoint of a [rows, H] tensor: codes int8 [rows, H] and one
     fp32 scale for each 128 columns of a row, scales [rows, ceil(H / 128)]."""
@@ -147,6 +162,7 @@ def _load():
             ("ln_backward", [vp, i64, vp, i64, qp, i32, i64, i32, vp, vp, vp, vp, i64, vp, i64, vp, vp, i32, vp, sz, vp]),
             ("lin_workspace_size", [i32, i64, i32, i32, i32, C.POINTER(sz)]),
             ("lin_workspace_size_unaligned", [i32, i64, i32, i32, i32, C.POINTER(sz)]),
+            ("lin_product_plan", [i32, i64, i32, i32, i32, C.POINTER(_LinPlan)]),
             ("lin_forward", [vp, i64, i32, i64, i32, i32, vp, i64, vp, i32, vp, i64, vp, i64, vp, i64, qp, vp, sz, vp]),
             ("lin_backward_act", [vp, i64, vp, i64, qp, i32, i64, i32, i32, vp, i64, vp]),
             ("lin_backward_input", [vp, i64, i32, i64, i32, i32, vp, i64, i32, vp, i64, qp, vp, i64, vp, sz, vp]),
@@ -174,7 +190,8 @@ EXPORTED = ("acsc_last_error", "acsc_version", "acsc_stats_enable", "acsc_stats_
             "ac_bern_mask", "ac_bern_pack", "ac_bern_unpack",
             "psgd_workspace_size", "psgd_project", "psgd_orthogonalize", "psgd_decompress", "psgd_step",
             "q8_encode", "q8_decode", "ln_forward", "ln_recompute", "ln_workspace_size", "ln_backward",
-            "lin_workspace_size", "lin_workspace_size_unaligned", "lin_forward", "lin_backward_act", "lin_backward_input", "lin_backward_weight")
+            "lin_workspace_size", "lin_workspace_size_unaligned", "lin_product_plan", "lin_forward", "lin_backward_act",
+            "lin_backward_input", "lin_backward_weight")
 
 
 def _check(rc: int):
@@ -910,6 +927,13 @@ def lin_workspace_size_unaligned(op: int, rows: int, n_in: int, n_out: int, dtyp
     code = BF16 if dtype == torch.bfloat16 else F32
     _check(lib.lin_workspace_size_unaligned(op, rows, n_in, n_out, code, C.byref(b)))
     return b.value
+
+
+def lin_product_plan(op: int, rows: int, n_in: int, n_out: int, dtype: torch.dtype) -> LinPlan:
+    """How that product runs, for operands as in lin_workspace_size."""
+    p = _LinPlan()
+    _check(lib.lin_product_plan(op, rows, n_in, n_out, BF16 if dtype == torch.bfloat16 else F32, C.byref(p)))
+    return LinPlan(p.tile_rows, p.tile_cols, p.whole, p.cut, p.pieces)
 
 
 def _lin_ws(op: int, rows: int, n_in: int, n_out: int, a, lda: int, b, ldb: int, ws: Optional[torch.Tensor]):

@@ -544,35 +544,65 @@ inline size_t recomputed_bytes(int64_t rows, int n_in, acsc_dtype dt)
 
 using namespace acsc;
 
-static int workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, bool any, size_t *bytes)
+static int check_product(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, const void *out)
 {
-    clear_error();
     if (int rc = check_layer(rows, n_in, n_out, dt))
         return rc;
-    ACSC_CHECK_ARG(bytes, ACSC_EINVAL, "null pointer bytes");
+    ACSC_CHECK_ARG(out, ACSC_EINVAL, "null pointer to the result");
     ACSC_CHECK_ARG(op == LIN_FORWARD || op == LIN_BACKWARD_INPUT || op == LIN_BACKWARD_WEIGHT, ACSC_EINVAL,
                    "unknown product %d", (int)op);
-    *bytes = 0;
-    if (rows == 0)
-        return ACSC_OK;
+    return ACSC_OK;
+}
+
+// The plan of a product, with the operands' copies that bits 0 (A) and 1 (B) of
+// `copies` add to those that are needed whatever the alignment.
+static int plan_product(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, int copies, Plan &p)
+{
     const EpiKind kind = op == LIN_FORWARD ? kForward : op == LIN_BACKWARD_INPUT ? kGate : kWeight;
     const Shape s = shape_of(kind, rows, n_in, n_out);
-    // the strides that the size is good for: all from the rows' own length on, of whole words
+    // the strides that the plan is good for: all from the rows' own length on, of whole words
     const auto best = [&](bool col, int64_t inner) {
         return readable(Operand{nullptr, dt == ACSC_F32 ? inner : (inner + 1) / 2 * 2}, col, inner, dt);
     };
     const bool a = best(s.acol, s.acol ? s.M : s.K), b = best(s.bcol, s.bcol ? s.N : s.K);
+    p = plan_of(kind, s, dt, a && !(copies & 1), b && !(copies & 2));
+    return check_tiles(p);
+}
+
+static int workspace_size(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, bool any, size_t *bytes)
+{
+    clear_error();
+    if (int rc = check_product(op, rows, n_in, n_out, dt, bytes))
+        return rc;
+    *bytes = 0;
+    if (rows == 0)
+        return ACSC_OK;
     // with any alignment: the most that either operand's copy, or its absence, takes
     size_t most = 0;
     for (int copies = 0; copies < (any ? 4 : 1); ++copies) {
-        const Plan p = plan_of(kind, s, dt, a && !(copies & 1), b && !(copies & 2));
-        if (int rc = check_tiles(p))
+        Plan p;
+        if (int rc = plan_product(op, rows, n_in, n_out, dt, copies, p))
             return rc;
         most = std::max(most, p.bytes());
     }
     *bytes = most;
-    if (kind == kWeight && rows > few_tokens(kind, true))
+    if (op == LIN_BACKWARD_WEIGHT && rows > few_tokens(kWeight, true))
         *bytes += recomputed_bytes(rows, n_in, dt);
+    return ACSC_OK;
+}
+
+extern "C" int lin_product_plan(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt, lin_plan *plan)
+{
+    clear_error();
+    if (int rc = check_product(op, rows, n_in, n_out, dt, plan))
+        return rc;
+    *plan = lin_plan{};
+    if (rows == 0)
+        return ACSC_OK;
+    Plan p;
+    if (int rc = plan_product(op, rows, n_in, n_out, dt, 0, p))
+        return rc;
+    *plan = {p.rows, p.tile, p.whole, static_cast<int64_t>(p.tm) * p.tn - p.whole, p.splits};
     return ACSC_OK;
 }
 
