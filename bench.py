@@ -659,13 +659,19 @@ def psgd_component(pk, mats, gs, calls, stream):
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "hotpath_70b_4layer_hbm_traffic.txt")
 
 
-def kernel_sources_digest() -> str:
-    """SHA-256 over the library's kernel sources (csrc/*.hip, csrc/*.h), in name order."""
+# What the timed step launches nothing of: the feed-forward block's kernels.
+BLOCK_SOURCES = ("lin.h", "lin.hip", "lin_few.hip", "lin_tile.hip", "ln.hip", "q8.h", "q8.hip")
+
+
+def kernel_sources_digest(block: bool = False) -> str:
+    """SHA-256 over the sources in csrc (*.hip, *.h, in name order) that the
+    step's kernels are built from, which is all but the feed-forward block's;
+    with block, over all of them."""
     import hashlib
     d = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_2609_14339_amd", "csrc")
     for name in sorted(os.listdir(csrc)):
-        if name.endswith((".hip", ".h")):
+        if name.endswith((".hip", ".h")) and (block or name not in BLOCK_SOURCES):
             with open(os.path.join(csrc, name), "rb") as f:
                 d.update(name.encode() + b"\0" + f.read())
     return d.hexdigest()

@@ -5,6 +5,8 @@
 
 #include "common.h"
 
+#include <algorithm>
+
 namespace acsc {
 
 constexpr int kGroup = ACSC_Q8_GROUP;
