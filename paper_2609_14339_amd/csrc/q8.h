@@ -117,20 +117,6 @@ __device__ __forceinline__ void store8(float *p, int nv, const float (&v)[8])
                 p[i] = v[i];
     }
 }
-// Four consecutive floats, as above.
-__device__ __forceinline__ void load4(const float *p, int nv, float (&v)[4])
-{
-    if (nv >= 4) {
-        const F4Any a = *reinterpret_cast<const F4Any *>(p);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            v[i] = a.v[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            v[i] = i < nv ? p[i] : 0.f;
-    }
-}
 
 // A code's value, rounded once as the format asks: not contracted into what
 // it is added to.
@@ -197,21 +183,17 @@ __device__ __forceinline__ void load_raw(const int8_t *p, int nv, Codes8 &r)
     }
 }
 
-// Values of N = 4 or 8 consecutive codes under one scale.
-template <int N>
-__device__ __forceinline__ void load_codes(const int8_t *p, int nv, float scale, float (&v)[N])
+// Values of eight consecutive codes under one scale.
+__device__ __forceinline__ void load_codes(const int8_t *p, int nv, float scale, float (&v)[8])
 {
-    if (nv >= N) {
-        struct __attribute__((packed, aligned(1))) Any {
-            uint32_t w[N / 4];
-        };
-        const Any c = *reinterpret_cast<const Any *>(p);
+    if (nv >= 8) {
+        const C8Any c = *reinterpret_cast<const C8Any *>(p);
 #pragma unroll
-        for (int i = 0; i < N; ++i)
+        for (int i = 0; i < 8; ++i)
             v[i] = code_value(static_cast<float>(static_cast<int8_t>(c.w[i / 4] >> (8 * (i % 4)))), scale);
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
+        for (int i = 0; i < 8; ++i)
             v[i] = i < nv ? code_value(static_cast<float>(p[i]), scale) : 0.f;
     }
 }
@@ -251,18 +233,17 @@ __device__ __forceinline__ void group_scale(uint32_t a, float &scale, float &inv
     }
 }
 
-// Codes of N values: rint(x * inv), in -127 .. 127 because |x| <= a makes
+// Codes of eight values: rint(x * inv), in -127 .. 127 because |x| <= a makes
 // |x * inv| round to at most 127 (1 + 2^-23).  Adding 1.5 * 2^23 rounds to a
 // whole number, ties to even, whose low byte is the code; the product is
 // rounded before that, as the format asks (no contraction).  inv = 0 gives
 // zeros, for the non-finite values of a NaN group too.
-template <int N>
-__device__ __forceinline__ void store_codes(int8_t *p, int nv, float inv, const float (&v)[N])
+__device__ __forceinline__ void store_codes(int8_t *p, int nv, float inv, const float (&v)[8])
 {
 #pragma clang fp contract(off)
-    uint32_t w[N / 4];
+    uint32_t w[2];
 #pragma unroll
-    for (int q = 0; q < N / 4; ++q) {
+    for (int q = 0; q < 2; ++q) {
         uint32_t b[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -272,18 +253,11 @@ __device__ __forceinline__ void store_codes(int8_t *p, int nv, float inv, const 
         const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400), hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0c);
         w[q] = inv == 0.f ? 0u : lo | hi;
     }
-    if (nv >= N) {
-        struct __attribute__((packed, aligned(1))) Any {
-            uint32_t w[N / 4];
-        };
-        Any c;
-#pragma unroll
-        for (int q = 0; q < N / 4; ++q)
-            c.w[q] = w[q];
-        *reinterpret_cast<Any *>(p) = c;
+    if (nv >= 8) {
+        *reinterpret_cast<C8Any *>(p) = C8Any{{w[0], w[1]}};
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
+        for (int i = 0; i < 8; ++i)
             if (i < nv)
                 p[i] = static_cast<int8_t>(w[i / 4] >> (8 * (i % 4)));
     }
