@@ -519,7 +519,8 @@ int ln_workspace_size(int64_t rows, int H, size_t *bytes);
  *   dx = rstd (g - mean(g) - h mean(g h)) + add
  *   dgamma (+)= sum over rows of dy h,   dbeta (+)= sum over rows of dy
  * add          device [rows, ld_add] of dt or NULL: the gradient that reaches x
- *              past the norm (the residual branch).  dx may equal dy or add.
+ *              past the norm (the residual branch).  dx may equal dy, x or add
+ *              (with its row stride).
  * dgamma, dbeta  device fp32 [H], each or both NULL; accumulate != 0 adds to
  *              what they hold (gradients of several microbatches).  Sums are
  *              taken in a fixed order: the same call gives the same bits.
@@ -560,7 +561,8 @@ int lin_product_plan(lin_op op, int64_t rows, int n_in, int n_out, acsc_dtype dt
  * bias     device [n_out] of dt or NULL;  residual device [rows, ld_res] of dt
  *          or NULL (may equal y, with ld_res == ld_y).
  * y        device [rows, ld_y] of dt; must not overlap x or W.
- * z        device [rows, ld_z] of dt or NULL: receives the pre-activation.
+ * z        device [rows, ld_z] of dt or NULL: receives the pre-activation; must
+ *          not overlap x or W.
  * q        NULL, or a checkpoint of the pre-activation [rows, n_out], coded
  *          from its fp32 values.
  * Products accumulate in fp32 and the epilogue works on the fp32 sum; y is
@@ -575,14 +577,15 @@ int lin_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t rows, int n_
                 hipStream_t stream);
 
 /* dz = dy act'(z), from the kept pre-activation (exactly one of z and q is
- * not NULL).  dz may equal dy.  relu'(0) = 0. */
+ * not NULL).  dz may equal dy or z (with its row stride).  relu'(0) = 0. */
 int lin_backward_act(const void *dy, int64_t ld_dy, const void *z, int64_t ld_z, const q8_tensor *q, acsc_dtype dt,
                      int64_t rows, int n_out, acsc_act act, void *dz, int64_t ld_dz, hipStream_t stream);
 
 /* Gradient of the layer's input: dx = dz W.  With act != ACSC_ACT_NONE the
  * input was act(z) of the layer before, and the gradient of its z is wanted:
  *   dx = (dz W) act'(z)
- * from that layer's kept pre-activation (one of z and q; [rows, n_in]). */
+ * from that layer's kept pre-activation (one of z and q; [rows, n_in]).  dx may
+ * equal z (with ld_dx == ld_z); it must not overlap dz or W. */
 int lin_backward_input(const void *dz, int64_t ld_dz, acsc_dtype dt, int64_t rows, int n_in, int n_out,
                        const void *W, int64_t ld_w, acsc_act act, const void *z, int64_t ld_z, const q8_tensor *q,
                        void *dx, int64_t ld_dx, void *ws, size_t ws_bytes, hipStream_t stream);
@@ -594,7 +597,8 @@ int lin_backward_input(const void *dz, int64_t ld_dz, acsc_dtype dt, int64_t row
  *          before; its activation is recomputed inside the call and, for more
  *          than eight rows, rounded to dt, as that layer's output was.
  * dW       device [n_out, ld_dw] of dw_dt (the gradient's type: bf16 goes to
- *          sc_correct as it is, fp32 serves accumulation).
+ *          sc_correct as it is, fp32 serves accumulation); must not overlap dz
+ *          or x.
  * db       device fp32 [n_out] or NULL.
  * accumulate != 0 adds to what dW and db hold.  rows == 0 gives zero sums. */
 int lin_backward_weight(const void *dz, int64_t ld_dz, const void *x, int64_t ld_x, const q8_tensor *q,

@@ -642,6 +642,7 @@ extern "C" int lin_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t r
     if (z)
         if (int rc = check_mat(z, some, ld_z, n_out, dt, "z"))
             return rc;
+    ACSC_CHECK_ARG(!some || !z || (z != x && z != W), ACSC_EINVAL, "z must not overlap x or W");
     if (q)
         if (int rc = check_q8(q, rows, n_out))
             return rc;
@@ -676,6 +677,7 @@ extern "C" int lin_backward_act(const void *dy, int64_t ld_dy, const void *z, in
     if (int rc = check_mat(dz, rows > 0, ld_dz, n_out, dt, "dz"))
         return rc;
     ACSC_CHECK_ARG(dz != dy || rows == 0 || ld_dz == ld_dy, ACSC_EINVAL, "dz in place of dy needs ld_dz == ld_dy");
+    ACSC_CHECK_ARG(dz != z || rows == 0 || ld_dz == ld_z, ACSC_EINVAL, "dz in place of z needs ld_dz == ld_z");
     if (rows == 0)
         return ACSC_OK;
     const int64_t blocks = std::min<int64_t>((rows * ((n_out + 511) / 512) + 3) / 4, 1 << 20);
@@ -711,6 +713,7 @@ extern "C" int lin_backward_input(const void *dz, int64_t ld_dz, acsc_dtype dt, 
     if (int rc = check_mat(dx, some, ld_dx, n_in, dt, "dx"))
         return rc;
     ACSC_CHECK_ARG(!some || (dx != dz && dx != W), ACSC_EINVAL, "dx must not overlap dz or W");
+    ACSC_CHECK_ARG(!some || act == ACSC_ACT_NONE || dx != z || ld_dx == ld_z, ACSC_EINVAL, "dx in place of z needs ld_dx == ld_z");
     if (!some)
         return ACSC_OK;
     Gemm g{};
@@ -744,6 +747,7 @@ extern "C" int lin_backward_weight(const void *dz, int64_t ld_dz, const void *x,
         return rc;
     if (int rc = check_mat(dW, true, ld_dw, n_in, dw_dt, "dW"))
         return rc;
+    ACSC_CHECK_ARG(!some || (dW != dz && dW != x), ACSC_EINVAL, "dW must not overlap dz or x");
     ACSC_CHECK_ARG(aligned(db, 4), ACSC_EALIGN, "db not 4-byte aligned");
     if (!some) {
         if (accumulate)

@@ -710,6 +710,7 @@ extern "C" int ln_backward(const void *dy, int64_t ld_dy, const void *x, int64_t
     if (int rc = check_mat(dx, rows, ld_dx, H, dt, "dx"))
         return rc;
     ACSC_CHECK_ARG(dx != dy || rows == 0 || ld_dx == ld_dy, ACSC_EINVAL, "dx in place of dy needs ld_dx == ld_dy");
+    ACSC_CHECK_ARG(dx != x || rows == 0 || ld_dx == ld_x, ACSC_EINVAL, "dx in place of x needs ld_dx == ld_x");
     ACSC_CHECK_ARG(dx != add || rows == 0 || ld_dx == ld_add, ACSC_EINVAL, "dx in place of add needs ld_dx == ld_add");
     ACSC_CHECK_ARG(rows == 0 || (mean && rstd), ACSC_EINVAL, "null statistics");
     ACSC_CHECK_ARG(aligned(mean, 4) && aligned(rstd, 4) && aligned(dgamma, 4) && aligned(dbeta, 4), ACSC_EALIGN,

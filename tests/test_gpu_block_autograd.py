@@ -148,3 +148,27 @@ def test_norm_from_its_checkpoint(ops):
     assert rel(out, ref) <= 1e-6
     for k, g, w in zip(names, got, want):
         assert rel(g, w) <= (1e-5 if k == "beta" else 2e-2), k
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,H,F", [(300, 520, 1100), (5, 9000, 64), (40, 17000, 40)])
+def test_gradients_in_the_place_of_what_they_read(dtype, rows, H, F):
+    """dx over z, dz over z, and the norm's dx over x, dy or add: the values of a call of its own."""
+    import paper_2609_14339_amd as pk
+    mk = lambda *s: torch.randn(*s, device="cuda").to(dtype)
+    dz, W, z = mk(rows, F), mk(F, H), mk(rows, H)
+    want = pk.lin_backward_input(dz, W, "silu", z)
+    over = z.clone()
+    pk.lin_backward_input(dz, W, "silu", over, dx=over)
+    assert torch.equal(over, want)
+    dy, over = mk(rows, H), z.clone()
+    want = pk.lin_backward_act(dy, z, "gelu")
+    pk.lin_backward_act(dy, over, "gelu", dz=over)
+    assert torch.equal(over, want)
+    add, gamma = mk(rows, H), mk(H)
+    _, mean, rstd, _ = pk.ln_forward(z)
+    want = pk.ln_backward(dy, z, mean, rstd, gamma, add=add)
+    for which in range(3):
+        at = [dy.clone(), z.clone(), add.clone()]
+        got = pk.ln_backward(at[0], at[1], mean, rstd, gamma, add=at[2], dx=at[which])
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), which

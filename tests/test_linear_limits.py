@@ -53,3 +53,18 @@ def test_products_of_more_threads_than_a_launch_has(pk, op, dt):
                                             1 << 62, None)) if op == 0 else \
         (lambda rows: pk.lib.lin_backward_input(W, 8, dt, rows, 8, 8, 2 * W, 8, 0, None, 8, None, 3 * W, 8, W, 1 << 62, None))
     assert call((1 << 31) - 1) == EINVAL and b"too large" in pk.lib.acsc_last_error()
+
+
+def test_outputs_in_the_place_of_inputs(pk):
+    """What a product still reads while it writes is refused; element by element, a place is taken with its row stride."""
+    F, n = 0x10000, 1 << 30
+    lin = lambda z, ldz=64: pk.lib.lin_forward(F, 64, 1, 40, 64, 64, 2 * F, 64, None, 1, None, 0, 3 * F, 64, z, ldz, None, F, n,
+                                               None)
+    assert lin(F) == EINVAL and lin(2 * F) == EINVAL and b"z must not overlap" in pk.lib.acsc_last_error()
+    dx = lambda at, ld: pk.lib.lin_backward_input(F, 64, 1, 40, 64, 64, 2 * F, 64, 2, 4 * F, 64, None, at, ld, F, n, None)
+    assert dx(4 * F, 72) == EINVAL and b"place of z" in pk.lib.acsc_last_error()
+    dw = lambda at: pk.lib.lin_backward_weight(F, 64, 2 * F, 64, None, 0, 1, 64, 64, 64, at, 1, 64, None, 0, F, n, None)
+    assert dw(F) == EINVAL and dw(2 * F) == EINVAL and b"overlap" in pk.lib.acsc_last_error()
+    assert pk.lib.lin_backward_act(F, 64, 2 * F, 64, None, 1, 40, 64, 2, 2 * F, 72, None) == EINVAL
+    assert pk.lib.ln_backward(F, 64, 2 * F, 64, None, 1, 40, 64, F, F, F, None, 0, 2 * F, 72, None, None, 0, None, 0,
+                              None) == EINVAL and b"place of x" in pk.lib.acsc_last_error()
