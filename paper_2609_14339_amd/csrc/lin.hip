@@ -95,9 +95,12 @@ struct Jobs {
     Job j[3];
 };
 
-// An operand: a wave takes 512 columns of a row, eight a lane.  Sums: 512
-// columns and one slice of rows a workgroup, whose four waves take every
-// fourth row and meet in LDS in order.
+// An operand: a wave takes 512 columns of a row, eight a lane.  An activation
+// is rounded to T here, as the forward product's input was: dW of 8192 x 14336
+// -> 4096 in bf16 is 2.3e-3 off with it and 1.7e-3, its own rounding, without;
+// that would take its product in fp32 (by their rates 7.4 ms, 0.72 so) or
+// twice, in two halves.  Sums: 512 columns and one slice of rows a workgroup,
+// whose four waves take every fourth row and meet in LDS in order.
 template <typename T>
 __global__ __launch_bounds__(256) void lin_prepare_kernel(Jobs jobs)
 {

@@ -26,9 +26,9 @@
 // compiler moves between register files all the time; steps of half the length
 // in rings of three to five stages read lines of 64 bytes and lose 8%.)
 //
-// Measured, bf16 TFLOP/s, forward / input gradient / weight gradient: 8192 x
-// 28672 -> 8192 1415 / 1406 / 1390, 8192 x 8192 -> 8192 1456 / 1400 / 1400,
-// 16384 x 2048 -> 8192 1308 / 1342 / 1376; fp32 4096^3 127 / 134 / 134 of 157
+// Measured, TFLOP/s, forward / input gradient / weight gradient: bf16 8192 x
+// 28672 -> 8192 1448 / 1385 / 1361, 8192 x 8192 -> 8192 1441 / 1385 / 1364,
+// 16384 x 2048 -> 8192 1297 / 1336 / 1360; fp32 4096^3 147 / 144 / 137 of 157
 // that the matrix cores have at 2.4 GHz.  What bounds it: at 8192 x 28672 ->
 // 8192 the products alone, from registers, run at 2260 (the clock is near 1.7
 // GHz by then), with their LDS reads at 1750, the DMA alone, two
