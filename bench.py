@@ -660,7 +660,8 @@ TRAFFIC_FILE = os.path.join(ROOT, "profiles", "hotpath_70b_4layer_hbm_traffic.tx
 
 
 # What the timed step launches nothing of: the feed-forward block's kernels.
-BLOCK_SOURCES = ("lin.h", "lin.hip", "lin_few.hip", "lin_tile.hip", "ln.hip", "q8.h", "q8.hip")
+BLOCK_SOURCES = ("drop.h", "drop.hip", "glu.hip", "glu_tile.hip", "join.hip", "lin.h", "lin.hip", "lin_few.hip", "lin_plan.h",
+                 "lin_tile.h", "lin_tile.hip", "ln.hip", "prf.h", "q8.h", "q8.hip", "rows.h")
 
 
 def kernel_sources_digest(block: bool = False) -> str:

@@ -605,6 +605,139 @@ int lin_backward_weight(const void *dz, int64_t ld_dz, const void *x, int64_t ld
                         acsc_act act, acsc_dtype dt, int64_t rows, int n_in, int n_out, void *dW, acsc_dtype dw_dt,
                         int64_t ld_dw, float *db, int accumulate, void *ws, size_t ws_bytes, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * The gated feed-forward block: root-mean-square norms joined with the gate,
+ * dropout and residual between two blocks, and the gated linear layer (Sec. 5
+ * setup: the models that the method trains are of this form).
+ * ---------------------------------------------------------------------- */
+
+/* Dropout D of a [rows, H] tensor at one place (`site`) of one layer: a value
+ * is kept where 16 bits drawn from the key are below T = floor((1 - p) 65536 +
+ * 1/2), and then multiplied by 65536 / T; others become +0, whatever they
+ * held.  The draws are those of ac_bern_mask with another row key: with k the
+ * chain over the key's fields, k' = mix64((k ^ (0x64726F70 2^32 + site)) +
+ * gamma), so no dropout shares them with a boundary or with another site.  The
+ * same key gives the same mask in the backward pass; none is stored.
+ * 0 <= p <= 1 - 2^-17, rows == key.B * key.S, H == key.H. */
+typedef struct drop_mask {
+    ac_mask_key key;
+    uint32_t site;
+    double p;
+} drop_mask;
+
+/* y <- D(x) + residual, rounded once; its gradient is the same call on dy
+ * (without the residual).  residual: device [rows, ld_res] of dt or NULL.  y may
+ * equal x or residual (with its row stride).  0 <= rows < 2^31,
+ * 1 <= H <= 2^22. */
+int drop_apply(const void *x, acsc_dtype dt, int64_t rows, int H, int64_t ld_x, const drop_mask *drop,
+               const void *residual, int64_t ld_res, void *y, int64_t ld_y, hipStream_t stream);
+
+/* Root-mean-square norm of the rows of x [rows, ld_x] of dt, 1 <= H <= 32768:
+ *   rho = 1 / sqrt(mean(x^2) + eps),   y = x rho gamma
+ * gamma        device [H] of dt; NULL: ones.
+ * rstd         device fp32 [rows] or NULL: receives rho (the backward pass
+ *              needs it).
+ * q            NULL, or a checkpoint of x written in the same pass.
+ * y may equal x (with ld_y == ld_x).  eps > 0.  Statistics are fp32. */
+int rms_forward(const void *x, acsc_dtype dt, int64_t rows, int H, int64_t ld_x, const void *gamma, float eps, void *y,
+                int64_t ld_y, float *rstd, const q8_tensor *q, hipStream_t stream);
+
+/* y of rms_forward again, from the kept rstd and either x or its checkpoint. */
+int rms_recompute(const void *x, int64_t ld_x, const q8_tensor *q, acsc_dtype dt, int64_t rows, int H, const float *rstd,
+                  const void *gamma, void *y, int64_t ld_y, hipStream_t stream);
+
+/* Bytes of workspace that rms_backward and join_backward need. */
+int join_workspace_size(int64_t rows, int H, size_t *bytes);
+
+/* Gradients of rms_forward, from x or its checkpoint (exactly one of x and q):
+ *   h = x rstd,  g = dy gamma,  dx = rstd (g - h mean(g h)) + add
+ *   dgamma (+)= sum over rows of dy h
+ * The arguments are ln_backward's. */
+int rms_backward(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, const q8_tensor *q, acsc_dtype dt, int64_t rows,
+                 int H, const float *rstd, const void *gamma, const void *add, int64_t ld_add, void *dx, int64_t ld_dx,
+                 float *dgamma, int accumulate, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Between two blocks, in one pass over the residual stream r and the branch b
+ * (both [rows, H] of dt, 1 <= H <= 32768):
+ *   t = b rho1 post,  rho1 = 1 / sqrt(mean(b^2) + eps)      (post == NULL: t = b)
+ *   out = scale r + D(gate t)
+ *   y = out rho2 pre, rho2 = 1 / sqrt(mean(out^2) + eps)    (y == NULL: none)
+ * post, gate, pre  device [H] of dt or NULL; gate, pre: ones.
+ * drop             NULL: no dropout.
+ * rstd_post, rstd_pre  device fp32 [rows] or NULL: receive rho1 and rho2.
+ * q_out, q_b       NULL, or checkpoints of out and b written in the same pass.
+ * y is taken from out before its rounding.  out and y may each equal r or b
+ * (with its row stride), but not each other. */
+int join_forward(const void *r, int64_t ld_r, const void *b, int64_t ld_b, acsc_dtype dt, int64_t rows, int H,
+                 const void *post, const void *gate, float scale, const drop_mask *drop, const void *pre, float eps, void *out,
+                 int64_t ld_out, void *y, int64_t ld_y, float *rstd_post, float *rstd_pre, const q8_tensor *q_out,
+                 const q8_tensor *q_b, hipStream_t stream);
+
+/* Gradients of join_forward, from dout and dy (either may be NULL; dy where
+ * there was no y):
+ *   h2 = out rho2, g = dy pre,  t = dout + rho2 (g - h2 mean(g h2)),  dr = scale t
+ *   u = D(t) (the same mask),  h1 = b rho1 (or b),  e = u gate post
+ *   db = rho1 (e - h1 mean(e h1)) (or e)
+ *   dpre (+)= sum of dy h2;  with s = sum of u h1:  dpost (+)= s gate,
+ *   dgate (+)= s post
+ * out or q_out is needed with dy, b or q_b with post or gate; where both are
+ * needed they are both tensors or both checkpoints.  dr may be NULL.  dr and
+ * db may each equal any input tensor (with its row stride), but not each
+ * other.  dpost, dgate, dpre: device fp32 [H] or NULL; accumulate != 0 adds to
+ * what they hold.  Sums are taken in a fixed order.  rows == 0 gives zero sums.
+ * ws is needed only with dpost, dgate or dpre. */
+int join_backward(const void *dout, int64_t ld_dout, const void *dy, int64_t ld_dy, const void *out, int64_t ld_out,
+                  const q8_tensor *q_out, const void *b, int64_t ld_b, const q8_tensor *q_b, acsc_dtype dt, int64_t rows, int H,
+                  const void *post, const void *gate, float scale, const drop_mask *drop, const void *pre,
+                  const float *rstd_post, const float *rstd_pre, void *dr, int64_t ld_dr, void *db, int64_t ld_db, float *dpost,
+                  float *dgate, float *dpre, int accumulate, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Which product of a gated linear layer a workspace is for. */
+typedef enum glu_op { GLU_FORWARD = 0, GLU_BACKWARD_INPUT = 1 } glu_op;
+
+/* Bytes of workspace for glu_forward (n_in inputs, F hidden columns;
+ * checkpoint != 0: it writes q_gate and q_up) and for glu_backward_input (n_in
+ * is the down projection's n_out), with the operands of lin_workspace_size and
+ * of lin_workspace_size_unaligned; and how that product runs.  A tile of the
+ * forward product holds tile_cols / 2 hidden columns. */
+int glu_workspace_size(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int checkpoint, size_t *bytes);
+int glu_workspace_size_unaligned(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int checkpoint, size_t *bytes);
+int glu_product_plan(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int checkpoint, lin_plan *plan);
+
+/* The gated linear layer, both projections in one product:
+ *   g = x Wg^T + bg,  u = x Wu^T + bu,  h = act(g) u
+ * x        device [rows, ld_x] of dt (n_in columns).
+ * W        device [2 F, ld_w]: Wg's rows, then Wu's.
+ * bias     device [2 F] of dt or NULL: bg, then bu.
+ * h        device [rows, ld_h] of dt (F columns).
+ * z        device [rows, ld_z] of dt or NULL: receives g, then u, in 2 F columns.
+ * q_gate, q_up  NULL, or checkpoints of g and u (each [rows, F]), coded from
+ *          their fp32 values; both or none.
+ * h and z overlap neither x nor W nor each other.  Arithmetic and limits as
+ * lin_forward, with 1 <= F <= 2^21; h is formed from the fp32 g and u and
+ * rounded once. */
+int glu_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t rows, int n_in, int F, const void *W, int64_t ld_w,
+                const void *bias, acsc_act act, void *h, int64_t ld_h, void *z, int64_t ld_z, const q8_tensor *q_gate,
+                const q8_tensor *q_up, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* The gradient of h through the gate, from kept g and u (z, or both
+ * checkpoints):  dz = (dh u act'(g), dh act(g)) in 2 F columns.  h: device
+ * [rows, ld_h] of dt or NULL: receives act(g) u again.  dz may equal z, and h
+ * dh (with its row stride).  With dz, the layer's other gradients are those of
+ * a linear layer with the weights W: lin_backward_input and
+ * lin_backward_weight with 2 F outputs. */
+int glu_backward_act(const void *dh, int64_t ld_dh, const void *z, int64_t ld_z, const q8_tensor *q_gate,
+                     const q8_tensor *q_up, acsc_dtype dt, int64_t rows, int F, acsc_act act, void *dz, int64_t ld_dz, void *h,
+                     int64_t ld_h, hipStream_t stream);
+
+/* The same with dh = dy W of the linear layer behind (W [n_out, F]), in the
+ * epilogue of that product; dh is not written.  dz may equal z; dz and h
+ * overlap neither dy nor W. */
+int glu_backward_input(const void *dy, int64_t ld_dy, acsc_dtype dt, int64_t rows, int F, int n_out, const void *W,
+                       int64_t ld_w, acsc_act act, const void *z, int64_t ld_z, const q8_tensor *q_gate,
+                       const q8_tensor *q_up, void *dz, int64_t ld_dz, void *h, int64_t ld_h, void *ws, size_t ws_bytes,
+                       hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

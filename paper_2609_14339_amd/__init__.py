@@ -75,6 +75,11 @@ class _Q8Tensor(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("ld_codes", C.c_int64), ("ld_scales", C.c_int64)]
 
 
+class _DropMask(C.Structure):
+    """drop_mask: the key, site and probability of a dropout."""
+    _fields_ = [("key", MaskKey), ("site", C.c_uint32), ("p", C.c_double)]
+
+
 class _LinPlan(C.Structure):
     """lin_plan: how a product of a linear layer is cut."""
     _fields_ = [("tile_rows", C.c_int), ("tile_cols", C.c_int), ("whole", C.c_int64), ("cut", C.c_int64), ("pieces", C.c_int)]
@@ -95,6 +100,34 @@ class Q8(NamedTuple):
     fp32 scale for each 128 columns of a row, scales [rows, ceil(H / 128)]."""
     codes: torch.Tensor
     scales: torch.Tensor
+
+
+class Drop(NamedTuple):
+    """Dropout of a [rows, H] tensor with probability p: its mask comes from the
+    step's key (make_key; B S = rows) and the place in the layer, and is the same
+    wherever that key is given again."""
+    p: float
+    key: MaskKey
+    site: int = 0
+
+
+class Joined(NamedTuple):
+    """What join_forward returns; None for what was not asked for."""
+    out: torch.Tensor
+    y: Optional[torch.Tensor]
+    rstd_post: Optional[torch.Tensor]
+    rstd_pre: Optional[torch.Tensor]
+    q_out: Optional[Q8]
+    q_b: Optional[Q8]
+
+
+class JoinGrads(NamedTuple):
+    """What join_backward returns; None for what was not asked for."""
+    dr: Optional[torch.Tensor]
+    db: torch.Tensor
+    dpost: Optional[torch.Tensor]
+    dgate: Optional[torch.Tensor]
+    dpre: Optional[torch.Tensor]
 
 
 def _load():
@@ -152,7 +185,7 @@ def _load():
         fn = getattr(lib, name)
         fn.restype = i32
         fn.argtypes = [i32, C.POINTER(PsgdMatrix), i32, i32, vp]
-    qp = C.POINTER(_Q8Tensor)
+    qp, dp = C.POINTER(_Q8Tensor), C.POINTER(_DropMask)
     for name, types in (
             ("q8_encode", [vp, i32, i64, i32, i64, qp, vp]),
             ("q8_decode", [qp, i64, i32, i32, vp, i32, i64, vp]),
@@ -166,7 +199,21 @@ def _load():
             ("lin_forward", [vp, i64, i32, i64, i32, i32, vp, i64, vp, i32, vp, i64, vp, i64, vp, i64, qp, vp, sz, vp]),
             ("lin_backward_act", [vp, i64, vp, i64, qp, i32, i64, i32, i32, vp, i64, vp]),
             ("lin_backward_input", [vp, i64, i32, i64, i32, i32, vp, i64, i32, vp, i64, qp, vp, i64, vp, sz, vp]),
-            ("lin_backward_weight", [vp, i64, vp, i64, qp, i32, i32, i64, i32, i32, vp, i32, i64, vp, i32, vp, sz, vp])):
+            ("lin_backward_weight", [vp, i64, vp, i64, qp, i32, i32, i64, i32, i32, vp, i32, i64, vp, i32, vp, sz, vp]),
+            ("drop_apply", [vp, i32, i64, i32, i64, dp, vp, i64, vp, i64, vp]),
+            ("rms_forward", [vp, i32, i64, i32, i64, vp, f32, vp, i64, vp, qp, vp]),
+            ("rms_recompute", [vp, i64, qp, i32, i64, i32, vp, vp, vp, i64, vp]),
+            ("rms_backward", [vp, i64, vp, i64, qp, i32, i64, i32, vp, vp, vp, i64, vp, i64, vp, i32, vp, sz, vp]),
+            ("join_workspace_size", [i64, i32, C.POINTER(sz)]),
+            ("join_forward", [vp, i64, vp, i64, i32, i64, i32, vp, vp, f32, dp, vp, f32, vp, i64, vp, i64, vp, vp, qp, qp, vp]),
+            ("join_backward", [vp, i64, vp, i64, vp, i64, qp, vp, i64, qp, i32, i64, i32, vp, vp, f32, dp, vp, vp, vp, vp, i64,
+                               vp, i64, vp, vp, vp, i32, vp, sz, vp]),
+            ("glu_workspace_size", [i32, i64, i32, i32, i32, i32, C.POINTER(sz)]),
+            ("glu_workspace_size_unaligned", [i32, i64, i32, i32, i32, i32, C.POINTER(sz)]),
+            ("glu_product_plan", [i32, i64, i32, i32, i32, i32, C.POINTER(_LinPlan)]),
+            ("glu_forward", [vp, i64, i32, i64, i32, i32, vp, i64, vp, i32, vp, i64, vp, i64, qp, qp, vp, sz, vp]),
+            ("glu_backward_act", [vp, i64, vp, i64, qp, qp, i32, i64, i32, i32, vp, i64, vp, i64, vp]),
+            ("glu_backward_input", [vp, i64, i32, i64, i32, i32, vp, i64, i32, vp, i64, qp, qp, vp, i64, vp, i64, vp, sz, vp])):
         fn = getattr(lib, name)
         fn.restype = i32
         fn.argtypes = types
@@ -191,7 +238,10 @@ EXPORTED = ("acsc_last_error", "acsc_version", "acsc_stats_enable", "acsc_stats_
             "psgd_workspace_size", "psgd_project", "psgd_orthogonalize", "psgd_decompress", "psgd_step",
             "q8_encode", "q8_decode", "ln_forward", "ln_recompute", "ln_workspace_size", "ln_backward",
             "lin_workspace_size", "lin_workspace_size_unaligned", "lin_product_plan", "lin_forward", "lin_backward_act",
-            "lin_backward_input", "lin_backward_weight")
+            "lin_backward_input", "lin_backward_weight",
+            "drop_apply", "rms_forward", "rms_recompute", "rms_backward", "join_workspace_size", "join_forward", "join_backward",
+            "glu_workspace_size", "glu_workspace_size_unaligned", "glu_product_plan", "glu_forward", "glu_backward_act",
+            "glu_backward_input")
 
 
 def _check(rc: int):
@@ -1058,3 +1108,366 @@ def lin_backward_weight(dz: torch.Tensor, x: Union[torch.Tensor, Q8], act: str =
     if rc:
         _check(rc)
     return dW, db
+
+
+# ---------------------------------------------------------------------------
+# The gated feed-forward block (include/acsc.h has the formulas).
+# ---------------------------------------------------------------------------
+GLU_FORWARD, GLU_BACKWARD_INPUT = 0, 1
+
+
+def _here(*ts):
+    """Calls run on the current device: their tensors have to be there."""
+    dev = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in ts) else None
+    for t in ts:
+        if t is not None and t.is_cuda and t.get_device() != dev:
+            raise AcscError(ACSC_EINVAL, f"a tensor is on cuda:{t.get_device()}, the current device is cuda:{dev}")
+
+
+def _drop_ref(drop: Optional[Drop]):
+    if drop is None:
+        return None
+    p, key, site = drop
+    if not isinstance(key, MaskKey):
+        raise AcscError(ACSC_EINVAL, "a dropout's key comes from make_key")
+    if not 0 <= site < 1 << 32:
+        raise AcscError(ACSC_EINVAL, f"site={site} outside [0, 2^32)")
+    return C.byref(_DropMask(key, site, p))
+
+
+def _opt(t: Optional[torch.Tensor], shape, dtype: torch.dtype, name: str):
+    """(address, row stride) of a tensor that may be None."""
+    return (None, 0) if t is None else (t.data_ptr(), _rows(t, shape, dtype, name))
+
+
+def _optvec(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, name: str):
+    return None if t is None else _vec(t, n, dtype, name)
+
+
+def _new(t: Optional[torch.Tensor], shape, dtype: torch.dtype, device, name: str):
+    """(tensor, row stride) of an output: the given one, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device), max(shape[1], 1)
+    return t, _rows(t, shape, dtype, name)
+
+
+def _sums(t: Optional[torch.Tensor], want: bool, H: int, accumulate: bool, device, name: str):
+    """A column sum's fp32 [H] output: the given one or a new one; None where it is not wanted."""
+    if not want:
+        if t is not None:
+            raise AcscError(ACSC_EINVAL, f"{name} is given, but not wanted")
+        return None
+    if t is None:
+        if accumulate:
+            raise AcscError(ACSC_EINVAL, f"accumulate needs {name}")
+        return torch.empty(H, dtype=torch.float32, device=device)
+    return t
+
+
+def drop_apply(x: torch.Tensor, drop: Drop, residual: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """D(x) + residual for x [rows, H]; D's gradient is the same call on dy."""
+    if stream is not None:
+        return _on(stream, drop_apply, x, drop, residual, y)
+    shape = rows, H = _two_d(x, "x")
+    _here(x, residual, y)
+    dtype = x.dtype
+    ld = _rows(x, shape, dtype, "x")
+    pr, ldr = _opt(residual, shape, dtype, "residual")
+    y, ldy = _new(y, (rows, H), dtype, x.device, "y")
+    rc = lib.drop_apply(x.data_ptr(), _dt(x), rows, H, ld, _drop_ref(drop), pr, ldr, y.data_ptr(), ldy, _raw_stream())
+    if rc:
+        _check(rc)
+    return y
+
+
+def rms_forward(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, eps: float = 1e-5, checkpoint: bool = False,
+                y: Optional[torch.Tensor] = None, stream=None):
+    """Root-mean-square norm of the rows of x [rows, H]: (y, rstd [rows], q), q
+    the 8-bit checkpoint of x if asked for, else None."""
+    if stream is not None:
+        return _on(stream, rms_forward, x, gamma, eps, checkpoint, y)
+    shape = rows, H = _two_d(x, "x")
+    _here(x, gamma, y)
+    dtype, dev = x.dtype, x.device
+    ld = _rows(x, shape, dtype, "x")
+    pg = _optvec(gamma, H, dtype, "gamma")
+    y, ldy = _new(y, (rows, H), dtype, dev, "y")
+    rstd = torch.empty(rows, dtype=torch.float32, device=dev)
+    q = _q8_new(rows, H, dev) if checkpoint else None
+    rc = lib.rms_forward(x.data_ptr(), _dt(x), rows, H, ld, pg, eps, y.data_ptr(), ldy, rstd.data_ptr(),
+                         None if q is None else _q8_ref(q, rows, H), _raw_stream())
+    if rc:
+        _check(rc)
+    return y, rstd, q
+
+
+def rms_recompute(src: Union[torch.Tensor, Q8], rstd: torch.Tensor, gamma: Optional[torch.Tensor] = None,
+                  dtype: torch.dtype = torch.bfloat16, y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """rms_forward's y again from x or its checkpoint and the kept rstd."""
+    if stream is not None:
+        return _on(stream, rms_recompute, src, rstd, gamma, dtype, y)
+    rows, H = _two_d(src.codes if isinstance(src, Q8) else src, "src")
+    _here(*(src if isinstance(src, Q8) else (src,)), rstd, gamma, y)
+    p, ld, q = _kept(src, (rows, H), dtype, "src")
+    pr = _vec(rstd, rows, torch.float32, "rstd")
+    pg = _optvec(gamma, H, dtype, "gamma")
+    y, ldy = _new(y, (rows, H), dtype, rstd.device, "y")
+    _check(lib.rms_recompute(p, ld, q, _dt(y), rows, H, pr, pg, y.data_ptr(), ldy, _raw_stream()))
+    return y
+
+
+def join_workspace_size(rows: int, H: int) -> int:
+    b = C.c_size_t(0)
+    _check(lib.join_workspace_size(rows, H, C.byref(b)))
+    return b.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _join_bytes(rows: int, H: int) -> int:
+    return join_workspace_size(rows, H)
+
+
+def rms_backward(dy: torch.Tensor, src: Union[torch.Tensor, Q8], rstd: torch.Tensor, gamma: Optional[torch.Tensor] = None,
+                 add: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                 dgamma: Optional[torch.Tensor] = None, accumulate: bool = False, ws: Optional[torch.Tensor] = None,
+                 stream=None, weights: bool = True):
+    """(dx, dgamma) of rms_forward from x or its checkpoint; add: the gradient
+    that reaches x past the norm.  dgamma: fp32 [H]; with accumulate it is given
+    and added to; without weights it is not formed, and None."""
+    if stream is not None:
+        return _on(stream, rms_backward, dy, src, rstd, gamma, add, dx, dgamma, accumulate, ws, None, weights)
+    shape = rows, H = _two_d(dy, "dy")
+    _here(dy, *(src if isinstance(src, Q8) else (src,)), rstd, gamma, add, dx, dgamma, ws)
+    dtype, dev = dy.dtype, dy.device
+    lddy = _rows(dy, shape, dtype, "dy")
+    p, ld, q = _kept(src, shape, dtype, "src")
+    pa, ldadd = _opt(add, shape, dtype, "add")
+    dx, lddx = _new(dx, (rows, H), dtype, dev, "dx")
+    dgamma = _sums(dgamma, weights, H, accumulate, dev, "dgamma")
+    pdg = _optvec(dgamma, H, torch.float32, "dgamma")
+    wp, wn, hold = _ws(_join_bytes(rows, H), ws, dev) if weights else (None, 0, None)
+    pr, pg = _vec(rstd, rows, torch.float32, "rstd"), _optvec(gamma, H, dtype, "gamma")
+    rc = lib.rms_backward(dy.data_ptr(), lddy, p, ld, q, _dt(dy), rows, H, pr, pg, pa, ldadd, dx.data_ptr(), lddx, pdg,
+                          int(accumulate), wp, wn, _raw_stream())
+    if rc:
+        _check(rc)
+    return dx, dgamma
+
+
+def join_forward(r: torch.Tensor, b: torch.Tensor, post: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                 pre: Optional[torch.Tensor] = None, scale: float = 1.0, drop: Optional[Drop] = None, eps: float = 1e-5,
+                 checkpoint: bool = False, out: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                 stream=None) -> Joined:
+    """out = scale r + D(gate norm(b)) and y = norm(out) for the residual stream
+    r and a branch b [rows, H], in one pass.  post, pre: the gains of the norms
+    of b and of out; None: no such norm (without pre, y is None).  checkpoint:
+    8-bit checkpoints of out and b too."""
+    if stream is not None:
+        return _on(stream, join_forward, r, b, post, gate, pre, scale, drop, eps, checkpoint, out, y)
+    shape = rows, H = _two_d(r, "r")
+    _here(r, b, post, gate, pre, out, y)
+    dtype, dev = r.dtype, r.device
+    ldr, ldb = _rows(r, shape, dtype, "r"), _rows(b, shape, dtype, "b")
+    pp, pg, pn = _optvec(post, H, dtype, "post"), _optvec(gate, H, dtype, "gate"), _optvec(pre, H, dtype, "pre")
+    out, ldo = _new(out, (rows, H), dtype, dev, "out")
+    py, ldy = None, 0
+    if pre is not None:
+        y, ldy = _new(y, (rows, H), dtype, dev, "y")
+        py = y.data_ptr()
+    elif y is not None:
+        raise AcscError(ACSC_EINVAL, "y is given, but there is no norm after (pre)")
+    rstd_post = torch.empty(rows, dtype=torch.float32, device=dev) if post is not None else None
+    rstd_pre = torch.empty(rows, dtype=torch.float32, device=dev) if pre is not None else None
+    q_out, q_b = (_q8_new(rows, H, dev), _q8_new(rows, H, dev)) if checkpoint else (None, None)
+    rc = lib.join_forward(r.data_ptr(), ldr, b.data_ptr(), ldb, _dt(r), rows, H, pp, pg, scale, _drop_ref(drop), pn, eps,
+                          out.data_ptr(), ldo, py, ldy, None if rstd_post is None else rstd_post.data_ptr(),
+                          None if rstd_pre is None else rstd_pre.data_ptr(), None if q_out is None else _q8_ref(q_out, rows, H),
+                          None if q_b is None else _q8_ref(q_b, rows, H), _raw_stream())
+    if rc:
+        _check(rc)
+    return Joined(out, y, rstd_post, rstd_pre, q_out, q_b)
+
+
+def join_backward(dout: Optional[torch.Tensor], dy: Optional[torch.Tensor], out: Union[torch.Tensor, Q8, None],
+                  b: Union[torch.Tensor, Q8, None], rstd_post: Optional[torch.Tensor] = None,
+                  rstd_pre: Optional[torch.Tensor] = None, post: Optional[torch.Tensor] = None,
+                  gate: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, scale: float = 1.0,
+                  drop: Optional[Drop] = None, dr: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None,
+                  dpost: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None,
+                  dpre: Optional[torch.Tensor] = None, accumulate: bool = False, ws: Optional[torch.Tensor] = None,
+                  stream=None, weights: bool = True) -> JoinGrads:
+    """Gradients of join_forward from dout and dy (one of them may be None), out
+    and b or their checkpoints, and the kept statistics.  dpost, dgate, dpre: fp32
+    [H], of the gains that there are (dpre where there is dy); with accumulate
+    they are given and added to; without weights they are not formed."""
+    if stream is not None:
+        return _on(stream, join_backward, dout, dy, out, b, rstd_post, rstd_pre, post, gate, pre, scale, drop, dr, db, dpost,
+                   dgate, dpre, accumulate, ws, None, weights)
+    one = dout if dout is not None else dy
+    if one is None:
+        raise AcscError(ACSC_EINVAL, "one of dout and dy is needed")
+    shape = rows, H = _two_d(one, "dout" if one is dout else "dy")
+    _here(dout, dy, *(out if isinstance(out, Q8) else (out,)), *(b if isinstance(b, Q8) else (b,)), rstd_post, rstd_pre, post,
+          gate, pre, dr, db, dpost, dgate, dpre, ws)
+    if dy is not None and pre is None:
+        raise AcscError(ACSC_EINVAL, "dy without the norm after (pre)")
+    dtype, dev = one.dtype, one.device
+    pdo, lddo = _opt(dout, shape, dtype, "dout")
+    pdy, lddy = _opt(dy, shape, dtype, "dy")
+    po, ldo, qo = _kept(out, shape, dtype, "out")
+    pb, ldb, qb = _kept(b, shape, dtype, "b")
+    pp, pg, pn = _optvec(post, H, dtype, "post"), _optvec(gate, H, dtype, "gate"), _optvec(pre, H, dtype, "pre")
+    prp, prn = _optvec(rstd_post, rows, torch.float32, "rstd_post"), _optvec(rstd_pre, rows, torch.float32, "rstd_pre")
+    dr, lddr = _new(dr, (rows, H), dtype, dev, "dr")
+    db, lddb = _new(db, (rows, H), dtype, dev, "db")
+    dpost = _sums(dpost, weights and post is not None, H, accumulate, dev, "dpost")
+    dgate = _sums(dgate, weights and gate is not None, H, accumulate, dev, "dgate")
+    dpre = _sums(dpre, weights and dy is not None, H, accumulate, dev, "dpre")
+    pdp, pdg = _optvec(dpost, H, torch.float32, "dpost"), _optvec(dgate, H, torch.float32, "dgate")
+    pdn = _optvec(dpre, H, torch.float32, "dpre")
+    wp, wn, hold = (None, 0, None) if pdp is pdg is pdn is None else _ws(_join_bytes(rows, H), ws, dev)
+    rc = lib.join_backward(pdo, lddo, pdy, lddy, po, ldo, qo, pb, ldb, qb, _dt(one), rows, H, pp, pg, scale, _drop_ref(drop),
+                           pn, prp, prn, dr.data_ptr(), lddr, db.data_ptr(), lddb, pdp, pdg, pdn, int(accumulate), wp, wn,
+                           _raw_stream())
+    if rc:
+        _check(rc)
+    return JoinGrads(dr, db, dpost, dgate, dpre)
+
+
+def glu_workspace_size(op: int, rows: int, n_in: int, F: int, dtype: torch.dtype, checkpoint: bool = False) -> int:
+    """Bytes for glu_forward (GLU_FORWARD; checkpoint: keep="q8") or glu_backward_input (GLU_BACKWARD_INPUT, n_in its
+    n_out) with operands as in lin_workspace_size."""
+    b = C.c_size_t(0)
+    _check(lib.glu_workspace_size(op, rows, n_in, F, BF16 if dtype == torch.bfloat16 else F32, int(checkpoint), C.byref(b)))
+    return b.value
+
+
+def glu_workspace_size_unaligned(op: int, rows: int, n_in: int, F: int, dtype: torch.dtype, checkpoint: bool = False) -> int:
+    """The same for operands of any alignment and stride."""
+    b = C.c_size_t(0)
+    _check(lib.glu_workspace_size_unaligned(op, rows, n_in, F, BF16 if dtype == torch.bfloat16 else F32, int(checkpoint),
+                                            C.byref(b)))
+    return b.value
+
+
+def glu_product_plan(op: int, rows: int, n_in: int, F: int, dtype: torch.dtype, checkpoint: bool = False) -> LinPlan:
+    """How that product runs; a tile of the forward product holds tile_cols / 2 hidden columns."""
+    p = _LinPlan()
+    _check(lib.glu_product_plan(op, rows, n_in, F, BF16 if dtype == torch.bfloat16 else F32, int(checkpoint), C.byref(p)))
+    return LinPlan(p.tile_rows, p.tile_cols, p.whole, p.cut, p.pieces)
+
+
+@functools.lru_cache(maxsize=1024)
+def _glu_bytes(aligned: bool, op: int, rows: int, n_in: int, F: int, dtype: torch.dtype, checkpoint: bool) -> int:
+    return (glu_workspace_size if aligned else glu_workspace_size_unaligned)(op, rows, n_in, F, dtype, checkpoint)
+
+
+def _glu_ws(op: int, rows: int, n_in: int, F: int, checkpoint: bool, a, lda: int, b, ldb: int, ws: Optional[torch.Tensor]):
+    if ws is not None:
+        return _ws(0, ws, a.device)
+    aligned = lda < 1 << 21 and ldb < 1 << 21
+    if aligned and a.dtype is torch.bfloat16:
+        aligned = not ((lda | a.data_ptr() >> 1 | ldb | b.data_ptr() >> 1) & 1)
+    return _ws(_glu_bytes(aligned, op, rows, n_in, F, a.dtype, checkpoint), None, a.device)
+
+
+def _even(n: int, name: str) -> int:
+    if n % 2:
+        raise AcscError(ACSC_EINVAL, f"{name} has the gate's half and the up projection's: an even number, not {n}")
+    return n // 2
+
+
+def _kept_pair(z, rows: int, F: int, dtype: torch.dtype):
+    """(pointer, row stride, gate's checkpoint, up's checkpoint) of kept pre-activations."""
+    if isinstance(z, torch.Tensor):
+        return z.data_ptr(), _rows(z, (rows, 2 * F), dtype, "z"), None, None
+    if not (isinstance(z, tuple) and len(z) == 2 and isinstance(z[0], Q8) and isinstance(z[1], Q8)):
+        raise AcscError(ACSC_EINVAL, "z must be a [rows, 2 F] tensor or the pair of checkpoints that glu_forward keeps")
+    return None, 0, _q8_ref(z[0], rows, F), _q8_ref(z[1], rows, F)
+
+
+def _flat_kept(z):
+    return (z,) if isinstance(z, torch.Tensor) else [t for q in (z if isinstance(z, tuple) else ()) if isinstance(q, Q8) for t in q]
+
+
+def glu_forward(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "silu",
+                keep: Optional[str] = None, h: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """h = act(x Wg^T + bg) (x Wu^T + bu) for x [rows, n_in] and W [2 F, n_in],
+    Wg's rows first, bias [2 F] alike: (h [rows, F], kept), kept the
+    pre-activations [rows, 2 F] if keep is "z", their 8-bit checkpoints (gate,
+    up) if keep is "q8", else None."""
+    if stream is not None:
+        return _on(stream, glu_forward, x, W, bias, act, keep, h, ws)
+    rows, n_in = _two_d(x, "x")
+    n_out = _two_d(W, "W")[0]
+    F = _even(n_out, "W's rows")
+    _here(x, W, bias, h, ws)
+    dtype, dev = x.dtype, x.device
+    ldx, ldw = _rows(x, (rows, n_in), dtype, "x"), _rows(W, (n_out, n_in), dtype, "W")
+    pb = _optvec(bias, n_out, dtype, "bias")
+    h, ldh = _new(h, (rows, F), dtype, dev, "h")
+    kept = pz = qg = qu = None
+    if keep == "z":
+        kept = torch.empty((rows, n_out), dtype=dtype, device=dev)
+        pz = kept.data_ptr()
+    elif keep == "q8":
+        kept = _q8_new(rows, F, dev), _q8_new(rows, F, dev)
+        qg, qu = _q8_ref(kept[0], rows, F), _q8_ref(kept[1], rows, F)
+    elif keep is not None:
+        raise AcscError(ACSC_EINVAL, f"keep must be None, 'z' or 'q8', not {keep!r}")
+    wp, wn, hold = _glu_ws(GLU_FORWARD, rows, n_in, F, keep == "q8", x, ldx, W, ldw, ws)
+    rc = lib.glu_forward(x.data_ptr(), ldx, _dt(x), rows, n_in, F, W.data_ptr(), ldw, pb, _act(act), h.data_ptr(), ldh, pz,
+                         n_out, qg, qu, wp, wn, _raw_stream())
+    if rc:
+        _check(rc)
+    return h, kept
+
+
+def glu_backward_act(dh: torch.Tensor, z, act: str = "silu", hidden: bool = False, dz: Optional[torch.Tensor] = None,
+                     h: Optional[torch.Tensor] = None, stream=None):
+    """(dz [rows, 2 F], h) of glu_forward from dh [rows, F] and what it kept; h,
+    the hidden activation again, if hidden (or if it is given), else None."""
+    if stream is not None:
+        return _on(stream, glu_backward_act, dh, z, act, hidden, dz, h)
+    rows, F = _two_d(dh, "dh")
+    _here(dh, *_flat_kept(z), dz, h)
+    dtype, dev = dh.dtype, dh.device
+    lddh = _rows(dh, (rows, F), dtype, "dh")
+    pz, ldz, qg, qu = _kept_pair(z, rows, F, dtype)
+    dz, lddz = _new(dz, (rows, 2 * F), dtype, dev, "dz")
+    ph, ldh = None, 0
+    if hidden or h is not None:
+        h, ldh = _new(h, (rows, F), dtype, dev, "h")
+        ph = h.data_ptr()
+    rc = lib.glu_backward_act(dh.data_ptr(), lddh, pz, ldz, qg, qu, _dt(dh), rows, F, _act(act), dz.data_ptr(), lddz, ph, ldh,
+                              _raw_stream())
+    if rc:
+        _check(rc)
+    return dz, h
+
+
+def glu_backward_input(dy: torch.Tensor, W: torch.Tensor, z, act: str = "silu", hidden: bool = False,
+                       dz: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                       stream=None):
+    """glu_backward_act with dh = dy W of the linear layer behind, dy [rows,
+    n_out], W [n_out, F], in that product's epilogue: (dz [rows, 2 F], h)."""
+    if stream is not None:
+        return _on(stream, glu_backward_input, dy, W, z, act, hidden, dz, h, ws)
+    rows, n_out = _two_d(dy, "dy")
+    F = _two_d(W, "W")[1]
+    _here(dy, W, *_flat_kept(z), dz, h, ws)
+    dtype, dev = dy.dtype, dy.device
+    lddy, ldw = _rows(dy, (rows, n_out), dtype, "dy"), _rows(W, (n_out, F), dtype, "W")
+    pz, ldz, qg, qu = _kept_pair(z, rows, F, dtype)
+    dz, lddz = _new(dz, (rows, 2 * F), dtype, dev, "dz")
+    ph, ldh = None, 0
+    if hidden or h is not None:
+        h, ldh = _new(h, (rows, F), dtype, dev, "h")
+        ph = h.data_ptr()
+    wp, wn, hold = _glu_ws(GLU_BACKWARD_INPUT, rows, n_out, F, False, dy, lddy, W, ldw, ws)
+    rc = lib.glu_backward_input(dy.data_ptr(), lddy, _dt(dy), rows, F, n_out, W.data_ptr(), ldw, _act(act), pz, ldz, qg, qu,
+                                dz.data_ptr(), lddz, ph, ldh, wp, wn, _raw_stream())
+    if rc:
+        _check(rc)
+    return dz, h

@@ -15,7 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libacsc.so")
 OBJDIR = os.path.join(HERE, "_build")
 SOURCES = ["common.hip", "ac.hip", "sc.hip", "pass.hip", "blend.hip", "chol.hip", "orth.hip", "f32.hip",
-           "static_scratch.hip", "q8.hip", "ln.hip", "lin.hip", "lin_tile.hip", "lin_few.hip"]
+           "static_scratch.hip", "q8.hip", "ln.hip", "lin.hip", "lin_tile.hip", "lin_few.hip",
+           "glu.hip", "glu_tile.hip", "drop.hip", "join.hip"]
 ARCH = "gfx950"
 
 

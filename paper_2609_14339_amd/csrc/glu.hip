@@ -1,0 +1,378 @@
+// The gated linear layer, h = act(x Wg^T + bg) (x Wu^T + bu): the entry points,
+// the sum of a cut product's pieces, and the gradient through the gate alone.
+#include "lin_plan.h"
+
+namespace acsc {
+namespace {
+
+// Pieces of tiles: a workgroup takes 2048 hidden columns' worth of rows, a
+// thread eight columns, of units of UH columns: a tile's 64 or 128, or with a
+// checkpoint two tiles of 64, so that sixteen lanes hold a group.
+template <typename TO, int TM, int T, int UH>
+__global__ __launch_bounds__(256) void glu_join_kernel(Gemm g)
+{
+    constexpr int TC = T / 2, PER = TM * UH / 2048, SPAN = UH / TC;   // tiles of a unit
+    const int64_t count = static_cast<int64_t>(g.tm) * g.tn - g.whole, unit = blockIdx.x / PER;
+    const int c = (blockIdx.x % PER) * 256 + threadIdx.x, row = c / (UH / 8);
+    int col = c % (UH / 8) * 8, tile_m, tile_n;
+    int64_t id = unit;
+    if (SPAN > 1) {
+        // every tile is cut; the pairs of a row of tiles follow one another
+        const int pairs = (g.tn + 1) / 2;
+        tile_m = static_cast<int>(unit / pairs);
+        tile_n = static_cast<int>(unit % pairs) * 2 + col / TC;
+        col %= TC;
+        const int band = tile_m / 4, height = min(g.tm - band * 4, 4);
+        id = static_cast<int64_t>(band) * 4 * g.tn + static_cast<int64_t>(tile_n) * height + tile_m % 4;
+    } else {
+        tile_at(g, g.whole + id, tile_m, tile_n);
+    }
+    const int64_t m = static_cast<int64_t>(tile_m) * TM + row;
+    const int n = tile_n * TC + col, left = m < g.M ? g.N - n : 0;
+    float vg[8] = {}, vu[8] = {}, bg[8], bu[8];
+    if (left > 0) {
+        const float *p = g.part + (id * TM + row) * T + col / 64 * 128 + col % 64;
+        add_pieces(p, count * TM * T, g.splits, vg);
+        add_pieces(p + 64, count * TM * T, g.splits, vu);
+    }
+    glu_bias<TO>(g.e, g.N, n, bg, bu);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        vg[i] += bg[i];
+        vu[i] += bu[i];
+    }
+    glu_epilogue<TO>(g.e, g.N, vg, vu, max16(mag8(vg, left)), max16(mag8(vu, left)), m, n, left);
+}
+
+// Pieces of a product for few tokens: 2048 columns of a row a workgroup.
+template <typename TO>
+__global__ __launch_bounds__(256) void glu_join_few_kernel(Gemm g)
+{
+    const int64_t m = blockIdx.y, step = g.M * 2 * g.ldp;
+    const int n = (blockIdx.x * 256 + threadIdx.x) * 8, left = g.N - n;
+    float vg[8] = {}, vu[8] = {}, bg[8], bu[8];
+    if (left > 0) {
+        const float *p = g.part + m * 2 * g.ldp + n;
+        add_pieces(p, step, g.splits, vg);
+        add_pieces(p + g.ldp, step, g.splits, vu);
+    }
+    glu_bias<TO>(g.e, g.N, n, bg, bu);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        vg[i] += bg[i];
+        vu[i] += bu[i];
+    }
+    glu_epilogue<TO>(g.e, g.N, vg, vu, max16(mag8(vg, left)), max16(mag8(vu, left)), m, n, left);
+}
+
+// Pieces of dh, then the gate's gradient.
+template <typename TO, int TM, int T>
+__global__ __launch_bounds__(256) void glu_gate_join_kernel(Gemm g)
+{
+    constexpr int PER = TM * T / 2048;
+    const int64_t id = blockIdx.x / PER, count = static_cast<int64_t>(g.tm) * g.tn - g.whole;
+    const int c = (blockIdx.x % PER) * 256 + threadIdx.x, row = c / (T / 8), col = c % (T / 8) * 8;
+    int tile_m, tile_n;
+    tile_at(g, g.whole + id, tile_m, tile_n);
+    const int64_t m = static_cast<int64_t>(tile_m) * TM + row;
+    const int n = tile_n * T + col, left = m < g.M ? g.N - n : 0;
+    if (left <= 0)
+        return;
+    float v[8];
+    add_pieces(g.part + (id * TM + row) * T + col, count * TM * T, g.splits, v);
+    GluBeside<TO> beside;
+    load_glu_beside<TO>(g.e, g.N, beside, m, n, left);
+    glu_gate_epilogue<TO>(g.e, g.N, v, beside, m, n, left);
+}
+
+// The gate's gradient of a given dh: a wave takes 512 columns of a row, eight a
+// lane.
+template <typename T>
+__global__ __launch_bounds__(256) void glu_act_kernel(const T *dh, int64_t lddh, int64_t rows, int F, Epi e)
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int segs = (F + 511) / 512;
+    for (int64_t w = static_cast<int64_t>(blockIdx.x) * 4 + wave; w < rows * segs; w += static_cast<int64_t>(gridDim.x) * 4) {
+        const int64_t row = w / segs;
+        const int col = static_cast<int>(w - row * segs) * 512 + lane * 8, left = F - col;
+        if (left <= 0)
+            continue;
+        float v[8];
+        load8(dh + row * lddh + col, left, v);
+        GluBeside<T> beside;
+        load_glu_beside<T>(e, F, beside, row, col, left);
+        glu_gate_epilogue<T>(e, F, v, beside, row, col, left);
+    }
+}
+
+template <typename TO, int TM, int T>
+void launch_join(const Gemm &g, EpiKind kind, hipStream_t st)
+{
+    const int64_t tail = static_cast<int64_t>(g.tm) * g.tn - g.whole;
+    if (kind == kGluGate) {
+        ACSC_LAUNCH("glu_join", (glu_gate_join_kernel<TO, TM, T>), dim3(static_cast<unsigned>(tail * (TM * T / 2048))), dim3(256), 0,
+                    st, g);
+        return;
+    }
+    if constexpr (T >= 128) {
+        if (T == 128 && g.e.q.codes) {
+            const int64_t units = static_cast<int64_t>(g.tm) * ((g.tn + 1) / 2);
+            ACSC_LAUNCH("glu_join", (glu_join_kernel<TO, TM, T, 128>), dim3(static_cast<unsigned>(units * (TM * 128 / 2048))),
+                        dim3(256), 0, st, g);
+        } else {
+            ACSC_LAUNCH("glu_join", (glu_join_kernel<TO, TM, T, T / 2>), dim3(static_cast<unsigned>(tail * (TM * (T / 2) / 2048))),
+                        dim3(256), 0, st, g);
+        }
+    }
+}
+
+template <typename TO>
+void join_tiles(const Gemm &g, const Plan &p, EpiKind kind, hipStream_t st)
+{
+    if (p.rows == 256)
+        launch_join<TO, 256, 256>(g, kind, st);
+    else if (p.tile == 64)
+        launch_join<TO, 128, 64>(g, kind, st);
+    else if (p.rows == 128)
+        launch_join<TO, 128, 128>(g, kind, st);
+    else if (p.rows == 64)
+        launch_join<TO, 64, 128>(g, kind, st);
+    else
+        launch_join<TO, 32, 128>(g, kind, st);
+}
+
+// Host checks of kept pre-activations: z [rows, 2 F] or both checkpoints.
+inline int check_kept_pair(const void *z, int64_t ld_z, const q8_tensor *qg, const q8_tensor *qu, int64_t rows, int F, int dt)
+{
+    ACSC_CHECK_ARG(rows == 0 || (z != nullptr) != (qg != nullptr && qu != nullptr), ACSC_EINVAL,
+                   "exactly one of z and the pair of its checkpoints is needed");
+    ACSC_CHECK_ARG((qg != nullptr) == (qu != nullptr), ACSC_EINVAL, "one checkpoint of the pair is missing");
+    if (z)
+        return check_mat(z, true, ld_z, 2 * F, dt, "z");
+    if (!qg)
+        return ACSC_OK;
+    if (int rc = check_q8(qg, rows, F))
+        return rc;
+    return check_q8(qu, rows, F);
+}
+
+inline int check_glu(int64_t rows, int n_in, int F, int dt)
+{
+    if (int rc = check_layer(rows, n_in, F, dt))
+        return rc;
+    ACSC_CHECK_ARG(F <= (1 << 21), ACSC_EINVAL, "F=%d outside [1, 2^21]", F);
+    return ACSC_OK;
+}
+
+// The plan of a product, with the operands' copies that bits 0 (A) and 1 (B) of
+// `copies` add to those that are needed whatever the alignment.
+int plan_glu(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, bool codes, int copies, Plan &p)
+{
+    const EpiKind kind = op == GLU_FORWARD ? kGluForward : kGluGate;
+    // the gradient's product is the down projection's: its inputs are the F hidden columns
+    const Shape s = op == GLU_FORWARD ? shape_of(kind, rows, n_in, F) : shape_of(kind, rows, F, n_in);
+    const auto best = [&](bool col, int64_t inner) {
+        return readable(Operand{nullptr, dt == ACSC_F32 ? inner : (inner + 1) / 2 * 2}, col, inner, dt);
+    };
+    const bool a = best(s.acol, s.acol ? s.M : s.K), b = best(s.bcol, s.bcol ? s.N : s.K);
+    p = plan_of(kind, s, dt, a && !(copies & 1), b && !(copies & 2), codes);
+    return check_tiles(p);
+}
+
+int workspace_size(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int checkpoint, bool any, size_t *bytes)
+{
+    clear_error();
+    if (int rc = check_glu(rows, n_in, F, dt))
+        return rc;
+    ACSC_CHECK_ARG(bytes, ACSC_EINVAL, "null pointer to the result");
+    ACSC_CHECK_ARG(op == GLU_FORWARD || op == GLU_BACKWARD_INPUT, ACSC_EINVAL, "unknown product %d", (int)op);
+    *bytes = 0;
+    if (rows == 0)
+        return ACSC_OK;
+    // with any alignment: the most that either operand's copy, or its absence, takes
+    size_t most = 0;
+    for (int copies = 0; copies < (any ? 4 : 1); ++copies) {
+        Plan p;
+        if (int rc = plan_glu(op, rows, n_in, F, dt, op == GLU_FORWARD && checkpoint, copies, p))
+            return rc;
+        most = std::max(most, p.bytes());
+    }
+    *bytes = most;
+    return ACSC_OK;
+}
+
+}  // namespace
+
+void glu_join_run(const Gemm &g, const Plan &p, EpiKind kind, acsc_dtype dt, hipStream_t st)
+{
+    const bool b = dt == ACSC_BF16;
+    if (p.few) {
+        const dim3 grid((g.N + 2047) / 2048, static_cast<unsigned>(g.M));
+        if (b)
+            ACSC_LAUNCH("glu_join", glu_join_few_kernel<uint16_t>, grid, dim3(256), 0, st, g);
+        else
+            ACSC_LAUNCH("glu_join", glu_join_few_kernel<float>, grid, dim3(256), 0, st, g);
+    } else if (b) {
+        join_tiles<uint16_t>(g, p, kind, st);
+    } else {
+        join_tiles<float>(g, p, kind, st);
+    }
+}
+
+}  // namespace acsc
+
+using namespace acsc;
+
+extern "C" int glu_workspace_size(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int checkpoint, size_t *bytes)
+{
+    return workspace_size(op, rows, n_in, F, dt, checkpoint, false, bytes);
+}
+
+extern "C" int glu_workspace_size_unaligned(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int checkpoint, size_t *bytes)
+{
+    return workspace_size(op, rows, n_in, F, dt, checkpoint, true, bytes);
+}
+
+extern "C" int glu_product_plan(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int checkpoint, lin_plan *plan)
+{
+    clear_error();
+    if (int rc = check_glu(rows, n_in, F, dt))
+        return rc;
+    ACSC_CHECK_ARG(plan, ACSC_EINVAL, "null pointer to the result");
+    ACSC_CHECK_ARG(op == GLU_FORWARD || op == GLU_BACKWARD_INPUT, ACSC_EINVAL, "unknown product %d", (int)op);
+    *plan = lin_plan{};
+    if (rows == 0)
+        return ACSC_OK;
+    Plan p;
+    if (int rc = plan_glu(op, rows, n_in, F, dt, op == GLU_FORWARD && checkpoint, 0, p))
+        return rc;
+    *plan = {p.rows, p.tile, p.whole, static_cast<int64_t>(p.tm) * p.tn - p.whole, p.splits};
+    return ACSC_OK;
+}
+
+extern "C" int glu_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t rows, int n_in, int F, const void *W, int64_t ld_w,
+                           const void *bias, acsc_act act, void *h, int64_t ld_h, void *z, int64_t ld_z, const q8_tensor *q_gate,
+                           const q8_tensor *q_up, void *ws, size_t ws_bytes, hipStream_t stream)
+{
+    clear_error();
+    if (int rc = check_glu(rows, n_in, F, dt))
+        return rc;
+    if (int rc = check_act(act))
+        return rc;
+    const bool some = rows > 0;
+    if (int rc = check_mat(x, some, ld_x, n_in, dt, "x"))
+        return rc;
+    if (int rc = check_mat(W, some, ld_w, n_in, dt, "W"))
+        return rc;
+    if (int rc = check_mat(h, some, ld_h, F, dt, "h"))
+        return rc;
+    ACSC_CHECK_ARG(aligned(bias, dtype_size(dt)), ACSC_EALIGN, "bias not aligned to its elements");
+    if (z)
+        if (int rc = check_mat(z, some, ld_z, 2 * F, dt, "z"))
+            return rc;
+    ACSC_CHECK_ARG(!some || (h != x && h != W && h != z), ACSC_EINVAL, "h must not overlap x, W or z");
+    ACSC_CHECK_ARG(!some || !z || (z != x && z != W), ACSC_EINVAL, "z must not overlap x or W");
+    ACSC_CHECK_ARG((q_gate != nullptr) == (q_up != nullptr), ACSC_EINVAL, "one checkpoint of the pair is missing");
+    for (const q8_tensor *q : {q_gate, q_up})
+        if (q)
+            if (int rc = check_q8(q, rows, F))
+                return rc;
+    if (!some)
+        return ACSC_OK;
+    Gemm g{};
+    g.A = {x, ld_x};
+    g.B = {W, ld_w};
+    const Shape s = shape_of(kGluForward, rows, n_in, F);
+    const Plan p = plan_of(kGluForward, s, dt, readable(g.A, false, n_in, dt), readable(g.B, false, n_in, dt), q_gate != nullptr);
+    if (int rc = check_tiles(p))
+        return rc;
+    if (int rc = check_ws(ws, ws_bytes, p.bytes()))
+        return rc;
+    g.e = Epi{h, ld_h, bias, nullptr, 0, z, ld_z, q8_of(q_gate), act, 0, q8_of(q_up), nullptr, 0};
+    return run_product(g, kGluForward, p, s, dt, dt, static_cast<char *>(ws), nullptr, nullptr, stream, "glu_forward");
+}
+
+extern "C" int glu_backward_act(const void *dh, int64_t ld_dh, const void *z, int64_t ld_z, const q8_tensor *q_gate,
+                                const q8_tensor *q_up, acsc_dtype dt, int64_t rows, int F, acsc_act act, void *dz, int64_t ld_dz,
+                                void *h, int64_t ld_h, hipStream_t stream)
+{
+    clear_error();
+    if (int rc = check_glu(rows, 1, F, dt))
+        return rc;
+    if (int rc = check_act(act))
+        return rc;
+    const bool some = rows > 0;
+    if (int rc = check_mat(dh, some, ld_dh, F, dt, "dh"))
+        return rc;
+    if (int rc = check_kept_pair(z, ld_z, q_gate, q_up, rows, F, dt))
+        return rc;
+    if (int rc = check_mat(dz, some, ld_dz, 2 * F, dt, "dz"))
+        return rc;
+    if (h)
+        if (int rc = check_mat(h, some, ld_h, F, dt, "h"))
+            return rc;
+    ACSC_CHECK_ARG(!some || (dz != dh && dz != h), ACSC_EINVAL, "dz must not overlap dh or h");
+    ACSC_CHECK_ARG(!some || dz != z || ld_dz == ld_z, ACSC_EINVAL, "dz in place of z needs ld_dz == ld_z");
+    ACSC_CHECK_ARG(!some || !h || h != dh || ld_h == ld_dh, ACSC_EINVAL, "h in place of dh needs ld_h == ld_dh");
+    ACSC_CHECK_ARG(!some || !h || h != z, ACSC_EINVAL, "h must not overlap z");
+    if (!some)
+        return ACSC_OK;
+    Epi e{};
+    e.y = dz;
+    e.ldy = ld_dz;
+    e.z = const_cast<void *>(z);
+    e.ldz = ld_z;
+    e.q = q8_of(q_gate);
+    e.q_up = q8_of(q_up);
+    e.act = act;
+    e.hidden = h;
+    e.ldh = ld_h;
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>((rows * ((F + 511) / 512) + 3) / 4, 1 << 20)));
+    if (dt == ACSC_BF16)
+        ACSC_LAUNCH("glu_backward_act", glu_act_kernel<uint16_t>, grid, dim3(256), 0, stream, static_cast<const uint16_t *>(dh), ld_dh,
+                    rows, F, e);
+    else
+        ACSC_LAUNCH("glu_backward_act", glu_act_kernel<float>, grid, dim3(256), 0, stream, static_cast<const float *>(dh), ld_dh, rows,
+                    F, e);
+    return check_launch("glu_backward_act");
+}
+
+extern "C" int glu_backward_input(const void *dy, int64_t ld_dy, acsc_dtype dt, int64_t rows, int F, int n_out, const void *W,
+                                  int64_t ld_w, acsc_act act, const void *z, int64_t ld_z, const q8_tensor *q_gate,
+                                  const q8_tensor *q_up, void *dz, int64_t ld_dz, void *h, int64_t ld_h, void *ws, size_t ws_bytes,
+                                  hipStream_t stream)
+{
+    clear_error();
+    if (int rc = check_glu(rows, n_out, F, dt))
+        return rc;
+    if (int rc = check_act(act))
+        return rc;
+    const bool some = rows > 0;
+    if (int rc = check_mat(dy, some, ld_dy, n_out, dt, "dy"))
+        return rc;
+    if (int rc = check_mat(W, some, ld_w, F, dt, "W"))
+        return rc;
+    if (int rc = check_kept_pair(z, ld_z, q_gate, q_up, rows, F, dt))
+        return rc;
+    if (int rc = check_mat(dz, some, ld_dz, 2 * F, dt, "dz"))
+        return rc;
+    if (h)
+        if (int rc = check_mat(h, some, ld_h, F, dt, "h"))
+            return rc;
+    ACSC_CHECK_ARG(!some || (dz != dy && dz != W && dz != h), ACSC_EINVAL, "dz must not overlap dy, W or h");
+    ACSC_CHECK_ARG(!some || !h || (h != dy && h != W && h != z), ACSC_EINVAL, "h must not overlap dy, W or z");
+    ACSC_CHECK_ARG(!some || dz != z || ld_dz == ld_z, ACSC_EINVAL, "dz in place of z needs ld_dz == ld_z");
+    if (!some)
+        return ACSC_OK;
+    Gemm g{};
+    g.A = {dy, ld_dy};
+    g.B = {W, ld_w};
+    const Shape s = shape_of(kGluGate, rows, F, n_out);
+    const Plan p = plan_of(kGluGate, s, dt, readable(g.A, false, n_out, dt), readable(g.B, true, F, dt));
+    if (int rc = check_tiles(p))
+        return rc;
+    if (int rc = check_ws(ws, ws_bytes, p.bytes()))
+        return rc;
+    g.e = Epi{dz, ld_dz, nullptr, nullptr, 0, const_cast<void *>(z), ld_z, q8_of(q_gate), act, 0, q8_of(q_up), h, ld_h};
+    return run_product(g, kGluGate, p, s, dt, dt, static_cast<char *>(ws), nullptr, nullptr, stream, "glu_backward_input");
+}

@@ -20,7 +20,10 @@ struct Operand {
 
 // Epilogues.  Forward: z = C + bias, kept whole or coded, then act(z) +
 // residual.  Gate: C act'(z) of a kept z.  Weight: C, or added to the output.
-enum EpiKind { kForward = 0, kGate = 1, kWeight = 2 };
+// The gated product's, with rows of B for the gate and, F after each, for the
+// up projection: GluForward: g, u = C + bias, kept whole or coded, then
+// act(g) u.  GluGate: (C u act'(g), C act(g)) of kept g and u, and act(g) u.
+enum EpiKind { kForward = 0, kGate = 1, kWeight = 2, kGluForward = 3, kGluGate = 4 };
 
 struct Epi {
     void *y;
@@ -33,12 +36,18 @@ struct Epi {
     Q8 q;             // forward: out or none; gate: in or none
     int act;
     int accumulate;
+    // The gated product's: z [rows, 2 F] (gate, then up) or q and q_up, out
+    // (forward, where y is the hidden activation) or in (gate, where y is
+    // [rows, 2 F] and hidden an output or nullptr).
+    Q8 q_up;
+    void *hidden;
+    int64_t ldh;
 };
 
 struct Gemm {
     Operand A, B;
     int64_t M;
-    int N, K;
+    int N, K;         // kGluForward: N = F, and B has 2 F rows
     int tm, tn;       // tiles along M and N
     int whole;        // tiles that are not cut along K; the rest is cut into
     int splits;       // pieces of kchunk each
@@ -211,11 +220,175 @@ __device__ __forceinline__ void put_db(const Gemm &g, int64_t m0, int rows)
     }
 }
 
+// a = act(g) and s = act'(g), eight at a time.
+template <typename T>
+__device__ __forceinline__ void act_both(const float (&g)[8], int act, float (&a)[8], float (&s)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        a[i] = g[i];
+        s[i] = 1.f;
+    }
+    apply_act<T>(a, act);
+    apply_slope<T>(s, g, act);
+}
+
+// The gated product forward: eight columns n .. n + 7 of row m of g and u
+// through the epilogue; `left` of them exist.  ag, au: the largest magnitudes
+// of their groups of 128 columns (with codes only).
+template <typename T>
+__device__ __forceinline__ void glu_epilogue(const Epi &e, int F, float (&g)[8], float (&u)[8], uint32_t ag, uint32_t au,
+                                             int64_t m, int n, int left)
+{
+    if (e.z) {
+        T *z = static_cast<T *>(e.z) + m * e.ldz + n;
+        store8(z, left, g);
+        store8(z + F, left, u);
+    }
+    if (e.q.codes) {
+        const auto code = [&](const Q8 &q, uint32_t a, const float (&v)[8]) {
+            float scale, inv;
+            group_scale(a, scale, inv);
+            store_codes(q.codes + m * q.ldc + n, left, inv, v);
+            if (left > 0 && n % kGroup == 0)
+                q.scales[m * q.lds + n / kGroup] = scale;
+        };
+        code(e.q, ag, g);
+        code(e.q_up, au, u);
+    }
+    apply_act<T>(g, e.act);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        g[i] *= u[i];
+    store8(static_cast<T *>(e.y) + m * e.ldy + n, left, g);
+}
+// The largest magnitude of the first `left` of eight values.
+__device__ __forceinline__ uint32_t mag8(const float (&v)[8], int left)
+{
+    uint32_t a = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        a = max(a, i < left ? mag(v[i]) : 0u);
+    return a;
+}
+template <typename T>
+__device__ __forceinline__ void glu_bias(const Epi &e, int F, int n, float (&bg)[8], float (&bu)[8])
+{
+    const T *b = static_cast<const T *>(e.bias) + n;
+    load8(b, e.bias ? F - n : 0, bg);
+    load8(b + F, e.bias ? F - n : 0, bu);
+}
+
+// The gated product's gradient: eight columns of row m of dh = C through the
+// epilogue, from kept g and u.
+template <typename T>
+struct GluBeside {
+    Beside<T> g, u;
+};
+template <typename T>
+__device__ __forceinline__ void load_glu_beside(const Epi &e, int F, GluBeside<T> &b, int64_t m, int n, int left)
+{
+    GluBeside<T> r = {};
+    if (e.q.codes) {
+        load_raw(e.q.codes + m * e.q.ldc + n, left, r.g.codes);
+        load_raw(e.q_up.codes + m * e.q_up.ldc + n, left, r.u.codes);
+        r.g.scale = left > 0 ? e.q.scales[m * e.q.lds + n / kGroup] : 0.f;
+        r.u.scale = left > 0 ? e.q_up.scales[m * e.q_up.lds + n / kGroup] : 0.f;
+    } else {
+        const T *z = static_cast<const T *>(e.z) + m * e.ldz + n;
+        load_raw(z, left, r.g.v);
+        load_raw(z + F, left, r.u.v);
+    }
+    b = r;
+}
+template <typename T>
+__device__ __forceinline__ void glu_gate_epilogue(const Epi &e, int F, float (&v)[8], const GluBeside<T> &b, int64_t m, int n,
+                                                  int left)
+{
+    float g[8], u[8], a[8], s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        g[i] = e.q.codes ? code_value(b.g.codes.at(i), b.g.scale) : b.g.v.at(i);
+        u[i] = e.q.codes ? code_value(b.u.codes.at(i), b.u.scale) : b.u.v.at(i);
+    }
+    act_both<T>(g, e.act, a, s);
+    if (e.hidden) {
+        float h[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            h[i] = a[i] * u[i];
+        store8(static_cast<T *>(e.hidden) + m * e.ldh + n, left, h);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        s[i] *= v[i] * u[i];
+        a[i] *= v[i];
+    }
+    T *y = static_cast<T *>(e.y) + m * e.ldy + n;
+    store8(y, left, s);
+    store8(y + F, left, a);
+}
+
+// A wave's accumulators of 16 NA rows by 64 hidden columns through the gated
+// epilogue: fragments 0 .. 3 of a row hold g, 4 .. 7 u.  Eight lanes take a
+// row, eight rows a step.  tops: the rows' largest magnitudes [wn][g, u][row]
+// with codes, of both waves that hold a group.
+template <typename T, int NA>
+__device__ __forceinline__ void put_glu_rows(const Gemm &g, const char *lds, int64_t m0, int n0, const uint32_t *tops)
+{
+    const int lane = threadIdx.x & 63, n = n0 + (lane & 7) * 8, c = (lane & 7) * 2;
+    const int cols = g.N - n;
+    float bg[8], bu[8];
+    glu_bias<T>(g.e, g.N, n, bg, bu);
+#pragma unroll 1
+    for (int r0 = 0; r0 < NA * 16; r0 += 8) {
+        const int row = r0 + (lane >> 3);
+        const auto chunk = [&](int k) { return *reinterpret_cast<const f32x4 *>(lds + row * 512 + (k ^ (row & 31)) * 16); };
+        const f32x4 g0 = chunk(c), g1 = chunk(c + 1), u0 = chunk(16 + c), u1 = chunk(17 + c);
+        float vg[8] = {g0[0], g0[1], g0[2], g0[3], g1[0], g1[1], g1[2], g1[3]};
+        float vu[8] = {u0[0], u0[1], u0[2], u0[3], u1[0], u1[1], u1[2], u1[3]};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            vg[i] += bg[i];
+            vu[i] += bu[i];
+        }
+        uint32_t ag = 0, au = 0;
+        if (g.e.q.codes) {
+            ag = max(tops[row], tops[128 + row]);
+            au = max(tops[64 + row], tops[192 + row]);
+        }
+        const int64_t m = m0 + row;
+        glu_epilogue<T>(g.e, g.N, vg, vu, ag, au, m, n, m < g.M ? cols : 0);
+    }
+}
+template <typename T, int NA>
+__device__ __forceinline__ void put_glu_gate_rows(const Gemm &g, const char *lds, int64_t m0, int n0, int end)
+{
+    const int lane = threadIdx.x & 63, n = n0 + (lane & 15) * 8, c = (lane & 15) * 2;
+    const int cols = end - n;
+#pragma unroll 1
+    for (int r0 = 0; r0 < NA * 4; r0 += 4) {
+        GluBeside<T> beside[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            load_glu_beside<T>(g.e, g.N, beside[u], min<int64_t>(m0 + (r0 + u) * 4 + (lane >> 4), g.M - 1), n, cols);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int row = (r0 + u) * 4 + (lane >> 4);
+            const f32x4 lo = *reinterpret_cast<const f32x4 *>(lds + row * 512 + (c ^ (row & 31)) * 16);
+            const f32x4 hi = *reinterpret_cast<const f32x4 *>(lds + row * 512 + ((c + 1) ^ (row & 31)) * 16);
+            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            const int64_t m = m0 + row;
+            glu_gate_epilogue<T>(g.e, g.N, v, beside[u], m, n, m < g.M ? cols : 0);
+        }
+    }
+}
+
 // The tile's columns stop at `end`.  `part`: the piece's rows and columns of
-// this wave, ld a row, or nullptr.
+// this wave, ld a row, or nullptr.  `tops`: see put_glu_rows.
 template <typename T, int KIND, int NA>
 __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8], char *lds, int64_t m0, int n0,
-                                         int end, float *part, int ld)
+                                         int end, float *part, int ld, const uint32_t *tops)
 {
     const int lane = threadIdx.x & 63;
     if (part) {
@@ -239,7 +412,11 @@ __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    if (n0 + 128 <= end)
+    if constexpr (KIND == kGluForward)
+        put_glu_rows<T, NA>(g, lds, m0, n0, tops);
+    else if constexpr (KIND == kGluGate)
+        put_glu_gate_rows<T, NA>(g, lds, m0, n0, end);
+    else if (n0 + 128 <= end)
         put_rows<T, KIND, NA, true>(g, lds, m0, n0, end);
     else
         put_rows<T, KIND, NA, false>(g, lds, m0, n0, end);

@@ -1,48 +1,11 @@
 // Linear layers: the entry points, how a product is cut, and the kernels
 // before and after it.
-#include "lin.h"
+#include "lin_plan.h"
 
 namespace acsc {
 
-int lin_few_run(const Gemm &g, acsc_dtype dt, hipStream_t st, const char *tag);
-int lin_few_weight_run(const Gemm &g, const Kept &kept, acsc_dtype dt, acsc_dtype out, float *db, hipStream_t st,
-                       const char *tag);
-int lin_tile_run(const Gemm &g, int rows, int cols, EpiKind kind, acsc_dtype dt, acsc_dtype out, hipStream_t st,
-                 const char *tag);
-
 namespace {
 
-// Tokens up to which a product does without tiles.  Forward: W is read once
-// and unstaged; 4096 -> 14336, 1 / 8 / 16 tokens, us: bf16 24, 28, 35 against 31
-// by tiles for 4 to 64; fp32 53, 60, 68 against 56.  Where the tile kernel
-// cannot read W it has to be copied first, three times its bytes: there the
-// kernel is used as far as it goes.  Weight gradient: outer products of
-// unrounded activations; bf16 8192 -> 8192, 1 / 4 / 8 tokens: 25.6, 30.0, 38.8
-// against 43 by tiles.  (The input gradient by vector FMAs on rows of W read
-// once took 39 against 31 by tiles.)
-inline int few_tokens(EpiKind kind, bool fits_b)
-{
-    return kind == kForward ? (fits_b ? 8 : 16) : kind == kWeight ? 8 : 0;
-}
-
-// Adds the pieces of a cut product in order and takes the sum through the
-// epilogue, eight columns a thread: of few tokens, 2048 columns of a row a
-// workgroup; of tiles, 2048 elements of a tile.
-__device__ __forceinline__ void add_pieces(const float *p, int64_t step, int splits, float (&v)[8])
-{
-    const f32x4 *q = reinterpret_cast<const f32x4 *>(p);
-    f32x4 lo = q[0], hi = q[1];
-#pragma unroll 4
-    for (int i = 1; i < splits; ++i) {
-        lo += q[i * step / 4];
-        hi += q[i * step / 4 + 1];
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[i] = lo[i];
-        v[4 + i] = hi[i];
-    }
-}
 template <int KIND, typename TO>
 __device__ __forceinline__ void join(const Gemm &g, const float *p, int64_t step, bool on, int64_t m, int n)
 {
@@ -190,53 +153,6 @@ __global__ __launch_bounds__(256) void lin_act_kernel(const T *dy, int64_t lddy,
     }
 }
 
-inline size_t up256(size_t b) { return (b + 255) / 256 * 256; }
-
-// How a product is cut, and what of the workspace it takes: the pieces, db's
-// pieces, and copies of the operands that the tile kernel cannot read where
-// they are.
-struct Plan {
-    bool few;                               // the product for few tokens
-    int rows, tile;                         // of a tile: its rows and columns
-    int tm, tn, whole, splits, kchunk;
-    int slices, slice;                      // of the rows, for db
-    int64_t ldp;
-    bool pack_a, pack_b;
-    int64_t lda, ldb;                       // row strides of the copies
-    size_t part, db, a, b;                  // bytes
-    size_t bytes() const { return part + db + a + b; }
-};
-
-inline int up8(int n) { return (n + 7) / 8 * 8; }
-
-// A row operand keeps the sum's index in its rows, a col operand its own.
-struct Shape {
-    int64_t M;
-    int N, K;
-    bool acol, bcol;
-};
-inline Shape shape_of(EpiKind kind, int64_t rows, int n_in, int n_out)
-{
-    if (kind == kForward)
-        return {rows, n_out, n_in, false, false};
-    if (kind == kGate)
-        return {rows, n_in, n_out, false, true};
-    return {n_out, n_in, static_cast<int>(rows), true, true};
-}
-
-// Whether the tile kernel reads an operand where it is: rows at multiples of
-// the word that the DMA reads, rows of whole words, of a chunk at least if a
-// col operand's last chunk runs on into the next row, and offsets within a
-// tile and step of under 2^31 bytes.  Both sides, bf16 rows at odd words
-// copied first or read there, us: 20 x 4098 -> 14338 67 and 29, 8190 x 8190 ->
-// 8190 907 and 890, its input gradient 899 and 813.
-inline bool readable(const Operand &o, bool col, int64_t inner, acsc_dtype dt)
-{
-    const int es = static_cast<int>(dtype_size(dt)), chunk = 16 / es, unit = 4 / es;
-    return aligned(o.p, unit * es) && o.ld % unit == 0 && inner * es % 4 == 0 && (!col || inner % chunk == 0 || o.ld >= chunk) &&
-           o.ld * es * (col ? 64 : 256) < (1ll << 31);
-}
-
 // Tile and pieces of the sum, by the least estimated time.  A round is what
 // the card runs at once, `at_once` workgroups a CU.  Whole rounds of tiles are
 // not cut; the tiles of a last, partial one may be, so that their pieces fill
@@ -263,7 +179,9 @@ struct Tile {
     double step, alone;   // us of a step with as many, and with one
     double edge;
 };
-inline Cut cut_of(EpiKind kind, const Shape &s, int steps, bool bf16)
+// codes: a gated product's pre-activations are coded, whose groups lie in two
+// tiles of 128 columns each: there every tile goes through the pieces' sum.
+inline Cut cut_of(EpiKind kind, const Shape &s, int steps, bool bf16, bool codes)
 {
     static const Tile kBf16[] = {
         {256, 256, 1, 1.5, 1.5, 5}, {128, 128, 2, 1.0, 0.65, 3}, {64, 128, 3, 1.05, 0.85, 3}, {32, 128, 4, 1.0, 0.8, 3}, {128, 64, 2, 0.8, 0.55, 3}};
@@ -274,7 +192,7 @@ inline Cut cut_of(EpiKind kind, const Shape &s, int steps, bool bf16)
     for (const Tile *t = first; t != end; ++t) {
         // 32 rows of a col operand are not a whole block of it in LDS; 64
         // columns would split the group of a checkpoint that is written
-        if ((t->rows == 32 && kind == kWeight) || (t->cols == 64 && kind == kForward && s.N > 64))
+        if ((t->rows == 32 && kind == kWeight) || (t->cols == 64 && (kind == kGluForward || (kind == kForward && s.N > 64))))
             continue;
         const int64_t tiles = ((s.M + t->rows - 1) / t->rows) * ((s.N + t->cols - 1) / t->cols);
         const int slots = 256 * t->at_once;
@@ -283,23 +201,26 @@ inline Cut cut_of(EpiKind kind, const Shape &s, int steps, bool bf16)
             const double step = t->at_once > 1 ? t->alone + (t->step - t->alone) * static_cast<double>(beside) / (t->at_once - 1) : t->alone;
             return static_cast<double>(groups / slots) * (per * t->step + t->edge) + (rest ? per * step + t->edge : 0);
         };
-        const int64_t rest = tiles % slots;
+        const bool all = codes && kind == kGluForward && t->cols == 128;   // through the pieces' sum
+        const int64_t rest = all ? tiles : tiles % slots;
         for (int want = 1; want == 1 || (rest && want <= 64 && steps / want >= 4 && rest * want <= 2048);
              want += want < 8 ? 1 : 8) {
             const int per = (steps + want - 1) / want, n = (steps + per - 1) / per;
-            const double us = n == 1 ? rounds(tiles, steps)
+            const double us = n == 1 && !all ? rounds(tiles, steps)
                                      : rounds(tiles - rest, steps) + rounds(rest * n, per) + 10 +
                                            n * static_cast<double>(rest) * t->rows * t->cols * 8 / 4.5e6;
             if (least == 0 || us < least) {
                 least = us;
-                best = Cut{t->rows, t->cols, static_cast<int>(n == 1 ? tiles : tiles - rest), n, per};
+                best = Cut{t->rows, t->cols, static_cast<int>(n == 1 && !all ? tiles : tiles - rest), n, per};
             }
         }
     }
     return best;
 }
 
-inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bool fits_b)
+}  // namespace
+
+Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bool fits_b, bool codes)
 {
     Plan p{};
     const bool bf16 = dt == ACSC_BF16;
@@ -311,20 +232,21 @@ inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bo
         p.splits = 1;
         return p;
     }
-    if (kind == kForward && s.M <= few_tokens(kind, fits_b)) {
+    if ((kind == kForward || kind == kGluForward) && s.M <= few_tokens(kind, fits_b)) {
         // 16 outputs a workgroup: a cut only where they fill half the CUs at
         // most, at two rounds of eight lines a piece
-        const int groups = (s.N + 15) / 16, round = 8 * 128 / static_cast<int>(dtype_size(dt)), rounds = (s.K + round - 1) / round;
+        const int cols = kind == kGluForward ? s.N / 2 : s.N;   // 16 of the gate and 16 up ones
+        const int groups = (cols + 15) / 16, round = 8 * 128 / static_cast<int>(dtype_size(dt)), rounds = (s.K + round - 1) / round;
         const int want = groups >= 128 ? 1 : std::max(1, std::min((255 + groups) / groups, rounds / 2));
         const int per = (rounds + want - 1) / want;
         p.few = true;
         p.splits = (rounds + per - 1) / per;
         p.kchunk = per * round;
-        p.ldp = up8(s.N);
-        p.part = up256(static_cast<size_t>(p.splits) * s.M * p.ldp * 4);
+        p.ldp = up8(cols);
+        p.part = up256(static_cast<size_t>(p.splits) * s.M * p.ldp * 4 * (s.N / cols));
         return p;
     }
-    const Cut c = cut_of(kind, s, steps, bf16);
+    const Cut c = cut_of(kind, s, steps, bf16, codes);
     p.rows = c.rows;
     p.tile = c.tile;
     p.tm = static_cast<int>((s.M + p.rows - 1) / p.rows);
@@ -351,6 +273,8 @@ inline Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bo
     return p;
 }
 
+namespace {
+
 template <int KIND, typename TO>
 void launch_join(const Gemm &g, const Plan &p, hipStream_t st)
 {
@@ -376,13 +300,6 @@ void launch_join(const Gemm &g, const Plan &p, hipStream_t st)
     ACSC_LAUNCH("lin_join", (lin_join_kernel<KIND, TO, 128, 128>), grid, dim3(256), 0, st, g);
 }
 
-// An input of the weight gradient that is formed again from what was kept.
-struct Again {
-    Operand from;
-    void *to;
-    Kept kept;
-};
-
 inline void add_operand(Jobs &jobs, const Operand &from, int64_t rows, int cols, void *to, int64_t ld, const Kept &kept)
 {
     Job &j = jobs.j[jobs.n++];
@@ -397,13 +314,15 @@ inline void add_operand(Jobs &jobs, const Operand &from, int64_t rows, int cols,
     j.blocks = static_cast<int>(std::min<int64_t>((rows * ((cols + 511) / 512) + 3) / 4, 1 << 18));
 }
 
+}  // namespace
+
 // What comes first, the product and its pieces' sum; `out` is the type of the
 // output.
 int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype dt, acsc_dtype out, char *ws, float *db,
                 const Again *again, hipStream_t st, const char *tag)
 {
     g.M = s.M;
-    g.N = s.N;
+    g.N = kind == kGluForward ? s.N / 2 : s.N;
     g.K = s.K;
     g.tm = p.tm;
     g.tn = p.tn;
@@ -414,9 +333,10 @@ int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype
     const int chunk = 16 / static_cast<int>(dtype_size(dt));
     g.words_a = !p.pack_a && (s.acol ? s.M : s.K) % chunk;
     g.words_b = !p.pack_b && !again && (s.bcol ? s.N : s.K) % chunk;
-    // the product for few tokens: a piece goes through memory if there are
-    // more, or if its workgroups hold no whole checkpoint groups
-    const bool pieces = p.splits > 1 || (p.few && g.e.q.codes);
+    // a piece goes through memory if there are more, or if the workgroups of a
+    // product for few tokens, or of narrow tiles of a gated one, hold no whole
+    // checkpoint groups
+    const bool pieces = p.splits > 1 || (g.e.q.codes && (p.few || (kind == kGluForward && p.tile == 128)));
     g.part = pieces ? reinterpret_cast<float *>(ws) : nullptr;
     Jobs jobs{};
     if (again)
@@ -462,14 +382,17 @@ int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype
             return rc;
     }
     if (p.few) {
-        if (int rc = lin_few_run(g, dt, st, tag))
+        if (int rc = kind == kGluForward ? glu_few_run(g, dt, st, tag) : lin_few_run(g, dt, st, tag))
             return rc;
-    } else if (int rc = lin_tile_run(g, p.rows, p.tile, kind, dt, out, st, tag)) {
+    } else if (int rc = kind >= kGluForward ? glu_tile_run(g, p.rows, p.tile, kind, dt, st, tag)
+                                            : lin_tile_run(g, p.rows, p.tile, kind, dt, out, st, tag)) {
         return rc;
     }
     if (pieces) {
         const bool b = out == ACSC_BF16;
-        if (p.few) {
+        if (kind >= kGluForward) {
+            glu_join_run(g, p, kind, dt, st);
+        } else if (p.few) {
             const dim3 grid((g.N + 2047) / 2048, static_cast<unsigned>(g.M));
             if (b)
                 ACSC_LAUNCH("lin_join", lin_join_few_kernel<uint16_t>, grid, dim3(256), 0, st, g);
@@ -488,53 +411,7 @@ int run_product(Gemm &g, EpiKind kind, const Plan &p, const Shape &s, acsc_dtype
     return ACSC_OK;
 }
 
-inline int check_layer(int64_t rows, int n_in, int n_out, int dt)
-{
-    ACSC_CHECK_ARG(dt == ACSC_F32 || dt == ACSC_BF16, ACSC_EDTYPE, "unknown dtype %d", dt);
-    ACSC_CHECK_ARG(rows >= 0 && rows < (1ll << 31), ACSC_EINVAL, "rows=%lld outside [0, 2^31)", (long long)rows);
-    ACSC_CHECK_ARG(n_in >= 1 && n_in <= (1 << 22), ACSC_EINVAL, "n_in=%d outside [1, 2^22]", n_in);
-    ACSC_CHECK_ARG(n_out >= 1 && n_out <= (1 << 22), ACSC_EINVAL, "n_out=%d outside [1, 2^22]", n_out);
-    return ACSC_OK;
-}
-
-inline int check_mat(const void *p, bool need, int64_t ld, int cols, int dt, const char *name)
-{
-    ACSC_CHECK_ARG(!need || p, ACSC_EINVAL, "null pointer %s", name);
-    ACSC_CHECK_ARG(ld >= cols && ld < (1ll << 40), ACSC_EINVAL, "ld of %s is %lld for %d columns", name, (long long)ld, cols);
-    ACSC_CHECK_ARG(aligned(p, dtype_size(static_cast<acsc_dtype>(dt))), ACSC_EALIGN, "%s not aligned to its elements",
-                   name);
-    return ACSC_OK;
-}
-
-// A kept pre-activation: one of z and q.
-inline int check_kept(const void *z, int64_t ldz, const q8_tensor *q, int64_t rows, int cols, int dt)
-{
-    ACSC_CHECK_ARG(rows == 0 || (z != nullptr) != (q != nullptr), ACSC_EINVAL, "exactly one of the tensor and its checkpoint is needed");
-    if (z)
-        return check_mat(z, true, ldz, cols, dt, "z");
-    return q ? check_q8(q, rows, cols) : ACSC_OK;
-}
-
-inline int check_ws(const void *ws, size_t have, size_t need)
-{
-    if (need == 0)
-        return ACSC_OK;
-    ACSC_CHECK_ARG(ws, ACSC_EINVAL, "null workspace");
-    ACSC_CHECK_ARG(aligned(ws, 256), ACSC_EALIGN, "workspace not 256-byte aligned");
-    ACSC_CHECK_ARG(have >= need, ACSC_ENOSPC, "workspace of %zu bytes, %zu needed", have, need);
-    return ACSC_OK;
-}
-
-// The largest launch of tiles: a grid has under 2^32 threads along x.
-inline int check_tiles(const Plan &p)
-{
-    if (p.few)
-        return ACSC_OK;
-    const int64_t tiles = static_cast<int64_t>(p.tm) * p.tn, threads = 64 * waves(p.rows, p.tile);
-    ACSC_CHECK_ARG(tiles * threads < (1ll << 32) && (p.whole + (tiles - p.whole) * p.splits) * threads < (1ll << 32),
-                   ACSC_EINVAL, "product too large: %lld tiles of %d x %d", (long long)tiles, p.rows, p.tile);
-    return ACSC_OK;
-}
+namespace {
 
 // Bytes of an activation recomputed for the weight gradient.
 inline size_t recomputed_bytes(int64_t rows, int n_in, acsc_dtype dt)

@@ -7,7 +7,7 @@
 // lane) in flight, and multiply them with the same k of the tokens, which
 // stay in the caches.  Their sums meet in LDS in wave order.  One token, bf16
 // 4096 -> 14336: 24 us, 4.9 TB/s of weights, what a copy reaches.
-#include "lin.h"
+#include "lin_plan.h"
 
 namespace acsc {
 namespace {
@@ -119,6 +119,87 @@ __global__ __launch_bounds__(kWaves * 64) void lin_few_kernel(Gemm g)
     }
 }
 
+// The gated product for few tokens, the same way: a workgroup takes 16 hidden
+// columns, a wave the lines of both of their rows of W.
+template <typename T>
+__global__ __launch_bounds__(kWaves * 64) void glu_few_kernel(Gemm g)
+{
+    constexpr int E = 16 / sizeof(T), LINE = 8 * E, U = 4;   // k of a chunk and of a line; lines in flight
+    __shared__ __align__(16) float meet[kWaves][2][16][16];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int n0 = blockIdx.x * 16, split = blockIdx.y;
+    const int kbeg = split * g.kchunk, kend = min(g.K, kbeg + g.kchunk);
+    const int k = (lane >> 4) * E;
+    const T *w[2];
+    w[0] = static_cast<const T *>(g.B.p) + min(n0 + (lane & 15), g.N - 1) * g.B.ld;
+    w[1] = w[0] + g.N * g.B.ld;
+    const T *x = static_cast<const T *>(g.A.p) + min<int64_t>(lane & 15, g.M - 1) * g.A.ld;
+    f32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+
+    int k0 = kbeg + wave * LINE;
+    for (; k0 + ((U - 1) * kWaves + 1) * LINE <= kend; k0 += U * kWaves * LINE) {
+        Any16 a[2][U][2], b[U][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int o = 0; o < 2; ++o)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    a[o][u][h] = *reinterpret_cast<const Any16 *>(w[o] + k0 + u * kWaves * LINE + h * 4 * E + k);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                b[u][h] = *reinterpret_cast<const Any16 *>(x + k0 + u * kWaves * LINE + h * 4 * E + k);
+        __builtin_amdgcn_sched_barrier(0);   // all loads leave before the first product
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int o = 0; o < 2; ++o)
+                    acc[o] = multiply<T>(a[o][u][h], b[u][h], acc[o]);
+    }
+    for (; k0 < kend; k0 += kWaves * LINE)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int at = k0 + h * 4 * E + k;
+            const Any16 b = load16(x + at, kend - at);
+#pragma unroll
+            for (int o = 0; o < 2; ++o)
+                acc[o] = multiply<T>(load16(w[o] + at, kend - at), b, acc[o]);
+        }
+
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+        *reinterpret_cast<f32x4 *>(&meet[wave][o][lane & 15][(lane >> 4) * 4]) = acc[o];
+    __syncthreads();
+    const int m = threadIdx.x >> 1, c = (threadIdx.x & 1) * 8, n = n0 + c;
+    if (m >= 16 || m >= g.M)
+        return;
+    float v[2][8] = {};
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+        for (int i = 0; i < kWaves; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v[o][j] += meet[i][o][m][c + j];
+    if (g.part) {
+        float *part = g.part + (split * g.M + m) * 2 * g.ldp + n;
+        store8(part, g.N - n, v[0]);
+        store8(part + g.ldp, g.N - n, v[1]);
+        return;
+    }
+    float bias[2][8];
+    glu_bias<T>(g.e, g.N, n, bias[0], bias[1]);
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[o][j] += bias[o][j];
+    glu_epilogue<T>(g.e, g.N, v[0], v[1], 0, 0, m, n, g.N - n);   // without a checkpoint
+}
+
 // The weight gradient of few tokens: outer products, bound by writing dW.  A
 // lane holds eight columns of the T inputs in fp32 (formed here from what was
 // kept, so nothing is rounded on the way), a wave `per` rows of dW one after
@@ -206,6 +287,16 @@ int lin_few_run(const Gemm &g, acsc_dtype dt, hipStream_t st, const char *tag)
         ACSC_LAUNCH(tag, lin_few_kernel<uint16_t>, grid, dim3(kWaves * 64), 0, st, g);
     else
         ACSC_LAUNCH(tag, lin_few_kernel<float>, grid, dim3(kWaves * 64), 0, st, g);
+    return check_launch(tag);
+}
+
+int glu_few_run(const Gemm &g, acsc_dtype dt, hipStream_t st, const char *tag)
+{
+    const dim3 grid(static_cast<unsigned>((g.N + 15) / 16), g.splits);
+    if (dt == ACSC_BF16)
+        ACSC_LAUNCH(tag, glu_few_kernel<uint16_t>, grid, dim3(kWaves * 64), 0, st, g);
+    else
+        ACSC_LAUNCH(tag, glu_few_kernel<float>, grid, dim3(kWaves * 64), 0, st, g);
     return check_launch(tag);
 }
 

@@ -7,7 +7,7 @@
 // values), and the result is written.  NT threads share a row, in chunks of
 // 8 NT columns; rows of up to 2048 columns belong to one wave, which needs no
 // barrier, wider ones to a workgroup.
-#include "q8.h"
+#include "rows.h"
 
 #include <type_traits>
 
@@ -15,45 +15,6 @@ namespace acsc {
 namespace {
 
 constexpr int kMaxH = 32768;
-
-// Sum over the wave, in every lane: rows of 16 by row_ror, then across rows.
-__device__ __forceinline__ float wave_sum(float x)
-{
-#define ACSC_ROR(n) x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + n, 0xF, 0xF, false))
-    ACSC_ROR(8);
-    ACSC_ROR(4);
-    ACSC_ROR(2);
-    ACSC_ROR(1);
-#undef ACSC_ROR
-    x += __shfl_xor(x, 16);
-    x += __shfl_xor(x, 32);
-    return x;
-}
-
-// Sums over the NT threads of a row.  `slot` holds NT / 64 values per sum and
-// is written once between two barriers of the caller's row loop.
-template <int NT, int N>
-__device__ __forceinline__ void row_sum(float (&s)[N], float *slot)
-{
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        s[i] = wave_sum(s[i]);
-    if (NT > 64) {
-        constexpr int W = NT / 64;
-        if ((threadIdx.x & 63) == 0)
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                slot[i * W + (threadIdx.x >> 6)] = s[i];
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            s[i] = 0.f;
-#pragma unroll
-            for (int w = 0; w < W; ++w)
-                s[i] += slot[i * W + w];
-        }
-    }
-}
 
 template <typename T>
 struct Fwd {
@@ -174,20 +135,6 @@ struct Bwd {
     int64_t rows;
     int H;
 };
-
-// Makes the compiler take what it knows of stored words as new: values are
-// then formed from them again instead of being kept in registers.
-template <int N>
-__device__ __forceinline__ void again(uint32_t (&w)[N])
-{
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        asm volatile("" : "+v"(w[i]));
-}
-template <int N>
-__device__ __forceinline__ void again(float (&)[N])
-{
-}
 
 // A workgroup walks rows blockIdx.x, + gridDim.x, ... (four at a time where a
 // wave holds a row) and keeps the column sums of dy h and dy in registers;
