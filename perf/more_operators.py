@@ -273,11 +273,11 @@ def _run_own(st):
             return dict(h=h, kept=kept)
         return dict(h=h, kept_gate=acsc.q8_decode(kept[0], dt), kept_up=acsc.q8_decode(kept[1], dt))
     z = tuple(acsc.Q8(*q) for q in st["z"]) if case["ckpt"] else st["z"]
-    dz, h = acsc.glu_backward_input(st["dy"], st["W2"], z, act=case["act"], hidden=True)
+    dz, h, dbias = acsc.glu_backward_input(st["dy"], st["W2"], z, act=case["act"], hidden=True, bias=case["whole"])
     if not case["whole"]:
         return dict(dz=dz, h=h)
     dW2, _ = acsc.lin_backward_weight(st["dy"], h, bias=False)
-    dW, dbias = acsc.lin_backward_weight(dz, st["x"])
+    dW, _ = acsc.lin_backward_weight(dz, st["x"], bias=False)
     return dict(dx=acsc.lin_backward_input(dz, st["W"]), dW=dW, dbias=dbias, dW2=dW2)
 
 
