@@ -695,14 +695,14 @@ int join_backward(const void *dout, int64_t ld_dout, const void *dy, int64_t ld_
 /* Which product of a gated linear layer a workspace is for. */
 typedef enum glu_op { GLU_FORWARD = 0, GLU_BACKWARD_INPUT = 1 } glu_op;
 
-/* Bytes of workspace for glu_forward (n_in inputs, F hidden columns;
- * checkpoint != 0: it writes q_gate and q_up) and for glu_backward_input (n_in
- * is the down projection's n_out), with the operands of lin_workspace_size and
+/* Bytes of workspace for glu_forward (n_in inputs, F hidden columns; extra !=
+ * 0: it writes q_gate and q_up) and for glu_backward_input (n_in is the down
+ * projection's n_out; extra != 0: it forms dbias), with the operands of lin_workspace_size and
  * of lin_workspace_size_unaligned; and how that product runs.  A tile of the
  * forward product holds tile_cols / 2 hidden columns. */
-int glu_workspace_size(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int checkpoint, size_t *bytes);
-int glu_workspace_size_unaligned(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int checkpoint, size_t *bytes);
-int glu_product_plan(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int checkpoint, lin_plan *plan);
+int glu_workspace_size(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int extra, size_t *bytes);
+int glu_workspace_size_unaligned(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int extra, size_t *bytes);
+int glu_product_plan(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int extra, lin_plan *plan);
 
 /* The gated linear layer, both projections in one product:
  *   g = x Wg^T + bg,  u = x Wu^T + bu,  h = act(g) u
@@ -725,18 +725,21 @@ int glu_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t rows, int n_
  * [rows, ld_h] of dt or NULL: receives act(g) u again.  dz may equal z, and h
  * dh (with its row stride).  With dz, the layer's other gradients are those of
  * a linear layer with the weights W: lin_backward_input and
- * lin_backward_weight with 2 F outputs. */
+ * lin_backward_weight with 2 F outputs (its db sums the rounded dz). */
 int glu_backward_act(const void *dh, int64_t ld_dh, const void *z, int64_t ld_z, const q8_tensor *q_gate,
                      const q8_tensor *q_up, acsc_dtype dt, int64_t rows, int F, acsc_act act, void *dz, int64_t ld_dz, void *h,
                      int64_t ld_h, hipStream_t stream);
 
 /* The same with dh = dy W of the linear layer behind (W [n_out, F]), in the
  * epilogue of that product; dh is not written.  dz may equal z; dz and h
- * overlap neither dy nor W. */
+ * overlap neither dy nor W.
+ * dbias    device fp32 [2 F] or NULL: (+)= sum over rows of dz before its
+ *          rounding, the gradients of bg and bu (accumulate != 0 adds to what
+ *          it holds; a fixed order).  rows == 0 gives zero sums. */
 int glu_backward_input(const void *dy, int64_t ld_dy, acsc_dtype dt, int64_t rows, int F, int n_out, const void *W,
                        int64_t ld_w, acsc_act act, const void *z, int64_t ld_z, const q8_tensor *q_gate,
-                       const q8_tensor *q_up, void *dz, int64_t ld_dz, void *h, int64_t ld_h, void *ws, size_t ws_bytes,
-                       hipStream_t stream);
+                       const q8_tensor *q_up, void *dz, int64_t ld_dz, void *h, int64_t ld_h, float *dbias, int accumulate,
+                       void *ws, size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -213,7 +213,7 @@ def _load():
             ("glu_product_plan", [i32, i64, i32, i32, i32, i32, C.POINTER(_LinPlan)]),
             ("glu_forward", [vp, i64, i32, i64, i32, i32, vp, i64, vp, i32, vp, i64, vp, i64, qp, qp, vp, sz, vp]),
             ("glu_backward_act", [vp, i64, vp, i64, qp, qp, i32, i64, i32, i32, vp, i64, vp, i64, vp]),
-            ("glu_backward_input", [vp, i64, i32, i64, i32, i32, vp, i64, i32, vp, i64, qp, qp, vp, i64, vp, i64, vp, sz, vp])):
+            ("glu_backward_input", [vp, i64, i32, i64, i32, i32, vp, i64, i32, vp, i64, qp, qp, vp, i64, vp, i64, vp, i32, vp, sz, vp])):
         fn = getattr(lib, name)
         fn.restype = i32
         fn.argtypes = types
@@ -1335,41 +1335,41 @@ def join_backward(dout: Optional[torch.Tensor], dy: Optional[torch.Tensor], out:
     return JoinGrads(dr, db, dpost, dgate, dpre)
 
 
-def glu_workspace_size(op: int, rows: int, n_in: int, F: int, dtype: torch.dtype, checkpoint: bool = False) -> int:
-    """Bytes for glu_forward (GLU_FORWARD; checkpoint: keep="q8") or glu_backward_input (GLU_BACKWARD_INPUT, n_in its
-    n_out) with operands as in lin_workspace_size."""
+def glu_workspace_size(op: int, rows: int, n_in: int, F: int, dtype: torch.dtype, extra: bool = False) -> int:
+    """Bytes for glu_forward (GLU_FORWARD; extra: keep="q8") or glu_backward_input (GLU_BACKWARD_INPUT, n_in its n_out;
+    extra: with bias) with operands as in lin_workspace_size."""
     b = C.c_size_t(0)
-    _check(lib.glu_workspace_size(op, rows, n_in, F, BF16 if dtype == torch.bfloat16 else F32, int(checkpoint), C.byref(b)))
+    _check(lib.glu_workspace_size(op, rows, n_in, F, BF16 if dtype == torch.bfloat16 else F32, int(extra), C.byref(b)))
     return b.value
 
 
-def glu_workspace_size_unaligned(op: int, rows: int, n_in: int, F: int, dtype: torch.dtype, checkpoint: bool = False) -> int:
+def glu_workspace_size_unaligned(op: int, rows: int, n_in: int, F: int, dtype: torch.dtype, extra: bool = False) -> int:
     """The same for operands of any alignment and stride."""
     b = C.c_size_t(0)
-    _check(lib.glu_workspace_size_unaligned(op, rows, n_in, F, BF16 if dtype == torch.bfloat16 else F32, int(checkpoint),
+    _check(lib.glu_workspace_size_unaligned(op, rows, n_in, F, BF16 if dtype == torch.bfloat16 else F32, int(extra),
                                             C.byref(b)))
     return b.value
 
 
-def glu_product_plan(op: int, rows: int, n_in: int, F: int, dtype: torch.dtype, checkpoint: bool = False) -> LinPlan:
+def glu_product_plan(op: int, rows: int, n_in: int, F: int, dtype: torch.dtype, extra: bool = False) -> LinPlan:
     """How that product runs; a tile of the forward product holds tile_cols / 2 hidden columns."""
     p = _LinPlan()
-    _check(lib.glu_product_plan(op, rows, n_in, F, BF16 if dtype == torch.bfloat16 else F32, int(checkpoint), C.byref(p)))
+    _check(lib.glu_product_plan(op, rows, n_in, F, BF16 if dtype == torch.bfloat16 else F32, int(extra), C.byref(p)))
     return LinPlan(p.tile_rows, p.tile_cols, p.whole, p.cut, p.pieces)
 
 
 @functools.lru_cache(maxsize=1024)
-def _glu_bytes(aligned: bool, op: int, rows: int, n_in: int, F: int, dtype: torch.dtype, checkpoint: bool) -> int:
-    return (glu_workspace_size if aligned else glu_workspace_size_unaligned)(op, rows, n_in, F, dtype, checkpoint)
+def _glu_bytes(aligned: bool, op: int, rows: int, n_in: int, F: int, dtype: torch.dtype, extra: bool) -> int:
+    return (glu_workspace_size if aligned else glu_workspace_size_unaligned)(op, rows, n_in, F, dtype, extra)
 
 
-def _glu_ws(op: int, rows: int, n_in: int, F: int, checkpoint: bool, a, lda: int, b, ldb: int, ws: Optional[torch.Tensor]):
+def _glu_ws(op: int, rows: int, n_in: int, F: int, extra: bool, a, lda: int, b, ldb: int, ws: Optional[torch.Tensor]):
     if ws is not None:
         return _ws(0, ws, a.device)
     aligned = lda < 1 << 21 and ldb < 1 << 21
     if aligned and a.dtype is torch.bfloat16:
         aligned = not ((lda | a.data_ptr() >> 1 | ldb | b.data_ptr() >> 1) & 1)
-    return _ws(_glu_bytes(aligned, op, rows, n_in, F, a.dtype, checkpoint), None, a.device)
+    return _ws(_glu_bytes(aligned, op, rows, n_in, F, a.dtype, extra), None, a.device)
 
 
 def _even(n: int, name: str) -> int:
@@ -1447,16 +1447,19 @@ def glu_backward_act(dh: torch.Tensor, z, act: str = "silu", hidden: bool = Fals
     return dz, h
 
 
-def glu_backward_input(dy: torch.Tensor, W: torch.Tensor, z, act: str = "silu", hidden: bool = False,
-                       dz: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+def glu_backward_input(dy: torch.Tensor, W: torch.Tensor, z, act: str = "silu", hidden: bool = False, bias: bool = False,
+                       dz: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None,
+                       dbias: Optional[torch.Tensor] = None, accumulate: bool = False, ws: Optional[torch.Tensor] = None,
                        stream=None):
     """glu_backward_act with dh = dy W of the linear layer behind, dy [rows,
-    n_out], W [n_out, F], in that product's epilogue: (dz [rows, 2 F], h)."""
+    n_out], W [n_out, F], in that product's epilogue: (dz [rows, 2 F], h, dbias),
+    dbias the fp32 [2 F] sums of the unrounded dz if bias, else None; with
+    accumulate it is given and added to."""
     if stream is not None:
-        return _on(stream, glu_backward_input, dy, W, z, act, hidden, dz, h, ws)
+        return _on(stream, glu_backward_input, dy, W, z, act, hidden, bias, dz, h, dbias, accumulate, ws)
     rows, n_out = _two_d(dy, "dy")
     F = _two_d(W, "W")[1]
-    _here(dy, W, *_flat_kept(z), dz, h, ws)
+    _here(dy, W, *_flat_kept(z), dz, h, dbias, ws)
     dtype, dev = dy.dtype, dy.device
     lddy, ldw = _rows(dy, (rows, n_out), dtype, "dy"), _rows(W, (n_out, F), dtype, "W")
     pz, ldz, qg, qu = _kept_pair(z, rows, F, dtype)
@@ -1465,9 +1468,11 @@ def glu_backward_input(dy: torch.Tensor, W: torch.Tensor, z, act: str = "silu", 
     if hidden or h is not None:
         h, ldh = _new(h, (rows, F), dtype, dev, "h")
         ph = h.data_ptr()
-    wp, wn, hold = _glu_ws(GLU_BACKWARD_INPUT, rows, n_out, F, False, dy, lddy, W, ldw, ws)
+    dbias = _sums(dbias, bias, 2 * F, accumulate, dev, "dbias")
+    pdb = _optvec(dbias, 2 * F, torch.float32, "dbias")
+    wp, wn, hold = _glu_ws(GLU_BACKWARD_INPUT, rows, n_out, F, bias, dy, lddy, W, ldw, ws)
     rc = lib.glu_backward_input(dy.data_ptr(), lddy, _dt(dy), rows, F, n_out, W.data_ptr(), ldw, _act(act), pz, ldz, qg, qu,
-                                dz.data_ptr(), lddz, ph, ldh, wp, wn, _raw_stream())
+                                dz.data_ptr(), lddz, ph, ldh, pdb, int(accumulate), wp, wn, _raw_stream())
     if rc:
         _check(rc)
-    return dz, h
+    return dz, h, dbias

@@ -257,13 +257,13 @@ class _GluBlock(torch.autograd.Function):
             dr, db, dpost, dgate = d.dr, d.db, d.dpost, d.dgate
         dz = h = None
         if any(need[:6]):
-            dz, h = glu_backward_input(db, W2, z, ctx.act, hidden=need[4] or need[5])
+            dz, h, dbias = glu_backward_input(db, W2, z, ctx.act, hidden=need[4] or need[5], bias=need[3])
         if need[4] or need[5]:
             dW2, dbias2 = lin_backward_weight(db, h, bias=need[5])
         del h
-        if need[2] or need[3]:
+        if need[2]:
             y = rms_recompute(x, rstd, gamma, dtype=db.dtype)
-            dW, dbias = lin_backward_weight(dz, y, bias=need[3])
+            dW, _ = lin_backward_weight(dz, y, bias=False)
             del y
         if need[0] or need[1]:
             dx, dgamma = rms_backward(lin_backward_input(dz, W), x, rstd, gamma, add=dr, weights=need[1])

@@ -69,20 +69,76 @@ __global__ __launch_bounds__(256) void glu_join_few_kernel(Gemm g)
 template <typename TO, int TM, int T>
 __global__ __launch_bounds__(256) void glu_gate_join_kernel(Gemm g)
 {
-    constexpr int PER = TM * T / 2048;
+    constexpr int PER = TM * T / 2048, ROWS = 2048 / T;
+    __shared__ float meet[ROWS][2][T];
     const int64_t id = blockIdx.x / PER, count = static_cast<int64_t>(g.tm) * g.tn - g.whole;
     const int c = (blockIdx.x % PER) * 256 + threadIdx.x, row = c / (T / 8), col = c % (T / 8) * 8;
     int tile_m, tile_n;
     tile_at(g, g.whole + id, tile_m, tile_n);
     const int64_t m = static_cast<int64_t>(tile_m) * TM + row;
     const int n = tile_n * T + col, left = m < g.M ? g.N - n : 0;
-    if (left <= 0)
+    float sg[8] = {}, su[8] = {};
+    if (left > 0) {
+        float v[8];
+        add_pieces(g.part + (id * TM + row) * T + col, count * TM * T, g.splits, v);
+        GluBeside<TO> beside;
+        load_glu_beside<TO>(g.e, g.N, beside, m, n, left);
+        glu_gate_epilogue<TO>(g.e, g.N, v, beside, m, n, left, sg, su);
+    }
+    if (!g.e.sums)
         return;
-    float v[8];
-    add_pieces(g.part + (id * TM + row) * T + col, count * TM * T, g.splits, v);
-    GluBeside<TO> beside;
-    load_glu_beside<TO>(g.e, g.N, beside, m, n, left);
-    glu_gate_epilogue<TO>(g.e, g.N, v, beside, m, n, left);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        meet[row % ROWS][0][col + i] = sg[i];
+        meet[row % ROWS][1][col + i] = su[i];
+    }
+    __syncthreads();
+    float *out = g.e.sums + (static_cast<int64_t>(tile_m) * g.e.cut_slots + blockIdx.x % PER) * 2 * g.N;
+    for (int k = threadIdx.x; k < 2 * T; k += 256) {
+        float s = 0.f;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+            s += meet[r][k / T][k % T];
+        if (tile_n * T + k % T < g.N)
+            out[static_cast<int64_t>(k / T) * g.N + tile_n * T + k % T] = s;
+    }
+}
+
+// The column sums' partials, in order: 64 columns and 16 slices of the rows of
+// tiles a workgroup, the slices joined in order.
+constexpr int kSlices = 16;
+__global__ __launch_bounds__(64 * kSlices) void glu_sums_kernel(Gemm g, int tile, float *db, int accumulate)
+{
+    __shared__ float meet[kSlices][64];
+    const int lane = threadIdx.x & 63, sl = threadIdx.x >> 6, F = g.N;
+    const int col = blockIdx.x * 64 + lane, n = col % F;      // over 2 F
+    const int per = (g.tm + kSlices - 1) / kSlices, end = min(g.tm, (sl + 1) * per);
+    float s = 0.f;
+    if (col < 2 * F)
+        for (int m = sl * per; m < end; ++m) {
+            const int band = m / 4, height = min(g.tm - band * 4, 4);
+            const int64_t id = static_cast<int64_t>(band) * 4 * g.tn + static_cast<int64_t>(n / tile) * height + m % 4;
+            const int slots = id < g.whole ? 1 : g.e.cut_slots;
+            const float *p = g.e.sums + static_cast<int64_t>(m) * g.e.cut_slots * 2 * F + col;
+            for (int i = 0; i < slots; ++i)
+                s += p[static_cast<int64_t>(i) * 2 * F];
+        }
+    meet[sl][lane] = s;
+    __syncthreads();
+    if (sl || col >= 2 * F)
+        return;
+    s = meet[0][lane];
+#pragma unroll
+    for (int i = 1; i < kSlices; ++i)
+        s += meet[i][lane];
+    db[col] = accumulate ? db[col] + s : s;
+}
+
+__global__ __launch_bounds__(256) void glu_zero_kernel(float *y, int n)
+{
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < n)
+        y[i] = 0.f;
 }
 
 // The gate's gradient of a given dh: a wave takes 512 columns of a row, eight a
@@ -101,7 +157,8 @@ __global__ __launch_bounds__(256) void glu_act_kernel(const T *dh, int64_t lddh,
         load8(dh + row * lddh + col, left, v);
         GluBeside<T> beside;
         load_glu_beside<T>(e, F, beside, row, col, left);
-        glu_gate_epilogue<T>(e, F, v, beside, row, col, left);
+        float sg[8] = {}, su[8] = {};
+        glu_gate_epilogue<T>(e, F, v, beside, row, col, left, sg, su);
     }
 }
 
@@ -179,7 +236,17 @@ int plan_glu(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, bool codes
     return check_tiles(p);
 }
 
-int workspace_size(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int checkpoint, bool any, size_t *bytes)
+// Partials of a tile that is cut: one for each workgroup of its pieces' sum.
+inline int cut_slots(const Plan &p)
+{
+    return p.whole < static_cast<int64_t>(p.tm) * p.tn ? p.rows * p.tile / 2048 : 1;
+}
+inline size_t sums_bytes(const Plan &p, int F)
+{
+    return up256(static_cast<size_t>(p.tm) * cut_slots(p) * 2 * F * sizeof(float));
+}
+
+int workspace_size(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int extra, bool any, size_t *bytes)
 {
     clear_error();
     if (int rc = check_glu(rows, n_in, F, dt))
@@ -193,9 +260,9 @@ int workspace_size(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int 
     size_t most = 0;
     for (int copies = 0; copies < (any ? 4 : 1); ++copies) {
         Plan p;
-        if (int rc = plan_glu(op, rows, n_in, F, dt, op == GLU_FORWARD && checkpoint, copies, p))
+        if (int rc = plan_glu(op, rows, n_in, F, dt, op == GLU_FORWARD && extra, copies, p))
             return rc;
-        most = std::max(most, p.bytes());
+        most = std::max(most, p.bytes() + (op == GLU_BACKWARD_INPUT && extra ? sums_bytes(p, F) : 0));
     }
     *bytes = most;
     return ACSC_OK;
@@ -223,17 +290,17 @@ void glu_join_run(const Gemm &g, const Plan &p, EpiKind kind, acsc_dtype dt, hip
 
 using namespace acsc;
 
-extern "C" int glu_workspace_size(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int checkpoint, size_t *bytes)
+extern "C" int glu_workspace_size(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int extra, size_t *bytes)
 {
-    return workspace_size(op, rows, n_in, F, dt, checkpoint, false, bytes);
+    return workspace_size(op, rows, n_in, F, dt, extra, false, bytes);
 }
 
-extern "C" int glu_workspace_size_unaligned(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int checkpoint, size_t *bytes)
+extern "C" int glu_workspace_size_unaligned(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int extra, size_t *bytes)
 {
-    return workspace_size(op, rows, n_in, F, dt, checkpoint, true, bytes);
+    return workspace_size(op, rows, n_in, F, dt, extra, true, bytes);
 }
 
-extern "C" int glu_product_plan(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int checkpoint, lin_plan *plan)
+extern "C" int glu_product_plan(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int extra, lin_plan *plan)
 {
     clear_error();
     if (int rc = check_glu(rows, n_in, F, dt))
@@ -244,7 +311,7 @@ extern "C" int glu_product_plan(glu_op op, int64_t rows, int n_in, int F, acsc_d
     if (rows == 0)
         return ACSC_OK;
     Plan p;
-    if (int rc = plan_glu(op, rows, n_in, F, dt, op == GLU_FORWARD && checkpoint, 0, p))
+    if (int rc = plan_glu(op, rows, n_in, F, dt, op == GLU_FORWARD && extra, 0, p))
         return rc;
     *plan = {p.rows, p.tile, p.whole, static_cast<int64_t>(p.tm) * p.tn - p.whole, p.splits};
     return ACSC_OK;
@@ -288,7 +355,7 @@ extern "C" int glu_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t r
         return rc;
     if (int rc = check_ws(ws, ws_bytes, p.bytes()))
         return rc;
-    g.e = Epi{h, ld_h, bias, nullptr, 0, z, ld_z, q8_of(q_gate), act, 0, q8_of(q_up), nullptr, 0};
+    g.e = Epi{h, ld_h, bias, nullptr, 0, z, ld_z, q8_of(q_gate), act, 0, q8_of(q_up), nullptr, 0, nullptr, 0};
     return run_product(g, kGluForward, p, s, dt, dt, static_cast<char *>(ws), nullptr, nullptr, stream, "glu_forward");
 }
 
@@ -339,8 +406,8 @@ extern "C" int glu_backward_act(const void *dh, int64_t ld_dh, const void *z, in
 
 extern "C" int glu_backward_input(const void *dy, int64_t ld_dy, acsc_dtype dt, int64_t rows, int F, int n_out, const void *W,
                                   int64_t ld_w, acsc_act act, const void *z, int64_t ld_z, const q8_tensor *q_gate,
-                                  const q8_tensor *q_up, void *dz, int64_t ld_dz, void *h, int64_t ld_h, void *ws, size_t ws_bytes,
-                                  hipStream_t stream)
+                                  const q8_tensor *q_up, void *dz, int64_t ld_dz, void *h, int64_t ld_h, float *dbias, int accumulate,
+                                  void *ws, size_t ws_bytes, hipStream_t stream)
 {
     clear_error();
     if (int rc = check_glu(rows, n_out, F, dt))
@@ -362,8 +429,13 @@ extern "C" int glu_backward_input(const void *dy, int64_t ld_dy, acsc_dtype dt, 
     ACSC_CHECK_ARG(!some || (dz != dy && dz != W && dz != h), ACSC_EINVAL, "dz must not overlap dy, W or h");
     ACSC_CHECK_ARG(!some || !h || (h != dy && h != W && h != z), ACSC_EINVAL, "h must not overlap dy, W or z");
     ACSC_CHECK_ARG(!some || dz != z || ld_dz == ld_z, ACSC_EINVAL, "dz in place of z needs ld_dz == ld_z");
-    if (!some)
-        return ACSC_OK;
+    ACSC_CHECK_ARG(aligned(dbias, 4), ACSC_EALIGN, "dbias not 4-byte aligned");
+    if (!some) {
+        if (!dbias || accumulate)
+            return ACSC_OK;
+        ACSC_LAUNCH("glu_zero", glu_zero_kernel, dim3((2 * F + 255) / 256), dim3(256), 0, stream, dbias, 2 * F);
+        return check_launch("glu_zero");
+    }
     Gemm g{};
     g.A = {dy, ld_dy};
     g.B = {W, ld_w};
@@ -371,8 +443,15 @@ extern "C" int glu_backward_input(const void *dy, int64_t ld_dy, acsc_dtype dt, 
     const Plan p = plan_of(kGluGate, s, dt, readable(g.A, false, n_out, dt), readable(g.B, true, F, dt));
     if (int rc = check_tiles(p))
         return rc;
-    if (int rc = check_ws(ws, ws_bytes, p.bytes()))
+    const size_t sums = dbias ? sums_bytes(p, F) : 0;
+    if (int rc = check_ws(ws, ws_bytes, sums + p.bytes()))
         return rc;
-    g.e = Epi{dz, ld_dz, nullptr, nullptr, 0, const_cast<void *>(z), ld_z, q8_of(q_gate), act, 0, q8_of(q_up), h, ld_h};
-    return run_product(g, kGluGate, p, s, dt, dt, static_cast<char *>(ws), nullptr, nullptr, stream, "glu_backward_input");
+    g.e = Epi{dz, ld_dz, nullptr, nullptr, 0, const_cast<void *>(z), ld_z, q8_of(q_gate), act, 0, q8_of(q_up), h, ld_h,
+              dbias ? static_cast<float *>(ws) : nullptr, cut_slots(p)};
+    if (int rc = run_product(g, kGluGate, p, s, dt, dt, static_cast<char *>(ws) + sums, nullptr, nullptr, stream, "glu_backward_input"))
+        return rc;
+    if (!dbias)
+        return ACSC_OK;
+    ACSC_LAUNCH("glu_sums", glu_sums_kernel, dim3((2 * F + 63) / 64), dim3(64 * kSlices), 0, stream, g, p.tile, dbias, accumulate);
+    return check_launch("glu_sums");
 }

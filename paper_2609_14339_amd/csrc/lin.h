@@ -42,6 +42,11 @@ struct Epi {
     Q8 q_up;
     void *hidden;
     int64_t ldh;
+    // gate: column sums of both halves of y before their rounding, a partial of
+    // each tile's rows (of a cut tile `cut_slots` of them), [tm][cut_slots][2][F],
+    // or nullptr
+    float *sums;
+    int cut_slots;
 };
 
 struct Gemm {
@@ -280,7 +285,7 @@ __device__ __forceinline__ void glu_bias(const Epi &e, int F, int n, float (&bg)
 }
 
 // The gated product's gradient: eight columns of row m of dh = C through the
-// epilogue, from kept g and u.
+// epilogue, from kept g and u.  sg, su: what is added to their column sums.
 template <typename T>
 struct GluBeside {
     Beside<T> g, u;
@@ -303,7 +308,7 @@ __device__ __forceinline__ void load_glu_beside(const Epi &e, int F, GluBeside<T
 }
 template <typename T>
 __device__ __forceinline__ void glu_gate_epilogue(const Epi &e, int F, float (&v)[8], const GluBeside<T> &b, int64_t m, int n,
-                                                  int left)
+                                                  int left, float (&sg)[8], float (&su)[8])
 {
     float g[8], u[8], a[8], s[8];
 #pragma unroll
@@ -324,6 +329,12 @@ __device__ __forceinline__ void glu_gate_epilogue(const Epi &e, int F, float (&v
         s[i] *= v[i] * u[i];
         a[i] *= v[i];
     }
+    if (e.sums)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            sg[i] += i < left ? s[i] : 0.f;
+            su[i] += i < left ? a[i] : 0.f;
+        }
     T *y = static_cast<T *>(e.y) + m * e.ldy + n;
     store8(y, left, s);
     store8(y + F, left, a);
@@ -362,7 +373,8 @@ __device__ __forceinline__ void put_glu_rows(const Gemm &g, const char *lds, int
     }
 }
 template <typename T, int NA>
-__device__ __forceinline__ void put_glu_gate_rows(const Gemm &g, const char *lds, int64_t m0, int n0, int end)
+__device__ __forceinline__ void put_glu_gate_rows(const Gemm &g, const char *lds, int64_t m0, int n0, int end, float (&sg)[8],
+                                                  float (&su)[8])
 {
     const int lane = threadIdx.x & 63, n = n0 + (lane & 15) * 8, c = (lane & 15) * 2;
     const int cols = end - n;
@@ -379,16 +391,17 @@ __device__ __forceinline__ void put_glu_gate_rows(const Gemm &g, const char *lds
             const f32x4 hi = *reinterpret_cast<const f32x4 *>(lds + row * 512 + ((c + 1) ^ (row & 31)) * 16);
             float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
             const int64_t m = m0 + row;
-            glu_gate_epilogue<T>(g.e, g.N, v, beside[u], m, n, m < g.M ? cols : 0);
+            glu_gate_epilogue<T>(g.e, g.N, v, beside[u], m, n, m < g.M ? cols : 0, sg, su);
         }
     }
 }
 
 // The tile's columns stop at `end`.  `part`: the piece's rows and columns of
-// this wave, ld a row, or nullptr.  `tops`: see put_glu_rows.
+// this wave, ld a row, or nullptr.  `tops`: see put_glu_rows; sg, su:
+// see glu_gate_epilogue.
 template <typename T, int KIND, int NA>
 __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8], char *lds, int64_t m0, int n0,
-                                         int end, float *part, int ld, const uint32_t *tops)
+                                         int end, float *part, int ld, const uint32_t *tops, float (&sg)[8], float (&su)[8])
 {
     const int lane = threadIdx.x & 63;
     if (part) {
@@ -415,7 +428,7 @@ __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8
     if constexpr (KIND == kGluForward)
         put_glu_rows<T, NA>(g, lds, m0, n0, tops);
     else if constexpr (KIND == kGluGate)
-        put_glu_gate_rows<T, NA>(g, lds, m0, n0, end);
+        put_glu_gate_rows<T, NA>(g, lds, m0, n0, end, sg, su);
     else if (n0 + 128 <= end)
         put_rows<T, KIND, NA, true>(g, lds, m0, n0, end);
     else

@@ -497,11 +497,44 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
             tops = at;
         }
     }
+    float sg[8] = {}, su[8] = {};
 #pragma unroll
     for (int a = 0; a < FA; a += PUT)
         put_tile<TO, KIND, PUT>(g, reinterpret_cast<const f32x4(&)[PUT][8]>(acc[a]), own, m0 + (wm * FA + a) * 16,
                                n0 + wn * (GLU ? 64 : 128), min(g.N, n0 + TC), part ? part + a * 16 * T : nullptr, T,
-                               tops ? tops + a * 16 : nullptr);
+                               tops ? tops + a * 16 : nullptr, sg, su);
+    if constexpr (KIND == kGluGate) {
+        // the waves' column sums meet in LDS, in order: four lanes hold eight
+        // columns of every fourth row each
+        if (g.e.sums && !part) {
+            constexpr int WM = waves(TM, T) / WN, WC = FB * 16;
+            float *at = reinterpret_cast<float *>(smem);
+            __syncthreads();
+            const int lane = threadIdx.x & 63;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                sg[i] += __shfl_xor(sg[i], 16);
+                su[i] += __shfl_xor(su[i], 16);
+                sg[i] += __shfl_xor(sg[i], 32);
+                su[i] += __shfl_xor(su[i], 32);
+                if (lane * 8 < WC && lane < 16) {
+                    at[(wm * 2 + 0) * T + wn * 128 + lane * 8 + i] = sg[i];
+                    at[(wm * 2 + 1) * T + wn * 128 + lane * 8 + i] = su[i];
+                }
+            }
+            __syncthreads();
+            float *out = g.e.sums + static_cast<int64_t>(tile_m) * g.e.cut_slots * 2 * g.N;
+            for (int c = threadIdx.x; c < 2 * T; c += blockDim.x) {
+                float s = 0.f;
+#pragma unroll
+                for (int w = 0; w < WM; ++w)
+                    s += at[w * 2 * T + c];
+                const int half = c / T, n = n0 + c % T;
+                if (n < g.N)
+                    out[static_cast<int64_t>(half) * g.N + n] = s;
+            }
+        }
+    }
 }
 
 template <typename E, int TM, int T, bool ACOL, bool BCOL, int KIND, typename TO>

@@ -118,11 +118,12 @@ def test_glu(pk):
     assert act(dz=F) == EINVAL and act(dz=2 * F, lddz=80) == EINVAL and act(h=2 * F) == EINVAL and act(h=F, ldh=40) == EINVAL
     assert act(a=4) == EINVAL and act(dt=3) == EDTYPE and act(h=3 * F) == EINVAL
 
-    def inp(dy=F, W=2 * F, z=3 * F, qg=None, qu=None, dz=4 * F, lddz=64, h=None, dt=1, ws=F, ldw=32):
-        return pk.lib.glu_backward_input(dy, 64, dt, 4, 32, 64, W, ldw, 3, z, 64, qg, qu, dz, lddz, h, 32, ws, 1 << 30, None)
+    def inp(dy=F, W=2 * F, z=3 * F, qg=None, qu=None, dz=4 * F, lddz=64, h=None, dt=1, ws=F, ldw=32, db=None, n=1 << 30):
+        return pk.lib.glu_backward_input(dy, 64, dt, 4, 32, 64, W, ldw, 3, z, 64, qg, qu, dz, lddz, h, 32, db, 0, ws, n, None)
     assert inp(z=None) == EINVAL and inp(z=None, qu=q8(pk)) == EINVAL and inp(dy=None) == EINVAL and inp(W=None) == EINVAL
     assert inp(dz=F) == EINVAL and inp(dz=2 * F) == EINVAL and inp(h=4 * F) == EINVAL and inp(h=3 * F) == EINVAL
     assert inp(dz=3 * F, lddz=80) == EINVAL and inp(ldw=31) == EINVAL and inp(dt=5) == EDTYPE
+    assert inp(db=F + 1) == EALIGN and inp(db=F, n=0) == ENOSPC and inp(db=F, ws=None) == EINVAL
 
 
 def test_plans_and_workspaces(pk):

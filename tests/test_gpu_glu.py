@@ -108,10 +108,18 @@ def check_backward(pk, dtype, rows, n_out, F, act, kept_as, pad=0):
         within(dz, want, (tol + 4 * U * want.abs()) * (1 + 2.0 ** -8) + store(dtype, want))
         if h is not None:
             within(h, a * u, (ea * u.abs() + 2 * U * (a * u).abs()) * (1 + 2.0 ** -8) + store(dtype, a * u))
-    dz, h = pk.glu_backward_input(dy, W, kept, act, hidden=True)
+    dz, h, db = pk.glu_backward_input(dy, W, kept, act, hidden=True, bias=True)
     against(dz, h, dh, eh)
-    dz2, none = pk.glu_backward_input(dy, W, kept, act)
-    assert none is None and torch.equal(dz2, dz)
+    dz2, none, nodb = pk.glu_backward_input(dy, W, kept, act)
+    assert none is nodb is None and torch.equal(dz2, dz)
+    # sums of what dz is before its rounding, in some order
+    want = torch.cat((dh * u * slope, dh * a), 1)
+    size = torch.cat((u.abs() * (eh * slope.abs() + (dh.abs() + eh) * es), eh * a.abs() + (dh.abs() + eh) * ea), 1)
+    within(db, want.sum(0), (size + U * (rows + 8) * want.abs()).sum(0))
+    base = randn(2 * F, dtype=F32, seed=s + 3)
+    more = base.clone()
+    pk.glu_backward_input(dy, W, kept, act, bias=True, dbias=more, accumulate=True)
+    assert torch.equal(more, base + db)
     # of a given dh
     given = dh.to(dtype)
     dz3, h3 = pk.glu_backward_act(given, kept, act, hidden=True)
@@ -163,8 +171,8 @@ def test_no_rows_and_columns_behind_the_last(pk):
     e = torch.empty(0, 64, dtype=BF16, device="cuda")
     h, z = pk.glu_forward(e, W, None, keep="z")
     assert h.shape == (0, 96) and z.shape == (0, 192)
-    dz, h = pk.glu_backward_input(e, randn(64, 96, dtype=BF16, seed=3), z, hidden=True)
-    assert dz.shape == (0, 192) and h.shape == (0, 96)
+    dz, h, db = pk.glu_backward_input(e, randn(64, 96, dtype=BF16, seed=3), z, hidden=True, bias=True)
+    assert dz.shape == (0, 192) and h.shape == (0, 96) and (db == 0).all()
     for rows in (4, 150):
         x = randn(rows, 64, dtype=BF16, seed=4)
         wide = torch.full((rows + 1, 101), 9.0, dtype=BF16, device="cuda")
@@ -182,8 +190,7 @@ def test_streams_and_graphs(pk, rows):
 
     def both(s=None):
         h, kept = pk.glu_forward(x, W, b, keep="q8", stream=s)
-        dz, again = pk.glu_backward_input(dy, W2, kept, hidden=True, stream=s)
-        return [h, *kept[0], *kept[1], dz, again]
+        return [h, *kept[0], *kept[1], *pk.glu_backward_input(dy, W2, kept, hidden=True, bias=True, stream=s)]
     want = both()
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
