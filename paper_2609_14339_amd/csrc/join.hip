@@ -18,6 +18,7 @@ namespace acsc {
 namespace {
 
 constexpr int kMaxH = 32768;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 template <typename T>
 struct Fwd {
@@ -208,8 +209,10 @@ struct Src {
 //   dpre = sum of dy h2,   s = sum of u h1, dgate = s post, dpost = s gate
 // A workgroup walks rows blockIdx.x, + gridDim.x, ... (four at a time where a
 // wave holds a row) and keeps both column sums in registers; its waves' sums
-// meet in LDS in wave order, and every workgroup leaves one partial.
-template <typename T, int NT, int CH, bool JOIN, bool KEPT>
+// meet in LDS in wave order, and every workgroup leaves one partial.  AHEAD:
+// the next row's loads leave before a row is worked on, and the gains stay in
+// registers.
+template <typename T, int NT, int CH, bool JOIN, bool KEPT, bool AHEAD>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_backward_kernel(Bwd<T> p)
 {
     constexpr int RPB = NT < 256 ? 256 / NT : 1;
@@ -217,54 +220,96 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
     __shared__ float meet[RPB > 1 ? 2 * NT * CH * 8 : 1];
     const int t = threadIdx.x % NT;
     const int sub = RPB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
+    const bool branch = JOIN && (p.post || p.gate);     // whether the formula reads b
     float s2[CH][8], s1[CH][8];
+    Raw8<T> pre[CH], post[CH], gate[CH];
+    const auto load_gains = [&]() {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * NT + t) * 8, left = p.H - col;
+            if (p.pre)
+                load_raw(p.pre + col, left, pre[c]);
+            if (JOIN && p.post)
+                load_raw(p.post + col, left, post[c]);
+            if (JOIN && p.gate)
+                load_raw(p.gate + col, left, gate[c]);
+        }
+    };
+    if (AHEAD)
+        load_gains();
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             s2[c][i] = s1[c][i] = 0.f;
-    int flip = 0;
-    const int64_t stride = static_cast<int64_t>(gridDim.x) * RPB, first = static_cast<int64_t>(blockIdx.x) * RPB + sub;
-    for (int64_t row = first; row < p.rows; row += stride, flip ^= 1) {
-        float v[CH][8];
-        Src<T, KEPT> b[CH];
+    // a row as it is stored
+    struct Row {
+        Raw8<T> dout[CH], dy[CH];
+        Src<T, KEPT> x[CH], b[CH];
+        float pre, post;
+    };
+    const auto load = [&](Row &r, int64_t row) {
+        r.pre = p.dy ? p.rstd_pre[row] : 0.f;
+        r.post = JOIN && p.post ? p.rstd_post[row] : 1.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * NT + t) * 8, left = p.H - col;
-            load8(p.dout ? p.dout + row * p.lddo + col : nullptr, p.dout ? left : 0, v[c]);
-            if (JOIN && (p.post || p.gate))
-                b[c].load(p.b, p.ldb, p.q_b, row, col, left);
+            if (p.dy) {
+                r.x[c].load(p.out, p.ldo, p.q_out, row, col, left);
+                load_raw(p.dy + row * p.lddy + col, left, r.dy[c]);
+            }
+            load_raw(p.dout + row * p.lddo + col, p.dout ? left : 0, r.dout[c]);
+            if (branch)
+                r.b[c].load(p.b, p.ldb, p.q_b, row, col, left);
         }
+    };
+    int flip = 0;
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * RPB, first = static_cast<int64_t>(blockIdx.x) * RPB + sub;
+    Row cur, next;
+    if (AHEAD && first < p.rows)
+        load(next, first);
+    for (int64_t row = first; row < p.rows; row += stride, flip ^= 1) {
+        if (AHEAD) {
+            cur = next;
+            if (row + stride < p.rows)
+                load(next, row + stride);
+        } else {
+            load(cur, row);
+            load_gains();
+        }
+        float v[CH][8];
         if (p.dy) {
-            Src<T, KEPT> x[CH];
-            Raw8<T> dy[CH], w[CH];
-            const float rs = p.rstd_pre[row];
+            const float rs = cur.pre;
             float s[1] = {0.f};
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const int col = (c * NT + t) * 8, left = p.H - col;
-                x[c].load(p.out, p.ldo, p.q_out, row, col, left);
-                load_raw(p.dy + row * p.lddy + col, left, dy[c]);
-                if (p.pre)
-                    load_raw(p.pre + col, left, w[c]);
-            }
-#pragma unroll
-            for (int c = 0; c < CH; ++c)
+                again(pre[c].w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float h = x[c].at(i) * rs, d = dy[c].at(i), g = p.pre ? d * w[c].at(i) : d;
+                    const float h = cur.x[c].at(i) * rs, d = cur.dy[c].at(i), g = p.pre ? d * pre[c].at(i) : d;
                     s2[c][i] += d * h;       // past the end of the row dy = 0
                     s[0] += g * h;
                 }
+            }
             row_sum<NT>(s, slots[flip][0]);
             const float m = s[0] / p.H;
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
+            for (int c = 0; c < CH; ++c) {
+                again(cur.x[c].x.w);
+                again(cur.dy[c].w);
+                again(pre[c].w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float h = x[c].at(i) * rs, d = dy[c].at(i), g = p.pre ? d * w[c].at(i) : d;
-                    v[c][i] += rs * (g - h * m);
+                    const float h = cur.x[c].at(i) * rs, d = cur.dy[c].at(i), g = p.pre ? d * pre[c].at(i) : d;
+                    v[c][i] = cur.dout[c].at(i) + rs * (g - h * m);
                 }
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    v[c][i] = cur.dout[c].at(i);
         }
         if (p.dr)
 #pragma unroll
@@ -285,29 +330,23 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
             for (int c = 0; c < CH; ++c)
                 drop8(p.drop, d, (c * NT + t) * 8, v[c]);
         }
-        const float rs = p.post ? p.rstd_post[row] : 1.f;
+        const float rs = cur.post;
         float s[1] = {0.f};
-        if (p.post || p.gate)
+        if (branch)
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const int col = (c * NT + t) * 8, left = p.H - col;
-                float w[8];
+                const int left = p.H - (c * NT + t) * 8;
+                again(post[c].w);
+                again(gate[c].w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    s1[c][i] += left > i ? v[c][i] * (b[c].at(i) * rs) : 0.f;
-                if (p.gate) {
-                    load8(p.gate + col, left, w);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        v[c][i] *= w[i];
-                }
-                if (p.post) {
-                    load8(p.post + col, left, w);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        v[c][i] *= w[i];     // zeros past the end of the row
-                        s[0] += v[c][i] * (b[c].at(i) * rs);
-                    }
+                for (int i = 0; i < 8; ++i) {
+                    const float h = cur.b[c].at(i) * rs;
+                    s1[c][i] += left > i ? v[c][i] * h : 0.f;
+                    if (p.gate)
+                        v[c][i] *= gate[c].at(i);
+                    if (p.post)
+                        v[c][i] *= post[c].at(i);     // zeros past the end of the row
+                    s[0] += v[c][i] * h;
                 }
             }
         float m = 0.f;
@@ -318,12 +357,13 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * NT + t) * 8, left = p.H - col;
+            again(cur.b[c].x.w);
             if (left <= 0)
                 continue;
             if (p.post)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    v[c][i] = rs * (v[c][i] - b[c].at(i) * rs * m);
+                    v[c][i] = rs * (v[c][i] - cur.b[c].at(i) * rs * m);
             store8(p.db + row * p.lddb + col, left, v[c]);
         }
     }
@@ -363,6 +403,169 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
             store8(part + p.H + col, left, s1[c]);
         }
     }
+}
+
+// Rows past 8192 columns, which with their sums leave no registers: a workgroup
+// reads a row once for each of its means and once, from the caches, for the
+// results, and adds to its column sums in LDS, or past 16384 columns (LDS_SUMS
+// false) in its partial itself; each thread owns its columns.
+template <typename T, bool JOIN, bool KEPT, bool LDS_SUMS>
+__global__ __launch_bounds__(1024, 4) void join_backward_wide_kernel(Bwd<T> p)
+{
+    extern __shared__ __align__(16) float held[];
+    __shared__ float slots[2][2][16];
+    float *part = p.part ? p.part + static_cast<int64_t>(blockIdx.x) * 2 * p.H : nullptr;
+    const int padded = (p.H + 7) / 8 * 8;
+    const bool branch = JOIN && (p.post || p.gate);
+    // eight columns of sum `which`, added to (first: begun)
+    const auto add = [&](int which, int col, int left, bool first, const float (&v)[8]) {
+        if (!part)
+            return;
+        float old[8] = {};
+        if constexpr (LDS_SUMS) {
+            f32x4 *at = reinterpret_cast<f32x4 *>(held + which * padded + col);
+            f32x4 lo = {v[0], v[1], v[2], v[3]}, hi = {v[4], v[5], v[6], v[7]};
+            at[0] = first ? lo : at[0] + lo;
+            at[1] = first ? hi : at[1] + hi;
+        } else {
+            if (!first)
+                load8(part + which * p.H + col, left, old);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                old[i] += v[i];
+            store8(part + which * p.H + col, left, old);
+        }
+    };
+    int flip = 0;
+    bool first = true;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, flip ^= 1, first = false) {
+        const float r2 = p.dy ? p.rstd_pre[row] : 0.f, r1 = JOIN && p.post ? p.rstd_post[row] : 1.f;
+        const DropRow d = drop_row(p.drop, row);
+        // eight columns of h2 and dy
+        const auto after = [&](int col, int left, float (&h)[8], float (&dy)[8]) {
+            Src<T, KEPT> x;
+            x.load(p.out, p.ldo, p.q_out, row, col, left);
+            load8(p.dy + row * p.lddy + col, left, dy);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                h[i] = x.at(i) * r2;
+        };
+        const auto times = [&](const T *w, int col, int left, float (&v)[8]) {
+            float g[8];
+            if (!w)
+                return;
+            load8(w + col, left, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                v[i] *= g[i];
+        };
+        float m2 = 0.f, m1 = 0.f;
+        if (p.dy) {
+            float s[1] = {0.f};
+#pragma unroll 1
+            for (int col = threadIdx.x * 8; col < p.H; col += 8192) {
+                const int left = p.H - col;
+                float h[8], g[8];
+                after(col, left, h, g);
+                times(p.pre, col, left, g);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    s[0] += g[i] * h[i];     // past the end of the row g = 0
+            }
+            row_sum<1024>(s, slots[flip][0]);
+            m2 = s[0] / p.H;
+        }
+        // eight columns of t (and, for the column sums, dy h2)
+        const auto whole = [&](int col, int left, bool sums, float (&v)[8]) {
+            load8(p.dout + row * p.lddo + col, p.dout ? left : 0, v);
+            if (!p.dy)
+                return;
+            float h[8], g[8];
+            after(col, left, h, g);
+            if (sums) {
+                float o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    o[i] = g[i] * h[i];
+                add(0, col, left, first, o);
+            }
+            times(p.pre, col, left, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                v[i] += r2 * (g[i] - h[i] * m2);
+        };
+        // eight columns of e and h1 from t (and, for the column sums, u h1)
+        const auto before = [&](int col, int left, bool sums, float (&v)[8], float (&h)[8]) {
+            Src<T, KEPT> b;
+            b.load(p.b, p.ldb, p.q_b, row, col, left);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                h[i] = b.at(i) * r1;
+            if (sums) {
+                float o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    o[i] = i < left ? v[i] * h[i] : 0.f;
+                add(1, col, left, first, o);
+            }
+            times(p.gate, col, left, v);
+            times(p.post, col, left, v);
+        };
+        if (JOIN && p.post) {
+            float s[1] = {0.f};
+#pragma unroll 1
+            for (int col = threadIdx.x * 8; col < p.H; col += 8192) {
+                const int left = p.H - col;
+                float v[8], h[8];
+                whole(col, left, false, v);
+                if (p.drop.below)
+                    drop8(p.drop, d, col, v);
+                before(col, left, false, v, h);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    s[0] += v[i] * h[i];     // zeros past the end of the row
+            }
+            row_sum<1024>(s, slots[flip][1]);
+            m1 = s[0] / p.H;
+        }
+#pragma unroll 1
+        for (int col = threadIdx.x * 8; col < p.H; col += 8192) {
+            const int left = p.H - col;
+            float v[8], o[8], h[8];
+            whole(col, left, true, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                o[i] = JOIN ? p.scale * v[i] : v[i];
+            if (JOIN) {
+                if (p.drop.below)
+                    drop8(p.drop, d, col, v);
+                if (branch)
+                    before(col, left, true, v, h);
+                if (p.post)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        v[i] = r1 * (v[i] - h[i] * m1);
+            }
+            // after everything that is read of these columns: dr and db may take its place
+            if (p.dr)
+                store8(p.dr + row * p.lddr + col, left, o);
+            if (JOIN)
+                store8(p.db + row * p.lddb + col, left, v);
+        }
+    }
+    if (!part || (!LDS_SUMS && !first))
+        return;
+    for (int col = threadIdx.x * 8; col < p.H; col += 8192)
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            // nothing was added where there are no rows, or no such sum
+            const bool some = !first && (which ? branch : p.dy != nullptr);
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                v[i] = LDS_SUMS && some ? held[which * padded + col + i] : 0.f;
+            store8(part + which * p.H + col, p.H - col, v);
+        }
 }
 
 // Column sums over the partials, and what the gradients of the gains are of
@@ -435,7 +638,7 @@ inline Shape forward_shape(int H, bool f32)
         return {1024, 2};
     return {1024, 4};
 }
-inline Shape backward_shape(int H)
+inline Shape backward_shape(int H, bool f32)
 {
     if (H <= 512)
         return {64, 1};
@@ -444,19 +647,17 @@ inline Shape backward_shape(int H)
     if (H <= 2048)
         return {256, 1};
     if (H <= 4096)
-        return {256, 2};
+        return f32 ? Shape{512, 1} : Shape{256, 2};
     if (H <= 8192)
-        return {512, 2};
-    if (H <= 16384)
-        return {512, 4};
-    return {512, 8};
+        return f32 ? Shape{1024, 1} : Shape{512, 2};
+    return {0, 0};   // the kernel for wide rows
 }
 
 // Workgroups of the backward pass, which is also its number of partials.
 inline int bwd_groups(int64_t rows, int H)
 {
-    const int rpb = backward_shape(H).nt == 64 ? 4 : 1;
-    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((rows + rpb - 1) / rpb, 512)));
+    const int rpb = H <= 1024 ? 4 : 1;
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((rows + rpb - 1) / rpb, H <= 8192 ? 512 : 256)));
 }
 
 inline int check_common(int64_t rows, int H, int dt)
@@ -535,19 +736,32 @@ int run_forward(const Fwd<T> &p, hipStream_t st, const char *tag)
 template <typename T, bool JOIN, bool KEPT>
 int run_backward(const Bwd<T> &p, int groups, hipStream_t st, const char *tag)
 {
-    const Shape s = backward_shape(p.H);
+    const Shape s = backward_shape(p.H, sizeof(T) == 4);
     const dim3 grid(groups);
-#define ACSC_CASE(NT, CH)           \
+#define ACSC_CASE(NT, CH, AHEAD)    \
     if (s.nt == NT && s.ch == CH) \
-        ACSC_LAUNCH(tag, (join_backward_kernel<T, NT, CH, JOIN, KEPT>), grid, dim3(NT < 256 ? 256 : NT), 0, st, p);
-    ACSC_CASE(64, 1)
-    ACSC_CASE(64, 2)
-    ACSC_CASE(256, 1)
-    ACSC_CASE(256, 2)
-    ACSC_CASE(512, 2)
-    ACSC_CASE(512, 4)
-    ACSC_CASE(512, 8)
+        ACSC_LAUNCH(tag, (join_backward_kernel<T, NT, CH, JOIN, KEPT, AHEAD>), grid, dim3(NT < 256 ? 256 : NT), 0, st, p);
+    ACSC_CASE(64, 1, true)
+    ACSC_CASE(64, 2, true)
+    ACSC_CASE(256, 1, true)
+    if constexpr (sizeof(T) == 4) {
+        ACSC_CASE(512, 1, true)
+        ACSC_CASE(1024, 1, false)
+    } else {
+        ACSC_CASE(256, 2, true)
+        ACSC_CASE(512, 2, true)
+    }
 #undef ACSC_CASE
+    if (!s.nt) {
+        if (p.H <= 16384) {
+            const size_t lds = static_cast<size_t>((p.H + 7) / 8 * 8) * 2 * sizeof(float);
+            if (int rc = allow_lds(join_backward_wide_kernel<T, JOIN, KEPT, true>, lds))
+                return rc;
+            ACSC_LAUNCH(tag, (join_backward_wide_kernel<T, JOIN, KEPT, true>), grid, dim3(1024), lds, st, p);
+        } else {
+            ACSC_LAUNCH(tag, (join_backward_wide_kernel<T, JOIN, KEPT, false>), grid, dim3(1024), 0, st, p);
+        }
+    }
     return check_launch(tag);
 }
 
