@@ -41,7 +41,7 @@ __global__ __launch_bounds__(256) void glu_join_kernel(Gemm g)
         vg[i] += bg[i];
         vu[i] += bu[i];
     }
-    glu_epilogue<TO>(g.e, g.N, vg, vu, max16(mag8(vg, left)), max16(mag8(vu, left)), m, n, left);
+    glu_epilogue<TO>(g.e, g.N, vg, vu, m, n, left);
 }
 
 // Pieces of a product for few tokens: 2048 columns of a row a workgroup.
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(256) void glu_join_few_kernel(Gemm g)
         vg[i] += bg[i];
         vu[i] += bu[i];
     }
-    glu_epilogue<TO>(g.e, g.N, vg, vu, max16(mag8(vg, left)), max16(mag8(vu, left)), m, n, left);
+    glu_epilogue<TO>(g.e, g.N, vg, vu, m, n, left);
 }
 
 // Pieces of dh, then the gate's gradient.

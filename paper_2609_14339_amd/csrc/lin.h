@@ -238,35 +238,6 @@ __device__ __forceinline__ void act_both(const float (&g)[8], int act, float (&a
     apply_slope<T>(s, g, act);
 }
 
-// The gated product forward: eight columns n .. n + 7 of row m of g and u
-// through the epilogue; `left` of them exist.  ag, au: the largest magnitudes
-// of their groups of 128 columns (with codes only).
-template <typename T>
-__device__ __forceinline__ void glu_epilogue(const Epi &e, int F, float (&g)[8], float (&u)[8], uint32_t ag, uint32_t au,
-                                             int64_t m, int n, int left)
-{
-    if (e.z) {
-        T *z = static_cast<T *>(e.z) + m * e.ldz + n;
-        store8(z, left, g);
-        store8(z + F, left, u);
-    }
-    if (e.q.codes) {
-        const auto code = [&](const Q8 &q, uint32_t a, const float (&v)[8]) {
-            float scale, inv;
-            group_scale(a, scale, inv);
-            store_codes(q.codes + m * q.ldc + n, left, inv, v);
-            if (left > 0 && n % kGroup == 0)
-                q.scales[m * q.lds + n / kGroup] = scale;
-        };
-        code(e.q, ag, g);
-        code(e.q_up, au, u);
-    }
-    apply_act<T>(g, e.act);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        g[i] *= u[i];
-    store8(static_cast<T *>(e.y) + m * e.ldy + n, left, g);
-}
 // The largest magnitude of the first `left` of eight values.
 __device__ __forceinline__ uint32_t mag8(const float (&v)[8], int left)
 {
@@ -275,6 +246,44 @@ __device__ __forceinline__ uint32_t mag8(const float (&v)[8], int left)
     for (int i = 0; i < 8; ++i)
         a = max(a, i < left ? mag(v[i]) : 0u);
     return a;
+}
+// What the other half of sixteen lanes holds (row_ror 8).
+__device__ __forceinline__ float other8(float x)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xF, 0xF, false));
+}
+
+// The gated product forward: eight columns n .. n + 7 of row m of g and u
+// through the epilogue; `left` of them exist.  With a checkpoint sixteen lanes
+// of the wave, aligned, hold a group of 128 columns of both; half of them forms
+// the gate's scale, the other the up projection's.
+template <typename T, bool CODES = true>
+__device__ __forceinline__ void glu_epilogue(const Epi &e, int F, float (&g)[8], float (&u)[8], int64_t m, int n, int left)
+{
+    if (e.z) {
+        T *z = static_cast<T *>(e.z) + m * e.ldz + n;
+        store8(z, left, g);
+        store8(z + F, left, u);
+    }
+    if (CODES && e.q.codes) {
+        const bool low = (threadIdx.x & 8) == 0;
+        const uint32_t ag = max16(mag8(g, left)), au = max16(mag8(u, left));
+        float scale, inv;
+        group_scale(low ? ag : au, scale, inv);
+        const float inv2 = other8(inv);
+        store_codes(e.q.codes + m * e.q.ldc + n, left, low ? inv : inv2, g);
+        store_codes(e.q_up.codes + m * e.q_up.ldc + n, left, low ? inv2 : inv, u);
+        const float scale2 = other8(scale);
+        if (left > 0 && n % kGroup == 0) {
+            e.q.scales[m * e.q.lds + n / kGroup] = scale;
+            e.q_up.scales[m * e.q_up.lds + n / kGroup] = scale2;
+        }
+    }
+    apply_act<T>(g, e.act);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        g[i] *= u[i];
+    store8(static_cast<T *>(e.y) + m * e.ldy + n, left, g);
 }
 template <typename T>
 __device__ __forceinline__ void glu_bias(const Epi &e, int F, int n, float (&bg)[8], float (&bu)[8])
@@ -341,19 +350,24 @@ __device__ __forceinline__ void glu_gate_epilogue(const Epi &e, int F, float (&v
 }
 
 // A wave's accumulators of 16 NA rows by 64 hidden columns through the gated
-// epilogue: fragments 0 .. 3 of a row hold g, 4 .. 7 u.  Eight lanes take a
-// row, eight rows a step.  tops: the rows' largest magnitudes [wn][g, u][row]
-// with codes, of both waves that hold a group.
-template <typename T, int NA>
-__device__ __forceinline__ void put_glu_rows(const Gemm &g, const char *lds, int64_t m0, int n0, const uint32_t *tops)
+// epilogue: fragments 0 .. 3 of a row hold g, 4 .. 7 u.  Alone, eight lanes take
+// a row, eight rows a step (no checkpoint then).  PAIR: two waves hold the 128
+// columns of a group, in neighbouring parts of LDS, and each takes half of the
+// rows whole, sixteen lanes a row.
+template <typename T, int NA, bool PAIR>
+__device__ __forceinline__ void put_glu_rows(const Gemm &g, const char *lds, int64_t m0, int n0, int wn)
 {
-    const int lane = threadIdx.x & 63, n = n0 + (lane & 7) * 8, c = (lane & 7) * 2;
-    const int cols = g.N - n;
+    constexpr int L = PAIR ? 16 : 8, STEP = 64 / L, ROWS = PAIR ? NA * 8 : NA * 16;
+    const int lane = threadIdx.x & 63, at = lane % L;
+    const int n = n0 - (PAIR ? wn * 64 : 0) + at * 8, c = (at & 7) * 2, cols = g.N - n;
+    const int first = PAIR ? wn * ROWS : 0;
+    if (PAIR)
+        lds += (at / 8 - wn) * NA * 8192;
     float bg[8], bu[8];
     glu_bias<T>(g.e, g.N, n, bg, bu);
 #pragma unroll 1
-    for (int r0 = 0; r0 < NA * 16; r0 += 8) {
-        const int row = r0 + (lane >> 3);
+    for (int r0 = 0; r0 < ROWS; r0 += STEP) {
+        const int row = first + r0 + lane / L;
         const auto chunk = [&](int k) { return *reinterpret_cast<const f32x4 *>(lds + row * 512 + (k ^ (row & 31)) * 16); };
         const f32x4 g0 = chunk(c), g1 = chunk(c + 1), u0 = chunk(16 + c), u1 = chunk(17 + c);
         float vg[8] = {g0[0], g0[1], g0[2], g0[3], g1[0], g1[1], g1[2], g1[3]};
@@ -363,13 +377,8 @@ __device__ __forceinline__ void put_glu_rows(const Gemm &g, const char *lds, int
             vg[i] += bg[i];
             vu[i] += bu[i];
         }
-        uint32_t ag = 0, au = 0;
-        if (g.e.q.codes) {
-            ag = max(tops[row], tops[128 + row]);
-            au = max(tops[64 + row], tops[192 + row]);
-        }
         const int64_t m = m0 + row;
-        glu_epilogue<T>(g.e, g.N, vg, vu, ag, au, m, n, m < g.M ? cols : 0);
+        glu_epilogue<T, PAIR>(g.e, g.N, vg, vu, m, n, m < g.M ? cols : 0);
     }
 }
 template <typename T, int NA>
@@ -396,12 +405,21 @@ __device__ __forceinline__ void put_glu_gate_rows(const Gemm &g, const char *lds
     }
 }
 
+// The workgroup's waves meet with their LDS accesses done; what they still have
+// to store goes on (a barrier with a fence waits for it).
+__device__ __forceinline__ void lds_meet()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // The tile's columns stop at `end`.  `part`: the piece's rows and columns of
-// this wave, ld a row, or nullptr.  `tops`: see put_glu_rows; sg, su:
-// see glu_gate_epilogue.
-template <typename T, int KIND, int NA>
+// this wave, ld a row, or nullptr.  wn: the wave's place along
+// the columns; sg, su: see glu_gate_epilogue.
+template <typename T, int KIND, int NA, int WN>
 __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8], char *lds, int64_t m0, int n0,
-                                         int end, float *part, int ld, const uint32_t *tops, float (&sg)[8], float (&su)[8])
+                                         int end, float *part, int ld, int wn, float (&sg)[8], float (&su)[8])
 {
     const int lane = threadIdx.x & 63;
     if (part) {
@@ -421,12 +439,19 @@ __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8
             const int row = a * 16 + (lane & 15), chunk = (j * 4 + (lane >> 4)) ^ (row & 31);
             *reinterpret_cast<f32x4 *>(lds + row * 512 + chunk * 16) = acc[a][j];
         }
+    if constexpr (KIND == kGluForward && WN == 2)
+        if (g.e.q.codes) {
+            lds_meet();
+            put_glu_rows<T, NA, true>(g, lds, m0, n0, wn);
+            lds_meet();   // before the parts are written again
+            return;
+        }
     // the wave reads what its own lanes wrote: LDS keeps a wave's order
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     if constexpr (KIND == kGluForward)
-        put_glu_rows<T, NA>(g, lds, m0, n0, tops);
+        put_glu_rows<T, NA, false>(g, lds, m0, n0, wn);
     else if constexpr (KIND == kGluGate)
         put_glu_gate_rows<T, NA>(g, lds, m0, n0, end, sg, su);
     else if (n0 + 128 <= end)

@@ -462,47 +462,12 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
         part += wm * FA * 16 * T + wn * 128;
     constexpr int PUT = FA < 2 ? FA : 2;        // fragments' rows at a time
     char *own = reinterpret_cast<char *>(smem) + wave * PUT * 8192;
-    const uint32_t *tops = nullptr;
-    if constexpr (GLU && T == 256) {
-        // a group of 128 columns lies in two waves: the largest magnitudes of a
-        // row of each meet in LDS behind the waves' own parts
-        if (g.e.q.codes && !part) {
-            uint32_t *at = reinterpret_cast<uint32_t *>(smem + waves(TM, T) * PUT * 8192) + wm * 256;
-            const int lane = threadIdx.x & 63, n = n0 + wn * 64 + (lane >> 4) * 4;
-            const TO *bias = static_cast<const TO *>(g.e.bias);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t top[FA] = {};
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int col = n + j * 16 + i;
-                        if (col >= g.N)
-                            continue;
-                        const float b = bias ? to_float(bias[col + (h ? g.N : 0)]) : 0.f;
-#pragma unroll
-                        for (int a = 0; a < FA; ++a)
-                            top[a] = max(top[a], mag(acc[a][h * 4 + j][i] + b));
-                    }
-#pragma unroll
-                for (int a = 0; a < FA; ++a) {
-                    top[a] = max(top[a], static_cast<uint32_t>(__shfl_xor(static_cast<int>(top[a]), 16)));
-                    top[a] = max(top[a], static_cast<uint32_t>(__shfl_xor(static_cast<int>(top[a]), 32)));
-                    if (lane < 16)
-                        at[wn * 128 + h * 64 + a * 16 + lane] = top[a];
-                }
-            }
-            __syncthreads();
-            tops = at;
-        }
-    }
     float sg[8] = {}, su[8] = {};
 #pragma unroll
     for (int a = 0; a < FA; a += PUT)
-        put_tile<TO, KIND, PUT>(g, reinterpret_cast<const f32x4(&)[PUT][8]>(acc[a]), own, m0 + (wm * FA + a) * 16,
+        put_tile<TO, KIND, PUT, WN>(g, reinterpret_cast<const f32x4(&)[PUT][8]>(acc[a]), own, m0 + (wm * FA + a) * 16,
                                n0 + wn * (GLU ? 64 : 128), min(g.N, n0 + TC), part ? part + a * 16 * T : nullptr, T,
-                               tops ? tops + a * 16 : nullptr, sg, su);
+                               wn, sg, su);
     if constexpr (KIND == kGluGate) {
         // the waves' column sums meet in LDS, in order: four lanes hold eight
         // columns of every fourth row each
