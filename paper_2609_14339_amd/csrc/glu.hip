@@ -41,7 +41,7 @@ __global__ __launch_bounds__(256) void glu_join_kernel(Gemm g)
         vg[i] += bg[i];
         vu[i] += bu[i];
     }
-    glu_epilogue<TO>(g.e, g.N, vg, vu, m, n, left);
+    glu_epilogue<TO>(g.e, g.N, vg, vu, GluAt<TO>(g.e, m, n), n, left);
 }
 
 // Pieces of a product for few tokens: 2048 columns of a row a workgroup.
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(256) void glu_join_few_kernel(Gemm g)
         vg[i] += bg[i];
         vu[i] += bu[i];
     }
-    glu_epilogue<TO>(g.e, g.N, vg, vu, m, n, left);
+    glu_epilogue<TO>(g.e, g.N, vg, vu, GluAt<TO>(g.e, m, n), n, left);
 }
 
 // Pieces of dh, then the gate's gradient.
@@ -82,8 +82,9 @@ __global__ __launch_bounds__(256) void glu_gate_join_kernel(Gemm g)
         float v[8];
         add_pieces(g.part + (id * TM + row) * T + col, count * TM * T, g.splits, v);
         GluBeside<TO> beside;
-        load_glu_beside<TO>(g.e, g.N, beside, m, n, left);
-        glu_gate_epilogue<TO>(g.e, g.N, v, beside, m, n, left, sg, su);
+        const GluAt<TO> at(g.e, m, n);
+        load_glu_beside<TO>(g.e, g.N, beside, at, left);
+        glu_gate_epilogue<TO>(g.e, g.N, v, beside, at, left, sg, su);
     }
     if (!g.e.sums)
         return;
@@ -156,9 +157,10 @@ __global__ __launch_bounds__(256) void glu_act_kernel(const T *dh, int64_t lddh,
         float v[8];
         load8(dh + row * lddh + col, left, v);
         GluBeside<T> beside;
-        load_glu_beside<T>(e, F, beside, row, col, left);
+        const GluAt<T> at(e, row, col);
+        load_glu_beside<T>(e, F, beside, at, left);
         float sg[8] = {}, su[8] = {};
-        glu_gate_epilogue<T>(e, F, v, beside, row, col, left, sg, su);
+        glu_gate_epilogue<T>(e, F, v, beside, at, left, sg, su);
     }
 }
 

@@ -225,17 +225,45 @@ __device__ __forceinline__ void put_db(const Gemm &g, int64_t m0, int rows)
     }
 }
 
-// a = act(g) and s = act'(g), eight at a time.
+// a = act(g) and s = act'(g), eight at a time, from one exponential.  bf16:
+// silu's 1 - s is a difference, within 2^-24 absolutely, and meets 1 + g (1 - s).
 template <typename T>
 __device__ __forceinline__ void act_both(const float (&g)[8], int act, float (&a)[8], float (&s)[8])
 {
+    const auto each = [&](auto one) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        a[i] = g[i];
-        s[i] = 1.f;
-    }
-    apply_act<T>(a, act);
-    apply_slope<T>(s, g, act);
+        for (int i = 0; i < 8; ++i)
+            one(g[i], a[i], s[i]);
+    };
+    if (act == ACSC_ACT_SILU)
+        each([](float z, float &a, float &s) {
+            float t, c;
+            if (sizeof(T) == 2) {
+                t = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z));
+                c = 1.f - t;
+            } else {
+                sigmoid<T>(z, t, c);
+            }
+            a = z * t;
+            s = t * __builtin_fmaf(z, c, 1.f);
+        });
+    else if (act == ACSC_ACT_GELU)
+        each([](float z, float &a, float &s) {
+            float e;
+            const float q = normal_tail<T>(z, e);
+            a = __builtin_fmaf(-fabsf(z > 64.f ? 64.f : z), q, z < 0.f ? 0.f : z);
+            s = __builtin_fmaf(z * 0.39894228040143268f, e, z < 0.f ? q : 1.f - q);
+        });
+    else if (act == ACSC_ACT_RELU)
+        each([](float z, float &a, float &s) {
+            a = act_value<float>(z, ACSC_ACT_RELU);
+            s = act_slope<float>(z, ACSC_ACT_RELU);
+        });
+    else
+        each([](float z, float &a, float &s) {
+            a = z;
+            s = 1.f;
+        });
 }
 
 // The largest magnitude of the first `left` of eight values.
@@ -253,37 +281,65 @@ __device__ __forceinline__ float other8(float x)
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xF, 0xF, false));
 }
 
-// The gated product forward: eight columns n .. n + 7 of row m of g and u
+// Where eight columns n .. n + 7 of row m of what the gated epilogues read and
+// write lie; a step of rows adds uniform strides (the 64-bit products of every
+// row's addresses took a quarter of the epilogue).
+template <typename T>
+struct GluAt {
+    int8_t *cg, *cu;      // codes, or nullptr
+    float *sg, *su;
+    T *z, *y, *h;
+    __device__ __forceinline__ GluAt(const Epi &e, int64_t m, int n)
+    {
+        cg = e.q.codes + m * e.q.ldc + n;
+        cu = e.q_up.codes + m * e.q_up.ldc + n;
+        sg = e.q.scales + m * e.q.lds + n / kGroup;
+        su = e.q_up.scales + m * e.q_up.lds + n / kGroup;
+        z = static_cast<T *>(e.z) + m * e.ldz + n;
+        y = static_cast<T *>(e.y) + m * e.ldy + n;
+        h = static_cast<T *>(e.hidden) + m * e.ldh + n;
+    }
+    __device__ __forceinline__ void step(const Epi &e, int rows)
+    {
+        cg += rows * e.q.ldc;
+        cu += rows * e.q_up.ldc;
+        sg += rows * e.q.lds;
+        su += rows * e.q_up.lds;
+        z += rows * e.ldz;
+        y += rows * e.ldy;
+        h += rows * e.ldh;
+    }
+};
+
+// The gated product forward: eight columns from n on of a row of g and u
 // through the epilogue; `left` of them exist.  With a checkpoint sixteen lanes
 // of the wave, aligned, hold a group of 128 columns of both; half of them forms
 // the gate's scale, the other the up projection's.
 template <typename T, bool CODES = true>
-__device__ __forceinline__ void glu_epilogue(const Epi &e, int F, float (&g)[8], float (&u)[8], int64_t m, int n, int left)
+__device__ __forceinline__ void glu_epilogue(const Epi &e, int F, float (&g)[8], float (&u)[8], const GluAt<T> &at, int n, int left)
 {
     if (e.z) {
-        T *z = static_cast<T *>(e.z) + m * e.ldz + n;
-        store8(z, left, g);
-        store8(z + F, left, u);
+        store8(at.z, left, g);
+        store8(at.z + F, left, u);
     }
     if (CODES && e.q.codes) {
         const bool low = (threadIdx.x & 8) == 0;
         const uint32_t ag = max16(mag8(g, left)), au = max16(mag8(u, left));
         float scale, inv;
         group_scale(low ? ag : au, scale, inv);
-        const float inv2 = other8(inv);
-        store_codes(e.q.codes + m * e.q.ldc + n, left, low ? inv : inv2, g);
-        store_codes(e.q_up.codes + m * e.q_up.ldc + n, left, low ? inv2 : inv, u);
-        const float scale2 = other8(scale);
+        const float inv2 = other8(inv), scale2 = other8(scale);
+        store_codes(at.cg, left, low ? inv : inv2, g);
+        store_codes(at.cu, left, low ? inv2 : inv, u);
         if (left > 0 && n % kGroup == 0) {
-            e.q.scales[m * e.q.lds + n / kGroup] = scale;
-            e.q_up.scales[m * e.q_up.lds + n / kGroup] = scale2;
+            *at.sg = scale;
+            *at.su = scale2;
         }
     }
     apply_act<T>(g, e.act);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         g[i] *= u[i];
-    store8(static_cast<T *>(e.y) + m * e.ldy + n, left, g);
+    store8(at.y, left, g);
 }
 template <typename T>
 __device__ __forceinline__ void glu_bias(const Epi &e, int F, int n, float (&bg)[8], float (&bu)[8])
@@ -300,24 +356,23 @@ struct GluBeside {
     Beside<T> g, u;
 };
 template <typename T>
-__device__ __forceinline__ void load_glu_beside(const Epi &e, int F, GluBeside<T> &b, int64_t m, int n, int left)
+__device__ __forceinline__ void load_glu_beside(const Epi &e, int F, GluBeside<T> &b, const GluAt<T> &at, int left)
 {
     GluBeside<T> r = {};
     if (e.q.codes) {
-        load_raw(e.q.codes + m * e.q.ldc + n, left, r.g.codes);
-        load_raw(e.q_up.codes + m * e.q_up.ldc + n, left, r.u.codes);
-        r.g.scale = left > 0 ? e.q.scales[m * e.q.lds + n / kGroup] : 0.f;
-        r.u.scale = left > 0 ? e.q_up.scales[m * e.q_up.lds + n / kGroup] : 0.f;
+        load_raw(at.cg, left, r.g.codes);
+        load_raw(at.cu, left, r.u.codes);
+        r.g.scale = left > 0 ? *at.sg : 0.f;
+        r.u.scale = left > 0 ? *at.su : 0.f;
     } else {
-        const T *z = static_cast<const T *>(e.z) + m * e.ldz + n;
-        load_raw(z, left, r.g.v);
-        load_raw(z + F, left, r.u.v);
+        load_raw(at.z, left, r.g.v);
+        load_raw(at.z + F, left, r.u.v);
     }
     b = r;
 }
 template <typename T>
-__device__ __forceinline__ void glu_gate_epilogue(const Epi &e, int F, float (&v)[8], const GluBeside<T> &b, int64_t m, int n,
-                                                  int left, float (&sg)[8], float (&su)[8])
+__device__ __forceinline__ void glu_gate_epilogue(const Epi &e, int F, const float (&v)[8], const GluBeside<T> &b,
+                                                  const GluAt<T> &at, int left, float (&sg)[8], float (&su)[8])
 {
     float g[8], u[8], a[8], s[8];
 #pragma unroll
@@ -331,7 +386,7 @@ __device__ __forceinline__ void glu_gate_epilogue(const Epi &e, int F, float (&v
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             h[i] = a[i] * u[i];
-        store8(static_cast<T *>(e.hidden) + m * e.ldh + n, left, h);
+        store8(at.h, left, h);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -344,9 +399,8 @@ __device__ __forceinline__ void glu_gate_epilogue(const Epi &e, int F, float (&v
             sg[i] += i < left ? s[i] : 0.f;
             su[i] += i < left ? a[i] : 0.f;
         }
-    T *y = static_cast<T *>(e.y) + m * e.ldy + n;
-    store8(y, left, s);
-    store8(y + F, left, a);
+    store8(at.y, left, s);
+    store8(at.y + F, left, a);
 }
 
 // A wave's accumulators of 16 NA rows by 64 hidden columns through the gated
@@ -358,15 +412,16 @@ template <typename T, int NA, bool PAIR>
 __device__ __forceinline__ void put_glu_rows(const Gemm &g, const char *lds, int64_t m0, int n0, int wn)
 {
     constexpr int L = PAIR ? 16 : 8, STEP = 64 / L, ROWS = PAIR ? NA * 8 : NA * 16;
-    const int lane = threadIdx.x & 63, at = lane % L;
-    const int n = n0 - (PAIR ? wn * 64 : 0) + at * 8, c = (at & 7) * 2, cols = g.N - n;
+    const int lane = threadIdx.x & 63, place = lane % L;
+    const int n = n0 - (PAIR ? wn * 64 : 0) + place * 8, c = (place & 7) * 2, cols = g.N - n;
     const int first = PAIR ? wn * ROWS : 0;
     if (PAIR)
-        lds += (at / 8 - wn) * NA * 8192;
+        lds += (place / 8 - wn) * NA * 8192;
     float bg[8], bu[8];
     glu_bias<T>(g.e, g.N, n, bg, bu);
+    GluAt<T> at(g.e, m0 + first + lane / L, n);
 #pragma unroll 1
-    for (int r0 = 0; r0 < ROWS; r0 += STEP) {
+    for (int r0 = 0; r0 < ROWS; r0 += STEP, at.step(g.e, STEP)) {
         const int row = first + r0 + lane / L;
         const auto chunk = [&](int k) { return *reinterpret_cast<const f32x4 *>(lds + row * 512 + (k ^ (row & 31)) * 16); };
         const f32x4 g0 = chunk(c), g1 = chunk(c + 1), u0 = chunk(16 + c), u1 = chunk(17 + c);
@@ -377,8 +432,7 @@ __device__ __forceinline__ void put_glu_rows(const Gemm &g, const char *lds, int
             vg[i] += bg[i];
             vu[i] += bu[i];
         }
-        const int64_t m = m0 + row;
-        glu_epilogue<T, PAIR>(g.e, g.N, vg, vu, m, n, m < g.M ? cols : 0);
+        glu_epilogue<T, PAIR>(g.e, g.N, vg, vu, at, n, m0 + row < g.M ? cols : 0);
     }
 }
 template <typename T, int NA>
@@ -387,20 +441,22 @@ __device__ __forceinline__ void put_glu_gate_rows(const Gemm &g, const char *lds
 {
     const int lane = threadIdx.x & 63, n = n0 + (lane & 15) * 8, c = (lane & 15) * 2;
     const int cols = end - n;
+    GluAt<T> at(g.e, m0 + (lane >> 4), n);
 #pragma unroll 1
     for (int r0 = 0; r0 < NA * 4; r0 += 4) {
         GluBeside<T> beside[4];
+        const auto left = [&](int u) { return m0 + (r0 + u) * 4 + (lane >> 4) < g.M ? cols : 0; };
+        GluAt<T> ahead = at;
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            load_glu_beside<T>(g.e, g.N, beside[u], min<int64_t>(m0 + (r0 + u) * 4 + (lane >> 4), g.M - 1), n, cols);
+        for (int u = 0; u < 4; ++u, ahead.step(g.e, 4))
+            load_glu_beside<T>(g.e, g.N, beside[u], ahead, left(u));
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < 4; ++u, at.step(g.e, 4)) {
             const int row = (r0 + u) * 4 + (lane >> 4);
             const f32x4 lo = *reinterpret_cast<const f32x4 *>(lds + row * 512 + (c ^ (row & 31)) * 16);
             const f32x4 hi = *reinterpret_cast<const f32x4 *>(lds + row * 512 + ((c + 1) ^ (row & 31)) * 16);
-            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            const int64_t m = m0 + row;
-            glu_gate_epilogue<T>(g.e, g.N, v, beside[u], m, n, m < g.M ? cols : 0, sg, su);
+            const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            glu_gate_epilogue<T>(g.e, g.N, v, beside[u], at, left(u), sg, su);
         }
     }
 }

@@ -197,7 +197,7 @@ __global__ __launch_bounds__(kWaves * 64) void glu_few_kernel(Gemm g)
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             v[o][j] += bias[o][j];
-    glu_epilogue<T>(g.e, g.N, v[0], v[1], m, n, g.N - n);   // without a checkpoint
+    glu_epilogue<T, false>(g.e, g.N, v[0], v[1], GluAt<T>(g.e, m, n), n, g.N - n);
 }
 
 // The weight gradient of few tokens: outer products, bound by writing dW.  A
