@@ -312,10 +312,10 @@ struct GluAt {
 };
 
 // The gated product forward: eight columns from n on of a row of g and u
-// through the epilogue; `left` of them exist.  With a checkpoint sixteen lanes
-// of the wave, aligned, hold a group of 128 columns of both; half of them forms
+// through the epilogue; `left` of them exist (WHOLE: all, of a row that does).
+// With a checkpoint sixteen lanes of the wave, aligned, hold a group of 128 columns of both; half of them forms
 // the gate's scale, the other the up projection's.
-template <typename T, bool CODES = true>
+template <typename T, bool CODES = true, bool WHOLE = false>
 __device__ __forceinline__ void glu_epilogue(const Epi &e, int F, float (&g)[8], float (&u)[8], const GluAt<T> &at, int n, int left)
 {
     if (e.z) {
@@ -324,7 +324,7 @@ __device__ __forceinline__ void glu_epilogue(const Epi &e, int F, float (&g)[8],
     }
     if (CODES && e.q.codes) {
         const bool low = (threadIdx.x & 8) == 0;
-        const uint32_t ag = max16(mag8(g, left)), au = max16(mag8(u, left));
+        const uint32_t ag = max16(mag8(g, WHOLE ? 8 : left)), au = max16(mag8(u, WHOLE ? 8 : left));
         float scale, inv;
         group_scale(low ? ag : au, scale, inv);
         const float inv2 = other8(inv), scale2 = other8(scale);
@@ -335,7 +335,14 @@ __device__ __forceinline__ void glu_epilogue(const Epi &e, int F, float (&g)[8],
             *at.su = scale2;
         }
     }
-    apply_act<T>(g, e.act);
+    if (sizeof(T) == 2 && e.act == ACSC_ACT_SILU) {
+        // one branch less than for fp32: an overflowing exponential gives 0
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            g[i] *= __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * g[i]));
+    } else {
+        apply_act<T>(g, e.act);
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         g[i] *= u[i];
@@ -407,13 +414,14 @@ __device__ __forceinline__ void glu_gate_epilogue(const Epi &e, int F, const flo
 // epilogue: fragments 0 .. 3 of a row hold g, 4 .. 7 u.  Alone, eight lanes take
 // a row, eight rows a step (no checkpoint then).  PAIR: two waves hold the 128
 // columns of a group, in neighbouring parts of LDS, and each takes half of the
-// rows whole, sixteen lanes a row.
-template <typename T, int NA, bool PAIR>
+// rows whole, sixteen lanes a row.  WHOLE: its columns all exist.
+template <typename T, int NA, bool PAIR, bool WHOLE>
 __device__ __forceinline__ void put_glu_rows(const Gemm &g, const char *lds, int64_t m0, int n0, int wn)
 {
     constexpr int L = PAIR ? 16 : 8, STEP = 64 / L, ROWS = PAIR ? NA * 8 : NA * 16;
     const int lane = threadIdx.x & 63, place = lane % L;
-    const int n = n0 - (PAIR ? wn * 64 : 0) + place * 8, c = (place & 7) * 2, cols = g.N - n;
+    const int n = n0 - (PAIR ? wn * 64 : 0) + place * 8, c = (place & 7) * 2;
+    const int cols = WHOLE ? 8 : g.N - n;
     const int first = PAIR ? wn * ROWS : 0;
     if (PAIR)
         lds += (place / 8 - wn) * NA * 8192;
@@ -432,7 +440,7 @@ __device__ __forceinline__ void put_glu_rows(const Gemm &g, const char *lds, int
             vg[i] += bg[i];
             vu[i] += bu[i];
         }
-        glu_epilogue<T, PAIR>(g.e, g.N, vg, vu, at, n, m0 + row < g.M ? cols : 0);
+        glu_epilogue<T, PAIR, WHOLE>(g.e, g.N, vg, vu, at, n, m0 + row < g.M ? cols : 0);
     }
 }
 template <typename T, int NA>
@@ -498,7 +506,10 @@ __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8
     if constexpr (KIND == kGluForward && WN == 2)
         if (g.e.q.codes) {
             lds_meet();
-            put_glu_rows<T, NA, true>(g, lds, m0, n0, wn);
+            if (n0 - wn * 64 + 128 <= g.N)
+                put_glu_rows<T, NA, true, true>(g, lds, m0, n0, wn);
+            else
+                put_glu_rows<T, NA, true, false>(g, lds, m0, n0, wn);
             lds_meet();   // before the parts are written again
             return;
         }
@@ -507,7 +518,7 @@ __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     if constexpr (KIND == kGluForward)
-        put_glu_rows<T, NA, false>(g, lds, m0, n0, wn);
+        put_glu_rows<T, NA, false, false>(g, lds, m0, n0, wn);
     else if constexpr (KIND == kGluGate)
         put_glu_gate_rows<T, NA>(g, lds, m0, n0, end, sg, su);
     else if (n0 + 128 <= end)
