@@ -178,14 +178,15 @@ struct Tile {
     int at_once;          // workgroups of a CU
     double step, alone;   // us of a step with as many, and with one
     double edge;
+    double gated;         // more beside them with the gated product's gradient in the epilogue
 };
 // codes: a gated product's pre-activations are coded, whose groups lie in two
 // tiles of 128 columns each: there every tile goes through the pieces' sum.
 inline Cut cut_of(EpiKind kind, const Shape &s, int steps, bool bf16, bool codes)
 {
     static const Tile kBf16[] = {
-        {256, 256, 1, 1.5, 1.5, 5}, {128, 128, 2, 1.0, 0.65, 3}, {64, 128, 3, 1.05, 0.85, 3}, {32, 128, 4, 1.0, 0.8, 3}, {128, 64, 2, 0.8, 0.55, 3}};
-    static const Tile kF32[] = {{128, 128, 2, 4.1, 2.2, 3}, {64, 128, 3, 3.2, 1.2, 3}, {32, 128, 4, 2.3, 1.2, 3}, {128, 64, 2, 2.2, 1.2, 3}};
+        {256, 256, 1, 1.5, 1.5, 5, 20}, {128, 128, 2, 1.0, 0.65, 3, 9}, {64, 128, 3, 1.05, 0.85, 3, 6}, {32, 128, 4, 1.0, 0.8, 3, 4}, {128, 64, 2, 0.8, 0.55, 3, 12}};
+    static const Tile kF32[] = {{128, 128, 2, 4.1, 2.2, 3, 9}, {64, 128, 3, 3.2, 1.2, 3, 6}, {32, 128, 4, 2.3, 1.2, 3, 4}, {128, 64, 2, 2.2, 1.2, 3, 12}};
     const Tile *first = bf16 ? kBf16 : kF32, *end = bf16 ? std::end(kBf16) : std::end(kF32);
     Cut best{};
     double least = 0;
@@ -196,18 +197,19 @@ inline Cut cut_of(EpiKind kind, const Shape &s, int steps, bool bf16, bool codes
             continue;
         const int64_t tiles = ((s.M + t->rows - 1) / t->rows) * ((s.N + t->cols - 1) / t->cols);
         const int slots = 256 * t->at_once;
-        const auto rounds = [&](int64_t groups, int per) {
+        const auto rounds = [&](int64_t groups, int per, bool whole) {
+            const double edge = t->edge + (whole && kind == kGluGate ? t->gated : 0);
             const int64_t rest = groups % slots, beside = (rest + 255) / 256 - 1;
             const double step = t->at_once > 1 ? t->alone + (t->step - t->alone) * static_cast<double>(beside) / (t->at_once - 1) : t->alone;
-            return static_cast<double>(groups / slots) * (per * t->step + t->edge) + (rest ? per * step + t->edge : 0);
+            return static_cast<double>(groups / slots) * (per * t->step + edge) + (rest ? per * step + edge : 0);
         };
         const bool all = codes && kind == kGluForward && t->cols == 128;   // through the pieces' sum
         const int64_t rest = all ? tiles : tiles % slots;
         for (int want = 1; want == 1 || (rest && want <= 64 && steps / want >= 4 && rest * want <= 2048);
              want += want < 8 ? 1 : 8) {
             const int per = (steps + want - 1) / want, n = (steps + per - 1) / per;
-            const double us = n == 1 && !all ? rounds(tiles, steps)
-                                     : rounds(tiles - rest, steps) + rounds(rest * n, per) + 10 +
+            const double us = n == 1 && !all ? rounds(tiles, steps, true)
+                                     : rounds(tiles - rest, steps, true) + rounds(rest * n, per, false) + 10 +
                                            n * static_cast<double>(rest) * t->rows * t->cols * 8 / 4.5e6;
             if (least == 0 || us < least) {
                 least = us;
@@ -233,10 +235,10 @@ Plan plan_of(EpiKind kind, const Shape &s, acsc_dtype dt, bool fits_a, bool fits
         return p;
     }
     if ((kind == kForward || kind == kGluForward) && s.M <= few_tokens(kind, fits_b)) {
-        // 16 outputs a workgroup: a cut only where they fill half the CUs at
+        // 16 outputs (or eight of each kind) a workgroup: a cut only where they fill half the CUs at
         // most, at two rounds of eight lines a piece
-        const int cols = kind == kGluForward ? s.N / 2 : s.N;   // 16 of the gate and 16 up ones
-        const int groups = (cols + 15) / 16, round = 8 * 128 / static_cast<int>(dtype_size(dt)), rounds = (s.K + round - 1) / round;
+        const int cols = kind == kGluForward ? s.N / 2 : s.N, groups = kind == kGluForward ? (cols + 7) / 8 : (cols + 15) / 16;
+        const int round = 8 * 128 / static_cast<int>(dtype_size(dt)), rounds = (s.K + round - 1) / round;
         const int want = groups >= 128 ? 1 : std::max(1, std::min((255 + groups) / groups, rounds / 2));
         const int per = (rounds + want - 1) / want;
         p.few = true;
