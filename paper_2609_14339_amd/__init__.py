@@ -1116,12 +1116,15 @@ def lin_backward_weight(dz: torch.Tensor, x: Union[torch.Tensor, Q8], act: str =
 GLU_FORWARD, GLU_BACKWARD_INPUT = 0, 1
 
 
-def _here(*ts):
-    """Calls run on the current device: their tensors have to be there."""
-    dev = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in ts) else None
+def _here(first: torch.Tensor, *ts):
+    """Calls run on the current device: their tensors have to be there.  (A
+    tensor on the host, device -1, is refused where its shape is looked at.)"""
+    dev = first.get_device()
+    if dev >= 0 and dev != torch._C._cuda_getDevice():
+        raise AcscError(ACSC_EINVAL, f"tensors are on cuda:{dev}, the current device is cuda:{torch._C._cuda_getDevice()}")
     for t in ts:
-        if t is not None and t.is_cuda and t.get_device() != dev:
-            raise AcscError(ACSC_EINVAL, f"a tensor is on cuda:{t.get_device()}, the current device is cuda:{dev}")
+        if t is not None and t.get_device() != dev and t.is_cuda and dev >= 0:
+            raise AcscError(ACSC_EINVAL, f"tensors are on cuda:{dev} and cuda:{t.get_device()}")
 
 
 def _drop_ref(drop: Optional[Drop]):
@@ -1208,7 +1211,7 @@ def rms_recompute(src: Union[torch.Tensor, Q8], rstd: torch.Tensor, gamma: Optio
     if stream is not None:
         return _on(stream, rms_recompute, src, rstd, gamma, dtype, y)
     rows, H = _two_d(src.codes if isinstance(src, Q8) else src, "src")
-    _here(*(src if isinstance(src, Q8) else (src,)), rstd, gamma, y)
+    _here(rstd, *(src if isinstance(src, Q8) else (src,)), gamma, y)
     p, ld, q = _kept(src, (rows, H), dtype, "src")
     pr = _vec(rstd, rows, torch.float32, "rstd")
     pg = _optvec(gamma, H, dtype, "gamma")
@@ -1308,7 +1311,7 @@ def join_backward(dout: Optional[torch.Tensor], dy: Optional[torch.Tensor], out:
     if one is None:
         raise AcscError(ACSC_EINVAL, "one of dout and dy is needed")
     shape = rows, H = _two_d(one, "dout" if one is dout else "dy")
-    _here(dout, dy, *(out if isinstance(out, Q8) else (out,)), *(b if isinstance(b, Q8) else (b,)), rstd_post, rstd_pre, post,
+    _here(one, dy, *(out if isinstance(out, Q8) else (out,)), *(b if isinstance(b, Q8) else (b,)), rstd_post, rstd_pre, post,
           gate, pre, dr, db, dpost, dgate, dpre, ws)
     if dy is not None and pre is None:
         raise AcscError(ACSC_EINVAL, "dy without the norm after (pre)")
