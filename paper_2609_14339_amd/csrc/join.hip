@@ -406,14 +406,16 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
 }
 
 // Rows past 8192 columns, which with their sums leave no registers: a workgroup
-// reads a row once for each of its means and once, from the caches, for the
-// results, and adds to its column sums in LDS, or past 16384 columns (LDS_SUMS
-// false) in its partial itself; each thread owns its columns.
+// reads a row for its means and again, from the caches, for the results, and
+// adds to its column sums in LDS, or past 16384 columns (LDS_SUMS false) in its
+// partial itself; each thread owns its columns.  What bounds it is arithmetic:
+// both passes draw the mask and decode.  4096 x 16384 bf16 290 us, of which HBM
+// asks 156; with the means in a pass each 1035 x 9984 fp32 took 112, 86 so.
 template <typename T, bool JOIN, bool KEPT, bool LDS_SUMS>
 __global__ __launch_bounds__(1024, 4) void join_backward_wide_kernel(Bwd<T> p)
 {
     extern __shared__ __align__(16) float held[];
-    __shared__ float slots[2][2][16];
+    __shared__ float slots[2][3 * 16];
     float *part = p.part ? p.part + static_cast<int64_t>(blockIdx.x) * 2 * p.H : nullptr;
     const int padded = (p.H + 7) / 8 * 8;
     const bool branch = JOIN && (p.post || p.gate);
@@ -459,80 +461,89 @@ __global__ __launch_bounds__(1024, 4) void join_backward_wide_kernel(Bwd<T> p)
             for (int i = 0; i < 8; ++i)
                 v[i] *= g[i];
         };
+        // Both means from one pass: with t0 = dout + rho2 g, t = t0 - rho2 h2 m2,
+        // and D and the gains are linear, so the sum of e h1 is that of t0's less
+        // rho2 m2 times that of h2's.
         float m2 = 0.f, m1 = 0.f;
-        if (p.dy) {
-            float s[1] = {0.f};
-#pragma unroll 1
+        const bool after_mean = p.dy != nullptr, before_mean = JOIN && p.post;
+        if (after_mean || before_mean) {
+            float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll 2
             for (int col = threadIdx.x * 8; col < p.H; col += 8192) {
                 const int left = p.H - col;
-                float h[8], g[8];
-                after(col, left, h, g);
-                times(p.pre, col, left, g);
+                float v[8] = {}, h[8] = {}, g[8] = {};
+                if (after_mean) {
+                    after(col, left, h, g);
+                    times(p.pre, col, left, g);
+                }
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     s[0] += g[i] * h[i];     // past the end of the row g = 0
+                if (!before_mean)
+                    continue;
+                load8(p.dout + row * p.lddo + col, p.dout ? left : 0, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    v[i] += r2 * g[i];
+                Src<T, KEPT> b;
+                b.load(p.b, p.ldb, p.q_b, row, col, left);
+                float w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    w[i] = b.at(i) * r1;
+                times(p.gate, col, left, w);
+                times(p.post, col, left, w);   // zeros past the end of the row
+                if (p.drop.below)
+                    drop8(p.drop, d, col, v);
+                if (p.drop.below && after_mean)
+                    drop8(p.drop, d, col, h);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    s[1] += v[i] * w[i];
+                    s[2] += h[i] * w[i];
+                }
             }
-            row_sum<1024>(s, slots[flip][0]);
+            row_sum<1024>(s, slots[flip]);
             m2 = s[0] / p.H;
+            m1 = (s[1] - r2 * m2 * s[2]) / p.H;
         }
-        // eight columns of t (and, for the column sums, dy h2)
-        const auto whole = [&](int col, int left, bool sums, float (&v)[8]) {
+        // eight columns of t, with dy h2 for the column sums
+        const auto whole = [&](int col, int left, float (&v)[8]) {
             load8(p.dout + row * p.lddo + col, p.dout ? left : 0, v);
             if (!p.dy)
                 return;
             float h[8], g[8];
             after(col, left, h, g);
-            if (sums) {
-                float o[8];
+            float o[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    o[i] = g[i] * h[i];
-                add(0, col, left, first, o);
-            }
+            for (int i = 0; i < 8; ++i)
+                o[i] = g[i] * h[i];
+            add(0, col, left, first, o);
             times(p.pre, col, left, g);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 v[i] += r2 * (g[i] - h[i] * m2);
         };
-        // eight columns of e and h1 from t (and, for the column sums, u h1)
-        const auto before = [&](int col, int left, bool sums, float (&v)[8], float (&h)[8]) {
+        // eight columns of e and h1 from u, with u h1 for the column sums
+        const auto before = [&](int col, int left, float (&v)[8], float (&h)[8]) {
             Src<T, KEPT> b;
             b.load(p.b, p.ldb, p.q_b, row, col, left);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 h[i] = b.at(i) * r1;
-            if (sums) {
-                float o[8];
+            float o[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    o[i] = i < left ? v[i] * h[i] : 0.f;
-                add(1, col, left, first, o);
-            }
+            for (int i = 0; i < 8; ++i)
+                o[i] = i < left ? v[i] * h[i] : 0.f;
+            add(1, col, left, first, o);
             times(p.gate, col, left, v);
             times(p.post, col, left, v);
         };
-        if (JOIN && p.post) {
-            float s[1] = {0.f};
-#pragma unroll 1
-            for (int col = threadIdx.x * 8; col < p.H; col += 8192) {
-                const int left = p.H - col;
-                float v[8], h[8];
-                whole(col, left, false, v);
-                if (p.drop.below)
-                    drop8(p.drop, d, col, v);
-                before(col, left, false, v, h);
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    s[0] += v[i] * h[i];     // zeros past the end of the row
-            }
-            row_sum<1024>(s, slots[flip][1]);
-            m1 = s[0] / p.H;
-        }
 #pragma unroll 1
         for (int col = threadIdx.x * 8; col < p.H; col += 8192) {
             const int left = p.H - col;
             float v[8], o[8], h[8];
-            whole(col, left, true, v);
+            whole(col, left, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 o[i] = JOIN ? p.scale * v[i] : v[i];
@@ -540,7 +551,7 @@ __global__ __launch_bounds__(1024, 4) void join_backward_wide_kernel(Bwd<T> p)
                 if (p.drop.below)
                     drop8(p.drop, d, col, v);
                 if (branch)
-                    before(col, left, true, v, h);
+                    before(col, left, v, h);
                 if (p.post)
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
@@ -653,11 +664,14 @@ inline Shape backward_shape(int H, bool f32)
     return {0, 0};   // the kernel for wide rows
 }
 
-// Workgroups of the backward pass, which is also its number of partials.
-inline int bwd_groups(int64_t rows, int H)
+// Workgroups of the backward pass, which is also its number of partials: what
+// the card holds at once.
+inline int bwd_groups(int64_t rows, int H, bool f32)
 {
-    const int rpb = H <= 1024 ? 4 : 1;
-    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((rows + rpb - 1) / rpb, H <= 8192 ? 512 : 256)));
+    const int64_t blocks = H <= 1024 ? (rows + 3) / 4 : rows;
+    // registers: 105 to 146 a lane for one chunk, to 242 for two
+    const int most = H <= 512 ? 1024 : H <= 1024 ? 512 : H <= 2048 ? (f32 ? 768 : 1024) : H <= 4096 && !f32 ? 512 : 256;
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(blocks, most)));
 }
 
 inline int check_common(int64_t rows, int H, int dt)
@@ -810,7 +824,7 @@ int launch_backward(const BwdArgs &a, int64_t rows, int H, int groups, float *pa
 int backward(const BwdArgs &a, acsc_dtype dt, int64_t rows, int H, void *ws, size_t ws_bytes, hipStream_t st, const char *tag)
 {
     const bool sums = a.dpost || a.dgate || a.dpre;
-    const int groups = bwd_groups(rows, H);
+    const int groups = bwd_groups(rows, H, dt == ACSC_F32);
     if (sums) {
         ACSC_CHECK_ARG(ws, ACSC_EINVAL, "null workspace");
         ACSC_CHECK_ARG(aligned(ws, 256), ACSC_EALIGN, "workspace not 256-byte aligned");
@@ -903,7 +917,7 @@ extern "C" int join_workspace_size(int64_t rows, int H, size_t *bytes)
     clear_error();
     ACSC_TRY(check_common(rows, H, ACSC_F32));
     ACSC_CHECK_ARG(bytes, ACSC_EINVAL, "null pointer bytes");
-    *bytes = static_cast<size_t>(bwd_groups(rows, H)) * 2 * H * sizeof(float);
+    *bytes = static_cast<size_t>(std::max(bwd_groups(rows, H, false), bwd_groups(rows, H, true))) * 2 * H * sizeof(float);
     return ACSC_OK;
 }
 
