@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256) void glu_gate_join_kernel(Gemm g)
         meet[row % ROWS][1][col + i] = su[i];
     }
     __syncthreads();
-    float *out = g.e.sums + (static_cast<int64_t>(tile_m) * g.e.cut_slots + blockIdx.x % PER) * 2 * g.N;
+    float *out = g.e.sums + (g.tm + static_cast<int64_t>(tile_m - g.e.cut_first) * g.e.cut_slots + blockIdx.x % PER) * 2 * g.N;
     for (int k = threadIdx.x; k < 2 * T; k += 256) {
         float s = 0.f;
 #pragma unroll
@@ -119,8 +119,10 @@ __global__ __launch_bounds__(64 * kSlices) void glu_sums_kernel(Gemm g, int tile
         for (int m = sl * per; m < end; ++m) {
             const int band = m / 4, height = min(g.tm - band * 4, 4);
             const int64_t id = static_cast<int64_t>(band) * 4 * g.tn + static_cast<int64_t>(n / tile) * height + m % 4;
-            const int slots = id < g.whole ? 1 : g.e.cut_slots;
-            const float *p = g.e.sums + static_cast<int64_t>(m) * g.e.cut_slots * 2 * F + col;
+            const bool whole = id < g.whole;
+            const int slots = whole ? 1 : g.e.cut_slots;
+            const int64_t at = whole ? m : g.tm + static_cast<int64_t>(m - g.e.cut_first) * slots;
+            const float *p = g.e.sums + at * 2 * F + col;
             for (int i = 0; i < slots; ++i)
                 s += p[static_cast<int64_t>(i) * 2 * F];
         }
@@ -238,14 +240,17 @@ int plan_glu(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, bool codes
     return check_tiles(p);
 }
 
-// Partials of a tile that is cut: one for each workgroup of its pieces' sum.
-inline int cut_slots(const Plan &p)
+// Partials of the column sums: of a cut tile, one for each workgroup of its
+// pieces' sum.
+inline int cut_slots(const Plan &p) { return p.rows * p.tile / 2048; }
+inline int cut_first(const Plan &p)
 {
-    return p.whole < static_cast<int64_t>(p.tm) * p.tn ? p.rows * p.tile / 2048 : 1;
+    return p.whole < static_cast<int64_t>(p.tm) * p.tn ? static_cast<int>(p.whole / (4ll * p.tn) * 4) : p.tm;
 }
 inline size_t sums_bytes(const Plan &p, int F)
 {
-    return up256(static_cast<size_t>(p.tm) * cut_slots(p) * 2 * F * sizeof(float));
+    const size_t partials = p.tm + static_cast<size_t>(p.tm - cut_first(p)) * cut_slots(p);
+    return up256(partials * 2 * F * sizeof(float));
 }
 
 int workspace_size(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int extra, bool any, size_t *bytes)
@@ -357,7 +362,7 @@ extern "C" int glu_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t r
         return rc;
     if (int rc = check_ws(ws, ws_bytes, p.bytes()))
         return rc;
-    g.e = Epi{h, ld_h, bias, nullptr, 0, z, ld_z, q8_of(q_gate), act, 0, q8_of(q_up), nullptr, 0, nullptr, 0};
+    g.e = Epi{h, ld_h, bias, nullptr, 0, z, ld_z, q8_of(q_gate), act, 0, q8_of(q_up), nullptr, 0, nullptr, 0, 0};
     return run_product(g, kGluForward, p, s, dt, dt, static_cast<char *>(ws), nullptr, nullptr, stream, "glu_forward");
 }
 
@@ -449,7 +454,7 @@ extern "C" int glu_backward_input(const void *dy, int64_t ld_dy, acsc_dtype dt, 
     if (int rc = check_ws(ws, ws_bytes, sums + p.bytes()))
         return rc;
     g.e = Epi{dz, ld_dz, nullptr, nullptr, 0, const_cast<void *>(z), ld_z, q8_of(q_gate), act, 0, q8_of(q_up), h, ld_h,
-              dbias ? static_cast<float *>(ws) : nullptr, cut_slots(p)};
+              dbias ? static_cast<float *>(ws) : nullptr, cut_first(p), cut_slots(p)};
     if (int rc = run_product(g, kGluGate, p, s, dt, dt, static_cast<char *>(ws) + sums, nullptr, nullptr, stream, "glu_backward_input"))
         return rc;
     if (!dbias)

@@ -12,6 +12,7 @@
 #include "drop.h"
 #include "rows.h"
 
+#include <atomic>
 #include <type_traits>
 
 namespace acsc {
@@ -769,8 +770,17 @@ int run_backward(const Bwd<T> &p, int groups, hipStream_t st, const char *tag)
     if (!s.nt) {
         if (p.H <= 16384) {
             const size_t lds = static_cast<size_t>((p.H + 7) / 8 * 8) * 2 * sizeof(float);
-            if (int rc = allow_lds(join_backward_wide_kernel<T, JOIN, KEPT, true>, lds))
-                return rc;
+            // once a device: asked for on every call it costs the host more than the launch
+            static std::atomic<uint64_t> allowed{0};
+            int dev = 0;
+            if (hipGetDevice(&dev) != hipSuccess)
+                return set_error(ACSC_EHIP, "cannot query the device");
+            if (dev > 63 || !(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
+                if (int rc = allow_lds(join_backward_wide_kernel<T, JOIN, KEPT, true>, 16384 * 2 * sizeof(float)))
+                    return rc;
+                if (dev < 64)
+                    allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
+            }
             ACSC_LAUNCH(tag, (join_backward_wide_kernel<T, JOIN, KEPT, true>), grid, dim3(1024), lds, st, p);
         } else {
             ACSC_LAUNCH(tag, (join_backward_wide_kernel<T, JOIN, KEPT, false>), grid, dim3(1024), 0, st, p);

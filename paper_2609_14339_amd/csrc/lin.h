@@ -42,11 +42,11 @@ struct Epi {
     Q8 q_up;
     void *hidden;
     int64_t ldh;
-    // gate: column sums of both halves of y before their rounding, a partial of
-    // each tile's rows (of a cut tile `cut_slots` of them), [tm][cut_slots][2][F],
-    // or nullptr
+    // gate: column sums of both halves of y before their rounding, or nullptr: a
+    // partial of each row of tiles, [tm][2][F], and behind them those of cut tiles,
+    // `cut_slots` of each row of tiles from cut_first on
     float *sums;
-    int cut_slots;
+    int cut_first, cut_slots;
 };
 
 struct Gemm {
@@ -225,8 +225,7 @@ __device__ __forceinline__ void put_db(const Gemm &g, int64_t m0, int rows)
     }
 }
 
-// a = act(g) and s = act'(g), eight at a time, from one exponential.  bf16:
-// silu's 1 - s is a difference, within 2^-24 absolutely, and meets 1 + g (1 - s).
+// a = act(g) and s = act'(g), eight at a time, from one exponential.
 template <typename T>
 __device__ __forceinline__ void act_both(const float (&g)[8], int act, float (&a)[8], float (&s)[8])
 {
@@ -238,12 +237,7 @@ __device__ __forceinline__ void act_both(const float (&g)[8], int act, float (&a
     if (act == ACSC_ACT_SILU)
         each([](float z, float &a, float &s) {
             float t, c;
-            if (sizeof(T) == 2) {
-                t = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z));
-                c = 1.f - t;
-            } else {
-                sigmoid<T>(z, t, c);
-            }
+            sigmoid<T>(z, t, c);
             a = z * t;
             s = t * __builtin_fmaf(z, c, 1.f);
         });
@@ -335,14 +329,7 @@ __device__ __forceinline__ void glu_epilogue(const Epi &e, int F, float (&g)[8],
             *at.su = scale2;
         }
     }
-    if (sizeof(T) == 2 && e.act == ACSC_ACT_SILU) {
-        // one branch less than for fp32: an overflowing exponential gives 0
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            g[i] *= __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * g[i]));
-    } else {
-        apply_act<T>(g, e.act);
-    }
+    apply_act<T>(g, e.act);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         g[i] *= u[i];

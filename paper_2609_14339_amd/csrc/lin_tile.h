@@ -488,7 +488,7 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
                 }
             }
             __syncthreads();
-            float *out = g.e.sums + static_cast<int64_t>(tile_m) * g.e.cut_slots * 2 * g.N;
+            float *out = g.e.sums + static_cast<int64_t>(tile_m) * 2 * g.N;
             for (int c = threadIdx.x; c < 2 * T; c += blockDim.x) {
                 float s = 0.f;
 #pragma unroll

@@ -200,7 +200,7 @@ def test_a_step_in_a_graph(pk):
     g = torch.randn(rows, H, device="cuda").bfloat16()
     d = make(pk, rows, H, 0.1)
     leaves = [x, *p.values()]
-    step = lambda: [o := glu_block(x, **p, drop=d), *torch.autograd.grad(o, leaves, g)]
+    step = lambda: [(o := glu_block(x, **p, drop=d)).detach(), *torch.autograd.grad(o, leaves, g)]
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
@@ -216,3 +216,17 @@ def test_a_step_in_a_graph(pk):
         torch.cuda.synchronize()
         for a, b in zip(held, step()):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("wanted", ["x", "gamma", "W", "bias", "W2", "bias2", "post", "gate"])
+def test_only_one_gradient_wanted(pk, wanted):
+    """Each gradient by itself is the one that all of them together give."""
+    from paper_2609_14339_amd.block import glu_block
+    p = {k: v.detach() for k, v in params(96, 64, F32, 6).items()}
+    p["x"] = torch.randn(40, 96, generator=torch.Generator().manual_seed(1)).cuda()
+    g, d = torch.randn(40, 96, generator=torch.Generator().manual_seed(2)).cuda(), make(pk, 40, 96, 0.1)
+    every = {k: v.clone().requires_grad_() for k, v in p.items()}
+    want = dict(zip(every, torch.autograd.grad(glu_block(**every, drop=d), list(every.values()), g)))
+    one = {k: v.clone().requires_grad_(k == wanted) for k, v in p.items()}
+    got, = torch.autograd.grad(glu_block(**one, drop=d), [one[wanted]], g)
+    assert torch.equal(got, want[wanted])

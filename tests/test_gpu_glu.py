@@ -229,3 +229,28 @@ def test_workspace_and_refusals_on_the_device(pk):
         pk.glu_backward_act(h, z[:, :128])
     with pytest.raises(pk.AcscError, match="overlap"):
         pk.glu_forward(x, W, h=x[:, :128])
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [2, 40])
+def test_gates_at_the_ends_of_the_range(pk, act, dtype, rows):
+    """Gates that all but close, times large up values: h and its gradient keep their relative accuracy as far as the
+    activation of a linear layer does."""
+    g = torch.tensor([-95.0, -89.0, -88.0, -80.0, -40.0, -13.0, -5.0, 0.0, 5.0, 40.0, 89.0, 1e4]).to(dtype).cuda()
+    F = g.numel()
+    # z = x W' + b of x = 1 and W = 0
+    x = torch.ones(rows, 8, dtype=dtype, device="cuda")
+    W = torch.zeros(2 * F, 8, dtype=dtype, device="cuda")
+    big = torch.full((F,), 1e30, dtype=dtype, device="cuda")
+    big[-1] = 1.0
+    h, z = pk.glu_forward(x, W, torch.cat((g, big)), act, keep="z")
+    a = pk.lin_forward(x, W[:F], g, act)[0].double()
+    want = a * big.double()
+    # one rounding of a and one of h more than the exact product has
+    eps = 2.0 ** -7 if dtype == BF16 else 2.0 ** -22
+    assert ((h.double() - want).abs() <= eps * want.abs() + 1e-8).all()
+    dz, _ = pk.glu_backward_act(torch.ones_like(h), z, act)
+    assert ((dz[:, F:].double() - a).abs() <= eps * a.abs() + 1e-38).all()
+    slope = pk.lin_backward_act(torch.ones_like(h), z[:, :F].contiguous(), act).double()
+    assert ((dz[:, :F].double() - slope * big.double()).abs() <= eps * (slope * big.double()).abs() + 1e-8).all()

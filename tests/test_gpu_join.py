@@ -302,3 +302,44 @@ def test_streams_and_graphs(pk):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held, both()))
+
+
+@pytest.mark.parametrize("kept_as", ["whole", "q8"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H", [700, 3000, 8192, 9001, 17000])
+def test_gradients_in_the_place_of_every_input(pk, dtype, H, kept_as):
+    """dr and db may each take the place of any tensor that the call reads."""
+    rows = 600
+    t = tensors(rows, H, dtype, 0)
+    drop = make(pk, rows, H, 0.1, 3)
+    j = pk.join_forward(t["r"], t["b"], t["post"], t["gate"], t["pre"], SCALE, drop, EPS, checkpoint=True)
+    src = dict(dout=t["dout"], dy=t["dy"], out=j.out, b=t["b"])
+
+    def call(v, **places):
+        out, b = (v["out"], v["b"]) if kept_as == "whole" else (j.q_out, j.q_b)
+        return pk.join_backward(v["dout"], v["dy"], out, b, j.rstd_post, j.rstd_pre, t["post"], t["gate"], t["pre"], SCALE, drop,
+                                **places)
+    want = call(src)
+    names = ["dout", "dy", "out", "b"] if kept_as == "whole" else ["dout", "dy"]
+    for i, name in enumerate(names):
+        v = {k: s.clone() for k, s in src.items()}
+        d = call(v, dr=v[name], db=v[names[i - 1]])
+        assert all(torch.equal(a, b) for a, b in zip(d, want)), name
+
+
+def test_a_stream_that_wants_no_gradient(pk):
+    """dr == NULL: the other gradients, and nothing is written in its place."""
+    for H in (300, 9001):
+        rows = 50
+        t = tensors(rows, H, F32, 0)
+        j = pk.join_forward(t["r"], t["b"], t["post"], t["gate"], t["pre"], SCALE, None, EPS)
+        want = pk.join_backward(t["dout"], t["dy"], j.out, t["b"], j.rstd_post, j.rstd_pre, t["post"], t["gate"], t["pre"], SCALE)
+        db, sums = torch.empty_like(want.db), [torch.empty(H, device="cuda") for _ in range(3)]
+        ws = torch.empty(pk.join_workspace_size(rows, H), dtype=torch.uint8, device="cuda")
+        p = lambda v: v.data_ptr()
+        rc = pk.lib.join_backward(p(t["dout"]), t["dout"].stride(0), p(t["dy"]), H, p(j.out), H, None, p(t["b"]), t["b"].stride(0),
+                                  None, pk.F32, rows, H, p(t["post"]), p(t["gate"]), SCALE, None, p(t["pre"]), p(j.rstd_post),
+                                  p(j.rstd_pre), None, 0, p(db), H, *map(p, sums), 0, p(ws), ws.numel(), pk._raw_stream())
+        assert rc == 0, pk.lib.acsc_last_error()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((db, *sums), want[1:]))
