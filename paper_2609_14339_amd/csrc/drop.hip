@@ -5,7 +5,9 @@ namespace acsc {
 namespace {
 
 // A wave takes 512 columns of one row, eight a lane.  y = D(x) + residual: one
-// rounding.  The gradient is the same call on dy.
+// rounding.  The gradient is the same call on dy.  HBM bounds it: 16384 x 8192
+// bf16 with a residual 140 us, its 805 MB at 5.8 TB/s (partly from the caches);
+// the draws, four 32-bit products a pair of values, stay beneath that.
 template <typename T>
 __global__ __launch_bounds__(256) void drop_kernel(const T *x, int64_t ldx, int64_t rows, int H, Drop d, const T *res,
                                                    int64_t ldr, T *y, int64_t ldy)

@@ -1,5 +1,12 @@
 // The gated linear layer, h = act(x Wg^T + bg) (x Wu^T + bu): the entry points,
 // the sum of a cut product's pieces, and the gradient through the gate alone.
+//
+// With dh the gradient of h, and g and u the pre-activations:
+//   dg = dh u act'(g),  du = dh act(g),  dx = (dg, du) (Wg; Wu),  dW = (dg, du)^T x
+// so that with dz = (dg, du) in one tensor and the two weights in one, the rest
+// of the gradient is a linear layer's.  The bias gradient is summed from dz
+// before its rounding, in the epilogue that forms it (from the rounded dz it is
+// 1e-3 off in bf16).
 #include "lin_plan.h"
 
 namespace acsc {

@@ -169,7 +169,10 @@ __global__ __launch_bounds__(256) void lin_act_kernel(const T *dy, int64_t lddy,
 // -> 3000 (not chosen) 88 or 80; 4096 -> 14336, forward / input gradient of 12,
 // 52, 128 tokens: tiles of 32 rows bf16 29/31, 57/39, 63/57, fp32 -/56, 86/87,
 // 207/139; of 64 31/37, 31/38, 60/44, -/78, 84/83, 151/137; of 128 44/40, 46/41,
-// 46/46, -/136, 147/131, 143/137.
+// 46/46, -/136, 147/131, 143/137.  The gated product's gradient: whole tiles wait for their epilogue, the
+// pieces' sum has it spread over the card (128 x 4096 -> 14336: 63 us in whole
+// tiles of 128 x 64, 41 in two pieces of 128 x 128).  Against each tile alone
+// on twelve shapes of 256 to 14455 rows the choice is within 4% of the best.
 struct Cut {
     int rows, tile, whole, splits, per;
 };
