@@ -1267,12 +1267,12 @@ def rms_backward(dy: torch.Tensor, src: Union[torch.Tensor, Q8], rstd: torch.Ten
 
 def join_forward(r: torch.Tensor, b: torch.Tensor, post: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
                  pre: Optional[torch.Tensor] = None, scale: float = 1.0, drop: Optional[Drop] = None, eps: float = 1e-5,
-                 checkpoint: bool = False, out: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                 checkpoint: Union[bool, str] = False, out: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
                  stream=None) -> Joined:
     """out = scale r + D(gate norm(b)) and y = norm(out) for the residual stream
     r and a branch b [rows, H], in one pass.  post, pre: the gains of the norms
     of b and of out; None: no such norm (without pre, y is None).  checkpoint:
-    8-bit checkpoints of out and b too."""
+    8-bit checkpoints too, of out and b, or of "out" or "b" alone."""
     if stream is not None:
         return _on(stream, join_forward, r, b, post, gate, pre, scale, drop, eps, checkpoint, out, y)
     shape = rows, H = _two_d(r, "r")
@@ -1289,7 +1289,10 @@ def join_forward(r: torch.Tensor, b: torch.Tensor, post: Optional[torch.Tensor] 
         raise AcscError(ACSC_EINVAL, "y is given, but there is no norm after (pre)")
     rstd_post = torch.empty(rows, dtype=torch.float32, device=dev) if post is not None else None
     rstd_pre = torch.empty(rows, dtype=torch.float32, device=dev) if pre is not None else None
-    q_out, q_b = (_q8_new(rows, H, dev), _q8_new(rows, H, dev)) if checkpoint else (None, None)
+    if checkpoint not in (False, True, "out", "b"):
+        raise AcscError(ACSC_EINVAL, f"checkpoint must be a bool, 'out' or 'b', not {checkpoint!r}")
+    q_out = _q8_new(rows, H, dev) if checkpoint in (True, "out") else None
+    q_b = _q8_new(rows, H, dev) if checkpoint in (True, "b") else None
     rc = lib.join_forward(r.data_ptr(), ldr, b.data_ptr(), ldb, _dt(r), rows, H, pp, pg, scale, _drop_ref(drop), pn, eps,
                           out.data_ptr(), ldo, py, ldy, None if rstd_post is None else rstd_post.data_ptr(),
                           None if rstd_pre is None else rstd_pre.data_ptr(), None if q_out is None else _q8_ref(q_out, rows, H),

@@ -177,8 +177,10 @@ class _Join(torch.autograd.Function):
     @staticmethod
     def forward(ctx, r, b, post, gate, pre, scale: float, drop, eps: float, checkpoint: bool):
         r2, b2 = _flat(r), _flat(b)
-        j = join_forward(r2, b2, post, gate, pre, scale, drop, eps, checkpoint)
         branch = post is not None or gate is not None
+        # of what the backward pass reads
+        parts = checkpoint and {(1, 1): True, (1, 0): "out", (0, 1): "b", (0, 0): False}[pre is not None, branch]
+        j = join_forward(r2, b2, post, gate, pre, scale, drop, eps, parts)
         src_out = None if pre is None else j.q_out if checkpoint else j.out
         src_b = None if not branch else j.q_b if checkpoint else b2
         ctx.save_for_backward(post, gate, pre, j.rstd_post, j.rstd_pre, *_save(src_out), *_save(src_b))
@@ -236,9 +238,10 @@ class _GluBlock(torch.autograd.Function):
             out, _ = lin_forward(h, W2, bias2, residual=x2)
         else:
             b, _ = lin_forward(h, W2, bias2)
-            j = join_forward(x2, b, post, gate, None, scale, drop, eps, checkpoint)
+            branch = post is not None or gate is not None
+            j = join_forward(x2, b, post, gate, None, scale, drop, eps, "b" if checkpoint and branch else False)
             out, rstd_post = j.out, j.rstd_post
-            b = None if post is None and gate is None else j.q_b if checkpoint else b
+            b = None if not branch else j.q_b if checkpoint else b
         ctx.scale, ctx.drop, ctx.act = scale, drop, act
         ctx.save_for_backward(rstd, gamma, W, bias, W2, bias2, post, gate, rstd_post, *_save(q if checkpoint else x2), *_save(b),
                               *_save_pair(z))

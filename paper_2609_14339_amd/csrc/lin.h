@@ -515,13 +515,14 @@ __device__ __forceinline__ void put_tile(const Gemm &g, const f32x4 (&acc)[NA][8
 }
 
 // Tile `id` of the product's order: bands of four rows of tiles, column by
-// column, so that what an XCD's CUs read together stays in its L2.
-__device__ __forceinline__ void tile_at(const Gemm &g, int64_t id, int &tile_m, int &tile_n)
+// column, so that what an XCD's CUs read together stays in its L2.  A launch has
+// under 2^26 tiles.
+__device__ __forceinline__ void tile_at(const Gemm &g, uint32_t id, int &tile_m, int &tile_n)
 {
-    const int64_t band = id / (4 * g.tn), in = id - band * 4 * g.tn;
-    const int height = static_cast<int>(min<int64_t>(g.tm - band * 4, 4));
-    tile_m = static_cast<int>(band * 4 + in % height);
-    tile_n = static_cast<int>(in / height);
+    const uint32_t wide = 4u * g.tn, band = id / wide, in = id - band * wide, height = min(g.tm - band * 4, 4u);
+    const uint32_t col = height == 4 ? in / 4 : in / height;
+    tile_m = static_cast<int>(band * 4 + in - col * height);
+    tile_n = static_cast<int>(col);
 }
 
 }  // namespace acsc

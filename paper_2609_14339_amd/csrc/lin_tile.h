@@ -273,19 +273,19 @@ __global__ __launch_bounds__(64 * waves(TM, T), TM == 64 ? 3 : 2) void lin_tile_
     // Workgroups go to the eight XCDs in turn; each XCD takes a run of tiles
     // of its own.  First the whole tiles, then the pieces of the others, a
     // piece of each in turn.
-    int64_t id = blockIdx.x, count = g.whole, first = 0;
+    uint32_t id = blockIdx.x, count = g.whole, first = 0;
     int split = -1;
-    if (id >= g.whole) {
-        first = g.whole;
-        count = static_cast<int64_t>(g.tm) * g.tn - g.whole;
+    if (id >= count) {
+        first = count;
+        count = static_cast<uint32_t>(g.tm) * g.tn - first;
         split = static_cast<int>((id - first) / count);
-        id = (id - first) % count;
+        id = id - first - split * count;
     }
     {
-        const int64_t q = count / 8, r = count % 8, x = id % 8;
+        const uint32_t q = count / 8, r = count % 8, x = id % 8;
         id = x * q + min(x, r) + id / 8;
     }
-    float *part = split < 0 ? nullptr : g.part + (split * count + id) * TM * T;
+    float *part = split < 0 ? nullptr : g.part + (static_cast<int64_t>(split) * count + id) * TM * T;
     int tile_m, tile_n;
     tile_at(g, first + id, tile_m, tile_n);
     const int64_t m0 = static_cast<int64_t>(tile_m) * TM;

@@ -125,6 +125,11 @@ def test_join_forward(pk, dtype, rows, H, pad):
         else:                      # coded before the rounding to bf16
             v, top = pk.q8_decode(j.q_out, F32).double(), j.q_out.scales.repeat_interleave(128, 1)[:, :H].double()
             assert ((v - ref["out"]).abs() <= 0.51 * top + 100 * U * ref["size"]).all()
+        for part in ("out", "b"):
+            k = pk.join_forward(t["r"], t["b"], **kw, checkpoint=part)
+            assert (k.q_out is None) == (part == "b") and (k.q_b is None) == (part == "out")
+            q, want = (k.q_out, j.q_out) if part == "out" else (k.q_b, j.q_b)
+            assert torch.equal(q.codes, want.codes) and torch.equal(q.scales, want.scales) and torch.equal(k.out, j.out)
         k = pk.join_forward(t["r"], t["b"], **kw)
         assert torch.equal(k.out, j.out) and (k.y is None or torch.equal(k.y, j.y)) and k.q_out is k.q_b is None
 
