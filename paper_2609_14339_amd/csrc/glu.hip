@@ -232,6 +232,18 @@ inline int check_glu(int64_t rows, int n_in, int F, int dt)
     return ACSC_OK;
 }
 
+// The largest launches: of tiles, and with a checkpoint of the sum of pieces
+// that every narrow tile goes through.
+inline int check_launches(const Plan &p, bool codes)
+{
+    if (int rc = check_tiles(p))
+        return rc;
+    const int64_t groups = static_cast<int64_t>(p.tm) * ((p.tn + 1) / 2) * (p.rows * 128 / 2048);
+    ACSC_CHECK_ARG(p.few || !codes || p.tile != 128 || groups * 256 < (1ll << 32), ACSC_EINVAL,
+                   "product too large: %lld workgroups for its checkpoint", (long long)groups);
+    return ACSC_OK;
+}
+
 // The plan of a product, with the operands' copies that bits 0 (A) and 1 (B) of
 // `copies` add to those that are needed whatever the alignment.
 int plan_glu(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, bool codes, int copies, Plan &p)
@@ -244,7 +256,7 @@ int plan_glu(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, bool codes
     };
     const bool a = best(s.acol, s.acol ? s.M : s.K), b = best(s.bcol, s.bcol ? s.N : s.K);
     p = plan_of(kind, s, dt, a && !(copies & 1), b && !(copies & 2), codes);
-    return check_tiles(p);
+    return check_launches(p, codes);
 }
 
 // Partials of the column sums: of a cut tile, one for each workgroup of its
@@ -365,7 +377,7 @@ extern "C" int glu_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t r
     g.B = {W, ld_w};
     const Shape s = shape_of(kGluForward, rows, n_in, F);
     const Plan p = plan_of(kGluForward, s, dt, readable(g.A, false, n_in, dt), readable(g.B, false, n_in, dt), q_gate != nullptr);
-    if (int rc = check_tiles(p))
+    if (int rc = check_launches(p, q_gate != nullptr))
         return rc;
     if (int rc = check_ws(ws, ws_bytes, p.bytes()))
         return rc;

@@ -134,6 +134,10 @@ def test_plans_and_workspaces(pk):
         assert pk.lib.glu_workspace_size(op, 4, 64, 64, 1, 0, None) == EINVAL
         assert pk.lib.glu_workspace_size_unaligned(op, 40, 65, 63, 1, 0, C.byref(b)) == 0 and b.value > 0
     assert pk.lib.glu_workspace_size(2, 4, 64, 64, 1, 0, C.byref(b)) == EINVAL
+    # launches of 2^32 threads and more: of tiles, and of the sum that a checkpoint's narrow tiles go through
+    for dt, rows, Fh, extra in ((1, 1 << 30, 1 << 20, 0), (1, 1 << 30, 1 << 20, 1), (0, 1 << 26, 1 << 10, 1)):
+        assert pk.lib.glu_workspace_size(0, rows, 64, Fh, dt, extra, C.byref(b)) == EINVAL and "too large" in err(pk)
+    assert pk.lib.glu_workspace_size(0, 1 << 26, 64, 1 << 10, 0, 0, C.byref(b)) == 0
     bf, f32 = torch.bfloat16, torch.float32
     assert pk.glu_product_plan(0, 1, 4096, 14336, bf)[:2] == (0, 0)
     for rows, n_in, Fh, dt in ((8192, 8192, 28672, bf), (300, 1243, 90, bf), (8452, 706, 225, f32), (20, 450, 150, f32)):
