@@ -224,6 +224,13 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
     const int t = threadIdx.x % NT;
     const int sub = RPB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
     const bool branch = JOIN && (p.post || p.gate);     // whether the formula reads b
+    // one chunk leaves room for what two form again from the stored words (fp32 of
+    // 1024 threads does not: 21834 x 64 bf16 and 8192 x 8192 fp32 with what was
+    // formed 29.5 and 392 us, formed again 33.6 and 348)
+    const auto keep = [](auto &w) {
+        if (CH > 1 || !AHEAD)
+            again(w);
+    };
     float s2[CH][8], s1[CH][8];
     Raw8<T> pre[CH], post[CH], gate[CH];
     const auto load_gains = [&]() {
@@ -286,7 +293,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
             float s[1] = {0.f};
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                again(pre[c].w);
+                keep(pre[c].w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float h = cur.x[c].at(i) * rs, d = cur.dy[c].at(i), g = p.pre ? d * pre[c].at(i) : d;
@@ -298,9 +305,9 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
             const float m = s[0] / p.H;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                again(cur.x[c].x.w);
-                again(cur.dy[c].w);
-                again(pre[c].w);
+                keep(cur.x[c].x.w);
+                keep(cur.dy[c].w);
+                keep(pre[c].w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float h = cur.x[c].at(i) * rs, d = cur.dy[c].at(i), g = p.pre ? d * pre[c].at(i) : d;
@@ -338,13 +345,12 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
         if (branch)
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const int left = p.H - (c * NT + t) * 8;
-                again(post[c].w);
-                again(gate[c].w);
+                keep(post[c].w);
+                keep(gate[c].w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float h = cur.b[c].at(i) * rs;
-                    s1[c][i] += left > i ? v[c][i] * h : 0.f;
+                    s1[c][i] += v[c][i] * h;          // past the end of the row nobody takes it
                     if (p.gate)
                         v[c][i] *= gate[c].at(i);
                     if (p.post)
@@ -360,7 +366,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * NT + t) * 8, left = p.H - col;
-            again(cur.b[c].x.w);
+            keep(cur.b[c].x.w);
             if (left <= 0)
                 continue;
             if (p.post)

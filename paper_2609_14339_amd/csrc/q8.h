@@ -40,9 +40,6 @@ inline int check_act(int act)
     return ACSC_OK;
 }
 
-__device__ __forceinline__ float to_float(uint16_t x) { return bf16_to_f32(x); }
-__device__ __forceinline__ float to_float(float x) { return x; }
-
 struct __attribute__((packed, aligned(1))) C8Any {
     uint32_t w[2];
 };
