@@ -211,9 +211,9 @@ struct Src {
 //   dpre = sum of dy h2,   s = sum of u h1, dgate = s post, dpost = s gate
 // A workgroup walks rows blockIdx.x, + gridDim.x, ... (four at a time where a
 // wave holds a row) and keeps both column sums in registers; its waves' sums
-// meet in LDS in wave order, and every workgroup leaves one partial.  AHEAD:
-// the next row's loads leave before a row is worked on, and the gains stay in
-// registers (16384 x 4096 bf16 167 us; 233 without either).  Sums of a row's
+// meet in LDS in wave order, and every workgroup leaves one partial.  The gains
+// stay in registers, and, AHEAD, the next row's loads leave before a row is
+// worked on (16384 x 4096 bf16 167 us; 233 without either).  Sums of a row's
 // terms and of columns are fp32; dr and db are rounded once, from t.
 template <typename T, int NT, int CH, bool JOIN, bool KEPT, bool AHEAD>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_backward_kernel(Bwd<T> p)
@@ -224,29 +224,24 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
     const int t = threadIdx.x % NT;
     const int sub = RPB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
     const bool branch = JOIN && (p.post || p.gate);     // whether the formula reads b
-    // one chunk leaves room for what two form again from the stored words (fp32 of
-    // 1024 threads does not: 21834 x 64 bf16 and 8192 x 8192 fp32 with what was
-    // formed 29.5 and 392 us, formed again 33.6 and 348)
+    // one chunk leaves room for what two form again from the stored words (21834 x
+    // 64 bf16 29.5 us, formed again 33.6), but in the 128 registers of 1024 threads
     const auto keep = [](auto &w) {
         if (CH > 1 || !AHEAD)
             again(w);
     };
     float s2[CH][8], s1[CH][8];
     Raw8<T> pre[CH], post[CH], gate[CH];
-    const auto load_gains = [&]() {
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int col = (c * NT + t) * 8, left = p.H - col;
-            if (p.pre)
-                load_raw(p.pre + col, left, pre[c]);
-            if (JOIN && p.post)
-                load_raw(p.post + col, left, post[c]);
-            if (JOIN && p.gate)
-                load_raw(p.gate + col, left, gate[c]);
-        }
-    };
-    if (AHEAD)
-        load_gains();
+    for (int c = 0; c < CH; ++c) {
+        const int col = (c * NT + t) * 8, left = p.H - col;
+        if (p.pre)
+            load_raw(p.pre + col, left, pre[c]);
+        if (JOIN && p.post)
+            load_raw(p.post + col, left, post[c]);
+        if (JOIN && p.gate)
+            load_raw(p.gate + col, left, gate[c]);
+    }
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -285,7 +280,6 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
                 load(next, row + stride);
         } else {
             load(cur, row);
-            load_gains();
         }
         float v[CH][8];
         if (p.dy) {
