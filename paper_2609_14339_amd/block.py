@@ -60,6 +60,12 @@ def _load_pair(t):
     return t[0] if t[1] is None else (Q8(t[0], t[1]), Q8(t[2], t[3]))
 
 
+def _keep(checkpoint, *ts):
+    """How an op keeps what its backward pass reads: in 8 bits (True), whole
+    (False), or not at all (None), where no gradient is wanted."""
+    return bool(checkpoint) if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in ts) else None
+
+
 def _as(t, like):
     return None if t is None or like is None else t.to(like.dtype)
 
@@ -145,10 +151,11 @@ class _MlpBlock(torch.autograd.Function):
 
 class _RmsNorm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, gamma, eps: float, checkpoint: bool):
+    def forward(ctx, x, gamma, eps: float, keep):
         x2 = _flat(x)
-        y, rstd, q = rms_forward(x2, gamma, eps, checkpoint=checkpoint)
-        ctx.save_for_backward(rstd, gamma, *_save(q if checkpoint else x2))
+        y, rstd, q = rms_forward(x2, gamma, eps, checkpoint=bool(keep))
+        if keep is not None:
+            ctx.save_for_backward(rstd, gamma, *_save(q if keep else x2))
         return y.view(x.shape)
 
     @staticmethod
@@ -175,15 +182,16 @@ class _Dropout(torch.autograd.Function):
 
 class _Join(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, r, b, post, gate, pre, scale: float, drop, eps: float, checkpoint: bool):
+    def forward(ctx, r, b, post, gate, pre, scale: float, drop, eps: float, keep):
         r2, b2 = _flat(r), _flat(b)
         branch = post is not None or gate is not None
         # of what the backward pass reads
-        parts = checkpoint and {(1, 1): True, (1, 0): "out", (0, 1): "b", (0, 0): False}[pre is not None, branch]
+        parts = bool(keep) and {(1, 1): True, (1, 0): "out", (0, 1): "b", (0, 0): False}[pre is not None, branch]
         j = join_forward(r2, b2, post, gate, pre, scale, drop, eps, parts)
-        src_out = None if pre is None else j.q_out if checkpoint else j.out
-        src_b = None if not branch else j.q_b if checkpoint else b2
-        ctx.save_for_backward(post, gate, pre, j.rstd_post, j.rstd_pre, *_save(src_out), *_save(src_b))
+        if keep is not None:
+            src_out = None if pre is None else j.q_out if keep else j.out
+            src_b = None if not branch else j.q_b if keep else b2
+            ctx.save_for_backward(post, gate, pre, j.rstd_post, j.rstd_pre, *_save(src_out), *_save(src_b))
         ctx.scale, ctx.drop, ctx.shapes = scale, drop, (r.shape, b.shape)
         ctx.set_materialize_grads(False)
         out = j.out.view(r.shape)
@@ -202,13 +210,17 @@ class _Join(torch.autograd.Function):
                 None, None, None, None)
 
 
+_GLU_KEEP = {True: "q8", False: "z", None: None}
+
+
 class _Glu(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, W, bias, act: str, checkpoint: bool):
+    def forward(ctx, x, W, bias, act: str, keep):
         x2 = _flat(x)
-        h, z = glu_forward(x2, W, bias, act, keep="q8" if checkpoint else "z")
+        h, z = glu_forward(x2, W, bias, act, _GLU_KEEP[keep])
         ctx.act = act
-        ctx.save_for_backward(x2, W, bias, *_save_pair(z))
+        if keep is not None:
+            ctx.save_for_backward(x2, W, bias, *_save_pair(z))
         return h.view(*x.shape[:-1], h.shape[1])
 
     @staticmethod
@@ -228,10 +240,10 @@ class _Glu(torch.autograd.Function):
 
 class _GluBlock(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, gamma, W, bias, W2, bias2, post, gate, scale: float, drop, act: str, eps: float, checkpoint: bool):
+    def forward(ctx, x, gamma, W, bias, W2, bias2, post, gate, scale: float, drop, act: str, eps: float, keep):
         x2 = _flat(x)
-        y, rstd, q = rms_forward(x2, gamma, eps, checkpoint=checkpoint)
-        h, z = glu_forward(y, W, bias, act, keep="q8" if checkpoint else "z")
+        y, rstd, q = rms_forward(x2, gamma, eps, checkpoint=bool(keep))
+        h, z = glu_forward(y, W, bias, act, _GLU_KEEP[keep])
         ctx.plain = post is None and gate is None and drop is None and scale == 1.0
         rstd_post = b = None
         if ctx.plain:
@@ -239,12 +251,13 @@ class _GluBlock(torch.autograd.Function):
         else:
             b, _ = lin_forward(h, W2, bias2)
             branch = post is not None or gate is not None
-            j = join_forward(x2, b, post, gate, None, scale, drop, eps, "b" if checkpoint and branch else False)
+            j = join_forward(x2, b, post, gate, None, scale, drop, eps, "b" if keep and branch else False)
             out, rstd_post = j.out, j.rstd_post
-            b = None if not branch else j.q_b if checkpoint else b
+            b = None if not branch else j.q_b if keep else b
         ctx.scale, ctx.drop, ctx.act = scale, drop, act
-        ctx.save_for_backward(rstd, gamma, W, bias, W2, bias2, post, gate, rstd_post, *_save(q if checkpoint else x2), *_save(b),
-                              *_save_pair(z))
+        if keep is not None:
+            ctx.save_for_backward(rstd, gamma, W, bias, W2, bias2, post, gate, rstd_post, *_save(q if keep else x2), *_save(b),
+                                  *_save_pair(z))
         return out.view(x.shape)
 
     @staticmethod
@@ -293,7 +306,7 @@ def mlp_block(x, gamma, beta, W1, b1, W2, b2, act: str = "gelu", eps: float = 1e
 
 def rms_norm(x, gamma=None, eps: float = 1e-5, checkpoint: bool = False):
     """Root-mean-square norm over the last dimension; checkpoint keeps x in 8 bits."""
-    return _RmsNorm.apply(x, gamma, float(eps), bool(checkpoint))
+    return _RmsNorm.apply(x, gamma, float(eps), _keep(checkpoint, x, gamma))
 
 
 def dropout(x, drop, residual=None):
@@ -305,13 +318,13 @@ def join(r, b, post=None, gate=None, pre=None, scale: float = 1.0, drop=None, ep
     """Between two blocks: out = scale r + D(gate norm(b)), with post the gains
     of the norm (None: b as it is); with pre, (out, norm(out)), the input of the
     next block, from the same pass.  checkpoint keeps out and b in 8 bits."""
-    return _Join.apply(r, b, post, gate, pre, float(scale), drop, float(eps), bool(checkpoint))
+    return _Join.apply(r, b, post, gate, pre, float(scale), drop, float(eps), _keep(checkpoint, r, b, post, gate, pre))
 
 
 def glu(x, W, bias=None, act: str = "silu", checkpoint: bool = False):
     """act(x Wg^T + bg) (x Wu^T + bu), W [2 F, H] with Wg's rows first;
     checkpoint keeps the pre-activations in 8 bits."""
-    return _Glu.apply(x, W, bias, act, bool(checkpoint))
+    return _Glu.apply(x, W, bias, act, _keep(checkpoint, x, W, bias))
 
 
 def glu_block(x, gamma, W, bias, W2, bias2, post=None, gate=None, scale: float = 1.0, drop=None, act: str = "silu",
@@ -319,4 +332,5 @@ def glu_block(x, gamma, W, bias, W2, bias2, post=None, gate=None, scale: float =
     """scale x + D(gate norm(W2 h + bias2)), h = glu(norm(x)), for x [..., H],
     W [2 F, H], W2 [H, F].  gamma, post: the gains of the norms before and after
     (post None: no norm after); biases, gate and drop may be None."""
-    return _GluBlock.apply(x, gamma, W, bias, W2, bias2, post, gate, float(scale), drop, act, float(eps), bool(checkpoint))
+    return _GluBlock.apply(x, gamma, W, bias, W2, bias2, post, gate, float(scale), drop, act, float(eps),
+                           _keep(checkpoint, x, gamma, W, bias, W2, bias2, post, gate))
