@@ -715,7 +715,8 @@ int glu_product_plan(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, in
  *          their fp32 values; both or none.
  * h and z overlap neither x nor W nor each other.  Arithmetic and limits as
  * lin_forward, with 1 <= F <= 2^21; h is formed from the fp32 g and u and
- * rounded once. */
+ * rounded once.  What is kept may cut the sums another way: h is the same in
+ * every call that keeps the same, and within the fp32 sums' error otherwise. */
 int glu_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t rows, int n_in, int F, const void *W, int64_t ld_w,
                 const void *bias, acsc_act act, void *h, int64_t ld_h, void *z, int64_t ld_z, const q8_tensor *q_gate,
                 const q8_tensor *q_up, void *ws, size_t ws_bytes, hipStream_t stream);
