@@ -345,35 +345,59 @@ __device__ __forceinline__ void glu_bias(const Epi &e, int F, int n, float (&bg)
 
 // The gated product's gradient: eight columns of row m of dh = C through the
 // epilogue, from kept g and u.  sg, su: what is added to their column sums.
+// Kept values as they are stored, of either form in the same registers (in two
+// sets of their own 8192 x 4096 -> 14336 from codes took 878 us, 868 so).
 template <typename T>
 struct GluBeside {
-    Beside<T> g, u;
+    static constexpr int W = sizeof(T) * 2;
+    uint32_t g[W], u[W];
+    float sg, su;
 };
 template <typename T>
 __device__ __forceinline__ void load_glu_beside(const Epi &e, int F, GluBeside<T> &b, const GluAt<T> &at, int left)
 {
     GluBeside<T> r = {};
     if (e.q.codes) {
-        load_raw(at.cg, left, r.g.codes);
-        load_raw(at.cu, left, r.u.codes);
-        r.g.scale = left > 0 ? *at.sg : 0.f;
-        r.u.scale = left > 0 ? *at.su : 0.f;
+        Codes8 c;
+        load_raw(at.cg, left, c);
+        __builtin_memcpy(r.g, &c, sizeof c);
+        load_raw(at.cu, left, c);
+        __builtin_memcpy(r.u, &c, sizeof c);
+        r.sg = left > 0 ? *at.sg : 0.f;
+        r.su = left > 0 ? *at.su : 0.f;
     } else {
-        load_raw(at.z, left, r.g.v);
-        load_raw(at.z + F, left, r.u.v);
+        Raw8<T> v;
+        load_raw(at.z, left, v);
+        __builtin_memcpy(r.g, &v, sizeof v);
+        load_raw(at.z + F, left, v);
+        __builtin_memcpy(r.u, &v, sizeof v);
     }
     b = r;
+}
+template <typename T>
+__device__ __forceinline__ void kept_values(const uint32_t (&w)[GluBeside<T>::W], bool codes, float scale, float (&v)[8])
+{
+    Codes8 c;
+    Raw8<T> r;
+    __builtin_memcpy(&c, w, sizeof c);
+    __builtin_memcpy(&r, w, sizeof r);
+    if (codes) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = code_value(c.at(i), scale);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = r.at(i);
+    }
 }
 template <typename T>
 __device__ __forceinline__ void glu_gate_epilogue(const Epi &e, int F, const float (&v)[8], const GluBeside<T> &b,
                                                   const GluAt<T> &at, int left, float (&sg)[8], float (&su)[8])
 {
     float g[8], u[8], a[8], s[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        g[i] = e.q.codes ? code_value(b.g.codes.at(i), b.g.scale) : b.g.v.at(i);
-        u[i] = e.q.codes ? code_value(b.u.codes.at(i), b.u.scale) : b.u.v.at(i);
-    }
+    kept_values<T>(b.g, e.q.codes != nullptr, b.sg, g);
+    kept_values<T>(b.u, e.q.codes != nullptr, b.su, u);
     act_both<T>(g, e.act, a, s);
     if (e.hidden) {
         float h[8];
