@@ -59,6 +59,16 @@ __device__ __forceinline__ void put_codes(const Q8 &q, int64_t row, int col, int
     }
 }
 
+// Zeros in the place of values past a row's end, which a norm's NaN (0 rho) has
+// made NaN: they share sums and groups with values that exist.
+__device__ __forceinline__ void clear_past(float (&v)[8], int left)
+{
+    if (left < 8)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = i < left ? v[i] : 0.f;
+}
+
 // NT threads a row; workgroups of max(NT, 256) threads.  JOIN: with a branch b;
 // AGAIN: y from a kept rho2.  y is taken from out before it is rounded.
 template <typename T, int NT, int CH, bool JOIN, bool AGAIN>
@@ -113,6 +123,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void join_forward_kernel(Fwd<T
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     v[c][i] = v[c][i] * rs * w[i];
+                clear_past(v[c], left);
             }
             if (p.gate) {
                 load8(p.gate + col, left, w);
@@ -307,6 +318,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
                     const float h = cur.x[c].at(i) * rs, d = cur.dy[c].at(i), g = p.pre ? d * pre[c].at(i) : d;
                     v[c][i] = cur.dout[c].at(i) + rs * (g - h * m);
                 }
+                clear_past(v[c], p.H - (c * NT + t) * 8);
             }
         } else {
 #pragma unroll
@@ -496,10 +508,14 @@ __global__ __launch_bounds__(1024, 4) void join_backward_wide_kernel(Bwd<T> p)
                     w[i] = b.at(i) * r1;
                 times(p.gate, col, left, w);
                 times(p.post, col, left, w);   // zeros past the end of the row
-                if (p.drop.below)
+                if (p.drop.below) {
                     drop8(p.drop, d, col, v);
-                if (p.drop.below && after_mean)
+                    clear_past(v, left);
+                }
+                if (p.drop.below && after_mean) {
                     drop8(p.drop, d, col, h);
+                    clear_past(h, left);
+                }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     s[1] += v[i] * w[i];
@@ -508,7 +524,8 @@ __global__ __launch_bounds__(1024, 4) void join_backward_wide_kernel(Bwd<T> p)
             }
             row_sum<1024>(s, slots[flip]);
             m2 = s[0] / p.H;
-            m1 = (s[1] - r2 * m2 * s[2]) / p.H;
+            // no h2 that counts: of a row that is dropped whole, whose m2 may be NaN
+            m1 = (s[2] == 0.f ? s[1] : s[1] - r2 * m2 * s[2]) / p.H;
         }
         // eight columns of t, with dy h2 for the column sums
         const auto whole = [&](int col, int left, float (&v)[8]) {
