@@ -60,7 +60,8 @@ __device__ __forceinline__ void put_codes(const Q8 &q, int64_t row, int col, int
 }
 
 // Zeros in the place of values past a row's end, which a norm's NaN (0 rho) has
-// made NaN: they share sums and groups with values that exist.
+// made NaN: they share sums and groups with values that exist, of which the mask
+// may have kept none (without one the row is NaN throughout).
 __device__ __forceinline__ void clear_past(float (&v)[8], int left)
 {
     if (left < 8)
@@ -123,7 +124,6 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void join_forward_kernel(Fwd<T
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     v[c][i] = v[c][i] * rs * w[i];
-                clear_past(v[c], left);
             }
             if (p.gate) {
                 load8(p.gate + col, left, w);
@@ -131,8 +131,10 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void join_forward_kernel(Fwd<T
                 for (int i = 0; i < 8; ++i)
                     v[c][i] *= w[i];
             }
-            if (p.drop.below)
+            if (p.drop.below) {
                 drop8(p.drop, d, col, v[c]);
+                clear_past(v[c], left);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 v[c][i] = __builtin_fmaf(p.scale, r[c].at(i), v[c][i]);
@@ -318,7 +320,6 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
                     const float h = cur.x[c].at(i) * rs, d = cur.dy[c].at(i), g = p.pre ? d * pre[c].at(i) : d;
                     v[c][i] = cur.dout[c].at(i) + rs * (g - h * m);
                 }
-                clear_past(v[c], p.H - (c * NT + t) * 8);
             }
         } else {
 #pragma unroll
@@ -343,8 +344,10 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 2 : 1) void join_b
         if (p.drop.below) {
             const DropRow d = drop_row(p.drop, row);
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
+            for (int c = 0; c < CH; ++c) {
                 drop8(p.drop, d, (c * NT + t) * 8, v[c]);
+                clear_past(v[c], p.H - (c * NT + t) * 8);
+            }
         }
         const float rs = cur.post;
         float s[1] = {0.f};
