@@ -1073,7 +1073,7 @@ extern "C" int join_backward(const void *dout, int64_t ld_dout, const void *dy, 
     ACSC_CHECK_ARG(!post || rows == 0 || rstd_post, ACSC_EINVAL, "null pointer rstd_post");
     ACSC_CHECK_ARG(post || !dpost, ACSC_EINVAL, "dpost without post");
     ACSC_CHECK_ARG(gate || !dgate, ACSC_EINVAL, "dgate without gate");
-    ACSC_CHECK_ARG(!(out && dy && q_b) && !(b && (post || gate) && q_out && dy), ACSC_EINVAL,
+    ACSC_CHECK_ARG(!dy || (!post && !gate) || (!(out && q_b) && !(b && q_out)), ACSC_EINVAL,
                    "out and b must both be tensors or both be checkpoints");
     for (const Mat *m : {&a.dout, &a.dy, &a.out, &a.b, &a.dr})
         if (m->p)

@@ -69,3 +69,17 @@ def test_a_wide_row_that_is_dropped_whole(pk, dtype, H):
     t["dy"][:, 0] = NAN
     d = pk.join_backward(t["dout"], t["dy"], j.out, t["b"], j.rstd_post, j.rstd_pre, t["post"], t["gate"], t["pre"], SCALE, drop)
     assert (d.db[whole] == 0).all() and torch.isnan(d.dr).all() and torch.isnan(d.db[~whole]).all()
+
+
+def test_a_source_of_the_other_form_that_is_not_read(pk):
+    """A tensor beside a checkpoint, of which the formula reads one: the other has no say."""
+    rows, H = 50, 300
+    t = tensors(rows, H, F32, 0)
+    q = pk.q8_encode(t["b"])
+    j = pk.join_forward(t["r"], t["b"], None, None, t["pre"], SCALE, None, EPS)
+    want = pk.join_backward(t["dout"], t["dy"], j.out, None, None, j.rstd_pre, pre=t["pre"], scale=SCALE)
+    got = pk.join_backward(t["dout"], t["dy"], j.out, q, None, j.rstd_pre, pre=t["pre"], scale=SCALE)
+    assert all(torch.equal(a, b) for a, b in zip(got, want) if b is not None)
+    want = pk.join_backward(t["dout"], None, None, t["b"], gate=t["gate"], scale=SCALE)
+    got = pk.join_backward(t["dout"], None, q, t["b"], gate=t["gate"], scale=SCALE)
+    assert all(torch.equal(a, b) for a, b in zip(got, want) if b is not None)
