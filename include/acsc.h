@@ -726,12 +726,20 @@ int glu_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t rows, int n_
  * [rows, ld_h] of dt or NULL: receives act(g) u again.  dz may equal z, and h
  * dh (with its row stride).  With dz, the layer's other gradients are those of
  * a linear layer with the weights W: lin_backward_input and
- * lin_backward_weight with 2 F outputs (its db sums the rounded dz). */
+ * lin_backward_weight with 2 F outputs (its db sums the rounded dz;
+ * glu_backward_act_bias the unrounded). */
 int glu_backward_act(const void *dh, int64_t ld_dh, const void *z, int64_t ld_z, const q8_tensor *q_gate,
                      const q8_tensor *q_up, acsc_dtype dt, int64_t rows, int F, acsc_act act, void *dz, int64_t ld_dz, void *h,
                      int64_t ld_h, hipStream_t stream);
 
-/* The same with dh = dy W of the linear layer behind (W [n_out, F]), in the
+/* The same, and dbias as glu_backward_input has it (device fp32 [2 F], not
+ * NULL); the bytes of workspace that it needs. */
+int glu_bias_workspace_size(int64_t rows, int F, size_t *bytes);
+int glu_backward_act_bias(const void *dh, int64_t ld_dh, const void *z, int64_t ld_z, const q8_tensor *q_gate,
+                          const q8_tensor *q_up, acsc_dtype dt, int64_t rows, int F, acsc_act act, void *dz, int64_t ld_dz,
+                          void *h, int64_t ld_h, float *dbias, int accumulate, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* glu_backward_act with dh = dy W of the linear layer behind (W [n_out, F]), in the
  * epilogue of that product; dh is not written.  dz may equal z; dz and h
  * overlap neither dy nor W.
  * dbias    device fp32 [2 F] or NULL: (+)= sum over rows of dz before its

@@ -213,6 +213,8 @@ def _load():
             ("glu_product_plan", [i32, i64, i32, i32, i32, i32, C.POINTER(_LinPlan)]),
             ("glu_forward", [vp, i64, i32, i64, i32, i32, vp, i64, vp, i32, vp, i64, vp, i64, qp, qp, vp, sz, vp]),
             ("glu_backward_act", [vp, i64, vp, i64, qp, qp, i32, i64, i32, i32, vp, i64, vp, i64, vp]),
+            ("glu_bias_workspace_size", [i64, i32, C.POINTER(sz)]),
+            ("glu_backward_act_bias", [vp, i64, vp, i64, qp, qp, i32, i64, i32, i32, vp, i64, vp, i64, vp, i32, vp, sz, vp]),
             ("glu_backward_input", [vp, i64, i32, i64, i32, i32, vp, i64, i32, vp, i64, qp, qp, vp, i64, vp, i64, vp, i32, vp, sz, vp])):
         fn = getattr(lib, name)
         fn.restype = i32
@@ -241,7 +243,7 @@ EXPORTED = ("acsc_last_error", "acsc_version", "acsc_stats_enable", "acsc_stats_
             "lin_backward_input", "lin_backward_weight",
             "drop_apply", "rms_forward", "rms_recompute", "rms_backward", "join_workspace_size", "join_forward", "join_backward",
             "glu_workspace_size", "glu_workspace_size_unaligned", "glu_product_plan", "glu_forward", "glu_backward_act",
-            "glu_backward_input")
+            "glu_bias_workspace_size", "glu_backward_act_bias", "glu_backward_input")
 
 
 def _check(rc: int):
@@ -1437,14 +1439,9 @@ def glu_forward(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
     return h, kept
 
 
-def glu_backward_act(dh: torch.Tensor, z, act: str = "silu", hidden: bool = False, dz: Optional[torch.Tensor] = None,
-                     h: Optional[torch.Tensor] = None, stream=None):
-    """(dz [rows, 2 F], h) of glu_forward from dh [rows, F] and what it kept; h,
-    the hidden activation again, if hidden (or if it is given), else None."""
-    if stream is not None:
-        return _on(stream, glu_backward_act, dh, z, act, hidden, dz, h)
+def _act_args(dh: torch.Tensor, z, act: str, hidden: bool, dz: Optional[torch.Tensor], h: Optional[torch.Tensor]):
+    """What the gradient of a given dh is asked for: (dz, h, the call's arguments up to h's row stride)."""
     rows, F = _two_d(dh, "dh")
-    _here(dh, *_flat_kept(z), dz, h)
     dtype, dev = dh.dtype, dh.device
     lddh = _rows(dh, (rows, F), dtype, "dh")
     pz, ldz, qg, qu = _kept_pair(z, rows, F, dtype)
@@ -1453,11 +1450,53 @@ def glu_backward_act(dh: torch.Tensor, z, act: str = "silu", hidden: bool = Fals
     if hidden or h is not None:
         h, ldh = _new(h, (rows, F), dtype, dev, "h")
         ph = h.data_ptr()
-    rc = lib.glu_backward_act(dh.data_ptr(), lddh, pz, ldz, qg, qu, _dt(dh), rows, F, _act(act), dz.data_ptr(), lddz, ph, ldh,
-                              _raw_stream())
+    return dz, h, (dh.data_ptr(), lddh, pz, ldz, qg, qu, _dt(dh), rows, F, _act(act), dz.data_ptr(), lddz, ph, ldh)
+
+
+def glu_backward_act(dh: torch.Tensor, z, act: str = "silu", hidden: bool = False, dz: Optional[torch.Tensor] = None,
+                     h: Optional[torch.Tensor] = None, stream=None):
+    """(dz [rows, 2 F], h) of glu_forward from dh [rows, F] and what it kept; h,
+    the hidden activation again, if hidden (or if it is given), else None."""
+    if stream is not None:
+        return _on(stream, glu_backward_act, dh, z, act, hidden, dz, h)
+    _two_d(dh, "dh")
+    _here(dh, *_flat_kept(z), dz, h)
+    dz, h, args = _act_args(dh, z, act, hidden, dz, h)
+    rc = lib.glu_backward_act(*args, _raw_stream())
     if rc:
         _check(rc)
     return dz, h
+
+
+def glu_bias_workspace_size(rows: int, F: int) -> int:
+    """Bytes for glu_backward_act_bias."""
+    b = C.c_size_t(0)
+    _check(lib.glu_bias_workspace_size(rows, F, C.byref(b)))
+    return b.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _glu_bias_bytes(rows: int, F: int) -> int:
+    return glu_bias_workspace_size(rows, F)
+
+
+def glu_backward_act_bias(dh: torch.Tensor, z, act: str = "silu", hidden: bool = False, dz: Optional[torch.Tensor] = None,
+                          h: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None, accumulate: bool = False,
+                          ws: Optional[torch.Tensor] = None, stream=None):
+    """glu_backward_act with the bias gradient: (dz, h, dbias), dbias the fp32
+    [2 F] sums of the unrounded dz; with accumulate it is given and added to."""
+    if stream is not None:
+        return _on(stream, glu_backward_act_bias, dh, z, act, hidden, dz, h, dbias, accumulate, ws)
+    rows, F = _two_d(dh, "dh")
+    _here(dh, *_flat_kept(z), dz, h, dbias, ws)
+    dz, h, args = _act_args(dh, z, act, hidden, dz, h)
+    dbias = _sums(dbias, True, 2 * F, accumulate, dh.device, "dbias")
+    pdb = _vec(dbias, 2 * F, torch.float32, "dbias")
+    wp, wn, hold = _ws(_glu_bias_bytes(rows, F), ws, dh.device)
+    rc = lib.glu_backward_act_bias(*args, pdb, int(accumulate), wp, wn, _raw_stream())
+    if rc:
+        _check(rc)
+    return dz, h, dbias
 
 
 def glu_backward_input(dy: torch.Tensor, W: torch.Tensor, z, act: str = "silu", hidden: bool = False, bias: bool = False,

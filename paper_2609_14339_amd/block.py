@@ -32,7 +32,7 @@ from __future__ import annotations
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import (Q8, drop_apply, glu_backward_act, glu_backward_input, glu_forward, join_backward, join_forward,
+from . import (Q8, drop_apply, glu_backward_act, glu_backward_act_bias, glu_backward_input, glu_forward, join_backward, join_forward,
                lin_backward_act, lin_backward_input, lin_backward_weight, lin_forward, ln_backward, ln_forward, ln_recompute,
                rms_backward, rms_forward, rms_recompute)
 
@@ -230,11 +230,14 @@ class _Glu(torch.autograd.Function):
         need = ctx.needs_input_grad
         dx = dW = db = None
         if any(need[:3]):
-            dz, _ = glu_backward_act(_flat(g), _load_pair(kept), ctx.act)
+            if need[2]:
+                dz, _, db = glu_backward_act_bias(_flat(g), _load_pair(kept), ctx.act)
+            else:
+                dz, _ = glu_backward_act(_flat(g), _load_pair(kept), ctx.act)
             if need[0]:
                 dx = lin_backward_input(dz, W).view(*g.shape[:-1], W.shape[1])
-            if need[1] or need[2]:
-                dW, db = lin_backward_weight(dz, x2, bias=need[2])
+            if need[1]:
+                dW, _ = lin_backward_weight(dz, x2, bias=False)
         return dx, dW, _as(db, bias), None, None
 
 

@@ -173,6 +173,60 @@ __global__ __launch_bounds__(256) void glu_act_kernel(const T *dh, int64_t lddh,
     }
 }
 
+// The same with the column sums of both halves before their rounding: a
+// workgroup takes 512 columns of `per` rows, every fourth row a wave; its waves
+// meet in LDS in order and it leaves one partial, [2][F], or the result where
+// there is one workgroup along the rows.  HBM bounds it: 8192 x 14336 bf16, z
+// kept, 250 us with the partials' sum, 4.7 TB/s (205 without sums, partly from
+// the caches, and 68 for those of the rounded dz in a pass of their own).
+template <typename T>
+__global__ __launch_bounds__(256) void glu_act_sums_kernel(const T *dh, int64_t lddh, int64_t rows, int F, Epi e, int64_t per,
+                                                           int accumulate)
+{
+    __shared__ float meet[4][2][512];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int col = blockIdx.x * 512 + lane * 8, left = F - col;
+    const int64_t end = min(rows, (blockIdx.y + static_cast<int64_t>(1)) * per);
+    float sg[8] = {}, su[8] = {};
+    if (left > 0)
+        for (int64_t row = blockIdx.y * per + wave; row < end; row += 4) {
+            float v[8];
+            load8(dh + row * lddh + col, left, v);
+            GluBeside<T> beside;
+            const GluAt<T> at(e, row, col);
+            load_glu_beside<T>(e, F, beside, at, left);
+            glu_gate_epilogue<T>(e, F, v, beside, at, left, sg, su);
+        }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        // consecutive lanes in consecutive banks
+        meet[wave][0][i * 64 + lane] = sg[i];
+        meet[wave][1][i * 64 + lane] = su[i];
+    }
+    __syncthreads();
+    float *out = e.sums + blockIdx.y * static_cast<int64_t>(2) * F;
+    for (int c = threadIdx.x; c < 1024; c += 256) {
+        const int half = c / 512, k = c % 512, at = (k & 7) * 64 + (k >> 3), n = blockIdx.x * 512 + k;
+        if (n < F) {
+            const float s = ((meet[0][half][at] + meet[1][half][at]) + meet[2][half][at]) + meet[3][half][at];
+            float *to = out + static_cast<int64_t>(half) * F + n;
+            *to = accumulate ? *to + s : s;
+        }
+    }
+}
+
+// Partials of those sums: about eight workgroups a CU, of 16 rows at least; and their bytes.
+inline int act_partials(int64_t rows, int F)
+{
+    const int segs = (F + 511) / 512;
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((rows + 15) / 16, 2048 / segs)));
+}
+inline size_t act_bytes(int64_t rows, int F)
+{
+    const int parts = act_partials(rows, F);
+    return parts > 1 ? up256(static_cast<size_t>(parts) * 2 * F * sizeof(float)) : 0;
+}
+
 template <typename TO, int TM, int T>
 void launch_join(const Gemm &g, EpiKind kind, hipStream_t st)
 {
@@ -294,6 +348,47 @@ int workspace_size(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int 
     return ACSC_OK;
 }
 
+// What the gradient of a given dh is asked for: its checks, and the epilogue's arguments.
+inline int check_backward_act(const void *dh, int64_t ld_dh, const void *z, int64_t ld_z, const q8_tensor *q_gate,
+                              const q8_tensor *q_up, acsc_dtype dt, int64_t rows, int F, acsc_act act, const void *dz, int64_t ld_dz,
+                              const void *h, int64_t ld_h)
+{
+    if (int rc = check_glu(rows, 1, F, dt))
+        return rc;
+    if (int rc = check_act(act))
+        return rc;
+    const bool some = rows > 0;
+    if (int rc = check_mat(dh, some, ld_dh, F, dt, "dh"))
+        return rc;
+    if (int rc = check_kept_pair(z, ld_z, q_gate, q_up, rows, F, dt))
+        return rc;
+    if (int rc = check_mat(dz, some, ld_dz, 2 * F, dt, "dz"))
+        return rc;
+    if (h)
+        if (int rc = check_mat(h, some, ld_h, F, dt, "h"))
+            return rc;
+    ACSC_CHECK_ARG(!some || (dz != dh && dz != h), ACSC_EINVAL, "dz must not overlap dh or h");
+    ACSC_CHECK_ARG(!some || dz != z || ld_dz == ld_z, ACSC_EINVAL, "dz in place of z needs ld_dz == ld_z");
+    ACSC_CHECK_ARG(!some || !h || h != dh || ld_h == ld_dh, ACSC_EINVAL, "h in place of dh needs ld_h == ld_dh");
+    ACSC_CHECK_ARG(!some || !h || h != z, ACSC_EINVAL, "h must not overlap z");
+    return ACSC_OK;
+}
+inline Epi epi_backward_act(const void *z, int64_t ld_z, const q8_tensor *q_gate, const q8_tensor *q_up, acsc_act act, void *dz,
+                            int64_t ld_dz, void *h, int64_t ld_h)
+{
+    Epi e{};
+    e.y = dz;
+    e.ldy = ld_dz;
+    e.z = const_cast<void *>(z);
+    e.ldz = ld_z;
+    e.q = q8_of(q_gate);
+    e.q_up = q8_of(q_up);
+    e.act = act;
+    e.hidden = h;
+    e.ldh = ld_h;
+    return e;
+}
+
 }  // namespace
 
 void glu_join_run(const Gemm &g, const Plan &p, EpiKind kind, acsc_dtype dt, hipStream_t st)
@@ -390,36 +485,11 @@ extern "C" int glu_backward_act(const void *dh, int64_t ld_dh, const void *z, in
                                 void *h, int64_t ld_h, hipStream_t stream)
 {
     clear_error();
-    if (int rc = check_glu(rows, 1, F, dt))
+    if (int rc = check_backward_act(dh, ld_dh, z, ld_z, q_gate, q_up, dt, rows, F, act, dz, ld_dz, h, ld_h))
         return rc;
-    if (int rc = check_act(act))
-        return rc;
-    const bool some = rows > 0;
-    if (int rc = check_mat(dh, some, ld_dh, F, dt, "dh"))
-        return rc;
-    if (int rc = check_kept_pair(z, ld_z, q_gate, q_up, rows, F, dt))
-        return rc;
-    if (int rc = check_mat(dz, some, ld_dz, 2 * F, dt, "dz"))
-        return rc;
-    if (h)
-        if (int rc = check_mat(h, some, ld_h, F, dt, "h"))
-            return rc;
-    ACSC_CHECK_ARG(!some || (dz != dh && dz != h), ACSC_EINVAL, "dz must not overlap dh or h");
-    ACSC_CHECK_ARG(!some || dz != z || ld_dz == ld_z, ACSC_EINVAL, "dz in place of z needs ld_dz == ld_z");
-    ACSC_CHECK_ARG(!some || !h || h != dh || ld_h == ld_dh, ACSC_EINVAL, "h in place of dh needs ld_h == ld_dh");
-    ACSC_CHECK_ARG(!some || !h || h != z, ACSC_EINVAL, "h must not overlap z");
-    if (!some)
+    if (rows == 0)
         return ACSC_OK;
-    Epi e{};
-    e.y = dz;
-    e.ldy = ld_dz;
-    e.z = const_cast<void *>(z);
-    e.ldz = ld_z;
-    e.q = q8_of(q_gate);
-    e.q_up = q8_of(q_up);
-    e.act = act;
-    e.hidden = h;
-    e.ldh = ld_h;
+    const Epi e = epi_backward_act(z, ld_z, q_gate, q_up, act, dz, ld_dz, h, ld_h);
     const dim3 grid(static_cast<unsigned>(std::min<int64_t>((rows * ((F + 511) / 512) + 3) / 4, 1 << 20)));
     if (dt == ACSC_BF16)
         ACSC_LAUNCH("glu_backward_act", glu_act_kernel<uint16_t>, grid, dim3(256), 0, stream, static_cast<const uint16_t *>(dh), ld_dh,
@@ -428,6 +498,59 @@ extern "C" int glu_backward_act(const void *dh, int64_t ld_dh, const void *z, in
         ACSC_LAUNCH("glu_backward_act", glu_act_kernel<float>, grid, dim3(256), 0, stream, static_cast<const float *>(dh), ld_dh, rows,
                     F, e);
     return check_launch("glu_backward_act");
+}
+
+extern "C" int glu_bias_workspace_size(int64_t rows, int F, size_t *bytes)
+{
+    clear_error();
+    if (int rc = check_glu(rows, 1, F, ACSC_F32))
+        return rc;
+    ACSC_CHECK_ARG(bytes, ACSC_EINVAL, "null pointer to the result");
+    *bytes = act_bytes(rows, F);
+    return ACSC_OK;
+}
+
+extern "C" int glu_backward_act_bias(const void *dh, int64_t ld_dh, const void *z, int64_t ld_z, const q8_tensor *q_gate,
+                                     const q8_tensor *q_up, acsc_dtype dt, int64_t rows, int F, acsc_act act, void *dz,
+                                     int64_t ld_dz, void *h, int64_t ld_h, float *dbias, int accumulate, void *ws,
+                                     size_t ws_bytes, hipStream_t stream)
+{
+    clear_error();
+    if (int rc = check_backward_act(dh, ld_dh, z, ld_z, q_gate, q_up, dt, rows, F, act, dz, ld_dz, h, ld_h))
+        return rc;
+    ACSC_CHECK_ARG(dbias, ACSC_EINVAL, "null pointer dbias");
+    ACSC_CHECK_ARG(aligned(dbias, 4), ACSC_EALIGN, "dbias not 4-byte aligned");
+    if (rows == 0) {
+        if (accumulate)
+            return ACSC_OK;
+        ACSC_LAUNCH("glu_zero", glu_zero_kernel, dim3((2 * F + 255) / 256), dim3(256), 0, stream, dbias, 2 * F);
+        return check_launch("glu_zero");
+    }
+    const int parts = act_partials(rows, F);
+    if (int rc = check_ws(ws, ws_bytes, act_bytes(rows, F)))
+        return rc;
+    // the sum over the partials takes them for rows of one tile each
+    Gemm g{};
+    g.N = F;
+    g.tm = g.whole = parts;
+    g.tn = 1;
+    g.e = epi_backward_act(z, ld_z, q_gate, q_up, act, dz, ld_dz, h, ld_h);
+    g.e.sums = parts > 1 ? static_cast<float *>(ws) : dbias;
+    const int add = parts == 1 && accumulate;
+    const dim3 grid((F + 511) / 512, parts);
+    const int64_t per = (rows + parts - 1) / parts;
+    if (dt == ACSC_BF16)
+        ACSC_LAUNCH("glu_backward_act", glu_act_sums_kernel<uint16_t>, grid, dim3(256), 0, stream, static_cast<const uint16_t *>(dh),
+                    ld_dh, rows, F, g.e, per, add);
+    else
+        ACSC_LAUNCH("glu_backward_act", glu_act_sums_kernel<float>, grid, dim3(256), 0, stream, static_cast<const float *>(dh), ld_dh,
+                    rows, F, g.e, per, add);
+    if (int rc = check_launch("glu_backward_act"))
+        return rc;
+    if (parts == 1)
+        return ACSC_OK;
+    ACSC_LAUNCH("glu_sums", glu_sums_kernel, dim3((2 * F + 63) / 64), dim3(64 * kSlices), 0, stream, g, F, dbias, accumulate);
+    return check_launch("glu_sums");
 }
 
 extern "C" int glu_backward_input(const void *dy, int64_t ld_dy, acsc_dtype dt, int64_t rows, int F, int n_out, const void *W,

@@ -26,3 +26,24 @@ def test_a_source_that_is_not_read_may_be_of_either_form(pk):
     for mixed in (dict(out=3 * F, qb=q), dict(qo=q, b=4 * F)):
         assert call(dy=2 * F, gate=F, **mixed) == EINVAL
         assert "both" in pk.lib.acsc_last_error().decode()
+
+
+def test_the_bias_gradient_of_a_given_gradient(pk):
+    EALIGN, ENOSPC = -3, -5
+    q = C.byref(pk._Q8Tensor(F, F, 32, 1))
+
+    def call(dh=F, z=2 * F, qg=None, qu=None, dt=1, rows=40, a=3, dz=3 * F, lddz=64, h=None, ldh=32, ldz=64, db=4 * F, ws=5 * F,
+             n=1 << 30, acc=0, Fh=32):
+        return pk.lib.glu_backward_act_bias(dh, 32, z, ldz, qg, qu, dt, rows, Fh, a, dz, lddz, h, ldh, db, acc, ws, n, None)
+    assert call(db=None) == EINVAL and call(db=4 * F + 2) == EALIGN
+    assert call(ws=None) == EINVAL and call(ws=5 * F + 16) == EALIGN and call(n=255) == ENOSPC
+    assert call(z=None) == EINVAL and call(qg=q, qu=q) == EINVAL and call(z=None, qg=q) == EINVAL
+    assert call(dh=None) == EINVAL and call(dz=None) == EINVAL and call(lddz=63) == EINVAL and call(ldz=63) == EINVAL
+    assert call(dz=F) == EINVAL and call(dz=2 * F, lddz=80) == EINVAL and call(h=2 * F) == EINVAL and call(h=F, ldh=40) == EINVAL
+    assert call(a=4) == EINVAL and call(dt=3) == -2 and call(h=3 * F) == EINVAL and call(rows=-1) == EINVAL and call(Fh=0) == EINVAL
+    assert call(dh=None, z=None, dz=None, rows=0, acc=1, ws=None, n=0) == 0
+    b = C.c_size_t(0)
+    assert pk.lib.glu_bias_workspace_size(0, 32, C.byref(b)) == 0 and b.value == 0
+    assert pk.lib.glu_bias_workspace_size(4, 32, None) == EINVAL and pk.lib.glu_bias_workspace_size(4, 0, C.byref(b)) == EINVAL
+    for rows, Fh, parts in ((1, 1, 0), (16, 4096, 0), (16384, 8192, 1), ((1 << 31) - 1, 1 << 21, 0), (1 << 30, 512, 1), (1 << 30, 513, 1)):
+        assert pk.lib.glu_bias_workspace_size(rows, Fh, C.byref(b)) == 0 and b.value <= 32 << 20 and (b.value > 0) == bool(parts)
