@@ -699,7 +699,10 @@ typedef enum glu_op { GLU_FORWARD = 0, GLU_BACKWARD_INPUT = 1 } glu_op;
  * 0: it writes q_gate and q_up) and for glu_backward_input (n_in is the down
  * projection's n_out; extra != 0: it forms dbias), with the operands of lin_workspace_size and
  * of lin_workspace_size_unaligned; and how that product runs.  A tile of the
- * forward product holds tile_cols / 2 hidden columns. */
+ * forward product holds tile_cols / 2 hidden columns.  In fp32 (and in small
+ * bf16 products) q_gate and q_up are coded from pre-activations that go through
+ * the workspace, up to 256 MiB of them at a time, or one row of tiles (up to
+ * 1 KiB F); such a product has under 2^35 values of h, in whole tiles. */
 int glu_workspace_size(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int extra, size_t *bytes);
 int glu_workspace_size_unaligned(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int extra, size_t *bytes);
 int glu_product_plan(glu_op op, int64_t rows, int n_in, int F, acsc_dtype dt, int extra, lin_plan *plan);

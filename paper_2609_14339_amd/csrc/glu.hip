@@ -467,17 +467,41 @@ extern "C" int glu_forward(const void *x, int64_t ld_x, acsc_dtype dt, int64_t r
                 return rc;
     if (!some)
         return ACSC_OK;
-    Gemm g{};
-    g.A = {x, ld_x};
-    g.B = {W, ld_w};
-    const Shape s = shape_of(kGluForward, rows, n_in, F);
-    const Plan p = plan_of(kGluForward, s, dt, readable(g.A, false, n_in, dt), readable(g.B, false, n_in, dt), q_gate != nullptr);
+    Operand w{W, ld_w};
+    Shape s = shape_of(kGluForward, rows, n_in, F);
+    Plan p = plan_of(kGluForward, s, dt, readable({x, ld_x}, false, n_in, dt), readable(w, false, n_in, dt), q_gate != nullptr);
     if (int rc = check_launches(p, q_gate != nullptr))
         return rc;
     if (int rc = check_ws(ws, ws_bytes, p.bytes()))
         return rc;
-    g.e = Epi{h, ld_h, bias, nullptr, 0, z, ld_z, q8_of(q_gate), act, 0, q8_of(q_up), nullptr, 0, nullptr, 0, 0};
-    return run_product(g, kGluForward, p, s, dt, dt, static_cast<char *>(ws), nullptr, nullptr, stream, "glu_forward");
+    const int64_t es = static_cast<int64_t>(dtype_size(dt));
+    // rows of the tensors from `row` on
+    const auto product = [&](int64_t row) {
+        const auto from = [&](const void *t, int64_t ld) { return t ? static_cast<const char *>(t) + row * ld * es : nullptr; };
+        const auto out = [&](void *t, int64_t ld) { return t ? static_cast<char *>(t) + row * ld * es : nullptr; };
+        const auto codes = [&](const q8_tensor *q) {
+            return q ? Q8{q->codes + row * q->ld_codes, q->scales + row * q->ld_scales, q->ld_codes, q->ld_scales} : q8_of(q);
+        };
+        Gemm g{};
+        g.A = {from(x, ld_x), ld_x};
+        g.B = w;
+        g.e = Epi{out(h, ld_h), ld_h, bias, nullptr, 0, out(z, ld_z), ld_z, codes(q_gate), act, 0, codes(q_up), nullptr, 0, nullptr, 0, 0};
+        const int rc = run_product(g, kGluForward, p, s, dt, dt, static_cast<char *>(ws), nullptr, nullptr, stream, "glu_forward");
+        w = g.B;   // where it was copied, the next run finds the copy
+        p.pack_b = false;
+        return rc;
+    };
+    if (p.band == p.tm)
+        return product(0);
+    // runs that take the workspace in turn
+    for (int first = 0, tm = p.tm; first < tm; first += p.band) {
+        const int64_t row = static_cast<int64_t>(first) * p.rows;
+        p.tm = std::min(p.band, tm - first);
+        s.M = std::min(static_cast<int64_t>(p.tm) * p.rows, rows - row);
+        if (int rc = product(row))
+            return rc;
+    }
+    return ACSC_OK;
 }
 
 extern "C" int glu_backward_act(const void *dh, int64_t ld_dh, const void *z, int64_t ld_z, const q8_tensor *q_gate,

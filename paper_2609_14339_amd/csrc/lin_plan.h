@@ -28,6 +28,7 @@ struct Plan {
     bool few;                               // the product for few tokens
     int rows, tile;                         // of a tile: its rows and columns
     int tm, tn, whole, splits, kchunk;
+    int band;                               // rows of tiles of a run: all, or of a coded product as its pieces fit
     int slices, slice;                      // of the rows, for db
     int64_t ldp;
     bool pack_a, pack_b;

@@ -47,3 +47,15 @@ def test_the_bias_gradient_of_a_given_gradient(pk):
     assert pk.lib.glu_bias_workspace_size(4, 32, None) == EINVAL and pk.lib.glu_bias_workspace_size(4, 0, C.byref(b)) == EINVAL
     for rows, Fh, parts in ((1, 1, 0), (16, 4096, 0), (16384, 8192, 1), ((1 << 31) - 1, 1 << 21, 0), (1 << 30, 512, 1), (1 << 30, 513, 1)):
         assert pk.lib.glu_bias_workspace_size(rows, Fh, C.byref(b)) == 0 and b.value <= 32 << 20 and (b.value > 0) == bool(parts)
+
+
+def test_coded_products_take_a_bounded_workspace(pk):
+    """Where a product's tiles hold no whole groups its pre-activations go through the workspace, a part of them at a time:
+    256 MiB at most, however many rows there are, or one row of tiles (of 128 rows of 2 F fp32 values at most)."""
+    import torch
+    for rows, n_in, Fh in ((16384, 2048, 8192), (4096, 4096, 14336), (1 << 20, 64, 1024), (65536, 33, 100), (300, 64, 1 << 20)):
+        for dt in (torch.float32, torch.bfloat16):
+            most = max(256 << 20, 128 * 4 * 2 * (Fh + 64)) + (1 << 20)
+            copies = dt.itemsize * ((rows + 2 * Fh) * (n_in + 8))
+            assert pk.glu_workspace_size(pk.GLU_FORWARD, rows, n_in, Fh, dt, True) <= most + (copies if n_in % 2 else 0)
+            assert pk.glu_workspace_size_unaligned(pk.GLU_FORWARD, rows, n_in, Fh, dt, True) <= most + copies
