@@ -17,7 +17,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
-from typing import NamedTuple, Optional, Union
+from typing import NamedTuple, Optional, Sequence, Union
 
 import torch
 
@@ -1304,6 +1304,9 @@ def join_forward(r: torch.Tensor, b: torch.Tensor, post: Optional[torch.Tensor] 
     return Joined(out, y, rstd_post, rstd_pre, q_out, q_b)
 
 
+_GAINS = ("post", "gate", "pre")
+
+
 def join_backward(dout: Optional[torch.Tensor], dy: Optional[torch.Tensor], out: Union[torch.Tensor, Q8, None],
                   b: Union[torch.Tensor, Q8, None], rstd_post: Optional[torch.Tensor] = None,
                   rstd_pre: Optional[torch.Tensor] = None, post: Optional[torch.Tensor] = None,
@@ -1311,14 +1314,16 @@ def join_backward(dout: Optional[torch.Tensor], dy: Optional[torch.Tensor], out:
                   drop: Optional[Drop] = None, dr: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None,
                   dpost: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None,
                   dpre: Optional[torch.Tensor] = None, accumulate: bool = False, ws: Optional[torch.Tensor] = None,
-                  stream=None, weights: bool = True) -> JoinGrads:
+                  stream=None, weights: Union[bool, Sequence[str]] = True, want_dr: bool = True) -> JoinGrads:
     """Gradients of join_forward from dout and dy (one of them may be None), out
     and b or their checkpoints, and the kept statistics.  dpost, dgate, dpre: fp32
     [H], of the gains that there are (dpre where there is dy); with accumulate
-    they are given and added to; without weights they are not formed."""
+    they are given and added to; without weights they are not formed, or those
+    of "post", "gate" and "pre" alone that weights names.  Without want_dr the
+    stream's gradient is not formed."""
     if stream is not None:
         return _on(stream, join_backward, dout, dy, out, b, rstd_post, rstd_pre, post, gate, pre, scale, drop, dr, db, dpost,
-                   dgate, dpre, accumulate, ws, None, weights)
+                   dgate, dpre, accumulate, ws, None, weights, want_dr)
     one = dout if dout is not None else dy
     if one is None:
         raise AcscError(ACSC_EINVAL, "one of dout and dy is needed")
@@ -1334,16 +1339,25 @@ def join_backward(dout: Optional[torch.Tensor], dy: Optional[torch.Tensor], out:
     pb, ldb, qb = _kept(b, shape, dtype, "b")
     pp, pg, pn = _optvec(post, H, dtype, "post"), _optvec(gate, H, dtype, "gate"), _optvec(pre, H, dtype, "pre")
     prp, prn = _optvec(rstd_post, rows, torch.float32, "rstd_post"), _optvec(rstd_pre, rows, torch.float32, "rstd_pre")
-    dr, lddr = _like(dr, one, "dr")
+    pdr, lddr = None, 0
+    if want_dr:
+        dr, lddr = _like(dr, one, "dr")
+        pdr = dr.data_ptr()
+    elif dr is not None:
+        raise AcscError(ACSC_EINVAL, "dr is given, but not wanted")
     db, lddb = _like(db, one, "db")
-    dpost = _sums(dpost, weights and post is not None, H, accumulate, dev, "dpost")
-    dgate = _sums(dgate, weights and gate is not None, H, accumulate, dev, "dgate")
-    dpre = _sums(dpre, weights and dy is not None, H, accumulate, dev, "dpre")
+    if not isinstance(weights, (str, list, tuple, set, frozenset)):
+        weights = _GAINS if weights else ()
+    elif isinstance(weights, str) or not all(w in _GAINS for w in weights):
+        raise AcscError(ACSC_EINVAL, f"weights must be a bool or some of {_GAINS}, not {weights!r}")
+    dpost = _sums(dpost, post is not None and "post" in weights, H, accumulate, dev, "dpost")
+    dgate = _sums(dgate, gate is not None and "gate" in weights, H, accumulate, dev, "dgate")
+    dpre = _sums(dpre, dy is not None and "pre" in weights, H, accumulate, dev, "dpre")
     pdp, pdg = _optvec(dpost, H, torch.float32, "dpost"), _optvec(dgate, H, torch.float32, "dgate")
     pdn = _optvec(dpre, H, torch.float32, "dpre")
     wp, wn, hold = (None, 0, None) if pdp is pdg is pdn is None else _ws(_join_bytes(rows, H), ws, dev)
     rc = lib.join_backward(pdo, lddo, pdy, lddy, po, ldo, qo, pb, ldb, qb, _dt(one), rows, H, pp, pg, scale, _drop_ref(drop),
-                           pn, prp, prn, dr.data_ptr(), lddr, db.data_ptr(), lddb, pdp, pdg, pdn, int(accumulate), wp, wn,
+                           pn, prp, prn, pdr, lddr, db.data_ptr(), lddb, pdp, pdg, pdn, int(accumulate), wp, wn,
                            _raw_stream())
     if rc:
         _check(rc)

@@ -205,9 +205,15 @@ class _Join(torch.autograd.Function):
         if gout is None and gy is None:
             return (None,) * 9
         d = join_backward(None if gout is None else _flat(gout), None if gy is None else _flat(gy), _load(*kept[:2]),
-                          _load(*kept[2:]), rstd_post, rstd_pre, post, gate, pre, ctx.scale, ctx.drop, weights=any(need[2:5]))
-        return (d.dr.view(ctx.shapes[0]), d.db.view(ctx.shapes[1]), _as(d.dpost, post), _as(d.dgate, gate), _as(d.dpre, pre),
-                None, None, None, None)
+                          _load(*kept[2:]), rstd_post, rstd_pre, post, gate, pre, ctx.scale, ctx.drop,
+                          weights=_wanted(need[2:5]), want_dr=need[0])
+        return (d.dr.view(ctx.shapes[0]) if need[0] else None, d.db.view(ctx.shapes[1]), _as(d.dpost, post), _as(d.dgate, gate),
+                _as(d.dpre, pre), None, None, None, None)
+
+
+def _wanted(need):
+    """The gains whose gradients are wanted, as join_backward names them."""
+    return tuple(name for name, k in zip(("post", "gate", "pre"), need) if k)
 
 
 _GLU_KEEP = {True: "q8", False: "z", None: None}
@@ -272,8 +278,13 @@ class _GluBlock(torch.autograd.Function):
         dx = dgamma = dW = dbias = dW2 = dbias2 = dpost = dgate = None
         dr = db = _flat(g)
         if not ctx.plain:
-            d = join_backward(db, None, None, b, rstd_post, None, post, gate, None, ctx.scale, ctx.drop, weights=need[6] or need[7])
-            dr, db, dpost, dgate = d.dr, d.db, d.dpost, d.dgate
+            # where the stream is not scaled its gradient is g itself
+            scaled = need[0] and ctx.scale != 1.0
+            d = join_backward(db, None, None, b, rstd_post, None, post, gate, None, ctx.scale, ctx.drop, weights=_wanted(need[6:8]),
+                              want_dr=scaled)
+            db, dpost, dgate = d.db, d.dpost, d.dgate
+            if scaled:
+                dr = d.dr
         dz = h = None
         if any(need[:6]):
             dz, h, dbias = glu_backward_input(db, W2, z, ctx.act, hidden=need[4] or need[5], bias=need[3])
@@ -285,7 +296,7 @@ class _GluBlock(torch.autograd.Function):
             dW, _ = lin_backward_weight(dz, y, bias=False)
             del y
         if need[0] or need[1]:
-            dx, dgamma = rms_backward(lin_backward_input(dz, W), x, rstd, gamma, add=dr, weights=need[1])
+            dx, dgamma = rms_backward(lin_backward_input(dz, W), x, rstd, gamma, add=dr if need[0] else None, weights=need[1])
             dx = dx.view(g.shape)
         return (dx, _as(dgamma, gamma), dW, _as(dbias, bias), dW2, _as(dbias2, bias2), _as(dpost, post), _as(dgate, gate), None,
                 None, None, None, None)
