@@ -24,8 +24,9 @@ passes, and is kept nowhere.
 
 The ops are differentiable once: the gradient of a gradient raises an error.
 Gradients of W1 and W2 come out in the weights' dtype, as sc_correct takes
-them.  Every operation is a library call; this module only wires them into
-autograd.
+them.  The gated product's bias gradient is summed before its terms are rounded;
+that of a linear layer from the gradient that reaches it, in its tensor's dtype.
+Every operation is a library call; this module only wires them into autograd.
 """
 from __future__ import annotations
 

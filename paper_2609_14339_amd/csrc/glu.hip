@@ -5,8 +5,8 @@
 //   dg = dh u act'(g),  du = dh act(g),  dx = (dg, du) (Wg; Wu),  dW = (dg, du)^T x
 // so that with dz = (dg, du) in one tensor and the two weights in one, the rest
 // of the gradient is a linear layer's.  The bias gradient is summed from dz
-// before its rounding, in the epilogue that forms it (from the rounded dz it is
-// 1e-3 off in bf16).
+// before its rounding, in the epilogue or the pass that forms it (from the
+// rounded dz it is 1e-3 off in bf16).
 #include "lin_plan.h"
 
 namespace acsc {
